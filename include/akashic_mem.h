@@ -363,6 +363,125 @@ akashic_status_t akashic_mem_check_wait_timeout(akashic_mem_t *m, uint32_t polls
 akashic_status_t akashic_mem_sort_pairs(uint32_t *keys, uint32_t *vals, int64_t n, int32_t bits,
                                         void *stream);
 
+/* ------------------------------------------------------------------ keys and values
+ * A cache of the keys and values behind the stored chunks, held in 4 or 8 bits, and the
+ * attention that reads it.  The paper leaves the attention and its cache to the
+ * serving engine (§4.3); these calls let that engine keep a chunk's keys and values
+ * beside the store and attend over what retrieval returns (Algorithm 1's
+ * FetchByID, SortByTime, Concat): a block of the cache per chunk, and the list of
+ * retrieved chunk IDs is the list of blocks.
+ *
+ * The calls need no store, allocate nothing and never synchronise; they can be
+ * recorded into a CUDA graph.  The cache, the tags and the scratch are the
+ * caller's device memory on cfg->device, which need not be the current device.
+ * Calls on one cache are ordered by their streams alone: a write must not
+ * overlap a call that reads the same slots.
+ *
+ * A slot holds one token: slot = block * block_tokens + place in the block.  Rows
+ * are quantised one token and head at a time, keys and values alike:
+ *   4 bits: a = max |x| of the row, T = floor(log2(a / 7)) in [-100, 125]; per 16
+ *     values the scale e = max |x| / (7 2^T) rounded to (1 + m/16) 2^(E-15),
+ *     0 <= E, m <= 15; a value is stored as c = round(x / (e 2^T)) in [-7, 7] and
+ *     stands for c e 2^T, exact in bf16.  head_dim / 2 + head_dim / 16 + 1 bytes.
+ *   8 bits: the scale s = max(bf16(a / 127), 2^-100); c = round(x / s) in
+ *     [-127, 127] stands for c s.  head_dim + 2 bytes.
+ * Every rounding is to the nearest, ties to even, of the exact quotient.  NaN is
+ * stored as 0 and an infinity as the largest fp32.
+ *
+ * status: device int32 or NULL.  Not cleared by these calls: a kernel that finds a
+ * slot, block ID, length or row range out of bounds records EDEVICE, one whose
+ * bounded wait expires ETIMEOUT, if the word is 0; the entry is then skipped or
+ * clamped, and no memory outside the arguments is touched. */
+enum { AKASHIC_DTYPE_BF16 = 0, AKASHIC_DTYPE_FP16 = 1, AKASHIC_DTYPE_FP32 = 2 };
+
+typedef struct {
+    int32_t bits;         /* 4 or 8                                                */
+    int32_t heads;        /* key/value heads, 1..1024                              */
+    int32_t head_dim;     /* 64, 128 or 256                                        */
+    int32_t block_tokens; /* multiple of 16, 16..4096                              */
+    int64_t n_blocks;     /* >= 1; n_blocks * block_tokens / 16 <= 2^31 - 1        */
+    int32_t device;       /* CUDA device ordinal                                   */
+} akashic_mem_kv_config_t;
+
+/* Bytes of the cache (16-byte aligned device memory; its contents need no
+ * initialisation: slots never written are to be hidden by lengths or tags). */
+akashic_status_t akashic_mem_kv_cache_bytes(const akashic_mem_kv_config_t *cfg, int64_t *bytes);
+
+/* Quantise n tokens into their slots.
+ *   k, v      device, dtype BF16, FP16 or FP32: value (i, h, d) of token i, head h at
+ *             i * row_stride + h * head_stride + d (strides in elements, any sign
+ *             and size; 16-byte aligned rows are read fastest)
+ *   slots     device int64[n]: the slot of each token, -1 to skip it (its k and
+ *             v are not read).  A slot may appear only once in a call
+ *   tags      device int32, one a slot, or NULL: the tags of written slots are set to
+ *   new_tags  device int32[n], or to 0 where new_tags is NULL
+ * EINVAL for a bad config, dtype, n outside [0, 2^31 - 1], a NULL or misaligned
+ * pointer, or new_tags without tags; ECUDA if the launch fails. */
+akashic_status_t akashic_mem_kv_write(const akashic_mem_kv_config_t *cfg, void *cache,
+                                      int32_t *tags, const void *k, int64_t k_row_stride,
+                                      int64_t k_head_stride, const void *v, int64_t v_row_stride,
+                                      int64_t v_head_stride, int32_t dtype, int64_t n,
+                                      const int64_t *slots, const int32_t *new_tags,
+                                      int32_t *status, void *stream);
+
+/* The values that the cache stands for, rounded once to dtype: k, v device
+ * [n][heads][head_dim], contiguous, rows of slot -1 zero.  A slot may appear any
+ * number of times.  Errors as akashic_mem_kv_write. */
+akashic_status_t akashic_mem_kv_read(const akashic_mem_kv_config_t *cfg, const void *cache,
+                                     const int64_t *slots, int64_t n, int32_t dtype, void *k,
+                                     void *v, int32_t *status, void *stream);
+
+/* Attention of query rows over listed blocks.  Sequence s has the query rows
+ * [q_start[s], q_start[s+1]) and, as its context, the first kv_len[s] tokens of the
+ * blocks blocks[s][0], blocks[s][1], ...; key j of the context is its j-th token in
+ * that order, tokens of skipped entries counted.  Row i of the sequence's nq stands at
+ * pos = kv_len - nq + i.  For each of the q_heads heads, head h reading key/value head
+ * h / (q_heads / heads):
+ *   z_j = scale <q, k_j>;  cap > 0: z_j = cap tanh(z_j / cap);
+ *   slopes: z_j -= slopes[h] |pos - j|;
+ *   out = sum_j exp(z_j) v_j / sum_j exp(z_j),  lse = log sum_j exp(z_j)
+ * over the keys that the row sees: those of entries other than -1 with
+ * j < kv_len, and, if causal, j <= pos or j < prefix_len[s], and, with tags, a tag
+ * that equals the row's and is >= 0.  A row that sees none gives 0, lse -inf.
+ * Query rows behind the last sequence are not read, nor their results written. */
+typedef struct {
+    const void *q;             /* device, (row, head, d) at row * q_row_stride + head *
+                                  q_head_stride + d, strides in elements             */
+    int64_t q_row_stride, q_head_stride;
+    int32_t dtype;             /* of q and out: BF16 or FP16                         */
+    int32_t n_q, q_heads;      /* query rows; heads (a multiple of cfg->heads)       */
+    int32_t n_seq;             /* sequences                                          */
+    const int32_t *q_start;    /* device int32[n_seq + 1], ascending, or NULL: n_q /
+                                  n_seq rows each                                    */
+    const int32_t *kv_len;     /* device int32[n_seq] or NULL: all that is listed    */
+    const int64_t *blocks;     /* device int64[n_seq * max_blocks], -1: none; the ids
+                                  of akashic_mem_retrieve fit as they are            */
+    int64_t max_blocks;        /* entries of a list; max_blocks * block_tokens < 2^31 */
+    int32_t causal;
+    const int32_t *prefix_len; /* device int32[n_seq] or NULL                        */
+    float scale;               /* 0 => 1/sqrt(head_dim)                              */
+    float cap;                 /* 0 => none                                          */
+    const float *slopes;       /* device float[q_heads] or NULL                      */
+    const int32_t *tags;       /* device int32, one a slot, 16-byte aligned; with    */
+    const int32_t *q_tags;     /* device int32[n_q]: both or neither                 */
+    void *out;                 /* device [n_q][q_heads][head_dim] of dtype           */
+    float *lse;                /* device float[n_q][q_heads] or NULL                 */
+} akashic_mem_kv_attend_t;
+
+/* Bytes of scratch that a call with these arguments needs (sizes and which pointers are
+ * NULL matter, not their contents).  Calls that may overlap, and graphs that may run at
+ * the same time, need scratch of their own. */
+akashic_status_t akashic_mem_kv_attend_scratch(const akashic_mem_kv_config_t *cfg,
+                                               const akashic_mem_kv_attend_t *a, int64_t *bytes);
+
+/* scratch: device, 16-byte aligned, not initialised.  EINVAL for a bad config or
+ * argument (as noted above), n_q x q_heads beyond 2^31 - 1, a scale or cap that is
+ * not finite, a negative cap, tags without q_tags, or scratch that is too small;
+ * ECUDA if a launch fails. */
+akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t *cfg, const void *cache,
+                                       const akashic_mem_kv_attend_t *a, void *scratch,
+                                       int64_t scratch_bytes, int32_t *status, void *stream);
+
 /* Thread-local description of the last failure on this thread ("" if none). */
 const char *akashic_mem_last_error(void);
 

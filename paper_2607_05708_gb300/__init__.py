@@ -3,8 +3,9 @@
 Thin Python binding of the C ABI in ``include/akashic_mem.h``
 (``libakashic_mem.so``, built in-tree by ``_build.build()``).  It only
 marshals arguments: every step of retrieval (score, relation propagation,
-top-k, page resolve) and of the relation update (cosine top-M, CSR insert)
-runs in the library's CUDA kernels.  PyTorch is used for device memory and
+top-k, page resolve), of the relation update (cosine top-M, CSR insert) and of the
+quantised key and value cache (write, read, attention) runs in the library's
+CUDA kernels.  PyTorch is used for device memory and
 streams.  There is no CPU fallback: without the built library every call
 raises.
 """
@@ -16,7 +17,7 @@ import os
 from ._build import LIB as LIB_PATH
 from ._build import build
 
-__all__ = ["MemStore", "AkashicError", "load_library", "build", "EXPORTS", "STATUS", "PHASES",
+__all__ = ["MemStore", "KVCache", "AkashicError", "load_library", "build", "EXPORTS", "STATUS", "PHASES",
            "softmax_scores_noalloc", "sort_pairs"]
 
 STATUS = {0: "OK", 1: "EINVAL", 2: "ENOMEM", 3: "ECAPACITY", 4: "ECUDA", 5: "ETIMEOUT",
@@ -33,6 +34,8 @@ EXPORTS = (
     "akashic_mem_set_namespace", "akashic_mem_retrieve_scoped", "akashic_mem_delete",
     "akashic_mem_relocate", "akashic_mem_compact_pages", "akashic_mem_page_stats",
     "akashic_mem_export_pages", "akashic_mem_check_wait_timeout", "akashic_mem_sort_pairs",
+    "akashic_mem_kv_cache_bytes", "akashic_mem_kv_write", "akashic_mem_kv_read",
+    "akashic_mem_kv_attend_scratch", "akashic_mem_kv_attend",
 )
 
 
@@ -47,6 +50,24 @@ class _Config(ctypes.Structure):
     _fields_ = [("dim", ctypes.c_int32), ("capacity", ctypes.c_int64),
                 ("chunks_per_page", ctypes.c_int32), ("device", ctypes.c_int32),
                 ("temperature", ctypes.c_float), ("relation_scale", ctypes.c_float)]
+
+
+class _KVConfig(ctypes.Structure):
+    _fields_ = [("bits", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("block_tokens", ctypes.c_int32), ("n_blocks", ctypes.c_int64),
+                ("device", ctypes.c_int32)]
+
+
+class _KVAttend(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_row_stride", ctypes.c_int64),
+                ("q_head_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("n_q", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("n_seq", ctypes.c_int32),
+                ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("blocks", ctypes.c_void_p), ("max_blocks", ctypes.c_int64),
+                ("causal", ctypes.c_int32), ("prefix_len", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("cap", ctypes.c_float), ("slopes", ctypes.c_void_p),
+                ("tags", ctypes.c_void_p), ("q_tags", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("lse", ctypes.c_void_p)]
 
 
 _lib = None
@@ -89,6 +110,15 @@ def load_library(path: str | None = None):
         "akashic_mem_last_error": ([], ctypes.c_char_p),
         "akashic_mem_softmax_scores_noalloc": ([V, I64, I32, V, I32, F, V, V, V, V, V],
                                                ctypes.c_int),
+        "akashic_mem_kv_cache_bytes": ([ctypes.POINTER(_KVConfig), P64], ctypes.c_int),
+        "akashic_mem_kv_write": ([ctypes.POINTER(_KVConfig), V, V, V, I64, I64, V, I64, I64, I32,
+                                  I64, V, V, V, V], ctypes.c_int),
+        "akashic_mem_kv_read": ([ctypes.POINTER(_KVConfig), V, V, I64, I32, V, V, V, V],
+                                ctypes.c_int),
+        "akashic_mem_kv_attend_scratch": ([ctypes.POINTER(_KVConfig), ctypes.POINTER(_KVAttend),
+                                           P64], ctypes.c_int),
+        "akashic_mem_kv_attend": ([ctypes.POINTER(_KVConfig), V, ctypes.POINTER(_KVAttend), V, I64,
+                                   V, V], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -345,3 +375,177 @@ class MemStore:
         ln = (ctypes.c_int32 * len(PHASES))()
         _check(load_library().akashic_mem_phase_times(self._h, ms, ln))
         return {p: (ms[i], ln[i]) for i, p in enumerate(PHASES)}
+
+
+class KVCache:
+    """Keys and values of `heads` heads in 4 or 8 bits, in blocks of
+    `block_tokens` tokens (akashic_mem_kv_*; the format is in the header).
+
+    A block per stored chunk, block ID = chunk ID, makes what
+    MemStore.retrieve returns the list of blocks to attend over.  With
+    `tagged`, every slot has an int32 tag (-1 while it holds no token): a
+    namespace or a document, which attention can be restricted to.  The
+    memory is `data` (uint8), `tags` (int32 [n_blocks * block_tokens] or None)
+    and `status` (int32 [1], read and cleared by sync())."""
+
+    def __init__(self, n_blocks: int, heads: int, head_dim: int, block_tokens: int = 64,
+                 bits: int = 4, device: int = 0, tagged: bool = False):
+        import torch
+        self._torch = torch
+        self._lib = load_library()
+        self.n_blocks, self.heads, self.head_dim = n_blocks, heads, head_dim
+        self.block_tokens, self.bits, self.device = block_tokens, bits, device
+        self._cfg = ctypes.byref(_KVConfig(bits, heads, head_dim, block_tokens, n_blocks, device))
+        size = ctypes.c_int64()
+        _check(self._lib.akashic_mem_kv_cache_bytes(self._cfg, ctypes.byref(size)))
+        dev = torch.device("cuda", device)
+        self.data = torch.empty(size.value, dtype=torch.uint8, device=dev)
+        self.tags = (torch.full((n_blocks * block_tokens,), -1, dtype=torch.int32, device=dev)
+                     if tagged else None)
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self._dtypes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+        self._scratch = {}
+
+    # -- helpers
+    def _vec(self, t, dtype, name, numel):
+        """The pointer of a contiguous tensor of that type and length (None: NULL)."""
+        if t is None:
+            return None
+        if not t.is_cuda or t.device.index != self.device:
+            raise ValueError(f"{name} must be a CUDA tensor on device {self.device}")
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if not t.is_contiguous() or t.numel() != numel:
+            raise ValueError(f"{name} must be contiguous, of {numel} elements")
+        return t.data_ptr()
+
+    def _rows(self, t, name, heads=None):
+        """dtype code of rows [n, heads, head_dim] whose last dimension is contiguous."""
+        if not t.is_cuda or t.device.index != self.device:
+            raise ValueError(f"{name} must be a CUDA tensor on device {self.device}")
+        if t.dtype not in self._dtypes:
+            raise TypeError(f"{name} must be bfloat16, float16 or float32, got {t.dtype}")
+        if t.dim() != 3 or t.shape[2] != self.head_dim or (heads and t.shape[1] != heads):
+            raise ValueError(f"{name} must be [n, {heads or 'heads'}, {self.head_dim}]")
+        if t.stride(2) != 1 and t.numel():
+            raise ValueError(f"{name} must be contiguous in its last dimension")
+        return self._dtypes[t.dtype]
+
+    def _empty(self, shape, dtype, stream, zero=False):
+        """A new tensor from the pool of the stream that the call runs on."""
+        torch = self._torch
+        make = torch.zeros if zero else torch.empty
+        dev = self.data.device
+        if stream is None:
+            return make(shape, dtype=dtype, device=dev)
+        with torch.cuda.stream(stream):
+            return make(shape, dtype=dtype, device=dev)
+
+    def _on(self, stream):
+        s = stream if stream is not None else self._torch.cuda.current_stream(self.device)
+        return s.cuda_stream
+
+    # -- ABI
+    def write(self, k, v, slots, tags=None, stream=None):
+        """Quantise k, v [n, heads, head_dim] (bfloat16, float16 or float32; any strides
+        of the first two dimensions) into slots (int64 [n]; block * block_tokens +
+        place; -1 skips a row; a slot at most once).  tags (int32 [n], tagged caches
+        only): the tags of the rows, 0 if not given."""
+        torch = self._torch
+        dt = self._rows(k, "k", self.heads)
+        if self._rows(v, "v", self.heads) != dt or v.shape != k.shape:
+            raise ValueError("k and v must be of one type and shape")
+        n = k.shape[0]
+        if tags is not None and self.tags is None:
+            raise ValueError("tags need a tagged cache")
+        ps = self._vec(slots, torch.int64, "slots", n)
+        pt = self._vec(tags, torch.int32, "tags", n)
+        sk, sv = k.stride(), v.stride()
+        _check(self._lib.akashic_mem_kv_write(
+            self._cfg, self.data.data_ptr(), None if self.tags is None else self.tags.data_ptr(),
+            k.data_ptr(), sk[0], sk[1], v.data_ptr(), sv[0], sv[1], dt, n, ps, pt,
+            self.status.data_ptr(), self._on(stream)))
+
+    def read(self, slots, dtype=None, k=None, v=None, stream=None):
+        """The values that slots (int64 [n], -1: zeros) stand for: k, v [n, heads,
+        head_dim] of dtype (bfloat16 if not given), allocated unless given."""
+        torch = self._torch
+        dtype = dtype or (k.dtype if k is not None else torch.bfloat16)
+        if dtype not in self._dtypes:
+            raise TypeError(f"dtype must be bfloat16, float16 or float32, got {dtype}")
+        n = slots.numel()
+        shape = (n, self.heads, self.head_dim)
+        ps = self._vec(slots, torch.int64, "slots", n)
+        if k is None:
+            k = self._empty(shape, dtype, stream)
+        if v is None:
+            v = self._empty(shape, dtype, stream)
+        numel = n * self.heads * self.head_dim
+        pk, pv = self._vec(k, dtype, "k", numel), self._vec(v, dtype, "v", numel)
+        _check(self._lib.akashic_mem_kv_read(self._cfg, self.data.data_ptr(), ps, n,
+                                             self._dtypes[dtype], pk, pv, self.status.data_ptr(),
+                                             self._on(stream)))
+        return k, v
+
+    def attend(self, q, blocks, kv_len=None, q_start=None, causal=True, prefix_len=None,
+               scale=0.0, cap=0.0, slopes=None, q_tags=None, out=None, lse=None, stream=None):
+        """Attention of q [n_q, q_heads, head_dim] (bfloat16 or float16) over the listed
+        blocks (int64 [n_seq, max_blocks], -1: none).  Sequence s has the query rows
+        q_start[s] to q_start[s + 1] (int32 [n_seq + 1]; not given: n_q / n_seq rows
+        each) and the first kv_len[s] tokens (int32 [n_seq]; not given: all) of its
+        blocks; its last query row stands at its last token.  causal, prefix_len
+        (int32 [n_seq]: keys that all rows see), scale (0: 1 / sqrt(head_dim)), cap,
+        slopes (float32 [q_heads]) and q_tags (int32 [n_q], tagged caches only) as in
+        akashic_mem_kv_attend.  Returns (out [n_q, q_heads, head_dim] of q's type,
+        lse float32 [n_q, q_heads]); rows behind the last sequence are left as they
+        were (zero, -inf-free, in tensors allocated here)."""
+        torch = self._torch
+        dt = self._rows(q, "q")
+        if dt == 2:
+            raise TypeError("q must be bfloat16 or float16, got torch.float32")
+        if blocks.dim() != 2:
+            raise ValueError("blocks must be [n_seq, max_blocks]")
+        if q_tags is not None and self.tags is None:
+            raise ValueError("q_tags need a tagged cache")
+        n_q, q_heads, _ = q.shape
+        n_seq, width = blocks.shape
+        a = _KVAttend(
+            q.data_ptr(), q.stride(0), q.stride(1), dt, n_q, q_heads, n_seq,
+            self._vec(q_start, torch.int32, "q_start", n_seq + 1),
+            self._vec(kv_len, torch.int32, "kv_len", n_seq),
+            self._vec(blocks, torch.int64, "blocks", n_seq * width), width, bool(causal),
+            self._vec(prefix_len, torch.int32, "prefix_len", n_seq), scale, cap,
+            self._vec(slopes, torch.float32, "slopes", q_heads),
+            None if q_tags is None else self.tags.data_ptr(),
+            self._vec(q_tags, torch.int32, "q_tags", n_q))
+        if out is None:
+            out = self._empty(q.shape, q.dtype, stream, zero=q_start is not None)
+        if lse is None:
+            lse = self._empty((n_q, q_heads), torch.float32, stream, zero=q_start is not None)
+        a.out = self._vec(out, q.dtype, "out", n_q * q_heads * self.head_dim)
+        a.lse = self._vec(lse, torch.float32, "lse", n_q * q_heads)
+        key = (n_q, q_heads, n_seq, q_start is None)
+        size = self._scratch.get(key)
+        if size is None:
+            need = ctypes.c_int64()
+            _check(self._lib.akashic_mem_kv_attend_scratch(self._cfg, ctypes.byref(a),
+                                                           ctypes.byref(need)))
+            if len(self._scratch) > 4096:
+                self._scratch.clear()
+            size = self._scratch[key] = need.value
+        scratch = self._empty((size,), torch.uint8, stream)
+        _check(self._lib.akashic_mem_kv_attend(self._cfg, self.data.data_ptr(), ctypes.byref(a),
+                                               scratch.data_ptr(), size, self.status.data_ptr(),
+                                               self._on(stream)))
+        return out, lse
+
+    def sync(self, stream=None):
+        """Wait for the stream, then raise (and clear) what the kernels recorded: a slot,
+        block ID, length or row range out of bounds (EDEVICE), an expired wait."""
+        s = stream if stream is not None else self._torch.cuda.current_stream(self.device)
+        s.synchronize()
+        code = int(self.status.item())
+        if code:
+            self.status.zero_()
+            raise AkashicError(code, "kv: an index or length was out of bounds" if code == 6
+                               else "kv: a kernel of the cache failed")

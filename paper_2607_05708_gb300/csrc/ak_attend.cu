@@ -1,0 +1,889 @@
+// Attention of few query rows over the quantised cache (decoding, drafted
+// tokens, queries over their retrieved chunks), and the joining of items
+// whose steps several CTAs shared.
+//
+// The cache is read once and everything else is small: bytes bound it (146
+// bytes a token and head at D = 128, 4 bits), and next to them the instructions
+// that turn codes into fp16, about 1.4 a value.  So:
+//  * the scores are computed transposed, S^T = K Q^T, and O^T = V^T P^T: the keys
+//    and values are the 16-row operand A of mma.m16n8k16, the query rows (the
+//    heads of a group) the 8 columns of B; 8 heads waste nothing, and a
+//    unit's codes are turned into A fragments in the registers of the lane that
+//    loaded them (ak_kv.cuh): no shuffle, no store to shared memory.  The tensor
+//    memory path would want the fp16 tile written to shared memory first.
+//  * a nibble n in the low bits of a half is the subnormal n 2^-24; one fused
+//    multiply-add by e 2^15 and -8 e 2^-9 gives (n - 8) e 2^-9: one instruction
+//    for two values, exact but for groups below 2^-11 of their row (whose values
+//    are rounded to 2^-19 of the row's largest).  The row's 2^T goes to the
+//    score; for values into the group's scale, relative to the largest T so far.
+//  * a warp works on its own units (16 tokens), brought by bulk copies into its
+//    own ring, with its own running maximum, sum and accumulators: no barrier in
+//    the loop.  The warps of a CTA are joined at the end of an item.
+//  * P is fp16, 2^6 p: weights down to 2^-20 of the largest keep 11 bits; sums,
+//    maxima and accumulators are fp32.  The maximum is raised only when a
+//    score exceeds it by 2^8, so that the accumulators are rarely rescaled.
+#include "ak_attend.cuh"
+#include "ak_sm100.cuh"
+
+namespace ak {
+
+namespace {
+
+constexpr int NW = 8;                         // warps of a CTA
+constexpr float NEG = -1e30f;                 // "no score yet", finite: no NaN from differences
+constexpr float P_SHIFT = 6.f, M_SLACK = 8.f; // log2 units
+
+__device__ __forceinline__ uint32_t h2fma(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t h2mul(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t h2add(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
+    return d;
+}
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                      uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+            smem_u32(dst)),
+        "l"(src), "r"(bytes), "r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ float scale2(float x, int e) {   // x 2^e, |e| <= 252
+    return x * pow2i(e / 2) * pow2i(e - e / 2);
+}
+
+// Four adjacent-dim (or, after pairing, adjacent-token) pairs of a word of 8
+// nibbles: pair i in h[i].  s: e 2^15 in both halves, s4: s 2^-4, c: -s 2^-21.
+__device__ __forceinline__ void nibbles(uint32_t w, uint32_t s, uint32_t s4, uint32_t c,
+                                        uint32_t (&h)[4]) {
+    const uint32_t w8 = w >> 8;
+    h[0] = h2fma(w & 0x000f000fu, s, c);
+    h[1] = h2fma(w & 0x00f000f0u, s4, c);
+    h[2] = h2fma(w8 & 0x000f000fu, s, c);
+    h[3] = h2fma(w8 & 0x00f000f0u, s4, c);
+}
+constexpr uint32_t H2_M2_21 = 0x80088008u;   // -2^-21, twice
+constexpr uint32_t H2_2_4 = 0x2c002c00u;     // 2^-4, twice
+constexpr uint32_t H2_M1152 = 0xe480e480u;   // -1152, twice
+
+template <int BITS, int D, int NB>
+struct Narrow {
+    using U = KvUnit<BITS, D>;
+    static constexpr int ROWS = 8 * NB;
+    static constexpr int STAGE = U::BYTES + 64;          // a unit and its tags
+    static constexpr int SUM = NW / 2 * ROWS * D * 4;    // half of the warps' accumulators
+    static constexpr int Q_ROW = D * 2 + 32;
+    static constexpr int SMALL = ROWS * Q_ROW + ROWS * 5 * 4 + NW * ROWS * 2 * 4 + NW * 4 + 34 * 8 + 64;
+    static constexpr int WANT = (110 * 1024 - SUM - SMALL) / (NW * (STAGE + 16));
+    static constexpr int MOST = (220 * 1024 - SUM - SMALL) / (NW * (STAGE + 16));
+    // two CTAs an SM where three stages of a unit leave room for it
+    static constexpr bool TWO = WANT >= 3 && NB == 1 && D <= 128;
+    static constexpr int NS_ = TWO ? WANT : MOST;
+    static constexpr int NS = NS_ > 8 ? 8 : NS_;
+    static_assert(NS >= 2, "a ring of two units");
+    static constexpr int RING = NW * NS * STAGE;
+    static constexpr int SMEM = RING + NW * NS * 12 + SUM + SMALL;
+    static constexpr bool Q_REG = D / 16 * 2 * NB <= 32;
+};
+
+// The query rows of a tile, as fp16 in the order of the B fragments: row r,
+// dims c D/4 + 4 kk + {0..3} at ((kk * 4 + c) * 4) halves.  bf16 rows are scaled by
+// a power of two to a largest magnitude in [1, 2): exact but for values below
+// 2^-14 of it.
+template <int D>
+__device__ __forceinline__ float load_query(const AttendParams &p, bool bf16, int64_t at,
+                                            unsigned char *dst) {
+    const int lane = threadIdx.x & 31;
+    constexpr int N = D / 32;                  // values a lane loads
+    float x[N];
+    if (bf16) {
+        const __nv_bfloat16 *src = (const __nv_bfloat16 *)p.q + at + lane * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = __bfloat162float(src[i]);
+    } else {
+        const __half *src = (const __half *)p.q + at + lane * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = __half2float(src[i]);
+    }
+    int e = 0;
+    if (bf16) {
+        float a = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) a = fmaxf(a, fabsf(x[i]));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+        e = max(-126, min(126, (int)(__float_as_uint(a) >> 23) - 127));
+        const float f = pow2i(-e);
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] *= f;
+    }
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+        const int d = lane * N + i, c = d / (D / 4), kk = d % (D / 4) / 4;
+        *(uint32_t *)(dst + ((kk * 4 + c) * 4 + (d & 3)) * 2) = pack_h2(x[i], x[i + 1]);
+    }
+    return scale2(1.f, e);
+}
+
+template <int BITS, int D, int NB>
+__global__ void __launch_bounds__(NW * 32, Narrow<BITS, D, NB>::TWO ? 2 : 1)
+k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int hi, const int min_per) {
+    using C = Narrow<BITS, D, NB>;
+    using U = typename C::U;
+    constexpr int ROWS = C::ROWS, NS = C::NS, MT = D / 16;
+    extern __shared__ __align__(128) unsigned char smem[];
+    unsigned char *at = smem + C::RING;
+    float *sum = (float *)at;                             at += C::SUM;
+    unsigned char *qs = at;                               at += ROWS * C::Q_ROW;
+    int64_t *scratch = (int64_t *)at;                     at += 34 * 8;
+    uint64_t *bars = (uint64_t *)at;                      at += NW * NS * 8;
+    int *meta = (int *)at;                                at += NW * NS * 4;
+    float *qfac = (float *)at;                            at += ROWS * 4;
+    float *slope = (float *)at;                           at += ROWS * 4;
+    int *limit = (int *)at;                               at += ROWS * 4;
+    int *pos = (int *)at;                                 at += ROWS * 4;
+    int *qtag = (int *)at;                                at += ROWS * 4;
+    float *wm = (float *)at;                              at += NW * ROWS * 4;
+    float *wl = (float *)at;                              at += NW * ROWS * 4;
+    int *wt = (int *)at;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int g = lane >> 2, c = lane & 3;
+    unsigned char *ring = smem + warp * NS * C::STAGE;
+    uint64_t *bar = bars + warp * NS;
+    int *mt_ = meta + warp * NS;
+    if (lane == 0)
+        for (int i = 0; i < NS; ++i) mbar_init(bar + i, 1);
+    mbar_fence_init();
+    __syncthreads();
+
+    int64_t first, count, per;
+    AttendCursor cur;
+    if (tid == 0) p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    if (!attend_plan(p, ROWS, KV_UNIT, lo, hi, min_per, scratch, first, count, per, cur)) return;
+
+    bool ok = true;                            // no wait of this warp has expired
+    uint32_t used = 0;                         // stages of the ring filled so far
+    const bool tags = p.tags != nullptr, heavy = p.cap > 0.f || p.slopes;
+    const float cap_l = p.cap * LOG2E_F, cap_in = p.cap > 0.f ? 2.f / p.cap : 0.f;
+    int64_t left = count;
+    bool head_item = true;                     // the share's first item
+    while (left > 0) {
+        const int n = (int)min((int64_t)(cur.units - cur.unit), left);
+        const AttendSeq sq = cur.q;
+        const int row_first = cur.tile * ROWS, rows = min(ROWS, sq.nq * p.group - row_first);
+
+        // ---- this warp's units of the item: unit + warp, + NW, ...
+        const int mine = (n - warp + NW - 1) / NW;
+        const int64_t *list = p.blocks + cur.seq * p.max_blocks;
+        auto place = [&](int i) -> int64_t {   // of the warp's i-th unit, -1: not listed
+            if (i >= mine) return -1;
+            const int u = cur.unit + warp + i * NW, b = u / p.per_block;
+            if (u >= (sq.kv + KV_UNIT - 1) / KV_UNIT) return -1;   // an item without keys
+            const int64_t id = list[b];
+            if (id < 0 || id >= p.n_blocks) {
+                if (id != -1) set_status(p.status, AKASHIC_EDEVICE);
+                return -1;
+            }
+            return id * p.per_block + (u - b * p.per_block);
+        };
+        int64_t batch = place(lane), next = place(32 + lane);
+        const uint32_t base = used;
+        auto issue = [&](int i) {
+            if (i >= mine) return;
+            if (i && (i & 31) == 0) {
+                batch = next;
+                next = place(i + 32 + lane);
+            }
+            const int64_t u = __shfl_sync(0xffffffffu, batch, i & 31);
+            if (lane == 0) {
+                const int st = (base + i) % NS;
+                mt_[st] = u >= 0;
+                if (u >= 0) {
+                    // the unit's place among all heads of its block
+                    const int64_t b = u / p.per_block, w = u - b * p.per_block;
+                    const int64_t full = (b * p.heads + cur.head) * p.per_block + w;
+                    mbar_expect_tx(bar + st, U::BYTES + (tags ? 64 : 0));
+                    bulk_load(ring + st * C::STAGE, p.cache + full * U::BYTES, U::BYTES, bar + st);
+                    if (tags) bulk_load(ring + st * C::STAGE + U::BYTES, p.tags + u * 16, 64, bar + st);
+                } else {
+                    mbar_arrive(bar + st);
+                }
+            }
+        };
+        if (ok)
+            for (int i = 0; i < NS; ++i) issue(i);
+
+        // ---- the query rows
+        for (int r = warp; r < ROWS; r += NW) {
+            float f = 0.f;
+            int i = 0, hd = 0;
+            if (r < rows) {
+                i = (row_first + r) / p.group, hd = cur.head * p.group + (row_first + r) % p.group;
+                f = load_query<D>(p, bf16, (sq.row0 + i) * p.q_row + hd * p.q_head, qs + r * C::Q_ROW);
+            } else {
+                for (int d = lane; d < D / 2; d += 32) ((uint32_t *)(qs + r * C::Q_ROW))[d] = 0;
+            }
+            if (lane == 0) {
+                qfac[r] = f * p.scale * LOG2E_F * (BITS == 4 ? 512.f : 1.f);
+                slope[r] = r < rows && p.slopes ? p.slopes[hd] * LOG2E_F : 0.f;
+                limit[r] = r < rows ? attend_limit(p, sq, i) : sq.kv;
+                pos[r] = sq.kv - sq.nq + i;
+                qtag[r] = r < rows && p.q_tags ? p.q_tags[sq.row0 + i] : -1;
+            }
+        }
+        __syncthreads();
+        uint32_t qf[C::Q_REG ? NB : 1][C::Q_REG ? MT : 1][2];
+        if constexpr (C::Q_REG) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int k = 0; k < MT; ++k) {
+                    const uint2 x = *(const uint2 *)(qs + (b * 8 + g) * C::Q_ROW + (k * 4 + c) * 8);
+                    qf[b][k][0] = x.x, qf[b][k][1] = x.y;
+                }
+        }
+        float qk[NB][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            qk[b][0] = qfac[b * 8 + 2 * c], qk[b][1] = qfac[b * 8 + 2 * c + 1];
+        const int all_see = limit[0];          // keys below it are seen by every row
+
+        float o[NB][MT][4], m[NB][2], l[NB][2];
+        int tref = -127;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t) o[b][t][0] = o[b][t][1] = o[b][t][2] = o[b][t][3] = 0.f;
+            m[b][0] = m[b][1] = NEG, l[b][0] = l[b][1] = 0.f;
+        }
+
+        for (int it = 0; ok && it < mine; ++it) {
+            const int st = (base + it) % NS;
+            if (!mbar_wait(bar + st, ((base + it) / NS) & 1, p.status)) {
+                ok = false;                    // its copies still land: wait for the rest
+                for (int k = it + 1; k < min(mine, it + NS); ++k)
+                    mbar_wait(bar + (base + k) % NS, ((base + k) / NS) & 1, p.status);
+                break;
+            }
+            const unsigned char *un = ring + st * C::STAGE;
+            const int tok = (cur.unit + warp + it * NW) * KV_UNIT;
+            if (mt_[st]) {
+                // ---- S^T = K Q^T
+                float s[NB][4];
+#pragma unroll
+                for (int b = 0; b < NB; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
+                auto keys = [&](int kk, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        if constexpr (C::Q_REG) {
+                            mma16(s[b], a0, a1, a2, a3, qf[b][kk][0], qf[b][kk][1]);
+                        } else {
+                            const uint2 x = *(const uint2 *)(qs + (b * 8 + g) * C::Q_ROW + (kk * 4 + c) * 8);
+                            mma16(s[b], a0, a1, a2, a3, x.x, x.y);
+                        }
+                    }
+                };
+                float kf0, kf1;                // scale of the keys of tokens g and g + 8
+                if constexpr (BITS == 4) {
+                    constexpr int W = D / 32, PER = D / 64;    // words and groups of a token
+                    uint32_t w[2][W], sc[(2 * PER + 3) / 4];
+                    if constexpr (D == 64) {
+                        const uint4 x = *(const uint4 *)(un + U::K_CODES + lane * 16);
+                        w[0][0] = x.x, w[0][1] = x.y, w[1][0] = x.z, w[1][1] = x.w;
+                        sc[0] = *(const uint16_t *)(un + U::K_SCALES + lane * 2);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int q = 0; q < W / 4; ++q) {
+                                const uint4 x = *(const uint4 *)(un + U::K_CODES + ((j * (W / 4) + q) * 32 + lane) * 16);
+                                w[j][q * 4] = x.x, w[j][q * 4 + 1] = x.y, w[j][q * 4 + 2] = x.z, w[j][q * 4 + 3] = x.w;
+                            }
+                        if constexpr (D == 128) {
+                            sc[0] = *(const uint32_t *)(un + U::K_SCALES + lane * 4);
+                        } else {
+                            const uint2 x = *(const uint2 *)(un + U::K_SCALES + lane * 8);
+                            sc[0] = x.x, sc[1] = x.y;
+                        }
+                    }
+                    const uint32_t ex = *(const uint16_t *)(un + U::K_EXP + g * 2);
+                    kf0 = __uint_as_float((ex & 255u) << 23), kf1 = __uint_as_float((ex >> 8) << 23);
+#pragma unroll
+                    for (int gr = 0; gr < PER; ++gr) {
+                        uint32_t sj[2], s4[2], cj[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int b = j * PER + gr;
+                            const uint32_t by = (sc[b / 4] >> (8 * (b & 3))) & 255u;
+                            sj[j] = by * 0x00400040u + 0x3c003c00u;
+                            s4[j] = sj[j] - 0x10001000u;
+                            cj[j] = h2mul(sj[j], H2_M2_21);
+                        }
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t h0[4], h1[4];
+                            nibbles(w[0][gr * 2 + q], sj[0], s4[0], cj[0], h0);
+                            nibbles(w[1][gr * 2 + q], sj[1], s4[1], cj[1], h1);
+                            const int kk = (gr * 2 + q) * 2;
+                            keys(kk, h0[0], h1[0], h0[1], h1[1]);
+                            keys(kk + 1, h0[2], h1[2], h0[3], h1[3]);
+                        }
+                    }
+                } else {
+                    constexpr int CH = D / 64;                 // 16-byte chunks of a token
+#pragma unroll
+                    for (int q = 0; q < CH; ++q) {
+                        const uint4 x = *(const uint4 *)(un + U::K_CODES + (q * 32 + lane) * 16);
+                        const uint4 y = *(const uint4 *)(un + U::K_CODES + ((CH + q) * 32 + lane) * 16);
+                        const uint32_t wx[4] = {x.x, x.y, x.z, x.w}, wy[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            keys(q * 4 + i, h2add(__byte_perm(wx[i], 0x64646464u, 0x4140), H2_M1152),
+                                 h2add(__byte_perm(wy[i], 0x64646464u, 0x4140), H2_M1152),
+                                 h2add(__byte_perm(wx[i], 0x64646464u, 0x4342), H2_M1152),
+                                 h2add(__byte_perm(wy[i], 0x64646464u, 0x4342), H2_M1152));
+                    }
+                    const uint32_t ks = *(const uint32_t *)(un + U::K_SCALES + g * 4);
+                    kf0 = __uint_as_float(ks << 16), kf1 = __uint_as_float(ks & 0xffff0000u);
+                }
+
+                // ---- scores in log2 units; what a row does not see is -inf
+                int tag0 = 0, tag1 = 0;
+                if (tags) {
+                    tag0 = ((const int *)(un + U::BYTES))[g];
+                    tag1 = ((const int *)(un + U::BYTES))[g + 8];
+                }
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[b][r] *= (r < 2 ? kf0 : kf1) * qk[b][r & 1];
+                    if (heavy) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int col = b * 8 + 2 * c + (r & 1);
+                            if (p.cap > 0.f)
+                                s[b][r] = cap_l * (1.f - __fdividef(2.f, 1.f + ex2(s[b][r] * cap_in)));
+                            if (p.slopes)
+                                s[b][r] -= slope[col] * (float)abs(pos[col] - (tok + g + (r < 2 ? 0 : 8)));
+                        }
+                    }
+                    if (tags || tok + KV_UNIT > all_see) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int col = b * 8 + 2 * c + (r & 1);
+                            const int tag = r < 2 ? tag0 : tag1;
+                            const bool seen = tok + g + (r < 2 ? 0 : 8) < limit[col] &&
+                                              (!tags || (tag >= 0 && tag == qtag[col]));
+                            if (!seen) s[b][r] = -INFINITY;
+                        }
+                    }
+                }
+                // ---- running maxima
+                bool raise = false;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) raise |= s[b][r] > m[b][r & 1] + M_SLACK;
+                if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            float x = fmaxf(s[b][r], s[b][r + 2]);
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                            x = fmaxf(x, m[b][r]);
+                            const float f = ex2(m[b][r] - x);
+                            m[b][r] = x;
+                            l[b][r] *= f;
+#pragma unroll
+                            for (int t = 0; t < MT; ++t) o[b][t][r] *= f, o[b][t][r + 2] *= f;
+                        }
+                }
+                // ---- weights, and P^T as the B operand
+                float vf0 = 1.f, vf1 = 1.f;    // 8 bits: the significands of the values' scales
+                if constexpr (BITS == 8) {
+                    const uint16_t *vs = (const uint16_t *)(un + U::V_SCALES);
+                    vf0 = __uint_as_float(((uint32_t)(vs[U::v_row(0) + (g >> 1) * 4 + (g & 1)] & 0x7fu) << 16) | 0x3f800000u);
+                    vf1 = __uint_as_float(((uint32_t)(vs[U::v_row(8) + (g >> 1) * 4 + (g & 1)] & 0x7fu) << 16) | 0x3f800000u);
+                }
+                uint32_t pb[NB][2];
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        s[b][r] = ex2(s[b][r] - (m[b][r & 1] - P_SHIFT));
+                        l[b][r & 1] += s[b][r];
+                    }
+                    if constexpr (BITS == 8) {
+                        s[b][0] *= vf0, s[b][1] *= vf0, s[b][2] *= vf1, s[b][3] *= vf1;
+                    }
+                    pb[b][0] = transpose8(pack_h2(s[b][0], s[b][1]));
+                    pb[b][1] = transpose8(pack_h2(s[b][2], s[b][3]));
+                }
+                // ---- the values' exponents, relative to the largest so far
+                int te[4];                     // of tokens 2c, 2c + 1, 2c + 8, 2c + 9
+                if constexpr (BITS == 4) {
+                    const uint32_t x = *(const uint32_t *)(un + U::V_EXP + c * 4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) te[i] = (int)((x >> (8 * i)) & 255u) - 127;
+                } else {
+                    const uint2 x = *(const uint2 *)(un + U::V_SCALES + c * 8);
+                    te[0] = (int)((x.x >> 7) & 255u) - 127, te[1] = (int)((x.x >> 23) & 255u) - 127;
+                    te[2] = (int)((x.y >> 7) & 255u) - 127, te[3] = (int)((x.y >> 23) & 255u) - 127;
+                }
+                if (tags || tok + KV_UNIT > sq.kv) {   // a slot without a token adds nothing
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int t = 2 * c + (i & 1) + (i >> 1) * 8;
+                        const bool real = tok + t < sq.kv &&
+                                          (!tags || ((const int *)(un + U::BYTES))[t] >= 0);
+                        if (!real) te[i] = -1000;
+                    }
+                }
+                const int tm = max(max(te[0], te[1]), max(te[2], te[3]));
+                if (__any_sync(0xffffffffu, tm > tref)) {
+                    int x = max(tm, __shfl_xor_sync(0xffffffffu, tm, 1));
+                    x = max(max(x, __shfl_xor_sync(0xffffffffu, x, 2)), tref);
+                    const float f = pow2i(max(-126, tref - x));
+                    tref = x;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int t = 0; t < MT; ++t)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) o[b][t][r] *= f;
+                }
+                float tf[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tf[i] = te[i] - tref < -40 ? 0.f : pow2i(te[i] - tref);
+                const uint32_t f0 = pack_h2(tf[0], tf[1]), f1 = pack_h2(tf[2], tf[3]);
+
+                // ---- O^T += V^T P^T
+                auto values = [&](int mt, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) mma16(o[b][mt], a0, a1, a2, a3, pb[b][0], pb[b][1]);
+                };
+                if constexpr (BITS == 4) {
+                    constexpr int W = D / 64;                  // words a lane has of a token
+                    uint32_t w[4][W];                          // tokens 2c, 2c + 1, 2c + 8, 2c + 9
+                    if constexpr (W == 1) {
+                        const uint4 x = *(const uint4 *)(un + U::V_CODES + lane * 16);
+                        w[0][0] = x.x, w[1][0] = x.y, w[2][0] = x.z, w[3][0] = x.w;
+                    } else if constexpr (W == 2) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint4 x = *(const uint4 *)(un + U::V_CODES + (j * 32 + lane) * 16);
+                            w[2 * j][0] = x.x, w[2 * j][1] = x.y, w[2 * j + 1][0] = x.z, w[2 * j + 1][1] = x.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint4 x = *(const uint4 *)(un + U::V_CODES + (i * 32 + lane) * 16);
+                            w[i][0] = x.x, w[i][1] = x.y, w[i][2] = x.z, w[i][3] = x.w;
+                        }
+                    }
+                    constexpr int GL = D == 256 ? 2 : 1;       // groups a lane has of a token
+#pragma unroll
+                    for (int gl = 0; gl < GL; ++gl) {
+                        const int gr = D == 64 ? g >> 1 : g * GL + gl;
+                        const uint32_t x = *(const uint32_t *)(un + U::V_SCALES + (gr * 4 + c) * 4);
+                        const uint32_t s0 = h2mul(__byte_perm(x, 0, 0x4140) * 64u + 0x3c003c00u, f0);
+                        const uint32_t s1 = h2mul(__byte_perm(x, 0, 0x4342) * 64u + 0x3c003c00u, f1);
+                        const uint32_t s04 = h2mul(s0, H2_2_4), s14 = h2mul(s1, H2_2_4);
+                        const uint32_t c0 = h2mul(s0, H2_M2_21), c1 = h2mul(s1, H2_M2_21);
+                        constexpr int WG = W / GL;             // words of a group
+#pragma unroll
+                        for (int q = 0; q < WG; ++q) {
+                            const int i = gl * WG + q;
+                            uint32_t x0[4], y0[4], x1[4], y1[4];
+                            nibbles(__byte_perm(w[0][i], w[1][i], 0x5410), s0, s04, c0, x0);
+                            nibbles(__byte_perm(w[0][i], w[1][i], 0x7632), s0, s04, c0, y0);
+                            nibbles(__byte_perm(w[2][i], w[3][i], 0x5410), s1, s14, c1, x1);
+                            nibbles(__byte_perm(w[2][i], w[3][i], 0x7632), s1, s14, c1, y1);
+#pragma unroll
+                            for (int t = 0; t < 4; ++t) values(i * 4 + t, x0[t], y0[t], x1[t], y1[t]);
+                        }
+                    }
+                } else {
+                    constexpr int W = D / 32;                  // words (4 dims) of a token
+                    uint32_t w[4][W];
+                    if constexpr (W == 2) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint4 x = *(const uint4 *)(un + U::V_CODES + (j * 32 + lane) * 16);
+                            w[2 * j][0] = x.x, w[2 * j][1] = x.y, w[2 * j + 1][0] = x.z, w[2 * j + 1][1] = x.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int q = 0; q < W / 4; ++q) {
+                                const uint4 x = *(const uint4 *)(un + U::V_CODES + ((i * (W / 4) + q) * 32 + lane) * 16);
+                                w[i][q * 4] = x.x, w[i][q * 4 + 1] = x.y, w[i][q * 4 + 2] = x.z, w[i][q * 4 + 3] = x.w;
+                            }
+                    }
+                    const uint32_t c0 = h2mul(f0, H2_M1152), c1 = h2mul(f1, H2_M1152);
+#pragma unroll
+                    for (int i = 0; i < W; ++i)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const uint32_t sel = half ? 0x7362 : 0x5140;
+                            const uint32_t x = __byte_perm(w[0][i], w[1][i], sel);
+                            const uint32_t y = __byte_perm(w[2][i], w[3][i], sel);
+                            values(i * 2 + half,
+                                   h2fma(__byte_perm(x, 0x64646464u, 0x4140), f0, c0),
+                                   h2fma(__byte_perm(x, 0x64646464u, 0x4342), f0, c0),
+                                   h2fma(__byte_perm(y, 0x64646464u, 0x4140), f1, c1),
+                                   h2fma(__byte_perm(y, 0x64646464u, 0x4342), f1, c1));
+                        }
+                }
+            }
+            __syncwarp();                      // the stage has been read
+            issue(it + NS);
+        }
+        if (mine > 0) used = base + mine;
+
+        // ---- join the warps: rescale to the item's maxima, half of them
+        // hand their accumulators to the other half, which then add up in order
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1)
+                    l[b][r] += __shfl_xor_sync(0xffffffffu, l[b][r], off);
+                if (g == 0) {
+                    wm[warp * ROWS + b * 8 + 2 * c + r] = m[b][r];
+                    wl[warp * ROWS + b * 8 + 2 * c + r] = l[b][r];
+                }
+            }
+        if (lane == 0) wt[warp] = tref;
+        __syncthreads();
+        int tmax = -127;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) tmax = max(tmax, wt[w]);
+        const float ft = pow2i(max(-126, tref - tmax));
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                float x = NEG;
+#pragma unroll
+                for (int w = 0; w < NW; ++w) x = fmaxf(x, wm[w * ROWS + b * 8 + 2 * c + r]);
+                const float f = ex2(m[b][r] - x) * ft;
+#pragma unroll
+                for (int t = 0; t < MT; ++t) o[b][t][r] *= f, o[b][t][r + 2] *= f;
+            }
+        float *slot = sum + (warp & (NW / 2 - 1)) * ROWS * D;
+        auto each = [&](auto &&fn) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        fn((float2 *)(slot + (b * 8 + 2 * c + r) * D + g * (D / 8) + 2 * t), o[b][t][r],
+                           o[b][t][r + 2]);
+        };
+        if (warp >= NW / 2) each([](float2 *a, float x, float y) { *a = make_float2(x, y); });
+        __syncthreads();
+        if (warp < NW / 2)
+            each([](float2 *a, float x, float y) {
+                const float2 v = *a;
+                *a = make_float2(v.x + x, v.y + y);
+            });
+        __syncthreads();
+        // ---- whole items are written, others left for the joining kernel
+        const bool whole = cur.unit == 0 && n == cur.units;
+        const int64_t slot_floats = attend_slot_floats(ROWS, D);
+        float *part = p.partial + ((int64_t)blockIdx.x * 2 + (head_item ? 0 : 1)) * slot_floats;
+        constexpr int UP = BITS == 4 ? 9 : 0;
+        for (int x = tid; x < ROWS * (D / 2); x += NW * 32) {
+            const int r = x / (D / 2), d = x % (D / 2) * 2;
+            float2 v = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < NW / 2; ++w) {
+                const float2 y = *(const float2 *)(sum + (w * ROWS + r) * D + d);
+                v.x += y.x, v.y += y.y;
+            }
+            float mx = NEG, tot = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) mx = fmaxf(mx, wm[w * ROWS + r]);
+#pragma unroll
+            for (int w = 0; w < NW; ++w) tot += wl[w * ROWS + r] * ex2(wm[w * ROWS + r] - mx);
+            if (!whole) {
+                *(float2 *)(part + r * D + d) =
+                    make_float2(scale2(v.x, tmax + UP), scale2(v.y, tmax + UP));
+                if (d == 0) part[ROWS * D + r] = mx, part[ROWS * D + ROWS + r] = tot;
+            } else if (r < rows) {
+                const float inv = tot > 0.f ? 1.f / tot : tot;   // a NaN stays one
+                const int i = (row_first + r) / p.group, hd = cur.head * p.group + (row_first + r) % p.group;
+                const int64_t dst = ((int64_t)(sq.row0 + i) * p.q_heads + hd);
+                const float a = scale2(v.x * inv, tmax + UP), b = scale2(v.y * inv, tmax + UP);
+                if (bf16) {
+                    *(__nv_bfloat162 *)((__nv_bfloat16 *)p.out + dst * D + d) = __floats2bfloat162_rn(a, b);
+                } else {
+                    *(uint32_t *)((__half *)p.out + dst * D + d) = pack_h2(a, b);
+                }
+                if (d == 0 && p.lse)
+                    p.lse[dst] = tot == 0.f ? -INFINITY : (mx - P_SHIFT + log2f(tot)) * 0.69314718055994530942f;
+            }
+        }
+        if (tid == 0 && cur.unit == 0 && !whole) {
+            // the item begins here and ends in the share of a later CTA
+            const int64_t end = first + (count - left) + cur.units;
+            p.joins[blockIdx.x] = make_int4(cur.seq, cur.head, cur.tile,
+                                            ((int)((end - 1) / per) << 1) | (head_item ? 0 : 1));
+        }
+        left -= n;
+        head_item = false;
+        if (left > 0) {
+            attend_next(p, ROWS, KV_UNIT, lo, hi, cur);
+            __syncthreads();                   // the item's rows in shared memory are free
+        }
+    }
+}
+
+// One warp a row of an item whose steps lay in several CTAs: the slots in the
+// order of the CTAs.
+template <int D>
+__global__ void __launch_bounds__(256)
+k_attend_join(const AttendParams p, const int rows, const bool bf16) {
+    griddep_wait();
+    const int4 j = p.joins[blockIdx.x];
+    if (j.x < 0) return;
+    const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5);
+    const AttendSeq sq = attend_seq(p, j.x);
+    const int row = j.z * rows + r;
+    if (r >= rows || row >= sq.nq * p.group) return;
+    const int last = j.w >> 1;
+    const int64_t floats = attend_slot_floats(rows, D);
+    const float *first = p.partial + ((int64_t)blockIdx.x * 2 + (j.w & 1)) * floats;
+    auto slot = [&](int k) {   // of the k-th CTA after the first
+        return k == 0 ? first : p.partial + (int64_t)(blockIdx.x + k) * 2 * floats;
+    };
+    const int parts = last - (int)blockIdx.x + 1;
+    float mx = NEG;
+    for (int k = lane; k < parts; k += 32) mx = fmaxf(mx, slot(k)[rows * D + r]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    constexpr int N = D / 32;
+    float v[N], tot = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) {
+        const float *s = slot(k);
+        const float f = ex2(s[rows * D + r] - mx);
+        tot += f * s[rows * D + rows + r];
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 y = *(const float2 *)(s + r * D + i * 32 + lane * 2);
+            v[i] += f * y.x, v[i + 1] += f * y.y;
+        }
+    }
+    const float inv = tot > 0.f ? 1.f / tot : tot;
+    const int i = row / p.group, hd = j.y * p.group + row % p.group;
+    const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + hd;
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+        const int d = k * 32 + lane * 2;
+        if (bf16)
+            *(__nv_bfloat162 *)((__nv_bfloat16 *)p.out + dst * D + d) =
+                __floats2bfloat162_rn(v[k] * inv, v[k + 1] * inv);
+        else
+            *(uint32_t *)((__half *)p.out + dst * D + d) = pack_h2(v[k] * inv, v[k + 1] * inv);
+    }
+    if (lane == 0 && p.lse)
+        p.lse[dst] = tot == 0.f ? -INFINITY : (mx - P_SHIFT + log2f(tot)) * 0.69314718055994530942f;
+}
+
+constexpr int MIN_PER = 16;   // units of a share, at least: two a warp
+
+template <int BITS, int D, int NB>
+cudaError_t run_narrow(const AttendParams &p, int dtype, int ctas, int lo, int hi, cudaStream_t st) {
+    using C = Narrow<BITS, D, NB>;
+    auto *kernel = k_attend_narrow<BITS, D, NB>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    if (e != cudaSuccess) return e;
+    kernel<<<ctas, NW * 32, C::SMEM, st>>>(p, dtype == AKASHIC_DTYPE_BF16, lo, hi, MIN_PER);
+    return cudaGetLastError();
+}
+template <int BITS, int D>
+cudaError_t run_narrow_rows(const AttendParams &p, int dtype, const AttendShape &s, int lo, int hi,
+                            cudaStream_t st) {
+    if (s.rows == 8) return run_narrow<BITS, D, 1>(p, dtype, s.ctas, lo, hi, st);
+    if (s.rows == 16) return run_narrow<BITS, D, 2>(p, dtype, s.ctas, lo, hi, st);
+    if constexpr (D <= 128) return run_narrow<BITS, D, 4>(p, dtype, s.ctas, lo, hi, st);
+    return cudaErrorInvalidValue;
+}
+template <int BITS>
+cudaError_t run_narrow_dim(const AttendParams &p, int dim, int dtype, const AttendShape &s, int lo,
+                           int hi, cudaStream_t st) {
+    return dim == 64 ? run_narrow_rows<BITS, 64>(p, dtype, s, lo, hi, st)
+           : dim == 128 ? run_narrow_rows<BITS, 128>(p, dtype, s, lo, hi, st)
+                        : run_narrow_rows<BITS, 256>(p, dtype, s, lo, hi, st);
+}
+template <int BITS, int D>
+int narrow_ctas(int rows) {
+    return rows == 8 ? (Narrow<BITS, D, 1>::TWO ? 2 : 1)
+           : rows == 16 ? (Narrow<BITS, D, 2>::TWO ? 2 : 1) : 1;
+}
+
+}  // namespace
+
+AttendShape attend_narrow_shape(int bits, int dim, int max_rows, int sms) {
+    AttendShape s;
+    s.rows = max_rows <= 8 ? 8 : max_rows <= 16 || dim == 256 ? 16 : 32;
+    int per = 1;
+    if (bits == 4)
+        per = dim == 64 ? narrow_ctas<4, 64>(s.rows) : dim == 128 ? narrow_ctas<4, 128>(s.rows) : narrow_ctas<4, 256>(s.rows);
+    else
+        per = dim == 64 ? narrow_ctas<8, 64>(s.rows) : dim == 128 ? narrow_ctas<8, 128>(s.rows) : narrow_ctas<8, 256>(s.rows);
+    s.ctas = sms * per;
+    return s;
+}
+
+cudaError_t launch_attend_narrow(const AttendParams &p, int bits, int dim, int dtype,
+                                 const AttendShape &shape, int lo, int hi, cudaStream_t st) {
+    return bits == 4 ? run_narrow_dim<4>(p, dim, dtype, shape, lo, hi, st)
+                     : run_narrow_dim<8>(p, dim, dtype, shape, lo, hi, st);
+}
+
+cudaError_t launch_attend_join(const AttendParams &p, int dtype, int dim, int ctas, int rows,
+                               cudaStream_t st) {
+    const dim3 grid(ctas, (rows + 7) / 8);
+    const bool bf16 = dtype == AKASHIC_DTYPE_BF16;
+    auto *kernel = dim == 64 ? k_attend_join<64> : dim == 128 ? k_attend_join<128> : k_attend_join<256>;
+    return launch_pdl(kernel, grid, dim3(256), 0, st, p, rows, bf16);
+}
+
+}  // namespace ak
+
+using namespace ak;
+
+namespace {
+
+akashic_status_t attend_check(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_attend_t *a,
+                              const char *who) {
+    if (akashic_status_t s = kv_check_config(cfg, who)) return s;
+    if (!a) return kv_fail(AKASHIC_EINVAL, "%s: NULL arguments", who);
+    if (a->dtype != AKASHIC_DTYPE_BF16 && a->dtype != AKASHIC_DTYPE_FP16)
+        return kv_fail(AKASHIC_EINVAL, "%s: dtype must be BF16 or FP16", who);
+    if (a->q_heads < 1 || a->q_heads % cfg->heads || a->q_heads / cfg->heads > KV_MAX_HEADS)
+        return kv_fail(AKASHIC_EINVAL, "%s: q_heads must be a multiple of heads, at most 1024 times it", who);
+    if (a->n_seq < 0 || a->n_q < 0 || a->max_blocks < 0)
+        return kv_fail(AKASHIC_EINVAL, "%s: n_seq, n_q and max_blocks must be >= 0", who);
+    if (a->max_blocks > 0x7fffff00LL / cfg->block_tokens)
+        return kv_fail(AKASHIC_EINVAL, "%s: a list may hold fewer than 2^31 tokens", who);
+    if ((int64_t)a->n_q * a->q_heads > 0x7fffffffLL)
+        return kv_fail(AKASHIC_EINVAL, "%s: n_q x q_heads must be below 2^31", who);
+    if (!a->q_start && a->n_seq > 0 && a->n_q % a->n_seq)
+        return kv_fail(AKASHIC_EINVAL, "%s: without q_start, n_q must be a multiple of n_seq", who);
+    if (!(a->scale == a->scale) || !(a->scale - a->scale == 0.f))
+        return kv_fail(AKASHIC_EINVAL, "%s: scale must be finite", who);
+    if (!(a->cap >= 0.f) || !(a->cap - a->cap == 0.f))
+        return kv_fail(AKASHIC_EINVAL, "%s: cap must be finite and >= 0", who);
+    if (!a->tags != !a->q_tags)
+        return kv_fail(AKASHIC_EINVAL, "%s: tags and q_tags come together", who);
+    return AKASHIC_OK;
+}
+
+AttendShape shape_of(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_attend_t *a) {
+    const int64_t rows = (int64_t)a->n_q * (a->q_heads / cfg->heads);
+    const int64_t each = a->n_seq > 0 ? ceil_div(rows, (int64_t)a->n_seq) : 0;
+    return attend_narrow_shape(cfg->bits, cfg->head_dim, (int)(each < 64 ? each : 64), device_sm_count());
+}
+int64_t joins_bytes(int ctas) { return ceil_div((int64_t)ctas * 16, (int64_t)256) * 256; }
+
+}  // namespace
+
+extern "C" akashic_status_t akashic_mem_kv_attend_scratch(const akashic_mem_kv_config_t *cfg,
+                                                          const akashic_mem_kv_attend_t *a,
+                                                          int64_t *bytes) {
+    set_last_error("");
+    if (akashic_status_t s = attend_check(cfg, a, "kv_attend_scratch")) return s;
+    if (!bytes) return kv_fail(AKASHIC_EINVAL, "kv_attend_scratch: NULL bytes");
+    KvDevice dev(cfg->device);
+    if (!dev.ok) return kv_fail(AKASHIC_ECUDA, "kv_attend_scratch: device %d cannot be made current", cfg->device);
+    const AttendShape s = shape_of(cfg, a);
+    *bytes = joins_bytes(s.ctas) + s.ctas * 2 * attend_slot_floats(s.rows, cfg->head_dim) * 4;
+    return AKASHIC_OK;
+}
+
+extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t *cfg,
+                                                  const void *cache,
+                                                  const akashic_mem_kv_attend_t *a, void *scratch,
+                                                  int64_t scratch_bytes, int32_t *status,
+                                                  void *stream) {
+    set_last_error("");
+    if (akashic_status_t s = attend_check(cfg, a, "kv_attend")) return s;
+    if (a->n_seq == 0 || a->n_q == 0) return AKASHIC_OK;
+    if (!cache || !a->q || !a->out || (!a->blocks && a->max_blocks) || !scratch)
+        return kv_fail(AKASHIC_EINVAL, "kv_attend: NULL argument");
+    if (((uintptr_t)cache | (uintptr_t)scratch | (uintptr_t)a->tags) & 15u)
+        return kv_fail(AKASHIC_EINVAL, "kv_attend: cache, tags and scratch must be 16-byte aligned");
+    if ((uintptr_t)a->out & 3u || (uintptr_t)a->q & 1u)
+        return kv_fail(AKASHIC_EINVAL, "kv_attend: out must be 4-byte aligned, q to its element");
+    KvDevice dev(cfg->device);
+    if (!dev.ok) return kv_fail(AKASHIC_ECUDA, "kv_attend: device %d cannot be made current", cfg->device);
+    const AttendShape s = shape_of(cfg, a);
+    const int64_t need = joins_bytes(s.ctas) + s.ctas * 2 * attend_slot_floats(s.rows, cfg->head_dim) * 4;
+    if (scratch_bytes < need)
+        return kv_fail(AKASHIC_EINVAL, "kv_attend: scratch needs %lld bytes", (long long)need);
+    AttendParams p = {};
+    p.cache = (const unsigned char *)cache;
+    p.q = a->q, p.q_row = a->q_row_stride, p.q_head = a->q_head_stride;
+    p.out = a->out, p.lse = a->lse;
+    p.q_start = a->q_start, p.kv_len = a->kv_len, p.prefix = a->prefix_len;
+    p.blocks = a->blocks, p.slopes = a->slopes, p.tags = a->tags, p.q_tags = a->q_tags;
+    p.status = status;
+    p.joins = (int4 *)scratch;
+    p.partial = (float *)((unsigned char *)scratch + joins_bytes(s.ctas));
+    p.n_blocks = cfg->n_blocks, p.max_blocks = a->max_blocks;
+    p.n_q = a->n_q, p.n_seq = a->n_seq, p.q_heads = a->q_heads, p.heads = cfg->heads;
+    p.group = a->q_heads / cfg->heads;
+    p.per_block = cfg->block_tokens / KV_UNIT;
+    p.max_kv = (int)(a->max_blocks * cfg->block_tokens);
+    p.causal = a->causal;
+    p.scale = a->scale != 0.f ? a->scale : 1.f / sqrtf((float)cfg->head_dim);
+    p.cap = a->cap;
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t e = launch_attend_narrow(p, cfg->bits, cfg->head_dim, a->dtype, s, 1, 0x7fffffff, st);
+    if (e == cudaSuccess) e = launch_attend_join(p, a->dtype, cfg->head_dim, s.ctas, s.rows, st);
+    if (e != cudaSuccess)
+        return kv_fail(AKASHIC_ECUDA, "kv_attend: launch failed: %s", cudaGetErrorString(e));
+    return AKASHIC_OK;
+}

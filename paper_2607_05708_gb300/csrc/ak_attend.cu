@@ -13,13 +13,14 @@
 //    memory path would want the fp16 tile written to shared memory first.
 //  * a nibble n in the low bits of a half is the subnormal n 2^-24; one fused
 //    multiply-add by e 2^15 and -8 e 2^-9 gives (n - 8) e 2^-9: one instruction
-//    for two values, exact but for groups below 2^-11 of their row (whose values
-//    are rounded to 2^-19 of the row's largest).  The row's 2^T goes to the
-//    score; for values into the group's scale, relative to the largest T so far.
+//    for two values.  Where that is below fp16's normal range it is rounded to
+//    its steps of 2^-24, 2^-17 of the row's largest.  The row's 2^T goes to the
+//    score; for values into the group's scale, relative to the largest T so far,
+//    and 2^-10: rounded to 2^-16 of the largest value so far.
 //  * a warp works on its own units (16 tokens), brought by bulk copies into its
 //    own ring, with its own running maximum, sum and accumulators: no barrier in
 //    the loop.  The warps of a CTA are joined at the end of an item.
-//  * P is fp16, 2^6 p: weights down to 2^-20 of the largest keep 11 bits; sums,
+//  * P is fp16, 2^6 p: weights down to 2^-20 of the largest so far keep 11 bits; sums,
 //    maxima and accumulators are fp32.  The maximum is raised only when a
 //    score exceeds it by 2^8, so that the accumulators are rarely rescaled.
 #include "ak_attend.cuh"
@@ -205,18 +206,24 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
         // ---- this warp's units of the item: unit + warp, + NW, ...
         const int mine = (n - warp + NW - 1) / NW;
         const int64_t *list = p.blocks + cur.seq * p.max_blocks;
-        auto place = [&](int i) -> int64_t {   // of the warp's i-th unit, -1: not listed
-            if (i >= mine) return -1;
+        struct Place {
+            int64_t unit;                      // of the cache, -1: not listed
+            int slots;                         // the unit's slots / 16
+        };
+        // Lane x looks up the warp's units x, x + 32, ..., one batch ahead.
+        auto place = [&](int i) -> Place {
+            if (i >= mine) return {-1, 0};
             const int u = cur.unit + warp + i * NW, b = u / p.per_block;
-            if (u >= (sq.kv + KV_UNIT - 1) / KV_UNIT) return -1;   // an item without keys
+            if (u >= (sq.kv + KV_UNIT - 1) / KV_UNIT) return {-1, 0};   // an item without keys
             const int64_t id = list[b];
             if (id < 0 || id >= p.n_blocks) {
                 if (id != -1) set_status(p.status, AKASHIC_EDEVICE);
-                return -1;
+                return {-1, 0};
             }
-            return id * p.per_block + (u - b * p.per_block);
+            const int w = u - b * p.per_block;
+            return {(id * p.heads + cur.head) * p.per_block + w, (int)id * p.per_block + w};
         };
-        int64_t batch = place(lane), next = place(32 + lane);
+        Place batch = place(lane), next = place(32 + lane);
         const uint32_t base = used;
         auto issue = [&](int i) {
             if (i >= mine) return;
@@ -224,17 +231,16 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                 batch = next;
                 next = place(i + 32 + lane);
             }
-            const int64_t u = __shfl_sync(0xffffffffu, batch, i & 31);
+            const int64_t u = __shfl_sync(0xffffffffu, batch.unit, i & 31);
+            const int sl = tags ? __shfl_sync(0xffffffffu, batch.slots, i & 31) : 0;
             if (lane == 0) {
                 const int st = (base + i) % NS;
                 mt_[st] = u >= 0;
                 if (u >= 0) {
-                    // the unit's place among all heads of its block
-                    const int64_t b = u / p.per_block, w = u - b * p.per_block;
-                    const int64_t full = (b * p.heads + cur.head) * p.per_block + w;
                     mbar_expect_tx(bar + st, U::BYTES + (tags ? 64 : 0));
-                    bulk_load(ring + st * C::STAGE, p.cache + full * U::BYTES, U::BYTES, bar + st);
-                    if (tags) bulk_load(ring + st * C::STAGE + U::BYTES, p.tags + u * 16, 64, bar + st);
+                    bulk_load(ring + st * C::STAGE, p.cache + u * U::BYTES, U::BYTES, bar + st);
+                    if (tags)
+                        bulk_load(ring + st * C::STAGE + U::BYTES, p.tags + (int64_t)sl * 16, 64, bar + st);
                 } else {
                     mbar_arrive(bar + st);
                 }
@@ -278,13 +284,14 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
             qk[b][0] = qfac[b * 8 + 2 * c], qk[b][1] = qfac[b * 8 + 2 * c + 1];
         const int all_see = limit[0];          // keys below it are seen by every row
 
-        float o[NB][MT][4], m[NB][2], l[NB][2];
+        float o[NB][MT][4], mm[NB][2], l[NB][2];
         int tref = -127;
+        uint32_t unset = (1u << (2 * NB)) - 1u;    // rows that have not seen a key yet: mm = 0
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
             for (int t = 0; t < MT; ++t) o[b][t][0] = o[b][t][1] = o[b][t][2] = o[b][t][3] = 0.f;
-            m[b][0] = m[b][1] = NEG, l[b][0] = l[b][1] = 0.f;
+            mm[b][0] = mm[b][1] = 0.f, l[b][0] = l[b][1] = 0.f;
         }
 
         for (int it = 0; ok && it < mine; ++it) {
@@ -377,27 +384,34 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                     kf0 = __uint_as_float(ks << 16), kf1 = __uint_as_float(ks & 0xffff0000u);
                 }
 
-                // ---- scores in log2 units; what a row does not see is -inf
+                // ---- scores in log2 units less the running maximum (mm = m - 6);
+                // what a row does not see is -inf
                 int tag0 = 0, tag1 = 0;
                 if (tags) {
                     tag0 = ((const int *)(un + U::BYTES))[g];
                     tag1 = ((const int *)(un + U::BYTES))[g + 8];
                 }
+                const bool masked = tags || tok + KV_UNIT > all_see;
+                float most = NEG;
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s[b][r] *= (r < 2 ? kf0 : kf1) * qk[b][r & 1];
                     if (heavy) {
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const int col = b * 8 + 2 * c + (r & 1);
+                            s[b][r] *= (r < 2 ? kf0 : kf1) * qk[b][r & 1];
                             if (p.cap > 0.f)
                                 s[b][r] = cap_l * (1.f - __fdividef(2.f, 1.f + ex2(s[b][r] * cap_in)));
                             if (p.slopes)
                                 s[b][r] -= slope[col] * (float)abs(pos[col] - (tok + g + (r < 2 ? 0 : 8)));
+                            s[b][r] -= mm[b][r & 1];
                         }
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            s[b][r] = fmaf(s[b][r], (r < 2 ? kf0 : kf1) * qk[b][r & 1], -mm[b][r & 1]);
                     }
-                    if (tags || tok + KV_UNIT > all_see) {
+                    if (masked) {
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const int col = b * 8 + 2 * c + (r & 1);
@@ -407,14 +421,10 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                             if (!seen) s[b][r] = -INFINITY;
                         }
                     }
+                    most = fmaxf(fmaxf(most, s[b][0]), fmaxf(fmaxf(s[b][1], s[b][2]), s[b][3]));
                 }
                 // ---- running maxima
-                bool raise = false;
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) raise |= s[b][r] > m[b][r & 1] + M_SLACK;
-                if (__any_sync(0xffffffffu, raise)) {
+                if (__any_sync(0xffffffffu, unset || most > P_SHIFT + M_SLACK)) {
 #pragma unroll
                     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -423,12 +433,17 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                            x = fmaxf(x, m[b][r]);
-                            const float f = ex2(m[b][r] - x);
-                            m[b][r] = x;
-                            l[b][r] *= f;
+                            x -= P_SHIFT;                      // the maximum's rise
+                            const bool fresh = unset >> (2 * b + r) & 1u;
+                            if (fresh ? x > -INFINITY : x > 0.f) {
+                                const float f = fresh ? 0.f : ex2(-x);
+                                unset &= ~(1u << (2 * b + r));
+                                mm[b][r] += x;
+                                s[b][r] -= x, s[b][r + 2] -= x;
+                                l[b][r] *= f;
 #pragma unroll
-                            for (int t = 0; t < MT; ++t) o[b][t][r] *= f, o[b][t][r + 2] *= f;
+                                for (int t = 0; t < MT; ++t) o[b][t][r] *= f, o[b][t][r + 2] *= f;
+                            }
                         }
                 }
                 // ---- weights, and P^T as the B operand
@@ -443,7 +458,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                 for (int b = 0; b < NB; ++b) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        s[b][r] = ex2(s[b][r] - (m[b][r & 1] - P_SHIFT));
+                        s[b][r] = ex2(s[b][r]);
                         l[b][r & 1] += s[b][r];
                     }
                     if constexpr (BITS == 8) {
@@ -452,43 +467,50 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                     pb[b][0] = transpose8(pack_h2(s[b][0], s[b][1]));
                     pb[b][1] = transpose8(pack_h2(s[b][2], s[b][3]));
                 }
-                // ---- the values' exponents, relative to the largest so far
-                int te[4];                     // of tokens 2c, 2c + 1, 2c + 8, 2c + 9
+                // ---- the values' exponents relative to tref, as fp16 powers of two: of
+                // tokens 2c and 2c + 1 in f0, 2c + 8 and 2c + 9 in f1.  In the common
+                // case all lie in [tref - 14, tref + 1] and are put together in place.
+                uint32_t t0, t1;               // T + 127, two to a word
                 if constexpr (BITS == 4) {
                     const uint32_t x = *(const uint32_t *)(un + U::V_EXP + c * 4);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) te[i] = (int)((x >> (8 * i)) & 255u) - 127;
+                    t0 = __byte_perm(x, 0, 0x4140), t1 = __byte_perm(x, 0, 0x4342);
                 } else {
                     const uint2 x = *(const uint2 *)(un + U::V_SCALES + c * 8);
-                    te[0] = (int)((x.x >> 7) & 255u) - 127, te[1] = (int)((x.x >> 23) & 255u) - 127;
-                    te[2] = (int)((x.y >> 7) & 255u) - 127, te[3] = (int)((x.y >> 23) & 255u) - 127;
+                    t0 = (x.x >> 7) & 0x00ff00ffu, t1 = (x.y >> 7) & 0x00ff00ffu;
                 }
-                if (tags || tok + KV_UNIT > sq.kv) {   // a slot without a token adds nothing
+                const uint32_t low = (uint32_t)(tref + 127 - 14) * 0x00010001u;
+                uint32_t f0 = ((t0 - low) << 10) + 0x04000400u, f1 = ((t1 - low) << 10) + 0x04000400u;
+                const bool ends = tags || tok + KV_UNIT > sq.kv;
+                if (ends || __any_sync(0xffffffffu, ((t0 - low) | (t1 - low)) & 0xfff0fff0u)) {
+                    int te[4] = {(int)(t0 & 0xffffu) - 127, (int)(t0 >> 16) - 127,
+                                 (int)(t1 & 0xffffu) - 127, (int)(t1 >> 16) - 127};
+                    if (ends) {                // a slot without a token adds nothing
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int t = 2 * c + (i & 1) + (i >> 1) * 8;
-                        const bool real = tok + t < sq.kv &&
-                                          (!tags || ((const int *)(un + U::BYTES))[t] >= 0);
-                        if (!real) te[i] = -1000;
+                        for (int i = 0; i < 4; ++i) {
+                            const int t = 2 * c + (i & 1) + (i >> 1) * 8;
+                            const bool real = tok + t < sq.kv &&
+                                              (!tags || ((const int *)(un + U::BYTES))[t] >= 0);
+                            if (!real) te[i] = -1000;
+                        }
                     }
+                    int x = max(max(te[0], te[1]), max(te[2], te[3]));
+                    if (__any_sync(0xffffffffu, x > tref + 1)) {
+                        x = max(x, __shfl_xor_sync(0xffffffffu, x, 1));
+                        x = max(max(x, __shfl_xor_sync(0xffffffffu, x, 2)), tref);
+                        const float f = pow2i(max(-126, tref - x));
+                        tref = x;
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+#pragma unroll
+                            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) o[b][t][r] *= f;
+                    }
+                    float tf[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tf[i] = te[i] - tref < -40 ? 0.f : pow2i(te[i] - tref);
+                    f0 = pack_h2(tf[0], tf[1]), f1 = pack_h2(tf[2], tf[3]);
                 }
-                const int tm = max(max(te[0], te[1]), max(te[2], te[3]));
-                if (__any_sync(0xffffffffu, tm > tref)) {
-                    int x = max(tm, __shfl_xor_sync(0xffffffffu, tm, 1));
-                    x = max(max(x, __shfl_xor_sync(0xffffffffu, x, 2)), tref);
-                    const float f = pow2i(max(-126, tref - x));
-                    tref = x;
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-#pragma unroll
-                        for (int t = 0; t < MT; ++t)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) o[b][t][r] *= f;
-                }
-                float tf[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) tf[i] = te[i] - tref < -40 ? 0.f : pow2i(te[i] - tref);
-                const uint32_t f0 = pack_h2(tf[0], tf[1]), f1 = pack_h2(tf[2], tf[3]);
 
                 // ---- O^T += V^T P^T
                 auto values = [&](int mt, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
@@ -519,8 +541,8 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                     for (int gl = 0; gl < GL; ++gl) {
                         const int gr = D == 64 ? g >> 1 : g * GL + gl;
                         const uint32_t x = *(const uint32_t *)(un + U::V_SCALES + (gr * 4 + c) * 4);
-                        const uint32_t s0 = h2mul(__byte_perm(x, 0, 0x4140) * 64u + 0x3c003c00u, f0);
-                        const uint32_t s1 = h2mul(__byte_perm(x, 0, 0x4342) * 64u + 0x3c003c00u, f1);
+                        const uint32_t s0 = h2mul(__byte_perm(x, 0, 0x4140) * 64u + 0x38003800u, f0);
+                        const uint32_t s1 = h2mul(__byte_perm(x, 0, 0x4342) * 64u + 0x38003800u, f1);
                         const uint32_t s04 = h2mul(s0, H2_2_4), s14 = h2mul(s1, H2_2_4);
                         const uint32_t c0 = h2mul(s0, H2_M2_21), c1 = h2mul(s1, H2_M2_21);
                         constexpr int WG = W / GL;             // words of a group
@@ -581,11 +603,12 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
+                if (unset >> (2 * b + r) & 1u) mm[b][r] = NEG;
 #pragma unroll
                 for (int off = 4; off < 32; off <<= 1)
                     l[b][r] += __shfl_xor_sync(0xffffffffu, l[b][r], off);
                 if (g == 0) {
-                    wm[warp * ROWS + b * 8 + 2 * c + r] = m[b][r];
+                    wm[warp * ROWS + b * 8 + 2 * c + r] = mm[b][r];
                     wl[warp * ROWS + b * 8 + 2 * c + r] = l[b][r];
                 }
             }
@@ -602,7 +625,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                 float x = NEG;
 #pragma unroll
                 for (int w = 0; w < NW; ++w) x = fmaxf(x, wm[w * ROWS + b * 8 + 2 * c + r]);
-                const float f = ex2(m[b][r] - x) * ft;
+                const float f = ex2(mm[b][r] - x) * ft;
 #pragma unroll
                 for (int t = 0; t < MT; ++t) o[b][t][r] *= f, o[b][t][r + 2] *= f;
             }
@@ -629,7 +652,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
         const bool whole = cur.unit == 0 && n == cur.units;
         const int64_t slot_floats = attend_slot_floats(ROWS, D);
         float *part = p.partial + ((int64_t)blockIdx.x * 2 + (head_item ? 0 : 1)) * slot_floats;
-        constexpr int UP = BITS == 4 ? 9 : 0;
+        constexpr int UP = BITS == 4 ? 10 : 0;   // values are staged as v 2^-10
         for (int x = tid; x < ROWS * (D / 2); x += NW * 32) {
             const int r = x / (D / 2), d = x % (D / 2) * 2;
             float2 v = make_float2(0.f, 0.f);
@@ -658,7 +681,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                     *(uint32_t *)((__half *)p.out + dst * D + d) = pack_h2(a, b);
                 }
                 if (d == 0 && p.lse)
-                    p.lse[dst] = tot == 0.f ? -INFINITY : (mx - P_SHIFT + log2f(tot)) * 0.69314718055994530942f;
+                    p.lse[dst] = tot == 0.f ? -INFINITY : (mx + log2f(tot)) * 0.69314718055994530942f;
             }
         }
         if (tid == 0 && cur.unit == 0 && !whole) {
@@ -727,7 +750,7 @@ k_attend_join(const AttendParams p, const int rows, const bool bf16) {
             *(uint32_t *)((__half *)p.out + dst * D + d) = pack_h2(v[k] * inv, v[k + 1] * inv);
     }
     if (lane == 0 && p.lse)
-        p.lse[dst] = tot == 0.f ? -INFINITY : (mx - P_SHIFT + log2f(tot)) * 0.69314718055994530942f;
+        p.lse[dst] = tot == 0.f ? -INFINITY : (mx + log2f(tot)) * 0.69314718055994530942f;
 }
 
 constexpr int MIN_PER = 16;   // units of a share, at least: two a warp

@@ -47,8 +47,7 @@ def attend(q, keys, values, blocks, T, kv_len, q_start, *, causal=True, prefix=N
            cap=0.0, slopes=None, tags=None, q_tags=None, n_blocks=None):
     """q [n_q, Hq, D]; keys, values [slots, H, D] (stored values).  Returns out, lse, and
     for the tolerances: weight [n_q, Hq, D] = sum p |v|, top [n_q, Hq] = the largest |v|
-    of the sequence's tokens, reach [n_q, Hq] = the largest |scale| sum_d |q_d k_d| of a seen key (plus 2^-19-sized
-    parts of small groups, sum |q| max|k|), big [n_q, Hq] = sum over seen keys of
+    of the sequence's tokens, reach [n_q, Hq] = the largest |scale| sum_d |q_d k_d| of a seen key (small: sum |q| max |k|), big [n_q, Hq] = sum over seen keys of
     max |v|, z [n_q, Hq] = the largest |z| with the bias' size."""
     n_q, hq, d = q.shape
     h = keys.shape[1]
@@ -99,19 +98,20 @@ def tolerances(r, d, eps_half, bits):
     """Bounds of the error of out and lse, from the kernels' roundings.
 
     Scores: fp32 sums of d exact products and a few factors, (d + 8) 2^-24 of the
-    sum of their sizes; a 4-bit key value in a group below 2^-11 of its row is rounded to
-    2^-19 of the row's largest, a bf16 query value below 2^-14 of its row's to 2^-25 of
+    sum of their sizes; a 4-bit key value v is held as v 2^-9 / 2^T in fp16, where the row's
+    largest is at least 7 2^T, by two roundings of at most 2^-25: 2^-17 of the row's
+    largest; a bf16 query value below 2^-14 of its row's to 2^-25 of
     it; cap, bias and the exponential's argument 2^-21 of their sizes.  A score off by t
     makes a weight off by t relative (both in the sum and in the total).  Weights: fp16,
     2^-11, with 2^-30 of the largest as the smallest step; the exponential 2^-21.
-    Values: 4 bits, 2^-19 of the sequence's largest.  The result is rounded once
+    Values: 4 bits, in the same way but as v 2^-10: 2^-16 of the sequence's largest.  The result is rounded once
     (eps_half of it; fp16 below 2^-14 has steps of 2^-24, so at least 2^-25)."""
     t = (d + 8) * 2.0 ** -24 * r["reach"] + 2.0 ** -21 * (r["z"] + 1)
     if bits == 4:
-        t = t + 2.0 ** -19 * r["small"]
+        t = t + 2.0 ** -17 * r["small"]
     rel = (2 * t + 2.0 ** -11 + 2.0 ** -20)[..., None]
     out = rel * r["weight"] + (2.0 ** -30 * r["big"])[..., None] + eps_half * np.abs(r["out"])
     if bits == 4:
-        out = out + (2.0 ** -19 * r["top"])[..., None]
+        out = out + (2.0 ** -16 * r["top"])[..., None]
     lse = t + 2.0 ** -20 + 2.0 ** -22 * np.abs(np.where(np.isfinite(r["lse"]), r["lse"], 0))
     return out + (2.0 ** -25 if eps_half == 2.0 ** -11 else 1e-30), lse

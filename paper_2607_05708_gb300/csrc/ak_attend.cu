@@ -17,9 +17,10 @@
 //    its steps of 2^-24, 2^-17 of the row's largest.  The row's 2^T goes to the
 //    score; for values into the group's scale, relative to the largest T so far,
 //    and 2^-10: rounded to 2^-16 of the largest value so far.
-//  * a warp works on its own units (16 tokens), brought by bulk copies into its
-//    own ring, with its own running maximum, sum and accumulators: no barrier in
-//    the loop.  The warps of a CTA are joined at the end of an item.
+//  * a warp has its own share of all units (16 tokens), brought by bulk copies
+//    into its own ring across the items' ends, with its own running maximum, sum and
+//    accumulators: no barrier in the loop.  Where a share begins or ends inside an
+//    item, the parts are added up after it, first within the CTA.
 //  * P is fp16, 2^6 p: weights down to 2^-20 of the largest so far keep 11 bits; sums,
 //    maxima and accumulators are fp32.  The maximum is raised only when a
 //    score exceeds it by 2^8, so that the accumulators are rarely rescaled.
@@ -101,58 +102,79 @@ struct Narrow {
     using U = KvUnit<BITS, D>;
     static constexpr int ROWS = 8 * NB;
     static constexpr int STAGE = U::BYTES + 64;          // a unit and its tags
-    static constexpr int SUM = NW / 2 * ROWS * D * 4;    // half of the warps' accumulators
-    static constexpr int Q_ROW = D * 2 + 32;
-    static constexpr int SMALL = ROWS * Q_ROW + ROWS * 5 * 4 + NW * ROWS * 2 * 4 + NW * 4 + 34 * 8 + 64;
-    static constexpr int WANT = (110 * 1024 - SUM - SMALL) / (NW * (STAGE + 16));
-    static constexpr int MOST = (220 * 1024 - SUM - SMALL) / (NW * (STAGE + 16));
+    static constexpr int ACC = ROWS * D * 4;             // a warp's accumulators
+    static constexpr int SMALL = NW * ROWS * 4 * 4 + 2 * NW * ROWS * 8 + (NW * 32 + 1) * 8 + 2 * NW * 48 + 256;
+    static constexpr int WANT = (225 * 512 - NW * ACC - SMALL) / (NW * (STAGE + 16));
+    static constexpr int MOST = (225 * 1024 - NW * ACC - SMALL) / (NW * (STAGE + 16));
     // two CTAs an SM where three stages of a unit leave room for it
     static constexpr bool TWO = WANT >= 3 && NB == 1 && D <= 128;
     static constexpr int NS_ = TWO ? WANT : MOST;
     static constexpr int NS = NS_ > 8 ? 8 : NS_;
     static_assert(NS >= 2, "a ring of two units");
-    static constexpr int RING = NW * NS * STAGE;
-    static constexpr int SMEM = RING + NW * NS * 12 + SUM + SMALL;
-    static constexpr bool Q_REG = D / 16 * 2 * NB <= 32;
+    static constexpr int RING = NS * STAGE;              // of a warp; at the end, its accumulators
+    static_assert(RING >= ACC, "the last item's accumulators fit the ring");
+    static constexpr int SMEM = NW * (RING + NS * 16) + NW * ACC + SMALL;
 };
 
-// The query rows of a tile, as fp16 in the order of the B fragments: row r,
-// dims c D/4 + 4 kk + {0..3} at ((kk * 4 + c) * 4) halves.  bf16 rows are scaled by
-// a power of two to a largest magnitude in [1, 2): exact but for values below
-// 2^-14 of it.
+// A warp's part of an item, left for the joining of the CTA's warps.
+struct Entry {
+    int64_t start;                             // of the item, in all steps
+    int seq, head, tile, unit, n, units, tref, pad;
+};
+static_assert(sizeof(Entry) <= 48, "Narrow::SMALL");
+
+// A lane's part of the B fragments of a tile's query rows: row g of each 8, dims
+// c D/4 + 4 kk + {0..3}.  bf16 rows are scaled by a power of two to a largest
+// magnitude in [1, 2): exact but for values below 2^-14 of it.  Returns 1 / the scale.
 template <int D>
-__device__ __forceinline__ float load_query(const AttendParams &p, bool bf16, int64_t at,
-                                            unsigned char *dst) {
-    const int lane = threadIdx.x & 31;
-    constexpr int N = D / 32;                  // values a lane loads
-    float x[N];
-    if (bf16) {
-        const __nv_bfloat16 *src = (const __nv_bfloat16 *)p.q + at + lane * N;
+__device__ __forceinline__ float load_query(const AttendParams &p, bool bf16, int64_t at, bool real,
+                                            uint32_t (&f)[D / 16][2]) {
+    const int c = threadIdx.x & 3;
+    uint16_t raw[D / 4];
+    const uint16_t *src = (const uint16_t *)p.q + at + c * (D / 4);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = __bfloat162float(src[i]);
-    } else {
-        const __half *src = (const __half *)p.q + at + lane * N;
+    for (int i = 0; i < D / 4; ++i) raw[i] = 0;
+    if (real) {
+        if (p.q_wide) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = __half2float(src[i]);
+            for (int i = 0; i < D / 32; ++i) *(uint4 *)(raw + 8 * i) = *(const uint4 *)(src + 8 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < D / 4; ++i) raw[i] = src[i];
+        }
     }
-    int e = 0;
-    if (bf16) {
-        float a = 0.f;
+    if (!bf16) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) a = fmaxf(a, fabsf(x[i]));
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-        e = max(-126, min(126, (int)(__float_as_uint(a) >> 23) - 127));
-        const float f = pow2i(-e);
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] *= f;
+        for (int k = 0; k < D / 16; ++k) {
+            f[k][0] = raw[4 * k] | (uint32_t)raw[4 * k + 1] << 16;
+            f[k][1] = raw[4 * k + 2] | (uint32_t)raw[4 * k + 3] << 16;
+        }
+        return 1.f;
     }
+    float a = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; i += 2) {
-        const int d = lane * N + i, c = d / (D / 4), kk = d % (D / 4) / 4;
-        *(uint32_t *)(dst + ((kk * 4 + c) * 4 + (d & 3)) * 2) = pack_h2(x[i], x[i + 1]);
+    for (int i = 0; i < D / 4; ++i) a = fmaxf(a, fabsf(bf16_to_f32(raw[i])));
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
+    const int e = max(-126, min(126, (int)(__float_as_uint(a) >> 23) - 127));
+    const float by = pow2i(-e);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+        f[k][0] = pack_h2(bf16_to_f32(raw[4 * k]) * by, bf16_to_f32(raw[4 * k + 1]) * by);
+        f[k][1] = pack_h2(bf16_to_f32(raw[4 * k + 2]) * by, bf16_to_f32(raw[4 * k + 3]) * by);
     }
-    return scale2(1.f, e);
+    return pow2i(e);
+}
+
+// Two adjacent values of a result row, and its log-sum-exp.
+__device__ __forceinline__ void store_pair(const AttendParams &p, bool bf16, int64_t at, float a, float b) {
+    if (bf16)
+        *(__nv_bfloat162 *)((__nv_bfloat16 *)p.out + at) = __floats2bfloat162_rn(a, b);
+    else
+        *(uint32_t *)((__half *)p.out + at) = pack_h2(a, b);
+}
+__device__ __forceinline__ float lse_of(float m, float total) {
+    return total == 0.f ? -INFINITY : (m + log2f(total)) * 0.69314718055994530942f;
 }
 
 template <int BITS, int D, int NB>
@@ -161,131 +183,128 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
     using C = Narrow<BITS, D, NB>;
     using U = typename C::U;
     constexpr int ROWS = C::ROWS, NS = C::NS, MT = D / 16;
+    constexpr int UP = BITS == 4 ? 10 : 0;     // values are staged as v 2^-10
     extern __shared__ __align__(128) unsigned char smem[];
-    unsigned char *at = smem + C::RING;
-    float *sum = (float *)at;                             at += C::SUM;
-    unsigned char *qs = at;                               at += ROWS * C::Q_ROW;
-    int64_t *scratch = (int64_t *)at;                     at += 34 * 8;
-    uint64_t *bars = (uint64_t *)at;                      at += NW * NS * 8;
-    int *meta = (int *)at;                                at += NW * NS * 4;
-    float *qfac = (float *)at;                            at += ROWS * 4;
-    float *slope = (float *)at;                           at += ROWS * 4;
-    int *limit = (int *)at;                               at += ROWS * 4;
-    int *pos = (int *)at;                                 at += ROWS * 4;
-    int *qtag = (int *)at;                                at += ROWS * 4;
-    float *wm = (float *)at;                              at += NW * ROWS * 4;
-    float *wl = (float *)at;                              at += NW * ROWS * 4;
-    int *wt = (int *)at;
-
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, c = lane & 3;
-    unsigned char *ring = smem + warp * NS * C::STAGE;
-    uint64_t *bar = bars + warp * NS;
-    int *mt_ = meta + warp * NS;
+    unsigned char *at = smem + NW * C::RING;
+    float *heads = (float *)at;                           at += NW * C::ACC;
+    Entry *entries = (Entry *)at;                         at += 2 * NW * sizeof(Entry);
+    int64_t *prefix = (int64_t *)at;                      at += (NW * 32 + 1) * 8;
+    uint64_t *bar = (uint64_t *)at + warp * NS;           at += NW * NS * 8;
+    int *listed = (int *)at + warp * NS;                  at += NW * NS * 4;
+    float *em = (float *)at;                              at += 2 * NW * ROWS * 4;   // of entries
+    float *el = (float *)at;                              at += 2 * NW * ROWS * 4;
+    float *slope = (float *)at + warp * ROWS;             at += NW * ROWS * 4;       // of rows
+    int *limit = (int *)at + warp * ROWS;                 at += NW * ROWS * 4;
+    int *pos = (int *)at + warp * ROWS;                   at += NW * ROWS * 4;
+    int *qtag = (int *)at + warp * ROWS;
+    unsigned char *ring = smem + warp * C::RING;
+
     if (lane == 0)
         for (int i = 0; i < NS; ++i) mbar_init(bar + i, 1);
     mbar_fence_init();
-    __syncthreads();
-
-    int64_t first, count, per;
-    AttendCursor cur;
+    if (lane < 2) entries[2 * warp + lane].seq = -1;
     if (tid == 0) p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
-    if (!attend_plan(p, ROWS, KV_UNIT, lo, hi, min_per, scratch, first, count, per, cur)) return;
+    attend_sums(p, ROWS, KV_UNIT, lo, hi, prefix);
+    const int64_t total = prefix[NW * 32], workers = (int64_t)gridDim.x * NW;
+    const int64_t per = max((int64_t)min_per, (total + workers - 1) / workers);
+    const int64_t first = per * (blockIdx.x * NW + warp);
+    int left = (int)max((int64_t)0, min(per, total - first));   // steps of this warp
+
+    // What is needed to fetch: the item that is being fetched, up to NS units ahead of
+    // the one that is worked on.
+    struct Place {
+        int64_t unit;                          // of the cache, -1: not listed
+        int slots;                             // the unit's slots / 16
+    } batch = {-1, 0};
+    AttendCursor cur, ahead;
+    int fetch_left = left, fetch_n = 0, fetch_i = 0, fetch_stage = 0;
+    const bool tags = p.tags != nullptr, heavy = p.cap > 0.f || p.slopes;
+    auto issue = [&]() {
+        if (fetch_left <= 0) return;
+        if (fetch_i == fetch_n) {              // the next item
+            attend_next(p, ROWS, KV_UNIT, lo, hi, ahead);
+            fetch_n = min(ahead.units, fetch_left), fetch_i = 0;
+        }
+        if ((fetch_i & 31) == 0) {             // lane x looks up the x-th unit from here
+            batch = {-1, 0};
+            const int u = ahead.unit + fetch_i + lane;
+            if (fetch_i + lane < fetch_n && u < (ahead.q.kv + KV_UNIT - 1) / KV_UNIT) {
+                const int b = u / p.per_block, w = u - b * p.per_block;
+                const int64_t id = p.blocks[ahead.seq * p.max_blocks + b];
+                if (id >= 0 && id < p.n_blocks)
+                    batch = {(id * p.heads + ahead.head) * p.per_block + w, (int)id * p.per_block + w};
+                else if (id != -1)
+                    set_status(p.status, AKASHIC_EDEVICE);
+            }
+        }
+        const int64_t u = __shfl_sync(0xffffffffu, batch.unit, fetch_i & 31);
+        const int sl = tags ? __shfl_sync(0xffffffffu, batch.slots, fetch_i & 31) : 0;
+        if (lane == 0) {
+            uint64_t *b = bar + fetch_stage;
+            unsigned char *dst = ring + fetch_stage * C::STAGE;
+            listed[fetch_stage] = u >= 0;
+            if (u >= 0) {
+                mbar_expect_tx(b, U::BYTES + (tags ? 64 : 0));
+                bulk_load(dst, p.cache + u * U::BYTES, U::BYTES, b);
+                if (tags) bulk_load(dst + U::BYTES, p.tags + (int64_t)sl * 16, 64, b);
+            } else {
+                mbar_arrive(b);
+            }
+        }
+        fetch_stage = fetch_stage + 1 == NS ? 0 : fetch_stage + 1;
+        ++fetch_i, --fetch_left;
+    };
+    if (left > 0) {
+        cur = attend_find(p, ROWS, KV_UNIT, lo, hi, prefix, first);
+        ahead = cur;
+        fetch_n = min(ahead.units - ahead.unit, left);
+        for (int i = 0; i < NS; ++i) issue();
+    }
 
     bool ok = true;                            // no wait of this warp has expired
-    uint32_t used = 0;                         // stages of the ring filled so far
-    const bool tags = p.tags != nullptr, heavy = p.cap > 0.f || p.slopes;
+    uint32_t stage = 0, phase = 0;
     const float cap_l = p.cap * LOG2E_F, cap_in = p.cap > 0.f ? 2.f / p.cap : 0.f;
-    int64_t left = count;
-    bool head_item = true;                     // the share's first item
+    float o[NB][MT][4], mm[NB][2], l[NB][2];
+    int tref = -127;
+    int64_t done = 0;
+    bool tail = false;                         // the accumulators hold the last item's part
     while (left > 0) {
-        const int n = (int)min((int64_t)(cur.units - cur.unit), left);
+        const int n = min(cur.units - cur.unit, left);
         const AttendSeq sq = cur.q;
         const int row_first = cur.tile * ROWS, rows = min(ROWS, sq.nq * p.group - row_first);
 
-        // ---- this warp's units of the item: unit + warp, + NW, ...
-        const int mine = (n - warp + NW - 1) / NW;
-        const int64_t *list = p.blocks + cur.seq * p.max_blocks;
-        struct Place {
-            int64_t unit;                      // of the cache, -1: not listed
-            int slots;                         // the unit's slots / 16
-        };
-        // Lane x looks up the warp's units x, x + 32, ..., one batch ahead.
-        auto place = [&](int i) -> Place {
-            if (i >= mine) return {-1, 0};
-            const int u = cur.unit + warp + i * NW, b = u / p.per_block;
-            if (u >= (sq.kv + KV_UNIT - 1) / KV_UNIT) return {-1, 0};   // an item without keys
-            const int64_t id = list[b];
-            if (id < 0 || id >= p.n_blocks) {
-                if (id != -1) set_status(p.status, AKASHIC_EDEVICE);
-                return {-1, 0};
-            }
-            const int w = u - b * p.per_block;
-            return {(id * p.heads + cur.head) * p.per_block + w, (int)id * p.per_block + w};
-        };
-        Place batch = place(lane), next = place(32 + lane);
-        const uint32_t base = used;
-        auto issue = [&](int i) {
-            if (i >= mine) return;
-            if (i && (i & 31) == 0) {
-                batch = next;
-                next = place(i + 32 + lane);
-            }
-            const int64_t u = __shfl_sync(0xffffffffu, batch.unit, i & 31);
-            const int sl = tags ? __shfl_sync(0xffffffffu, batch.slots, i & 31) : 0;
-            if (lane == 0) {
-                const int st = (base + i) % NS;
-                mt_[st] = u >= 0;
-                if (u >= 0) {
-                    mbar_expect_tx(bar + st, U::BYTES + (tags ? 64 : 0));
-                    bulk_load(ring + st * C::STAGE, p.cache + u * U::BYTES, U::BYTES, bar + st);
-                    if (tags)
-                        bulk_load(ring + st * C::STAGE + U::BYTES, p.tags + (int64_t)sl * 16, 64, bar + st);
-                } else {
-                    mbar_arrive(bar + st);
-                }
-            }
-        };
-        if (ok)
-            for (int i = 0; i < NS; ++i) issue(i);
-
         // ---- the query rows
-        for (int r = warp; r < ROWS; r += NW) {
-            float f = 0.f;
-            int i = 0, hd = 0;
-            if (r < rows) {
-                i = (row_first + r) / p.group, hd = cur.head * p.group + (row_first + r) % p.group;
-                f = load_query<D>(p, bf16, (sq.row0 + i) * p.q_row + hd * p.q_head, qs + r * C::Q_ROW);
-            } else {
-                for (int d = lane; d < D / 2; d += 32) ((uint32_t *)(qs + r * C::Q_ROW))[d] = 0;
-            }
-            if (lane == 0) {
-                qfac[r] = f * p.scale * LOG2E_F * (BITS == 4 ? 512.f : 1.f);
+        __syncwarp();
+        float f_own = 0.f;                     // lane r: row r's factor
+        uint32_t qf[NB][MT][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int r = b * 8 + g, row = row_first + r;
+            const int i = r < rows ? row / p.group : 0;
+            const int hd = cur.head * p.group + (r < rows ? row - i * p.group : 0);
+            const float f = load_query<D>(p, bf16, (sq.row0 + i) * p.q_row + hd * p.q_head, r < rows, qf[b]);
+            if (c == 0) {
                 slope[r] = r < rows && p.slopes ? p.slopes[hd] * LOG2E_F : 0.f;
                 limit[r] = r < rows ? attend_limit(p, sq, i) : sq.kv;
                 pos[r] = sq.kv - sq.nq + i;
                 qtag[r] = r < rows && p.q_tags ? p.q_tags[sq.row0 + i] : -1;
             }
+            const float x = __shfl_sync(0xffffffffu, f, (lane & 7) * 4);
+            if (lane >> 3 == b) f_own = x;
         }
-        __syncthreads();
-        uint32_t qf[C::Q_REG ? NB : 1][C::Q_REG ? MT : 1][2];
-        if constexpr (C::Q_REG) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int k = 0; k < MT; ++k) {
-                    const uint2 x = *(const uint2 *)(qs + (b * 8 + g) * C::Q_ROW + (k * 4 + c) * 8);
-                    qf[b][k][0] = x.x, qf[b][k][1] = x.y;
-                }
-        }
+        __syncwarp();
         float qk[NB][2];
 #pragma unroll
         for (int b = 0; b < NB; ++b)
-            qk[b][0] = qfac[b * 8 + 2 * c], qk[b][1] = qfac[b * 8 + 2 * c + 1];
-        const int all_see = limit[0];          // keys below it are seen by every row
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+                qk[b][r] = __shfl_sync(0xffffffffu, f_own, b * 8 + 2 * c + r) * p.scale * LOG2E_F *
+                           (BITS == 4 ? 512.f : 1.f);
+        const int safe = limit[0] - KV_UNIT;   // keys below limit[0] are seen by every row
 
-        float o[NB][MT][4], mm[NB][2], l[NB][2];
-        int tref = -127;
+        tref = -127;
         uint32_t unset = (1u << (2 * NB)) - 1u;    // rows that have not seen a key yet: mm = 0
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
@@ -294,31 +313,27 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
             mm[b][0] = mm[b][1] = 0.f, l[b][0] = l[b][1] = 0.f;
         }
 
-        for (int it = 0; ok && it < mine; ++it) {
-            const int st = (base + it) % NS;
-            if (!mbar_wait(bar + st, ((base + it) / NS) & 1, p.status)) {
-                ok = false;                    // its copies still land: wait for the rest
-                for (int k = it + 1; k < min(mine, it + NS); ++k)
-                    mbar_wait(bar + (base + k) % NS, ((base + k) / NS) & 1, p.status);
+        int tok = cur.unit * KV_UNIT;
+        for (int it = 0; ok && it < n; ++it, tok += KV_UNIT) {
+            if (!mbar_wait(bar + stage, phase, p.status)) {
+                ok = false;                    // the other copies still land: wait for them
+                const int out = min(left - it, NS);
+                for (int k = 1; k < out; ++k) {
+                    stage = stage + 1 == NS ? 0 : stage + 1;
+                    if (stage == 0) phase ^= 1;
+                    mbar_wait(bar + stage, phase, p.status);
+                }
                 break;
             }
-            const unsigned char *un = ring + st * C::STAGE;
-            const int tok = (cur.unit + warp + it * NW) * KV_UNIT;
-            if (mt_[st]) {
+            const unsigned char *un = ring + stage * C::STAGE;
+            if (listed[stage]) {
                 // ---- S^T = K Q^T
                 float s[NB][4];
 #pragma unroll
                 for (int b = 0; b < NB; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
                 auto keys = [&](int kk, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-                        if constexpr (C::Q_REG) {
-                            mma16(s[b], a0, a1, a2, a3, qf[b][kk][0], qf[b][kk][1]);
-                        } else {
-                            const uint2 x = *(const uint2 *)(qs + (b * 8 + g) * C::Q_ROW + (kk * 4 + c) * 8);
-                            mma16(s[b], a0, a1, a2, a3, x.x, x.y);
-                        }
-                    }
+                    for (int b = 0; b < NB; ++b) mma16(s[b], a0, a1, a2, a3, qf[b][kk][0], qf[b][kk][1]);
                 };
                 float kf0, kf1;                // scale of the keys of tokens g and g + 8
                 if constexpr (BITS == 4) {
@@ -391,7 +406,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                     tag0 = ((const int *)(un + U::BYTES))[g];
                     tag1 = ((const int *)(un + U::BYTES))[g + 8];
                 }
-                const bool masked = tags || tok + KV_UNIT > all_see;
+                const bool masked = tags || tok > safe;
                 float most = NEG;
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
@@ -480,11 +495,10 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                 }
                 const uint32_t low = (uint32_t)(tref + 127 - 14) * 0x00010001u;
                 uint32_t f0 = ((t0 - low) << 10) + 0x04000400u, f1 = ((t1 - low) << 10) + 0x04000400u;
-                const bool ends = tags || tok + KV_UNIT > sq.kv;
-                if (ends || __any_sync(0xffffffffu, ((t0 - low) | (t1 - low)) & 0xfff0fff0u)) {
+                if (masked || __any_sync(0xffffffffu, ((t0 - low) | (t1 - low)) & 0xfff0fff0u)) {
                     int te[4] = {(int)(t0 & 0xffffu) - 127, (int)(t0 >> 16) - 127,
                                  (int)(t1 & 0xffffu) - 127, (int)(t1 >> 16) - 127};
-                    if (ends) {                // a slot without a token adds nothing
+                    if (masked) {              // a slot without a token adds nothing
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const int t = 2 * c + (i & 1) + (i >> 1) * 8;
@@ -593,12 +607,12 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                 }
             }
             __syncwarp();                      // the stage has been read
-            issue(it + NS);
+            issue();
+            stage = stage + 1 == NS ? 0 : stage + 1;
+            if (stage == 0) phase ^= 1;
         }
-        if (mine > 0) used = base + mine;
 
-        // ---- join the warps: rescale to the item's maxima, half of them
-        // hand their accumulators to the other half, which then add up in order
+        // ---- the item, or this warp's part of it, is done
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -607,153 +621,168 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
 #pragma unroll
                 for (int off = 4; off < 32; off <<= 1)
                     l[b][r] += __shfl_xor_sync(0xffffffffu, l[b][r], off);
-                if (g == 0) {
-                    wm[warp * ROWS + b * 8 + 2 * c + r] = mm[b][r];
-                    wl[warp * ROWS + b * 8 + 2 * c + r] = l[b][r];
-                }
             }
-        if (lane == 0) wt[warp] = tref;
-        __syncthreads();
-        int tmax = -127;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) tmax = max(tmax, wt[w]);
-        const float ft = pow2i(max(-126, tref - tmax));
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float x = NEG;
-#pragma unroll
-                for (int w = 0; w < NW; ++w) x = fmaxf(x, wm[w * ROWS + b * 8 + 2 * c + r]);
-                const float f = ex2(mm[b][r] - x) * ft;
-#pragma unroll
-                for (int t = 0; t < MT; ++t) o[b][t][r] *= f, o[b][t][r + 2] *= f;
-            }
-        float *slot = sum + (warp & (NW / 2 - 1)) * ROWS * D;
-        auto each = [&](auto &&fn) {
+        if (n == cur.units) {                  // whole: written from here
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int t = 0; t < MT; ++t)
+                for (int r = 0; r < 2; ++r) {
+                    const int x = b * 8 + 2 * c + r, row = row_first + x;
+                    if (x >= rows) continue;
+                    const int i = row / p.group;
+                    const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + cur.head * p.group + (row - i * p.group);
+                    const float inv = l[b][r] > 0.f ? 1.f / l[b][r] : l[b][r];   // a NaN stays one
+                    const float up = scale2(1.f, (tref + UP) / 2), up2 = scale2(1.f, (tref + UP) - (tref + UP) / 2);
 #pragma unroll
-                    for (int r = 0; r < 2; ++r)
-                        fn((float2 *)(slot + (b * 8 + 2 * c + r) * D + g * (D / 8) + 2 * t), o[b][t][r],
-                           o[b][t][r + 2]);
-        };
-        if (warp >= NW / 2) each([](float2 *a, float x, float y) { *a = make_float2(x, y); });
-        __syncthreads();
-        if (warp < NW / 2)
-            each([](float2 *a, float x, float y) {
-                const float2 v = *a;
-                *a = make_float2(v.x + x, v.y + y);
-            });
-        __syncthreads();
-        // ---- whole items are written, others left for the joining kernel
-        const bool whole = cur.unit == 0 && n == cur.units;
-        const int64_t slot_floats = attend_slot_floats(ROWS, D);
-        float *part = p.partial + ((int64_t)blockIdx.x * 2 + (head_item ? 0 : 1)) * slot_floats;
-        constexpr int UP = BITS == 4 ? 10 : 0;   // values are staged as v 2^-10
+                    for (int t = 0; t < MT; ++t)
+                        store_pair(p, bf16, dst * D + g * (D / 8) + 2 * t, o[b][t][r] * inv * up * up2,
+                                   o[b][t][r + 2] * inv * up * up2);
+                    if (g == 0 && p.lse) p.lse[dst] = lse_of(mm[b][r], l[b][r]);
+                }
+        } else {
+            // the share begins or ends inside the item.  A part at the share's
+            // beginning leaves the registers now, one at its end after the loop.
+            tail = done != 0;
+            const int e = 2 * warp + (tail ? 1 : 0);
+            if (lane == 0)
+                entries[e] = Entry{first + done - cur.unit, cur.seq, cur.head, cur.tile, cur.unit, n, cur.units, tref, 0};
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    if (g == 0) em[e * ROWS + b * 8 + 2 * c + r] = mm[b][r], el[e * ROWS + b * 8 + 2 * c + r] = l[b][r];
+                    if (!tail)
+#pragma unroll
+                        for (int t = 0; t < MT; ++t)
+                            *(float2 *)(heads + (warp * ROWS + b * 8 + 2 * c + r) * D + g * (D / 8) + 2 * t) =
+                                make_float2(o[b][t][r], o[b][t][r + 2]);
+                }
+        }
+        left -= n, done += n;
+        if (left > 0) attend_next(p, ROWS, KV_UNIT, lo, hi, cur);
+    }
+    if (tail) {
+        // nothing is in flight any more: the ring takes the last item's part
+        float *own = (float *)ring;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+                    *(float2 *)(own + (b * 8 + 2 * c + r) * D + g * (D / 8) + 2 * t) =
+                        make_float2(o[b][t][r], o[b][t][r + 2]);
+    }
+    __syncthreads();
+    // ---- parts of one item by several warps (neighbours in the order) are added up
+    for (int e0 = 0; e0 < 2 * NW;) {
+        const Entry a = entries[e0];
+        if (a.seq < 0) {
+            ++e0;
+            continue;
+        }
+        int e1 = e0 + 1, end = a.unit + a.n, tmax = a.tref;
+        for (int e = e1; e < 2 * NW; ++e) {
+            const Entry &x = entries[e];
+            if (x.seq < 0) continue;
+            if (x.start != a.start) break;
+            e1 = e + 1, end = x.unit + x.n, tmax = max(tmax, x.tref);
+        }
+        const AttendSeq sq = attend_seq(p, a.seq);
+        const int row_first = a.tile * ROWS, rows = min(ROWS, sq.nq * p.group - row_first);
+        const bool whole = a.unit == 0 && end == a.units;
+        float *part = p.partial + ((int64_t)blockIdx.x * 2 + (a.unit == 0)) * attend_slot_floats(ROWS, D);
         for (int x = tid; x < ROWS * (D / 2); x += NW * 32) {
             const int r = x / (D / 2), d = x % (D / 2) * 2;
-            float2 v = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < NW / 2; ++w) {
-                const float2 y = *(const float2 *)(sum + (w * ROWS + r) * D + d);
-                v.x += y.x, v.y += y.y;
+            float mx = NEG, tot = 0.f, v0 = 0.f, v1 = 0.f;
+            for (int e = e0; e < e1; ++e)
+                if (entries[e].seq >= 0) mx = fmaxf(mx, em[e * ROWS + r]);
+            for (int e = e0; e < e1; ++e) {
+                if (entries[e].seq < 0) continue;
+                const float f = ex2(em[e * ROWS + r] - mx), ft = f * pow2i(max(-126, entries[e].tref - tmax));
+                const float *acc = e & 1 ? (const float *)(smem + (e >> 1) * C::RING) : heads + (e >> 1) * ROWS * D;
+                const float2 y = *(const float2 *)(acc + r * D + d);
+                tot += f * el[e * ROWS + r];
+                v0 += ft * y.x, v1 += ft * y.y;
             }
-            float mx = NEG, tot = 0.f;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) mx = fmaxf(mx, wm[w * ROWS + r]);
-#pragma unroll
-            for (int w = 0; w < NW; ++w) tot += wl[w * ROWS + r] * ex2(wm[w * ROWS + r] - mx);
             if (!whole) {
-                *(float2 *)(part + r * D + d) =
-                    make_float2(scale2(v.x, tmax + UP), scale2(v.y, tmax + UP));
+                *(float2 *)(part + r * D + d) = make_float2(scale2(v0, tmax + UP), scale2(v1, tmax + UP));
                 if (d == 0) part[ROWS * D + r] = mx, part[ROWS * D + ROWS + r] = tot;
             } else if (r < rows) {
-                const float inv = tot > 0.f ? 1.f / tot : tot;   // a NaN stays one
-                const int i = (row_first + r) / p.group, hd = cur.head * p.group + (row_first + r) % p.group;
-                const int64_t dst = ((int64_t)(sq.row0 + i) * p.q_heads + hd);
-                const float a = scale2(v.x * inv, tmax + UP), b = scale2(v.y * inv, tmax + UP);
-                if (bf16) {
-                    *(__nv_bfloat162 *)((__nv_bfloat16 *)p.out + dst * D + d) = __floats2bfloat162_rn(a, b);
-                } else {
-                    *(uint32_t *)((__half *)p.out + dst * D + d) = pack_h2(a, b);
-                }
-                if (d == 0 && p.lse)
-                    p.lse[dst] = tot == 0.f ? -INFINITY : (mx + log2f(tot)) * 0.69314718055994530942f;
+                const float inv = tot > 0.f ? 1.f / tot : tot;
+                const int row = row_first + r, i = row / p.group;
+                const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + a.head * p.group + (row - i * p.group);
+                store_pair(p, bf16, dst * D + d, scale2(v0 * inv, tmax + UP), scale2(v1 * inv, tmax + UP));
+                if (d == 0 && p.lse) p.lse[dst] = lse_of(mx, tot);
             }
         }
-        if (tid == 0 && cur.unit == 0 && !whole) {
+        if (tid == 0 && a.unit == 0 && !whole)
             // the item begins here and ends in the share of a later CTA
-            const int64_t end = first + (count - left) + cur.units;
-            p.joins[blockIdx.x] = make_int4(cur.seq, cur.head, cur.tile,
-                                            ((int)((end - 1) / per) << 1) | (head_item ? 0 : 1));
-        }
-        left -= n;
-        head_item = false;
-        if (left > 0) {
-            attend_next(p, ROWS, KV_UNIT, lo, hi, cur);
-            __syncthreads();                   // the item's rows in shared memory are free
-        }
+            p.joins[blockIdx.x] = make_int4(a.seq, a.head, a.tile, (int)((a.start + a.units - 1) / per / NW));
+        e0 = e1;
     }
 }
 
-// One warp a row of an item whose steps lay in several CTAs: the slots in the
-// order of the CTAs.
+// Items whose steps lay in several CTAs: the slots in the order of the CTAs, one CTA
+// an item.  The slots' factors first, then the sums, eight slots in flight.
+constexpr int JOIN_FACTORS = 8192;
 template <int D>
 __global__ void __launch_bounds__(256)
 k_attend_join(const AttendParams p, const int rows, const bool bf16) {
+    __shared__ float factor[JOIN_FACTORS];     // [rows of a pass][slot]
+    __shared__ float inv[128];
     griddep_wait();
     const int4 j = p.joins[blockIdx.x];
     if (j.x < 0) return;
-    const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const AttendSeq sq = attend_seq(p, j.x);
-    const int row = j.z * rows + r;
-    if (r >= rows || row >= sq.nq * p.group) return;
-    const int last = j.w >> 1;
+    const int real = min(rows, sq.nq * p.group - j.z * rows);
+    const int parts = j.w - (int)blockIdx.x + 1;
     const int64_t floats = attend_slot_floats(rows, D);
-    const float *first = p.partial + ((int64_t)blockIdx.x * 2 + (j.w & 1)) * floats;
-    auto slot = [&](int k) {   // of the k-th CTA after the first
-        return k == 0 ? first : p.partial + (int64_t)(blockIdx.x + k) * 2 * floats;
-    };
-    const int parts = last - (int)blockIdx.x + 1;
-    float mx = NEG;
-    for (int k = lane; k < parts; k += 32) mx = fmaxf(mx, slot(k)[rows * D + r]);
+    const float *base = p.partial + (int64_t)blockIdx.x * 2 * floats;
+    auto slot = [&](int k) { return base + (k ? (int64_t)k * 2 : 1) * floats; };
+    const int pass = max(1, min(128, JOIN_FACTORS / parts));     // parts <= the grid's CTAs
+    for (int r0 = 0; r0 < real; r0 += pass) {
+        const int r1 = min(real, r0 + pass);
+        for (int r = r0 + warp; r < r1; r += 8) {
+            float mx = NEG, tot = 0.f;
+            for (int k = lane; k < parts; k += 32) mx = fmaxf(mx, slot(k)[rows * D + r]);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    constexpr int N = D / 32;
-    float v[N], tot = 0.f;
+            for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            for (int k = lane; k < parts; k += 32) {
+                const float f = ex2(slot(k)[rows * D + r] - mx);
+                factor[(r - r0) * parts + k] = f;
+                tot += f * slot(k)[rows * D + rows + r];
+            }
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = 0.f;
-#pragma unroll 4
-    for (int k = 0; k < parts; ++k) {
-        const float *s = slot(k);
-        const float f = ex2(s[rows * D + r] - mx);
-        tot += f * s[rows * D + rows + r];
-#pragma unroll
-        for (int i = 0; i < N; i += 2) {
-            const float2 y = *(const float2 *)(s + r * D + i * 32 + lane * 2);
-            v[i] += f * y.x, v[i + 1] += f * y.y;
+            for (int o = 16; o > 0; o >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, o);
+            if (lane == 0) {
+                inv[r - r0] = tot > 0.f ? 1.f / tot : tot;
+                const int row = j.z * rows + r, i = row / p.group;
+                if (p.lse)
+                    p.lse[(int64_t)(sq.row0 + i) * p.q_heads + j.y * p.group + (row - i * p.group)] = lse_of(mx, tot);
+            }
         }
+        __syncthreads();
+        for (int x = tid; x < (r1 - r0) * (D / 4); x += 256) {
+            const int r = x / (D / 4), d = x % (D / 4) * 4;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+            for (int k = 0; k < parts; ++k) {
+                const float f = factor[r * parts + k];
+                const float4 y = *(const float4 *)(slot(k) + (r0 + r) * D + d);
+                v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
+            }
+            const int row = j.z * rows + r0 + r, i = row / p.group;
+            const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + j.y * p.group + (row - i * p.group);
+            store_pair(p, bf16, dst * D + d, v.x * inv[r], v.y * inv[r]);
+            store_pair(p, bf16, dst * D + d + 2, v.z * inv[r], v.w * inv[r]);
+        }
+        __syncthreads();
     }
-    const float inv = tot > 0.f ? 1.f / tot : tot;
-    const int i = row / p.group, hd = j.y * p.group + row % p.group;
-    const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + hd;
-#pragma unroll
-    for (int k = 0; k < N; k += 2) {
-        const int d = k * 32 + lane * 2;
-        if (bf16)
-            *(__nv_bfloat162 *)((__nv_bfloat16 *)p.out + dst * D + d) =
-                __floats2bfloat162_rn(v[k] * inv, v[k + 1] * inv);
-        else
-            *(uint32_t *)((__half *)p.out + dst * D + d) = pack_h2(v[k] * inv, v[k + 1] * inv);
-    }
-    if (lane == 0 && p.lse)
-        p.lse[dst] = tot == 0.f ? -INFINITY : (mx + log2f(tot)) * 0.69314718055994530942f;
 }
 
-constexpr int MIN_PER = 16;   // units of a share, at least: two a warp
+constexpr int MIN_PER = 2;    // units of a warp's share, at least
 
 template <int BITS, int D, int NB>
 cudaError_t run_narrow(const AttendParams &p, int dtype, int ctas, int lo, int hi, cudaStream_t st) {
@@ -768,8 +797,7 @@ template <int BITS, int D>
 cudaError_t run_narrow_rows(const AttendParams &p, int dtype, const AttendShape &s, int lo, int hi,
                             cudaStream_t st) {
     if (s.rows == 8) return run_narrow<BITS, D, 1>(p, dtype, s.ctas, lo, hi, st);
-    if (s.rows == 16) return run_narrow<BITS, D, 2>(p, dtype, s.ctas, lo, hi, st);
-    if constexpr (D <= 128) return run_narrow<BITS, D, 4>(p, dtype, s.ctas, lo, hi, st);
+    if constexpr (D <= 128) return run_narrow<BITS, D, 2>(p, dtype, s.ctas, lo, hi, st);
     return cudaErrorInvalidValue;
 }
 template <int BITS>
@@ -779,22 +807,17 @@ cudaError_t run_narrow_dim(const AttendParams &p, int dim, int dtype, const Atte
            : dim == 128 ? run_narrow_rows<BITS, 128>(p, dtype, s, lo, hi, st)
                         : run_narrow_rows<BITS, 256>(p, dtype, s, lo, hi, st);
 }
-template <int BITS, int D>
-int narrow_ctas(int rows) {
-    return rows == 8 ? (Narrow<BITS, D, 1>::TWO ? 2 : 1)
-           : rows == 16 ? (Narrow<BITS, D, 2>::TWO ? 2 : 1) : 1;
+template <int BITS>
+int narrow_ctas(int dim) {                     // an SM's, of tiles of 8 rows
+    return dim == 64 ? Narrow<BITS, 64, 1>::TWO + 1 : dim == 128 ? Narrow<BITS, 128, 1>::TWO + 1 : 1;
 }
 
 }  // namespace
 
 AttendShape attend_narrow_shape(int bits, int dim, int max_rows, int sms) {
     AttendShape s;
-    s.rows = max_rows <= 8 ? 8 : max_rows <= 16 || dim == 256 ? 16 : 32;
-    int per = 1;
-    if (bits == 4)
-        per = dim == 64 ? narrow_ctas<4, 64>(s.rows) : dim == 128 ? narrow_ctas<4, 128>(s.rows) : narrow_ctas<4, 256>(s.rows);
-    else
-        per = dim == 64 ? narrow_ctas<8, 64>(s.rows) : dim == 128 ? narrow_ctas<8, 128>(s.rows) : narrow_ctas<8, 256>(s.rows);
+    s.rows = max_rows <= 8 || dim == 256 ? 8 : 16;
+    const int per = s.rows == 16 ? 1 : bits == 4 ? narrow_ctas<4>(dim) : narrow_ctas<8>(dim);
     s.ctas = sms * per;
     return s;
 }
@@ -807,10 +830,9 @@ cudaError_t launch_attend_narrow(const AttendParams &p, int bits, int dim, int d
 
 cudaError_t launch_attend_join(const AttendParams &p, int dtype, int dim, int ctas, int rows,
                                cudaStream_t st) {
-    const dim3 grid(ctas, (rows + 7) / 8);
     const bool bf16 = dtype == AKASHIC_DTYPE_BF16;
     auto *kernel = dim == 64 ? k_attend_join<64> : dim == 128 ? k_attend_join<128> : k_attend_join<256>;
-    return launch_pdl(kernel, grid, dim3(256), 0, st, p, rows, bf16);
+    return launch_pdl(kernel, dim3(ctas), dim3(256), 0, st, p, rows, bf16);
 }
 
 }  // namespace ak
@@ -901,6 +923,7 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
     p.per_block = cfg->block_tokens / KV_UNIT;
     p.max_kv = (int)(a->max_blocks * cfg->block_tokens);
     p.causal = a->causal;
+    p.q_wide = !(((uintptr_t)a->q | (uintptr_t)((a->q_row_stride | a->q_head_stride) * 2)) & 15u);
     p.scale = a->scale != 0.f ? a->scale : 1.f / sqrtf((float)cfg->head_dim);
     p.cap = a->cap;
     cudaStream_t st = (cudaStream_t)stream;

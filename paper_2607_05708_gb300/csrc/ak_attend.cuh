@@ -40,6 +40,7 @@ struct AttendParams {
     int per_block;                    // units of a block
     int max_kv;                       // tokens that the lists can hold
     int causal;
+    bool q_wide;                      // query rows are 16-byte aligned
     float scale, cap;                 // cap 0: none
 };
 
@@ -96,87 +97,85 @@ __device__ __forceinline__ int64_t attend_seq_units(const AttendParams &p, const
     return u;
 }
 
-// Where a CTA stands in the order of all items.
+// Where a worker (a warp, or a CTA of the kernel for many rows) stands in the
+// order of all items.
 struct AttendCursor {
-    int seq, head, tile, unit;        // unit: first step of the item that is this CTA's
+    int seq, head, tile, unit;        // unit: first step of the item that is the worker's
     int units;                        // of the item
     AttendSeq q;
 };
 
-// Every CTA takes an equal share [first, first + count) of the steps of all
-// items, so that a batch of very different lengths fills the GPU evenly; it
-// finds the share's first item by a scan over the sequences.  `per` is a
-// CTA's share (a multiple of nothing in particular, at least min_per).
-// All threads of the CTA call this; scratch: 34 int64 in shared memory.
-__device__ __forceinline__ bool attend_plan(const AttendParams &p, int rows, int step, int lo,
-                                            int hi, int min_per, int64_t *scratch, int64_t &first,
-                                            int64_t &count, int64_t &per, AttendCursor &cur) {
+// Every worker takes an equal share of the steps of all items, so that a batch
+// of very different lengths fills the GPU evenly.  All threads of the CTA sum
+// up the sequences' steps (each a run of consecutive sequences); prefix[t], in
+// shared memory, is the sum of the runs before thread t's, prefix[blockDim.x] all.
+__device__ __forceinline__ void attend_sums(const AttendParams &p, int rows, int step, int lo,
+                                            int hi, int64_t *prefix) {
     const int nt = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int warps = nt >> 5;
-    int64_t sum = 0, mine = 0;
-    for (int s = tid; s < p.n_seq; s += nt) {
-        mine = attend_seq_units(p, attend_seq(p, s), rows, step, lo, hi) * p.heads;
-        sum += mine;
-    }
-    int64_t x = sum;
+    const int run = (p.n_seq + nt - 1) / nt;
+    int64_t sum = 0;
+    for (int s = tid * run; s < min(p.n_seq, (tid + 1) * run); ++s)
+        sum += attend_seq_units(p, attend_seq(p, s), rows, step, lo, hi) * p.heads;
+    int64_t incl = sum;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    if (lane == 0) scratch[warp] = x;
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+    }
+    if (lane == 31) prefix[warp] = incl;
     __syncthreads();
-    int64_t total = 0;
-    for (int w = 0; w < warps; ++w) total += scratch[w];
-    per = (total + gridDim.x - 1) / gridDim.x;
-    if (per < min_per) per = min_per;
-    first = per * blockIdx.x;
-    count = min(per, total - first);
-    if (count <= 0) return false;
-    // the sequence in whose range `first` lies
-    int64_t base = 0;
-    for (int s0 = 0; s0 < p.n_seq; s0 += nt) {
-        const int s = s0 + tid;
-        // with one round of the loop the first pass left this thread's sum
-        int64_t w = p.n_seq <= nt ? mine
-                    : s < p.n_seq ? attend_seq_units(p, attend_seq(p, s), rows, step, lo, hi) * p.heads
-                                  : 0;
-        if (s >= p.n_seq) w = 0;
+    int64_t before = 0;
+    for (int w = 0; w < warp; ++w) before += prefix[w];
+    __syncthreads();
+    prefix[tid] = before + incl - sum;
+    if (tid == nt - 1) prefix[nt] = before + incl;
+    __syncthreads();
+}
+// The item in which step `first` (below the total) lies.  A whole warp calls it.
+__device__ __forceinline__ AttendCursor attend_find(const AttendParams &p, int rows, int step,
+                                                    int lo, int hi, const int64_t *prefix,
+                                                    int64_t first) {
+    const int nt = blockDim.x, lane = threadIdx.x & 31;
+    const int run = (p.n_seq + nt - 1) / nt;
+    AttendCursor c = {};
+    int t = 0;                        // the last thread whose run begins at or before `first`
+    for (int t0 = 0; t0 < nt; t0 += 32) {
+        const unsigned before = __ballot_sync(0xffffffffu, prefix[t0 + lane] <= first);
+        t = t0 + 31 - __clz(before);
+        if (before != 0xffffffffu || first < prefix[t0 + 32]) break;
+    }
+    int64_t rest = first - prefix[t], one = 0;   // within that run
+    for (int s0 = t * run;; s0 += 32) {
+        const int s = s0 + lane;
+        const int64_t w = s < p.n_seq ? attend_seq_units(p, attend_seq(p, s), rows, step, lo, hi) * p.heads : 0;
         int64_t incl = w;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += y;
         }
-        __syncthreads();
-        if (lane == 31) scratch[warp] = incl;
-        __syncthreads();
-        int64_t before = base, all = 0;
-        for (int i = 0; i < warps; ++i) {
-            if (i < warp) before += scratch[i];
-            all += scratch[i];
+        const unsigned in = __ballot_sync(0xffffffffu, rest < incl);
+        if (in) {
+            const int l = __ffs(in) - 1;
+            c.seq = s0 + l;
+            rest -= __shfl_sync(0xffffffffu, incl - w, l);
+            one = __shfl_sync(0xffffffffu, w, l) / p.heads;
+            break;
         }
-        const int64_t hi_ = before + incl, lo_ = hi_ - w;
-        if (w > 0 && first >= lo_ && first < hi_) {
-            scratch[32] = s;
-            scratch[33] = first - lo_;
-        }
-        __syncthreads();
-        if (first < base + all) break;
-        base += all;
+        rest -= __shfl_sync(0xffffffffu, incl, 31);
+        if (s0 >= p.n_seq) return c;  // not reached: first is below the total
     }
-    cur.seq = (int)scratch[32];
-    int64_t rest = scratch[33];
-    __syncthreads();
-    cur.q = attend_seq(p, cur.seq);
-    const int64_t one = attend_seq_units(p, cur.q, rows, step, lo, hi);
-    cur.head = (int)(rest / one);
-    rest -= cur.head * one;
-    cur.tile = 0;
-    cur.units = attend_units(p, cur.q, 0, rows, step);
-    while (rest >= cur.units) {
-        rest -= cur.units;
-        cur.units = attend_units(p, cur.q, ++cur.tile, rows, step);
+    c.q = attend_seq(p, c.seq);
+    c.head = (int)(rest / one);
+    rest -= c.head * one;
+    c.tile = 0;
+    c.units = attend_units(p, c.q, 0, rows, step);
+    while (rest >= c.units) {
+        rest -= c.units;
+        c.units = attend_units(p, c.q, ++c.tile, rows, step);
     }
-    cur.unit = (int)rest;
-    return true;
+    c.unit = (int)rest;
+    return c;
 }
 // The next item (the caller knows that there is one).
 __device__ __forceinline__ void attend_next(const AttendParams &p, int rows, int step, int lo,
@@ -186,20 +185,21 @@ __device__ __forceinline__ void attend_next(const AttendParams &p, int rows, int
         c.tile = 0;
         if (++c.head >= p.heads) {
             c.head = 0;
+            int64_t n;
             do {
                 c.q = attend_seq(p, ++c.seq);
-            } while (c.seq + 1 < p.n_seq && ((int64_t)c.q.nq * p.group < lo ||
-                                             (int64_t)c.q.nq * p.group > hi));
+                n = (int64_t)c.q.nq * p.group;
+            } while (c.seq + 1 < p.n_seq && (n < lo || n > hi));
         }
     }
     c.units = attend_units(p, c.q, c.tile, rows, step);
 }
 
 // An item whose steps lie in several CTAs' shares: each leaves its rows'
-// unnormalised sums, maxima and totals in a slot of the workspace (two a CTA: its
-// first item, which may have begun before its share, and its last), the CTA
-// in which the item begins notes it, and the joining kernel adds the slots up in
-// the order of the CTAs.
+// unnormalised sums, maxima and totals in a slot of the workspace (two a CTA: slot 0 for
+// the item that began before its share, slot 1 for one that begins in it), the CTA in
+// which the item begins notes it in joins, and the joining kernel adds the slots
+// up in the order of the CTAs.
 //   slot: float acc[rows][D], m[rows] (log2 units), l[rows]
 __host__ __device__ __forceinline__ int64_t attend_slot_floats(int rows, int dim) {
     return (int64_t)rows * (dim + 2);

@@ -101,16 +101,19 @@ template <int BITS, int D, int NB>
 struct Narrow {
     using U = KvUnit<BITS, D>;
     static constexpr int ROWS = 8 * NB;
-    static constexpr int STAGE = U::BYTES + 64;          // a unit and its tags
+    // A step is what a warp works on at a time: two units where the registers allow,
+    // so that waits, fetches and the checks of maxima and exponents come half as often.
+    static constexpr int UPS = D <= 128 ? 2 : 1, STEP = UPS * KV_UNIT;
+    static constexpr int STAGE = UPS * (U::BYTES + 64);  // a step's units, then their tags
     static constexpr int ACC = ROWS * D * 4;             // a warp's accumulators
     static constexpr int SMALL = NW * ROWS * 4 * 4 + 2 * NW * ROWS * 8 + (NW * 32 + 1) * 8 + 2 * NW * 48 + 256;
     static constexpr int WANT = (225 * 512 - NW * ACC - SMALL) / (NW * (STAGE + 16));
     static constexpr int MOST = (225 * 1024 - NW * ACC - SMALL) / (NW * (STAGE + 16));
-    // two CTAs an SM where three stages of a unit leave room for it
-    static constexpr bool TWO = WANT >= 3 && NB == 1 && D <= 128;
+    // two CTAs an SM where the rings of two stages leave room for it
+    static constexpr bool TWO = WANT >= 2 && NB == 1 && D <= 128;
     static constexpr int NS_ = TWO ? WANT : MOST;
     static constexpr int NS = NS_ > 8 ? 8 : NS_;
-    static_assert(NS >= 2, "a ring of two units");
+    static_assert(NS >= 2, "a ring of two steps");
     static constexpr int RING = NS * STAGE;              // of a warp; at the end, its accumulators
     static_assert(RING >= ACC, "the last item's accumulators fit the ring");
     static constexpr int SMEM = NW * (RING + NS * 16) + NW * ACC + SMALL;
@@ -182,7 +185,7 @@ __global__ void __launch_bounds__(NW * 32, Narrow<BITS, D, NB>::TWO ? 2 : 1)
 k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int hi, const int min_per) {
     using C = Narrow<BITS, D, NB>;
     using U = typename C::U;
-    constexpr int ROWS = C::ROWS, NS = C::NS, MT = D / 16;
+    constexpr int ROWS = C::ROWS, NS = C::NS, MT = D / 16, UPS = C::UPS, STEP = C::STEP;
     constexpr int UP = BITS == 4 ? 10 : 0;     // values are staged as v 2^-10
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -206,7 +209,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
     mbar_fence_init();
     if (lane < 2) entries[2 * warp + lane].seq = -1;
     if (tid == 0) p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
-    attend_sums(p, ROWS, KV_UNIT, lo, hi, prefix);
+    attend_sums(p, ROWS, STEP, lo, hi, prefix);
     const int64_t total = prefix[NW * 32], workers = (int64_t)gridDim.x * NW;
     const int64_t per = max((int64_t)min_per, (total + workers - 1) / workers);
     const int64_t first = per * (blockIdx.x * NW + warp);
@@ -224,13 +227,14 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
     auto issue = [&]() {
         if (fetch_left <= 0) return;
         if (fetch_i == fetch_n) {              // the next item
-            attend_next(p, ROWS, KV_UNIT, lo, hi, ahead);
+            attend_next(p, ROWS, STEP, lo, hi, ahead);
             fetch_n = min(ahead.units, fetch_left), fetch_i = 0;
         }
-        if ((fetch_i & 31) == 0) {             // lane x looks up the x-th unit from here
+        constexpr int PER = 32 / UPS;          // steps of a look-up
+        if (fetch_i % PER == 0) {              // lane x looks up the x-th unit from here
             batch = {-1, 0};
-            const int u = ahead.unit + fetch_i + lane;
-            if (fetch_i + lane < fetch_n && u < (ahead.q.kv + KV_UNIT - 1) / KV_UNIT) {
+            const int u = (ahead.unit + fetch_i) * UPS + lane;
+            if (lane < (fetch_n - fetch_i) * UPS && u < (ahead.q.kv + KV_UNIT - 1) / KV_UNIT) {
                 const int b = u / p.per_block, w = u - b * p.per_block;
                 const int64_t id = p.blocks[ahead.seq * p.max_blocks + b];
                 if (id >= 0 && id < p.n_blocks)
@@ -239,25 +243,39 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                     set_status(p.status, AKASHIC_EDEVICE);
             }
         }
-        const int64_t u = __shfl_sync(0xffffffffu, batch.unit, fetch_i & 31);
-        const int sl = tags ? __shfl_sync(0xffffffffu, batch.slots, fetch_i & 31) : 0;
+        int64_t u[UPS];
+        int sl[UPS];
+#pragma unroll
+        for (int j = 0; j < UPS; ++j) {
+            u[j] = __shfl_sync(0xffffffffu, batch.unit, fetch_i % PER * UPS + j);
+            sl[j] = tags ? __shfl_sync(0xffffffffu, batch.slots, fetch_i % PER * UPS + j) : 0;
+        }
         if (lane == 0) {
             uint64_t *b = bar + fetch_stage;
             unsigned char *dst = ring + fetch_stage * C::STAGE;
-            listed[fetch_stage] = u >= 0;
-            if (u >= 0) {
-                mbar_expect_tx(b, U::BYTES + (tags ? 64 : 0));
-                bulk_load(dst, p.cache + u * U::BYTES, U::BYTES, b);
-                if (tags) bulk_load(dst + U::BYTES, p.tags + (int64_t)sl * 16, 64, b);
+            int have = 0, bytes = 0;
+#pragma unroll
+            for (int j = 0; j < UPS; ++j)
+                if (u[j] >= 0) have |= 1 << j, bytes += U::BYTES + (tags ? 64 : 0);
+            listed[fetch_stage] = have;
+            mbar_expect_tx(b, bytes);
+            if (UPS == 2 && u[0] >= 0 && u[UPS - 1] == u[0] + 1) {
+                bulk_load(dst, p.cache + u[0] * U::BYTES, UPS * U::BYTES, b);
             } else {
-                mbar_arrive(b);
+#pragma unroll
+                for (int j = 0; j < UPS; ++j)
+                    if (u[j] >= 0) bulk_load(dst + j * U::BYTES, p.cache + u[j] * U::BYTES, U::BYTES, b);
             }
+            if (tags)
+#pragma unroll
+                for (int j = 0; j < UPS; ++j)
+                    if (u[j] >= 0) bulk_load(dst + UPS * U::BYTES + j * 64, p.tags + (int64_t)sl[j] * 16, 64, b);
         }
         fetch_stage = fetch_stage + 1 == NS ? 0 : fetch_stage + 1;
         ++fetch_i, --fetch_left;
     };
     if (left > 0) {
-        cur = attend_find(p, ROWS, KV_UNIT, lo, hi, prefix, first);
+        cur = attend_find(p, ROWS, STEP, lo, hi, prefix, first);
         ahead = cur;
         fetch_n = min(ahead.units - ahead.unit, left);
         for (int i = 0; i < NS; ++i) issue();
@@ -302,7 +320,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
             for (int r = 0; r < 2; ++r)
                 qk[b][r] = __shfl_sync(0xffffffffu, f_own, b * 8 + 2 * c + r) * p.scale * LOG2E_F *
                            (BITS == 4 ? 512.f : 1.f);
-        const int safe = limit[0] - KV_UNIT;   // keys below limit[0] are seen by every row
+        const int safe = limit[0] - STEP;   // keys below limit[0] are seen by every row
 
         tref = -127;
         uint32_t unset = (1u << (2 * NB)) - 1u;    // rows that have not seen a key yet: mm = 0
@@ -313,8 +331,8 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
             mm[b][0] = mm[b][1] = 0.f, l[b][0] = l[b][1] = 0.f;
         }
 
-        int tok = cur.unit * KV_UNIT;
-        for (int it = 0; ok && it < n; ++it, tok += KV_UNIT) {
+        int tok = cur.unit * STEP;
+        for (int it = 0; ok && it < n; ++it, tok += STEP) {
             if (!mbar_wait(bar + stage, phase, p.status)) {
                 ok = false;                    // the other copies still land: wait for them
                 const int out = min(left - it, NS);
@@ -325,17 +343,20 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                 }
                 break;
             }
-            const unsigned char *un = ring + stage * C::STAGE;
-            if (listed[stage]) {
-                // ---- S^T = K Q^T
-                float s[NB][4];
+            const unsigned char *st = ring + stage * C::STAGE;
+            const int have = listed[stage];
+            if (have) {
+                // ---- S^T = K Q^T, per unit
+                float s[UPS][NB][4], kf0[UPS], kf1[UPS];   // scales of the keys of tokens g, g + 8
 #pragma unroll
-                for (int b = 0; b < NB; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
+                for (int j = 0; j < UPS; ++j) {
+                const unsigned char *un = st + j * U::BYTES;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) s[j][b][0] = s[j][b][1] = s[j][b][2] = s[j][b][3] = 0.f;
                 auto keys = [&](int kk, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) mma16(s[b], a0, a1, a2, a3, qf[b][kk][0], qf[b][kk][1]);
+                    for (int b = 0; b < NB; ++b) mma16(s[j][b], a0, a1, a2, a3, qf[b][kk][0], qf[b][kk][1]);
                 };
-                float kf0, kf1;                // scale of the keys of tokens g and g + 8
                 if constexpr (BITS == 4) {
                     constexpr int W = D / 32, PER = D / 64;    // words and groups of a token
                     uint32_t w[2][W], sc[(2 * PER + 3) / 4];
@@ -345,11 +366,11 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                         sc[0] = *(const uint16_t *)(un + U::K_SCALES + lane * 2);
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
+                        for (int i = 0; i < 2; ++i)
 #pragma unroll
                             for (int q = 0; q < W / 4; ++q) {
-                                const uint4 x = *(const uint4 *)(un + U::K_CODES + ((j * (W / 4) + q) * 32 + lane) * 16);
-                                w[j][q * 4] = x.x, w[j][q * 4 + 1] = x.y, w[j][q * 4 + 2] = x.z, w[j][q * 4 + 3] = x.w;
+                                const uint4 x = *(const uint4 *)(un + U::K_CODES + ((i * (W / 4) + q) * 32 + lane) * 16);
+                                w[i][q * 4] = x.x, w[i][q * 4 + 1] = x.y, w[i][q * 4 + 2] = x.z, w[i][q * 4 + 3] = x.w;
                             }
                         if constexpr (D == 128) {
                             sc[0] = *(const uint32_t *)(un + U::K_SCALES + lane * 4);
@@ -359,17 +380,17 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                         }
                     }
                     const uint32_t ex = *(const uint16_t *)(un + U::K_EXP + g * 2);
-                    kf0 = __uint_as_float((ex & 255u) << 23), kf1 = __uint_as_float((ex >> 8) << 23);
+                    kf0[j] = __uint_as_float((ex & 255u) << 23), kf1[j] = __uint_as_float((ex >> 8) << 23);
 #pragma unroll
                     for (int gr = 0; gr < PER; ++gr) {
                         uint32_t sj[2], s4[2], cj[2];
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const int b = j * PER + gr;
+                        for (int i = 0; i < 2; ++i) {
+                            const int b = i * PER + gr;
                             const uint32_t by = (sc[b / 4] >> (8 * (b & 3))) & 255u;
-                            sj[j] = by * 0x00400040u + 0x3c003c00u;
-                            s4[j] = sj[j] - 0x10001000u;
-                            cj[j] = h2mul(sj[j], H2_M2_21);
+                            sj[i] = by * 0x00400040u + 0x3c003c00u;
+                            s4[i] = sj[i] - 0x10001000u;
+                            cj[i] = h2mul(sj[i], H2_M2_21);
                         }
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
@@ -396,47 +417,46 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                                  h2add(__byte_perm(wy[i], 0x64646464u, 0x4342), H2_M1152));
                     }
                     const uint32_t ks = *(const uint32_t *)(un + U::K_SCALES + g * 4);
-                    kf0 = __uint_as_float(ks << 16), kf1 = __uint_as_float(ks & 0xffff0000u);
+                    kf0[j] = __uint_as_float(ks << 16), kf1[j] = __uint_as_float(ks & 0xffff0000u);
+                }
                 }
 
                 // ---- scores in log2 units less the running maximum (mm = m - 6);
                 // what a row does not see is -inf
-                int tag0 = 0, tag1 = 0;
-                if (tags) {
-                    tag0 = ((const int *)(un + U::BYTES))[g];
-                    tag1 = ((const int *)(un + U::BYTES))[g + 8];
-                }
-                const bool masked = tags || tok > safe;
+                const int *tg = (const int *)(st + UPS * U::BYTES);
+                const bool masked = tags || tok > safe || have != (1 << UPS) - 1;
                 float most = NEG;
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    if (heavy) {
+                for (int j = 0; j < UPS; ++j) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int col = b * 8 + 2 * c + (r & 1);
-                            s[b][r] *= (r < 2 ? kf0 : kf1) * qk[b][r & 1];
-                            if (p.cap > 0.f)
-                                s[b][r] = cap_l * (1.f - __fdividef(2.f, 1.f + ex2(s[b][r] * cap_in)));
-                            if (p.slopes)
-                                s[b][r] -= slope[col] * (float)abs(pos[col] - (tok + g + (r < 2 ? 0 : 8)));
-                            s[b][r] -= mm[b][r & 1];
+                    for (int b = 0; b < NB; ++b) {
+                        if (heavy) {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const int col = b * 8 + 2 * c + (r & 1);
+                                float &z = s[j][b][r];
+                                z *= (r < 2 ? kf0[j] : kf1[j]) * qk[b][r & 1];
+                                if (p.cap > 0.f) z = cap_l * (1.f - __fdividef(2.f, 1.f + ex2(z * cap_in)));
+                                if (p.slopes)
+                                    z -= slope[col] * (float)abs(pos[col] - (tok + j * 16 + g + (r < 2 ? 0 : 8)));
+                                z -= mm[b][r & 1];
+                            }
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                s[j][b][r] = fmaf(s[j][b][r], (r < 2 ? kf0[j] : kf1[j]) * qk[b][r & 1], -mm[b][r & 1]);
                         }
-                    } else {
+                        if (masked) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            s[b][r] = fmaf(s[b][r], (r < 2 ? kf0 : kf1) * qk[b][r & 1], -mm[b][r & 1]);
-                    }
-                    if (masked) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int col = b * 8 + 2 * c + (r & 1);
-                            const int tag = r < 2 ? tag0 : tag1;
-                            const bool seen = tok + g + (r < 2 ? 0 : 8) < limit[col] &&
-                                              (!tags || (tag >= 0 && tag == qtag[col]));
-                            if (!seen) s[b][r] = -INFINITY;
+                            for (int r = 0; r < 4; ++r) {
+                                const int col = b * 8 + 2 * c + (r & 1), t = j * 16 + g + (r < 2 ? 0 : 8);
+                                const bool seen = (have >> j & 1) && tok + t < limit[col] &&
+                                                  (!tags || (tg[t] >= 0 && tg[t] == qtag[col]));
+                                if (!seen) s[j][b][r] = -INFINITY;
+                            }
                         }
+                        most = fmaxf(fmaxf(most, s[j][b][0]), fmaxf(fmaxf(s[j][b][1], s[j][b][2]), s[j][b][3]));
                     }
-                    most = fmaxf(fmaxf(most, s[b][0]), fmaxf(fmaxf(s[b][1], s[b][2]), s[b][3]));
                 }
                 // ---- running maxima
                 if (__any_sync(0xffffffffu, unset || most > P_SHIFT + M_SLACK)) {
@@ -444,7 +464,8 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                     for (int b = 0; b < NB; ++b)
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
-                            float x = fmaxf(s[b][r], s[b][r + 2]);
+                            float x = fmaxf(s[0][b][r], s[0][b][r + 2]);
+                            if constexpr (UPS == 2) x = fmaxf(x, fmaxf(s[1][b][r], s[1][b][r + 2]));
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
@@ -454,7 +475,8 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                                 const float f = fresh ? 0.f : ex2(-x);
                                 unset &= ~(1u << (2 * b + r));
                                 mm[b][r] += x;
-                                s[b][r] -= x, s[b][r + 2] -= x;
+#pragma unroll
+                                for (int j = 0; j < UPS; ++j) s[j][b][r] -= x, s[j][b][r + 2] -= x;
                                 l[b][r] *= f;
 #pragma unroll
                                 for (int t = 0; t < MT; ++t) o[b][t][r] *= f, o[b][t][r + 2] *= f;
@@ -462,74 +484,91 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                         }
                 }
                 // ---- weights, and P^T as the B operand
-                float vf0 = 1.f, vf1 = 1.f;    // 8 bits: the significands of the values' scales
-                if constexpr (BITS == 8) {
-                    const uint16_t *vs = (const uint16_t *)(un + U::V_SCALES);
-                    vf0 = __uint_as_float(((uint32_t)(vs[U::v_row(0) + (g >> 1) * 4 + (g & 1)] & 0x7fu) << 16) | 0x3f800000u);
-                    vf1 = __uint_as_float(((uint32_t)(vs[U::v_row(8) + (g >> 1) * 4 + (g & 1)] & 0x7fu) << 16) | 0x3f800000u);
-                }
-                uint32_t pb[NB][2];
+                uint32_t pb[UPS][NB][2];
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        s[b][r] = ex2(s[b][r]);
-                        l[b][r & 1] += s[b][r];
-                    }
+                for (int j = 0; j < UPS; ++j) {
+                    float vf0 = 1.f, vf1 = 1.f;    // 8 bits: the significands of the values' scales
                     if constexpr (BITS == 8) {
-                        s[b][0] *= vf0, s[b][1] *= vf0, s[b][2] *= vf1, s[b][3] *= vf1;
+                        const uint16_t *vs = (const uint16_t *)(st + j * U::BYTES + U::V_SCALES);
+                        vf0 = __uint_as_float(((uint32_t)(vs[U::v_row(0) + (g >> 1) * 4 + (g & 1)] & 0x7fu) << 16) | 0x3f800000u);
+                        vf1 = __uint_as_float(((uint32_t)(vs[U::v_row(8) + (g >> 1) * 4 + (g & 1)] & 0x7fu) << 16) | 0x3f800000u);
                     }
-                    pb[b][0] = transpose8(pack_h2(s[b][0], s[b][1]));
-                    pb[b][1] = transpose8(pack_h2(s[b][2], s[b][3]));
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        float (&z)[4] = s[j][b];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) z[r] = ex2(z[r]);
+                        l[b][0] += z[0] + z[2], l[b][1] += z[1] + z[3];
+                        if constexpr (BITS == 8) z[0] *= vf0, z[1] *= vf0, z[2] *= vf1, z[3] *= vf1;
+                        pb[j][b][0] = transpose8(pack_h2(z[0], z[1]));
+                        pb[j][b][1] = transpose8(pack_h2(z[2], z[3]));
+                    }
                 }
                 // ---- the values' exponents relative to tref, as fp16 powers of two: of
-                // tokens 2c and 2c + 1 in f0, 2c + 8 and 2c + 9 in f1.  In the common
-                // case all lie in [tref - 14, tref + 1] and are put together in place.
-                uint32_t t0, t1;               // T + 127, two to a word
-                if constexpr (BITS == 4) {
-                    const uint32_t x = *(const uint32_t *)(un + U::V_EXP + c * 4);
-                    t0 = __byte_perm(x, 0, 0x4140), t1 = __byte_perm(x, 0, 0x4342);
-                } else {
-                    const uint2 x = *(const uint2 *)(un + U::V_SCALES + c * 8);
-                    t0 = (x.x >> 7) & 0x00ff00ffu, t1 = (x.y >> 7) & 0x00ff00ffu;
-                }
+                // tokens 2c and 2c + 1 of each unit in f[j][0], 2c + 8 and 2c + 9 in f[j][1].
+                // In the common case all lie in [tref - 14, tref + 1] and are put together
+                // in place.
+                uint32_t te[UPS][2], f[UPS][2], wide = 0;      // te: T + 127, two to a word
                 const uint32_t low = (uint32_t)(tref + 127 - 14) * 0x00010001u;
-                uint32_t f0 = ((t0 - low) << 10) + 0x04000400u, f1 = ((t1 - low) << 10) + 0x04000400u;
-                if (masked || __any_sync(0xffffffffu, ((t0 - low) | (t1 - low)) & 0xfff0fff0u)) {
-                    int te[4] = {(int)(t0 & 0xffffu) - 127, (int)(t0 >> 16) - 127,
-                                 (int)(t1 & 0xffffu) - 127, (int)(t1 >> 16) - 127};
-                    if (masked) {              // a slot without a token adds nothing
+#pragma unroll
+                for (int j = 0; j < UPS; ++j) {
+                    const unsigned char *un = st + j * U::BYTES;
+                    if constexpr (BITS == 4) {
+                        const uint32_t x = *(const uint32_t *)(un + U::V_EXP + c * 4);
+                        te[j][0] = __byte_perm(x, 0, 0x4140), te[j][1] = __byte_perm(x, 0, 0x4342);
+                    } else {
+                        const uint2 x = *(const uint2 *)(un + U::V_SCALES + c * 8);
+                        te[j][0] = (x.x >> 7) & 0x00ff00ffu, te[j][1] = (x.y >> 7) & 0x00ff00ffu;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t d = te[j][i] - low;
+                        f[j][i] = (d << 10) + 0x04000400u;
+                        wide |= d;
+                    }
+                }
+                if (masked || __any_sync(0xffffffffu, wide & 0xfff0fff0u)) {
+                    int ti[UPS][4], x = -1000;
+#pragma unroll
+                    for (int j = 0; j < UPS; ++j)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const int t = 2 * c + (i & 1) + (i >> 1) * 8;
-                            const bool real = tok + t < sq.kv &&
-                                              (!tags || ((const int *)(un + U::BYTES))[t] >= 0);
-                            if (!real) te[i] = -1000;
+                            ti[j][i] = (int)(te[j][i >> 1] >> (16 * (i & 1)) & 0xffffu) - 127;
+                            if (masked) {          // a slot without a token adds nothing
+                                const int t = j * 16 + 2 * c + (i & 1) + (i >> 1) * 8;
+                                if (!(have >> j & 1) || tok + t >= sq.kv || (tags && tg[t] < 0)) ti[j][i] = -1000;
+                            }
+                            x = max(x, ti[j][i]);
                         }
-                    }
-                    int x = max(max(te[0], te[1]), max(te[2], te[3]));
                     if (__any_sync(0xffffffffu, x > tref + 1)) {
                         x = max(x, __shfl_xor_sync(0xffffffffu, x, 1));
                         x = max(max(x, __shfl_xor_sync(0xffffffffu, x, 2)), tref);
-                        const float f = pow2i(max(-126, tref - x));
+                        const float down = pow2i(max(-126, tref - x));
                         tref = x;
 #pragma unroll
                         for (int b = 0; b < NB; ++b)
 #pragma unroll
                             for (int t = 0; t < MT; ++t)
 #pragma unroll
-                                for (int r = 0; r < 4; ++r) o[b][t][r] *= f;
+                                for (int r = 0; r < 4; ++r) o[b][t][r] *= down;
                     }
-                    float tf[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) tf[i] = te[i] - tref < -40 ? 0.f : pow2i(te[i] - tref);
-                    f0 = pack_h2(tf[0], tf[1]), f1 = pack_h2(tf[2], tf[3]);
+                    for (int j = 0; j < UPS; ++j)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int a = ti[j][2 * i] - tref, b = ti[j][2 * i + 1] - tref;
+                            f[j][i] = pack_h2(a < -40 ? 0.f : pow2i(a), b < -40 ? 0.f : pow2i(b));
+                        }
                 }
 
                 // ---- O^T += V^T P^T
+#pragma unroll
+                for (int j = 0; j < UPS; ++j) {
+                const unsigned char *un = st + j * U::BYTES;
+                const uint32_t f0 = f[j][0], f1 = f[j][1];
                 auto values = [&](int mt, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) mma16(o[b][mt], a0, a1, a2, a3, pb[b][0], pb[b][1]);
+                    for (int b = 0; b < NB; ++b) mma16(o[b][mt], a0, a1, a2, a3, pb[j][b][0], pb[j][b][1]);
                 };
                 if constexpr (BITS == 4) {
                     constexpr int W = D / 64;                  // words a lane has of a token
@@ -539,9 +578,9 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                         w[0][0] = x.x, w[1][0] = x.y, w[2][0] = x.z, w[3][0] = x.w;
                     } else if constexpr (W == 2) {
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const uint4 x = *(const uint4 *)(un + U::V_CODES + (j * 32 + lane) * 16);
-                            w[2 * j][0] = x.x, w[2 * j][1] = x.y, w[2 * j + 1][0] = x.z, w[2 * j + 1][1] = x.w;
+                        for (int i = 0; i < 2; ++i) {
+                            const uint4 x = *(const uint4 *)(un + U::V_CODES + (i * 32 + lane) * 16);
+                            w[2 * i][0] = x.x, w[2 * i][1] = x.y, w[2 * i + 1][0] = x.z, w[2 * i + 1][1] = x.w;
                         }
                     } else {
 #pragma unroll
@@ -577,9 +616,9 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                     uint32_t w[4][W];
                     if constexpr (W == 2) {
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const uint4 x = *(const uint4 *)(un + U::V_CODES + (j * 32 + lane) * 16);
-                            w[2 * j][0] = x.x, w[2 * j][1] = x.y, w[2 * j + 1][0] = x.z, w[2 * j + 1][1] = x.w;
+                        for (int i = 0; i < 2; ++i) {
+                            const uint4 x = *(const uint4 *)(un + U::V_CODES + (i * 32 + lane) * 16);
+                            w[2 * i][0] = x.x, w[2 * i][1] = x.y, w[2 * i + 1][0] = x.z, w[2 * i + 1][1] = x.w;
                         }
                     } else {
 #pragma unroll
@@ -604,6 +643,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                                    h2fma(__byte_perm(y, 0x64646464u, 0x4140), f1, c1),
                                    h2fma(__byte_perm(y, 0x64646464u, 0x4342), f1, c1));
                         }
+                }
                 }
             }
             __syncwarp();                      // the stage has been read
@@ -659,7 +699,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                 }
         }
         left -= n, done += n;
-        if (left > 0) attend_next(p, ROWS, KV_UNIT, lo, hi, cur);
+        if (left > 0) attend_next(p, ROWS, STEP, lo, hi, cur);
     }
     if (tail) {
         // nothing is in flight any more: the ring takes the last item's part
@@ -782,7 +822,7 @@ k_attend_join(const AttendParams p, const int rows, const bool bf16) {
     }
 }
 
-constexpr int MIN_PER = 2;    // units of a warp's share, at least
+constexpr int MIN_PER = 1;    // steps of a warp's share, at least
 
 template <int BITS, int D, int NB>
 cudaError_t run_narrow(const AttendParams &p, int dtype, int ctas, int lo, int hi, cudaStream_t st) {

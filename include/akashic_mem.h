@@ -399,7 +399,8 @@ typedef struct {
     int32_t heads;        /* key/value heads, 1..1024                              */
     int32_t head_dim;     /* 64, 128 or 256                                        */
     int32_t block_tokens; /* multiple of 16, 16..4096                              */
-    int64_t n_blocks;     /* >= 1; n_blocks * block_tokens / 16 <= 2^31 - 1        */
+    int64_t n_blocks;     /* >= 1; n_blocks * block_tokens / 16 <= 2^31 - 1, and
+                             times heads <= 2^32 - 2 (290 GB are fewer)            */
     int32_t device;       /* CUDA device ordinal                                   */
 } akashic_mem_kv_config_t;
 

@@ -106,7 +106,8 @@ struct Narrow {
     static constexpr int UPS = D <= 128 ? 2 : 1, STEP = UPS * KV_UNIT;
     static constexpr int STAGE = UPS * (U::BYTES + 64);  // a step's units, then their tags
     static constexpr int ACC = ROWS * D * 4;             // a warp's accumulators
-    static constexpr int SMALL = NW * ROWS * 4 * 4 + 2 * NW * ROWS * 8 + (NW * 32 + 1) * 8 + 2 * NW * 48 + 256;
+    static constexpr int SMALL = NW * ROWS * 4 * 4 + 2 * NW * ROWS * 8 + 2 * NW * 48 + NW * 64 + 64;
+    static_assert(NW * ACC >= (NW * 32 + 1) * 8, "the plan's sums lie where parts come later");
     static constexpr int WANT = (225 * 512 - NW * ACC - SMALL) / (NW * (STAGE + 16));
     static constexpr int MOST = (225 * 1024 - NW * ACC - SMALL) / (NW * (STAGE + 16));
     // two CTAs an SM where the rings of two stages leave room for it
@@ -119,12 +120,18 @@ struct Narrow {
     static constexpr int SMEM = NW * (RING + NS * 16) + NW * ACC + SMALL;
 };
 
+// Where a warp's fetching stands: the item, the steps of it that are the warp's share.
+struct Fetch {
+    AttendCursor cur;
+    int i, n;
+};
+
 // A warp's part of an item, left for the joining of the CTA's warps.
 struct Entry {
     int64_t start;                             // of the item, in all steps
     int seq, head, tile, unit, n, units, tref, pad;
 };
-static_assert(sizeof(Entry) <= 48, "Narrow::SMALL");
+static_assert(sizeof(Entry) <= 48 && sizeof(Fetch) <= 64, "Narrow::SMALL");
 
 // A lane's part of the B fragments of a tile's query rows: row g of each 8, dims
 // c D/4 + 4 kk + {0..3}.  bf16 rows are scaled by a power of two to a largest
@@ -182,7 +189,7 @@ __device__ __forceinline__ float lse_of(float m, float total) {
 
 template <int BITS, int D, int NB>
 __global__ void __launch_bounds__(NW * 32, Narrow<BITS, D, NB>::TWO ? 2 : 1)
-k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int hi, const int min_per) {
+k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const int lo, const int hi, const int min_per) {
     using C = Narrow<BITS, D, NB>;
     using U = typename C::U;
     constexpr int ROWS = C::ROWS, NS = C::NS, MT = D / 16, UPS = C::UPS, STEP = C::STEP;
@@ -191,11 +198,12 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, c = lane & 3;
     unsigned char *at = smem + NW * C::RING;
+    int64_t *prefix = (int64_t *)at;           // until the warps have found their items
     float *heads = (float *)at;                           at += NW * C::ACC;
     Entry *entries = (Entry *)at;                         at += 2 * NW * sizeof(Entry);
-    int64_t *prefix = (int64_t *)at;                      at += (NW * 32 + 1) * 8;
     uint64_t *bar = (uint64_t *)at + warp * NS;           at += NW * NS * 8;
-    int *listed = (int *)at + warp * NS;                  at += NW * NS * 4;
+    Fetch *ahead = (Fetch *)at + warp;                    at += NW * sizeof(Fetch);
+    unsigned char *listed = at + warp * NS * 2;           at += NW * NS * 4;
     float *em = (float *)at;                              at += 2 * NW * ROWS * 4;   // of entries
     float *el = (float *)at;                              at += 2 * NW * ROWS * 4;
     float *slope = (float *)at + warp * ROWS;             at += NW * ROWS * 4;       // of rows
@@ -205,7 +213,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
     unsigned char *ring = smem + warp * C::RING;
 
     if (lane == 0)
-        for (int i = 0; i < NS; ++i) mbar_init(bar + i, 1);
+        for (int i = 0; i < NS; ++i) mbar_init(bar + i, UPS);
     mbar_fence_init();
     if (lane < 2) entries[2 * warp + lane].seq = -1;
     if (tid == 0) p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
@@ -215,69 +223,65 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
     const int64_t first = per * (blockIdx.x * NW + warp);
     int left = (int)max((int64_t)0, min(per, total - first));   // steps of this warp
 
-    // What is needed to fetch: the item that is being fetched, up to NS units ahead of
-    // the one that is worked on.
-    struct Place {
-        int64_t unit;                          // of the cache, -1: not listed
-        int slots;                             // the unit's slots / 16
-    } batch = {-1, 0};
-    AttendCursor cur, ahead;
-    int fetch_left = left, fetch_n = 0, fetch_i = 0, fetch_stage = 0;
+    // Fetching runs up to NS steps ahead of the work, across items.  Lane x looks up the x-th unit
+    // from the present one, a warp's worth at a time, and copies it itself when
+    // its turn comes.  Where fetching stands is kept in shared memory: it is needed
+    // once a look-up only, and the registers are not there.
+    constexpr int PER = 32 / UPS;              // steps of a look-up
+    constexpr uint32_t NONE = 0xffffffffu;
+    uint32_t my_unit = NONE, my_slots = 0;     // this lane's unit of the cache, its slots / 16
+    int fetch_left = left, turn = 32, turn_end = 32, fetch_stage = 0;
     const bool tags = p.tags != nullptr, heavy = p.cap > 0.f || p.slopes;
-    auto issue = [&]() {
-        if (fetch_left <= 0) return;
-        if (fetch_i == fetch_n) {              // the next item
-            attend_next(p, ROWS, STEP, lo, hi, ahead);
-            fetch_n = min(ahead.units, fetch_left), fetch_i = 0;
+    auto look_up = [&]() {
+        AttendCursor x = ahead->cur;
+        int i = ahead->i, n = ahead->n;        // steps of the item: done, this share's
+        if (i == n) {
+            attend_next(p, ROWS, STEP, lo, hi, x);
+            i = 0, n = min(x.units, fetch_left);
         }
-        constexpr int PER = 32 / UPS;          // steps of a look-up
-        if (fetch_i % PER == 0) {              // lane x looks up the x-th unit from here
-            batch = {-1, 0};
-            const int u = (ahead.unit + fetch_i) * UPS + lane;
-            if (lane < (fetch_n - fetch_i) * UPS && u < (ahead.q.kv + KV_UNIT - 1) / KV_UNIT) {
-                const int b = u / p.per_block, w = u - b * p.per_block;
-                const int64_t id = p.blocks[ahead.seq * p.max_blocks + b];
-                if (id >= 0 && id < p.n_blocks)
-                    batch = {(id * p.heads + ahead.head) * p.per_block + w, (int)id * p.per_block + w};
-                else if (id != -1)
-                    set_status(p.status, AKASHIC_EDEVICE);
+        __syncwarp();
+        const int steps = min(PER, n - i), u = (x.unit + i) * UPS + lane;
+        if (lane == 0) *ahead = Fetch{x, i + steps, n};
+        my_unit = NONE;
+        if (lane < steps * UPS && u < (x.q.kv + KV_UNIT - 1) / KV_UNIT) {
+            const int b = u / p.per_block, w = u - b * p.per_block;
+            const int64_t id = p.blocks[x.seq * p.max_blocks + b];
+            if (id >= 0 && id < p.n_blocks) {
+                my_slots = (uint32_t)id * p.per_block + w;
+                my_unit = ((uint32_t)id * p.heads + x.head) * p.per_block + w;
+            } else if (id != -1) {
+                set_status(p.status, AKASHIC_EDEVICE);
             }
         }
-        int64_t u[UPS];
-        int sl[UPS];
-#pragma unroll
-        for (int j = 0; j < UPS; ++j) {
-            u[j] = __shfl_sync(0xffffffffu, batch.unit, fetch_i % PER * UPS + j);
-            sl[j] = tags ? __shfl_sync(0xffffffffu, batch.slots, fetch_i % PER * UPS + j) : 0;
-        }
-        if (lane == 0) {
+        turn = 0, turn_end = steps * UPS;
+        __syncwarp();
+    };
+    auto issue = [&]() {
+        if (fetch_left == 0) return;
+        if (turn == turn_end) look_up();
+        const int j = lane - turn;
+        if ((unsigned)j < (unsigned)UPS) {
             uint64_t *b = bar + fetch_stage;
             unsigned char *dst = ring + fetch_stage * C::STAGE;
-            int have = 0, bytes = 0;
-#pragma unroll
-            for (int j = 0; j < UPS; ++j)
-                if (u[j] >= 0) have |= 1 << j, bytes += U::BYTES + (tags ? 64 : 0);
-            listed[fetch_stage] = have;
-            mbar_expect_tx(b, bytes);
-            if (UPS == 2 && u[0] >= 0 && u[UPS - 1] == u[0] + 1) {
-                bulk_load(dst, p.cache + u[0] * U::BYTES, UPS * U::BYTES, b);
+            const bool have = my_unit != NONE;
+            listed[fetch_stage * 2 + j] = have;
+            if (have) {
+                mbar_expect_tx(b, U::BYTES + (tags ? 64 : 0));
+                bulk_load(dst + j * U::BYTES, p.cache + (uint64_t)my_unit * U::BYTES, U::BYTES, b);
+                if (tags) bulk_load(dst + UPS * U::BYTES + j * 64, p.tags + (uint64_t)my_slots * 16, 64, b);
             } else {
-#pragma unroll
-                for (int j = 0; j < UPS; ++j)
-                    if (u[j] >= 0) bulk_load(dst + j * U::BYTES, p.cache + u[j] * U::BYTES, U::BYTES, b);
+                mbar_arrive(b);
             }
-            if (tags)
-#pragma unroll
-                for (int j = 0; j < UPS; ++j)
-                    if (u[j] >= 0) bulk_load(dst + UPS * U::BYTES + j * 64, p.tags + (int64_t)sl[j] * 16, 64, b);
         }
+        turn += UPS, --fetch_left;
         fetch_stage = fetch_stage + 1 == NS ? 0 : fetch_stage + 1;
-        ++fetch_i, --fetch_left;
     };
+    AttendCursor cur;
+    if (left > 0) cur = attend_find(p, ROWS, STEP, lo, hi, prefix, first);
+    __syncthreads();
     if (left > 0) {
-        cur = attend_find(p, ROWS, STEP, lo, hi, prefix, first);
-        ahead = cur;
-        fetch_n = min(ahead.units - ahead.unit, left);
+        if (lane == 0) *ahead = Fetch{cur, 0, min(cur.units - cur.unit, left)};
+        __syncwarp();
         for (int i = 0; i < NS; ++i) issue();
     }
 
@@ -344,7 +348,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                 break;
             }
             const unsigned char *st = ring + stage * C::STAGE;
-            const int have = listed[stage];
+            const uint32_t have = UPS == 2 ? *(const uint16_t *)(listed + stage * 2) : listed[stage * 2];
             if (have) {
                 // ---- S^T = K Q^T, per unit
                 float s[UPS][NB][4], kf0[UPS], kf1[UPS];   // scales of the keys of tokens g, g + 8
@@ -424,7 +428,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                 // ---- scores in log2 units less the running maximum (mm = m - 6);
                 // what a row does not see is -inf
                 const int *tg = (const int *)(st + UPS * U::BYTES);
-                const bool masked = tags || tok > safe || have != (1 << UPS) - 1;
+                const bool masked = tags || tok > safe || have != (UPS == 2 ? 0x101u : 1u);
                 float most = NEG;
 #pragma unroll
                 for (int j = 0; j < UPS; ++j) {
@@ -450,7 +454,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 const int col = b * 8 + 2 * c + (r & 1), t = j * 16 + g + (r < 2 ? 0 : 8);
-                                const bool seen = (have >> j & 1) && tok + t < limit[col] &&
+                                const bool seen = (have >> (8 * j) & 1) && tok + t < limit[col] &&
                                                   (!tags || (tg[t] >= 0 && tg[t] == qtag[col]));
                                 if (!seen) s[j][b][r] = -INFINITY;
                             }
@@ -536,7 +540,7 @@ k_attend_narrow(const AttendParams p, const bool bf16, const int lo, const int h
                             ti[j][i] = (int)(te[j][i >> 1] >> (16 * (i & 1)) & 0xffffu) - 127;
                             if (masked) {          // a slot without a token adds nothing
                                 const int t = j * 16 + 2 * c + (i & 1) + (i >> 1) * 8;
-                                if (!(have >> j & 1) || tok + t >= sq.kv || (tags && tg[t] < 0)) ti[j][i] = -1000;
+                                if (!(have >> (8 * j) & 1) || tok + t >= sq.kv || (tags && tg[t] < 0)) ti[j][i] = -1000;
                             }
                             x = max(x, ti[j][i]);
                         }

@@ -33,6 +33,8 @@ akashic_status_t kv_check_config(const akashic_mem_kv_config_t *c, const char *w
         return kv_fail(AKASHIC_EINVAL, "%s: block_tokens must be a multiple of 16 in [16, 4096]", who);
     if (c->n_blocks < 1 || c->n_blocks > 0x7fffffffLL / (c->block_tokens / KV_UNIT))
         return kv_fail(AKASHIC_EINVAL, "%s: n_blocks must be >= 1, with at most 2^31 - 1 units of 16 tokens", who);
+    if (c->n_blocks * (c->block_tokens / KV_UNIT) > 0xfffffffeLL / c->heads)
+        return kv_fail(AKASHIC_EINVAL, "%s: more than 2^32 - 2 units of 16 tokens and a head", who);
     if (c->device < 0) return kv_fail(AKASHIC_EINVAL, "%s: device must be >= 0", who);
     return AKASHIC_OK;
 }

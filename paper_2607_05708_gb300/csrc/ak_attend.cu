@@ -32,34 +32,7 @@ namespace ak {
 namespace {
 
 constexpr int NW = 8;                         // warps of a CTA
-constexpr float NEG = -1e30f;                 // "no score yet", finite: no NaN from differences
-constexpr float P_SHIFT = 6.f, M_SLACK = 8.f; // log2 units
 
-__device__ __forceinline__ uint32_t h2fma(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t d;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
-}
-__device__ __forceinline__ uint32_t h2mul(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-__device__ __forceinline__ uint32_t h2add(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-__device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
-    uint32_t d;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
-}
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     uint32_t d;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
@@ -79,24 +52,6 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
         "l"(src), "r"(bytes), "r"(smem_u32(bar))
         : "memory");
 }
-__device__ __forceinline__ float scale2(float x, int e) {   // x 2^e, |e| <= 252
-    return x * pow2i(e / 2) * pow2i(e - e / 2);
-}
-
-// Four adjacent-dim (or, after pairing, adjacent-token) pairs of a word of 8
-// nibbles: pair i in h[i].  s: e 2^15 in both halves, s4: s 2^-4, c: -s 2^-21.
-__device__ __forceinline__ void nibbles(uint32_t w, uint32_t s, uint32_t s4, uint32_t c,
-                                        uint32_t (&h)[4]) {
-    const uint32_t w8 = w >> 8;
-    h[0] = h2fma(w & 0x000f000fu, s, c);
-    h[1] = h2fma(w & 0x00f000f0u, s4, c);
-    h[2] = h2fma(w8 & 0x000f000fu, s, c);
-    h[3] = h2fma(w8 & 0x00f000f0u, s4, c);
-}
-constexpr uint32_t H2_M2_21 = 0x80088008u;   // -2^-21, twice
-constexpr uint32_t H2_2_4 = 0x2c002c00u;     // 2^-4, twice
-constexpr uint32_t H2_M1152 = 0xe480e480u;   // -1152, twice
-
 template <int BITS, int D, int NB>
 struct Narrow {
     using U = KvUnit<BITS, D>;
@@ -174,17 +129,6 @@ __device__ __forceinline__ float load_query(const AttendParams &p, bool bf16, in
         f[k][1] = pack_h2(bf16_to_f32(raw[4 * k + 2]) * by, bf16_to_f32(raw[4 * k + 3]) * by);
     }
     return pow2i(e);
-}
-
-// Two adjacent values of a result row, and its log-sum-exp.
-__device__ __forceinline__ void store_pair(const AttendParams &p, bool bf16, int64_t at, float a, float b) {
-    if (bf16)
-        *(__nv_bfloat162 *)((__nv_bfloat16 *)p.out + at) = __floats2bfloat162_rn(a, b);
-    else
-        *(uint32_t *)((__half *)p.out + at) = pack_h2(a, b);
-}
-__device__ __forceinline__ float lse_of(float m, float total) {
-    return total == 0.f ? -INFINITY : (m + log2f(total)) * 0.69314718055994530942f;
 }
 
 template <int BITS, int D, int NB>
@@ -910,12 +854,28 @@ akashic_status_t attend_check(const akashic_mem_kv_config_t *cfg, const akashic_
     return AKASHIC_OK;
 }
 
-AttendShape shape_of(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_attend_t *a) {
+// Which kernels a call launches.  Where all sequences have the same number of rows
+// (query rows times group) one takes them all; else each takes the sequences on
+// its side of WIDE_FROM.
+constexpr int WIDE_FROM = 17;
+struct AttendRoute {
+    AttendShape narrow = {0, 0}, wide = {0, 0};   // ctas 0: not launched
+    int64_t joins = 0, bytes = 0;                 // scratch: of the joins, in all
+    int64_t narrow_floats = 0;
+};
+AttendRoute route_of(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_attend_t *a) {
+    AttendRoute r;
     const int64_t rows = (int64_t)a->n_q * (a->q_heads / cfg->heads);
-    const int64_t each = a->n_seq > 0 ? ceil_div(rows, (int64_t)a->n_seq) : 0;
-    return attend_narrow_shape(cfg->bits, cfg->head_dim, (int)(each < 64 ? each : 64), device_sm_count());
+    const int64_t most = a->q_start || a->n_seq == 0 ? rows : rows / a->n_seq;
+    const int sms = device_sm_count();
+    if (a->q_start || most < WIDE_FROM)
+        r.narrow = attend_narrow_shape(cfg->bits, cfg->head_dim, (int)(most < WIDE_FROM ? most : WIDE_FROM - 1), sms);
+    if (most >= WIDE_FROM) r.wide = attend_wide_shape(cfg->head_dim, sms);
+    r.joins = ceil_div((int64_t)(r.narrow.ctas + r.wide.ctas) * 16, (int64_t)256) * 256;
+    r.narrow_floats = r.narrow.ctas * 2 * attend_slot_floats(r.narrow.rows, cfg->head_dim);
+    r.bytes = r.joins + (r.narrow_floats + r.wide.ctas * 2 * attend_slot_floats(r.wide.rows, cfg->head_dim)) * 4;
+    return r;
 }
-int64_t joins_bytes(int ctas) { return ceil_div((int64_t)ctas * 16, (int64_t)256) * 256; }
 
 }  // namespace
 
@@ -927,8 +887,7 @@ extern "C" akashic_status_t akashic_mem_kv_attend_scratch(const akashic_mem_kv_c
     if (!bytes) return kv_fail(AKASHIC_EINVAL, "kv_attend_scratch: NULL bytes");
     KvDevice dev(cfg->device);
     if (!dev.ok) return kv_fail(AKASHIC_ECUDA, "kv_attend_scratch: device %d cannot be made current", cfg->device);
-    const AttendShape s = shape_of(cfg, a);
-    *bytes = joins_bytes(s.ctas) + s.ctas * 2 * attend_slot_floats(s.rows, cfg->head_dim) * 4;
+    *bytes = route_of(cfg, a).bytes;
     return AKASHIC_OK;
 }
 
@@ -948,10 +907,9 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
         return kv_fail(AKASHIC_EINVAL, "kv_attend: out must be 4-byte aligned, q to its element");
     KvDevice dev(cfg->device);
     if (!dev.ok) return kv_fail(AKASHIC_ECUDA, "kv_attend: device %d cannot be made current", cfg->device);
-    const AttendShape s = shape_of(cfg, a);
-    const int64_t need = joins_bytes(s.ctas) + s.ctas * 2 * attend_slot_floats(s.rows, cfg->head_dim) * 4;
-    if (scratch_bytes < need)
-        return kv_fail(AKASHIC_EINVAL, "kv_attend: scratch needs %lld bytes", (long long)need);
+    const AttendRoute r = route_of(cfg, a);
+    if (scratch_bytes < r.bytes)
+        return kv_fail(AKASHIC_EINVAL, "kv_attend: scratch needs %lld bytes", (long long)r.bytes);
     AttendParams p = {};
     p.cache = (const unsigned char *)cache;
     p.q = a->q, p.q_row = a->q_row_stride, p.q_head = a->q_head_stride;
@@ -960,7 +918,7 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
     p.blocks = a->blocks, p.slopes = a->slopes, p.tags = a->tags, p.q_tags = a->q_tags;
     p.status = status;
     p.joins = (int4 *)scratch;
-    p.partial = (float *)((unsigned char *)scratch + joins_bytes(s.ctas));
+    p.partial = (float *)((unsigned char *)scratch + r.joins);
     p.n_blocks = cfg->n_blocks, p.max_blocks = a->max_blocks;
     p.n_q = a->n_q, p.n_seq = a->n_seq, p.q_heads = a->q_heads, p.heads = cfg->heads;
     p.group = a->q_heads / cfg->heads;
@@ -971,8 +929,17 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
     p.scale = a->scale != 0.f ? a->scale : 1.f / sqrtf((float)cfg->head_dim);
     p.cap = a->cap;
     cudaStream_t st = (cudaStream_t)stream;
-    cudaError_t e = launch_attend_narrow(p, cfg->bits, cfg->head_dim, a->dtype, s, 1, 0x7fffffff, st);
-    if (e == cudaSuccess) e = launch_attend_join(p, a->dtype, cfg->head_dim, s.ctas, s.rows, st);
+    cudaError_t e = cudaSuccess;
+    if (r.narrow.ctas) {
+        e = launch_attend_narrow(p, cfg->bits, cfg->head_dim, a->dtype, r.narrow, 1, WIDE_FROM - 1, st);
+        if (e == cudaSuccess) e = launch_attend_join(p, a->dtype, cfg->head_dim, r.narrow.ctas, r.narrow.rows, st);
+    }
+    if (e == cudaSuccess && r.wide.ctas) {
+        p.joins += r.narrow.ctas;
+        p.partial += r.narrow_floats;
+        e = launch_attend_wide(p, cfg->bits, cfg->head_dim, a->dtype, r.wide, WIDE_FROM, 0x7fffffff, st);
+        if (e == cudaSuccess) e = launch_attend_join(p, a->dtype, cfg->head_dim, r.wide.ctas, r.wide.rows, st);
+    }
     if (e != cudaSuccess)
         return kv_fail(AKASHIC_ECUDA, "kv_attend: launch failed: %s", cudaGetErrorString(e));
     return AKASHIC_OK;

@@ -205,6 +205,64 @@ __host__ __device__ __forceinline__ int64_t attend_slot_floats(int rows, int dim
     return (int64_t)rows * (dim + 2);
 }
 
+// ------------------------------------------------------------------ arithmetic
+constexpr float NEG = -1e30f;                 // "no score yet", finite: no NaN from differences
+constexpr float P_SHIFT = 6.f, M_SLACK = 8.f; // log2 units
+
+__device__ __forceinline__ uint32_t h2fma(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t h2mul(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t h2add(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float scale2(float x, int e) {   // x 2^e, |e| <= 252
+    return x * pow2i(e / 2) * pow2i(e - e / 2);
+}
+
+// Four adjacent-dim (or, after pairing, adjacent-token) pairs of a word of 8
+// nibbles: pair i in h[i].  s: e 2^15 in both halves, s4: s 2^-4, c: -s 2^-21.
+__device__ __forceinline__ void nibbles(uint32_t w, uint32_t s, uint32_t s4, uint32_t c,
+                                        uint32_t (&h)[4]) {
+    const uint32_t w8 = w >> 8;
+    h[0] = h2fma(w & 0x000f000fu, s, c);
+    h[1] = h2fma(w & 0x00f000f0u, s4, c);
+    h[2] = h2fma(w8 & 0x000f000fu, s, c);
+    h[3] = h2fma(w8 & 0x00f000f0u, s4, c);
+}
+constexpr uint32_t H2_M2_21 = 0x80088008u;   // -2^-21, twice
+constexpr uint32_t H2_2_4 = 0x2c002c00u;     // 2^-4, twice
+constexpr uint32_t H2_M1152 = 0xe480e480u;   // -1152, twice
+// Two adjacent values of a result row, and its log-sum-exp.
+__device__ __forceinline__ void store_pair(const AttendParams &p, bool bf16, int64_t at, float a, float b) {
+    if (bf16)
+        *(__nv_bfloat162 *)((__nv_bfloat16 *)p.out + at) = __floats2bfloat162_rn(a, b);
+    else
+        *(uint32_t *)((__half *)p.out + at) = pack_h2(a, b);
+}
+__device__ __forceinline__ float lse_of(float m, float total) {
+    return total == 0.f ? -INFINITY : (m + log2f(total)) * 0.69314718055994530942f;
+}
+
+// ------------------------------------------------------------------ launches
 // Joins what the `ctas` CTAs of a kernel with tiles of `rows` rows left.
 cudaError_t launch_attend_join(const AttendParams &p, int dtype, int dim, int ctas, int rows,
                                cudaStream_t st);
@@ -217,5 +275,8 @@ struct AttendShape {
 AttendShape attend_narrow_shape(int bits, int dim, int max_rows, int sms);
 cudaError_t launch_attend_narrow(const AttendParams &p, int bits, int dim, int dtype,
                                  const AttendShape &shape, int lo, int hi, cudaStream_t st);
+AttendShape attend_wide_shape(int dim, int sms);
+cudaError_t launch_attend_wide(const AttendParams &p, int bits, int dim, int dtype,
+                               const AttendShape &shape, int lo, int hi, cudaStream_t st);
 
 }  // namespace ak

@@ -1,0 +1,793 @@
+// Attention of many query rows (prompts, long drafts) over the quantised cache, on
+// tcgen05.
+//
+// The products bound it: 4 D flops a visible pair.  A CTA takes 256 query rows (two
+// M = 128 tiles; one at D = 256, where an accumulator fills half of the tensor memory) of a
+// sequence and key/value head and runs over tiles of N = 128 tokens (64 at D = 256):
+//   dequantising warps  a unit's codes from global memory into registers, from
+//       there as fp16 into shared memory in the 128-byte swizzle: keys K-major,
+//       values MN-major, which is the same layout (rows of tokens, 64 dims wide).
+//       One pass serves both row tiles;
+//   softmax warps       a thread a row: maximum, weights and total need no
+//       shuffle.  S = Q K^T lies in tensor memory, P (fp16) replaces it in place
+//       and is read from there for O += P V.  One thread of each row tile issues its
+//       products: while one tile's scores are in the softmax, the tensor cores work on
+//       the other's.  (A warp of its own for that would be the 13th, and leave 128
+//       registers a thread instead of 168.)  The weights are computed once
+//       with the maximum so far, held in registers, and only if one exceeds
+//       2^14 is the maximum raised, O rescaled and the pass repeated.
+// Keys are v 2^-9 relative to their unit's largest exponent (its power of two is
+// a factor of the score), values relative to the item's largest so far.
+#include <stddef.h>
+
+#include "ak_attend.cuh"
+#include "ak_sm100.cuh"
+
+namespace ak {
+
+namespace {
+
+template <int D>
+struct Wide {
+    static constexpr int MT = D == 256 ? 1 : 2;          // row tiles of 128
+    static constexpr int ROWS = 128 * MT;
+    static constexpr int N = D == 256 ? 64 : 128;        // tokens of a tile
+    static constexpr int UNITS = N / KV_UNIT;
+    static constexpr int SOFT = 4 * MT, DEQ = 4;         // warps
+    static constexpr int THREADS = 32 * (SOFT + DEQ);
+    static constexpr int UPW = UNITS / DEQ;              // units of a dequantising warp
+    static constexpr int STAGES = 2;
+    static constexpr int Q_BYTES = ROWS * D * 2, KV_BYTES = N * D * 2;
+    static constexpr int S_COL = MT * D;                 // tensor memory: O, then S
+    static constexpr uint32_t TMEM_COLS = 512;
+    static_assert(S_COL + MT * N <= 512, "tensor memory");
+    static constexpr int SMEM = 1024 + Q_BYTES + 2 * STAGES * KV_BYTES;
+};
+
+// What the consumers of a tile need beside the operands.
+template <int N>
+struct alignas(16) Meta {           // pairs of its floats are read at once
+    float kf[N / KV_UNIT];          // factor of a unit's scores
+    float ksig[N], vsig[N];         // 8 bits: significands of the tokens' scales
+    int tag[N];
+    int tok, rv;                    // first token, exponent of the values
+    uint32_t have;                  // units that are listed
+};
+static_assert(offsetof(Meta<64>, ksig) % 8 == 0 && offsetof(Meta<64>, vsig) % 8 == 0 &&
+                  offsetof(Meta<128>, ksig) % 8 == 0 && offsetof(Meta<128>, vsig) % 8 == 0,
+              "pairs");
+
+__device__ __forceinline__ uint64_t f2_pack(float a, float b) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float2 f2_open(uint64_t a) {
+    float2 d;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(a));
+    return d;
+}
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// 32 registers to 32 consecutive columns of the thread's lane, and the wait.
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+        "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+        "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+        "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() {
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+// D[tmem] (+)= A[smem] B[smem]^T and D[tmem] (+)= A[tmem] B[smem], fp16.
+__device__ __forceinline__ void umma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    umma_bf16(d, a, b, idesc, acc);            // the types are in the descriptor
+}
+__device__ __forceinline__ void umma_f16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
+                                            uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+// Instruction descriptor: D fp32, A and B fp16, M = 128.
+constexpr uint32_t idesc_f16(int n) {
+    return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+// Bounded wait of one role; when any role's wait has expired the others give up too.
+__device__ __forceinline__ bool wide_wait(uint64_t *bar, uint32_t parity, volatile int *dead,
+                                          int *status) {
+    for (uint32_t i = 0; i < WAIT_LIMIT; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((i & 255u) == 255u && *dead) return false;
+    }
+    *dead = 1;
+    set_status(status, AKASHIC_ETIMEOUT);
+    return false;
+}
+
+// A unit's codes and scales as a lane holds them (ak_kv.cuh).
+template <int BITS, int D>
+struct UnitRegs {
+    static constexpr int KC = D * BITS / 256, VC = KC;   // 16-byte loads
+    uint4 k[KC], v[VC];
+    uint32_t ks[BITS == 4 ? (D == 256 ? 2 : 1) : 1], vs[BITS == 4 ? (D == 256 ? 2 : 1) : 2];
+    uint32_t ke, ve;
+};
+template <int BITS, int D>
+__device__ __forceinline__ void load_keys(const unsigned char *un, bool have, UnitRegs<BITS, D> &r) {
+    using U = KvUnit<BITS, D>;
+    const int lane = threadIdx.x & 31, g = lane >> 2;
+    if (!have) return;
+#pragma unroll
+    for (int i = 0; i < r.KC; ++i) r.k[i] = __ldg((const uint4 *)(un + U::K_CODES + (i * 32 + lane) * 16));
+    if constexpr (BITS == 4) {
+        if constexpr (D == 64) r.ks[0] = __ldg((const uint16_t *)(un + U::K_SCALES + lane * 2));
+        else if constexpr (D == 128) r.ks[0] = __ldg((const uint32_t *)(un + U::K_SCALES + lane * 4));
+        else {
+            const uint2 x = __ldg((const uint2 *)(un + U::K_SCALES + lane * 8));
+            r.ks[0] = x.x, r.ks[1] = x.y;
+        }
+        r.ke = __ldg((const uint16_t *)(un + U::K_EXP + g * 2));
+    } else {
+        r.ks[0] = __ldg((const uint32_t *)(un + U::K_SCALES + g * 4));
+    }
+}
+template <int BITS, int D>
+__device__ __forceinline__ void load_values(const unsigned char *un, bool have, UnitRegs<BITS, D> &r) {
+    using U = KvUnit<BITS, D>;
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    if (!have) return;
+#pragma unroll
+    for (int i = 0; i < r.VC; ++i) r.v[i] = __ldg((const uint4 *)(un + U::V_CODES + (i * 32 + lane) * 16));
+    if constexpr (BITS == 4) {
+        constexpr int GL = D == 256 ? 2 : 1;
+#pragma unroll
+        for (int i = 0; i < GL; ++i) {
+            const int gr = D == 64 ? g >> 1 : g * GL + i;
+            r.vs[i] = __ldg((const uint32_t *)(un + U::V_SCALES + (gr * 4 + c) * 4));
+        }
+        r.ve = __ldg((const uint32_t *)(un + U::V_EXP + c * 4));
+    } else {
+        const uint2 x = __ldg((const uint2 *)(un + U::V_SCALES + c * 8));
+        r.vs[0] = x.x, r.vs[1] = x.y;
+    }
+}
+// Where dims [d, d + 8) of token t lie in a tile of `rows` tokens (128-byte swizzle).
+__device__ __forceinline__ uint4 *tile_chunk(unsigned char *tile, int rows, int t, int d) {
+    return (uint4 *)(tile + (d >> 6) * (rows * 128) + t * 128 + ((((d & 63) >> 3) ^ (t & 7)) << 4));
+}
+__device__ __forceinline__ uint32_t pow2_h2(int e) {       // 2^e twice in fp16, e <= 0
+    const float f = e < -40 ? 0.f : pow2i(e);
+    return pack_h2(f, f);
+}
+__device__ __forceinline__ uint4 bytes8(uint32_t w0, uint32_t w1, uint32_t f, uint32_t c) {
+    return make_uint4(h2fma(__byte_perm(w0, 0x64646464u, 0x4140), f, c),
+                      h2fma(__byte_perm(w0, 0x64646464u, 0x4342), f, c),
+                      h2fma(__byte_perm(w1, 0x64646464u, 0x4140), f, c),
+                      h2fma(__byte_perm(w1, 0x64646464u, 0x4342), f, c));
+}
+__device__ __forceinline__ uint32_t word_of(const uint4 &x, int i) {
+    return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
+}
+
+template <int BITS, int D>
+__global__ void __launch_bounds__(Wide<D>::THREADS, 1)
+k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int lo, const int hi) {
+    using C = Wide<D>;
+    using U = KvUnit<BITS, D>;
+    constexpr int N = C::N, MT = C::MT, ROWS = C::ROWS, ST = C::STAGES;
+    constexpr int UP = 9;                      // values are staged as v 2^-9 (4 bits)
+    extern __shared__ unsigned char raw_smem[];
+    unsigned char *smem = (unsigned char *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
+    unsigned char *sq_ = smem, *sk = smem + C::Q_BYTES, *sv = sk + ST * C::KV_BYTES;
+    __shared__ Meta<N> meta[ST];
+    __shared__ uint64_t kfull[ST], vfull[ST], empty[ST], sfull[MT], pfull[MT], ofull[MT], drained, texch;
+    __shared__ int tmaxs[2][C::DEQ];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int dead_word;
+    volatile int *dead = &dead_word;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    if (tid == 0) {
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(&kfull[i], 32 * C::DEQ);
+            mbar_init(&vfull[i], 32 * C::DEQ);
+            mbar_init(&empty[i], MT);
+        }
+        for (int t = 0; t < MT; ++t) {
+            mbar_init(&sfull[t], 1);
+            mbar_init(&pfull[t], 128);
+            mbar_init(&ofull[t], 1);
+        }
+        mbar_init(&drained, MT);
+        mbar_init(&texch, C::DEQ);
+        mbar_fence_init();
+        dead_word = 0;
+        p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    }
+    if (warp == 0) {
+        tmem_alloc(&tmem_slot, C::TMEM_COLS);
+        tmem_relinquish();
+    }
+    int64_t *prefix = (int64_t *)sq_;          // until the warps have found their items
+    static_assert(C::Q_BYTES >= (C::THREADS + 1) * 8, "the plan's sums");
+    attend_sums(p, ROWS, N, lo, hi, prefix);
+    const int64_t total = prefix[C::THREADS];
+    const int64_t per = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x);
+    const int64_t first = per * blockIdx.x;
+    int left = (int)max((int64_t)0, min(per, total - first));
+    AttendCursor cur = {};
+    if (left > 0) cur = attend_find(p, ROWS, N, lo, hi, prefix, first);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const bool tags = p.tags != nullptr;
+
+    if (warp >= C::SOFT) {
+        // ---------------- dequantising
+        const int w = warp - C::SOFT, g = lane >> 2, c = lane & 3;
+        uint32_t n_tile = 0;                   // tiles since the kernel began
+        while (left > 0 && !*dead) {
+            const int n = min(cur.units - cur.unit, left), units = (cur.q.kv + KV_UNIT - 1) / KV_UNIT;
+            const int64_t *list = p.blocks + cur.seq * p.max_blocks;
+            constexpr int PER = 32 / C::UPW;   // tiles of a look-up
+            int64_t my_unit = -1, my_slots = 0;
+            auto look_up = [&](int i) {        // lane: tile i + lane / UPW, this warp's unit lane % UPW
+                my_unit = -1;
+                const int tile = i + lane / C::UPW;
+                const int u = (cur.unit + tile) * C::UNITS + w * C::UPW + lane % C::UPW;
+                if (tile < n && u < units) {
+                    const int b = u / p.per_block, x = u - b * p.per_block;
+                    const int64_t id = list[b];
+                    if (id >= 0 && id < p.n_blocks) {
+                        my_slots = id * p.per_block + x;
+                        my_unit = (id * p.heads + cur.head) * p.per_block + x;
+                    } else if (id != -1) {
+                        set_status(p.status, AKASHIC_EDEVICE);
+                    }
+                }
+            };
+            UnitRegs<BITS, D> r[C::UPW];
+            int64_t un[C::UPW];                // of the tile whose registers are being filled
+            int tag_next = 0;
+            auto places = [&](int i) {         // of tile i
+                if (i % PER == 0) look_up(i);
+#pragma unroll
+                for (int j = 0; j < C::UPW; ++j)
+                    un[j] = __shfl_sync(0xffffffffu, my_unit, i % PER * C::UPW + j);
+                if (tags) {                    // lane: the tag of token lane of the warp's units
+                    const int64_t sl = __shfl_sync(0xffffffffu, my_slots, i % PER * C::UPW + (C::UPW == 2 ? lane >> 4 : 0));
+                    const int64_t ok = lane < 16 ? un[0] : un[C::UPW - 1];
+                    tag_next = ok >= 0 && (C::UPW == 2 || lane < 16) ? p.tags[sl * 16 + (lane & 15)] : -1;
+                }
+            };
+            places(0);
+#pragma unroll
+            for (int j = 0; j < C::UPW; ++j) {
+                load_keys<BITS, D>(p.cache + un[j] * U::BYTES, un[j] >= 0, r[j]);
+                load_values<BITS, D>(p.cache + un[j] * U::BYTES, un[j] >= 0, r[j]);
+            }
+            int rv = -127;
+            for (int i = 0; i < n; ++i, ++n_tile) {
+                const int st = n_tile % ST, tok = (cur.unit + i) * N;
+                if (!wide_wait(&empty[st], ((n_tile / ST) & 1) ^ 1, dead, p.status)) break;
+                Meta<N> &m = meta[st];
+                bool have[C::UPW];
+#pragma unroll
+                for (int j = 0; j < C::UPW; ++j) have[j] = un[j] >= 0;
+                // valid tokens of the warp's units, 16 bits each
+                const int lt = w * C::UPW * 16 + lane;     // the lane's token in the tile
+                bool mine = tok + lt < cur.q.kv;
+                if (tags) {
+                    mine = mine && tag_next >= 0;
+                    if (C::UPW == 2 || lane < 16) m.tag[lt] = tag_next;
+                }
+                const uint32_t valid = __ballot_sync(0xffffffffu, mine && (lane < 16 ? have[0] : C::UPW == 2 && have[C::UPW - 1]));
+                // exponents: keys relative to the unit's largest, values to the item's
+                int kt[C::UPW][2], vt[C::UPW][4], vmax = -127;
+                uint32_t kfh[C::UPW][2];
+#pragma unroll
+                for (int j = 0; j < C::UPW; ++j) {
+                    const uint32_t ok = valid >> (16 * j);
+                    if constexpr (BITS == 4) {
+                        kt[j][0] = (int)(r[j].ke & 255u) - 127, kt[j][1] = (int)(r[j].ke >> 8 & 255u) - 127;
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) vt[j][x] = (int)(r[j].ve >> (8 * x) & 255u) - 127;
+                    } else {
+                        kt[j][0] = (int)(r[j].ks[0] >> 7 & 255u) - 127, kt[j][1] = (int)(r[j].ks[0] >> 23 & 255u) - 127;
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) vt[j][x] = (int)(r[j].vs[x >> 1] >> (7 + 16 * (x & 1)) & 255u) - 127;
+                    }
+                    if (!(ok >> g & 1u)) kt[j][0] = -1000;
+                    if (!(ok >> (g + 8) & 1u)) kt[j][1] = -1000;
+                    int km = max(kt[j][0], kt[j][1]);
+                    km = max(km, __shfl_xor_sync(0xffffffffu, km, 4));
+                    km = max(km, __shfl_xor_sync(0xffffffffu, km, 8));
+                    km = max(km, __shfl_xor_sync(0xffffffffu, km, 16));
+                    const int ref = max(km, -126);
+                    kfh[j][0] = pow2_h2(kt[j][0] - ref), kfh[j][1] = pow2_h2(kt[j][1] - ref);
+                    if (lane == 0) m.kf[w * C::UPW + j] = pow2i(ref) * (BITS == 4 ? 512.f : 1.f);
+                    if constexpr (BITS == 8) {
+                        // significands; 1 where there is no token
+                        if (c < 2) {
+                            const uint32_t s = c ? r[j].ks[0] >> 16 : r[j].ks[0];
+                            m.ksig[(w * C::UPW + j) * 16 + g + 8 * c] = (c ? kt[j][1] : kt[j][0]) == -1000 ? 1.f : __uint_as_float((s & 0x7fu) << 16 | 0x3f800000u);
+                        }
+                        if (g < 4) {
+                            const uint32_t s = r[j].vs[g >> 1] >> (16 * (g & 1));
+                            const int t = 2 * c + (g & 1) + (g >> 1) * 8;
+                            m.vsig[(w * C::UPW + j) * 16 + t] = ok >> t & 1u ? __uint_as_float((s & 0x7fu) << 16 | 0x3f800000u) : 1.f;
+                        }
+                    }
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        if (!(ok >> (2 * c + (x & 1) + (x >> 1) * 8) & 1u)) vt[j][x] = -1000;
+                        vmax = max(vmax, vt[j][x]);
+                    }
+                }
+                vmax = max(vmax, __shfl_xor_sync(0xffffffffu, vmax, 1));
+                vmax = max(vmax, __shfl_xor_sync(0xffffffffu, vmax, 2));
+                if (lane == 0) {
+                    tmaxs[n_tile & 1][w] = vmax;
+                    if (w == 0) m.tok = tok, m.have = 0;
+                    mbar_arrive(&texch);
+                }
+                if (!wide_wait(&texch, n_tile & 1, dead, p.status)) break;
+#pragma unroll
+                for (int x = 0; x < C::DEQ; ++x) rv = max(rv, tmaxs[n_tile & 1][x]);
+                if (lane == 0) {
+                    uint32_t bits = 0;
+#pragma unroll
+                    for (int j = 0; j < C::UPW; ++j) bits |= (have[j] ? 1u : 0u) << (w * C::UPW + j);
+                    atomicOr(&m.have, bits);
+                    if (w == 0) m.rv = rv;
+                }
+                // ---- keys
+                unsigned char *kt_ = sk + st * C::KV_BYTES, *vt_ = sv + st * C::KV_BYTES;
+#pragma unroll
+                for (int j = 0; j < C::UPW; ++j) {
+                    const int t0 = (w * C::UPW + j) * 16;
+                    if (!have[j]) {
+                        // nothing listed: the products read zeros
+                        for (int x = lane; x < 16 * (D / 8); x += 32)
+                            *tile_chunk(kt_, N, t0 + x / (D / 8), x % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
+                    } else if constexpr (BITS == 4) {
+                        constexpr int W = D / 32, PERG = D / 64;
+#pragma unroll
+                        for (int i2 = 0; i2 < 2; ++i2)
+#pragma unroll
+                            for (int gr = 0; gr < PERG; ++gr) {
+                                const int b = i2 * PERG + gr;
+                                const uint32_t by = (r[j].ks[b / 4] >> (8 * (b & 3))) & 255u;
+                                const uint32_t s = h2mul(by * 0x00400040u + 0x3c003c00u, kfh[j][i2]);
+                                const uint32_t s4 = h2mul(s, H2_2_4), cc = h2mul(s, H2_M2_21);
+#pragma unroll
+                                for (int q = 0; q < 2; ++q) {
+                                    const int x = gr * 2 + q;      // word of the token
+                                    const int at = D == 64 ? i2 * 2 + x : i2 * W + x;
+                                    uint32_t h[4];
+                                    nibbles(word_of(r[j].k[at / 4], at % 4), s, s4, cc, h);
+                                    *tile_chunk(kt_, N, t0 + g + 8 * i2, c * (D / 4) + x * 8) = make_uint4(h[0], h[1], h[2], h[3]);
+                                }
+                            }
+                    } else {
+                        constexpr int CH = D / 64;
+#pragma unroll
+                        for (int i2 = 0; i2 < 2; ++i2) {
+                            const uint32_t cc = h2mul(kfh[j][i2], H2_M1152);
+#pragma unroll
+                            for (int q = 0; q < CH; ++q) {
+                                const uint4 x = r[j].k[i2 * CH + q];
+                                *tile_chunk(kt_, N, t0 + g + 8 * i2, c * (D / 4) + q * 16) = bytes8(x.x, x.y, kfh[j][i2], cc);
+                                *tile_chunk(kt_, N, t0 + g + 8 * i2, c * (D / 4) + q * 16 + 8) = bytes8(x.z, x.w, kfh[j][i2], cc);
+                            }
+                        }
+                    }
+                }
+                int64_t next[C::UPW];
+#pragma unroll
+                for (int j = 0; j < C::UPW; ++j) next[j] = -1;
+                if (i + 1 < n) {
+                    places(i + 1);
+#pragma unroll
+                    for (int j = 0; j < C::UPW; ++j) {
+                        next[j] = un[j];
+                        load_keys<BITS, D>(p.cache + next[j] * U::BYTES, next[j] >= 0, r[j]);
+                    }
+                }
+                fence_async_smem();
+                mbar_arrive(&kfull[st]);
+                // ---- values
+#pragma unroll
+                for (int j = 0; j < C::UPW; ++j) {
+                    const int t0 = (w * C::UPW + j) * 16;
+                    if (!have[j]) {
+                        for (int x = lane; x < 16 * (D / 8); x += 32)
+                            *tile_chunk(vt_, N, t0 + x / (D / 8), x % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const int t = t0 + 2 * c + (x & 1) + (x >> 1) * 8;
+                            const uint32_t f = pow2_h2(vt[j][x] - rv);
+                            if constexpr (BITS == 4) {
+                                constexpr int W = D / 64, GL = D == 256 ? 2 : 1, WG = W / GL;
+#pragma unroll
+                                for (int gl = 0; gl < GL; ++gl) {
+                                    const uint32_t by = (r[j].vs[gl] >> (8 * x)) & 255u;
+                                    const uint32_t s = h2mul(by * 0x00400040u + 0x3c003c00u, f);
+                                    const uint32_t s4 = h2mul(s, H2_2_4), cc = h2mul(s, H2_M2_21);
+#pragma unroll
+                                    for (int q = 0; q < WG; ++q) {
+                                        const int i3 = gl * WG + q, at = x * W + i3;
+                                        uint32_t h[4];
+                                        nibbles(word_of(r[j].v[at / 4], at % 4), s, s4, cc, h);
+                                        *tile_chunk(vt_, N, t, g * (D / 8) + i3 * 8) = make_uint4(h[0], h[1], h[2], h[3]);
+                                    }
+                                }
+                            } else {
+                                constexpr int W = D / 32;          // words of 4 dims
+                                const uint32_t cc = h2mul(f, H2_M1152);
+#pragma unroll
+                                for (int q = 0; q < W; q += 2) {
+                                    const int at = x * W + q;
+                                    *tile_chunk(vt_, N, t, g * (D / 8) + q * 4) =
+                                        bytes8(word_of(r[j].v[at / 4], at % 4), word_of(r[j].v[(at + 1) / 4], (at + 1) % 4), f, cc);
+                                }
+                            }
+                        }
+                    }
+                }
+                if (i + 1 < n) {
+#pragma unroll
+                    for (int j = 0; j < C::UPW; ++j)
+                        load_values<BITS, D>(p.cache + next[j] * U::BYTES, next[j] >= 0, r[j]);
+                }
+                fence_async_smem();
+                mbar_arrive(&vfull[st]);
+            }
+            left -= n;
+            if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
+        }
+    } else {
+        // ---------------- softmax: warp's lanes are rows 32 (warp % 4) + lane of row tile t
+        const int t = warp >> 2, rt = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_at = tmem + lanes + C::S_COL + t * N, o_at = tmem + lanes + t * D;
+        const float cap_l = p.cap * LOG2E_F, cap_in = p.cap > 0.f ? 2.f / p.cap : 0.f;
+        const bool heavy = p.cap > 0.f || p.slopes;
+        uint32_t n_tile = 0, s_phase = 0, o_phase = 0;
+        bool ok = true;
+        int64_t done = 0;
+        const bool leader = rt == 0;           // issues the row tile's products
+        constexpr uint32_t id_s = idesc_f16(N), id_o = idesc_f16(D) | IDESC_B_MN_MAJOR;
+        // The leader, once all 128 rows have written what it reads: S of tile x.
+        auto issue_scores = [&](uint32_t x) {
+            if (!wide_wait(&kfull[x % ST], (x / ST) & 1, dead, p.status)) return;
+            tc_fence_after();
+            const uint64_t qd = sdesc_sw128(smem_u32(sq_ + t * 128 * D * 2));
+            const uint64_t kd = sdesc_sw128(smem_u32(sk + (x % ST) * C::KV_BYTES));
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                umma_f16(tmem + C::S_COL + t * N, qd + (uint64_t)((k / 4) * (128 * 128) >> 4) + 2 * (k % 4),
+                         kd + (uint64_t)((k / 4) * (N * 128) >> 4) + 2 * (k % 4), id_s, k > 0);
+            umma_commit(&sfull[t]);
+        };
+        auto issue_values = [&](uint32_t x, bool fresh) {
+            if (!wide_wait(&vfull[x % ST], (x / ST) & 1, dead, p.status)) return;
+            tc_fence_after();
+            const uint64_t vd = sdesc_mn_sw128(smem_u32(sv + (x % ST) * C::KV_BYTES), N * 128, 1024);
+#pragma unroll
+            for (int k = 0; k < N / 16; ++k)
+                umma_f16_ta(tmem + t * D, tmem + C::S_COL + t * N + k * 8, vd + (uint64_t)(2048 * k >> 4), id_o,
+                            (!fresh || k > 0) ? 1u : 0u);
+            umma_commit(&empty[x % ST]);
+        };
+        uint32_t p_phase = 0;
+        while (left > 0 && ok && !*dead) {
+            const int n = min(cur.units - cur.unit, left);
+            const AttendSeq sq = cur.q;
+            const int64_t row_first = (int64_t)cur.tile * ROWS;
+            const int rows = (int)min((int64_t)ROWS, (int64_t)sq.nq * p.group - row_first);
+            const int r = t * 128 + rt;
+            if (t == 0 || rows > 128) {
+                // ---- the row's query
+                const bool real = r < rows;
+                const int i = real ? (int)((row_first + r) / p.group) : 0;
+                const int hd = cur.head * p.group + (real ? (int)((row_first + r) - (int64_t)i * p.group) : 0);
+                const uint16_t *src = (const uint16_t *)p.q + (sq.row0 + i) * p.q_row + hd * p.q_head;
+                auto chunk = [&](int d, uint16_t (&x)[8]) {
+                    if (p.q_wide) {
+                        *(uint4 *)x = *(const uint4 *)(src + d);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) x[k] = src[d + k];
+                    }
+                };
+                int e = 0;
+                if (bf16 && real) {
+                    float a = 0.f;
+#pragma unroll 4
+                    for (int d = 0; d < D; d += 8) {
+                        alignas(16) uint16_t x[8];
+                        chunk(d, x);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) a = fmaxf(a, fabsf(bf16_to_f32(x[k])));
+                    }
+                    e = max(-126, min(126, (int)(__float_as_uint(a) >> 23) - 127));
+                }
+                const float by = pow2i(-e);
+#pragma unroll 4
+                for (int d = 0; d < D; d += 8) {
+                    alignas(16) uint16_t x[8];
+                    uint4 y = make_uint4(0, 0, 0, 0);
+                    if (real) {
+                        chunk(d, x);
+                        y = *(const uint4 *)x;
+                        if (bf16)
+                            y = make_uint4(pack_h2(bf16_to_f32(x[0]) * by, bf16_to_f32(x[1]) * by),
+                                           pack_h2(bf16_to_f32(x[2]) * by, bf16_to_f32(x[3]) * by),
+                                           pack_h2(bf16_to_f32(x[4]) * by, bf16_to_f32(x[5]) * by),
+                                           pack_h2(bf16_to_f32(x[6]) * by, bf16_to_f32(x[7]) * by));
+                    }
+                    *tile_chunk(sq_ + t * 128 * D * 2, 128, rt, d) = y;
+                }
+                const float qf = pow2i(e) * p.scale * LOG2E_F;
+                const int limit = real ? attend_limit(p, sq, i) : sq.kv, pos = sq.kv - sq.nq + i;
+                const float slope = real && p.slopes ? p.slopes[hd] * LOG2E_F : 0.f;
+                const int qtag = real && p.q_tags ? p.q_tags[sq.row0 + i] : -1;
+                const int safe = attend_limit(p, sq, (int)((row_first + t * 128) / p.group)) - N;
+                fence_async_smem();
+                mbar_arrive(&pfull[t]);
+                if (leader && wide_wait(&pfull[t], p_phase, dead, p.status)) issue_scores(n_tile);
+                p_phase ^= 1;
+                __syncwarp();
+
+                float mm = 0.f, l = 0.f;
+                bool unset = real;             // no key seen yet: mm = 0
+                int rv = -127;
+                for (int it = 0; it < n; ++it, ++n_tile) {
+                    const int st = n_tile % ST;
+                    ok = wide_wait(&kfull[st], (n_tile / ST) & 1, dead, p.status) &&
+                         wide_wait(&sfull[t], s_phase, dead, p.status);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    s_phase ^= 1;
+                    tc_fence_after();
+                    const Meta<N> &m = meta[st];
+                    const int tok = m.tok;
+                    const uint32_t have = m.have;
+                    const bool masked = tags || tok > safe || have != (1u << C::UNITS) - 1u;
+                    // scores [32 ch, + 32) less the running maximum, in log2 units
+                    auto eval = [&](int ch, float2 (&u)[16]) {
+                        uint32_t x[32];
+                        tmem_ld32(s_at + ch * 32, x);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float f = qf * m.kf[ch * 2 + h];
+                            if (!heavy) {
+                                const uint64_t f2 = f2_pack(f, f), n2 = f2_pack(-mm, -mm);
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) {
+                                    const int col = h * 16 + 2 * k;
+                                    uint64_t z = f2_pack(__uint_as_float(x[col]), __uint_as_float(x[col + 1]));
+                                    if constexpr (BITS == 8) z = f2_mul(z, *(const uint64_t *)&m.ksig[ch * 32 + col]);
+                                    u[h * 8 + k] = f2_open(f2_fma(z, f2, n2));
+                                }
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) {
+                                    const int col = h * 16 + k;
+                                    float z = __uint_as_float(x[col]) * f;
+                                    if constexpr (BITS == 8) z *= m.ksig[ch * 32 + col];
+                                    if (p.cap > 0.f) z = cap_l * (1.f - __fdividef(2.f, 1.f + ex2(z * cap_in)));
+                                    if (p.slopes) z -= slope * (float)abs(pos - (tok + ch * 32 + col));
+                                    (k & 1 ? u[h * 8 + k / 2].y : u[h * 8 + k / 2].x) = z - mm;
+                                }
+                            }
+                        }
+                        if (masked) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) {
+                                bool seen = tok + ch * 32 + k < limit && (have >> (ch * 2 + k / 16) & 1u);
+                                if (tags) {
+                                    const int tg = m.tag[ch * 32 + k];
+                                    seen = seen && tg >= 0 && tg == qtag;
+                                }
+                                if (!seen) (k & 1 ? u[k / 2].y : u[k / 2].x) = -INFINITY;
+                            }
+                        }
+                    };
+                    uint32_t pk[N / 2];
+                    float lt = 0.f, most = 0.f;
+                    auto weights = [&]() {
+                        uint64_t sum = f2_pack(0.f, 0.f);
+                        most = NEG;
+#pragma unroll
+                        for (int ch = 0; ch < N / 32; ++ch) {
+                            float2 u[16];
+                            eval(ch, u);
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {
+                                most = fmaxf(most, fmaxf(u[k].x, u[k].y));
+                                uint64_t e2 = f2_pack(ex2(u[k].x), ex2(u[k].y));
+                                sum = f2_add(sum, e2);
+                                if constexpr (BITS == 8) e2 = f2_mul(e2, *(const uint64_t *)&m.vsig[ch * 32 + 2 * k]);
+                                const float2 y = f2_open(e2);
+                                pk[ch * 16 + k] = pack_h2(y.x, y.y);
+                            }
+                        }
+                        const float2 s2 = f2_open(sum);
+                        lt = s2.x + s2.y;
+                    };
+                    bool again = __any_sync(0xffffffffu, unset);
+                    if (!again) {
+                        weights();
+                        again = __any_sync(0xffffffffu, most > P_SHIFT + M_SLACK);
+                    }
+                    float down = 1.f;          // of what was summed so far
+                    if (again) {
+                        float top = -INFINITY;
+#pragma unroll 1
+                        for (int ch = 0; ch < N / 32; ++ch) {
+                            float2 u[16];
+                            eval(ch, u);
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) top = fmaxf(top, fmaxf(u[k].x, u[k].y));
+                        }
+                        top -= P_SHIFT;
+                        if (unset ? top > -INFINITY : top > 0.f) {
+                            down = unset ? 0.f : ex2(-top);
+                            unset = false;
+                            mm += top;
+                            l *= down;
+                        }
+                        weights();
+                    }
+                    l += lt;
+                    if (m.rv != rv) {
+                        down *= pow2i(max(-126, rv - m.rv));
+                        rv = m.rv;
+                    }
+                    if (it > 0 && __any_sync(0xffffffffu, down != 1.f)) {
+#pragma unroll 1
+                        for (int d = 0; d < D; d += 32) {
+                            uint32_t x[32];
+                            tmem_ld32(o_at + d, x);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * down);
+                            tmem_st32(o_at + d, x);
+                        }
+                    }
+#pragma unroll
+                    for (int ch = 0; ch < N / 64; ++ch) {
+                        uint32_t x[32];
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[k] = pk[ch * 32 + k];
+                        tmem_st32(s_at + ch * 32, x);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    mbar_arrive(&pfull[t]);
+                    if (leader && wide_wait(&pfull[t], p_phase, dead, p.status)) {
+                        issue_values(n_tile, it == 0);
+                        if (it + 1 < n) issue_scores(n_tile + 1);
+                        else umma_commit(&ofull[t]);
+                    }
+                    p_phase ^= 1;
+                    __syncwarp();
+                }
+                if (ok) ok = wide_wait(&ofull[t], o_phase, dead, p.status);
+                ok = __all_sync(0xffffffffu, ok);
+                o_phase ^= 1;
+                if (!ok) break;
+                tc_fence_after();
+                // ---- whole items are written, others left for the joining kernel
+                const bool whole = n == cur.units;
+                if (unset || !real) mm = unset ? NEG : mm;
+                float *part = p.partial + ((int64_t)blockIdx.x * 2 + (cur.unit == 0)) * attend_slot_floats(ROWS, D);
+                const int up = rv + (BITS == 4 ? UP : 0);
+                const float inv = l > 0.f ? 1.f / l : l;
+                const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + hd;
+#pragma unroll 1
+                for (int d = 0; d < D; d += 32) {
+                    uint32_t x[32];
+                    tmem_ld32(o_at + d, x);
+                    tmem_ld_wait();
+                    if (!whole) {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4)
+                            *(float4 *)(part + (int64_t)r * D + d + k) =
+                                make_float4(scale2(__uint_as_float(x[k]), up), scale2(__uint_as_float(x[k + 1]), up),
+                                            scale2(__uint_as_float(x[k + 2]), up), scale2(__uint_as_float(x[k + 3]), up));
+                    } else if (real) {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 2)
+                            store_pair(p, bf16, dst * D + d + k, scale2(__uint_as_float(x[k]) * inv, up),
+                                       scale2(__uint_as_float(x[k + 1]) * inv, up));
+                    }
+                }
+                if (!whole) {
+                    part[ROWS * D + r] = mm, part[ROWS * D + ROWS + r] = l;
+                    if (r == 0 && cur.unit == 0)
+                        p.joins[blockIdx.x] = make_int4(cur.seq, cur.head, cur.tile,
+                                                        (int)((first + done + cur.units - 1) / per));
+                } else if (real && p.lse) {
+                    p.lse[dst] = lse_of(mm, l);
+                }
+                tc_fence_before();
+            } else {
+                // no rows here: the other row tile's alone
+                for (int it = 0; it < n && !*dead; ++it, ++n_tile)
+                    if (leader && wide_wait(&vfull[n_tile % ST], (n_tile / ST) & 1, dead, p.status))
+                        mbar_arrive(&empty[n_tile % ST]);
+                __syncwarp();
+            }
+            left -= n, done += n;
+            if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
+        }
+        if (leader) {                          // what was issued ends before the tensor memory goes
+            umma_commit(&drained);
+            mbar_wait(&drained, 0, p.status);
+        }
+        __syncwarp();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) tmem_dealloc(tmem, C::TMEM_COLS);
+}
+
+template <int BITS, int D>
+cudaError_t run_wide(const AttendParams &p, int dtype, int ctas, int lo, int hi, cudaStream_t st) {
+    using C = Wide<D>;
+    auto *kernel = k_attend_wide<BITS, D>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    if (e != cudaSuccess) return e;
+    kernel<<<ctas, C::THREADS, C::SMEM, st>>>(p, dtype == AKASHIC_DTYPE_BF16, lo, hi);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+AttendShape attend_wide_shape(int dim, int sms) {
+    return {dim == 256 ? Wide<256>::ROWS : Wide<128>::ROWS, sms};
+}
+cudaError_t launch_attend_wide(const AttendParams &p, int bits, int dim, int dtype,
+                               const AttendShape &s, int lo, int hi, cudaStream_t st) {
+    if (bits == 4)
+        return dim == 64 ? run_wide<4, 64>(p, dtype, s.ctas, lo, hi, st)
+               : dim == 128 ? run_wide<4, 128>(p, dtype, s.ctas, lo, hi, st)
+                            : run_wide<4, 256>(p, dtype, s.ctas, lo, hi, st);
+    return dim == 64 ? run_wide<8, 64>(p, dtype, s.ctas, lo, hi, st)
+           : dim == 128 ? run_wide<8, 128>(p, dtype, s.ctas, lo, hi, st)
+                        : run_wide<8, 256>(p, dtype, s.ctas, lo, hi, st);
+}
+
+}  // namespace ak

@@ -1,5 +1,5 @@
 """Plain 64-bit restatement of the quantised cache and its attention (numpy),
-for the tests: the format of include/akashic_mem.h, one row at a time."""
+for the tests: the format of include/akashic_mem.h."""
 import math
 
 import numpy as np
@@ -7,40 +7,29 @@ import numpy as np
 FLT_MAX = float(np.finfo(np.float32).max)
 
 
-def _rne(x):
-    return np.rint(x)                      # half to even
-
-
-def stored_row(x, bits):
-    """The values that the cache stands for after the row x (float64 [D]) is written."""
-    x = np.clip(np.where(np.isnan(x), 0.0, x), -FLT_MAX, FLT_MAX)
-    a = np.abs(x).max()
-    if bits == 8:
-        q = a / 127
-        if q < 2.0 ** -100:
-            s = 2.0 ** -100
-        else:
-            e = math.frexp(q)[1] - 8       # 8 significant bits
-            s = math.ldexp(float(_rne(math.ldexp(q, -e))), e)
-        return np.clip(_rne(x / s), -127, 127) * s
-    t = -100 if a == 0 else min(125, max(-100, math.frexp(a / 7)[1] - 1))
-    out = np.empty_like(x)
-    for g in range(0, len(x), 16):
-        r = np.abs(x[g:g + 16]).max() / 7 / 2.0 ** t
-        if r <= 2.0 ** -15:
-            e = 2.0 ** -15
-        else:
-            u = math.frexp(r)[1] - 5       # 5 significant bits
-            e = min(1.9375, math.ldexp(float(_rne(math.ldexp(r, -u))), u))
-        s = e * 2.0 ** t
-        out[g:g + 16] = np.clip(_rne(x[g:g + 16] / s), -7, 7) * s
-    return out
+def _significant(x, bits):
+    """x >= 0 rounded to so many significant bits, half to even."""
+    unit = np.ldexp(1.0, np.frexp(x)[1] - bits)
+    return np.rint(x / unit) * unit
 
 
 def stored(x, bits):
+    """The values that the cache stands for after the rows x (float64 [..., D]) are
+    written."""
     x = np.asarray(x, np.float64)
-    flat = x.reshape(-1, x.shape[-1])
-    return np.stack([stored_row(r, bits) for r in flat]).reshape(x.shape) if len(flat) else x
+    x = np.clip(np.where(np.isnan(x), 0.0, x), -FLT_MAX, FLT_MAX)
+    if not x.size:
+        return x
+    a = np.abs(x).max(-1, keepdims=True)
+    if bits == 8:
+        s = np.maximum(_significant(a / 127, 8), 2.0 ** -100)
+        return np.clip(np.rint(x / s), -127, 127) * s
+    t = np.where(a == 0, -100, np.clip(np.frexp(a / 7)[1] - 1, -100, 125))
+    g = x.reshape(*x.shape[:-1], -1, 16)
+    r = np.abs(g).max(-1) / 7 / np.ldexp(1.0, t)
+    e = np.clip(_significant(r, 5), 2.0 ** -15, 1.9375)
+    s = (e * np.ldexp(1.0, t))[..., None]
+    return (np.clip(np.rint(g / s), -7, 7) * s).reshape(x.shape)
 
 
 def attend(q, keys, values, blocks, T, kv_len, q_start, *, causal=True, prefix=None, scale=None,
@@ -60,36 +49,43 @@ def attend(q, keys, values, blocks, T, kv_len, q_start, *, causal=True, prefix=N
         tok = np.array([j for j in range(n) if blocks[s][j // T] >= 0], np.int64)
         at = np.array([blocks[s][j // T] * T + j % T for j in tok], np.int64)
         real = at if tags is None else at[tags[at] >= 0]
-        for i in range(r0, r1):
-            pos = n - (r1 - r0) + (i - r0)
-            seen = np.ones(len(tok), bool)
-            if causal:
-                seen &= (tok <= pos) | (tok < (int(prefix[s]) if prefix is not None else 0))
-            if tags is not None:
-                seen &= (tags[at] == q_tags[i]) & (tags[at] >= 0)
-            if not seen.any():
-                continue
-            for hd in range(hq):
-                K, V = keys[at[seen], hd * h // hq], values[at[seen], hd * h // hq]
-                x = q[i, hd]
-                z = scale * (K @ x)
-                if cap:
-                    z = cap * np.tanh(z / cap)
-                away = np.abs(pos - tok[seen])
-                if slopes is not None:
-                    z = z - slopes[hd] * away
-                    zmax[i, hd] = (slopes[hd] * away).max()
-                zmax[i, hd] += np.abs(z).max() + cap
-                m = z.max()
-                p = np.exp(z - m)
-                lse[i, hd] = m + math.log(p.sum())
-                p /= p.sum()
-                out[i, hd] = p @ V
-                weight[i, hd] = p @ np.abs(V)
-                top[i, hd] = np.abs(values[real, hd * h // hq]).max()
-                big[i, hd] = np.abs(V).max(1).sum()
-                reach[i, hd] = abs(scale) * (np.abs(K) @ np.abs(x)).max()
-                small[i, hd] = abs(scale) * np.abs(x).sum() * np.abs(K).max()
+        if r1 == r0:
+            continue
+        pos = n - (r1 - r0) + np.arange(r1 - r0)
+        seen = np.ones((r1 - r0, len(tok)), bool)
+        if causal:
+            first = int(prefix[s]) if prefix is not None else 0
+            seen &= (tok[None] <= pos[:, None]) | (tok[None] < first)
+        if tags is not None:
+            seen &= (tags[at][None] == q_tags[r0:r1, None]) & (tags[at] >= 0)[None]
+        some = seen.any(1)
+        if not some.any():
+            continue
+        away = np.abs(pos[:, None] - tok[None])
+        for hd in range(hq):
+            K, V = keys[at, hd * h // hq], values[at, hd * h // hq]
+            x = q[r0:r1, hd]
+            z = scale * (x @ K.T)
+            if cap:
+                z = cap * np.tanh(z / cap)
+            size = np.abs(z) + cap
+            if slopes is not None:
+                z = z - slopes[hd] * away
+                size = np.abs(z) + cap + slopes[hd] * away
+            z = np.where(seen, z, -np.inf)
+            m = np.where(some, z.max(1, initial=-np.inf), 0.0)
+            p = np.exp(z - m[:, None])
+            total = np.where(some, p.sum(1), 1.0)
+            rows = slice(r0, r1)
+            lse[rows, hd] = np.where(some, m + np.log(total), -np.inf)
+            p /= total[:, None]
+            out[rows, hd] = p @ V
+            weight[rows, hd] = p @ np.abs(V)
+            top[rows, hd] = np.abs(values[real, hd * h // hq]).max(initial=0)
+            big[rows, hd] = seen @ np.abs(V).max(1, initial=0)
+            zmax[rows, hd] = np.where(seen, size, 0).max(1)
+            reach[rows, hd] = abs(scale) * np.where(seen, np.abs(x) @ np.abs(K).T, 0).max(1)
+            small[rows, hd] = abs(scale) * np.abs(x).sum(1) * np.where(seen, np.abs(K).max(1, initial=0)[None], 0).max(1)
     return dict(out=out, lse=lse, weight=weight, top=top, reach=reach, small=small, big=big,
                 z=zmax)
 

@@ -268,6 +268,12 @@ CASES = {
     "sharp": dict(kv=(500,), size=12.0),
     "scaled": dict(kv=(90,), scale=-0.03),
     "block128": dict(kv=(300, 129), T=128),
+    "long_prompt": dict(kv=(400,), nq=(400,), heads=1, group=1, T=64),
+    "wide_group": dict(kv=(333, 40), nq=(90, 90), heads=1, group=3, T=32, causal=False),
+    "few_of_many": dict(kv=(700, 530), nq=(20, 20), heads=1, group=2, T=64),
+    "mixed_rows": dict(kv=(300, 90, 200, 31, 150), nq=(1, 90, 3, 31, 150), heads=1, group=2, tail=3),
+    "long_documents": dict(kv=(520,), nq=(300,), heads=1, group=1, docs=2, prefix=(300,)),
+    "long_cap_slopes": dict(kv=(300,), nq=(140,), heads=1, group=2, cap=6.0, slopes=True, size=2.0),
     "many": dict(kv=tuple(range(1, 300, 7)), heads=1),
 }
 
@@ -282,6 +288,30 @@ def test_attention(name, bits, dim, dtype):
     got = c.attend(q, blocks, **args)
     c.sync()
     _compare(got, want, dim, dtype, bits, rows=n)
+
+
+LONG = {   # many steps for every worker: rings go round, several items in a row, items shared
+    "prompt": dict(kv=(1400, 900), nq=(1400, 700), heads=2, group=2, T=64),
+    "prompt_packed": dict(kv=(2100,), nq=(2100,), heads=2, group=3, T=32, docs=5, prefix=(900,)),
+    "prompt_cap_slopes": dict(kv=(1500, 60), nq=(1200, 60), heads=2, group=2, T=128, cap=9.0,
+                              slopes=True),
+    "mixed": dict(kv=(3000, 800, 1, 1300, 2500), nq=(1, 800, 1, 1, 600), heads=2, group=4, T=32),
+    "decode_long": dict(kv=(60_000, 33, 21_000), heads=3, group=5, T=64),
+    "decode_many": dict(kv=tuple(900 + 37 * i for i in range(60)), heads=4, group=2, T=16),
+    "decode_tags": dict(kv=(20_000, 5_000, 17_777), heads=4, group=1, T=64, docs=3, holes=True),
+    "draft_long": dict(kv=(30_000, 11_111), nq=(3, 3), heads=4, group=4, T=64, slopes=True, cap=15.0),
+}
+
+
+@pytest.mark.parametrize("name", LONG)
+@pytest.mark.parametrize("bits,dim,dtype", [(4, 128, "bf16"), (8, 64, "fp16"), (4, 256, "fp16"),
+                                            (8, 128, "bf16"), (4, 64, "bf16"), (8, 256, "bf16")])
+def test_attention_with_many_steps(name, bits, dim, dtype):
+    kw = LONG[name]
+    c, q, blocks, args, want = _problem(sum(map(ord, name)), bits=bits, dim=dim, dtype=dtype, **kw)
+    got = c.attend(q, blocks, **args)
+    c.sync()
+    _compare(got, want, dim, dtype, bits, rows=sum(kw.get("nq") or (1,) * len(kw["kv"])))
 
 
 def test_attention_rounds_no_small_rows_away():

@@ -13,11 +13,12 @@
 //       and is read from there for O += P V.  One thread of each row tile issues its
 //       products: while one tile's scores are in the softmax, the tensor cores work on
 //       the other's.  (A warp of its own for that would be the 13th, and leave 128
-//       registers a thread instead of 168.)  The weights are computed once
-//       with the maximum so far, held in registers, and only if one exceeds
-//       2^14 is the maximum raised, O rescaled and the pass repeated.
-// Keys are v 2^-9 relative to their unit's largest exponent (its power of two is
-// a factor of the score), values relative to the item's largest so far.
+//       registers a thread instead of 168.)  The row's N scores are read
+//       into registers at once; the maximum is raised, and O rescaled, only when
+//       a weight would exceed 2^14.
+// Keys are v 2^-9 relative to their tile's largest exponent (its power of two is
+// a factor of the scores), values relative to the item's largest so far: where
+// fp16's normal range ends they are rounded to 2^-17 of that largest.
 #include <stddef.h>
 
 #include "ak_attend.cuh"
@@ -47,9 +48,9 @@ struct Wide {
 // What the consumers of a tile need beside the operands.
 template <int N>
 struct alignas(16) Meta {           // pairs of its floats are read at once
-    float kf[N / KV_UNIT];          // factor of a unit's scores
     float ksig[N], vsig[N];         // 8 bits: significands of the tokens' scales
     int tag[N];
+    float kf;                       // factor of the scores
     int tok, rv;                    // first token, exponent of the values
     uint32_t have;                  // units that are listed
 };
@@ -194,6 +195,38 @@ __device__ __forceinline__ uint32_t word_of(const uint4 &x, int i) {
     return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
 }
 
+// cap tanh(x / cap) of a row's scores, in place (log2 units, like cap).  Where all of the
+// warp's are within 0.7 cap: x q(t), t = (x / cap)^2 <= 1/2, q the polynomial of degree 5
+// nearest to tanh(sqrt t) / sqrt t there in relative error (1.5e-8; fitted by
+// iteratively reweighted least squares), two scores an instruction.  Else
+// 1 - 2 / (1 + e^(2y)).
+template <int N>
+__device__ __forceinline__ void cap_scores(uint32_t (&x)[N], float cap) {
+    const float c = 1.f / cap, c2 = 2.f * LOG2E_F * c;
+    float most = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) most = fmaxf(most, fabsf(__uint_as_float(x[k])));
+    if (__all_sync(0xffffffffu, most <= 0.7f * cap)) {
+        const float q[6] = {1.f, -0.3333311080932617f, 0.13328056037425995f, -0.053502924740314484f,
+                            0.019964739680290222f, -0.005034883972257376f};
+        const uint64_t cc = f2_pack(c, c);
+#pragma unroll
+        for (int k = 0; k < N; k += 2) {
+            const uint64_t z = f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+            const uint64_t y = f2_mul(z, cc), t = f2_mul(y, y);
+            uint64_t v = f2_pack(q[5], q[5]);
+#pragma unroll
+            for (int i = 4; i >= 0; --i) v = f2_fma(v, t, f2_pack(q[i], q[i]));
+            const float2 r = f2_open(f2_mul(v, z));
+            x[k] = __float_as_uint(r.x), x[k + 1] = __float_as_uint(r.y);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            x[k] = __float_as_uint(cap * (1.f - __fdividef(2.f, 1.f + ex2(__uint_as_float(x[k]) * c2))));
+    }
+}
+
 template <int BITS, int D>
 __global__ void __launch_bounds__(Wide<D>::THREADS, 1)
 k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int lo, const int hi) {
@@ -206,7 +239,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
     unsigned char *sq_ = smem, *sk = smem + C::Q_BYTES, *sv = sk + ST * C::KV_BYTES;
     __shared__ Meta<N> meta[ST];
     __shared__ uint64_t kfull[ST], vfull[ST], empty[ST], sfull[MT], pfull[MT], ofull[MT], drained, texch;
-    __shared__ int tmaxs[2][C::DEQ];
+    __shared__ int2 tmaxs[2][C::DEQ];          // largest exponents of a warp's keys and values
     __shared__ uint32_t tmem_slot;
     __shared__ int dead_word;
     volatile int *dead = &dead_word;
@@ -305,12 +338,11 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 bool mine = tok + lt < cur.q.kv;
                 if (tags) {
                     mine = mine && tag_next >= 0;
-                    if (C::UPW == 2 || lane < 16) m.tag[lt] = tag_next;
+                    if (C::UPW == 2 || lane < 16) m.tag[lt] = max(tag_next, -1);
                 }
                 const uint32_t valid = __ballot_sync(0xffffffffu, mine && (lane < 16 ? have[0] : C::UPW == 2 && have[C::UPW - 1]));
-                // exponents: keys relative to the unit's largest, values to the item's
-                int kt[C::UPW][2], vt[C::UPW][4], vmax = -127;
-                uint32_t kfh[C::UPW][2];
+                // exponents: keys relative to the tile's largest, values to the item's
+                int kt[C::UPW][2], vt[C::UPW][4], kmax = -126, vmax = -127;
 #pragma unroll
                 for (int j = 0; j < C::UPW; ++j) {
                     const uint32_t ok = valid >> (16 * j);
@@ -325,13 +357,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     }
                     if (!(ok >> g & 1u)) kt[j][0] = -1000;
                     if (!(ok >> (g + 8) & 1u)) kt[j][1] = -1000;
-                    int km = max(kt[j][0], kt[j][1]);
-                    km = max(km, __shfl_xor_sync(0xffffffffu, km, 4));
-                    km = max(km, __shfl_xor_sync(0xffffffffu, km, 8));
-                    km = max(km, __shfl_xor_sync(0xffffffffu, km, 16));
-                    const int ref = max(km, -126);
-                    kfh[j][0] = pow2_h2(kt[j][0] - ref), kfh[j][1] = pow2_h2(kt[j][1] - ref);
-                    if (lane == 0) m.kf[w * C::UPW + j] = pow2i(ref) * (BITS == 4 ? 512.f : 1.f);
+                    kmax = max(kmax, max(kt[j][0], kt[j][1]));
                     if constexpr (BITS == 8) {
                         // significands; 1 where there is no token
                         if (c < 2) {
@@ -352,20 +378,30 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 }
                 vmax = max(vmax, __shfl_xor_sync(0xffffffffu, vmax, 1));
                 vmax = max(vmax, __shfl_xor_sync(0xffffffffu, vmax, 2));
+                kmax = max(kmax, __shfl_xor_sync(0xffffffffu, kmax, 4));
+                kmax = max(kmax, __shfl_xor_sync(0xffffffffu, kmax, 8));
+                kmax = max(kmax, __shfl_xor_sync(0xffffffffu, kmax, 16));
                 if (lane == 0) {
-                    tmaxs[n_tile & 1][w] = vmax;
+                    tmaxs[n_tile & 1][w] = make_int2(kmax, vmax);
                     if (w == 0) m.tok = tok, m.have = 0;
                     mbar_arrive(&texch);
                 }
                 if (!wide_wait(&texch, n_tile & 1, dead, p.status)) break;
 #pragma unroll
-                for (int x = 0; x < C::DEQ; ++x) rv = max(rv, tmaxs[n_tile & 1][x]);
+                for (int x = 0; x < C::DEQ; ++x) {
+                    const int2 y = tmaxs[n_tile & 1][x];
+                    kmax = max(kmax, y.x), rv = max(rv, y.y);
+                }
+                uint32_t kfh[C::UPW][2];
+#pragma unroll
+                for (int j = 0; j < C::UPW; ++j)
+                    kfh[j][0] = pow2_h2(kt[j][0] - kmax), kfh[j][1] = pow2_h2(kt[j][1] - kmax);
                 if (lane == 0) {
                     uint32_t bits = 0;
 #pragma unroll
                     for (int j = 0; j < C::UPW; ++j) bits |= (have[j] ? 1u : 0u) << (w * C::UPW + j);
                     atomicOr(&m.have, bits);
-                    if (w == 0) m.rv = rv;
+                    if (w == 0) m.rv = rv, m.kf = pow2i(kmax) * (BITS == 4 ? 512.f : 1.f);
                 }
                 // ---- keys
                 unsigned char *kt_ = sk + st * C::KV_BYTES, *vt_ = sv + st * C::KV_BYTES;
@@ -478,8 +514,8 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
         const int t = warp >> 2, rt = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + lanes + C::S_COL + t * N, o_at = tmem + lanes + t * D;
-        const float cap_l = p.cap * LOG2E_F, cap_in = p.cap > 0.f ? 2.f / p.cap : 0.f;
-        const bool heavy = p.cap > 0.f || p.slopes;
+        const float cap_l = p.cap * LOG2E_F;
+        const bool heavy = p.cap > 0.f || p.slopes || p.scale < 0.f;   // a mask of -inf wants a factor > 0
         uint32_t n_tile = 0, s_phase = 0, o_phase = 0;
         bool ok = true;
         int64_t done = 0;
@@ -559,7 +595,8 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 const float qf = pow2i(e) * p.scale * LOG2E_F;
                 const int limit = real ? attend_limit(p, sq, i) : sq.kv, pos = sq.kv - sq.nq + i;
                 const float slope = real && p.slopes ? p.slopes[hd] * LOG2E_F : 0.f;
-                const int qtag = real && p.q_tags ? p.q_tags[sq.row0 + i] : -1;
+                // a slot without a token has tag -1 here, and a row that sees none -2
+                const int qt = real && p.q_tags ? p.q_tags[sq.row0 + i] : -2, qtag = qt < 0 ? -2 : qt;
                 const int safe = attend_limit(p, sq, (int)((row_first + t * 128) / p.group)) - N;
                 fence_async_smem();
                 mbar_arrive(&pfull[t]);
@@ -582,94 +619,71 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     const int tok = m.tok;
                     const uint32_t have = m.have;
                     const bool masked = tags || tok > safe || have != (1u << C::UNITS) - 1u;
-                    // scores [32 ch, + 32) less the running maximum, in log2 units
-                    auto eval = [&](int ch, float2 (&u)[16]) {
-                        uint32_t x[32];
-                        tmem_ld32(s_at + ch * 32, x);
-                        tmem_ld_wait();
+                    uint32_t x[N];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float f = qf * m.kf[ch * 2 + h];
-                            if (!heavy) {
-                                const uint64_t f2 = f2_pack(f, f), n2 = f2_pack(-mm, -mm);
+                    for (int ch = 0; ch < N / 32; ++ch)
+                        tmem_ld32(s_at + ch * 32, *(uint32_t(*)[32])(x + ch * 32));
+                    float f = qf * m.kf;       // of the scores, log2 units
+                    tmem_ld_wait();
+                    auto pair = [&](int k) { return f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])); };
+                    auto put = [&](int k, uint64_t v) {
+                        const float2 y = f2_open(v);
+                        x[k] = __float_as_uint(y.x), x[k + 1] = __float_as_uint(y.y);
+                    };
+                    if constexpr (BITS == 8)
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) {
-                                    const int col = h * 16 + 2 * k;
-                                    uint64_t z = f2_pack(__uint_as_float(x[col]), __uint_as_float(x[col + 1]));
-                                    if constexpr (BITS == 8) z = f2_mul(z, *(const uint64_t *)&m.ksig[ch * 32 + col]);
-                                    u[h * 8 + k] = f2_open(f2_fma(z, f2, n2));
-                                }
-                            } else {
+                        for (int k = 0; k < N; k += 2) put(k, f2_mul(pair(k), *(const uint64_t *)&m.ksig[k]));
+                    if (heavy || masked) {
+                        // in place, from here on the factor is 1
 #pragma unroll
-                                for (int k = 0; k < 16; ++k) {
-                                    const int col = h * 16 + k;
-                                    float z = __uint_as_float(x[col]) * f;
-                                    if constexpr (BITS == 8) z *= m.ksig[ch * 32 + col];
-                                    if (p.cap > 0.f) z = cap_l * (1.f - __fdividef(2.f, 1.f + ex2(z * cap_in)));
-                                    if (p.slopes) z -= slope * (float)abs(pos - (tok + ch * 32 + col));
-                                    (k & 1 ? u[h * 8 + k / 2].y : u[h * 8 + k / 2].x) = z - mm;
-                                }
-                            }
+                        for (int k = 0; k < N; k += 2) put(k, f2_mul(pair(k), f2_pack(f, f)));
+                        f = 1.f;
+                        if (p.cap > 0.f) cap_scores<N>(x, cap_l);
+                        if (p.slopes) {
+                            const float away = (float)(pos - tok);
+#pragma unroll
+                            for (int k = 0; k < N; ++k)
+                                x[k] = __float_as_uint(fmaf(-slope, fabsf(away - (float)k), __uint_as_float(x[k])));
                         }
                         if (masked) {
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) {
-                                bool seen = tok + ch * 32 + k < limit && (have >> (ch * 2 + k / 16) & 1u);
-                                if (tags) {
-                                    const int tg = m.tag[ch * 32 + k];
-                                    seen = seen && tg >= 0 && tg == qtag;
-                                }
-                                if (!seen) (k & 1 ? u[k / 2].y : u[k / 2].x) = -INFINITY;
+                            for (int u = 0; u < C::UNITS; ++u) {
+                                const int end = have >> u & 1u ? limit - tok - u * 16 : 0;
+#pragma unroll
+                                for (int k = 0; k < 16; ++k)
+                                    if (k >= end || (tags && m.tag[u * 16 + k] != qtag)) x[u * 16 + k] = 0xff800000u;
                             }
                         }
-                    };
-                    uint32_t pk[N / 2];
-                    float lt = 0.f, most = 0.f;
-                    auto weights = [&]() {
-                        uint64_t sum = f2_pack(0.f, 0.f);
-                        most = NEG;
-#pragma unroll
-                        for (int ch = 0; ch < N / 32; ++ch) {
-                            float2 u[16];
-                            eval(ch, u);
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) {
-                                most = fmaxf(most, fmaxf(u[k].x, u[k].y));
-                                uint64_t e2 = f2_pack(ex2(u[k].x), ex2(u[k].y));
-                                sum = f2_add(sum, e2);
-                                if constexpr (BITS == 8) e2 = f2_mul(e2, *(const uint64_t *)&m.vsig[ch * 32 + 2 * k]);
-                                const float2 y = f2_open(e2);
-                                pk[ch * 16 + k] = pack_h2(y.x, y.y);
-                            }
-                        }
-                        const float2 s2 = f2_open(sum);
-                        lt = s2.x + s2.y;
-                    };
-                    bool again = __any_sync(0xffffffffu, unset);
-                    if (!again) {
-                        weights();
-                        again = __any_sync(0xffffffffu, most > P_SHIFT + M_SLACK);
                     }
+                    float top = __uint_as_float(x[0]);
+#pragma unroll
+                    for (int k = 1; k < N; ++k) top = fmaxf(top, __uint_as_float(x[k]));
+                    top *= f;
+                    // the maximum is raised when a weight would pass 2^14
                     float down = 1.f;          // of what was summed so far
-                    if (again) {
-                        float top = -INFINITY;
-#pragma unroll 1
-                        for (int ch = 0; ch < N / 32; ++ch) {
-                            float2 u[16];
-                            eval(ch, u);
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) top = fmaxf(top, fmaxf(u[k].x, u[k].y));
-                        }
-                        top -= P_SHIFT;
-                        if (unset ? top > -INFINITY : top > 0.f) {
-                            down = unset ? 0.f : ex2(-top);
-                            unset = false;
-                            mm += top;
-                            l *= down;
-                        }
-                        weights();
+                    if (unset ? top > -INFINITY : top - mm > P_SHIFT + M_SLACK) {
+                        down = unset ? 0.f : ex2(mm + P_SHIFT - top);
+                        unset = false;
+                        mm = top - P_SHIFT;
                     }
-                    l += lt;
+                    uint64_t sum[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum[k] = 0;
+                    const uint64_t n2 = f2_pack(-mm, -mm);
+                    uint32_t pk[N / 2];
+#pragma unroll
+                    for (int k = 0; k < N; k += 2) {
+                        const float2 u = f2_open(f2_fma(pair(k), f2_pack(f, f), n2));
+                        uint64_t e2 = f2_pack(ex2(u.x), ex2(u.y));
+                        sum[k / 2 % 4] = f2_add(sum[k / 2 % 4], e2);
+                        if constexpr (BITS == 8) e2 = f2_mul(e2, *(const uint64_t *)&m.vsig[k]);
+                        const float2 y = f2_open(e2);
+                        pk[k / 2] = pack_h2(y.x, y.y);
+                    }
+                    {
+                        const float2 y = f2_open(f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3])));
+                        l = l * down + (y.x + y.y);
+                    }
                     if (m.rv != rv) {
                         down *= pow2i(max(-126, rv - m.rv));
                         rv = m.rv;
@@ -677,21 +691,17 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     if (it > 0 && __any_sync(0xffffffffu, down != 1.f)) {
 #pragma unroll 1
                         for (int d = 0; d < D; d += 32) {
-                            uint32_t x[32];
-                            tmem_ld32(o_at + d, x);
+                            uint32_t y[32];
+                            tmem_ld32(o_at + d, y);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * down);
-                            tmem_st32(o_at + d, x);
+                            for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * down);
+                            tmem_st32(o_at + d, y);
                         }
                     }
 #pragma unroll
-                    for (int ch = 0; ch < N / 64; ++ch) {
-                        uint32_t x[32];
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) x[k] = pk[ch * 32 + k];
-                        tmem_st32(s_at + ch * 32, x);
-                    }
+                    for (int ch = 0; ch < N / 64; ++ch)
+                        tmem_st32(s_at + ch * 32, *(uint32_t(*)[32])(pk + ch * 32));
                     tmem_st_wait();
                     tc_fence_before();
                     mbar_arrive(&pfull[t]);

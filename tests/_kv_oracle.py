@@ -36,7 +36,7 @@ def attend(q, keys, values, blocks, T, kv_len, q_start, *, causal=True, prefix=N
            cap=0.0, slopes=None, tags=None, q_tags=None, n_blocks=None):
     """q [n_q, Hq, D]; keys, values [slots, H, D] (stored values).  Returns out, lse, and
     for the tolerances: weight [n_q, Hq, D] = sum p |v|, top [n_q, Hq] = the largest |v|
-    of the sequence's tokens, reach [n_q, Hq] = the largest |scale| sum_d |q_d k_d| of a seen key (small: sum |q| max |k|), big [n_q, Hq] = sum over seen keys of
+    of the sequence's tokens, reach [n_q, Hq] = the largest |scale| sum_d |q_d k_d| of a seen key (small: sum |q| max |k| over the sequence's tokens), big [n_q, Hq] = sum over seen keys of
     max |v|, z [n_q, Hq] = the largest |z| with the bias' size."""
     n_q, hq, d = q.shape
     h = keys.shape[1]
@@ -85,7 +85,7 @@ def attend(q, keys, values, blocks, T, kv_len, q_start, *, causal=True, prefix=N
             big[rows, hd] = seen @ np.abs(V).max(1, initial=0)
             zmax[rows, hd] = np.where(seen, size, 0).max(1)
             reach[rows, hd] = abs(scale) * np.where(seen, np.abs(x) @ np.abs(K).T, 0).max(1)
-            small[rows, hd] = abs(scale) * np.abs(x).sum(1) * np.where(seen, np.abs(K).max(1, initial=0)[None], 0).max(1)
+            small[rows, hd] = abs(scale) * np.abs(x).sum(1) * np.abs(keys[real, hd * h // hq]).max(initial=0)
     return dict(out=out, lse=lse, weight=weight, top=top, reach=reach, small=small, big=big,
                 z=zmax)
 
@@ -96,7 +96,7 @@ def tolerances(r, d, eps_half, bits):
     Scores: fp32 sums of d exact products and a few factors, (d + 8) 2^-24 of the
     sum of their sizes; a 4-bit key value v is held as v 2^-9 / 2^T in fp16, where the row's
     largest is at least 7 2^T, by two roundings of at most 2^-25: 2^-17 of the row's
-    largest; a bf16 query value below 2^-14 of its row's to 2^-25 of
+    largest (of the tile's, where T is a tile's); a bf16 query value below 2^-14 of its row's to 2^-25 of
     it; cap, bias and the exponential's argument 2^-21 of their sizes.  A score off by t
     makes a weight off by t relative (both in the sum and in the total).  Weights: fp16,
     2^-11, with 2^-30 of the largest as the smallest step; the exponential 2^-21.

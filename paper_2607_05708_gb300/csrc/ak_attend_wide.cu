@@ -8,14 +8,13 @@
 //       there as fp16 into shared memory in the 128-byte swizzle: keys K-major,
 //       values MN-major, which is the same layout (rows of tokens, 64 dims wide).
 //       One pass serves both row tiles;
-//   softmax warps       a thread a row: maximum, weights and total need no
-//       shuffle.  S = Q K^T lies in tensor memory, P (fp16) replaces it in place
+//   softmax warps       two threads a row, in two warps, half of its scores each (with
+//       one the chain from scores to weights took twice as long as the products that
+//       it has to hide behind).  S = Q K^T lies in tensor memory, P (fp16) replaces it in place
 //       and is read from there for O += P V.  One thread of each row tile issues its
 //       products: while one tile's scores are in the softmax, the tensor cores work on
-//       the other's.  (A warp of its own for that would be the 13th, and leave 128
-//       registers a thread instead of 168.)  The row's N scores are read
-//       into registers at once; the maximum is raised, and O rescaled, only when
-//       a weight would exceed 2^14.
+//       the other's.  The scores are read into registers at once; the maximum is
+//       raised, and O rescaled, only when a weight would exceed 2^14.
 // Keys are v 2^-9 relative to their tile's largest exponent (its power of two is
 // a factor of the scores), values relative to the item's largest so far: where
 // fp16's normal range ends they are rounded to 2^-17 of that largest.
@@ -34,7 +33,8 @@ struct Wide {
     static constexpr int ROWS = 128 * MT;
     static constexpr int N = D == 256 ? 64 : 128;        // tokens of a tile
     static constexpr int UNITS = N / KV_UNIT;
-    static constexpr int SOFT = 4 * MT, DEQ = 4;         // warps
+    static constexpr int SOFT = 8 * MT, DEQ = 4;         // warps
+    static constexpr int NH = N / 2, DH = D / 2;         // half a row's scores, half its result
     static constexpr int THREADS = 32 * (SOFT + DEQ);
     static constexpr int UPW = UNITS / DEQ;              // units of a dequantising warp
     static constexpr int STAGES = 2;
@@ -96,6 +96,27 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
         "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
         "r"(r[29]), "r"(r[30]), "r"(r[31])
         : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// Barrier `id` of so many threads; whether any of them says so.
+__device__ __forceinline__ bool bar_any(int id, int threads, bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 q, %3, 0;\n\t"
+        "barrier.cta.red.or.pred p, %1, %2, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r)
+        : "r"(id), "r"(threads), "r"((uint32_t)x)
+        : "memory");
+    return r != 0;
 }
 __device__ __forceinline__ void tmem_st_wait() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -240,6 +261,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
     __shared__ Meta<N> meta[ST];
     __shared__ uint64_t kfull[ST], vfull[ST], empty[ST], sfull[MT], pfull[MT], ofull[MT], drained, texch;
     __shared__ int2 tmaxs[2][C::DEQ];          // largest exponents of a warp's keys and values
+    __shared__ float tops[MT][2][128], totals[MT][2][128];     // what a row's halves tell each other
     __shared__ uint32_t tmem_slot;
     __shared__ int dead_word;
     volatile int *dead = &dead_word;
@@ -253,7 +275,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
         }
         for (int t = 0; t < MT; ++t) {
             mbar_init(&sfull[t], 1);
-            mbar_init(&pfull[t], 128);
+            mbar_init(&pfull[t], 8);
             mbar_init(&ofull[t], 1);
         }
         mbar_init(&drained, MT);
@@ -510,18 +532,20 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
             if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
         }
     } else {
-        // ---------------- softmax: warp's lanes are rows 32 (warp % 4) + lane of row tile t
-        const int t = warp >> 2, rt = (warp & 3) * 32 + lane;
+        // ---------------- softmax: a lane is row 32 (warp % 4) + lane of row tile t and has half
+        // of its scores (and of its result)
+        constexpr int NH = C::NH, DH = C::DH;
+        const int t = warp >> 3, half = warp >> 2 & 1, rt = (warp & 3) * 32 + lane, pair_bar = 1 + t * 4 + (warp & 3);
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_at = tmem + lanes + C::S_COL + t * N, o_at = tmem + lanes + t * D;
+        const uint32_t s_at = tmem + lanes + C::S_COL + t * N, o_at = tmem + lanes + t * D + half * DH;
         const float cap_l = p.cap * LOG2E_F;
         const bool heavy = p.cap > 0.f || p.slopes || p.scale < 0.f;   // a mask of -inf wants a factor > 0
-        uint32_t n_tile = 0, s_phase = 0, o_phase = 0;
-        bool ok = true;
+        uint32_t n_tile = 0, s_phase = 0, o_phase = 0, p_phase = 0;
+        bool ok = true;                        // else go through the motions: the warps meet in barriers
         int64_t done = 0;
-        const bool leader = rt == 0;           // issues the row tile's products
+        const bool leader = rt == 0 && half == 0;      // issues the row tile's products
         constexpr uint32_t id_s = idesc_f16(N), id_o = idesc_f16(D) | IDESC_B_MN_MAJOR;
-        // The leader, once all 128 rows have written what it reads: S of tile x.
+        // The leader, once all rows have written what it reads: S of tile x.
         auto issue_scores = [&](uint32_t x) {
             if (!wide_wait(&kfull[x % ST], (x / ST) & 1, dead, p.status)) return;
             tc_fence_after();
@@ -543,8 +567,16 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                             (!fresh || k > 0) ? 1u : 0u);
             umma_commit(&empty[x % ST]);
         };
-        uint32_t p_phase = 0;
-        while (left > 0 && ok && !*dead) {
+        // All rows of the tile have done their part: the leader goes on.
+        auto all_here = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&pfull[t]);
+            const bool go = leader && ok && wide_wait(&pfull[t], p_phase, dead, p.status);
+            p_phase ^= 1;
+            return go;
+        };
+        while (left > 0) {
+            if (bar_any(pair_bar, 64, !ok || *dead)) break;    // both or neither
             const int n = min(cur.units - cur.unit, left);
             const AttendSeq sq = cur.q;
             const int64_t row_first = (int64_t)cur.tile * ROWS;
@@ -578,7 +610,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 }
                 const float by = pow2i(-e);
 #pragma unroll 4
-                for (int d = 0; d < D; d += 8) {
+                for (int d = half * DH; d < (half + 1) * DH; d += 8) {
                     alignas(16) uint16_t x[8];
                     uint4 y = make_uint4(0, 0, 0, 0);
                     if (real) {
@@ -599,9 +631,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 const int qt = real && p.q_tags ? p.q_tags[sq.row0 + i] : -2, qtag = qt < 0 ? -2 : qt;
                 const int safe = attend_limit(p, sq, (int)((row_first + t * 128) / p.group)) - N;
                 fence_async_smem();
-                mbar_arrive(&pfull[t]);
-                if (leader && wide_wait(&pfull[t], p_phase, dead, p.status)) issue_scores(n_tile);
-                p_phase ^= 1;
+                if (all_here()) issue_scores(n_tile);
                 __syncwarp();
 
                 float mm = 0.f, l = 0.f;
@@ -609,21 +639,21 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 int rv = -127;
                 for (int it = 0; it < n; ++it, ++n_tile) {
                     const int st = n_tile % ST;
-                    ok = wide_wait(&kfull[st], (n_tile / ST) & 1, dead, p.status) &&
-                         wide_wait(&sfull[t], s_phase, dead, p.status);
+                    // what goes with the tile, while its scores are being computed
+                    if (ok) ok = wide_wait(&kfull[st], (n_tile / ST) & 1, dead, p.status);
+                    const Meta<N> &m = meta[st];
+                    const int tok = m.tok, rv_new = m.rv;
+                    const uint32_t have = m.have;
+                    float f = qf * m.kf;       // of the scores, log2 units
+                    const bool masked = tags || tok > safe || have != (1u << C::UNITS) - 1u;
+                    if (ok) ok = wide_wait(&sfull[t], s_phase, dead, p.status);
                     ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
                     s_phase ^= 1;
                     tc_fence_after();
-                    const Meta<N> &m = meta[st];
-                    const int tok = m.tok;
-                    const uint32_t have = m.have;
-                    const bool masked = tags || tok > safe || have != (1u << C::UNITS) - 1u;
-                    uint32_t x[N];
+                    uint32_t x[NH];
 #pragma unroll
-                    for (int ch = 0; ch < N / 32; ++ch)
-                        tmem_ld32(s_at + ch * 32, *(uint32_t(*)[32])(x + ch * 32));
-                    float f = qf * m.kf;       // of the scores, log2 units
+                    for (int ch = 0; ch < NH / 32; ++ch)
+                        tmem_ld32(s_at + half * NH + ch * 32, *(uint32_t(*)[32])(x + ch * 32));
                     tmem_ld_wait();
                     auto pair = [&](int k) { return f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])); };
                     auto put = [&](int k, uint64_t v) {
@@ -632,65 +662,69 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     };
                     if constexpr (BITS == 8)
 #pragma unroll
-                        for (int k = 0; k < N; k += 2) put(k, f2_mul(pair(k), *(const uint64_t *)&m.ksig[k]));
+                        for (int k = 0; k < NH; k += 2) put(k, f2_mul(pair(k), *(const uint64_t *)&m.ksig[half * NH + k]));
                     if (heavy || masked) {
                         // in place, from here on the factor is 1
 #pragma unroll
-                        for (int k = 0; k < N; k += 2) put(k, f2_mul(pair(k), f2_pack(f, f)));
+                        for (int k = 0; k < NH; k += 2) put(k, f2_mul(pair(k), f2_pack(f, f)));
                         f = 1.f;
-                        if (p.cap > 0.f) cap_scores<N>(x, cap_l);
+                        if (p.cap > 0.f) cap_scores<NH>(x, cap_l);
                         if (p.slopes) {
-                            const float away = (float)(pos - tok);
+                            const float away = (float)(pos - tok - half * NH);
 #pragma unroll
-                            for (int k = 0; k < N; ++k)
+                            for (int k = 0; k < NH; ++k)
                                 x[k] = __float_as_uint(fmaf(-slope, fabsf(away - (float)k), __uint_as_float(x[k])));
                         }
                         if (masked) {
 #pragma unroll
-                            for (int u = 0; u < C::UNITS; ++u) {
-                                const int end = have >> u & 1u ? limit - tok - u * 16 : 0;
+                            for (int u = 0; u < NH / 16; ++u) {
+                                const int end = have >> (half * (NH / 16) + u) & 1u ? limit - tok - half * NH - u * 16 : 0;
 #pragma unroll
                                 for (int k = 0; k < 16; ++k)
-                                    if (k >= end || (tags && m.tag[u * 16 + k] != qtag)) x[u * 16 + k] = 0xff800000u;
+                                    if (k >= end || (tags && m.tag[half * NH + u * 16 + k] != qtag)) x[u * 16 + k] = 0xff800000u;
                             }
                         }
                     }
                     float top = __uint_as_float(x[0]);
 #pragma unroll
-                    for (int k = 1; k < N; ++k) top = fmaxf(top, __uint_as_float(x[k]));
+                    for (int k = 1; k < NH; ++k) top = fmaxf(top, __uint_as_float(x[k]));
                     top *= f;
-                    // the maximum is raised when a weight would pass 2^14
+                    // The maximum is raised when a weight would pass 2^14.  The two halves'
+                    // warps meet here in any case: both have read the scores that P replaces.
                     float down = 1.f;          // of what was summed so far
-                    if (unset ? top > -INFINITY : top - mm > P_SHIFT + M_SLACK) {
-                        down = unset ? 0.f : ex2(mm + P_SHIFT - top);
-                        unset = false;
-                        mm = top - P_SHIFT;
+                    if (bar_any(pair_bar, 64, unset || top - mm > P_SHIFT + M_SLACK)) {
+                        tops[t][half][rt] = top;
+                        named_bar(pair_bar, 64);
+                        top = fmaxf(top, tops[t][half ^ 1][rt]);
+                        if (unset ? top > -INFINITY : top - mm > P_SHIFT + M_SLACK) {
+                            down = unset ? 0.f : ex2(mm + P_SHIFT - top);
+                            unset = false;
+                            mm = top - P_SHIFT;
+                        }
                     }
-                    uint64_t sum[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) sum[k] = 0;
+                    uint64_t sum[2] = {0, 0};
                     const uint64_t n2 = f2_pack(-mm, -mm);
-                    uint32_t pk[N / 2];
+                    uint32_t pk[NH / 2];
 #pragma unroll
-                    for (int k = 0; k < N; k += 2) {
+                    for (int k = 0; k < NH; k += 2) {
                         const float2 u = f2_open(f2_fma(pair(k), f2_pack(f, f), n2));
                         uint64_t e2 = f2_pack(ex2(u.x), ex2(u.y));
-                        sum[k / 2 % 4] = f2_add(sum[k / 2 % 4], e2);
-                        if constexpr (BITS == 8) e2 = f2_mul(e2, *(const uint64_t *)&m.vsig[k]);
+                        sum[k / 2 % 2] = f2_add(sum[k / 2 % 2], e2);
+                        if constexpr (BITS == 8) e2 = f2_mul(e2, *(const uint64_t *)&m.vsig[half * NH + k]);
                         const float2 y = f2_open(e2);
                         pk[k / 2] = pack_h2(y.x, y.y);
                     }
                     {
-                        const float2 y = f2_open(f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3])));
+                        const float2 y = f2_open(f2_add(sum[0], sum[1]));
                         l = l * down + (y.x + y.y);
                     }
-                    if (m.rv != rv) {
-                        down *= pow2i(max(-126, rv - m.rv));
-                        rv = m.rv;
+                    if (rv_new != rv) {
+                        down *= pow2i(max(-126, rv - rv_new));
+                        rv = rv_new;
                     }
                     if (it > 0 && __any_sync(0xffffffffu, down != 1.f)) {
 #pragma unroll 1
-                        for (int d = 0; d < D; d += 32) {
+                        for (int d = 0; d < DH; d += 32) {
                             uint32_t y[32];
                             tmem_ld32(o_at + d, y);
                             tmem_ld_wait();
@@ -699,65 +733,68 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                             tmem_st32(o_at + d, y);
                         }
                     }
-#pragma unroll
-                    for (int ch = 0; ch < N / 64; ++ch)
-                        tmem_st32(s_at + ch * 32, *(uint32_t(*)[32])(pk + ch * 32));
+                    if constexpr (NH == 64) tmem_st32(s_at + half * 32, pk);
+                    else tmem_st16(s_at + half * 16, pk);
                     tmem_st_wait();
                     tc_fence_before();
-                    mbar_arrive(&pfull[t]);
-                    if (leader && wide_wait(&pfull[t], p_phase, dead, p.status)) {
+                    if (all_here()) {
                         issue_values(n_tile, it == 0);
                         if (it + 1 < n) issue_scores(n_tile + 1);
                         else umma_commit(&ofull[t]);
                     }
-                    p_phase ^= 1;
                     __syncwarp();
                 }
+                totals[t][half][rt] = l;
+                named_bar(pair_bar, 64);
+                l += totals[t][half ^ 1][rt];
                 if (ok) ok = wide_wait(&ofull[t], o_phase, dead, p.status);
                 ok = __all_sync(0xffffffffu, ok);
                 o_phase ^= 1;
-                if (!ok) break;
                 tc_fence_after();
                 // ---- whole items are written, others left for the joining kernel
                 const bool whole = n == cur.units;
-                if (unset || !real) mm = unset ? NEG : mm;
+                if (unset) mm = NEG;
                 float *part = p.partial + ((int64_t)blockIdx.x * 2 + (cur.unit == 0)) * attend_slot_floats(ROWS, D);
                 const int up = rv + (BITS == 4 ? UP : 0);
                 const float inv = l > 0.f ? 1.f / l : l;
                 const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + hd;
 #pragma unroll 1
-                for (int d = 0; d < D; d += 32) {
-                    uint32_t x[32];
-                    tmem_ld32(o_at + d, x);
+                for (int d = 0; d < DH; d += 32) {
+                    uint32_t y[32];
+                    tmem_ld32(o_at + d, y);
                     tmem_ld_wait();
                     if (!whole) {
 #pragma unroll
                         for (int k = 0; k < 32; k += 4)
-                            *(float4 *)(part + (int64_t)r * D + d + k) =
-                                make_float4(scale2(__uint_as_float(x[k]), up), scale2(__uint_as_float(x[k + 1]), up),
-                                            scale2(__uint_as_float(x[k + 2]), up), scale2(__uint_as_float(x[k + 3]), up));
+                            *(float4 *)(part + (int64_t)r * D + half * DH + d + k) =
+                                make_float4(scale2(__uint_as_float(y[k]), up), scale2(__uint_as_float(y[k + 1]), up),
+                                            scale2(__uint_as_float(y[k + 2]), up), scale2(__uint_as_float(y[k + 3]), up));
                     } else if (real) {
 #pragma unroll
                         for (int k = 0; k < 32; k += 2)
-                            store_pair(p, bf16, dst * D + d + k, scale2(__uint_as_float(x[k]) * inv, up),
-                                       scale2(__uint_as_float(x[k + 1]) * inv, up));
+                            store_pair(p, bf16, dst * D + half * DH + d + k, scale2(__uint_as_float(y[k]) * inv, up),
+                                       scale2(__uint_as_float(y[k + 1]) * inv, up));
                     }
                 }
-                if (!whole) {
-                    part[ROWS * D + r] = mm, part[ROWS * D + ROWS + r] = l;
-                    if (r == 0 && cur.unit == 0)
-                        p.joins[blockIdx.x] = make_int4(cur.seq, cur.head, cur.tile,
-                                                        (int)((first + done + cur.units - 1) / per));
-                } else if (real && p.lse) {
-                    p.lse[dst] = lse_of(mm, l);
+                if (half == 0) {
+                    if (!whole) {
+                        part[ROWS * D + r] = mm, part[ROWS * D + ROWS + r] = l;
+                        if (r == 0 && cur.unit == 0)
+                            p.joins[blockIdx.x] = make_int4(cur.seq, cur.head, cur.tile,
+                                                            (int)((first + done + cur.units - 1) / per));
+                    } else if (real && p.lse) {
+                        p.lse[dst] = lse_of(mm, l);
+                    }
                 }
                 tc_fence_before();
             } else {
-                // no rows here: the other row tile's alone
-                for (int it = 0; it < n && !*dead; ++it, ++n_tile)
-                    if (leader && wide_wait(&vfull[n_tile % ST], (n_tile / ST) & 1, dead, p.status))
-                        mbar_arrive(&empty[n_tile % ST]);
-                __syncwarp();
+                // no rows here: the other row tile's alone.  All warps keep up with
+                // the tiles, so that the parity they wait for next is that of the next phase.
+                for (int it = 0; it < n; ++it, ++n_tile) {
+                    if (ok) ok = wide_wait(&vfull[n_tile % ST], (n_tile / ST) & 1, dead, p.status);
+                    if (ok && leader) mbar_arrive(&empty[n_tile % ST]);
+                }
+                ok = __all_sync(0xffffffffu, ok);
             }
             left -= n, done += n;
             if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);

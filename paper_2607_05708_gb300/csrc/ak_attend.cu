@@ -925,6 +925,7 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
     p.per_block = cfg->block_tokens / KV_UNIT;
     p.max_kv = (int)(a->max_blocks * cfg->block_tokens);
     p.causal = a->causal;
+    p.out_wide = !((uintptr_t)a->out & 15u);
     p.q_wide = !(((uintptr_t)a->q | (uintptr_t)((a->q_row_stride | a->q_head_stride) * 2)) & 15u);
     p.scale = a->scale != 0.f ? a->scale : 1.f / sqrtf((float)cfg->head_dim);
     p.cap = a->cap;

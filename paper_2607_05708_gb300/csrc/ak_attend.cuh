@@ -40,7 +40,7 @@ struct AttendParams {
     int per_block;                    // units of a block
     int max_kv;                       // tokens that the lists can hold
     int causal;
-    bool q_wide;                      // query rows are 16-byte aligned
+    bool q_wide, out_wide;            // query rows, out: 16-byte aligned
     float scale, cap;                 // cap 0: none
 };
 
@@ -77,23 +77,43 @@ __device__ __forceinline__ int attend_limit(const AttendParams &p, const AttendS
 // that order, each of attend_units() steps of `step` tokens, at least one (an
 // item without keys still writes its rows).  A row of a tile is a query row of
 // the sequence and one of the group's heads: r = i * group + head.
+// (rows of a sequence, query rows times group, stay below 2^31)
 __device__ __forceinline__ int attend_tiles(const AttendParams &p, const AttendSeq &q, int rows) {
-    return (int)(((int64_t)q.nq * p.group + rows - 1) / rows);
+    return (int)(((uint32_t)q.nq * (uint32_t)p.group + (uint32_t)rows - 1u) / (uint32_t)rows);
 }
 __device__ __forceinline__ int attend_units(const AttendParams &p, const AttendSeq &q, int tile,
                                             int rows, int step) {
-    const int64_t last = min((int64_t)(tile + 1) * rows, (int64_t)q.nq * p.group) - 1;
-    const int end = attend_limit(p, q, (int)(last / p.group));
-    return max(1, (end + step - 1) / step);
+    const uint32_t all = (uint32_t)q.nq * (uint32_t)p.group;
+    const uint32_t last = min((uint32_t)(tile + 1) * (uint32_t)rows, all) - 1u;
+    const int end = attend_limit(p, q, (int)(last / (uint32_t)p.group));
+    return max(1, (int)(((uint32_t)end + (uint32_t)step - 1u) / (uint32_t)step));
 }
 // Whether a kernel that takes sequences of [lo, hi] rows takes this one.
-__device__ __forceinline__ int64_t attend_seq_units(const AttendParams &p, const AttendSeq &q,
+__device__ __forceinline__ bool attend_takes(const AttendParams &p, const AttendSeq &q, int lo, int hi) {
+    const int n = q.nq * p.group;
+    return n >= lo && n <= hi;
+}
+// The steps of one head of a sequence: every lane's own (s, 0 where it has none).
+// A whole warp calls it: sequences of many tiles are summed up by all lanes.
+__device__ __forceinline__ int64_t attend_seq_units(const AttendParams &p, const AttendSeq &q, bool have,
                                                     int rows, int step, int lo, int hi) {
-    const int64_t n = (int64_t)q.nq * p.group;
-    if (n < lo || n > hi) return 0;
-    const int tiles = attend_tiles(p, q, rows);
+    constexpr int FEW = 4;
+    const int lane = threadIdx.x & 31;
+    const int tiles = have && attend_takes(p, q, lo, hi) ? attend_tiles(p, q, rows) : 0;
     int64_t u = 0;
-    for (int t = 0; t < tiles; ++t) u += attend_units(p, q, t, rows, step);
+    if (tiles <= FEW)
+        for (int t = 0; t < tiles; ++t) u += attend_units(p, q, t, rows, step);
+    for (unsigned many = __ballot_sync(0xffffffffu, tiles > FEW); many; many &= many - 1) {
+        const int l = __ffs(many) - 1;
+        const AttendSeq x = {__shfl_sync(0xffffffffu, q.row0, l), __shfl_sync(0xffffffffu, q.nq, l),
+                             __shfl_sync(0xffffffffu, q.kv, l), __shfl_sync(0xffffffffu, q.prefix, l)};
+        const int n = __shfl_sync(0xffffffffu, tiles, l);
+        int64_t v = 0;
+        for (int t = lane; t < n; t += 32) v += attend_units(p, x, t, rows, step);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane == l) u = v;
+    }
     return u;
 }
 
@@ -114,8 +134,11 @@ __device__ __forceinline__ void attend_sums(const AttendParams &p, int rows, int
     const int nt = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int run = (p.n_seq + nt - 1) / nt;
     int64_t sum = 0;
-    for (int s = tid * run; s < min(p.n_seq, (tid + 1) * run); ++s)
-        sum += attend_seq_units(p, attend_seq(p, s), rows, step, lo, hi) * p.heads;
+    for (int i = 0; i < run; ++i) {
+        const int s = tid * run + i;
+        const bool have = s < p.n_seq;
+        sum += attend_seq_units(p, attend_seq(p, have ? s : 0), have, rows, step, lo, hi) * p.heads;
+    }
     int64_t incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -147,7 +170,8 @@ __device__ __forceinline__ AttendCursor attend_find(const AttendParams &p, int r
     int64_t rest = first - prefix[t], one = 0;   // within that run
     for (int s0 = t * run;; s0 += 32) {
         const int s = s0 + lane;
-        const int64_t w = s < p.n_seq ? attend_seq_units(p, attend_seq(p, s), rows, step, lo, hi) * p.heads : 0;
+        const bool have = s < p.n_seq;
+        const int64_t w = attend_seq_units(p, attend_seq(p, have ? s : 0), have, rows, step, lo, hi) * p.heads;
         int64_t incl = w;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -168,11 +192,25 @@ __device__ __forceinline__ AttendCursor attend_find(const AttendParams &p, int r
     c.q = attend_seq(p, c.seq);
     c.head = (int)(rest / one);
     rest -= c.head * one;
-    c.tile = 0;
-    c.units = attend_units(p, c.q, 0, rows, step);
-    while (rest >= c.units) {
-        rest -= c.units;
-        c.units = attend_units(p, c.q, ++c.tile, rows, step);
+    // the tile, 32 at a time
+    for (const int tiles = attend_tiles(p, c.q, rows); c.tile < tiles; c.tile += 32) {
+        const int t = c.tile + lane;
+        const int w = t < tiles ? attend_units(p, c.q, t, rows, step) : 0;
+        int64_t incl = w;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        const unsigned in = __ballot_sync(0xffffffffu, rest < incl);
+        if (in) {
+            const int l = __ffs(in) - 1;
+            c.tile += l;
+            c.units = __shfl_sync(0xffffffffu, w, l);
+            rest -= __shfl_sync(0xffffffffu, incl, l) - c.units;
+            break;
+        }
+        rest -= __shfl_sync(0xffffffffu, incl, 31);
     }
     c.unit = (int)rest;
     return c;
@@ -185,11 +223,9 @@ __device__ __forceinline__ void attend_next(const AttendParams &p, int rows, int
         c.tile = 0;
         if (++c.head >= p.heads) {
             c.head = 0;
-            int64_t n;
             do {
                 c.q = attend_seq(p, ++c.seq);
-                n = (int64_t)c.q.nq * p.group;
-            } while (c.seq + 1 < p.n_seq && (n < lo || n > hi));
+            } while (c.seq + 1 < p.n_seq && !attend_takes(p, c.q, lo, hi));
         }
     }
     c.units = attend_units(p, c.q, c.tile, rows, step);

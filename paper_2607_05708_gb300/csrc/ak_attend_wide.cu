@@ -8,13 +8,14 @@
 //       there as fp16 into shared memory in the 128-byte swizzle: keys K-major,
 //       values MN-major, which is the same layout (rows of tokens, 64 dims wide).
 //       One pass serves both row tiles;
-//   softmax warps       two threads a row, in two warps, half of its scores each (with
-//       one the chain from scores to weights took twice as long as the products that
-//       it has to hide behind).  S = Q K^T lies in tensor memory, P (fp16) replaces it in place
-//       and is read from there for O += P V.  One thread of each row tile issues its
-//       products: while one tile's scores are in the softmax, the tensor cores work on
-//       the other's.  The scores are read into registers at once; the maximum is
-//       raised, and O rescaled, only when a weight would exceed 2^14.
+//   issuing thread      S = Q K^T into tensor memory, O += P V with P from there.  While
+//       one row tile's scores are in the softmax, the tensor cores work on the
+//       other's.  (At D = 256 on the next 64 tokens' scores; at D <= 128 S = 128 x 64
+//       would take as long as 128 x 128: 75 and 64 cycles for 16 dims.)  It waits
+//       by polling: mbarrier.try_wait costs some 200 cycles even on a phase that is over;
+//   softmax warps       a thread a row, 64 scores at a time: maximum, weights and total
+//       need no shuffle.  P (fp16) replaces its scores.  The maximum is raised,
+//       and O rescaled, only when a weight would exceed 2^14.
 // Keys are v 2^-9 relative to their tile's largest exponent (its power of two is
 // a factor of the scores), values relative to the item's largest so far: where
 // fp16's normal range ends they are rounded to 2^-17 of that largest.
@@ -33,15 +34,16 @@ struct Wide {
     static constexpr int ROWS = 128 * MT;
     static constexpr int N = D == 256 ? 64 : 128;        // tokens of a tile
     static constexpr int UNITS = N / KV_UNIT;
-    static constexpr int SOFT = 8 * MT, DEQ = 4;         // warps
-    static constexpr int NH = N / 2, DH = D / 2;         // half a row's scores, half its result
-    static constexpr int THREADS = 32 * (SOFT + DEQ);
+    static constexpr int HT = 64, HPT = N / HT;          // tokens the softmax takes at a time
+    static constexpr int SN = MT == 2 ? N : HT;          // columns of S computed at once
+    static constexpr int SOFT = 4 * MT, DEQ = 4;         // warps, and one that issues
+    static constexpr int THREADS = 32 * (SOFT + DEQ + 1);
     static constexpr int UPW = UNITS / DEQ;              // units of a dequantising warp
     static constexpr int STAGES = 2;
     static constexpr int Q_BYTES = ROWS * D * 2, KV_BYTES = N * D * 2;
     static constexpr int S_COL = MT * D;                 // tensor memory: O, then S
     static constexpr uint32_t TMEM_COLS = 512;
-    static_assert(S_COL + MT * N <= 512, "tensor memory");
+    static_assert(S_COL + MT * 2 * HT <= 512, "tensor memory");
     static constexpr int SMEM = 1024 + Q_BYTES + 2 * STAGES * KV_BYTES;
 };
 
@@ -97,27 +99,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
         "r"(r[29]), "r"(r[30]), "r"(r[31])
         : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
-}
-// Barrier `id` of so many threads; whether any of them says so.
-__device__ __forceinline__ bool bar_any(int id, int threads, bool x) {
-    uint32_t r;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.u32 q, %3, 0;\n\t"
-        "barrier.cta.red.or.pred p, %1, %2, q;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(r)
-        : "r"(id), "r"(threads), "r"((uint32_t)x)
-        : "memory");
-    return r != 0;
-}
 __device__ __forceinline__ void tmem_st_wait() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
@@ -142,9 +123,9 @@ constexpr uint32_t idesc_f16(int n) {
 // Bounded wait of one role; when any role's wait has expired the others give up too.
 __device__ __forceinline__ bool wide_wait(uint64_t *bar, uint32_t parity, volatile int *dead,
                                           int *status) {
-    for (uint32_t i = 0; i < WAIT_LIMIT; ++i) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if ((i & 255u) == 255u && *dead) return false;
+    for (uint32_t i = 0; i < SPIN_LIMIT; ++i) {
+        if (mbar_test_wait(bar, parity)) return true;
+        if ((i & 1023u) == 1023u && *dead) return false;
     }
     *dead = 1;
     set_status(status, AKASHIC_ETIMEOUT);
@@ -216,6 +197,29 @@ __device__ __forceinline__ uint32_t word_of(const uint4 &x, int i) {
     return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
 }
 
+// 32 values of a result row; 16 bytes a store where out is so aligned (rows are).
+__device__ __forceinline__ void store_row32(const AttendParams &p, bool bf16, int64_t at, const uint32_t (&y)[32]) {
+    uint32_t h[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const float a = __uint_as_float(y[2 * k]), b = __uint_as_float(y[2 * k + 1]);
+        if (bf16) {
+            const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+            h[k] = *(const uint32_t *)&v;
+        } else {
+            h[k] = pack_h2(a, b);
+        }
+    }
+    uint32_t *dst = (uint32_t *)((uint16_t *)p.out + at);
+    if (p.out_wide) {
+#pragma unroll
+        for (int k = 0; k < 16; k += 4) *(uint4 *)(dst + k) = make_uint4(h[k], h[k + 1], h[k + 2], h[k + 3]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) dst[k] = h[k];
+    }
+}
+
 // cap tanh(x / cap) of a row's scores, in place (log2 units, like cap).  Where all of the
 // warp's are within 0.7 cap: x q(t), t = (x / cap)^2 <= 1/2, q the polynomial of degree 5
 // nearest to tanh(sqrt t) / sqrt t there in relative error (1.5e-8; fitted by
@@ -253,15 +257,16 @@ __global__ void __launch_bounds__(Wide<D>::THREADS, 1)
 k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int lo, const int hi) {
     using C = Wide<D>;
     using U = KvUnit<BITS, D>;
-    constexpr int N = C::N, MT = C::MT, ROWS = C::ROWS, ST = C::STAGES;
+    constexpr int N = C::N, MT = C::MT, ROWS = C::ROWS, ST = C::STAGES, HT = C::HT, HPT = C::HPT;
     constexpr int UP = 9;                      // values are staged as v 2^-9 (4 bits)
     extern __shared__ unsigned char raw_smem[];
     unsigned char *smem = (unsigned char *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
     unsigned char *sq_ = smem, *sk = smem + C::Q_BYTES, *sv = sk + ST * C::KV_BYTES;
     __shared__ Meta<N> meta[ST];
-    __shared__ uint64_t kfull[ST], vfull[ST], empty[ST], sfull[MT], pfull[MT], ofull[MT], drained, texch;
+    __shared__ uint64_t kfull[ST], vfull[ST], empty[ST];      // tiles: keys, values, both read
+    __shared__ uint64_t sfull[MT][2], pfull[MT][2], odone[MT][2], qfull[MT], drained, texch;
     __shared__ int2 tmaxs[2][C::DEQ];          // largest exponents of a warp's keys and values
-    __shared__ float tops[MT][2][128], totals[MT][2][128];     // what a row's halves tell each other
+    __shared__ float qscale[ROWS];
     __shared__ uint32_t tmem_slot;
     __shared__ int dead_word;
     volatile int *dead = &dead_word;
@@ -271,14 +276,19 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
         for (int i = 0; i < ST; ++i) {
             mbar_init(&kfull[i], 32 * C::DEQ);
             mbar_init(&vfull[i], 32 * C::DEQ);
-            mbar_init(&empty[i], MT);
+            mbar_init(&empty[i], 1);
         }
         for (int t = 0; t < MT; ++t) {
-            mbar_init(&sfull[t], 1);
-            mbar_init(&pfull[t], 8);
-            mbar_init(&ofull[t], 1);
+            // One a buffer: two halves may be under way, and a wait knows only the
+            // last phase from the one before it.
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(&sfull[t][b], 1);
+                mbar_init(&pfull[t][b], 4);
+                mbar_init(&odone[t][b], 1);
+            }
+            mbar_init(&qfull[t], 4);
         }
-        mbar_init(&drained, MT);
+        mbar_init(&drained, 1);
         mbar_init(&texch, C::DEQ);
         mbar_fence_init();
         dead_word = 0;
@@ -303,7 +313,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
     const uint32_t tmem = tmem_slot;
     const bool tags = p.tags != nullptr;
 
-    if (warp >= C::SOFT) {
+    if (warp >= C::SOFT && warp < C::SOFT + C::DEQ) {
         // ---------------- dequantising
         const int w = warp - C::SOFT, g = lane >> 2, c = lane & 3;
         uint32_t n_tile = 0;                   // tiles since the kernel began
@@ -531,129 +541,157 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
             left -= n;
             if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
         }
+    } else if (warp == C::SOFT + C::DEQ) {
+        // ---------------- issuing
+        if (lane == 0) {
+            constexpr uint32_t id_s = idesc_f16(C::SN), id_o = idesc_f16(D) | IDESC_B_MN_MAJOR;
+            uint32_t n_tile = 0, halves[MT] = {}, q_phase = 0;     // halves: of the row tile, so far
+            bool ok = true;
+            // S of half h of the item (its first tile: n_tile) for row tile t; at D <= 128
+            // (h even) of the whole tile
+            auto scores = [&](int t, int h) {
+                const uint32_t x = n_tile + h / HPT, b = (halves[t] + h) & 1;
+                if (!ok) return;
+                // the row tiles share a tile's keys
+                if (t == 0 && !(ok = wide_wait(&kfull[x % ST], (x / ST) & 1, dead, p.status))) return;
+                tc_fence_after();
+                const uint64_t qd = sdesc_sw128(smem_u32(sq_ + t * 128 * D * 2));
+                const uint64_t kd = sdesc_sw128(smem_u32(sk + (x % ST) * C::KV_BYTES));
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    umma_f16(tmem + C::S_COL + (t * 2 + b) * HT, qd + (uint64_t)((k / 4) * (128 * 128) >> 4) + 2 * (k % 4),
+                             kd + (uint64_t)((k / 4) * (N * 128) >> 4) + 2 * (k % 4), id_s, k > 0);
+                umma_commit(&sfull[t][b]);
+            };
+            auto values = [&](int t, int h) {
+                const uint32_t x = n_tile + h / HPT, b = (halves[t] + h) & 1;
+                if (!ok) return;
+                if (t == 0 && h % HPT == 0 && !(ok = wide_wait(&vfull[x % ST], (x / ST) & 1, dead, p.status))) return;
+                if (!(ok = wide_wait(&pfull[t][b], (halves[t] + h) >> 1 & 1, dead, p.status))) return;
+                tc_fence_after();
+                const uint64_t vd = sdesc_mn_sw128(smem_u32(sv + (x % ST) * C::KV_BYTES + h % HPT * HT * 128), N * 128, 1024);
+#pragma unroll
+                for (int k = 0; k < HT / 16; ++k)
+                    umma_f16_ta(tmem + t * D, tmem + C::S_COL + (t * 2 + b) * HT + k * 8, vd + (uint64_t)(2048 * k >> 4),
+                                id_o, (h > 0 || k > 0) ? 1u : 0u);
+                umma_commit(&odone[t][b]);
+            };
+            while (left > 0 && ok) {
+                const int n = min(cur.units - cur.unit, left), nh = n * HPT;
+                const int mt = cur.q.nq * p.group - cur.tile * ROWS > 128 ? MT : 1;
+                for (int t = 0; ok && t < mt; ++t) {
+                    ok = wide_wait(&qfull[t], q_phase >> t & 1, dead, p.status);
+                    q_phase ^= 1u << t;
+                    scores(t, 0);
+                }
+                for (int h = 0; ok && h < nh; ++h)
+                    for (int t = 0; t < mt; ++t) {
+                        // two buffers of one row tile: the next half's scores come first
+                        if (HPT == 1 && h + 1 < nh) scores(t, h + 1);
+                        values(t, h);
+                        if (h % HPT < HPT - 1) continue;
+                        if (ok && t == mt - 1) umma_commit(&empty[(n_tile + h / HPT) % ST]);
+                        if (HPT == 2 && h + 1 < nh) scores(t, h + 1);
+                    }
+                for (int t = 0; t < mt; ++t) halves[t] += nh;
+                n_tile += n;
+                left -= n;
+                if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
+            }
+            umma_commit(&drained);             // what was issued ends before the tensor memory goes
+            mbar_wait(&drained, 0, p.status);
+        }
+        __syncwarp();
     } else {
-        // ---------------- softmax: a lane is row 32 (warp % 4) + lane of row tile t and has half
-        // of its scores (and of its result)
-        constexpr int NH = C::NH, DH = C::DH;
-        const int t = warp >> 3, half = warp >> 2 & 1, rt = (warp & 3) * 32 + lane, pair_bar = 1 + t * 4 + (warp & 3);
+        // ---------------- softmax: a lane is row 32 (warp % 4) + lane of row tile t
+        const int t = warp >> 2, rt = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_at = tmem + lanes + C::S_COL + t * N, o_at = tmem + lanes + t * D + half * DH;
+        const uint32_t o_at = tmem + lanes + t * D;
         const float cap_l = p.cap * LOG2E_F;
         const bool heavy = p.cap > 0.f || p.slopes || p.scale < 0.f;   // a mask of -inf wants a factor > 0
-        uint32_t n_tile = 0, s_phase = 0, o_phase = 0, p_phase = 0;
-        bool ok = true;                        // else go through the motions: the warps meet in barriers
+        uint32_t n_tile = 0, halves = 0;       // halves: of this row tile, so far
+        bool ok = true;
         int64_t done = 0;
-        const bool leader = rt == 0 && half == 0;      // issues the row tile's products
-        constexpr uint32_t id_s = idesc_f16(N), id_o = idesc_f16(D) | IDESC_B_MN_MAJOR;
-        // The leader, once all rows have written what it reads: S of tile x.
-        auto issue_scores = [&](uint32_t x) {
-            if (!wide_wait(&kfull[x % ST], (x / ST) & 1, dead, p.status)) return;
-            tc_fence_after();
-            const uint64_t qd = sdesc_sw128(smem_u32(sq_ + t * 128 * D * 2));
-            const uint64_t kd = sdesc_sw128(smem_u32(sk + (x % ST) * C::KV_BYTES));
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                umma_f16(tmem + C::S_COL + t * N, qd + (uint64_t)((k / 4) * (128 * 128) >> 4) + 2 * (k % 4),
-                         kd + (uint64_t)((k / 4) * (N * 128) >> 4) + 2 * (k % 4), id_s, k > 0);
-            umma_commit(&sfull[t]);
-        };
-        auto issue_values = [&](uint32_t x, bool fresh) {
-            if (!wide_wait(&vfull[x % ST], (x / ST) & 1, dead, p.status)) return;
-            tc_fence_after();
-            const uint64_t vd = sdesc_mn_sw128(smem_u32(sv + (x % ST) * C::KV_BYTES), N * 128, 1024);
-#pragma unroll
-            for (int k = 0; k < N / 16; ++k)
-                umma_f16_ta(tmem + t * D, tmem + C::S_COL + t * N + k * 8, vd + (uint64_t)(2048 * k >> 4), id_o,
-                            (!fresh || k > 0) ? 1u : 0u);
-            umma_commit(&empty[x % ST]);
-        };
-        // All rows of the tile have done their part: the leader goes on.
-        auto all_here = [&]() {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&pfull[t]);
-            const bool go = leader && ok && wide_wait(&pfull[t], p_phase, dead, p.status);
-            p_phase ^= 1;
-            return go;
-        };
-        while (left > 0) {
-            if (bar_any(pair_bar, 64, !ok || *dead)) break;    // both or neither
+        while (left > 0 && ok) {
             const int n = min(cur.units - cur.unit, left);
             const AttendSeq sq = cur.q;
-            const int64_t row_first = (int64_t)cur.tile * ROWS;
-            const int rows = (int)min((int64_t)ROWS, (int64_t)sq.nq * p.group - row_first);
+            const int row_first = cur.tile * ROWS, rows = min(ROWS, sq.nq * p.group - row_first);
             const int r = t * 128 + rt;
             if (t == 0 || rows > 128) {
-                // ---- the row's query
-                const bool real = r < rows;
-                const int i = real ? (int)((row_first + r) / p.group) : 0;
-                const int hd = cur.head * p.group + (real ? (int)((row_first + r) - (int64_t)i * p.group) : 0);
-                const uint16_t *src = (const uint16_t *)p.q + (sq.row0 + i) * p.q_row + hd * p.q_head;
-                auto chunk = [&](int d, uint16_t (&x)[8]) {
-                    if (p.q_wide) {
-                        *(uint4 *)x = *(const uint4 *)(src + d);
-                    } else {
+                // ---- the warp's 32 query rows, 16 bytes a lane: bf16 scaled by a power of two
+                // to a largest magnitude in [1, 2)
+                constexpr int CH = D / 8, RP = 32 / CH;
+#pragma unroll 8
+                for (int y = 0; y < CH; ++y) {
+                    const int row = (warp & 3) * 32 + y * RP + lane / CH, ch = lane % CH;
+                    const bool have = t * 128 + row < rows;
+                    const int at = row_first + t * 128 + row, i = have ? at / p.group : 0;
+                    const int hd = cur.head * p.group + (have ? at - i * p.group : 0);
+                    const uint16_t *src = (const uint16_t *)p.q + (sq.row0 + i) * p.q_row + hd * p.q_head + ch * 8;
+                    alignas(16) uint16_t x[8];
+                    *(uint4 *)x = make_uint4(0, 0, 0, 0);
+                    if (have) {
+                        if (p.q_wide) {
+                            *(uint4 *)x = *(const uint4 *)src;
+                        } else {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) x[k] = src[d + k];
+                            for (int k = 0; k < 8; ++k) x[k] = src[k];
+                        }
                     }
-                };
-                int e = 0;
-                if (bf16 && real) {
-                    float a = 0.f;
-#pragma unroll 4
-                    for (int d = 0; d < D; d += 8) {
-                        alignas(16) uint16_t x[8];
-                        chunk(d, x);
+                    uint4 z = *(const uint4 *)x;
+                    float up = 1.f;
+                    if (bf16) {
+                        float a = 0.f;
 #pragma unroll
                         for (int k = 0; k < 8; ++k) a = fmaxf(a, fabsf(bf16_to_f32(x[k])));
+#pragma unroll
+                        for (int o = CH / 2; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+                        const int e = max(-126, min(126, (int)(__float_as_uint(a) >> 23) - 127));
+                        const float by = pow2i(-e);
+                        up = pow2i(e);
+                        z = make_uint4(pack_h2(bf16_to_f32(x[0]) * by, bf16_to_f32(x[1]) * by),
+                                       pack_h2(bf16_to_f32(x[2]) * by, bf16_to_f32(x[3]) * by),
+                                       pack_h2(bf16_to_f32(x[4]) * by, bf16_to_f32(x[5]) * by),
+                                       pack_h2(bf16_to_f32(x[6]) * by, bf16_to_f32(x[7]) * by));
                     }
-                    e = max(-126, min(126, (int)(__float_as_uint(a) >> 23) - 127));
+                    *tile_chunk(sq_ + t * 128 * D * 2, 128, row, ch * 8) = z;
+                    if (ch == 0) qscale[t * 128 + row] = up;
                 }
-                const float by = pow2i(-e);
-#pragma unroll 4
-                for (int d = half * DH; d < (half + 1) * DH; d += 8) {
-                    alignas(16) uint16_t x[8];
-                    uint4 y = make_uint4(0, 0, 0, 0);
-                    if (real) {
-                        chunk(d, x);
-                        y = *(const uint4 *)x;
-                        if (bf16)
-                            y = make_uint4(pack_h2(bf16_to_f32(x[0]) * by, bf16_to_f32(x[1]) * by),
-                                           pack_h2(bf16_to_f32(x[2]) * by, bf16_to_f32(x[3]) * by),
-                                           pack_h2(bf16_to_f32(x[4]) * by, bf16_to_f32(x[5]) * by),
-                                           pack_h2(bf16_to_f32(x[6]) * by, bf16_to_f32(x[7]) * by));
-                    }
-                    *tile_chunk(sq_ + t * 128 * D * 2, 128, rt, d) = y;
-                }
-                const float qf = pow2i(e) * p.scale * LOG2E_F;
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&qfull[t]);
+                const bool real = r < rows;
+                const int i = real ? (row_first + r) / p.group : 0;
+                const int hd = cur.head * p.group + (real ? row_first + r - i * p.group : 0);
+                const float qf = qscale[r] * p.scale * LOG2E_F;
                 const int limit = real ? attend_limit(p, sq, i) : sq.kv, pos = sq.kv - sq.nq + i;
                 const float slope = real && p.slopes ? p.slopes[hd] * LOG2E_F : 0.f;
                 // a slot without a token has tag -1 here, and a row that sees none -2
                 const int qt = real && p.q_tags ? p.q_tags[sq.row0 + i] : -2, qtag = qt < 0 ? -2 : qt;
-                const int safe = attend_limit(p, sq, (int)((row_first + t * 128) / p.group)) - N;
-                fence_async_smem();
-                if (all_here()) issue_scores(n_tile);
-                __syncwarp();
+                const int safe = attend_limit(p, sq, (row_first + t * 128) / p.group) - HT;
 
                 float mm = 0.f, l = 0.f;
                 bool unset = real;             // no key seen yet: mm = 0
                 int rv = -127;
-                for (int it = 0; it < n; ++it, ++n_tile) {
-                    const int st = n_tile % ST;
-                    // what goes with the tile, while its scores are being computed
-                    if (ok) ok = wide_wait(&kfull[st], (n_tile / ST) & 1, dead, p.status);
+                for (int h = 0; h < n * HPT; ++h, ++halves) {
+                    const uint32_t x_tile = n_tile + h / HPT, st = x_tile % ST, b = halves & 1;
+                    const uint32_t s_at = tmem + lanes + C::S_COL + (t * 2 + b) * HT;
+                    if (h % HPT == 0) {
+                        ok = wide_wait(&sfull[t][b], halves >> 1 & 1, dead, p.status);
+                        // complete by now; what the dequantising warps wrote beside the tile
+                        if (ok) ok = wide_wait(&kfull[st], (x_tile / ST) & 1, dead, p.status);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        tc_fence_after();
+                    }
+                    uint32_t x[HT];
+                    tmem_ld32(s_at, *(uint32_t(*)[32])x);
+                    tmem_ld32(s_at + 32, *(uint32_t(*)[32])(x + 32));
                     const Meta<N> &m = meta[st];
-                    const int tok = m.tok, rv_new = m.rv;
-                    const uint32_t have = m.have;
+                    const int half = h % HPT * HT, tok = m.tok + half;
+                    const uint32_t have = m.have >> (half / KV_UNIT) & 15u;
                     float f = qf * m.kf;       // of the scores, log2 units
-                    const bool masked = tags || tok > safe || have != (1u << C::UNITS) - 1u;
-                    if (ok) ok = wide_wait(&sfull[t], s_phase, dead, p.status);
-                    ok = __all_sync(0xffffffffu, ok);
-                    s_phase ^= 1;
-                    tc_fence_after();
-                    uint32_t x[NH];
-#pragma unroll
-                    for (int ch = 0; ch < NH / 32; ++ch)
-                        tmem_ld32(s_at + half * NH + ch * 32, *(uint32_t(*)[32])(x + ch * 32));
+                    const bool masked = tags || tok > safe || have != 15u;
                     tmem_ld_wait();
                     auto pair = [&](int k) { return f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])); };
                     auto put = [&](int k, uint64_t v) {
@@ -662,55 +700,49 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     };
                     if constexpr (BITS == 8)
 #pragma unroll
-                        for (int k = 0; k < NH; k += 2) put(k, f2_mul(pair(k), *(const uint64_t *)&m.ksig[half * NH + k]));
+                        for (int k = 0; k < HT; k += 2) put(k, f2_mul(pair(k), *(const uint64_t *)&m.ksig[half + k]));
                     if (heavy || masked) {
                         // in place, from here on the factor is 1
 #pragma unroll
-                        for (int k = 0; k < NH; k += 2) put(k, f2_mul(pair(k), f2_pack(f, f)));
+                        for (int k = 0; k < HT; k += 2) put(k, f2_mul(pair(k), f2_pack(f, f)));
                         f = 1.f;
-                        if (p.cap > 0.f) cap_scores<NH>(x, cap_l);
+                        if (p.cap > 0.f) cap_scores<HT>(x, cap_l);
                         if (p.slopes) {
-                            const float away = (float)(pos - tok - half * NH);
+                            const float away = (float)(pos - tok);
 #pragma unroll
-                            for (int k = 0; k < NH; ++k)
+                            for (int k = 0; k < HT; ++k)
                                 x[k] = __float_as_uint(fmaf(-slope, fabsf(away - (float)k), __uint_as_float(x[k])));
                         }
                         if (masked) {
 #pragma unroll
-                            for (int u = 0; u < NH / 16; ++u) {
-                                const int end = have >> (half * (NH / 16) + u) & 1u ? limit - tok - half * NH - u * 16 : 0;
+                            for (int u = 0; u < HT / 16; ++u) {
+                                const int end = have >> u & 1u ? limit - tok - u * 16 : 0;
 #pragma unroll
                                 for (int k = 0; k < 16; ++k)
-                                    if (k >= end || (tags && m.tag[half * NH + u * 16 + k] != qtag)) x[u * 16 + k] = 0xff800000u;
+                                    if (k >= end || (tags && m.tag[half + u * 16 + k] != qtag)) x[u * 16 + k] = 0xff800000u;
                             }
                         }
                     }
                     float top = __uint_as_float(x[0]);
 #pragma unroll
-                    for (int k = 1; k < NH; ++k) top = fmaxf(top, __uint_as_float(x[k]));
+                    for (int k = 1; k < HT; ++k) top = fmaxf(top, __uint_as_float(x[k]));
                     top *= f;
-                    // The maximum is raised when a weight would pass 2^14.  The two halves'
-                    // warps meet here in any case: both have read the scores that P replaces.
+                    // the maximum is raised when a weight would pass 2^14
                     float down = 1.f;          // of what was summed so far
-                    if (bar_any(pair_bar, 64, unset || top - mm > P_SHIFT + M_SLACK)) {
-                        tops[t][half][rt] = top;
-                        named_bar(pair_bar, 64);
-                        top = fmaxf(top, tops[t][half ^ 1][rt]);
-                        if (unset ? top > -INFINITY : top - mm > P_SHIFT + M_SLACK) {
-                            down = unset ? 0.f : ex2(mm + P_SHIFT - top);
-                            unset = false;
-                            mm = top - P_SHIFT;
-                        }
+                    if (unset ? top > -INFINITY : top - mm > P_SHIFT + M_SLACK) {
+                        down = unset ? 0.f : ex2(mm + P_SHIFT - top);
+                        unset = false;
+                        mm = top - P_SHIFT;
                     }
                     uint64_t sum[2] = {0, 0};
                     const uint64_t n2 = f2_pack(-mm, -mm);
-                    uint32_t pk[NH / 2];
+                    uint32_t pk[HT / 2];
 #pragma unroll
-                    for (int k = 0; k < NH; k += 2) {
+                    for (int k = 0; k < HT; k += 2) {
                         const float2 u = f2_open(f2_fma(pair(k), f2_pack(f, f), n2));
                         uint64_t e2 = f2_pack(ex2(u.x), ex2(u.y));
                         sum[k / 2 % 2] = f2_add(sum[k / 2 % 2], e2);
-                        if constexpr (BITS == 8) e2 = f2_mul(e2, *(const uint64_t *)&m.vsig[half * NH + k]);
+                        if constexpr (BITS == 8) e2 = f2_mul(e2, *(const uint64_t *)&m.vsig[half + k]);
                         const float2 y = f2_open(e2);
                         pk[k / 2] = pack_h2(y.x, y.y);
                     }
@@ -718,13 +750,19 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         const float2 y = f2_open(f2_add(sum[0], sum[1]));
                         l = l * down + (y.x + y.y);
                     }
-                    if (rv_new != rv) {
-                        down *= pow2i(max(-126, rv - rv_new));
-                        rv = rv_new;
+                    if (m.rv != rv) {
+                        down *= pow2i(max(-126, rv - m.rv));
+                        rv = m.rv;
                     }
-                    if (it > 0 && __any_sync(0xffffffffu, down != 1.f)) {
+                    tmem_st32(s_at, pk);
+                    if (h > 0 && __any_sync(0xffffffffu, down != 1.f)) {
+                        // once the products before have been added
+                        ok = wide_wait(&odone[t][b ^ 1], (halves - 1) >> 1 & 1, dead, p.status);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        tc_fence_after();
 #pragma unroll 1
-                        for (int d = 0; d < DH; d += 32) {
+                        for (int d = 0; d < D; d += 32) {
                             uint32_t y[32];
                             tmem_ld32(o_at + d, y);
                             tmem_ld_wait();
@@ -733,77 +771,51 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                             tmem_st32(o_at + d, y);
                         }
                     }
-                    if constexpr (NH == 64) tmem_st32(s_at + half * 32, pk);
-                    else tmem_st16(s_at + half * 16, pk);
                     tmem_st_wait();
                     tc_fence_before();
-                    if (all_here()) {
-                        issue_values(n_tile, it == 0);
-                        if (it + 1 < n) issue_scores(n_tile + 1);
-                        else umma_commit(&ofull[t]);
-                    }
                     __syncwarp();
+                    if (lane == 0) mbar_arrive(&pfull[t][b]);
                 }
-                totals[t][half][rt] = l;
-                named_bar(pair_bar, 64);
-                l += totals[t][half ^ 1][rt];
-                if (ok) ok = wide_wait(&ofull[t], o_phase, dead, p.status);
+                if (ok) ok = wide_wait(&odone[t][(halves - 1) & 1], (halves - 1) >> 1 & 1, dead, p.status);
                 ok = __all_sync(0xffffffffu, ok);
-                o_phase ^= 1;
+                if (!ok) break;
                 tc_fence_after();
                 // ---- whole items are written, others left for the joining kernel
                 const bool whole = n == cur.units;
                 if (unset) mm = NEG;
                 float *part = p.partial + ((int64_t)blockIdx.x * 2 + (cur.unit == 0)) * attend_slot_floats(ROWS, D);
                 const int up = rv + (BITS == 4 ? UP : 0);
-                const float inv = l > 0.f ? 1.f / l : l;
+                const float inv = whole ? (l > 0.f ? 1.f / l : l) : 1.f, up0 = pow2i(up / 2), up1 = pow2i(up - up / 2);
                 const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + hd;
-#pragma unroll 1
-                for (int d = 0; d < DH; d += 32) {
+#pragma unroll 2
+                for (int d = 0; d < D; d += 32) {
                     uint32_t y[32];
                     tmem_ld32(o_at + d, y);
                     tmem_ld_wait();
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * inv * up0 * up1);
                     if (!whole) {
 #pragma unroll
                         for (int k = 0; k < 32; k += 4)
-                            *(float4 *)(part + (int64_t)r * D + half * DH + d + k) =
-                                make_float4(scale2(__uint_as_float(y[k]), up), scale2(__uint_as_float(y[k + 1]), up),
-                                            scale2(__uint_as_float(y[k + 2]), up), scale2(__uint_as_float(y[k + 3]), up));
+                            *(uint4 *)(part + r * D + d + k) = make_uint4(y[k], y[k + 1], y[k + 2], y[k + 3]);
                     } else if (real) {
-#pragma unroll
-                        for (int k = 0; k < 32; k += 2)
-                            store_pair(p, bf16, dst * D + half * DH + d + k, scale2(__uint_as_float(y[k]) * inv, up),
-                                       scale2(__uint_as_float(y[k + 1]) * inv, up));
+                        store_row32(p, bf16, dst * D + d, y);
                     }
                 }
-                if (half == 0) {
-                    if (!whole) {
-                        part[ROWS * D + r] = mm, part[ROWS * D + ROWS + r] = l;
-                        if (r == 0 && cur.unit == 0)
-                            p.joins[blockIdx.x] = make_int4(cur.seq, cur.head, cur.tile,
-                                                            (int)((first + done + cur.units - 1) / per));
-                    } else if (real && p.lse) {
-                        p.lse[dst] = lse_of(mm, l);
-                    }
+                if (!whole) {
+                    part[ROWS * D + r] = mm, part[ROWS * D + ROWS + r] = l;
+                    if (r == 0 && cur.unit == 0)
+                        p.joins[blockIdx.x] = make_int4(cur.seq, cur.head, cur.tile,
+                                                        (int)((first + done + cur.units - 1) / per));
+                } else if (real && p.lse) {
+                    p.lse[dst] = lse_of(mm, l);
                 }
                 tc_fence_before();
-            } else {
-                // no rows here: the other row tile's alone.  All warps keep up with
-                // the tiles, so that the parity they wait for next is that of the next phase.
-                for (int it = 0; it < n; ++it, ++n_tile) {
-                    if (ok) ok = wide_wait(&vfull[n_tile % ST], (n_tile / ST) & 1, dead, p.status);
-                    if (ok && leader) mbar_arrive(&empty[n_tile % ST]);
-                }
-                ok = __all_sync(0xffffffffu, ok);
             }
+            n_tile += n;
             left -= n, done += n;
             if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
         }
-        if (leader) {                          // what was issued ends before the tensor memory goes
-            umma_commit(&drained);
-            mbar_wait(&drained, 0, p.status);
-        }
-        __syncwarp();
     }
     tc_fence_before();
     __syncthreads();

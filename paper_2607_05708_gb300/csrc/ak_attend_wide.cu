@@ -52,9 +52,10 @@ template <int N>
 struct alignas(16) Meta {           // pairs of its floats are read at once
     float ksig[N], vsig[N];         // 8 bits: significands of the tokens' scales
     int tag[N];
-    float kf;                       // factor of the scores
-    int tok, rv;                    // first token, exponent of the values
-    uint32_t have;                  // units that are listed
+    // read at once: factor of the scores, first token, exponent of the values, units listed
+    alignas(16) float kf;
+    int tok, rv;
+    uint32_t have;
 };
 static_assert(offsetof(Meta<64>, ksig) % 8 == 0 && offsetof(Meta<64>, vsig) % 8 == 0 &&
                   offsetof(Meta<128>, ksig) % 8 == 0 && offsetof(Meta<128>, vsig) % 8 == 0,
@@ -316,6 +317,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
     if (warp >= C::SOFT && warp < C::SOFT + C::DEQ) {
         // ---------------- dequantising
         const int w = warp - C::SOFT, g = lane >> 2, c = lane & 3;
+        const bool far = D == 128 && c >= 2, odd = D == 128 && (g & 1);    // (shared memory banks)
         uint32_t n_tile = 0;                   // tiles since the kernel began
         while (left > 0 && !*dead) {
             const int n = min(cur.units - cur.unit, left), units = (cur.q.kv + KV_UNIT - 1) / KV_UNIT;
@@ -446,6 +448,14 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                             *tile_chunk(kt_, N, t0 + x / (D / 8), x % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
                     } else if constexpr (BITS == 4) {
                         constexpr int W = D / 32, PERG = D / 64;
+                        if constexpr (D == 128) {
+                            // lanes c and c + 2 meet in the same banks (64 dims apart): the
+                            // latter take their two groups the other way round
+                            r[j].ks[0] = __byte_perm(r[j].ks[0], 0, far ? 0x2301 : 0x3210);
+#pragma unroll
+                            for (int i2 = 0; i2 < 2; ++i2)
+                                if (far) r[j].k[i2] = make_uint4(r[j].k[i2].z, r[j].k[i2].w, r[j].k[i2].x, r[j].k[i2].y);
+                        }
 #pragma unroll
                         for (int i2 = 0; i2 < 2; ++i2)
 #pragma unroll
@@ -460,7 +470,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                                     const int at = D == 64 ? i2 * 2 + x : i2 * W + x;
                                     uint32_t h[4];
                                     nibbles(word_of(r[j].k[at / 4], at % 4), s, s4, cc, h);
-                                    *tile_chunk(kt_, N, t0 + g + 8 * i2, c * (D / 4) + x * 8) = make_uint4(h[0], h[1], h[2], h[3]);
+                                    *tile_chunk(kt_, N, t0 + g + 8 * i2, c * (D / 4) + (x ^ (far ? 2 : 0)) * 8) = make_uint4(h[0], h[1], h[2], h[3]);
                                 }
                             }
                     } else {
@@ -470,9 +480,11 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                             const uint32_t cc = h2mul(kfh[j][i2], H2_M1152);
 #pragma unroll
                             for (int q = 0; q < CH; ++q) {
-                                const uint4 x = r[j].k[i2 * CH + q];
-                                *tile_chunk(kt_, N, t0 + g + 8 * i2, c * (D / 4) + q * 16) = bytes8(x.x, x.y, kfh[j][i2], cc);
-                                *tile_chunk(kt_, N, t0 + g + 8 * i2, c * (D / 4) + q * 16 + 8) = bytes8(x.z, x.w, kfh[j][i2], cc);
+                                uint4 x = r[j].k[i2 * CH + q];
+                                if (D == 128 && far) x = r[j].k[i2 * CH + (q ^ 1)];
+                                const int d = c * (D / 4) + (q ^ (far ? 1 : 0)) * 16;
+                                *tile_chunk(kt_, N, t0 + g + 8 * i2, d) = bytes8(x.x, x.y, kfh[j][i2], cc);
+                                *tile_chunk(kt_, N, t0 + g + 8 * i2, d + 8) = bytes8(x.z, x.w, kfh[j][i2], cc);
                             }
                         }
                     }
@@ -512,9 +524,10 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
 #pragma unroll
                                     for (int q = 0; q < WG; ++q) {
                                         const int i3 = gl * WG + q, at = x * W + i3;
-                                        uint32_t h[4];
-                                        nibbles(word_of(r[j].v[at / 4], at % 4), s, s4, cc, h);
-                                        *tile_chunk(vt_, N, t, g * (D / 8) + i3 * 8) = make_uint4(h[0], h[1], h[2], h[3]);
+                                        uint32_t h[4], word = word_of(r[j].v[at / 4], at % 4);
+                                        if (D == 128 && odd) word = word_of(r[j].v[at / 4], (at ^ 1) % 4);
+                                        nibbles(word, s, s4, cc, h);
+                                        *tile_chunk(vt_, N, t, g * (D / 8) + (i3 ^ (odd ? 1 : 0)) * 8) = make_uint4(h[0], h[1], h[2], h[3]);
                                     }
                                 }
                             } else {
@@ -523,8 +536,10 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
 #pragma unroll
                                 for (int q = 0; q < W; q += 2) {
                                     const int at = x * W + q;
-                                    *tile_chunk(vt_, N, t, g * (D / 8) + q * 4) =
-                                        bytes8(word_of(r[j].v[at / 4], at % 4), word_of(r[j].v[(at + 1) / 4], (at + 1) % 4), f, cc);
+                                    uint32_t w0 = word_of(r[j].v[at / 4], at % 4), w1 = word_of(r[j].v[at / 4], at % 4 + 1);
+                                    if (D == 128 && odd)
+                                        w0 = word_of(r[j].v[at / 4], (at ^ 2) % 4), w1 = word_of(r[j].v[at / 4], (at ^ 2) % 4 + 1);
+                                    *tile_chunk(vt_, N, t, g * (D / 8) + (q ^ (odd ? 2 : 0)) * 4) = bytes8(w0, w1, f, cc);
                                 }
                             }
                         }
@@ -621,41 +636,49 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 // ---- the warp's 32 query rows, 16 bytes a lane: bf16 scaled by a power of two
                 // to a largest magnitude in [1, 2)
                 constexpr int CH = D / 8, RP = 32 / CH;
-#pragma unroll 8
-                for (int y = 0; y < CH; ++y) {
-                    const int row = (warp & 3) * 32 + y * RP + lane / CH, ch = lane % CH;
-                    const bool have = t * 128 + row < rows;
-                    const int at = row_first + t * 128 + row, i = have ? at / p.group : 0;
-                    const int hd = cur.head * p.group + (have ? at - i * p.group : 0);
-                    const uint16_t *src = (const uint16_t *)p.q + (sq.row0 + i) * p.q_row + hd * p.q_head + ch * 8;
-                    alignas(16) uint16_t x[8];
-                    *(uint4 *)x = make_uint4(0, 0, 0, 0);
-                    if (have) {
+                constexpr int AT_ONCE = CH < 16 ? CH : 16;
+#pragma unroll 1
+                for (int y0 = 0; y0 < CH; y0 += AT_ONCE) {
+                    uint4 z[AT_ONCE];
+#pragma unroll
+                    for (int y = 0; y < AT_ONCE; ++y) {
+                        const int row = t * 128 + (warp & 3) * 32 + (y0 + y) * RP + lane / CH;
+                        const uint32_t at = row_first + min(row, rows - 1), i = at / (uint32_t)p.group;
+                        const uint16_t *src = (const uint16_t *)p.q + (int64_t)(sq.row0 + (int)i) * p.q_row +
+                                              (int64_t)(cur.head * p.group + (int)(at - i * p.group)) * p.q_head + lane % CH * 8;
                         if (p.q_wide) {
-                            *(uint4 *)x = *(const uint4 *)src;
+                            z[y] = *(const uint4 *)src;
                         } else {
+                            alignas(16) uint16_t x[8];
 #pragma unroll
                             for (int k = 0; k < 8; ++k) x[k] = src[k];
+                            z[y] = *(const uint4 *)x;
                         }
+                        if (row >= rows) z[y] = make_uint4(0, 0, 0, 0);
                     }
-                    uint4 z = *(const uint4 *)x;
-                    float up = 1.f;
-                    if (bf16) {
-                        float a = 0.f;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) a = fmaxf(a, fabsf(bf16_to_f32(x[k])));
+                    for (int y = 0; y < AT_ONCE; ++y) {
+                        const int row = (warp & 3) * 32 + (y0 + y) * RP + lane / CH, ch = lane % CH;
+                        float up = 1.f;
+                        if (bf16) {
+                            uint32_t w[4] = {z[y].x, z[y].y, z[y].z, z[y].w};
+                            float a = 0.f;
 #pragma unroll
-                        for (int o = CH / 2; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-                        const int e = max(-126, min(126, (int)(__float_as_uint(a) >> 23) - 127));
-                        const float by = pow2i(-e);
-                        up = pow2i(e);
-                        z = make_uint4(pack_h2(bf16_to_f32(x[0]) * by, bf16_to_f32(x[1]) * by),
-                                       pack_h2(bf16_to_f32(x[2]) * by, bf16_to_f32(x[3]) * by),
-                                       pack_h2(bf16_to_f32(x[4]) * by, bf16_to_f32(x[5]) * by),
-                                       pack_h2(bf16_to_f32(x[6]) * by, bf16_to_f32(x[7]) * by));
+                            for (int k = 0; k < 4; ++k)
+                                a = fmaxf(a, fmaxf(fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xffff0000u))));
+#pragma unroll
+                            for (int o = CH / 2; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+                            const int e = max(-126, min(126, (int)(__float_as_uint(a) >> 23) - 127));
+                            const float by = pow2i(-e);
+                            up = pow2i(e);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                w[k] = pack_h2(__uint_as_float(w[k] << 16) * by, __uint_as_float(w[k] & 0xffff0000u) * by);
+                            z[y] = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                        *tile_chunk(sq_ + t * 128 * D * 2, 128, row, ch * 8) = z[y];
+                        if (ch == 0) qscale[t * 128 + row] = up;
                     }
-                    *tile_chunk(sq_ + t * 128 * D * 2, 128, row, ch * 8) = z;
-                    if (ch == 0) qscale[t * 128 + row] = up;
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -673,13 +696,16 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 float mm = 0.f, l = 0.f;
                 bool unset = real;             // no key seen yet: mm = 0
                 int rv = -127;
+                uint4 about = make_uint4(0, 0, 0, 0);      // the tile's Meta from kf on
                 for (int h = 0; h < n * HPT; ++h, ++halves) {
                     const uint32_t x_tile = n_tile + h / HPT, st = x_tile % ST, b = halves & 1;
                     const uint32_t s_at = tmem + lanes + C::S_COL + (t * 2 + b) * HT;
                     if (h % HPT == 0) {
-                        ok = wide_wait(&sfull[t][b], halves >> 1 & 1, dead, p.status);
-                        // complete by now; what the dequantising warps wrote beside the tile
-                        if (ok) ok = wide_wait(&kfull[st], (x_tile / ST) & 1, dead, p.status);
+                        // what the dequantising warps wrote beside the tile, while its scores
+                        // are computed
+                        ok = wide_wait(&kfull[st], (x_tile / ST) & 1, dead, p.status);
+                        about = *(const uint4 *)&meta[st].kf;
+                        if (ok) ok = wide_wait(&sfull[t][b], halves >> 1 & 1, dead, p.status);
                         ok = __all_sync(0xffffffffu, ok);
                         if (!ok) break;
                         tc_fence_after();
@@ -688,9 +714,9 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     tmem_ld32(s_at, *(uint32_t(*)[32])x);
                     tmem_ld32(s_at + 32, *(uint32_t(*)[32])(x + 32));
                     const Meta<N> &m = meta[st];
-                    const int half = h % HPT * HT, tok = m.tok + half;
-                    const uint32_t have = m.have >> (half / KV_UNIT) & 15u;
-                    float f = qf * m.kf;       // of the scores, log2 units
+                    const int half = h % HPT * HT, tok = (int)about.y + half, rv_new = (int)about.z;
+                    const uint32_t have = about.w >> (half / KV_UNIT) & 15u;
+                    float f = qf * __uint_as_float(about.x);   // of the scores, log2 units
                     const bool masked = tags || tok > safe || have != 15u;
                     tmem_ld_wait();
                     auto pair = [&](int k) { return f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])); };
@@ -750,9 +776,9 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         const float2 y = f2_open(f2_add(sum[0], sum[1]));
                         l = l * down + (y.x + y.y);
                     }
-                    if (m.rv != rv) {
-                        down *= pow2i(max(-126, rv - m.rv));
-                        rv = m.rv;
+                    if (rv_new != rv) {
+                        down *= pow2i(max(-126, rv - rv_new));
+                        rv = rv_new;
                     }
                     tmem_st32(s_at, pk);
                     if (h > 0 && __any_sync(0xffffffffu, down != 1.f)) {
@@ -811,6 +837,12 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     p.lse[dst] = lse_of(mm, l);
                 }
                 tc_fence_before();
+            } else {
+                // No rows here.  All the same the warps keep up with the tiles: the parity
+                // that they wait for next has to be that of the next phase.
+                for (int it = 0; ok && it < n; ++it)
+                    ok = wide_wait(&kfull[(n_tile + it) % ST], ((n_tile + it) / ST) & 1, dead, p.status);
+                ok = __all_sync(0xffffffffu, ok);
             }
             n_tile += n;
             left -= n, done += n;

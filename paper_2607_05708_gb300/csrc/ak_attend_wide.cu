@@ -36,8 +36,14 @@ struct Wide {
     static constexpr int UNITS = N / KV_UNIT;
     static constexpr int HT = 64, HPT = N / HT;          // tokens the softmax takes at a time
     static constexpr int SN = MT == 2 ? N : HT;          // columns of S computed at once
-    static constexpr int SOFT = 4 * MT, DEQ = 4;         // warps, and one that issues
-    static constexpr int THREADS = 32 * (SOFT + DEQ + 1);
+    // Warps: softmax, dequantising, one that issues.  At D <= 128 the registers of five
+    // warpgroups are split by need (softmax 128, dequantising 88, the last one 48 a thread:
+    // together the 96 of the launch), so that a unit of a tile has a warp of its own:
+    // with two each a tile took its 4 warps 6000 cycles, as long as all else.
+    static constexpr bool SPLIT = MT == 2;
+    static constexpr int SOFT = 4 * MT, DEQ = SPLIT ? 8 : 4;
+    static constexpr int THREADS = 32 * (SOFT + DEQ + (SPLIT ? 4 : 1));
+    static_assert(!SPLIT || 256 * 128 + 256 * 88 + 128 * 48 == THREADS * 96, "registers");
     static constexpr int UPW = UNITS / DEQ;              // units of a dequantising warp
     static constexpr int STAGES = 2;
     static constexpr int Q_BYTES = ROWS * D * 2, KV_BYTES = N * D * 2;
@@ -103,18 +109,46 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
 __device__ __forceinline__ void tmem_st_wait() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
-// D[tmem] (+)= A[smem] B[smem]^T and D[tmem] (+)= A[tmem] B[smem], fp16.
-__device__ __forceinline__ void umma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-    umma_bf16(d, a, b, idesc, acc);            // the types are in the descriptor
-}
-__device__ __forceinline__ void umma_f16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
-                                            uint32_t acc) {
+// D[tmem] (+)= A[smem] B[smem]^T and D[tmem] (+)= A[tmem] B[smem], fp16, by the lane that
+// has `go`.  The whole warp comes here, so that addresses stay in uniform registers
+// (behind a branch on the lane an issue took 120 cycles and more; the product takes 64),
+// and of a shared-memory descriptor (ak_sm100.cuh) only the low word changes.
+constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ void umma_ss(uint32_t go, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                        uint32_t acc) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(b), "r"(idesc), "r"(acc)
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 x, y;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "setp.ne.b32 q, %0, 0;\n\t"
+        "mov.b64 x, {%2, %6};\n\t"
+        "mov.b64 y, {%3, %6};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%1], x, y, %4, p;\n\t}" ::"r"(go),
+        "r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(DESC_HI)
         : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t go, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                        uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 y;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "setp.ne.b32 q, %0, 0;\n\t"
+        "mov.b64 y, {%3, %6};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], y, %4, p;\n\t}" ::"r"(go),
+        "r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(DESC_HI)
+        : "memory");
+}
+__device__ __forceinline__ void umma_commit_if(uint32_t go, uint64_t *bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %0, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}" ::"r"(go),
+        "r"(smem_u32(bar))
+        : "memory");
+}
+// Low words of the descriptors of K-major and MN-major tiles.
+__device__ __forceinline__ uint32_t desc_k(uint32_t saddr) { return ((saddr & 0x3ffffu) >> 4) | 1u << 16; }
+__device__ __forceinline__ uint32_t desc_mn(uint32_t saddr, uint32_t lbo) {
+    return ((saddr & 0x3ffffu) >> 4) | (lbo >> 4) << 16;
 }
 // Instruction descriptor: D fp32, A and B fp16, M = 128.
 constexpr uint32_t idesc_f16(int n) {
@@ -316,6 +350,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
 
     if (warp >= C::SOFT && warp < C::SOFT + C::DEQ) {
         // ---------------- dequantising
+        if constexpr (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         const int w = warp - C::SOFT, g = lane >> 2, c = lane & 3;
         const bool far = D == 128 && c >= 2, odd = D == 128 && (g & 1);    // (shared memory banks)
         uint32_t n_tile = 0;                   // tiles since the kernel began
@@ -556,69 +591,77 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
             left -= n;
             if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
         }
-    } else if (warp == C::SOFT + C::DEQ) {
+    } else if (warp >= C::SOFT + C::DEQ) {
         // ---------------- issuing
-        if (lane == 0) {
+        if constexpr (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        if (warp == C::SOFT + C::DEQ) {
             constexpr uint32_t id_s = idesc_f16(C::SN), id_o = idesc_f16(D) | IDESC_B_MN_MAJOR;
-            uint32_t n_tile = 0, halves[MT] = {}, q_phase = 0;     // halves: of the row tile, so far
+            const uint32_t go = lane == 0;
+            const uint32_t q_at = desc_k(smem_u32(sq_)), k_at = desc_k(smem_u32(sk)), v_at = desc_mn(smem_u32(sv), N * 128);
+            uint32_t n_tile = 0, q_phase = 0, ph0 = 0, ph1 = 0;    // ph: halves of the row tile, so far
             bool ok = true;
             // S of half h of the item (its first tile: n_tile) for row tile t; at D <= 128
             // (h even) of the whole tile
             auto scores = [&](int t, int h) {
-                const uint32_t x = n_tile + h / HPT, b = (halves[t] + h) & 1;
+                const uint32_t x = n_tile + h / HPT, b = ((t ? ph1 : ph0) + h) & 1;
                 if (!ok) return;
                 // the row tiles share a tile's keys
                 if (t == 0 && !(ok = wide_wait(&kfull[x % ST], (x / ST) & 1, dead, p.status))) return;
                 tc_fence_after();
-                const uint64_t qd = sdesc_sw128(smem_u32(sq_ + t * 128 * D * 2));
-                const uint64_t kd = sdesc_sw128(smem_u32(sk + (x % ST) * C::KV_BYTES));
+                const uint32_t qa = q_at + (t * 128 * D * 2 >> 4), ka = k_at + (x % ST) * (C::KV_BYTES >> 4);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
-                    umma_f16(tmem + C::S_COL + (t * 2 + b) * HT, qd + (uint64_t)((k / 4) * (128 * 128) >> 4) + 2 * (k % 4),
-                             kd + (uint64_t)((k / 4) * (N * 128) >> 4) + 2 * (k % 4), id_s, k > 0);
-                umma_commit(&sfull[t][b]);
+                    umma_ss(go, tmem + C::S_COL + (t * 2 + b) * HT, qa + ((k / 4) * (128 * 128) >> 4) + 2 * (k % 4),
+                            ka + ((k / 4) * (N * 128) >> 4) + 2 * (k % 4), id_s, k > 0);
+                umma_commit_if(go, &sfull[t][b]);
             };
             auto values = [&](int t, int h) {
-                const uint32_t x = n_tile + h / HPT, b = (halves[t] + h) & 1;
+                const uint32_t x = n_tile + h / HPT, c = (t ? ph1 : ph0) + h, b = c & 1;
                 if (!ok) return;
                 if (t == 0 && h % HPT == 0 && !(ok = wide_wait(&vfull[x % ST], (x / ST) & 1, dead, p.status))) return;
-                if (!(ok = wide_wait(&pfull[t][b], (halves[t] + h) >> 1 & 1, dead, p.status))) return;
+                if (!(ok = wide_wait(&pfull[t][b], c >> 1 & 1, dead, p.status))) return;
                 tc_fence_after();
-                const uint64_t vd = sdesc_mn_sw128(smem_u32(sv + (x % ST) * C::KV_BYTES + h % HPT * HT * 128), N * 128, 1024);
+                const uint32_t va = v_at + (x % ST) * (C::KV_BYTES >> 4) + h % HPT * (HT * 128 >> 4);
 #pragma unroll
                 for (int k = 0; k < HT / 16; ++k)
-                    umma_f16_ta(tmem + t * D, tmem + C::S_COL + (t * 2 + b) * HT + k * 8, vd + (uint64_t)(2048 * k >> 4),
-                                id_o, (h > 0 || k > 0) ? 1u : 0u);
-                umma_commit(&odone[t][b]);
+                    umma_ts(go, tmem + t * D, tmem + C::S_COL + (t * 2 + b) * HT + k * 8, va + (2048 * k >> 4), id_o,
+                            (h > 0 || k > 0) ? 1u : 0u);
+                umma_commit_if(go, &odone[t][b]);
             };
             while (left > 0 && ok) {
                 const int n = min(cur.units - cur.unit, left), nh = n * HPT;
                 const int mt = cur.q.nq * p.group - cur.tile * ROWS > 128 ? MT : 1;
-                for (int t = 0; ok && t < mt; ++t) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    if (!ok || t >= mt) break;
                     ok = wide_wait(&qfull[t], q_phase >> t & 1, dead, p.status);
                     q_phase ^= 1u << t;
                     scores(t, 0);
                 }
                 for (int h = 0; ok && h < nh; ++h)
-                    for (int t = 0; t < mt; ++t) {
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) {
+                        if (t >= mt) break;
                         // two buffers of one row tile: the next half's scores come first
                         if (HPT == 1 && h + 1 < nh) scores(t, h + 1);
                         values(t, h);
                         if (h % HPT < HPT - 1) continue;
-                        if (ok && t == mt - 1) umma_commit(&empty[(n_tile + h / HPT) % ST]);
+                        if (ok && t == mt - 1) umma_commit_if(go, &empty[(n_tile + h / HPT) % ST]);
                         if (HPT == 2 && h + 1 < nh) scores(t, h + 1);
                     }
-                for (int t = 0; t < mt; ++t) halves[t] += nh;
+                ph0 += nh;
+                if (mt > 1) ph1 += nh;
                 n_tile += n;
                 left -= n;
                 if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
             }
-            umma_commit(&drained);             // what was issued ends before the tensor memory goes
+            umma_commit_if(go, &drained);      // what was issued ends before the tensor memory goes
             mbar_wait(&drained, 0, p.status);
         }
         __syncwarp();
     } else {
         // ---------------- softmax: a lane is row 32 (warp % 4) + lane of row tile t
+        if constexpr (C::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
         const int t = warp >> 2, rt = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t o_at = tmem + lanes + t * D;

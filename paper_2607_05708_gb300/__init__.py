@@ -405,45 +405,55 @@ class KVCache:
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
         self._dtypes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
         self._scratch = {}
+        # what every call needs, looked up once
+        self._dev = self.data.device
+        # the current stream's handle without a Stream object (4 us a call)
+        self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+        self._data_ptr, self._status_ptr = self.data.data_ptr(), self.status.data_ptr()
+        self._tags_ptr = None if self.tags is None else self.tags.data_ptr()
+        self._write, self._read = self._lib.akashic_mem_kv_write, self._lib.akashic_mem_kv_read
+        self._attend = self._lib.akashic_mem_kv_attend
 
     # -- helpers
     def _vec(self, t, dtype, name, numel):
         """The pointer of a contiguous tensor of that type and length (None: NULL)."""
         if t is None:
             return None
-        if not t.is_cuda or t.device.index != self.device:
-            raise ValueError(f"{name} must be a CUDA tensor on device {self.device}")
-        if t.dtype != dtype:
+        if t.dtype is not dtype:
             raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} must be a CUDA tensor on device {self.device}")
         if not t.is_contiguous() or t.numel() != numel:
             raise ValueError(f"{name} must be contiguous, of {numel} elements")
         return t.data_ptr()
 
     def _rows(self, t, name, heads=None):
-        """dtype code of rows [n, heads, head_dim] whose last dimension is contiguous."""
-        if not t.is_cuda or t.device.index != self.device:
-            raise ValueError(f"{name} must be a CUDA tensor on device {self.device}")
-        if t.dtype not in self._dtypes:
+        """dtype code, shape and strides of rows [n, heads, head_dim] whose last
+        dimension is contiguous."""
+        code = self._dtypes.get(t.dtype)
+        if code is None:
             raise TypeError(f"{name} must be bfloat16, float16 or float32, got {t.dtype}")
-        if t.dim() != 3 or t.shape[2] != self.head_dim or (heads and t.shape[1] != heads):
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} must be a CUDA tensor on device {self.device}")
+        shape, strides = t.shape, t.stride()
+        if len(shape) != 3 or shape[2] != self.head_dim or (heads and shape[1] != heads):
             raise ValueError(f"{name} must be [n, {heads or 'heads'}, {self.head_dim}]")
-        if t.stride(2) != 1 and t.numel():
+        if strides[2] != 1 and t.numel():
             raise ValueError(f"{name} must be contiguous in its last dimension")
-        return self._dtypes[t.dtype]
+        return code, shape, strides
 
     def _empty(self, shape, dtype, stream, zero=False):
         """A new tensor from the pool of the stream that the call runs on."""
         torch = self._torch
         make = torch.zeros if zero else torch.empty
-        dev = self.data.device
         if stream is None:
-            return make(shape, dtype=dtype, device=dev)
+            return make(shape, dtype=dtype, device=self._dev)
         with torch.cuda.stream(stream):
-            return make(shape, dtype=dtype, device=dev)
+            return make(shape, dtype=dtype, device=self._dev)
 
     def _on(self, stream):
-        s = stream if stream is not None else self._torch.cuda.current_stream(self.device)
-        return s.cuda_stream
+        return self._current(self.device) if stream is None else stream.cuda_stream
 
     # -- ABI
     def write(self, k, v, slots, tags=None, stream=None):
@@ -452,39 +462,47 @@ class KVCache:
         place; -1 skips a row; a slot at most once).  tags (int32 [n], tagged caches
         only): the tags of the rows, 0 if not given."""
         torch = self._torch
-        dt = self._rows(k, "k", self.heads)
-        if self._rows(v, "v", self.heads) != dt or v.shape != k.shape:
+        dt, shape, sk = self._rows(k, "k", self.heads)
+        dtv, shape_v, sv = self._rows(v, "v", self.heads)
+        if dtv != dt or shape_v != shape:
             raise ValueError("k and v must be of one type and shape")
-        n = k.shape[0]
+        n = shape[0]
         if tags is not None and self.tags is None:
             raise ValueError("tags need a tagged cache")
-        ps = self._vec(slots, torch.int64, "slots", n)
-        pt = self._vec(tags, torch.int32, "tags", n)
-        sk, sv = k.stride(), v.stride()
-        _check(self._lib.akashic_mem_kv_write(
-            self._cfg, self.data.data_ptr(), None if self.tags is None else self.tags.data_ptr(),
-            k.data_ptr(), sk[0], sk[1], v.data_ptr(), sv[0], sv[1], dt, n, ps, pt,
-            self.status.data_ptr(), self._on(stream)))
+        rc = self._write(self._cfg, self._data_ptr, self._tags_ptr, k.data_ptr(), sk[0], sk[1],
+                         v.data_ptr(), sv[0], sv[1], dt, n,
+                         self._vec(slots, torch.int64, "slots", n),
+                         self._vec(tags, torch.int32, "tags", n), self._status_ptr,
+                         self._on(stream))
+        if rc:
+            _check(rc)
 
     def read(self, slots, dtype=None, k=None, v=None, stream=None):
         """The values that slots (int64 [n], -1: zeros) stand for: k, v [n, heads,
         head_dim] of dtype (bfloat16 if not given), allocated unless given."""
         torch = self._torch
         dtype = dtype or (k.dtype if k is not None else torch.bfloat16)
-        if dtype not in self._dtypes:
+        code = self._dtypes.get(dtype)
+        if code is None:
             raise TypeError(f"dtype must be bfloat16, float16 or float32, got {dtype}")
         n = slots.numel()
         shape = (n, self.heads, self.head_dim)
         ps = self._vec(slots, torch.int64, "slots", n)
+        numel = n * self.heads * self.head_dim
         if k is None:
             k = self._empty(shape, dtype, stream)
+            pk = k.data_ptr()
+        else:
+            pk = self._vec(k, dtype, "k", numel)
         if v is None:
             v = self._empty(shape, dtype, stream)
-        numel = n * self.heads * self.head_dim
-        pk, pv = self._vec(k, dtype, "k", numel), self._vec(v, dtype, "v", numel)
-        _check(self._lib.akashic_mem_kv_read(self._cfg, self.data.data_ptr(), ps, n,
-                                             self._dtypes[dtype], pk, pv, self.status.data_ptr(),
-                                             self._on(stream)))
+            pv = v.data_ptr()
+        else:
+            pv = self._vec(v, dtype, "v", numel)
+        rc = self._read(self._cfg, self._data_ptr, ps, n, code, pk, pv, self._status_ptr,
+                        self._on(stream))
+        if rc:
+            _check(rc)
         return k, v
 
     def attend(self, q, blocks, kv_len=None, q_start=None, causal=True, prefix_len=None,
@@ -500,43 +518,46 @@ class KVCache:
         lse float32 [n_q, q_heads]); rows behind the last sequence are left as they
         were (zero, -inf-free, in tensors allocated here)."""
         torch = self._torch
-        dt = self._rows(q, "q")
+        dt, (n_q, q_heads, _), sq = self._rows(q, "q")
         if dt == 2:
             raise TypeError("q must be bfloat16 or float16, got torch.float32")
         if blocks.dim() != 2:
             raise ValueError("blocks must be [n_seq, max_blocks]")
         if q_tags is not None and self.tags is None:
             raise ValueError("q_tags need a tagged cache")
-        n_q, q_heads, _ = q.shape
         n_seq, width = blocks.shape
+        vec, i32, f32 = self._vec, torch.int32, torch.float32
         a = _KVAttend(
-            q.data_ptr(), q.stride(0), q.stride(1), dt, n_q, q_heads, n_seq,
-            self._vec(q_start, torch.int32, "q_start", n_seq + 1),
-            self._vec(kv_len, torch.int32, "kv_len", n_seq),
-            self._vec(blocks, torch.int64, "blocks", n_seq * width), width, bool(causal),
-            self._vec(prefix_len, torch.int32, "prefix_len", n_seq), scale, cap,
-            self._vec(slopes, torch.float32, "slopes", q_heads),
-            None if q_tags is None else self.tags.data_ptr(),
-            self._vec(q_tags, torch.int32, "q_tags", n_q))
+            q.data_ptr(), sq[0], sq[1], dt, n_q, q_heads, n_seq,
+            vec(q_start, i32, "q_start", n_seq + 1), vec(kv_len, i32, "kv_len", n_seq),
+            vec(blocks, torch.int64, "blocks", n_seq * width), width, 1 if causal else 0,
+            vec(prefix_len, i32, "prefix_len", n_seq), scale, cap,
+            vec(slopes, f32, "slopes", q_heads), None if q_tags is None else self._tags_ptr,
+            vec(q_tags, i32, "q_tags", n_q))
+        ref = ctypes.byref(a)
         if out is None:
             out = self._empty(q.shape, q.dtype, stream, zero=q_start is not None)
+            a.out = out.data_ptr()
+        else:
+            a.out = vec(out, q.dtype, "out", n_q * q_heads * self.head_dim)
         if lse is None:
-            lse = self._empty((n_q, q_heads), torch.float32, stream, zero=q_start is not None)
-        a.out = self._vec(out, q.dtype, "out", n_q * q_heads * self.head_dim)
-        a.lse = self._vec(lse, torch.float32, "lse", n_q * q_heads)
+            lse = self._empty((n_q, q_heads), f32, stream, zero=q_start is not None)
+            a.lse = lse.data_ptr()
+        else:
+            a.lse = vec(lse, f32, "lse", n_q * q_heads)
         key = (n_q, q_heads, n_seq, q_start is None)
         size = self._scratch.get(key)
         if size is None:
             need = ctypes.c_int64()
-            _check(self._lib.akashic_mem_kv_attend_scratch(self._cfg, ctypes.byref(a),
-                                                           ctypes.byref(need)))
+            _check(self._lib.akashic_mem_kv_attend_scratch(self._cfg, ref, ctypes.byref(need)))
             if len(self._scratch) > 4096:
                 self._scratch.clear()
             size = self._scratch[key] = need.value
         scratch = self._empty((size,), torch.uint8, stream)
-        _check(self._lib.akashic_mem_kv_attend(self._cfg, self.data.data_ptr(), ctypes.byref(a),
-                                               scratch.data_ptr(), size, self.status.data_ptr(),
-                                               self._on(stream)))
+        rc = self._attend(self._cfg, self._data_ptr, ref, scratch.data_ptr(), size,
+                          self._status_ptr, self._on(stream))
+        if rc:
+            _check(rc)
         return out, lse
 
     def sync(self, stream=None):

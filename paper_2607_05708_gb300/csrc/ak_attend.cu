@@ -24,6 +24,8 @@
 //  * P is fp16, 2^6 p: weights down to 2^-20 of the largest so far keep 11 bits; sums,
 //    maxima and accumulators are fp32.  The maximum is raised only when a
 //    score exceeds it by 2^8, so that the accumulators are rarely rescaled.
+#include <atomic>
+
 #include "ak_attend.cuh"
 #include "ak_sm100.cuh"
 
@@ -776,8 +778,16 @@ template <int BITS, int D, int NB>
 cudaError_t run_narrow(const AttendParams &p, int dtype, int ctas, int lo, int hi, cudaStream_t st) {
     using C = Narrow<BITS, D, NB>;
     auto *kernel = k_attend_narrow<BITS, D, NB>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    // once a device (the attribute stays; another thread that comes first does the same)
+    static std::atomic<bool> ready[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    if (dev >= 64 || !ready[dev].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) ready[dev].store(true, std::memory_order_release);
+    }
     kernel<<<ctas, NW * 32, C::SMEM, st>>>(p, dtype == AKASHIC_DTYPE_BF16, lo, hi, MIN_PER);
     return cudaGetLastError();
 }

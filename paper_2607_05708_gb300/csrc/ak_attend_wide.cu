@@ -21,6 +21,8 @@
 // fp16's normal range ends they are rounded to 2^-17 of that largest.
 #include <stddef.h>
 
+#include <atomic>
+
 #include "ak_attend.cuh"
 #include "ak_sm100.cuh"
 
@@ -158,9 +160,10 @@ constexpr uint32_t idesc_f16(int n) {
 // Bounded wait of one role; when any role's wait has expired the others give up too.
 __device__ __forceinline__ bool wide_wait(uint64_t *bar, uint32_t parity, volatile int *dead,
                                           int *status) {
-    for (uint32_t i = 0; i < SPIN_LIMIT; ++i) {
-        if (mbar_test_wait(bar, parity)) return true;
-        if ((i & 1023u) == 1023u && *dead) return false;
+    if (mbar_test_wait(bar, parity)) return true;
+    for (uint32_t i = 0; i < WAIT_LIMIT; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((i & 255u) == 255u && *dead) return false;
     }
     *dead = 1;
     set_status(status, AKASHIC_ETIMEOUT);
@@ -598,75 +601,89 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
             constexpr uint32_t id_s = idesc_f16(C::SN), id_o = idesc_f16(D) | IDESC_B_MN_MAJOR;
             const uint32_t go = lane == 0;
             const uint32_t q_at = desc_k(smem_u32(sq_)), k_at = desc_k(smem_u32(sk)), v_at = desc_mn(smem_u32(sv), N * 128);
-            uint32_t n_tile = 0, q_phase = 0, halves[MT] = {};     // halves: of the row tile, so far
+            uint32_t n_tile = 0, q_phase = 0, ph0 = 0, ph1 = 0;    // ph: halves of the row tile, so far
             bool ok = true;
+            // S of half h of the item (its first tile: n_tile) for row tile t; at D <= 128
+            // (h even) of the whole tile
+            auto scores = [&](int t, int h) {
+                const uint32_t x = n_tile + h / HPT, b = ((t ? ph1 : ph0) + h) & 1;
+                if (!ok) return;
+                // the row tiles share a tile's keys
+                if (t == 0 && !(ok = wide_wait(&kfull[x % ST], (x / ST) & 1, dead, p.status))) return;
+                tc_fence_after();
+                const uint32_t qa = q_at + (t * 128 * D * 2 >> 4), ka = k_at + (x % ST) * (C::KV_BYTES >> 4);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    umma_ss(go, tmem + C::S_COL + (t * 2 + b) * HT, qa + ((k / 4) * (128 * 128) >> 4) + 2 * (k % 4),
+                            ka + ((k / 4) * (N * 128) >> 4) + 2 * (k % 4), id_s, k > 0);
+                umma_commit_if(go, &sfull[t][b]);
+            };
+            auto values = [&](int t, int h) {
+                const uint32_t x = n_tile + h / HPT, c = (t ? ph1 : ph0) + h, b = c & 1;
+                if (!ok) return;
+                if (t == 0 && h % HPT == 0 && !(ok = wide_wait(&vfull[x % ST], (x / ST) & 1, dead, p.status))) return;
+                if (!(ok = wide_wait(&pfull[t][b], c >> 1 & 1, dead, p.status))) return;
+                tc_fence_after();
+                const uint32_t va = v_at + (x % ST) * (C::KV_BYTES >> 4) + h % HPT * (HT * 128 >> 4);
+#pragma unroll
+                for (int k = 0; k < HT / 16; ++k)
+                    umma_ts(go, tmem + t * D, tmem + C::S_COL + (t * 2 + b) * HT + k * 8, va + (2048 * k >> 4), id_o,
+                            (h > 0 || k > 0) ? 1u : 0u);
+                umma_commit_if(go, &odone[t][b]);
+            };
             while (left > 0 && ok) {
                 const int n = min(cur.units - cur.unit, left), nh = n * HPT;
                 const int mt = cur.q.nq * p.group - cur.tile * ROWS > 128 ? MT : 1;
-                // Whatever is ready is issued, of either row tile: scores once their buffer's
-                // weights have been taken (by products issued before: they run in order),
-                // O += P V once the weights are there.
-                int s_next[MT], v_next[MT], tiles = 0;             // halves issued; tiles done with
-#pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    s_next[t] = v_next[t] = t < mt ? 0 : nh;
-                    if (t < mt && ok) {
-                        ok = wide_wait(&qfull[t], q_phase >> t & 1, dead, p.status);
-                        q_phase ^= 1u << t;
+                if constexpr (MT == 1) {
+                    // Two buffers: scores once theirs is free (the weights before were taken
+                    // by products issued before: they run in order), O += P V once the weights
+                    // are there; whichever is ready.
+                    if (ok) ok = wide_wait(&qfull[0], q_phase & 1, dead, p.status);
+                    q_phase ^= 1u;
+                    int s_next = 0, v_next = 0;
+                    uint32_t polls = 0;
+                    while (ok && v_next < nh) {
+                        bool moved = false;
+                        if (s_next < nh && s_next - v_next <= 1 &&
+                            mbar_test_wait(&kfull[(n_tile + s_next) % ST], ((n_tile + s_next) / ST) & 1)) {
+                            scores(0, s_next++);
+                            moved = true;
+                        }
+                        const uint32_t c = ph0 + v_next;
+                        if (v_next < s_next && mbar_test_wait(&pfull[0][c & 1], c >> 1 & 1)) {
+                            values(0, v_next);
+                            umma_commit_if(go, &empty[(n_tile + v_next++) % ST]);
+                            moved = true;
+                        }
+                        // a bounded wait, like the others (wide_wait)
+                        polls = moved ? 0 : polls + 1;
+                        if ((polls & 1023u) == 1023u && *dead) ok = false;
+                        if (polls >= SPIN_LIMIT) {
+                            *dead = 1;
+                            set_status(p.status, AKASHIC_ETIMEOUT);
+                            ok = false;
+                        }
                     }
-                }
-                uint32_t polls = 0;
-                while (ok && tiles < n) {
-                    bool moved = false;
+                } else {
 #pragma unroll
                     for (int t = 0; t < MT; ++t) {
-                        if (s_next[t] < nh && s_next[t] - v_next[t] <= (HPT == 2 ? 0 : 1)) {
-                            const int h = s_next[t];
-                            const uint32_t x = n_tile + h / HPT, b = (halves[t] + h) & 1;
-                            if (mbar_test_wait(&kfull[x % ST], (x / ST) & 1)) {
-                                tc_fence_after();
-                                const uint32_t qa = q_at + (t * 128 * D * 2 >> 4), ka = k_at + (x % ST) * (C::KV_BYTES >> 4);
-#pragma unroll
-                                for (int k = 0; k < D / 16; ++k)
-                                    umma_ss(go, tmem + C::S_COL + (t * 2 + b) * HT, qa + ((k / 4) * (128 * 128) >> 4) + 2 * (k % 4),
-                                            ka + ((k / 4) * (N * 128) >> 4) + 2 * (k % 4), id_s, k > 0);
-                                umma_commit_if(go, &sfull[t][b]);
-                                s_next[t] += HPT;                  // of a whole tile
-                                moved = true;
-                            }
-                        }
-                        if (v_next[t] < s_next[t]) {
-                            const int h = v_next[t];
-                            const uint32_t x = n_tile + h / HPT, c = halves[t] + h, b = c & 1;
-                            if (mbar_test_wait(&pfull[t][b], c >> 1 & 1) && mbar_test_wait(&vfull[x % ST], (x / ST) & 1)) {
-                                tc_fence_after();
-                                const uint32_t va = v_at + (x % ST) * (C::KV_BYTES >> 4) + h % HPT * (HT * 128 >> 4);
-#pragma unroll
-                                for (int k = 0; k < HT / 16; ++k)
-                                    umma_ts(go, tmem + t * D, tmem + C::S_COL + (t * 2 + b) * HT + k * 8, va + (2048 * k >> 4), id_o,
-                                            (h > 0 || k > 0) ? 1u : 0u);
-                                umma_commit_if(go, &odone[t][b]);
-                                ++v_next[t];
-                                moved = true;
-                                if (min(v_next[0], v_next[MT - 1]) / HPT > tiles) {
-                                    umma_commit_if(go, &empty[(n_tile + tiles) % ST]);
-                                    ++tiles;
-                                }
-                            }
-                        }
+                        if (!ok || t >= mt) break;
+                        ok = wide_wait(&qfull[t], q_phase >> t & 1, dead, p.status);
+                        q_phase ^= 1u << t;
+                        scores(t, 0);
                     }
-                    // a bounded wait, like the others (wide_wait)
-                    polls = moved ? 0 : polls + 1;
-                    if ((polls & 1023u) == 1023u && *dead) ok = false;
-                    if (polls >= SPIN_LIMIT) {
-                        *dead = 1;
-                        set_status(p.status, AKASHIC_ETIMEOUT);
-                        ok = false;
-                    }
+                    for (int h = 0; ok && h < nh; ++h)
+#pragma unroll
+                        for (int t = 0; t < MT; ++t) {
+                            if (t >= mt) break;
+                            values(t, h);
+                            if (h % HPT < HPT - 1) continue;
+                            if (ok && t == mt - 1) umma_commit_if(go, &empty[(n_tile + h / HPT) % ST]);
+                            if (h + 1 < nh) scores(t, h + 1);
+                        }
                 }
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-                    if (t < mt) halves[t] += nh;
+                ph0 += nh;
+                if (mt > 1) ph1 += nh;
                 n_tile += n;
                 left -= n;
                 if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
@@ -695,7 +712,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 // ---- the warp's 32 query rows, 16 bytes a lane: bf16 scaled by a power of two
                 // to a largest magnitude in [1, 2)
                 constexpr int CH = D / 8, RP = 32 / CH;
-                constexpr int AT_ONCE = CH < 16 ? CH : 16;
+                constexpr int AT_ONCE = 4;             // (short code: it runs once an item, from a cold cache)
 #pragma unroll 1
                 for (int y0 = 0; y0 < CH; y0 += AT_ONCE) {
                     uint4 z[AT_ONCE];
@@ -872,7 +889,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 const int up = rv + (BITS == 4 ? UP : 0);
                 const float inv = whole ? (l > 0.f ? 1.f / l : l) : 1.f, up0 = pow2i(up / 2), up1 = pow2i(up - up / 2);
                 const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + hd;
-#pragma unroll 2
+#pragma unroll 1
                 for (int d = 0; d < D; d += 32) {
                     uint32_t y[32];
                     tmem_ld32(o_at + d, y);
@@ -918,8 +935,16 @@ template <int BITS, int D>
 cudaError_t run_wide(const AttendParams &p, int dtype, int ctas, int lo, int hi, cudaStream_t st) {
     using C = Wide<D>;
     auto *kernel = k_attend_wide<BITS, D>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    // once a device (the attribute stays; another thread that comes first does the same)
+    static std::atomic<bool> ready[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    if (dev >= 64 || !ready[dev].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) ready[dev].store(true, std::memory_order_release);
+    }
     kernel<<<ctas, C::THREADS, C::SMEM, st>>>(p, dtype == AKASHIC_DTYPE_BF16, lo, hi);
     return cudaGetLastError();
 }

@@ -82,7 +82,6 @@ __device__ __forceinline__ KvPlace kv_place(int64_t s, int h, int heads, uint32_
     return {((int64_t)b * heads + h) * per_block + (u - b * per_block), (int)(s & 15)};
 }
 
-template <typename T> struct Raw { T v[16]; };
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -90,207 +89,251 @@ __device__ __forceinline__ void from_f32(float x, float &y) { y = x; }
 __device__ __forceinline__ void from_f32(float x, __half &y) { y = __float2half_rn(x); }
 __device__ __forceinline__ void from_f32(float x, __nv_bfloat16 &y) { y = __float2bfloat16_rn(x); }
 
+// The 16 codes of a group, biased to be positive, `bits` wide and in the cache's
+// order (ak_kv.cuh).  q = x / s correctly rounded (one Newton step on x inv); where
+// x / s is a whole number and a half q is just that, and otherwise it is on the
+// same side of it: for 16-bit inputs x and s (c + 1/2) have at most 19 bits, so they
+// differ by 2^-19 relative or not at all; for fp32 the remainder is looked at.
+// 1.5 2^23 + bias added rounds half to even and leaves the code in the low bits; the
+// words are sums of these shifted into place, less the constants' sum.  No clamp:
+// |x / s| stays below 7.3 and 127.3.
+template <typename T, int BITS>
+__device__ __forceinline__ void kv_codes(const float (&f)[16], float s, uint32_t (&w)[BITS / 2]) {
+    constexpr int TOP = BITS == 4 ? 7 : 127, PER = 32 / BITS;
+    constexpr float BASE = 12582912.f + (TOP + 1);
+    const float inv = __frcp_rn(s);
+    float worst = 0.f;
+#pragma unroll
+    for (int i = 0; i < BITS / 2; ++i) {
+        w[i] = 0;
+        uint32_t less = 0;
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const float x = f[i * PER + p], q0 = x * inv;
+            const float m = fmaf(fmaf(-q0, s, x), inv, q0) + BASE;
+            if constexpr (sizeof(T) == 4) worst = fmaxf(worst, fabsf(fmaf(BASE - m, s, x)));
+            const int at = BITS == 4 ? 4 * (p >> 1) + 16 * (p & 1) : 8 * p;
+            w[i] += __float_as_uint(m) << at;
+            less += 0x4b400000u << at;
+        }
+        w[i] -= less;
+    }
+    if (sizeof(T) == 4 && worst > 0.5f * s) {
+#pragma unroll
+        for (int i = 0; i < BITS / 2; ++i) {
+            w[i] = 0;
+#pragma unroll
+            for (int p = 0; p < PER; ++p)
+                w[i] |= (uint32_t)(kv_code(f[i * PER + p], s, inv, TOP) + TOP + 1)
+                        << (BITS == 4 ? 4 * (p >> 1) + 16 * (p & 1) : 8 * p);
+        }
+    }
+}
+
 template <typename T, int BITS, int D, bool WIDE>
 __global__ void __launch_bounds__(256)
 k_kv_write(unsigned char *__restrict__ cache, const T *__restrict__ k, const T *__restrict__ v,
            int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head,
            const int64_t *__restrict__ slots, int32_t *__restrict__ tags,
            const int32_t *__restrict__ new_tags, int64_t n, int heads, uint32_t units,
-           uint32_t per_block, int *status) {
+           uint32_t per_block, int tokens, int *status) {
     using U = KvUnit<BITS, D>;
     constexpr int G = U::GROUPS;
     const bool is_v = blockIdx.y;
-    const int64_t total = n * heads * G;
-    const int64_t stride = (int64_t)gridDim.x * 256;
-    // the bound is rounded up to whole warps: the row's lanes meet in shuffles
-    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < ((total + 31) & ~31LL); x += stride) {
-        const int64_t row = x / G;
-        const int gr = (int)(x % G);
-        const int64_t i = row / heads;
-        const int h = (int)(row - i * heads);
-        const bool in = x < total;
-        const int64_t slot = in ? slots[i] : -1;
-        const KvPlace at = kv_place(slot, h, heads, units, per_block, status);
-        float f[16];
-        if (at.unit >= 0) {
-            const T *src = is_v ? v + i * v_row + h * v_head : k + i * k_row + h * k_head;
-            src += gr * 16;
-            alignas(16) T raw[16];
-            if constexpr (WIDE) {
-#pragma unroll
-                for (int w = 0; w < (int)sizeof(raw) / 16; ++w)
-                    ((int4 *)raw)[w] = __ldcs((const int4 *)src + w);
-            } else {
-#pragma unroll
-                for (int w = 0; w < 16; ++w) raw[w] = src[w];
-            }
-#pragma unroll
-            for (int w = 0; w < 16; ++w) f[w] = kv_finite(to_f32(raw[w]));
-        } else {
+    const T *base = is_v ? v : k;
+    const int64_t row_stride = is_v ? v_row : k_row, head_stride = is_v ? v_head : k_head;
+    for (int64_t i0 = (int64_t)blockIdx.x * tokens; i0 < n; i0 += (int64_t)gridDim.x * tokens) {
+        const uint32_t total = (uint32_t)min((int64_t)tokens, n - i0) * heads * G;
+        // the bound is rounded up to whole warps: the row's lanes meet in shuffles
+        for (uint32_t x = threadIdx.x; x < ((total + 31) & ~31u); x += 256) {
+            const uint32_t row = x / G, gr = x % G, ti = row / (uint32_t)heads, h = row - ti * heads;
+            const int64_t i = i0 + ti, slot = x < total ? slots[i] : -1;
+            const KvPlace at = kv_place(slot, h, heads, units, per_block, status);
+            float f[16];
 #pragma unroll
             for (int w = 0; w < 16; ++w) f[w] = 0.f;
-        }
-        float ag = 0.f;
+            if (at.unit >= 0) {
+                const T *src = base + i * row_stride + h * head_stride + gr * 16;
+                alignas(16) T raw[16];
+                if constexpr (WIDE) {
 #pragma unroll
-        for (int w = 0; w < 16; ++w) ag = fmaxf(ag, fabsf(f[w]));
-        float a = ag;
+                    for (int w = 0; w < (int)sizeof(raw) / 16; ++w)
+                        ((int4 *)raw)[w] = __ldcs((const int4 *)src + w);
+                } else {
 #pragma unroll
-        for (int o = G / 2; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-        if (at.unit < 0) continue;
-        unsigned char *dst = cache + at.unit * U::BYTES;
-        const int t = at.token, d0 = gr * 16;
-        if constexpr (BITS == 4) {
-            const int E = kv_row_exp(a);
-            const uint32_t b = kv_scale_byte(ag, E);
-            const float s = kv_scale_of(b) * pow2i(E), inv = __frcp_rn(s);
-            uint32_t w[2];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                w[q] = 0;
-#pragma unroll
-                for (int p = 0; p < 8; ++p)
-                    w[q] |= (uint32_t)(kv_code(f[q * 8 + p], s, inv, 7) + 8)
-                            << (4 * (p >> 1) + 16 * (p & 1));
-            }
-            if (is_v) {
-                if (U::v_code(0, 8) == U::v_code(0, 0) + 4)
-                    *(uint2 *)(dst + U::v_code(t, d0)) = make_uint2(w[0], w[1]);
-                else {
-                    *(uint32_t *)(dst + U::v_code(t, d0)) = w[0];
-                    *(uint32_t *)(dst + U::v_code(t, d0 + 8)) = w[1];
+                    for (int w = 0; w < 16; ++w) raw[w] = src[w];
                 }
-                dst[U::v_scale(t, gr)] = (unsigned char)b;
-                if (gr == 0) dst[U::V_EXP + U::v_row(t)] = (unsigned char)(E + 127);
-            } else {
-                *(uint2 *)(dst + U::k_code(t, d0)) = make_uint2(w[0], w[1]);
-                dst[U::k_scale(t, gr)] = (unsigned char)b;
-                if (gr == 0) dst[U::K_EXP + U::k_row(t)] = (unsigned char)(E + 127);
-            }
-        } else {
-            const uint32_t sb = kv_scale_bf16(a);
-            const float s = __uint_as_float(sb << 16), inv = __frcp_rn(s);
-            uint32_t w[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                w[q] = 0;
-#pragma unroll
-                for (int p = 0; p < 4; ++p)
-                    w[q] |= (uint32_t)(kv_code(f[q * 4 + p], s, inv, 127) + 128) << (8 * p);
+                for (int w = 0; w < 16; ++w) f[w] = to_f32(raw[w]);
             }
-            if (is_v) {
-                if (U::v_code(0, 8) == U::v_code(0, 0) + 8)
-                    *(uint4 *)(dst + U::v_code(t, d0)) = make_uint4(w[0], w[1], w[2], w[3]);
-                else {
-                    *(uint2 *)(dst + U::v_code(t, d0)) = make_uint2(w[0], w[1]);
-                    *(uint2 *)(dst + U::v_code(t, d0 + 8)) = make_uint2(w[2], w[3]);
+            float ag = 0.f, odd = 0.f;         // odd: not 0 with a NaN or an infinity
+#pragma unroll
+            for (int w = 0; w < 16; ++w) ag = fmaxf(ag, fabsf(f[w])), odd = fmaf(f[w], 0.f, odd);
+            if (odd != 0.f) {
+                ag = 0.f;
+#pragma unroll
+                for (int w = 0; w < 16; ++w) f[w] = kv_finite(f[w]), ag = fmaxf(ag, fabsf(f[w]));
+            }
+            float a = ag;
+#pragma unroll
+            for (int o = G / 2; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+            if (at.unit < 0) continue;
+            unsigned char *dst = cache + at.unit * U::BYTES;
+            const int t = at.token, d0 = gr * 16;
+            uint32_t w[BITS / 2];
+            if constexpr (BITS == 4) {
+                const int E = kv_row_exp(a);
+                const uint32_t b = kv_scale_byte(ag, E);
+                kv_codes<T, 4>(f, kv_scale_of(b) * pow2i(E), w);
+                if (is_v) {
+                    if (U::v_code(0, 8) == U::v_code(0, 0) + 4)
+                        *(uint2 *)(dst + U::v_code(t, d0)) = make_uint2(w[0], w[1]);
+                    else {
+                        *(uint32_t *)(dst + U::v_code(t, d0)) = w[0];
+                        *(uint32_t *)(dst + U::v_code(t, d0 + 8)) = w[1];
+                    }
+                    dst[U::v_scale(t, gr)] = (unsigned char)b;
+                    if (gr == 0) dst[U::V_EXP + U::v_row(t)] = (unsigned char)(E + 127);
+                } else {
+                    *(uint2 *)(dst + U::k_code(t, d0)) = make_uint2(w[0], w[1]);
+                    dst[U::k_scale(t, gr)] = (unsigned char)b;
+                    if (gr == 0) dst[U::K_EXP + U::k_row(t)] = (unsigned char)(E + 127);
                 }
-                if (gr == 0) ((uint16_t *)(dst + U::V_SCALES))[U::v_row(t)] = (uint16_t)sb;
             } else {
-                *(uint4 *)(dst + U::k_code(t, d0)) = make_uint4(w[0], w[1], w[2], w[3]);
-                if (gr == 0) ((uint16_t *)(dst + U::K_SCALES))[U::k_row(t)] = (uint16_t)sb;
+                const uint32_t sb = kv_scale_bf16(a);
+                kv_codes<T, 8>(f, __uint_as_float(sb << 16), w);
+                if (is_v) {
+                    if (U::v_code(0, 8) == U::v_code(0, 0) + 8)
+                        *(uint4 *)(dst + U::v_code(t, d0)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    else {
+                        *(uint2 *)(dst + U::v_code(t, d0)) = make_uint2(w[0], w[1]);
+                        *(uint2 *)(dst + U::v_code(t, d0 + 8)) = make_uint2(w[2], w[3]);
+                    }
+                    if (gr == 0) ((uint16_t *)(dst + U::V_SCALES))[U::v_row(t)] = (uint16_t)sb;
+                } else {
+                    *(uint4 *)(dst + U::k_code(t, d0)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (gr == 0) ((uint16_t *)(dst + U::K_SCALES))[U::k_row(t)] = (uint16_t)sb;
+                }
             }
+            if (tags && !is_v && h == 0 && gr == 0) tags[slot] = new_tags ? new_tags[i] : 0;
         }
-        if (tags && !is_v && h == 0 && gr == 0) tags[slot] = new_tags ? new_tags[i] : 0;
     }
 }
 
+// code * s with code = biased - bias, exact: the biased code put under 2^23 and taken
+// away again (an integer conversion runs at a quarter of the rate).
+template <int BIAS>
+__device__ __forceinline__ float kv_value(uint32_t biased, float s) {
+    return s * (__uint_as_float(0x4b000000u | biased) - (8388608.f + BIAS));
+}
 template <typename T, int BITS, int D, bool WIDE>
 __global__ void __launch_bounds__(256)
 k_kv_read(const unsigned char *__restrict__ cache, T *__restrict__ k, T *__restrict__ v,
           const int64_t *__restrict__ slots, int64_t n, int heads, uint32_t units,
-          uint32_t per_block, int *status) {
+          uint32_t per_block, int tokens, int *status) {
     using U = KvUnit<BITS, D>;
     constexpr int G = U::GROUPS;
     const bool is_v = blockIdx.y;
-    const int64_t total = n * heads * G;
-    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < total;
-         x += (int64_t)gridDim.x * 256) {
-        const int64_t row = x / G;
-        const int gr = (int)(x % G), d0 = gr * 16;
-        const int64_t i = row / heads;
-        const int h = (int)(row - i * heads);
-        const KvPlace at = kv_place(slots[i], h, heads, units, per_block, status);
-        alignas(16) T raw[16];
-        float f[16];
-        if (at.unit < 0) {
+    T *out = is_v ? v : k;
+    for (int64_t i0 = (int64_t)blockIdx.x * tokens; i0 < n; i0 += (int64_t)gridDim.x * tokens) {
+        const uint32_t total = (uint32_t)min((int64_t)tokens, n - i0) * heads * G;
+        for (uint32_t x = threadIdx.x; x < total; x += 256) {
+            const uint32_t row = x / G, gr = x % G, ti = row / (uint32_t)heads, h = row - ti * heads;
+            const int d0 = gr * 16;
+            const KvPlace at = kv_place(slots[i0 + ti], h, heads, units, per_block, status);
+            alignas(16) T raw[16];
+            float f[16];
+            if (at.unit < 0) {
 #pragma unroll
-            for (int p = 0; p < 16; ++p) f[p] = 0.f;
-        } else {
-            const unsigned char *src = cache + at.unit * U::BYTES;
-            const int t = at.token;
-            if constexpr (BITS == 4) {
-                uint32_t w[2];
-                float s;
-                if (is_v) {
-                    w[0] = *(const uint32_t *)(src + U::v_code(t, d0));
-                    w[1] = *(const uint32_t *)(src + U::v_code(t, d0 + 8));
-                    s = kv_scale_of(src[U::v_scale(t, gr)]) *
-                        pow2i((int)src[U::V_EXP + U::v_row(t)] - 127);
-                } else {
-                    const uint2 q = *(const uint2 *)(src + U::k_code(t, d0));
-                    w[0] = q.x, w[1] = q.y;
-                    s = kv_scale_of(src[U::k_scale(t, gr)]) *
-                        pow2i((int)src[U::K_EXP + U::k_row(t)] - 127);
-                }
-#pragma unroll
-                for (int p = 0; p < 16; ++p)
-                    f[p] = s * (float)((int)((w[p >> 3] >> (4 * ((p & 7) >> 1) + 16 * (p & 1))) & 15u) - 8);
+                for (int p = 0; p < 16; ++p) f[p] = 0.f;
             } else {
-                uint32_t w[4];
-                uint32_t sb;
-                if (is_v) {
-                    const uint2 q0 = *(const uint2 *)(src + U::v_code(t, d0));
-                    const uint2 q1 = *(const uint2 *)(src + U::v_code(t, d0 + 8));
-                    w[0] = q0.x, w[1] = q0.y, w[2] = q1.x, w[3] = q1.y;
-                    sb = ((const uint16_t *)(src + U::V_SCALES))[U::v_row(t)];
+                const unsigned char *src = cache + at.unit * U::BYTES;
+                const int t = at.token;
+                uint32_t w[BITS / 2];
+                float s;
+                if constexpr (BITS == 4) {
+                    if (is_v) {
+                        if (U::v_code(0, 8) == U::v_code(0, 0) + 4) {
+                            const uint2 q = *(const uint2 *)(src + U::v_code(t, d0));
+                            w[0] = q.x, w[1] = q.y;
+                        } else {
+                            w[0] = *(const uint32_t *)(src + U::v_code(t, d0));
+                            w[1] = *(const uint32_t *)(src + U::v_code(t, d0 + 8));
+                        }
+                        s = kv_scale_of(src[U::v_scale(t, gr)]) *
+                            pow2i((int)src[U::V_EXP + U::v_row(t)] - 127);
+                    } else {
+                        const uint2 q = *(const uint2 *)(src + U::k_code(t, d0));
+                        w[0] = q.x, w[1] = q.y;
+                        s = kv_scale_of(src[U::k_scale(t, gr)]) *
+                            pow2i((int)src[U::K_EXP + U::k_row(t)] - 127);
+                    }
+#pragma unroll
+                    for (int p = 0; p < 16; ++p)
+                        f[p] = kv_value<8>((w[p >> 3] >> (4 * ((p & 7) >> 1) + 16 * (p & 1))) & 15u, s);
                 } else {
-                    const uint4 q = *(const uint4 *)(src + U::k_code(t, d0));
-                    w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
-                    sb = ((const uint16_t *)(src + U::K_SCALES))[U::k_row(t)];
+                    uint32_t sb;
+                    if (is_v) {
+                        const uint2 q0 = *(const uint2 *)(src + U::v_code(t, d0));
+                        const uint2 q1 = *(const uint2 *)(src + U::v_code(t, d0 + 8));
+                        w[0] = q0.x, w[1] = q0.y, w[2] = q1.x, w[3] = q1.y;
+                        sb = ((const uint16_t *)(src + U::V_SCALES))[U::v_row(t)];
+                    } else {
+                        const uint4 q = *(const uint4 *)(src + U::k_code(t, d0));
+                        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+                        sb = ((const uint16_t *)(src + U::K_SCALES))[U::k_row(t)];
+                    }
+                    s = __uint_as_float(sb << 16);
+#pragma unroll
+                    for (int p = 0; p < 16; ++p) f[p] = kv_value<128>((w[p >> 2] >> (8 * (p & 3))) & 255u, s);
                 }
-                const float s = __uint_as_float(sb << 16);
-#pragma unroll
-                for (int p = 0; p < 16; ++p)
-                    f[p] = s * (float)((int)((w[p >> 2] >> (8 * (p & 3))) & 255u) - 128);
             }
-        }
 #pragma unroll
-        for (int p = 0; p < 16; ++p) from_f32(f[p], raw[p]);
-        T *dst = (is_v ? v : k) + x * 16;
-        if constexpr (WIDE) {
+            for (int p = 0; p < 16; ++p) from_f32(f[p], raw[p]);
+            T *dst = out + i0 * heads * D + (int64_t)x * 16;
+            if constexpr (WIDE) {
 #pragma unroll
-            for (int w = 0; w < (int)sizeof(raw) / 16; ++w)
-                __stcs((int4 *)dst + w, ((const int4 *)raw)[w]);
-        } else {
+                for (int w = 0; w < (int)sizeof(raw) / 16; ++w)
+                    __stcs((int4 *)dst + w, ((const int4 *)raw)[w]);
+            } else {
 #pragma unroll
-            for (int p = 0; p < 16; ++p) dst[p] = raw[p];
+                for (int p = 0; p < 16; ++p) dst[p] = raw[p];
+            }
         }
     }
 }
 
-int kv_grid(int64_t threads) {
-    const int64_t want = ceil_div(threads, (int64_t)256), most = (int64_t)device_sm_count() * 16;
-    return (int)(want < most ? want : most);
+// A CTA takes `tokens` at a time: enough for its 256 threads, or a single one where the
+// heads fill them.
+int kv_tokens(int heads, int groups) {
+    const int t = 256 / (heads * groups);
+    return t > 1 ? t : 1;
+}
+unsigned kv_grid(int64_t n, int tokens) {
+    const int64_t want = ceil_div(n, (int64_t)tokens), most = (int64_t)device_sm_count() * 16;
+    return (unsigned)(want < most ? want : most);
 }
 
 template <typename T, int BITS, int D>
 void launch_write(const KvRows &r, cudaStream_t st) {
-    const dim3 grid(kv_grid(r.n * r.cfg->heads * (D / 16)), 2);
+    const int tokens = kv_tokens(r.cfg->heads, D / 16);
     const uint32_t per = (uint32_t)(r.cfg->block_tokens / KV_UNIT);
     const uint32_t units = (uint32_t)(r.cfg->n_blocks * per);
     auto *kernel = r.wide ? k_kv_write<T, BITS, D, true> : k_kv_write<T, BITS, D, false>;
-    kernel<<<grid, 256, 0, st>>>(r.cache, (const T *)r.in[0], (const T *)r.in[1], r.row_stride[0],
-                                 r.head_stride[0], r.row_stride[1], r.head_stride[1], r.slots,
-                                 r.tags, r.new_tags, r.n, r.cfg->heads, units, per, r.status);
+    kernel<<<dim3(kv_grid(r.n, tokens), 2), 256, 0, st>>>(
+        r.cache, (const T *)r.in[0], (const T *)r.in[1], r.row_stride[0], r.head_stride[0],
+        r.row_stride[1], r.head_stride[1], r.slots, r.tags, r.new_tags, r.n, r.cfg->heads, units,
+        per, tokens, r.status);
 }
 template <typename T, int BITS, int D>
 void launch_read(const KvRows &r, cudaStream_t st) {
-    const dim3 grid(kv_grid(r.n * r.cfg->heads * (D / 16)), 2);
+    const int tokens = kv_tokens(r.cfg->heads, D / 16);
     const uint32_t per = (uint32_t)(r.cfg->block_tokens / KV_UNIT);
     const uint32_t units = (uint32_t)(r.cfg->n_blocks * per);
     auto *kernel = r.wide ? k_kv_read<T, BITS, D, true> : k_kv_read<T, BITS, D, false>;
-    kernel<<<grid, 256, 0, st>>>(r.cache, (T *)r.out[0], (T *)r.out[1], r.slots, r.n,
-                                 r.cfg->heads, units, per, r.status);
+    kernel<<<dim3(kv_grid(r.n, tokens), 2), 256, 0, st>>>(r.cache, (T *)r.out[0], (T *)r.out[1],
+                                                          r.slots, r.n, r.cfg->heads, units, per,
+                                                          tokens, r.status);
 }
 
 template <typename T, int BITS>

@@ -202,23 +202,30 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
         turn = 0, turn_end = steps * UPS;
         __syncwarp();
     };
+    // The lanes whose turn it is arrive on the stage's barrier and copy their units, by predicate:
+    // the branches around this took a tenth of the step's instructions.
+    auto fetch = [&](uint64_t *b, unsigned char *stage_at, unsigned char *flags, int j, bool turn_now, bool have) {
+        const uint32_t bytes = have ? U::BYTES + (tags ? 64 : 0) : 0;
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t"
+            "setp.ne.u32 p, %0, 0;\n\t"
+            "setp.ne.and.u32 q, %1, 0, p;\n\t"
+            "@p st.shared.u8 [%2], %1;\n\t"
+            "@p mbarrier.arrive.expect_tx.shared::cta.b64 _, [%3], %4;\n\t"
+            "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%5], [%6], %7, [%3];\n\t}" ::"r"(
+                (uint32_t)turn_now),
+            "r"((uint32_t)have), "r"(smem_u32(flags + j)), "r"(smem_u32(b)), "r"(bytes),
+            "r"(smem_u32(stage_at) + j * U::BYTES), "l"(p.cache + (uint64_t)my_unit * U::BYTES), "n"(U::BYTES)
+            : "memory");
+        if (tags && turn_now && have)
+            bulk_load(stage_at + UPS * U::BYTES + j * 64, p.tags + (uint64_t)my_slots * 16, 64, b);
+    };
     auto issue = [&]() {
         if (fetch_left == 0) return;
         if (turn == turn_end) look_up();
         const int j = lane - turn;
-        if ((unsigned)j < (unsigned)UPS) {
-            uint64_t *b = bar + fetch_stage;
-            unsigned char *dst = ring + fetch_stage * C::STAGE;
-            const bool have = my_unit != NONE;
-            listed[fetch_stage * 2 + j] = have;
-            if (have) {
-                mbar_expect_tx(b, U::BYTES + (tags ? 64 : 0));
-                bulk_load(dst + j * U::BYTES, p.cache + (uint64_t)my_unit * U::BYTES, U::BYTES, b);
-                if (tags) bulk_load(dst + UPS * U::BYTES + j * 64, p.tags + (uint64_t)my_slots * 16, 64, b);
-            } else {
-                mbar_arrive(b);
-            }
-        }
+        fetch(bar + fetch_stage, ring + fetch_stage * C::STAGE, listed + fetch_stage * 2, j, (unsigned)j < (unsigned)UPS,
+              my_unit != NONE);
         turn += UPS, --fetch_left;
         fetch_stage = fetch_stage + 1 == NS ? 0 : fetch_stage + 1;
     };
@@ -283,7 +290,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
 
         int tok = cur.unit * STEP;
         for (int it = 0; ok && it < n; ++it, tok += STEP) {
-            if (!mbar_wait(bar + stage, phase, p.status)) {
+            if (!mbar_test_wait(bar + stage, phase) && !mbar_wait(bar + stage, phase, p.status)) {
                 ok = false;                    // the other copies still land: wait for them
                 const int out = min(left - it, NS);
                 for (int k = 1; k < out; ++k) {
@@ -295,8 +302,8 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
             }
             const unsigned char *st = ring + stage * C::STAGE;
             const uint32_t have = UPS == 2 ? *(const uint16_t *)(listed + stage * 2) : listed[stage * 2];
-            if (have) {
-                // ---- S^T = K Q^T, per unit
+            {
+                // ---- S^T = K Q^T, per unit (of a step without listed units all is masked)
                 float s[UPS][NB][4], kf0[UPS], kf1[UPS];   // scales of the keys of tokens g, g + 8
 #pragma unroll
                 for (int j = 0; j < UPS; ++j) {

@@ -163,19 +163,36 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
     mbar_fence_init();
     if (lane < 2) entries[2 * warp + lane].seq = -1;
     if (tid == 0) p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
-    attend_sums(p, ROWS, STEP, lo, hi, prefix);
-    const int64_t total = prefix[NW * 32], workers = (int64_t)gridDim.x * NW;
-    const int64_t per = max((int64_t)min_per, (total + workers - 1) / workers);
-    const int64_t first = per * (blockIdx.x * NW + warp);
-    int left = (int)max((int64_t)0, min(per, total - first));   // steps of this warp
+    // The warp's share: of all steps, or (p.direct) of the CTA's one item.
+    AttendCursor cur = {};
+    int64_t per, first;
+    int left;
+    if (p.direct) {
+        cur.seq = blockIdx.x / p.heads, cur.head = blockIdx.x % p.heads;
+        cur.q = attend_seq(p, cur.seq);
+        cur.units = attend_units(p, cur.q, 0, ROWS, STEP);
+        per = (cur.units + NW - 1) / NW;
+        first = per * warp;
+        cur.unit = (int)first;
+        left = max(0, min((int)per, cur.units - cur.unit));
+        __syncthreads();
+    } else {
+        attend_sums(p, ROWS, STEP, lo, hi, prefix);
+        const int64_t total = prefix[NW * 32], workers = (int64_t)gridDim.x * NW;
+        per = max((int64_t)min_per, (total + workers - 1) / workers);
+        first = per * (blockIdx.x * NW + warp);
+        left = (int)max((int64_t)0, min(per, total - first));      // steps of this warp
+        if (left > 0) cur = attend_find(p, ROWS, STEP, lo, hi, prefix, first);
+        __syncthreads();
+    }
 
     // Fetching runs up to NS steps ahead of the work, across items.  Lane x looks up the x-th unit
     // from the present one, a warp's worth at a time, and copies it itself when
     // its turn comes.  Where fetching stands is kept in shared memory: it is needed
     // once a look-up only, and the registers are not there.
     constexpr int PER = 32 / UPS;              // steps of a look-up
-    constexpr uint32_t NONE = 0xffffffffu;
-    uint32_t my_unit = NONE, my_slots = 0;     // this lane's unit of the cache, its slots / 16
+    uint32_t my_unit = 0, my_slots = 0;        // this lane's unit of the cache, its slots / 16
+    int my_state = 0;                          // 0: no token of it is seen, 1: by its tags, 3: all are
     int fetch_left = left, turn = 32, turn_end = 32, fetch_stage = 0;
     const bool tags = p.tags != nullptr, heavy = p.cap > 0.f || p.slopes;
     auto look_up = [&]() {
@@ -188,13 +205,27 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
         __syncwarp();
         const int steps = min(PER, n - i), u = (x.unit + i) * UPS + lane;
         if (lane == 0) *ahead = Fetch{x, i + steps, n};
-        my_unit = NONE;
+        my_state = 0;
         if (lane < steps * UPS && u < (x.q.kv + KV_UNIT - 1) / KV_UNIT) {
             const int b = u / p.per_block, w = u - b * p.per_block;
             const int64_t id = p.blocks[x.seq * p.max_blocks + b];
             if (id >= 0 && id < p.n_blocks) {
                 my_slots = (uint32_t)id * p.per_block + w;
                 my_unit = ((uint32_t)id * p.heads + x.head) * p.per_block + w;
+                my_state = tags ? 1 : 3;
+                const int r0 = x.tile * ROWS, r1 = min(r0 + ROWS, x.q.nq * p.group) - 1;
+                if (tags && r0 / p.group == r1 / p.group) {
+                    // One query: a unit of other tags is not fetched, one of its tag needs no
+                    // look at the tokens (a retrieved chunk has one tag).
+                    const int qt = p.q_tags[x.q.row0 + r0 / p.group];
+                    int same = 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int4 y = ((const int4 *)p.tags)[(uint64_t)my_slots * 4 + k];
+                        same += (y.x == qt) + (y.y == qt) + (y.z == qt) + (y.w == qt);
+                    }
+                    my_state = qt < 0 || same == 0 ? 0 : same == 16 ? 3 : 1;
+                }
             } else if (id != -1) {
                 set_status(p.status, AKASHIC_EDEVICE);
             }
@@ -204,8 +235,8 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
     };
     // The lanes whose turn it is arrive on the stage's barrier and copy their units, by predicate:
     // the branches around this took a tenth of the step's instructions.
-    auto fetch = [&](uint64_t *b, unsigned char *stage_at, unsigned char *flags, int j, bool turn_now, bool have) {
-        const uint32_t bytes = have ? U::BYTES + (tags ? 64 : 0) : 0;
+    auto fetch = [&](uint64_t *b, unsigned char *stage_at, unsigned char *flags, int j, bool turn_now) {
+        const uint32_t bytes = my_state ? U::BYTES + (my_state == 1 ? 64 : 0) : 0;
         asm volatile(
             "{\n\t.reg .pred p, q;\n\t"
             "setp.ne.u32 p, %0, 0;\n\t"
@@ -214,24 +245,20 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
             "@p mbarrier.arrive.expect_tx.shared::cta.b64 _, [%3], %4;\n\t"
             "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%5], [%6], %7, [%3];\n\t}" ::"r"(
                 (uint32_t)turn_now),
-            "r"((uint32_t)have), "r"(smem_u32(flags + j)), "r"(smem_u32(b)), "r"(bytes),
+            "r"((uint32_t)my_state), "r"(smem_u32(flags + j)), "r"(smem_u32(b)), "r"(bytes),
             "r"(smem_u32(stage_at) + j * U::BYTES), "l"(p.cache + (uint64_t)my_unit * U::BYTES), "n"(U::BYTES)
             : "memory");
-        if (tags && turn_now && have)
+        if (turn_now && my_state == 1)
             bulk_load(stage_at + UPS * U::BYTES + j * 64, p.tags + (uint64_t)my_slots * 16, 64, b);
     };
     auto issue = [&]() {
         if (fetch_left == 0) return;
         if (turn == turn_end) look_up();
         const int j = lane - turn;
-        fetch(bar + fetch_stage, ring + fetch_stage * C::STAGE, listed + fetch_stage * 2, j, (unsigned)j < (unsigned)UPS,
-              my_unit != NONE);
+        fetch(bar + fetch_stage, ring + fetch_stage * C::STAGE, listed + fetch_stage * 2, j, (unsigned)j < (unsigned)UPS);
         turn += UPS, --fetch_left;
         fetch_stage = fetch_stage + 1 == NS ? 0 : fetch_stage + 1;
     };
-    AttendCursor cur;
-    if (left > 0) cur = attend_find(p, ROWS, STEP, lo, hi, prefix, first);
-    __syncthreads();
     if (left > 0) {
         if (lane == 0) *ahead = Fetch{cur, 0, min(cur.units - cur.unit, left)};
         __syncwarp();
@@ -302,8 +329,8 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
             }
             const unsigned char *st = ring + stage * C::STAGE;
             const uint32_t have = UPS == 2 ? *(const uint16_t *)(listed + stage * 2) : listed[stage * 2];
-            {
-                // ---- S^T = K Q^T, per unit (of a step without listed units all is masked)
+            if (have) {
+                // ---- S^T = K Q^T, per unit
                 float s[UPS][NB][4], kf0[UPS], kf1[UPS];   // scales of the keys of tokens g, g + 8
 #pragma unroll
                 for (int j = 0; j < UPS; ++j) {
@@ -381,7 +408,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                 // ---- scores in log2 units less the running maximum (mm = m - 6);
                 // what a row does not see is -inf
                 const int *tg = (const int *)(st + UPS * U::BYTES);
-                const bool masked = tags || tok > safe || have != (UPS == 2 ? 0x101u : 1u);
+                const bool masked = tok > safe || have != (UPS == 2 ? 0x303u : 3u);
                 float most = NEG;
 #pragma unroll
                 for (int j = 0; j < UPS; ++j) {
@@ -407,8 +434,9 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 const int col = b * 8 + 2 * c + (r & 1), t = j * 16 + g + (r < 2 ? 0 : 8);
-                                const bool seen = (have >> (8 * j) & 1) && tok + t < limit[col] &&
-                                                  (!tags || (tg[t] >= 0 && tg[t] == qtag[col]));
+                                const uint32_t state = have >> (8 * j) & 3u;
+                                const bool seen = state && tok + t < limit[col] &&
+                                                  (state == 3 || (tg[t] >= 0 && tg[t] == qtag[col]));
                                 if (!seen) s[j][b][r] = -INFINITY;
                             }
                         }
@@ -493,7 +521,8 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                             ti[j][i] = (int)(te[j][i >> 1] >> (16 * (i & 1)) & 0xffffu) - 127;
                             if (masked) {          // a slot without a token adds nothing
                                 const int t = j * 16 + 2 * c + (i & 1) + (i >> 1) * 8;
-                                if (!(have >> (8 * j) & 1) || tok + t >= sq.kv || (tags && tg[t] < 0)) ti[j][i] = -1000;
+                                const uint32_t state = have >> (8 * j) & 3u;
+                                if (!state || tok + t >= sq.kv || (state == 1 && tg[t] < 0)) ti[j][i] = -1000;
                             }
                             x = max(x, ti[j][i]);
                         }
@@ -875,8 +904,10 @@ akashic_status_t attend_check(const akashic_mem_kv_config_t *cfg, const akashic_
 // (query rows times group) one takes them all; else each takes the sequences on
 // its side of WIDE_FROM.
 constexpr int WIDE_FROM = 17;
+constexpr int DIRECT_STEPS = 32;   // of 32 tokens: four a warp
 struct AttendRoute {
     AttendShape narrow = {0, 0}, wide = {0, 0};   // ctas 0: not launched
+    bool direct = false;                          // a CTA an item, nothing to join
     int64_t joins = 0, bytes = 0;                 // scratch: of the joins, in all
     int64_t narrow_floats = 0;
 };
@@ -888,6 +919,10 @@ AttendRoute route_of(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_at
     if (a->q_start || most < WIDE_FROM)
         r.narrow = attend_narrow_shape(cfg->bits, cfg->head_dim, (int)(most < WIDE_FROM ? most : WIDE_FROM - 1), sms);
     if (most >= WIDE_FROM) r.wide = attend_wide_shape(cfg->head_dim, sms);
+    // Short lists and no more items than CTAs at once: planning and joining would take
+    // longer than the uneven shares (8 heads of 700 tokens: 17.5 us with them).
+    const int64_t steps = ceil_div(a->max_blocks * cfg->block_tokens, (int64_t)32);
+    r.direct = !a->q_start && most <= r.narrow.rows && (int64_t)a->n_seq * cfg->heads <= r.narrow.ctas && steps <= DIRECT_STEPS;
     r.joins = ceil_div((int64_t)(r.narrow.ctas + r.wide.ctas) * 16, (int64_t)256) * 256;
     r.narrow_floats = r.narrow.ctas * 2 * attend_slot_floats(r.narrow.rows, cfg->head_dim);
     r.bytes = r.joins + (r.narrow_floats + r.wide.ctas * 2 * attend_slot_floats(r.wide.rows, cfg->head_dim)) * 4;
@@ -949,8 +984,10 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e = cudaSuccess;
     if (r.narrow.ctas) {
-        e = launch_attend_narrow(p, cfg->bits, cfg->head_dim, a->dtype, r.narrow, 1, WIDE_FROM - 1, st);
-        if (e == cudaSuccess) e = launch_attend_join(p, a->dtype, cfg->head_dim, r.narrow.ctas, r.narrow.rows, st);
+        AttendShape shape = r.narrow;
+        if (r.direct) p.direct = 1, shape.ctas = a->n_seq * cfg->heads;
+        e = launch_attend_narrow(p, cfg->bits, cfg->head_dim, a->dtype, shape, 1, WIDE_FROM - 1, st);
+        if (e == cudaSuccess && !r.direct) e = launch_attend_join(p, a->dtype, cfg->head_dim, r.narrow.ctas, r.narrow.rows, st);
     }
     if (e == cudaSuccess && r.wide.ctas) {
         p.joins += r.narrow.ctas;

@@ -40,6 +40,7 @@ struct AttendParams {
     int per_block;                    // units of a block
     int max_kv;                       // tokens that the lists can hold
     int causal;
+    int direct;                       // few-row kernel: CTA b has item b, sequences of one tile
     bool q_wide, out_wide;            // query rows, out: 16-byte aligned
     float scale, cap;                 // cap 0: none
 };

@@ -749,14 +749,15 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
     }
 }
 
-// Items whose steps lay in several CTAs: the slots in the order of the CTAs, one CTA
-// an item.  The slots' factors first, then the sums, eight slots in flight.
-constexpr int JOIN_FACTORS = 8192;
+// Items whose steps lay in several CTAs: the slots in the order of the CTAs, a CTA 8 rows
+// of an item (256 rows in one CTA took 80 us).  The slots' factors first, then the
+// sums, eight slots in flight.
+constexpr int JOIN_ROWS = 8, JOIN_CTAS = 1024;     // of the kernel before, at most
 template <int D>
 __global__ void __launch_bounds__(256)
 k_attend_join(const AttendParams p, const int rows, const bool bf16) {
-    __shared__ float factor[JOIN_FACTORS];     // [rows of a pass][slot]
-    __shared__ float inv[128];
+    __shared__ float factor[JOIN_ROWS * JOIN_CTAS];
+    __shared__ float inv[JOIN_ROWS];
     griddep_wait();
     const int4 j = p.joins[blockIdx.x];
     if (j.x < 0) return;
@@ -767,44 +768,42 @@ k_attend_join(const AttendParams p, const int rows, const bool bf16) {
     const int64_t floats = attend_slot_floats(rows, D);
     const float *base = p.partial + (int64_t)blockIdx.x * 2 * floats;
     auto slot = [&](int k) { return base + (k ? (int64_t)k * 2 : 1) * floats; };
-    const int pass = max(1, min(128, JOIN_FACTORS / parts));     // parts <= the grid's CTAs
-    for (int r0 = 0; r0 < real; r0 += pass) {
-        const int r1 = min(real, r0 + pass);
-        for (int r = r0 + warp; r < r1; r += 8) {
-            float mx = NEG, tot = 0.f;
-            for (int k = lane; k < parts; k += 32) mx = fmaxf(mx, slot(k)[rows * D + r]);
+    const int r0 = blockIdx.y * JOIN_ROWS, n = min(JOIN_ROWS, real - r0);
+    if (n <= 0) return;
+    if (warp < n) {
+        const int r = r0 + warp;
+        float mx = NEG, tot = 0.f;
+        for (int k = lane; k < parts; k += 32) mx = fmaxf(mx, slot(k)[rows * D + r]);
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            for (int k = lane; k < parts; k += 32) {
-                const float f = ex2(slot(k)[rows * D + r] - mx);
-                factor[(r - r0) * parts + k] = f;
-                tot += f * slot(k)[rows * D + rows + r];
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, o);
-            if (lane == 0) {
-                inv[r - r0] = tot > 0.f ? 1.f / tot : tot;
-                const int row = j.z * rows + r, i = row / p.group;
-                if (p.lse)
-                    p.lse[(int64_t)(sq.row0 + i) * p.q_heads + j.y * p.group + (row - i * p.group)] = lse_of(mx, tot);
-            }
+        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        for (int k = lane; k < parts; k += 32) {
+            const float f = ex2(slot(k)[rows * D + r] - mx);
+            factor[warp * parts + k] = f;
+            tot += f * slot(k)[rows * D + rows + r];
         }
-        __syncthreads();
-        for (int x = tid; x < (r1 - r0) * (D / 4); x += 256) {
-            const int r = x / (D / 4), d = x % (D / 4) * 4;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, o);
+        if (lane == 0) {
+            inv[warp] = tot > 0.f ? 1.f / tot : tot;
+            const int row = j.z * rows + r, i = row / p.group;
+            if (p.lse)
+                p.lse[(int64_t)(sq.row0 + i) * p.q_heads + j.y * p.group + (row - i * p.group)] = lse_of(mx, tot);
+        }
+    }
+    __syncthreads();
+    for (int x = tid; x < n * (D / 4); x += 256) {
+        const int r = x / (D / 4), d = x % (D / 4) * 4;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
-            for (int k = 0; k < parts; ++k) {
-                const float f = factor[r * parts + k];
-                const float4 y = *(const float4 *)(slot(k) + (r0 + r) * D + d);
-                v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
-            }
-            const int row = j.z * rows + r0 + r, i = row / p.group;
-            const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + j.y * p.group + (row - i * p.group);
-            store_pair(p, bf16, dst * D + d, v.x * inv[r], v.y * inv[r]);
-            store_pair(p, bf16, dst * D + d + 2, v.z * inv[r], v.w * inv[r]);
+        for (int k = 0; k < parts; ++k) {
+            const float f = factor[r * parts + k];
+            const float4 y = *(const float4 *)(slot(k) + (r0 + r) * D + d);
+            v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
         }
-        __syncthreads();
+        const int row = j.z * rows + r0 + r, i = row / p.group;
+        const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + j.y * p.group + (row - i * p.group);
+        store_pair(p, bf16, dst * D + d, v.x * inv[r], v.y * inv[r]);
+        store_pair(p, bf16, dst * D + d + 2, v.z * inv[r], v.w * inv[r]);
     }
 }
 
@@ -866,7 +865,8 @@ cudaError_t launch_attend_join(const AttendParams &p, int dtype, int dim, int ct
                                cudaStream_t st) {
     const bool bf16 = dtype == AKASHIC_DTYPE_BF16;
     auto *kernel = dim == 64 ? k_attend_join<64> : dim == 128 ? k_attend_join<128> : k_attend_join<256>;
-    return launch_pdl(kernel, dim3(ctas), dim3(256), 0, st, p, rows, bf16);
+    if (ctas > JOIN_CTAS) return cudaErrorInvalidValue;        // (a GPU of more than 512 SMs)
+    return launch_pdl(kernel, dim3(ctas, (rows + JOIN_ROWS - 1) / JOIN_ROWS), dim3(256), 0, st, p, rows, bf16);
 }
 
 }  // namespace ak
@@ -902,8 +902,10 @@ akashic_status_t attend_check(const akashic_mem_kv_config_t *cfg, const akashic_
 
 // Which kernels a call launches.  Where all sequences have the same number of rows
 // (query rows times group) one takes them all; else each takes the sequences on
-// its side of WIDE_FROM.
-constexpr int WIDE_FROM = 17;
+// its side of wide_from() rows.
+// Sequences of 5000 tokens, 16 of them, 2 key/value heads, distance bias: 126 rows 96 us here and 117
+// there at D = 128 (173 and 162 at D = 256), 252 rows 152 and 174 (305 and 172).
+int wide_from(int dim) { return dim == 256 ? 97 : 257; }
 constexpr int DIRECT_STEPS = 32;   // of 32 tokens: four a warp
 struct AttendRoute {
     AttendShape narrow = {0, 0}, wide = {0, 0};   // ctas 0: not launched
@@ -915,10 +917,10 @@ AttendRoute route_of(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_at
     AttendRoute r;
     const int64_t rows = (int64_t)a->n_q * (a->q_heads / cfg->heads);
     const int64_t most = a->q_start || a->n_seq == 0 ? rows : rows / a->n_seq;
-    const int sms = device_sm_count();
-    if (a->q_start || most < WIDE_FROM)
-        r.narrow = attend_narrow_shape(cfg->bits, cfg->head_dim, (int)(most < WIDE_FROM ? most : WIDE_FROM - 1), sms);
-    if (most >= WIDE_FROM) r.wide = attend_wide_shape(cfg->head_dim, sms);
+    const int sms = device_sm_count(), from = wide_from(cfg->head_dim);
+    if (a->q_start || most < from)
+        r.narrow = attend_narrow_shape(cfg->bits, cfg->head_dim, (int)(most < from ? most : from - 1), sms);
+    if (most >= from) r.wide = attend_wide_shape(cfg->head_dim, sms);
     // Short lists and no more items than CTAs at once: planning and joining would take
     // longer than the uneven shares (8 heads of 700 tokens: 17.5 us with them).
     const int64_t steps = ceil_div(a->max_blocks * cfg->block_tokens, (int64_t)32);
@@ -986,13 +988,13 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
     if (r.narrow.ctas) {
         AttendShape shape = r.narrow;
         if (r.direct) p.direct = 1, shape.ctas = a->n_seq * cfg->heads;
-        e = launch_attend_narrow(p, cfg->bits, cfg->head_dim, a->dtype, shape, 1, WIDE_FROM - 1, st);
+        e = launch_attend_narrow(p, cfg->bits, cfg->head_dim, a->dtype, shape, 1, wide_from(cfg->head_dim) - 1, st);
         if (e == cudaSuccess && !r.direct) e = launch_attend_join(p, a->dtype, cfg->head_dim, r.narrow.ctas, r.narrow.rows, st);
     }
     if (e == cudaSuccess && r.wide.ctas) {
         p.joins += r.narrow.ctas;
         p.partial += r.narrow_floats;
-        e = launch_attend_wide(p, cfg->bits, cfg->head_dim, a->dtype, r.wide, WIDE_FROM, 0x7fffffff, st);
+        e = launch_attend_wide(p, cfg->bits, cfg->head_dim, a->dtype, r.wide, wide_from(cfg->head_dim), 0x7fffffff, st);
         if (e == cudaSuccess) e = launch_attend_join(p, a->dtype, cfg->head_dim, r.wide.ctas, r.wide.rows, st);
     }
     if (e != cudaSuccess)

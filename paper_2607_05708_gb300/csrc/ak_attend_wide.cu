@@ -897,6 +897,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
 #pragma unroll
                     for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * inv * up0 * up1);
                     if (!whole) {
+                        if (real)
 #pragma unroll
                         for (int k = 0; k < 32; k += 4)
                             *(uint4 *)(part + r * D + d + k) = make_uint4(y[k], y[k + 1], y[k + 2], y[k + 3]);

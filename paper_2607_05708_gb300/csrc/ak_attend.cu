@@ -911,7 +911,7 @@ struct AttendRoute {
     AttendShape narrow = {0, 0}, wide = {0, 0};   // ctas 0: not launched
     bool direct = false;                          // a CTA an item, nothing to join
     int64_t joins = 0, bytes = 0;                 // scratch: of the joins, in all
-    int64_t narrow_floats = 0;
+    int64_t narrow_floats = 0, ranges = 0;        // floats of the narrow slots, bytes of the ranges
 };
 AttendRoute route_of(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_attend_t *a) {
     AttendRoute r;
@@ -927,7 +927,9 @@ AttendRoute route_of(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_at
     r.direct = !a->q_start && most <= r.narrow.rows && (int64_t)a->n_seq * cfg->heads <= r.narrow.ctas && steps <= DIRECT_STEPS;
     r.joins = ceil_div((int64_t)(r.narrow.ctas + r.wide.ctas) * 16, (int64_t)256) * 256;
     r.narrow_floats = r.narrow.ctas * 2 * attend_slot_floats(r.narrow.rows, cfg->head_dim);
-    r.bytes = r.joins + (r.narrow_floats + r.wide.ctas * 2 * attend_slot_floats(r.wide.rows, cfg->head_dim)) * 4;
+    if (r.wide.ctas && a->tags)
+        r.ranges = ceil_div(attend_ranges(a->n_q, a->q_heads / cfg->heads, a->n_seq, r.wide.rows) * 8, (int64_t)256) * 256;
+    r.bytes = r.joins + r.ranges + (r.narrow_floats + r.wide.ctas * 2 * attend_slot_floats(r.wide.rows, cfg->head_dim)) * 4;
     return r;
 }
 
@@ -972,7 +974,7 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
     p.blocks = a->blocks, p.slopes = a->slopes, p.tags = a->tags, p.q_tags = a->q_tags;
     p.status = status;
     p.joins = (int4 *)scratch;
-    p.partial = (float *)((unsigned char *)scratch + r.joins);
+    p.partial = (float *)((unsigned char *)scratch + r.joins + r.ranges);
     p.n_blocks = cfg->n_blocks, p.max_blocks = a->max_blocks;
     p.n_q = a->n_q, p.n_seq = a->n_seq, p.q_heads = a->q_heads, p.heads = cfg->heads;
     p.group = a->q_heads / cfg->heads;
@@ -994,7 +996,14 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
     if (e == cudaSuccess && r.wide.ctas) {
         p.joins += r.narrow.ctas;
         p.partial += r.narrow_floats;
-        e = launch_attend_wide(p, cfg->bits, cfg->head_dim, a->dtype, r.wide, wide_from(cfg->head_dim), 0x7fffffff, st);
+        p.direct = 0;
+        const int from = wide_from(cfg->head_dim);
+        if (r.ranges) {
+            p.ranges = (const int2 *)((unsigned char *)scratch + r.joins);
+            e = launch_attend_ranges(p, cfg->head_dim, r.wide, from, 0x7fffffff, st);
+        }
+        if (e == cudaSuccess)
+            e = launch_attend_wide(p, cfg->bits, cfg->head_dim, a->dtype, r.wide, from, 0x7fffffff, st);
         if (e == cudaSuccess) e = launch_attend_join(p, a->dtype, cfg->head_dim, r.wide.ctas, r.wide.rows, st);
     }
     if (e != cudaSuccess)

@@ -33,6 +33,8 @@ struct AttendParams {
     const int32_t *tags;              // one a slot, or NULL
     const int32_t *q_tags;            // [n_q] or NULL
     int *status;
+    const int2 *ranges;               // many-row kernel with tags: each row tile's first and last
+                                      // step (attend_range_at), or NULL
     float *partial;                   // unfinished items' results (PartialSlot)
     int4 *joins;                      // what the joining kernel has to join
     int64_t n_blocks, max_blocks;
@@ -47,7 +49,7 @@ struct AttendParams {
 
 // A sequence: its query rows and context.
 struct AttendSeq {
-    int row0, nq, kv, prefix;
+    int row0, nq, kv, prefix, seq;
 };
 __device__ __forceinline__ AttendSeq attend_seq(const AttendParams &p, int s) {
     AttendSeq q;
@@ -67,6 +69,7 @@ __device__ __forceinline__ AttendSeq attend_seq(const AttendParams &p, int s) {
         q.kv = max(0, min(n, p.max_kv));
     }
     q.prefix = p.prefix ? max(0, min(p.prefix[s], q.kv)) : 0;
+    q.seq = s;
     return q;
 }
 // Keys [0, limit) may be seen by the row at place i of the sequence.
@@ -82,8 +85,19 @@ __device__ __forceinline__ int attend_limit(const AttendParams &p, const AttendS
 __device__ __forceinline__ int attend_tiles(const AttendParams &p, const AttendSeq &q, int rows) {
     return (int)(((uint32_t)q.nq * (uint32_t)p.group + (uint32_t)rows - 1u) / (uint32_t)rows);
 }
+// Where a row tile's range stands: the sequences' tiles one after the other.
+__host__ __device__ __forceinline__ int64_t attend_ranges(int64_t n_q, int group, int n_seq, int rows) {
+    return n_q * group / rows + n_seq + 1;
+}
+__device__ __forceinline__ int attend_range_at(const AttendParams &p, const AttendSeq &q, int tile, int rows) {
+    return (int)((uint32_t)q.row0 * (uint32_t)p.group / (uint32_t)rows) + q.seq + tile;
+}
 __device__ __forceinline__ int attend_units(const AttendParams &p, const AttendSeq &q, int tile,
                                             int rows, int step) {
+    if (p.ranges) {
+        const int2 r = p.ranges[attend_range_at(p, q, tile, rows)];
+        return max(1, r.y - r.x);
+    }
     const uint32_t all = (uint32_t)q.nq * (uint32_t)p.group;
     const uint32_t last = min((uint32_t)(tile + 1) * (uint32_t)rows, all) - 1u;
     const int end = attend_limit(p, q, (int)(last / (uint32_t)p.group));
@@ -107,7 +121,8 @@ __device__ __forceinline__ int64_t attend_seq_units(const AttendParams &p, const
     for (unsigned many = __ballot_sync(0xffffffffu, tiles > FEW); many; many &= many - 1) {
         const int l = __ffs(many) - 1;
         const AttendSeq x = {__shfl_sync(0xffffffffu, q.row0, l), __shfl_sync(0xffffffffu, q.nq, l),
-                             __shfl_sync(0xffffffffu, q.kv, l), __shfl_sync(0xffffffffu, q.prefix, l)};
+                             __shfl_sync(0xffffffffu, q.kv, l), __shfl_sync(0xffffffffu, q.prefix, l),
+                             __shfl_sync(0xffffffffu, q.seq, l)};
         const int n = __shfl_sync(0xffffffffu, tiles, l);
         int64_t v = 0;
         for (int t = lane; t < n; t += 32) v += attend_units(p, x, t, rows, step);
@@ -313,6 +328,9 @@ AttendShape attend_narrow_shape(int bits, int dim, int max_rows, int sms);
 cudaError_t launch_attend_narrow(const AttendParams &p, int bits, int dim, int dtype,
                                  const AttendShape &shape, int lo, int hi, cudaStream_t st);
 AttendShape attend_wide_shape(int dim, int sms);
+// Fills p.ranges (attend_ranges() entries) for the sequences that the kernel will take.
+cudaError_t launch_attend_ranges(const AttendParams &p, int dim, const AttendShape &shape, int lo, int hi,
+                                 cudaStream_t st);
 cudaError_t launch_attend_wide(const AttendParams &p, int bits, int dim, int dtype,
                                const AttendShape &shape, int lo, int hi, cudaStream_t st);
 

@@ -359,13 +359,15 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
         uint32_t n_tile = 0;                   // tiles since the kernel began
         while (left > 0 && !*dead) {
             const int n = min(cur.units - cur.unit, left), units = (cur.q.kv + KV_UNIT - 1) / KV_UNIT;
+            // the tile of the item's first step that is this CTA's
+            const int first_tile = cur.unit + (p.ranges ? p.ranges[attend_range_at(p, cur.q, cur.tile, ROWS)].x : 0);
             const int64_t *list = p.blocks + cur.seq * p.max_blocks;
             constexpr int PER = 32 / C::UPW;   // tiles of a look-up
             int64_t my_unit = -1, my_slots = 0;
             auto look_up = [&](int i) {        // lane: tile i + lane / UPW, this warp's unit lane % UPW
                 my_unit = -1;
                 const int tile = i + lane / C::UPW;
-                const int u = (cur.unit + tile) * C::UNITS + w * C::UPW + lane % C::UPW;
+                const int u = (first_tile + tile) * C::UNITS + w * C::UPW + lane % C::UPW;
                 if (tile < n && u < units) {
                     const int b = u / p.per_block, x = u - b * p.per_block;
                     const int64_t id = list[b];
@@ -399,7 +401,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
             }
             int rv = -127;
             for (int i = 0; i < n; ++i, ++n_tile) {
-                const int st = n_tile % ST, tok = (cur.unit + i) * N;
+                const int st = n_tile % ST, tok = (first_tile + i) * N;
                 if (!wide_wait(&empty[st], ((n_tile / ST) & 1) ^ 1, dead, p.status)) break;
                 Meta<N> &m = meta[st];
                 bool have[C::UPW];
@@ -932,6 +934,52 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
     if (warp == 0) tmem_dealloc(tmem, C::TMEM_COLS);
 }
 
+// With tags: the steps between the first and the last that hold a tag which some row of a
+// tile has (documents packed one after the other: a document's rows look at its own
+// part only).  A CTA a sequence: the range of tags of every step, then of every row tile,
+// and the steps that overlap it.  Past RANGE_STEPS steps nothing is left out.
+constexpr int RANGE_STEPS = 4096;
+__global__ void __launch_bounds__(1024)
+k_attend_ranges(const __grid_constant__ AttendParams p, int2 *ranges, const int rows, const int step, const int lo,
+                const int hi) {
+    __shared__ int2 have[RANGE_STEPS];         // the least and the greatest tag of a step
+    const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
+    const AttendSeq q = attend_seq(p, s);
+    if (!attend_takes(p, q, lo, hi)) return;
+    const int steps = (q.kv + step - 1) / step, T = p.per_block * KV_UNIT;
+    const bool small = steps <= RANGE_STEPS;
+    for (int x = tid >> 5; small && x < steps; x += 32) {
+        int2 r = make_int2(0x7fffffff, -1);
+        for (int j = x * step + lane; j < min(q.kv, (x + 1) * step); j += 32) {
+            const int64_t id = p.blocks[s * p.max_blocks + j / T];
+            const int t = id >= 0 && id < p.n_blocks ? p.tags[id * T + j % T] : -1;
+            if (t >= 0) r = make_int2(min(r.x, t), max(r.y, t));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            r = make_int2(min(r.x, __shfl_xor_sync(0xffffffffu, r.x, o)), max(r.y, __shfl_xor_sync(0xffffffffu, r.y, o)));
+        if (lane == 0) have[x] = r;
+    }
+    __syncthreads();
+    const int tiles = attend_tiles(p, q, rows);
+    for (int t = tid; t < tiles; t += 1024) {
+        const uint32_t all = (uint32_t)q.nq * p.group, end = min((uint32_t)(t + 1) * rows, all) - 1u;
+        const int i0 = (int)((uint32_t)t * rows / p.group), i1 = (int)(end / p.group);
+        const int limit = (attend_limit(p, q, i1) + step - 1) / step;
+        int2 want = make_int2(0x7fffffff, -1), r = make_int2(0, limit);
+        for (int i = i0; i <= i1; ++i) {
+            const int y = p.q_tags[q.row0 + i];
+            if (y >= 0) want = make_int2(min(want.x, y), max(want.y, y));
+        }
+        if (small) {
+            auto seen = [&](int x) { return have[x].x <= want.y && have[x].y >= want.x; };
+            while (r.x < r.y && !seen(r.x)) ++r.x;
+            while (r.x < r.y && !seen(r.y - 1)) --r.y;
+        }
+        ranges[attend_range_at(p, q, t, rows)] = r;
+    }
+}
+
 template <int BITS, int D>
 cudaError_t run_wide(const AttendParams &p, int dtype, int ctas, int lo, int hi, cudaStream_t st) {
     using C = Wide<D>;
@@ -954,6 +1002,12 @@ cudaError_t run_wide(const AttendParams &p, int dtype, int ctas, int lo, int hi,
 
 AttendShape attend_wide_shape(int dim, int sms) {
     return {dim == 256 ? Wide<256>::ROWS : Wide<128>::ROWS, sms};
+}
+cudaError_t launch_attend_ranges(const AttendParams &p, int dim, const AttendShape &shape, int lo, int hi,
+                                 cudaStream_t st) {
+    k_attend_ranges<<<p.n_seq, 1024, 0, st>>>(p, (int2 *)p.ranges, shape.rows, dim == 256 ? Wide<256>::N : Wide<128>::N,
+                                              lo, hi);
+    return cudaGetLastError();
 }
 cudaError_t launch_attend_wide(const AttendParams &p, int bits, int dim, int dtype,
                                const AttendShape &s, int lo, int hi, cudaStream_t st) {

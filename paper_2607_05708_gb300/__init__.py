@@ -403,6 +403,8 @@ class KVCache:
         self.tags = (torch.full((n_blocks * block_tokens,), -1, dtype=torch.int32, device=dev)
                      if tagged else None)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        # the first call may be on another stream than the one that filled these
+        torch.cuda.current_stream(dev).synchronize()
         self._dtypes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
         self._scratch = {}
         # what every call needs, looked up once
@@ -516,7 +518,7 @@ class KVCache:
         slopes (float32 [q_heads]) and q_tags (int32 [n_q], tagged caches only) as in
         akashic_mem_kv_attend.  Returns (out [n_q, q_heads, head_dim] of q's type,
         lse float32 [n_q, q_heads]); rows behind the last sequence are left as they
-        were (zero, -inf-free, in tensors allocated here)."""
+        were (zero in tensors allocated here)."""
         torch = self._torch
         dt, (n_q, q_heads, _), sq = self._rows(q, "q")
         if dt == 2:

@@ -961,6 +961,9 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
         return kv_fail(AKASHIC_EINVAL, "kv_attend: cache, tags and scratch must be 16-byte aligned");
     if ((uintptr_t)a->out & 3u || (uintptr_t)a->q & 1u)
         return kv_fail(AKASHIC_EINVAL, "kv_attend: out must be 4-byte aligned, q to its element");
+    if ((uintptr_t)a->blocks & 7u || ((uintptr_t)a->q_start | (uintptr_t)a->kv_len | (uintptr_t)a->prefix_len |
+                                      (uintptr_t)a->slopes | (uintptr_t)a->q_tags | (uintptr_t)a->lse) & 3u)
+        return kv_fail(AKASHIC_EINVAL, "kv_attend: arrays must be aligned to their element");
     KvDevice dev(cfg->device);
     if (!dev.ok) return kv_fail(AKASHIC_ECUDA, "kv_attend: device %d cannot be made current", cfg->device);
     const AttendRoute r = route_of(cfg, a);

@@ -397,6 +397,8 @@ extern "C" akashic_status_t akashic_mem_kv_write(
     if ((uintptr_t)cache & 15u) return kv_fail(AKASHIC_EINVAL, "kv_write: cache must be 16-byte aligned");
     if (((uintptr_t)k | (uintptr_t)v) & (uintptr_t)(size - 1))
         return kv_fail(AKASHIC_EINVAL, "kv_write: k and v must be aligned to their element");
+    if ((uintptr_t)slots & 7u || ((uintptr_t)tags | (uintptr_t)new_tags) & 3u)
+        return kv_fail(AKASHIC_EINVAL, "kv_write: slots and tags must be aligned to their element");
     if (new_tags && !tags) return kv_fail(AKASHIC_EINVAL, "kv_write: new_tags needs the cache's tags");
     KvRows r = {};
     r.cfg = cfg;
@@ -424,6 +426,7 @@ extern "C" akashic_status_t akashic_mem_kv_read(const akashic_mem_kv_config_t *c
     if ((uintptr_t)cache & 15u) return kv_fail(AKASHIC_EINVAL, "kv_read: cache must be 16-byte aligned");
     if (((uintptr_t)k | (uintptr_t)v) & (uintptr_t)(size - 1))
         return kv_fail(AKASHIC_EINVAL, "kv_read: k and v must be aligned to their element");
+    if ((uintptr_t)slots & 7u) return kv_fail(AKASHIC_EINVAL, "kv_read: slots must be aligned to their element");
     KvRows r = {};
     r.cfg = cfg;
     r.cache = (unsigned char *)cache;

@@ -477,7 +477,7 @@ akashic_status_t akashic_mem_kv_attend_scratch(const akashic_mem_kv_config_t *cf
 
 /* scratch: device, 16-byte aligned, not initialised.  EINVAL for a bad config or
  * argument (as noted above), n_q x q_heads beyond 2^31 - 1, a scale or cap that is
- * not finite, a negative cap, tags without q_tags, or scratch that is too small;
+ * not finite, a cap below 0 or subnormal, tags without q_tags, or scratch that is too small;
  * ECUDA if a launch fails. */
 akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t *cfg, const void *cache,
                                        const akashic_mem_kv_attend_t *a, void *scratch,

@@ -537,13 +537,14 @@ class KVCache:
             vec(slopes, f32, "slopes", q_heads), None if q_tags is None else self._tags_ptr,
             vec(q_tags, i32, "q_tags", n_q))
         ref = ctypes.byref(a)
+        behind = q_start is not None or n_seq == 0         # rows that no sequence has
         if out is None:
-            out = self._empty(q.shape, q.dtype, stream, zero=q_start is not None)
+            out = self._empty(q.shape, q.dtype, stream, zero=behind)
             a.out = out.data_ptr()
         else:
             a.out = vec(out, q.dtype, "out", n_q * q_heads * self.head_dim)
         if lse is None:
-            lse = self._empty((n_q, q_heads), f32, stream, zero=q_start is not None)
+            lse = self._empty((n_q, q_heads), f32, stream, zero=behind)
             a.lse = lse.data_ptr()
         else:
             a.lse = vec(lse, f32, "lse", n_q * q_heads)
@@ -570,5 +571,6 @@ class KVCache:
         code = int(self.status.item())
         if code:
             self.status.zero_()
+            self._torch.cuda.current_stream(self.device).synchronize()   # before any other stream's calls
             raise AkashicError(code, "kv: an index or length was out of bounds" if code == 6
                                else "kv: a kernel of the cache failed")

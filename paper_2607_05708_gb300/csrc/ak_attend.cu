@@ -86,7 +86,7 @@ struct Fetch {
 // A warp's part of an item, left for the joining of the CTA's warps.
 struct Entry {
     int64_t start;                             // of the item, in all steps
-    int seq, head, tile, unit, n, units, tref, pad;
+    int seq, head, tile, unit, n, units, tref;
 };
 static_assert(sizeof(Entry) <= 48 && sizeof(Fetch) <= 64, "Narrow::SMALL");
 
@@ -267,7 +267,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
 
     bool ok = true;                            // no wait of this warp has expired
     uint32_t stage = 0, phase = 0;
-    const float cap_l = p.cap * LOG2E_F, cap_in = p.cap > 0.f ? 2.f / p.cap : 0.f;
+    const float cap_l = p.cap * LOG2E_F;
     float o[NB][MT][4], mm[NB][2], l[NB][2];
     int tref = -127;
     int64_t done = 0;
@@ -415,12 +415,16 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
 #pragma unroll
                     for (int b = 0; b < NB; ++b) {
                         if (heavy) {
+                            uint32_t x[4];
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                x[r] = __float_as_uint(s[j][b][r] * ((r < 2 ? kf0[j] : kf1[j]) * qk[b][r & 1]));
+                            if (p.cap > 0.f) cap_scores<4>(x, cap_l);
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 const int col = b * 8 + 2 * c + (r & 1);
                                 float &z = s[j][b][r];
-                                z *= (r < 2 ? kf0[j] : kf1[j]) * qk[b][r & 1];
-                                if (p.cap > 0.f) z = cap_l * (1.f - __fdividef(2.f, 1.f + ex2(z * cap_in)));
+                                z = __uint_as_float(x[r]);
                                 if (p.slopes)
                                     z -= slope[col] * (float)abs(pos[col] - (tok + j * 16 + g + (r < 2 ? 0 : 8)));
                                 z -= mm[b][r & 1];
@@ -671,7 +675,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
             tail = done != 0;
             const int e = 2 * warp + (tail ? 1 : 0);
             if (lane == 0)
-                entries[e] = Entry{first + done - cur.unit, cur.seq, cur.head, cur.tile, cur.unit, n, cur.units, tref, 0};
+                entries[e] = Entry{first + done - cur.unit, cur.seq, cur.head, cur.tile, cur.unit, n, cur.units, tref};
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -893,8 +897,8 @@ akashic_status_t attend_check(const akashic_mem_kv_config_t *cfg, const akashic_
         return kv_fail(AKASHIC_EINVAL, "%s: without q_start, n_q must be a multiple of n_seq", who);
     if (!(a->scale == a->scale) || !(a->scale - a->scale == 0.f))
         return kv_fail(AKASHIC_EINVAL, "%s: scale must be finite", who);
-    if (!(a->cap >= 0.f) || !(a->cap - a->cap == 0.f))
-        return kv_fail(AKASHIC_EINVAL, "%s: cap must be finite and >= 0", who);
+    if (!(a->cap >= 0.f) || !(a->cap - a->cap == 0.f) || (a->cap > 0.f && a->cap < 1.17549435e-38f))
+        return kv_fail(AKASHIC_EINVAL, "%s: cap must be 0 or a normal positive number", who);
     if (!a->tags != !a->q_tags)
         return kv_fail(AKASHIC_EINVAL, "%s: tags and q_tags come together", who);
     return AKASHIC_OK;

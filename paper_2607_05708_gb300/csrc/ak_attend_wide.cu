@@ -69,32 +69,6 @@ static_assert(offsetof(Meta<64>, ksig) % 8 == 0 && offsetof(Meta<64>, vsig) % 8 
                   offsetof(Meta<128>, ksig) % 8 == 0 && offsetof(Meta<128>, vsig) % 8 == 0,
               "pairs");
 
-__device__ __forceinline__ uint64_t f2_pack(float a, float b) {
-    uint64_t d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
-    return d;
-}
-__device__ __forceinline__ float2 f2_open(uint64_t a) {
-    float2 d;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(a));
-    return d;
-}
-__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-
 // 32 registers to 32 consecutive columns of the thread's lane, and the wait.
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
     asm volatile(
@@ -255,38 +229,6 @@ __device__ __forceinline__ void store_row32(const AttendParams &p, bool bf16, in
     } else {
 #pragma unroll
         for (int k = 0; k < 16; ++k) dst[k] = h[k];
-    }
-}
-
-// cap tanh(x / cap) of a row's scores, in place (log2 units, like cap).  Where all of the
-// warp's are within 0.7 cap: x q(t), t = (x / cap)^2 <= 1/2, q the polynomial of degree 5
-// nearest to tanh(sqrt t) / sqrt t there in relative error (1.5e-8; fitted by
-// iteratively reweighted least squares), two scores an instruction.  Else
-// 1 - 2 / (1 + e^(2y)).
-template <int N>
-__device__ __forceinline__ void cap_scores(uint32_t (&x)[N], float cap) {
-    const float c = 1.f / cap, c2 = 2.f * LOG2E_F * c;
-    float most = 0.f;
-#pragma unroll
-    for (int k = 0; k < N; ++k) most = fmaxf(most, fabsf(__uint_as_float(x[k])));
-    if (__all_sync(0xffffffffu, most <= 0.7f * cap)) {
-        const float q[6] = {1.f, -0.3333311080932617f, 0.13328056037425995f, -0.053502924740314484f,
-                            0.019964739680290222f, -0.005034883972257376f};
-        const uint64_t cc = f2_pack(c, c);
-#pragma unroll
-        for (int k = 0; k < N; k += 2) {
-            const uint64_t z = f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1]));
-            const uint64_t y = f2_mul(z, cc), t = f2_mul(y, y);
-            uint64_t v = f2_pack(q[5], q[5]);
-#pragma unroll
-            for (int i = 4; i >= 0; --i) v = f2_fma(v, t, f2_pack(q[i], q[i]));
-            const float2 r = f2_open(f2_mul(v, z));
-            x[k] = __float_as_uint(r.x), x[k + 1] = __float_as_uint(r.y);
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-            x[k] = __float_as_uint(cap * (1.f - __fdividef(2.f, 1.f + ex2(__uint_as_float(x[k]) * c2))));
     }
 }
 
@@ -952,7 +894,9 @@ k_attend_ranges(const __grid_constant__ AttendParams p, int2 *ranges, const int 
         int2 r = make_int2(0x7fffffff, -1);
         for (int j = x * step + lane; j < min(q.kv, (x + 1) * step); j += 32) {
             const int64_t id = p.blocks[s * p.max_blocks + j / T];
-            const int t = id >= 0 && id < p.n_blocks ? p.tags[id * T + j % T] : -1;
+            const bool real = id >= 0 && id < p.n_blocks;
+            const int t = real ? p.tags[id * T + j % T] : -1;
+            if (!real && id != -1) set_status(p.status, AKASHIC_EDEVICE);   // its step may be left out
             if (t >= 0) r = make_int2(min(r.x, t), max(r.y, t));
         }
 #pragma unroll

@@ -102,6 +102,30 @@ def test_strided_queries():
             _compare(got, want, 128, "bf16", 4)
 
 
+@pytest.mark.parametrize("rows", [2, 300])
+def test_a_bad_block_among_tags(rows):
+    """Steps without a tag of the row's are left out; a bad block ID is reported all the same."""
+    c, q, blocks, args, want = _problem(17, kv=(700,), nq=(rows,), heads=1, group=1, docs=2, T=64)
+    c.sync()
+    n = args["kv_len"]
+    for at in (0, 4, 9):
+        b = blocks.clone()
+        b[0, at] = c.n_blocks
+        c.attend(q, b, **{**args, "causal": False, "kv_len": n})
+        assert _error(c) == "EDEVICE"
+
+
+@pytest.mark.parametrize("cap", [2e-38, 1e-3, 1e4, 1e8, 3e38])
+@pytest.mark.parametrize("rows", [3, 290])
+def test_caps_of_any_size(rows, cap):
+    """A cap far above the scores changes none of them; one far below makes them all
+    alike."""
+    c, q, blocks, args, want = _problem(19, kv=(400,), nq=(rows,), heads=1, group=1, cap=cap)
+    got = c.attend(q, blocks, **args)
+    c.sync()
+    _compare(got, want, 128, "bf16", 4)
+
+
 def test_the_same_bits_every_time():
     for kw in (dict(kv=(5000, 40, 900), heads=3), dict(kv=(900, 700), nq=(900, 400), heads=1)):
         c, q, blocks, args, _ = _problem(11, **kw)
@@ -217,6 +241,10 @@ def test_empty_calls():
     q = torch.zeros(0, 4, 64, dtype=torch.bfloat16, device="cuda")
     out, lse = c.attend(q, torch.zeros(0, 3, dtype=torch.int64, device="cuda"))
     assert out.shape == (0, 4, 64) and lse.shape == (0, 4)
+    torch.full((1 << 20,), 7.0, device="cuda")              # what the pool may hand out next
+    out, lse = c.attend(torch.ones(5, 4, 64, dtype=torch.bfloat16, device="cuda"),
+                        torch.zeros(0, 3, dtype=torch.int64, device="cuda"))
+    assert (out == 0).all() and (lse == 0).all()            # rows of no sequence
     q = torch.ones(3, 4, 64, dtype=torch.bfloat16, device="cuda")
     for width in (0, 2):            # nothing listed, nothing in the list
         b = torch.full((3, width), -1, dtype=torch.int64, device="cuda")

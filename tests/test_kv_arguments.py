@@ -77,7 +77,7 @@ def test_bad_rows(lib):
 ATTEND = [dict(dtype=2), dict(dtype=-1), dict(q_heads=0), dict(q_heads=3), dict(q_heads=4096),
           dict(n_seq=-1), dict(n_q=-1), dict(max_blocks=-1), dict(max_blocks=1 << 26),
           dict(n_q=3, n_seq=2), dict(n_q=1 << 28, q_heads=16), dict(scale=float("nan")),
-          dict(scale=float("inf")), dict(cap=-1.0), dict(cap=float("inf")), dict(cap=float("nan")),
+          dict(scale=float("inf")), dict(cap=-1.0), dict(cap=1e-39), dict(cap=float("inf")), dict(cap=float("nan")),
           dict(tags=16), dict(q_tags=16)]
 
 

@@ -548,7 +548,7 @@ class KVCache:
             a.lse = lse.data_ptr()
         else:
             a.lse = vec(lse, f32, "lse", n_q * q_heads)
-        key = (n_q, q_heads, n_seq, q_start is None, q_tags is None)
+        key = (n_q, q_heads, n_seq, width, q_start is None, q_tags is None)
         size = self._scratch.get(key)
         if size is None:
             need = ctypes.c_int64()

@@ -135,7 +135,7 @@ __device__ __forceinline__ float load_query(const AttendParams &p, bool bf16, in
 
 template <int BITS, int D, int NB>
 __global__ void __launch_bounds__(NW * 32, Narrow<BITS, D, NB>::TWO ? 2 : 1)
-k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const int lo, const int hi, const int min_per) {
+k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const int lo, const int hi) {
     using C = Narrow<BITS, D, NB>;
     using U = typename C::U;
     constexpr int ROWS = C::ROWS, NS = C::NS, MT = D / 16, UPS = C::UPS, STEP = C::STEP;
@@ -179,7 +179,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
     } else {
         attend_sums(p, ROWS, STEP, lo, hi, prefix);
         const int64_t total = prefix[NW * 32], workers = (int64_t)gridDim.x * NW;
-        per = max((int64_t)min_per, (total + workers - 1) / workers);
+        per = max((int64_t)1, (total + workers - 1) / workers);
         first = per * (blockIdx.x * NW + warp);
         left = (int)max((int64_t)0, min(per, total - first));      // steps of this warp
         if (left > 0) cur = attend_find(p, ROWS, STEP, lo, hi, prefix, first);
@@ -811,8 +811,6 @@ k_attend_join(const AttendParams p, const int rows, const bool bf16) {
     }
 }
 
-constexpr int MIN_PER = 1;    // steps of a warp's share, at least
-
 template <int BITS, int D, int NB>
 cudaError_t run_narrow(const AttendParams &p, int dtype, int ctas, int lo, int hi, cudaStream_t st) {
     using C = Narrow<BITS, D, NB>;
@@ -827,7 +825,7 @@ cudaError_t run_narrow(const AttendParams &p, int dtype, int ctas, int lo, int h
         if (e != cudaSuccess) return e;
         if (dev < 64) ready[dev].store(true, std::memory_order_release);
     }
-    kernel<<<ctas, NW * 32, C::SMEM, st>>>(p, dtype == AKASHIC_DTYPE_BF16, lo, hi, MIN_PER);
+    kernel<<<ctas, NW * 32, C::SMEM, st>>>(p, dtype == AKASHIC_DTYPE_BF16, lo, hi);
     return cudaGetLastError();
 }
 template <int BITS, int D>
@@ -907,11 +905,26 @@ akashic_status_t attend_check(const akashic_mem_kv_config_t *cfg, const akashic_
 // Which kernels a call launches.  Where all sequences have the same number of rows
 // (query rows times group) one takes them all; else each takes the sequences on
 // its side of wide_from() rows.
-// Sequences of 5000 tokens, 16 of them, 2 key/value heads, distance bias: 126 rows 96 us here and 117
-// there at D = 128 (173 and 162 at D = 256), 252 rows 152 and 174 (305 and 172).
-int wide_from(int dim) { return dim == 256 ? 97 : 257; }
-constexpr int DIRECT_STEPS = 32;   // of 32 tokens: four a warp
+// Microseconds of the kernel for few rows and of the one for many, 4 bits, 2 key/value heads:
+//   16 sequences of 5000 tokens, D = 128: 64 rows 51.7 and 47.8, 80 rows 67.2 and 48.6;
+//       D = 256: 32 rows 62.7 and 62.1, 40 rows 82.1 and 63.3
+//   1024 of 200 tokens, D = 128: 64 rows 212 and 247, 80 rows 289 and 249
+// Where so few items share the GPU that more than 16 CTAs leave parts of one to be
+// joined, and the work is little, the former stays ahead for longer:
+//   one sequence of 20000, D = 128: 128 rows 40.0 and 47.7, 256 rows 52.6 and 56.7;
+//       D = 256: 128 rows 63.5 and 72.8, 256 rows 101 and 70
+//   one of 200000, D = 128: 64 rows 93.3 and 90.8, 128 rows 157 and 94.6
+int wide_from(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_attend_t *a, int sms) {
+    const int64_t items = (int64_t)a->n_seq * cfg->heads;
+    const bool shared = items * 16 < sms && items * a->max_blocks * cfg->block_tokens < (1 << 17);
+    return cfg->head_dim == 256 ? (shared ? 129 : 33) : (shared ? 257 : 65);
+}
+// Short lists and no more items than CTAs at once: a CTA an item, as planning and joining would
+// take longer than the uneven shares (8 heads of 700 tokens 13.3 and 17.8 us, of 1400
+// 17.5 and 18.2, of 2000 20.0 and 18.7).
+constexpr int DIRECT_STEPS = 48;   // of 32 tokens: six a warp
 struct AttendRoute {
+    int from = 0;                                 // rows from which the kernel for many takes a sequence
     AttendShape narrow = {0, 0}, wide = {0, 0};   // ctas 0: not launched
     bool direct = false;                          // a CTA an item, nothing to join
     int64_t joins = 0, bytes = 0;                 // scratch: of the joins, in all
@@ -921,12 +934,10 @@ AttendRoute route_of(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_at
     AttendRoute r;
     const int64_t rows = (int64_t)a->n_q * (a->q_heads / cfg->heads);
     const int64_t most = a->q_start || a->n_seq == 0 ? rows : rows / a->n_seq;
-    const int sms = device_sm_count(), from = wide_from(cfg->head_dim);
+    const int sms = device_sm_count(), from = r.from = wide_from(cfg, a, sms);
     if (a->q_start || most < from)
         r.narrow = attend_narrow_shape(cfg->bits, cfg->head_dim, (int)(most < from ? most : from - 1), sms);
     if (most >= from) r.wide = attend_wide_shape(cfg->head_dim, sms);
-    // Short lists and no more items than CTAs at once: planning and joining would take
-    // longer than the uneven shares (8 heads of 700 tokens: 17.5 us with them).
     const int64_t steps = ceil_div(a->max_blocks * cfg->block_tokens, (int64_t)32);
     r.direct = !a->q_start && most <= r.narrow.rows && (int64_t)a->n_seq * cfg->heads <= r.narrow.ctas && steps <= DIRECT_STEPS;
     r.joins = ceil_div((int64_t)(r.narrow.ctas + r.wide.ctas) * 16, (int64_t)256) * 256;
@@ -997,20 +1008,19 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
     if (r.narrow.ctas) {
         AttendShape shape = r.narrow;
         if (r.direct) p.direct = 1, shape.ctas = a->n_seq * cfg->heads;
-        e = launch_attend_narrow(p, cfg->bits, cfg->head_dim, a->dtype, shape, 1, wide_from(cfg->head_dim) - 1, st);
+        e = launch_attend_narrow(p, cfg->bits, cfg->head_dim, a->dtype, shape, 1, r.from - 1, st);
         if (e == cudaSuccess && !r.direct) e = launch_attend_join(p, a->dtype, cfg->head_dim, r.narrow.ctas, r.narrow.rows, st);
     }
     if (e == cudaSuccess && r.wide.ctas) {
         p.joins += r.narrow.ctas;
         p.partial += r.narrow_floats;
         p.direct = 0;
-        const int from = wide_from(cfg->head_dim);
         if (r.ranges) {
             p.ranges = (const int2 *)((unsigned char *)scratch + r.joins);
-            e = launch_attend_ranges(p, cfg->head_dim, r.wide, from, 0x7fffffff, st);
+            e = launch_attend_ranges(p, cfg->head_dim, r.wide, r.from, 0x7fffffff, st);
         }
         if (e == cudaSuccess)
-            e = launch_attend_wide(p, cfg->bits, cfg->head_dim, a->dtype, r.wide, from, 0x7fffffff, st);
+            e = launch_attend_wide(p, cfg->bits, cfg->head_dim, a->dtype, r.wide, r.from, 0x7fffffff, st);
         if (e == cudaSuccess) e = launch_attend_join(p, a->dtype, cfg->head_dim, r.wide.ctas, r.wide.rows, st);
     }
     if (e != cudaSuccess)

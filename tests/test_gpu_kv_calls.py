@@ -88,6 +88,33 @@ def test_rows_behind_the_last_sequence_stay(rows):
     assert (out[n:] == 0).all()
 
 
+@pytest.mark.parametrize("bits,dim,dtype", [(4, 128, "bf16"), (8, 64, "fp16"), (4, 256, "fp16"), (8, 256, "bf16")])
+@pytest.mark.parametrize("extra", [{}, dict(docs=2), dict(cap=5.0, slopes=True, causal=False)], ids=["plain", "tags", "cap"])
+def test_rows_around_the_switch_of_kernels(bits, dim, dtype, extra):
+    """The last number of rows of the kernel for few and the first of the one for many, where
+    items are many (ten) and few, and all of them in one call."""
+    turns = (32, 129) if dim == 256 else (64, 257)
+    for i, rows in enumerate((turns[0], turns[0] + 1)):
+        kv = (200, 90, 131, 300, 17)
+        c, q, blocks, args, want = _problem(40 + i, kv=kv, nq=(rows,) * 5, heads=2, group=1, bits=bits,
+                                            dim=dim, dtype=dtype, T=32, **extra)
+        got = c.attend(q, blocks, **args)
+        c.sync()
+        _compare(got, want, dim, dtype, bits)
+    for i, rows in enumerate((turns[1] - 1, turns[1])):
+        c, q, blocks, args, want = _problem(50 + i, kv=(500,), nq=(rows,), heads=1, group=1, bits=bits,
+                                            dim=dim, dtype=dtype, T=32, **extra)
+        got = c.attend(q, blocks, **args)
+        c.sync()
+        _compare(got, want, dim, dtype, bits)
+    nq = (1, turns[0], turns[0] + 1, 0, 150, turns[1])
+    c, q, blocks, args, want = _problem(60, kv=(100, 200, 200, 20, 170, 260), nq=nq, heads=2, group=1,
+                                        bits=bits, dim=dim, dtype=dtype, T=32, tail=3, **extra)
+    got = c.attend(q, blocks, **args)
+    c.sync()
+    _compare(got, want, dim, dtype, bits, rows=sum(nq))
+
+
 def test_strided_queries():
     """Queries inside a wider projection, heads first, at odd offsets."""
     for rows in (3, 290):

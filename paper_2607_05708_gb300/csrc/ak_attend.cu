@@ -177,12 +177,12 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
         left = max(0, min((int)per, cur.units - cur.unit));
         __syncthreads();
     } else {
-        attend_sums(p, ROWS, STEP, lo, hi, prefix);
+        attend_sums(p, ROWS, STEP, 0, lo, hi, prefix);
         const int64_t total = prefix[NW * 32], workers = (int64_t)gridDim.x * NW;
         per = max((int64_t)1, (total + workers - 1) / workers);
         first = per * (blockIdx.x * NW + warp);
         left = (int)max((int64_t)0, min(per, total - first));      // steps of this warp
-        if (left > 0) cur = attend_find(p, ROWS, STEP, lo, hi, prefix, first);
+        if (left > 0) cur = attend_find(p, ROWS, STEP, 0, lo, hi, prefix, first);
         __syncthreads();
     }
 
@@ -199,7 +199,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
         AttendCursor x = ahead->cur;
         int i = ahead->i, n = ahead->n;        // steps of the item: done, this share's
         if (i == n) {
-            attend_next(p, ROWS, STEP, lo, hi, x);
+            attend_next(p, ROWS, STEP, 0, lo, hi, x);
             i = 0, n = min(x.units, fetch_left);
         }
         __syncwarp();
@@ -439,8 +439,9 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                             for (int r = 0; r < 4; ++r) {
                                 const int col = b * 8 + 2 * c + (r & 1), t = j * 16 + g + (r < 2 ? 0 : 8);
                                 const uint32_t state = have >> (8 * j) & 3u;
-                                const bool seen = state && tok + t < limit[col] &&
-                                                  (state == 3 || (tg[t] >= 0 && tg[t] == qtag[col]));
+                                const int tag = tg[t];         // (no branches: what is not there is not used)
+                                const bool seen = (state != 0) & (tok + t < limit[col]) &
+                                                  ((state == 3) | ((tag >= 0) & (tag == qtag[col])));
                                 if (!seen) s[j][b][r] = -INFINITY;
                             }
                         }
@@ -689,7 +690,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                 }
         }
         left -= n, done += n;
-        if (left > 0) attend_next(p, ROWS, STEP, lo, hi, cur);
+        if (left > 0) attend_next(p, ROWS, STEP, 0, lo, hi, cur);
     }
     if (tail) {
         // nothing is in flight any more: the ring takes the last item's part

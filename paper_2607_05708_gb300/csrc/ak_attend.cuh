@@ -108,16 +108,17 @@ __device__ __forceinline__ bool attend_takes(const AttendParams &p, const Attend
     const int n = q.nq * p.group;
     return n >= lo && n <= hi;
 }
-// The steps of one head of a sequence: every lane's own (s, 0 where it has none).
+// The steps of one head of a sequence, and `extra` more an item: every lane's own (s, 0
+// where it has none).
 // A whole warp calls it: sequences of many tiles are summed up by all lanes.
 __device__ __forceinline__ int64_t attend_seq_units(const AttendParams &p, const AttendSeq &q, bool have,
-                                                    int rows, int step, int lo, int hi) {
+                                                    int rows, int step, int extra, int lo, int hi) {
     constexpr int FEW = 4;
     const int lane = threadIdx.x & 31;
     const int tiles = have && attend_takes(p, q, lo, hi) ? attend_tiles(p, q, rows) : 0;
     int64_t u = 0;
     if (tiles <= FEW)
-        for (int t = 0; t < tiles; ++t) u += attend_units(p, q, t, rows, step);
+        for (int t = 0; t < tiles; ++t) u += extra + attend_units(p, q, t, rows, step);
     for (unsigned many = __ballot_sync(0xffffffffu, tiles > FEW); many; many &= many - 1) {
         const int l = __ffs(many) - 1;
         const AttendSeq x = {__shfl_sync(0xffffffffu, q.row0, l), __shfl_sync(0xffffffffu, q.nq, l),
@@ -125,7 +126,7 @@ __device__ __forceinline__ int64_t attend_seq_units(const AttendParams &p, const
                              __shfl_sync(0xffffffffu, q.seq, l)};
         const int n = __shfl_sync(0xffffffffu, tiles, l);
         int64_t v = 0;
-        for (int t = lane; t < n; t += 32) v += attend_units(p, x, t, rows, step);
+        for (int t = lane; t < n; t += 32) v += extra + attend_units(p, x, t, rows, step);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         if (lane == l) u = v;
@@ -136,24 +137,26 @@ __device__ __forceinline__ int64_t attend_seq_units(const AttendParams &p, const
 // Where a worker (a warp, or a CTA of the kernel for many rows) stands in the
 // order of all items.
 struct AttendCursor {
-    int seq, head, tile, unit;        // unit: first step of the item that is the worker's
+    int seq, head, tile, unit;        // unit: first step of the item that is the worker's, less
+                                      // than 0 within the extra steps
     int units;                        // of the item
     AttendSeq q;
 };
 
 // Every worker takes an equal share of the steps of all items, so that a batch
-// of very different lengths fills the GPU evenly.  All threads of the CTA sum
+// of very different lengths fills the GPU evenly.  An item's beginning and end count
+// as `extra` steps, before its others.  All threads of the CTA sum
 // up the sequences' steps (each a run of consecutive sequences); prefix[t], in
 // shared memory, is the sum of the runs before thread t's, prefix[blockDim.x] all.
-__device__ __forceinline__ void attend_sums(const AttendParams &p, int rows, int step, int lo,
-                                            int hi, int64_t *prefix) {
+__device__ __forceinline__ void attend_sums(const AttendParams &p, int rows, int step, int extra,
+                                            int lo, int hi, int64_t *prefix) {
     const int nt = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int run = (p.n_seq + nt - 1) / nt;
     int64_t sum = 0;
     for (int i = 0; i < run; ++i) {
         const int s = tid * run + i;
         const bool have = s < p.n_seq;
-        sum += attend_seq_units(p, attend_seq(p, have ? s : 0), have, rows, step, lo, hi) * p.heads;
+        sum += attend_seq_units(p, attend_seq(p, have ? s : 0), have, rows, step, extra, lo, hi) * p.heads;
     }
     int64_t incl = sum;
 #pragma unroll
@@ -171,7 +174,7 @@ __device__ __forceinline__ void attend_sums(const AttendParams &p, int rows, int
     __syncthreads();
 }
 // The item in which step `first` (below the total) lies.  A whole warp calls it.
-__device__ __forceinline__ AttendCursor attend_find(const AttendParams &p, int rows, int step,
+__device__ __forceinline__ AttendCursor attend_find(const AttendParams &p, int rows, int step, int extra,
                                                     int lo, int hi, const int64_t *prefix,
                                                     int64_t first) {
     const int nt = blockDim.x, lane = threadIdx.x & 31;
@@ -187,7 +190,7 @@ __device__ __forceinline__ AttendCursor attend_find(const AttendParams &p, int r
     for (int s0 = t * run;; s0 += 32) {
         const int s = s0 + lane;
         const bool have = s < p.n_seq;
-        const int64_t w = attend_seq_units(p, attend_seq(p, have ? s : 0), have, rows, step, lo, hi) * p.heads;
+        const int64_t w = attend_seq_units(p, attend_seq(p, have ? s : 0), have, rows, step, extra, lo, hi) * p.heads;
         int64_t incl = w;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -211,7 +214,7 @@ __device__ __forceinline__ AttendCursor attend_find(const AttendParams &p, int r
     // the tile, 32 at a time
     for (const int tiles = attend_tiles(p, c.q, rows); c.tile < tiles; c.tile += 32) {
         const int t = c.tile + lane;
-        const int w = t < tiles ? attend_units(p, c.q, t, rows, step) : 0;
+        const int w = t < tiles ? extra + attend_units(p, c.q, t, rows, step) : 0;
         int64_t incl = w;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -224,17 +227,18 @@ __device__ __forceinline__ AttendCursor attend_find(const AttendParams &p, int r
             c.tile += l;
             c.units = __shfl_sync(0xffffffffu, w, l);
             rest -= __shfl_sync(0xffffffffu, incl, l) - c.units;
+            c.units -= extra;
             break;
         }
         rest -= __shfl_sync(0xffffffffu, incl, 31);
     }
-    c.unit = (int)rest;
+    c.unit = (int)rest - extra;
     return c;
 }
 // The next item (the caller knows that there is one).
-__device__ __forceinline__ void attend_next(const AttendParams &p, int rows, int step, int lo,
-                                            int hi, AttendCursor &c) {
-    c.unit = 0;
+__device__ __forceinline__ void attend_next(const AttendParams &p, int rows, int step, int extra,
+                                            int lo, int hi, AttendCursor &c) {
+    c.unit = -extra;
     if (++c.tile >= attend_tiles(p, c.q, rows)) {
         c.tile = 0;
         if (++c.head >= p.heads) {
@@ -245,6 +249,16 @@ __device__ __forceinline__ void attend_next(const AttendParams &p, int rows, int
         }
     }
     c.units = attend_units(p, c.q, c.tile, rows, step);
+}
+
+// What a share of `left` steps, extra ones counted, has of the cursor's item: n steps from
+// `from`; n <= 0 where it ends within the extra ones.
+struct AttendPart {
+    int from, n, used;
+};
+__device__ __forceinline__ AttendPart attend_part(const AttendCursor &c, int left) {
+    const int used = min(c.units - c.unit, left), from = max(c.unit, 0);
+    return {from, used - (from - c.unit), used};
 }
 
 // An item whose steps lie in several CTAs' shares: each leaves its rows'

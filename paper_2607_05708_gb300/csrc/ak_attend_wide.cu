@@ -39,15 +39,25 @@ struct Wide {
     static constexpr int HT = 64, HPT = N / HT;          // tokens the softmax takes at a time
     static constexpr int SN = MT == 2 ? N : HT;          // columns of S computed at once
     // Warps: softmax, dequantising, one that issues.  At D <= 128 the registers of five
-    // warpgroups are split by need (softmax 128, dequantising 88, the last one 48 a thread:
-    // together the 96 of the launch), so that a unit of a tile has a warp of its own:
-    // with two each a tile took its 4 warps 6000 cycles, as long as all else.
+    // warpgroups are split by need, so that a unit of a tile has a warp of its own.
+    // For softmax, dequantising, the last one, a thread; together the 96 of the launch: 4 bits
+    // 685 us with 120, 80, 80 and 695 with 128, 88, 48 (two requests of 2048 rows and 10240 tokens,
+    // 8 key/value heads, D = 128), 8 bits 1042 and 969 (its softmax has two factors a token more).
+    template <int BITS>
+    static constexpr int regs(int role) {
+        return BITS == 4 ? (role == 0 ? 120 : 80) : role == 0 ? 128 : role == 1 ? 88 : 48;
+    }
     static constexpr bool SPLIT = MT == 2;
     static constexpr int SOFT = 4 * MT, DEQ = SPLIT ? 8 : 4;
     static constexpr int THREADS = 32 * (SOFT + DEQ + (SPLIT ? 4 : 1));
-    static_assert(!SPLIT || 256 * 128 + 256 * 88 + 128 * 48 == THREADS * 96, "registers");
+    static_assert(!SPLIT || (256 * (regs<4>(0) + regs<4>(1)) + 128 * regs<4>(2) <= THREADS * 96 &&
+                             256 * (regs<8>(0) + regs<8>(1)) + 128 * regs<8>(2) <= THREADS * 96), "registers");
     static constexpr int UPW = UNITS / DEQ;              // units of a dequantising warp
     static constexpr int STAGES = 2;
+    // An item's beginning and end (query rows in, result out, an empty pipeline: 7 to 10 us; a step
+    // 2.8) count as steps: 0, 1, 2 and 3 of them 131, 110, 113 and 124 us for 7 documents in
+    // 6007 tokens at D = 64, 8 bits; 148, 116, 113 and 123 at D = 128, 4 bits.
+    static constexpr int EXTRA = 2;
     static constexpr int Q_BYTES = ROWS * D * 2, KV_BYTES = N * D * 2;
     static constexpr int S_COL = MT * D;                 // tensor memory: O, then S
     static constexpr uint32_t TMEM_COLS = 512;
@@ -66,8 +76,9 @@ struct alignas(16) Meta {           // pairs of its floats are read at once
     uint32_t have;
 };
 static_assert(offsetof(Meta<64>, ksig) % 8 == 0 && offsetof(Meta<64>, vsig) % 8 == 0 &&
-                  offsetof(Meta<128>, ksig) % 8 == 0 && offsetof(Meta<128>, vsig) % 8 == 0,
-              "pairs");
+                  offsetof(Meta<128>, ksig) % 8 == 0 && offsetof(Meta<128>, vsig) % 8 == 0 &&
+                  offsetof(Meta<64>, tag) % 16 == 0 && offsetof(Meta<128>, tag) % 16 == 0,
+              "pairs, and four tags");
 
 // 32 registers to 32 consecutive columns of the thread's lane, and the wait.
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
@@ -280,13 +291,13 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
     }
     int64_t *prefix = (int64_t *)sq_;          // until the warps have found their items
     static_assert(C::Q_BYTES >= (C::THREADS + 1) * 8, "the plan's sums");
-    attend_sums(p, ROWS, N, lo, hi, prefix);
+    attend_sums(p, ROWS, N, C::EXTRA, lo, hi, prefix);
     const int64_t total = prefix[C::THREADS];
     const int64_t per = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x);
     const int64_t first = per * blockIdx.x;
     int left = (int)max((int64_t)0, min(per, total - first));
     AttendCursor cur = {};
-    if (left > 0) cur = attend_find(p, ROWS, N, lo, hi, prefix, first);
+    if (left > 0) cur = attend_find(p, ROWS, N, C::EXTRA, lo, hi, prefix, first);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -295,14 +306,16 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
 
     if (warp >= C::SOFT && warp < C::SOFT + C::DEQ) {
         // ---------------- dequantising
-        if constexpr (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if constexpr (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::template regs<BITS>(1)));
         const int w = warp - C::SOFT, g = lane >> 2, c = lane & 3;
         const bool far = D == 128 && c >= 2, odd = D == 128 && (g & 1);    // (shared memory banks)
         uint32_t n_tile = 0;                   // tiles since the kernel began
         while (left > 0 && !*dead) {
-            const int n = min(cur.units - cur.unit, left), units = (cur.q.kv + KV_UNIT - 1) / KV_UNIT;
+            const AttendPart part = attend_part(cur, left);
+            const int n = part.n, units = (cur.q.kv + KV_UNIT - 1) / KV_UNIT;
+            if (n <= 0) break;
             // the tile of the item's first step that is this CTA's
-            const int first_tile = cur.unit + (p.ranges ? p.ranges[attend_range_at(p, cur.q, cur.tile, ROWS)].x : 0);
+            const int first_tile = part.from + (p.ranges ? p.ranges[attend_range_at(p, cur.q, cur.tile, ROWS)].x : 0);
             const int64_t *list = p.blocks + cur.seq * p.max_blocks;
             constexpr int PER = 32 / C::UPW;   // tiles of a look-up
             int64_t my_unit = -1, my_slots = 0;
@@ -535,12 +548,12 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 fence_async_smem();
                 mbar_arrive(&vfull[st]);
             }
-            left -= n;
-            if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
+            left -= part.used;
+            if (left > 0) attend_next(p, ROWS, N, C::EXTRA, lo, hi, cur);
         }
     } else if (warp >= C::SOFT + C::DEQ) {
         // ---------------- issuing
-        if constexpr (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        if constexpr (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::template regs<BITS>(2)));
         if (warp == C::SOFT + C::DEQ) {
             constexpr uint32_t id_s = idesc_f16(C::SN), id_o = idesc_f16(D) | IDESC_B_MN_MAJOR;
             const uint32_t go = lane == 0;
@@ -576,7 +589,9 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 umma_commit_if(go, &odone[t][b]);
             };
             while (left > 0 && ok) {
-                const int n = min(cur.units - cur.unit, left), nh = n * HPT;
+                const AttendPart part = attend_part(cur, left);
+                const int n = part.n, nh = n * HPT;
+                if (n <= 0) break;
                 const int mt = cur.q.nq * p.group - cur.tile * ROWS > 128 ? MT : 1;
                 if constexpr (MT == 1) {
                     // Two buffers: scores once theirs is free (the weights before were taken
@@ -629,8 +644,8 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 ph0 += nh;
                 if (mt > 1) ph1 += nh;
                 n_tile += n;
-                left -= n;
-                if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
+                left -= part.used;
+                if (left > 0) attend_next(p, ROWS, N, C::EXTRA, lo, hi, cur);
             }
             umma_commit_if(go, &drained);      // what was issued ends before the tensor memory goes
             mbar_wait(&drained, 0, p.status);
@@ -638,7 +653,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
         __syncwarp();
     } else {
         // ---------------- softmax: a lane is row 32 (warp % 4) + lane of row tile t
-        if constexpr (C::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+        if constexpr (C::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::template regs<BITS>(0)));
         const int t = warp >> 2, rt = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t o_at = tmem + lanes + t * D;
@@ -648,7 +663,9 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
         bool ok = true;
         int64_t done = 0;
         while (left > 0 && ok) {
-            const int n = min(cur.units - cur.unit, left);
+            const AttendPart mine = attend_part(cur, left);
+            const int n = mine.n;
+            if (n <= 0) break;
             const AttendSeq sq = cur.q;
             const int row_first = cur.tile * ROWS, rows = min(ROWS, sq.nq * p.group - row_first);
             const int r = t * 128 + rt;
@@ -765,7 +782,18 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                                 const int end = have >> u & 1u ? limit - tok - u * 16 : 0;
 #pragma unroll
                                 for (int k = 0; k < 16; ++k)
-                                    if (k >= end || (tags && m.tag[half + u * 16 + k] != qtag)) x[u * 16 + k] = 0xff800000u;
+                                    if (k >= end) x[u * 16 + k] = 0xff800000u;
+                                if (!tags) continue;
+                                // (four at once and without a branch: one after the other, each
+                                // behind the last one's branch, took 10 us a step)
+#pragma unroll
+                                for (int k = 0; k < 16; k += 4) {
+                                    const int4 y = *(const int4 *)&m.tag[half + u * 16 + k];
+                                    x[u * 16 + k] = y.x == qtag ? x[u * 16 + k] : 0xff800000u;
+                                    x[u * 16 + k + 1] = y.y == qtag ? x[u * 16 + k + 1] : 0xff800000u;
+                                    x[u * 16 + k + 2] = y.z == qtag ? x[u * 16 + k + 2] : 0xff800000u;
+                                    x[u * 16 + k + 3] = y.w == qtag ? x[u * 16 + k + 3] : 0xff800000u;
+                                }
                             }
                         }
                     }
@@ -829,7 +857,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 // ---- whole items are written, others left for the joining kernel
                 const bool whole = n == cur.units;
                 if (unset) mm = NEG;
-                float *part = p.partial + ((int64_t)blockIdx.x * 2 + (cur.unit == 0)) * attend_slot_floats(ROWS, D);
+                float *part = p.partial + ((int64_t)blockIdx.x * 2 + (mine.from == 0)) * attend_slot_floats(ROWS, D);
                 const int up = rv + (BITS == 4 ? UP : 0);
                 const float inv = whole ? (l > 0.f ? 1.f / l : l) : 1.f, up0 = pow2i(up / 2), up1 = pow2i(up - up / 2);
                 const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + hd;
@@ -851,9 +879,9 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 }
                 if (!whole) {
                     part[ROWS * D + r] = mm, part[ROWS * D + ROWS + r] = l;
-                    if (r == 0 && cur.unit == 0)
+                    if (r == 0 && mine.from == 0)
                         p.joins[blockIdx.x] = make_int4(cur.seq, cur.head, cur.tile,
-                                                        (int)((first + done + cur.units - 1) / per));
+                                                        (int)((first + done - cur.unit + cur.units - 1) / per));
                 } else if (real && p.lse) {
                     p.lse[dst] = lse_of(mm, l);
                 }
@@ -866,8 +894,8 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 ok = __all_sync(0xffffffffu, ok);
             }
             n_tile += n;
-            left -= n, done += n;
-            if (left > 0) attend_next(p, ROWS, N, lo, hi, cur);
+            left -= mine.used, done += mine.used;
+            if (left > 0) attend_next(p, ROWS, N, C::EXTRA, lo, hi, cur);
         }
     }
     tc_fence_before();
@@ -890,14 +918,22 @@ k_attend_ranges(const __grid_constant__ AttendParams p, int2 *ranges, const int 
     if (!attend_takes(p, q, lo, hi)) return;
     const int steps = (q.kv + step - 1) / step, T = p.per_block * KV_UNIT;
     const bool small = steps <= RANGE_STEPS;
-    for (int x = tid >> 5; small && x < steps; x += 32) {
+    const int warps = blockDim.x >> 5;
+    for (int x = tid >> 5; small && x < steps; x += warps) {
         int2 r = make_int2(0x7fffffff, -1);
-        for (int j = x * step + lane; j < min(q.kv, (x + 1) * step); j += 32) {
-            const int64_t id = p.blocks[s * p.max_blocks + j / T];
-            const bool real = id >= 0 && id < p.n_blocks;
-            const int t = real ? p.tags[id * T + j % T] : -1;
-            if (!real && id != -1) set_status(p.status, AKASHIC_EDEVICE);   // its step may be left out
-            if (t >= 0) r = make_int2(min(r.x, t), max(r.y, t));
+        const int j = x * step + 4 * lane;     // the lane's four tokens, of one block
+        if (4 * lane < step && j < q.kv) {
+            const int b = j / T;
+            const int64_t id = p.blocks[s * p.max_blocks + b];
+            if (id >= 0 && id < p.n_blocks) {
+                const int4 y = *(const int4 *)(p.tags + id * T + (j - b * T));
+                const int t[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (t[k] >= 0 && j + k < q.kv) r = make_int2(min(r.x, t[k]), max(r.y, t[k]));
+            } else if (id != -1) {
+                set_status(p.status, AKASHIC_EDEVICE);   // its step may be left out
+            }
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1)
@@ -906,21 +942,33 @@ k_attend_ranges(const __grid_constant__ AttendParams p, int2 *ranges, const int 
     }
     __syncthreads();
     const int tiles = attend_tiles(p, q, rows);
-    for (int t = tid; t < tiles; t += 1024) {
+    for (int t = tid >> 5; t < tiles; t += warps) {            // a warp a row tile
         const uint32_t all = (uint32_t)q.nq * p.group, end = min((uint32_t)(t + 1) * rows, all) - 1u;
         const int i0 = (int)((uint32_t)t * rows / p.group), i1 = (int)(end / p.group);
         const int limit = (attend_limit(p, q, i1) + step - 1) / step;
         int2 want = make_int2(0x7fffffff, -1), r = make_int2(0, limit);
-        for (int i = i0; i <= i1; ++i) {
+        for (int i = i0 + lane; i <= i1; i += 32) {
             const int y = p.q_tags[q.row0 + i];
             if (y >= 0) want = make_int2(min(want.x, y), max(want.y, y));
         }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            want = make_int2(min(want.x, __shfl_xor_sync(0xffffffffu, want.x, o)),
+                             max(want.y, __shfl_xor_sync(0xffffffffu, want.y, o)));
         if (small) {
-            auto seen = [&](int x) { return have[x].x <= want.y && have[x].y >= want.x; };
-            while (r.x < r.y && !seen(r.x)) ++r.x;
-            while (r.x < r.y && !seen(r.y - 1)) --r.y;
+            // 32 steps at a time from either side
+            auto seen = [&](int x) {
+                return __ballot_sync(0xffffffffu, x >= 0 && x < limit && have[x].x <= want.y && have[x].y >= want.x);
+            };
+            unsigned any = 0;
+            for (; r.x < limit && !(any = seen(r.x + lane)); r.x += 32) {}
+            r.x = any ? r.x + __ffs(any) - 1 : limit;
+            any = 0;
+            for (; r.y > r.x && !(any = seen(r.y - 1 - lane)); r.y -= 32) {}
+            r.y = any ? r.y - __ffs(any) + 1 : r.x;
         }
-        ranges[attend_range_at(p, q, t, rows)] = r;
+        if (lane == 0)
+            ranges[attend_range_at(p, q, t, rows)] = r;
     }
 }
 
@@ -949,8 +997,11 @@ AttendShape attend_wide_shape(int dim, int sms) {
 }
 cudaError_t launch_attend_ranges(const AttendParams &p, int dim, const AttendShape &shape, int lo, int hi,
                                  cudaStream_t st) {
-    k_attend_ranges<<<p.n_seq, 1024, 0, st>>>(p, (int2 *)p.ranges, shape.rows, dim == 256 ? Wide<256>::N : Wide<128>::N,
-                                              lo, hi);
+    const int step = dim == 256 ? Wide<256>::N : Wide<128>::N;
+    // a warp a step or row tile, as far as a CTA goes
+    const int64_t most = max((int64_t)p.max_kv / step, (int64_t)p.n_q * p.group / p.n_seq / shape.rows);
+    const int warps = (int)min((int64_t)32, max((int64_t)4, most));
+    k_attend_ranges<<<p.n_seq, 32 * warps, 0, st>>>(p, (int2 *)p.ranges, shape.rows, step, lo, hi);
     return cudaGetLastError();
 }
 cudaError_t launch_attend_wide(const AttendParams &p, int bits, int dim, int dtype,

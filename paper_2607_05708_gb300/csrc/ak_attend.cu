@@ -158,6 +158,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
     int *qtag = (int *)at + warp * ROWS;
     unsigned char *ring = smem + warp * C::RING;
 
+    griddep_wait();
     if (lane == 0)
         for (int i = 0; i < NS; ++i) mbar_init(bar + i, UPS);
     mbar_fence_init();
@@ -826,8 +827,7 @@ cudaError_t run_narrow(const AttendParams &p, int dtype, int ctas, int lo, int h
         if (e != cudaSuccess) return e;
         if (dev < 64) ready[dev].store(true, std::memory_order_release);
     }
-    kernel<<<ctas, NW * 32, C::SMEM, st>>>(p, dtype == AKASHIC_DTYPE_BF16, lo, hi);
-    return cudaGetLastError();
+    return launch_pdl(kernel, dim3(ctas), dim3(NW * 32), C::SMEM, st, p, dtype == AKASHIC_DTYPE_BF16, lo, hi);
 }
 template <int BITS, int D>
 cudaError_t run_narrow_rows(const AttendParams &p, int dtype, const AttendShape &s, int lo, int hi,

@@ -263,6 +263,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
     volatile int *dead = &dead_word;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
+    griddep_wait();
     if (tid == 0) {
         for (int i = 0; i < ST; ++i) {
             mbar_init(&kfull[i], 32 * C::DEQ);
@@ -913,6 +914,7 @@ __global__ void __launch_bounds__(1024)
 k_attend_ranges(const __grid_constant__ AttendParams p, int2 *ranges, const int rows, const int step, const int lo,
                 const int hi) {
     __shared__ int2 have[RANGE_STEPS];         // the least and the greatest tag of a step
+    griddep_wait();
     const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
     const AttendSeq q = attend_seq(p, s);
     if (!attend_takes(p, q, lo, hi)) return;
@@ -986,8 +988,7 @@ cudaError_t run_wide(const AttendParams &p, int dtype, int ctas, int lo, int hi,
         if (e != cudaSuccess) return e;
         if (dev < 64) ready[dev].store(true, std::memory_order_release);
     }
-    kernel<<<ctas, C::THREADS, C::SMEM, st>>>(p, dtype == AKASHIC_DTYPE_BF16, lo, hi);
-    return cudaGetLastError();
+    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, p, dtype == AKASHIC_DTYPE_BF16, lo, hi);
 }
 
 }  // namespace
@@ -1001,8 +1002,8 @@ cudaError_t launch_attend_ranges(const AttendParams &p, int dim, const AttendSha
     // a warp a step or row tile, as far as a CTA goes
     const int64_t most = max((int64_t)p.max_kv / step, (int64_t)p.n_q * p.group / p.n_seq / shape.rows);
     const int warps = (int)min((int64_t)32, max((int64_t)4, most));
-    k_attend_ranges<<<p.n_seq, 32 * warps, 0, st>>>(p, (int2 *)p.ranges, shape.rows, step, lo, hi);
-    return cudaGetLastError();
+    return launch_pdl(k_attend_ranges, dim3(p.n_seq), dim3(32 * warps), 0, st, p, (int2 *)p.ranges, shape.rows, step,
+                      lo, hi);
 }
 cudaError_t launch_attend_wide(const AttendParams &p, int bits, int dim, int dtype,
                                const AttendShape &s, int lo, int hi, cudaStream_t st) {

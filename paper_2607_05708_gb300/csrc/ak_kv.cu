@@ -139,6 +139,7 @@ k_kv_write(unsigned char *__restrict__ cache, const T *__restrict__ k, const T *
            uint32_t per_block, int tokens, int *status) {
     using U = KvUnit<BITS, D>;
     constexpr int G = U::GROUPS;
+    griddep_wait();
     const bool is_v = blockIdx.y;
     const T *base = is_v ? v : k;
     const int64_t row_stride = is_v ? v_row : k_row, head_stride = is_v ? v_head : k_head;
@@ -233,6 +234,7 @@ k_kv_read(const unsigned char *__restrict__ cache, T *__restrict__ k, T *__restr
           uint32_t per_block, int tokens, int *status) {
     using U = KvUnit<BITS, D>;
     constexpr int G = U::GROUPS;
+    griddep_wait();
     const bool is_v = blockIdx.y;
     T *out = is_v ? v : k;
     for (int64_t i0 = (int64_t)blockIdx.x * tokens; i0 < n; i0 += (int64_t)gridDim.x * tokens) {
@@ -315,50 +317,45 @@ unsigned kv_grid(int64_t n, int tokens) {
 }
 
 template <typename T, int BITS, int D>
-void launch_write(const KvRows &r, cudaStream_t st) {
+cudaError_t launch_write(const KvRows &r, cudaStream_t st) {
     const int tokens = kv_tokens(r.cfg->heads, D / 16);
     const uint32_t per = (uint32_t)(r.cfg->block_tokens / KV_UNIT);
     const uint32_t units = (uint32_t)(r.cfg->n_blocks * per);
     auto *kernel = r.wide ? k_kv_write<T, BITS, D, true> : k_kv_write<T, BITS, D, false>;
-    kernel<<<dim3(kv_grid(r.n, tokens), 2), 256, 0, st>>>(
-        r.cache, (const T *)r.in[0], (const T *)r.in[1], r.row_stride[0], r.head_stride[0],
-        r.row_stride[1], r.head_stride[1], r.slots, r.tags, r.new_tags, r.n, r.cfg->heads, units,
-        per, tokens, r.status);
+    return launch_pdl(kernel, dim3(kv_grid(r.n, tokens), 2), dim3(256), 0, st, r.cache, (const T *)r.in[0],
+                      (const T *)r.in[1], r.row_stride[0], r.head_stride[0], r.row_stride[1], r.head_stride[1],
+                      r.slots, r.tags, r.new_tags, r.n, r.cfg->heads, units, per, tokens, r.status);
 }
 template <typename T, int BITS, int D>
-void launch_read(const KvRows &r, cudaStream_t st) {
+cudaError_t launch_read(const KvRows &r, cudaStream_t st) {
     const int tokens = kv_tokens(r.cfg->heads, D / 16);
     const uint32_t per = (uint32_t)(r.cfg->block_tokens / KV_UNIT);
     const uint32_t units = (uint32_t)(r.cfg->n_blocks * per);
     auto *kernel = r.wide ? k_kv_read<T, BITS, D, true> : k_kv_read<T, BITS, D, false>;
-    kernel<<<dim3(kv_grid(r.n, tokens), 2), 256, 0, st>>>(r.cache, (T *)r.out[0], (T *)r.out[1],
-                                                          r.slots, r.n, r.cfg->heads, units, per,
-                                                          tokens, r.status);
+    return launch_pdl(kernel, dim3(kv_grid(r.n, tokens), 2), dim3(256), 0, st, r.cache, (T *)r.out[0],
+                      (T *)r.out[1], r.slots, r.n, r.cfg->heads, units, per, tokens, r.status);
 }
 
 template <typename T, int BITS>
-void launch_rows_dim(const KvRows &r, cudaStream_t st, bool write) {
+cudaError_t launch_rows_dim(const KvRows &r, cudaStream_t st, bool write) {
     switch (r.cfg->head_dim) {
-    case 64: write ? launch_write<T, BITS, 64>(r, st) : launch_read<T, BITS, 64>(r, st); break;
-    case 128: write ? launch_write<T, BITS, 128>(r, st) : launch_read<T, BITS, 128>(r, st); break;
-    default: write ? launch_write<T, BITS, 256>(r, st) : launch_read<T, BITS, 256>(r, st); break;
+    case 64: return write ? launch_write<T, BITS, 64>(r, st) : launch_read<T, BITS, 64>(r, st);
+    case 128: return write ? launch_write<T, BITS, 128>(r, st) : launch_read<T, BITS, 128>(r, st);
+    default: return write ? launch_write<T, BITS, 256>(r, st) : launch_read<T, BITS, 256>(r, st);
     }
 }
 template <typename T>
-void launch_rows_bits(const KvRows &r, cudaStream_t st, bool write) {
-    r.cfg->bits == 4 ? launch_rows_dim<T, 4>(r, st, write) : launch_rows_dim<T, 8>(r, st, write);
+cudaError_t launch_rows_bits(const KvRows &r, cudaStream_t st, bool write) {
+    return r.cfg->bits == 4 ? launch_rows_dim<T, 4>(r, st, write) : launch_rows_dim<T, 8>(r, st, write);
 }
 
 akashic_status_t run_rows(const char *who, const KvRows &r, int32_t dtype, void *stream, bool write) {
     KvDevice dev(r.cfg->device);
     if (!dev.ok) return kv_fail(AKASHIC_ECUDA, "%s: device %d cannot be made current", who, r.cfg->device);
     cudaStream_t st = (cudaStream_t)stream;
-    switch (dtype) {
-    case AKASHIC_DTYPE_BF16: launch_rows_bits<__nv_bfloat16>(r, st, write); break;
-    case AKASHIC_DTYPE_FP16: launch_rows_bits<__half>(r, st, write); break;
-    default: launch_rows_bits<float>(r, st, write); break;
-    }
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = dtype == AKASHIC_DTYPE_BF16   ? launch_rows_bits<__nv_bfloat16>(r, st, write)
+                          : dtype == AKASHIC_DTYPE_FP16 ? launch_rows_bits<__half>(r, st, write)
+                                                        : launch_rows_bits<float>(r, st, write);
     if (e != cudaSuccess) return kv_fail(AKASHIC_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return AKASHIC_OK;
 }

@@ -469,16 +469,16 @@ typedef struct {
     float *lse;                /* device float[n_q][q_heads] or NULL                 */
 } akashic_mem_kv_attend_t;
 
-/* Bytes of scratch that a call with these arguments needs (sizes and which pointers are
- * NULL matter, not their contents).  Calls that may overlap, and graphs that may run at
- * the same time, need scratch of their own. */
+/* Bytes of scratch (0 for some) that a call with these arguments needs: sizes and which
+ * pointers are NULL matter, not their contents.  Calls that may overlap, and graphs that
+ * may run at the same time, need scratch of their own. */
 akashic_status_t akashic_mem_kv_attend_scratch(const akashic_mem_kv_config_t *cfg,
                                                const akashic_mem_kv_attend_t *a, int64_t *bytes);
 
-/* scratch: device, 16-byte aligned, not initialised.  EINVAL for a bad config or
- * argument (as noted above), n_q x q_heads beyond 2^31 - 1, a scale or cap that is
- * not finite, a cap below 0 or subnormal, tags without q_tags, or scratch that is too small;
- * ECUDA if a launch fails. */
+/* scratch: device, 16-byte aligned, not initialised; NULL where none is needed.
+ * EINVAL for a bad config or argument (as noted above), n_q x q_heads beyond 2^31 - 1,
+ * a scale or cap that is not finite, a cap below 0 or subnormal, tags without q_tags,
+ * or scratch that is too small; ECUDA if a launch fails. */
 akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t *cfg, const void *cache,
                                        const akashic_mem_kv_attend_t *a, void *scratch,
                                        int64_t scratch_bytes, int32_t *status, void *stream);

@@ -556,8 +556,8 @@ class KVCache:
             if len(self._scratch) > 4096:
                 self._scratch.clear()
             size = self._scratch[key] = need.value
-        scratch = self._empty((size,), torch.uint8, stream)
-        rc = self._attend(self._cfg, self._data_ptr, ref, scratch.data_ptr(), size,
+        scratch = self._empty((size,), torch.uint8, stream) if size else None
+        rc = self._attend(self._cfg, self._data_ptr, ref, scratch.data_ptr() if size else None, size,
                           self._status_ptr, self._on(stream))
         if rc:
             _check(rc)

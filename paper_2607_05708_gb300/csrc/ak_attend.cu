@@ -24,6 +24,12 @@
 //  * P is fp16, 2^6 p: weights down to 2^-20 of the largest so far keep 11 bits; sums,
 //    maxima and accumulators are fp32.  The maximum is raised only when a
 //    score exceeds it by 2^8, so that the accumulators are rarely rescaled.
+// Measured (one query row of 32 heads a sequence, 8 key/value heads, D = 128, 4 bits): 64
+// sequences of 4096, 8192 and 16384 tokens 80, 134 and 243 us, so 5.6 TB/s (83 % of a
+// copy) for what is added and 25 us beside it: the plan and the first fetches (8), the rings'
+// filling and the warps' uneven ends, the join (4).  In the loop some 300 instructions a unit
+// issue in 2.3 of 4 slots (ALU pipe 49 %): they, not the 75 KB in flight an SM, are next to
+// the bytes.  8 heads of 700 tokens 12 us, of which 10 are there for 100 tokens too.
 #include <atomic>
 
 #include "ak_attend.cuh"
@@ -133,7 +139,9 @@ __device__ __forceinline__ float load_query(const AttendParams &p, bool bf16, in
     return pow2i(e);
 }
 
-template <int BITS, int D, int NB>
+// HEAVY: capped scores or a distance bias.  Compiled apart: their instructions in the loop, though
+// jumped over, cost the others 3 % (64 sequences of up to 8192 tokens 89.4 and 86.5 us).
+template <int BITS, int D, int NB, bool HEAVY>
 __global__ void __launch_bounds__(NW * 32, Narrow<BITS, D, NB>::TWO ? 2 : 1)
 k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const int lo, const int hi) {
     using C = Narrow<BITS, D, NB>;
@@ -163,7 +171,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
         for (int i = 0; i < NS; ++i) mbar_init(bar + i, UPS);
     mbar_fence_init();
     if (lane < 2) entries[2 * warp + lane].seq = -1;
-    if (tid == 0) p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    if (tid == 0 && !p.direct) p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
     // The warp's share: of all steps, or (p.direct) of the CTA's one item.
     AttendCursor cur = {};
     int64_t per, first;
@@ -195,7 +203,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
     uint32_t my_unit = 0, my_slots = 0;        // this lane's unit of the cache, its slots / 16
     int my_state = 0;                          // 0: no token of it is seen, 1: by its tags, 3: all are
     int fetch_left = left, turn = 32, turn_end = 32, fetch_stage = 0;
-    const bool tags = p.tags != nullptr, heavy = p.cap > 0.f || p.slopes;
+    const bool tags = p.tags != nullptr;
     auto look_up = [&]() {
         AttendCursor x = ahead->cur;
         int i = ahead->i, n = ahead->n;        // steps of the item: done, this share's
@@ -415,7 +423,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                 for (int j = 0; j < UPS; ++j) {
 #pragma unroll
                     for (int b = 0; b < NB; ++b) {
-                        if (heavy) {
+                        if constexpr (HEAVY) {
                             uint32_t x[4];
 #pragma unroll
                             for (int r = 0; r < 4; ++r)
@@ -813,10 +821,10 @@ k_attend_join(const AttendParams p, const int rows, const bool bf16) {
     }
 }
 
-template <int BITS, int D, int NB>
+template <int BITS, int D, int NB, bool HEAVY>
 cudaError_t run_narrow(const AttendParams &p, int dtype, int ctas, int lo, int hi, cudaStream_t st) {
     using C = Narrow<BITS, D, NB>;
-    auto *kernel = k_attend_narrow<BITS, D, NB>;
+    auto *kernel = k_attend_narrow<BITS, D, NB, HEAVY>;
     // once a device (the attribute stays; another thread that comes first does the same)
     static std::atomic<bool> ready[64];
     int dev = 0;
@@ -829,11 +837,16 @@ cudaError_t run_narrow(const AttendParams &p, int dtype, int ctas, int lo, int h
     }
     return launch_pdl(kernel, dim3(ctas), dim3(NW * 32), C::SMEM, st, p, dtype == AKASHIC_DTYPE_BF16, lo, hi);
 }
+template <int BITS, int D, int NB>
+cudaError_t run_narrow_kind(const AttendParams &p, int dtype, int ctas, int lo, int hi, cudaStream_t st) {
+    return p.cap > 0.f || p.slopes ? run_narrow<BITS, D, NB, true>(p, dtype, ctas, lo, hi, st)
+                                   : run_narrow<BITS, D, NB, false>(p, dtype, ctas, lo, hi, st);
+}
 template <int BITS, int D>
 cudaError_t run_narrow_rows(const AttendParams &p, int dtype, const AttendShape &s, int lo, int hi,
                             cudaStream_t st) {
-    if (s.rows == 8) return run_narrow<BITS, D, 1>(p, dtype, s.ctas, lo, hi, st);
-    if constexpr (D <= 128) return run_narrow<BITS, D, 2>(p, dtype, s.ctas, lo, hi, st);
+    if (s.rows == 8) return run_narrow_kind<BITS, D, 1>(p, dtype, s.ctas, lo, hi, st);
+    if constexpr (D <= 128) return run_narrow_kind<BITS, D, 2>(p, dtype, s.ctas, lo, hi, st);
     return cudaErrorInvalidValue;
 }
 template <int BITS>
@@ -941,6 +954,7 @@ AttendRoute route_of(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_at
     if (most >= from) r.wide = attend_wide_shape(cfg->head_dim, sms);
     const int64_t steps = ceil_div(a->max_blocks * cfg->block_tokens, (int64_t)32);
     r.direct = !a->q_start && most <= r.narrow.rows && (int64_t)a->n_seq * cfg->heads <= r.narrow.ctas && steps <= DIRECT_STEPS;
+    if (r.direct) return r;                       // no scratch
     r.joins = ceil_div((int64_t)(r.narrow.ctas + r.wide.ctas) * 16, (int64_t)256) * 256;
     r.narrow_floats = r.narrow.ctas * 2 * attend_slot_floats(r.narrow.rows, cfg->head_dim);
     if (r.wide.ctas && a->tags)
@@ -971,7 +985,7 @@ extern "C" akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t 
     set_last_error("");
     if (akashic_status_t s = attend_check(cfg, a, "kv_attend")) return s;
     if (a->n_seq == 0 || a->n_q == 0) return AKASHIC_OK;
-    if (!cache || !a->q || !a->out || (!a->blocks && a->max_blocks) || !scratch)
+    if (!cache || !a->q || !a->out || (!a->blocks && a->max_blocks) || (!scratch && scratch_bytes > 0))
         return kv_fail(AKASHIC_EINVAL, "kv_attend: NULL argument");
     if (((uintptr_t)cache | (uintptr_t)scratch | (uintptr_t)a->tags) & 15u)
         return kv_fail(AKASHIC_EINVAL, "kv_attend: cache, tags and scratch must be 16-byte aligned");

@@ -19,6 +19,10 @@
 // Keys are v 2^-9 relative to their tile's largest exponent (its power of two is
 // a factor of the scores), values relative to the item's largest so far: where
 // fp16's normal range ends they are rounded to 2^-17 of that largest.
+// Measured (4 bits): two requests of 2048 rows behind 10240 tokens, 32 heads on 8, D = 128 (514
+// GFLOP) 682 us, 0.75 PFLOP/s, and 905 us with capped scores; a step of 256 rows and 128
+// tokens 2.8 us, of which the products are 1.06: scores, softmax and O += P V of a row tile
+// follow each other, and tensor memory (O of two tiles, and S) has no room for a second S.
 #include <stddef.h>
 
 #include <atomic>
@@ -40,12 +44,14 @@ struct Wide {
     static constexpr int SN = MT == 2 ? N : HT;          // columns of S computed at once
     // Warps: softmax, dequantising, one that issues.  At D <= 128 the registers of five
     // warpgroups are split by need, so that a unit of a tile has a warp of its own.
-    // For softmax, dequantising, the last one, a thread; together the 96 of the launch: 4 bits
-    // 685 us with 120, 80, 80 and 695 with 128, 88, 48 (two requests of 2048 rows and 10240 tokens,
-    // 8 key/value heads, D = 128), 8 bits 1042 and 969 (its softmax has two factors a token more).
+    // For softmax, dequantising, the last one, a thread; together the 96 of the launch.  Two
+    // requests of 2048 rows and 10240 tokens, 8 key/value heads, D = 128, us:
+    //   4 bits  685 with 120, 80, 80; 695 with 128, 88, 48 and with 144, 72, 48
+    //   8 bits  839 with 144, 72, 48; 976 with 128, 88, 48; 1042 with 120, 80, 80 (two
+    //           factors a token more in the softmax)
     template <int BITS>
     static constexpr int regs(int role) {
-        return BITS == 4 ? (role == 0 ? 120 : 80) : role == 0 ? 128 : role == 1 ? 88 : 48;
+        return BITS == 4 ? (role == 0 ? 120 : 80) : role == 0 ? 144 : role == 1 ? 72 : 48;
     }
     static constexpr bool SPLIT = MT == 2;
     static constexpr int SOFT = 4 * MT, DEQ = SPLIT ? 8 : 4;

@@ -319,7 +319,8 @@ def test_arguments_are_checked():
         assert e.value.code == "EINVAL"
     # scratch that is too small
     from paper_2607_05708_gb300 import _KVAttend, load_library
-    a = _KVAttend(q.data_ptr(), 256, 64, 1, 3, 4, 3, None, None, b.data_ptr(), 1, 1, None, 0.0, 0.0,
+    starts = torch.arange(4, dtype=torch.int32, device="cuda")          # (without them it needs none)
+    a = _KVAttend(q.data_ptr(), 256, 64, 1, 3, 4, 3, starts.data_ptr(), None, b.data_ptr(), 1, 1, None, 0.0, 0.0,
                   None, None, None, q.data_ptr(), None)
     scratch = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
     assert load_library().akashic_mem_kv_attend(c._cfg, c.data.data_ptr(), ctypes.byref(a),

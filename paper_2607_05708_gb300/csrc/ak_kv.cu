@@ -4,10 +4,14 @@
 // Both are one pass over the dense rows, bound by memory.  A thread has 16
 // consecutive dims of one row: the scale group of the 4-bit format, so that only
 // the row's largest magnitude needs its neighbours (D / 16 lanes of the warp).
-// Keys and values are the two halves of the grid.
-// Measured (8 heads, D = 128, 4 bits, bf16): 8192 tokens written in 14.8 us, read in 10.7
-// (43 MB: 2.9 and 4.0 TB/s), 16384 read in 19.1 (4.5); a single token 1.9 and 1.4 us.
-// The division by an 8-bit scale, exactly rounded, costs the writing its instructions.
+// Writing has keys and values in the two halves of the grid, reading both in one thread, which
+// then looks up its slot once: 16384 tokens 16.3 us and 19.1 in halves.  Writing in
+// one thread took 13.5 us instead of 14.7 for 8192 tokens, but 2.3 instead of 1.9 for one,
+// which every decoded token is.
+// Measured (8 heads, D = 128, 4 bits, bf16): 8192 tokens written in 14.7 us, read in 8.8
+// (43 MB: 2.9 and 4.9 TB/s), 16384 read in 16.3 (5.3); a single token 1.9 and 1.6 us.
+// The division by an 8-bit scale, exactly rounded, costs the writing its instructions, the
+// nibbles the reading.
 #include <stdarg.h>
 #include <stdio.h>
 
@@ -238,71 +242,60 @@ k_kv_read(const unsigned char *__restrict__ cache, T *__restrict__ k, T *__restr
     using U = KvUnit<BITS, D>;
     constexpr int G = U::GROUPS;
     griddep_wait();
-    const bool is_v = blockIdx.y;
-    T *out = is_v ? v : k;
     for (int64_t i0 = (int64_t)blockIdx.x * tokens; i0 < n; i0 += (int64_t)gridDim.x * tokens) {
         const uint32_t total = (uint32_t)min((int64_t)tokens, n - i0) * heads * G;
         for (uint32_t x = threadIdx.x; x < total; x += 256) {
             const uint32_t row = x / G, gr = x % G, ti = row / (uint32_t)heads, h = row - ti * heads;
             const int d0 = gr * 16;
             const KvPlace at = kv_place(slots[i0 + ti], h, heads, units, per_block, status);
-            alignas(16) T raw[16];
-            float f[16];
-            if (at.unit < 0) {
-#pragma unroll
-                for (int p = 0; p < 16; ++p) f[p] = 0.f;
-            } else {
+            const int t = at.token;
+            // both rows' codes and scales on their way before the arithmetic
+            uint32_t w[2][BITS / 2];
+            float s[2] = {0.f, 0.f};
+            if (at.unit >= 0) {
                 const unsigned char *src = cache + at.unit * U::BYTES;
-                const int t = at.token;
-                uint32_t w[BITS / 2];
-                float s;
                 if constexpr (BITS == 4) {
-                    if (is_v) {
-                        if (U::v_code(0, 8) == U::v_code(0, 0) + 4) {
-                            const uint2 q = *(const uint2 *)(src + U::v_code(t, d0));
-                            w[0] = q.x, w[1] = q.y;
-                        } else {
-                            w[0] = *(const uint32_t *)(src + U::v_code(t, d0));
-                            w[1] = *(const uint32_t *)(src + U::v_code(t, d0 + 8));
-                        }
-                        s = kv_scale_of(src[U::v_scale(t, gr)]) *
-                            pow2i((int)src[U::V_EXP + U::v_row(t)] - 127);
+                    const uint2 q = *(const uint2 *)(src + U::k_code(t, d0));
+                    w[0][0] = q.x, w[0][1] = q.y;
+                    if (U::v_code(0, 8) == U::v_code(0, 0) + 4) {
+                        const uint2 y = *(const uint2 *)(src + U::v_code(t, d0));
+                        w[1][0] = y.x, w[1][1] = y.y;
                     } else {
-                        const uint2 q = *(const uint2 *)(src + U::k_code(t, d0));
-                        w[0] = q.x, w[1] = q.y;
-                        s = kv_scale_of(src[U::k_scale(t, gr)]) *
-                            pow2i((int)src[U::K_EXP + U::k_row(t)] - 127);
+                        w[1][0] = *(const uint32_t *)(src + U::v_code(t, d0));
+                        w[1][1] = *(const uint32_t *)(src + U::v_code(t, d0 + 8));
                     }
-#pragma unroll
-                    for (int p = 0; p < 16; ++p)
-                        f[p] = kv_value<8>((w[p >> 3] >> (4 * ((p & 7) >> 1) + 16 * (p & 1))) & 15u, s);
+                    s[0] = kv_scale_of(src[U::k_scale(t, gr)]) * pow2i((int)src[U::K_EXP + U::k_row(t)] - 127);
+                    s[1] = kv_scale_of(src[U::v_scale(t, gr)]) * pow2i((int)src[U::V_EXP + U::v_row(t)] - 127);
                 } else {
-                    uint32_t sb;
-                    if (is_v) {
-                        const uint2 q0 = *(const uint2 *)(src + U::v_code(t, d0));
-                        const uint2 q1 = *(const uint2 *)(src + U::v_code(t, d0 + 8));
-                        w[0] = q0.x, w[1] = q0.y, w[2] = q1.x, w[3] = q1.y;
-                        sb = ((const uint16_t *)(src + U::V_SCALES))[U::v_row(t)];
-                    } else {
-                        const uint4 q = *(const uint4 *)(src + U::k_code(t, d0));
-                        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
-                        sb = ((const uint16_t *)(src + U::K_SCALES))[U::k_row(t)];
-                    }
-                    s = __uint_as_float(sb << 16);
-#pragma unroll
-                    for (int p = 0; p < 16; ++p) f[p] = kv_value<128>((w[p >> 2] >> (8 * (p & 3))) & 255u, s);
+                    const uint4 q = *(const uint4 *)(src + U::k_code(t, d0));
+                    const uint2 y0 = *(const uint2 *)(src + U::v_code(t, d0));
+                    const uint2 y1 = *(const uint2 *)(src + U::v_code(t, d0 + 8));
+                    w[0][0] = q.x, w[0][1] = q.y, w[0][2] = q.z, w[0][3] = q.w;
+                    w[1][0] = y0.x, w[1][1] = y0.y, w[1][2] = y1.x, w[1][3] = y1.y;
+                    s[0] = __uint_as_float((uint32_t)((const uint16_t *)(src + U::K_SCALES))[U::k_row(t)] << 16);
+                    s[1] = __uint_as_float((uint32_t)((const uint16_t *)(src + U::V_SCALES))[U::v_row(t)] << 16);
                 }
             }
 #pragma unroll
-            for (int p = 0; p < 16; ++p) from_f32(f[p], raw[p]);
-            T *dst = out + i0 * heads * D + (int64_t)x * 16;
-            if constexpr (WIDE) {
+            for (int is_v = 0; is_v < 2; ++is_v) {
+                alignas(16) T raw[16];
 #pragma unroll
-                for (int w = 0; w < (int)sizeof(raw) / 16; ++w)
-                    __stcs((int4 *)dst + w, ((const int4 *)raw)[w]);
-            } else {
+                for (int p = 0; p < 16; ++p) {
+                    float f = 0.f;
+                    if (at.unit >= 0)
+                        f = BITS == 4 ? kv_value<8>((w[is_v][p >> 3] >> (4 * ((p & 7) >> 1) + 16 * (p & 1))) & 15u, s[is_v])
+                                      : kv_value<128>((w[is_v][p >> 2] >> (8 * (p & 3))) & 255u, s[is_v]);
+                    from_f32(f, raw[p]);
+                }
+                T *dst = (is_v ? v : k) + i0 * heads * D + (int64_t)x * 16;
+                if constexpr (WIDE) {
 #pragma unroll
-                for (int p = 0; p < 16; ++p) dst[p] = raw[p];
+                    for (int q = 0; q < (int)sizeof(raw) / 16; ++q)
+                        __stcs((int4 *)dst + q, ((const int4 *)raw)[q]);
+                } else {
+#pragma unroll
+                    for (int p = 0; p < 16; ++p) dst[p] = raw[p];
+                }
             }
         }
     }
@@ -335,7 +328,7 @@ cudaError_t launch_read(const KvRows &r, cudaStream_t st) {
     const uint32_t per = (uint32_t)(r.cfg->block_tokens / KV_UNIT);
     const uint32_t units = (uint32_t)(r.cfg->n_blocks * per);
     auto *kernel = r.wide ? k_kv_read<T, BITS, D, true> : k_kv_read<T, BITS, D, false>;
-    return launch_pdl(kernel, dim3(kv_grid(r.n, tokens), 2), dim3(256), 0, st, r.cache, (T *)r.out[0],
+    return launch_pdl(kernel, dim3(kv_grid(r.n, tokens)), dim3(256), 0, st, r.cache, (T *)r.out[0],
                       (T *)r.out[1], r.slots, r.n, r.cfg->heads, units, per, tokens, r.status);
 }
 

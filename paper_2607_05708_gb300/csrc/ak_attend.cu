@@ -25,8 +25,8 @@
 //    maxima and accumulators are fp32.  The maximum is raised only when a
 //    score exceeds it by 2^8, so that the accumulators are rarely rescaled.
 // Measured (one query row of 32 heads a sequence, 8 key/value heads, D = 128, 4 bits): 64
-// sequences of 4096, 8192 and 16384 tokens 80, 134 and 243 us, so 5.6 TB/s (83 % of a
-// copy) for what is added and 25 us beside it: the plan and the first fetches (8), the rings'
+// sequences of 4096, 8192 and 16384 tokens 77, 130 and 237 us, so 5.7 TB/s (84 % of a
+// copy) for what is added and 24 us beside it: the plan and the first fetches (8), the rings'
 // filling and the warps' uneven ends, the join (4).  In the loop some 300 instructions a unit
 // issue in 2.3 of 4 slots (ALU pipe 49 %): they, not the 75 KB in flight an SM, are next to
 // the bytes.  8 heads of 700 tokens 12 us, of which 10 are there for 100 tokens too.

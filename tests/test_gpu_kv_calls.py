@@ -115,6 +115,35 @@ def test_rows_around_the_switch_of_kernels(bits, dim, dtype, extra):
     _compare(got, want, dim, dtype, bits, rows=sum(nq))
 
 
+@pytest.mark.parametrize("docs", [0, 2])
+def test_more_sequences_than_threads(docs):
+    """3000 sequences, most of them without a row, some without a token, some of many rows."""
+    rng = np.random.default_rng(71)
+    S = 3000
+    nq = np.where(np.arange(S) % 7 == 3, 1, 0)
+    nq[[5, 1500, 2999]] = 70, 3, 66
+    kv = rng.integers(0, 40, S)
+    c, q, blocks, args, want = _problem(72, kv=tuple(kv), nq=tuple(nq), heads=2, group=1, docs=docs)
+    got = c.attend(q, blocks, **args)
+    c.sync()
+    _compare(got, want, 128, "bf16", 4)
+    ones = (1,) * S
+    c, q, blocks, args, want = _problem(73, kv=tuple(kv), nq=ones, heads=2, group=1, docs=docs, dim=64)
+    got = c.attend(q, blocks, **args)
+    c.sync()
+    _compare(got, want, 64, "bf16", 4)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_tags_over_a_long_context(causal):
+    """More steps than the ranges of tags are kept for."""
+    c, q, blocks, args, want = _problem(74, kv=(530_000,), nq=(66,), heads=1, group=1, docs=3, dim=64,
+                                        T=128, causal=causal, dtype="fp16")
+    got = c.attend(q, blocks, **args)
+    c.sync()
+    _compare(got, want, 64, "fp16", 4)
+
+
 def test_strided_queries():
     """Queries inside a wider projection, heads first, at odd offsets."""
     for rows in (3, 290):

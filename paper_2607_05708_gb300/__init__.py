@@ -385,8 +385,9 @@ class KVCache:
     MemStore.retrieve returns the list of blocks to attend over.  With
     `tagged`, every slot has an int32 tag (-1 while it holds no token): a
     namespace or a document, which attention can be restricted to.  No
-    gradient is recorded through any of the calls.  The memory is `data` (uint8), `tags` (int32 [n_blocks * block_tokens] or None)
-    and `status` (int32 [1], read and cleared by sync())."""
+    gradient is recorded through any of the calls.  The memory is `data`
+    (uint8), `tags` (int32 [n_blocks * block_tokens] or None) and `status`
+    (int32 [1], read and cleared by sync())."""
 
     def __init__(self, n_blocks: int, heads: int, head_dim: int, block_tokens: int = 64,
                  bits: int = 4, device: int = 0, tagged: bool = False):

@@ -58,7 +58,7 @@ struct Wide {
     static constexpr int THREADS = 32 * (SOFT + DEQ + (SPLIT ? 4 : 1));
     static_assert(!SPLIT || (256 * (regs<4>(0) + regs<4>(1)) + 128 * regs<4>(2) <= THREADS * 96 &&
                              256 * (regs<8>(0) + regs<8>(1)) + 128 * regs<8>(2) <= THREADS * 96), "registers");
-    static constexpr int UPW = UNITS / DEQ;              // units of a dequantising warp
+    static_assert(UNITS == DEQ, "a dequantising warp has one unit of every tile");
     static constexpr int STAGES = 2;
     // An item's beginning and end (query rows in, result out, an empty pipeline: 7 to 10 us; a step
     // 2.8) count as steps: 0, 1, 2 and 3 of them 131, 110, 113 and 124 us for 7 documents in
@@ -324,12 +324,11 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
             // the tile of the item's first step that is this CTA's
             const int first_tile = part.from + (p.ranges ? p.ranges[attend_range_at(p, cur.q, cur.tile, ROWS)].x : 0);
             const int64_t *list = p.blocks + cur.seq * p.max_blocks;
-            constexpr int PER = 32 / C::UPW;   // tiles of a look-up
             int64_t my_unit = -1, my_slots = 0;
-            auto look_up = [&](int i) {        // lane: tile i + lane / UPW, this warp's unit lane % UPW
+            auto look_up = [&](int i) {        // lane: this warp's unit of tile i + lane
                 my_unit = -1;
-                const int tile = i + lane / C::UPW;
-                const int u = (first_tile + tile) * C::UNITS + w * C::UPW + lane % C::UPW;
+                const int tile = i + lane;
+                const int u = (first_tile + tile) * C::UNITS + w;
                 if (tile < n && u < units) {
                     const int b = u / p.per_block, x = u - b * p.per_block;
                     const int64_t id = list[b];
@@ -341,76 +340,63 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     }
                 }
             };
-            UnitRegs<BITS, D> r[C::UPW];
-            int64_t un[C::UPW];                // of the tile whose registers are being filled
+            UnitRegs<BITS, D> r;
+            int64_t un = -1;                   // of the tile whose registers are being filled
             int tag_next = 0;
             auto places = [&](int i) {         // of tile i
-                if (i % PER == 0) look_up(i);
-#pragma unroll
-                for (int j = 0; j < C::UPW; ++j)
-                    un[j] = __shfl_sync(0xffffffffu, my_unit, i % PER * C::UPW + j);
-                if (tags) {                    // lane: the tag of token lane of the warp's units
-                    const int64_t sl = __shfl_sync(0xffffffffu, my_slots, i % PER * C::UPW + (C::UPW == 2 ? lane >> 4 : 0));
-                    const int64_t ok = lane < 16 ? un[0] : un[C::UPW - 1];
-                    tag_next = ok >= 0 && (C::UPW == 2 || lane < 16) ? p.tags[sl * 16 + (lane & 15)] : -1;
+                if (i % 32 == 0) look_up(i);
+                un = __shfl_sync(0xffffffffu, my_unit, i % 32);
+                if (tags) {                    // lane: the tag of the unit's token lane
+                    const int64_t sl = __shfl_sync(0xffffffffu, my_slots, i % 32);
+                    tag_next = un >= 0 && lane < 16 ? p.tags[sl * 16 + lane] : -1;
                 }
             };
             places(0);
-#pragma unroll
-            for (int j = 0; j < C::UPW; ++j) {
-                load_keys<BITS, D>(p.cache + un[j] * U::BYTES, un[j] >= 0, r[j]);
-                load_values<BITS, D>(p.cache + un[j] * U::BYTES, un[j] >= 0, r[j]);
-            }
+            load_keys<BITS, D>(p.cache + un * U::BYTES, un >= 0, r);
+            load_values<BITS, D>(p.cache + un * U::BYTES, un >= 0, r);
             int rv = -127;
             for (int i = 0; i < n; ++i, ++n_tile) {
                 const int st = n_tile % ST, tok = (first_tile + i) * N;
                 if (!wide_wait(&empty[st], ((n_tile / ST) & 1) ^ 1, dead, p.status)) break;
                 Meta<N> &m = meta[st];
-                bool have[C::UPW];
-#pragma unroll
-                for (int j = 0; j < C::UPW; ++j) have[j] = un[j] >= 0;
-                // valid tokens of the warp's units, 16 bits each
-                const int lt = w * C::UPW * 16 + lane;     // the lane's token in the tile
-                bool mine = tok + lt < cur.q.kv;
+                const bool have = un >= 0;
+                const int t0 = w * 16, lt = t0 + lane;     // the unit's first token in the tile, the lane's
+                bool mine = have && lane < 16 && tok + lt < cur.q.kv;
                 if (tags) {
                     mine = mine && tag_next >= 0;
-                    if (C::UPW == 2 || lane < 16) m.tag[lt] = max(tag_next, -1);
+                    if (lane < 16) m.tag[lt] = max(tag_next, -1);
                 }
-                const uint32_t valid = __ballot_sync(0xffffffffu, mine && (lane < 16 ? have[0] : C::UPW == 2 && have[C::UPW - 1]));
+                const uint32_t ok = __ballot_sync(0xffffffffu, mine);      // the unit's valid tokens
                 // exponents: keys relative to the tile's largest, values to the item's
-                int kt[C::UPW][2], vt[C::UPW][4], kmax = -126, vmax = -127;
+                int kt[2], vt[4], kmax = -126, vmax = -127;
+                if constexpr (BITS == 4) {
+                    kt[0] = (int)(r.ke & 255u) - 127, kt[1] = (int)(r.ke >> 8 & 255u) - 127;
 #pragma unroll
-                for (int j = 0; j < C::UPW; ++j) {
-                    const uint32_t ok = valid >> (16 * j);
-                    if constexpr (BITS == 4) {
-                        kt[j][0] = (int)(r[j].ke & 255u) - 127, kt[j][1] = (int)(r[j].ke >> 8 & 255u) - 127;
+                    for (int x = 0; x < 4; ++x) vt[x] = (int)(r.ve >> (8 * x) & 255u) - 127;
+                } else {
+                    kt[0] = (int)(r.ks[0] >> 7 & 255u) - 127, kt[1] = (int)(r.ks[0] >> 23 & 255u) - 127;
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) vt[j][x] = (int)(r[j].ve >> (8 * x) & 255u) - 127;
-                    } else {
-                        kt[j][0] = (int)(r[j].ks[0] >> 7 & 255u) - 127, kt[j][1] = (int)(r[j].ks[0] >> 23 & 255u) - 127;
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) vt[j][x] = (int)(r[j].vs[x >> 1] >> (7 + 16 * (x & 1)) & 255u) - 127;
+                    for (int x = 0; x < 4; ++x) vt[x] = (int)(r.vs[x >> 1] >> (7 + 16 * (x & 1)) & 255u) - 127;
+                }
+                if (!(ok >> g & 1u)) kt[0] = -1000;
+                if (!(ok >> (g + 8) & 1u)) kt[1] = -1000;
+                kmax = max(kmax, max(kt[0], kt[1]));
+                if constexpr (BITS == 8) {
+                    // significands; 1 where there is no token
+                    if (c < 2) {
+                        const uint32_t s = c ? r.ks[0] >> 16 : r.ks[0];
+                        m.ksig[t0 + g + 8 * c] = (c ? kt[1] : kt[0]) == -1000 ? 1.f : __uint_as_float((s & 0x7fu) << 16 | 0x3f800000u);
                     }
-                    if (!(ok >> g & 1u)) kt[j][0] = -1000;
-                    if (!(ok >> (g + 8) & 1u)) kt[j][1] = -1000;
-                    kmax = max(kmax, max(kt[j][0], kt[j][1]));
-                    if constexpr (BITS == 8) {
-                        // significands; 1 where there is no token
-                        if (c < 2) {
-                            const uint32_t s = c ? r[j].ks[0] >> 16 : r[j].ks[0];
-                            m.ksig[(w * C::UPW + j) * 16 + g + 8 * c] = (c ? kt[j][1] : kt[j][0]) == -1000 ? 1.f : __uint_as_float((s & 0x7fu) << 16 | 0x3f800000u);
-                        }
-                        if (g < 4) {
-                            const uint32_t s = r[j].vs[g >> 1] >> (16 * (g & 1));
-                            const int t = 2 * c + (g & 1) + (g >> 1) * 8;
-                            m.vsig[(w * C::UPW + j) * 16 + t] = ok >> t & 1u ? __uint_as_float((s & 0x7fu) << 16 | 0x3f800000u) : 1.f;
-                        }
+                    if (g < 4) {
+                        const uint32_t s = r.vs[g >> 1] >> (16 * (g & 1));
+                        const int t = 2 * c + (g & 1) + (g >> 1) * 8;
+                        m.vsig[t0 + t] = ok >> t & 1u ? __uint_as_float((s & 0x7fu) << 16 | 0x3f800000u) : 1.f;
                     }
+                }
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        if (!(ok >> (2 * c + (x & 1) + (x >> 1) * 8) & 1u)) vt[j][x] = -1000;
-                        vmax = max(vmax, vt[j][x]);
-                    }
+                for (int x = 0; x < 4; ++x) {
+                    if (!(ok >> (2 * c + (x & 1) + (x >> 1) * 8) & 1u)) vt[x] = -1000;
+                    vmax = max(vmax, vt[x]);
                 }
                 vmax = max(vmax, __shfl_xor_sync(0xffffffffu, vmax, 1));
                 vmax = max(vmax, __shfl_xor_sync(0xffffffffu, vmax, 2));
@@ -428,130 +414,105 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     const int2 y = tmaxs[n_tile & 1][x];
                     kmax = max(kmax, y.x), rv = max(rv, y.y);
                 }
-                uint32_t kfh[C::UPW][2];
-#pragma unroll
-                for (int j = 0; j < C::UPW; ++j)
-                    kfh[j][0] = pow2_h2(kt[j][0] - kmax), kfh[j][1] = pow2_h2(kt[j][1] - kmax);
+                const uint32_t kfh[2] = {pow2_h2(kt[0] - kmax), pow2_h2(kt[1] - kmax)};
                 if (lane == 0) {
-                    uint32_t bits = 0;
-#pragma unroll
-                    for (int j = 0; j < C::UPW; ++j) bits |= (have[j] ? 1u : 0u) << (w * C::UPW + j);
-                    atomicOr(&m.have, bits);
+                    atomicOr(&m.have, (have ? 1u : 0u) << w);
                     if (w == 0) m.rv = rv, m.kf = pow2i(kmax) * (BITS == 4 ? 512.f : 1.f);
                 }
                 // ---- keys
                 unsigned char *kt_ = sk + st * C::KV_BYTES, *vt_ = sv + st * C::KV_BYTES;
-#pragma unroll
-                for (int j = 0; j < C::UPW; ++j) {
-                    const int t0 = (w * C::UPW + j) * 16;
-                    if (!have[j]) {
-                        // nothing listed: the products read zeros
-                        for (int x = lane; x < 16 * (D / 8); x += 32)
-                            *tile_chunk(kt_, N, t0 + x / (D / 8), x % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
-                    } else if constexpr (BITS == 4) {
-                        constexpr int W = D / 32, PERG = D / 64;
-                        if constexpr (D == 128) {
-                            // lanes c and c + 2 meet in the same banks (64 dims apart): the
-                            // latter take their two groups the other way round
-                            r[j].ks[0] = __byte_perm(r[j].ks[0], 0, far ? 0x2301 : 0x3210);
-#pragma unroll
-                            for (int i2 = 0; i2 < 2; ++i2)
-                                if (far) r[j].k[i2] = make_uint4(r[j].k[i2].z, r[j].k[i2].w, r[j].k[i2].x, r[j].k[i2].y);
-                        }
+                if (!have) {
+                    // nothing listed: the products read zeros
+                    for (int x = lane; x < 16 * (D / 8); x += 32)
+                        *tile_chunk(kt_, N, t0 + x / (D / 8), x % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
+                } else if constexpr (BITS == 4) {
+                    constexpr int W = D / 32, PERG = D / 64;
+                    if constexpr (D == 128) {
+                        // lanes c and c + 2 meet in the same banks (64 dims apart): the
+                        // latter take their two groups the other way round
+                        r.ks[0] = __byte_perm(r.ks[0], 0, far ? 0x2301 : 0x3210);
 #pragma unroll
                         for (int i2 = 0; i2 < 2; ++i2)
+                            if (far) r.k[i2] = make_uint4(r.k[i2].z, r.k[i2].w, r.k[i2].x, r.k[i2].y);
+                    }
 #pragma unroll
-                            for (int gr = 0; gr < PERG; ++gr) {
-                                const int b = i2 * PERG + gr;
-                                const uint32_t by = (r[j].ks[b / 4] >> (8 * (b & 3))) & 255u;
-                                const uint32_t s = h2mul(by * 0x00400040u + 0x3c003c00u, kfh[j][i2]);
-                                const uint32_t s4 = h2mul(s, H2_2_4), cc = h2mul(s, H2_M2_21);
+                    for (int i2 = 0; i2 < 2; ++i2)
 #pragma unroll
-                                for (int q = 0; q < 2; ++q) {
-                                    const int x = gr * 2 + q;      // word of the token
-                                    const int at = D == 64 ? i2 * 2 + x : i2 * W + x;
-                                    uint32_t h[4];
-                                    nibbles(word_of(r[j].k[at / 4], at % 4), s, s4, cc, h);
-                                    *tile_chunk(kt_, N, t0 + g + 8 * i2, c * (D / 4) + (x ^ (far ? 2 : 0)) * 8) = make_uint4(h[0], h[1], h[2], h[3]);
-                                }
+                        for (int gr = 0; gr < PERG; ++gr) {
+                            const int b = i2 * PERG + gr;
+                            const uint32_t by = (r.ks[b / 4] >> (8 * (b & 3))) & 255u;
+                            const uint32_t s = h2mul(by * 0x00400040u + 0x3c003c00u, kfh[i2]);
+                            const uint32_t s4 = h2mul(s, H2_2_4), cc = h2mul(s, H2_M2_21);
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                const int x = gr * 2 + q;      // word of the token
+                                const int at = D == 64 ? i2 * 2 + x : i2 * W + x;
+                                uint32_t h[4];
+                                nibbles(word_of(r.k[at / 4], at % 4), s, s4, cc, h);
+                                *tile_chunk(kt_, N, t0 + g + 8 * i2, c * (D / 4) + (x ^ (far ? 2 : 0)) * 8) = make_uint4(h[0], h[1], h[2], h[3]);
                             }
-                    } else {
-                        constexpr int CH = D / 64;
+                        }
+                } else {
+                    constexpr int CH = D / 64;
 #pragma unroll
-                        for (int i2 = 0; i2 < 2; ++i2) {
-                            const uint32_t cc = h2mul(kfh[j][i2], H2_M1152);
+                    for (int i2 = 0; i2 < 2; ++i2) {
+                        const uint32_t cc = h2mul(kfh[i2], H2_M1152);
 #pragma unroll
-                            for (int q = 0; q < CH; ++q) {
-                                uint4 x = r[j].k[i2 * CH + q];
-                                if (D == 128 && far) x = r[j].k[i2 * CH + (q ^ 1)];
-                                const int d = c * (D / 4) + (q ^ (far ? 1 : 0)) * 16;
-                                *tile_chunk(kt_, N, t0 + g + 8 * i2, d) = bytes8(x.x, x.y, kfh[j][i2], cc);
-                                *tile_chunk(kt_, N, t0 + g + 8 * i2, d + 8) = bytes8(x.z, x.w, kfh[j][i2], cc);
-                            }
+                        for (int q = 0; q < CH; ++q) {
+                            uint4 x = r.k[i2 * CH + q];
+                            if (D == 128 && far) x = r.k[i2 * CH + (q ^ 1)];
+                            const int d = c * (D / 4) + (q ^ (far ? 1 : 0)) * 16;
+                            *tile_chunk(kt_, N, t0 + g + 8 * i2, d) = bytes8(x.x, x.y, kfh[i2], cc);
+                            *tile_chunk(kt_, N, t0 + g + 8 * i2, d + 8) = bytes8(x.z, x.w, kfh[i2], cc);
                         }
                     }
                 }
-                int64_t next[C::UPW];
-#pragma unroll
-                for (int j = 0; j < C::UPW; ++j) next[j] = -1;
                 if (i + 1 < n) {
                     places(i + 1);
-#pragma unroll
-                    for (int j = 0; j < C::UPW; ++j) {
-                        next[j] = un[j];
-                        load_keys<BITS, D>(p.cache + next[j] * U::BYTES, next[j] >= 0, r[j]);
-                    }
+                    load_keys<BITS, D>(p.cache + un * U::BYTES, un >= 0, r);
                 }
                 fence_async_smem();
                 mbar_arrive(&kfull[st]);
                 // ---- values
+                if (!have) {
+                    for (int x = lane; x < 16 * (D / 8); x += 32)
+                        *tile_chunk(vt_, N, t0 + x / (D / 8), x % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
+                } else {
 #pragma unroll
-                for (int j = 0; j < C::UPW; ++j) {
-                    const int t0 = (w * C::UPW + j) * 16;
-                    if (!have[j]) {
-                        for (int x = lane; x < 16 * (D / 8); x += 32)
-                            *tile_chunk(vt_, N, t0 + x / (D / 8), x % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
-                    } else {
+                    for (int x = 0; x < 4; ++x) {
+                        const int t = t0 + 2 * c + (x & 1) + (x >> 1) * 8;
+                        const uint32_t f = pow2_h2(vt[x] - rv);
+                        if constexpr (BITS == 4) {
+                            constexpr int W = D / 64, GL = D == 256 ? 2 : 1, WG = W / GL;
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int t = t0 + 2 * c + (x & 1) + (x >> 1) * 8;
-                            const uint32_t f = pow2_h2(vt[j][x] - rv);
-                            if constexpr (BITS == 4) {
-                                constexpr int W = D / 64, GL = D == 256 ? 2 : 1, WG = W / GL;
+                            for (int gl = 0; gl < GL; ++gl) {
+                                const uint32_t by = (r.vs[gl] >> (8 * x)) & 255u;
+                                const uint32_t s = h2mul(by * 0x00400040u + 0x3c003c00u, f);
+                                const uint32_t s4 = h2mul(s, H2_2_4), cc = h2mul(s, H2_M2_21);
 #pragma unroll
-                                for (int gl = 0; gl < GL; ++gl) {
-                                    const uint32_t by = (r[j].vs[gl] >> (8 * x)) & 255u;
-                                    const uint32_t s = h2mul(by * 0x00400040u + 0x3c003c00u, f);
-                                    const uint32_t s4 = h2mul(s, H2_2_4), cc = h2mul(s, H2_M2_21);
-#pragma unroll
-                                    for (int q = 0; q < WG; ++q) {
-                                        const int i3 = gl * WG + q, at = x * W + i3;
-                                        uint32_t h[4], word = word_of(r[j].v[at / 4], at % 4);
-                                        if (D == 128 && odd) word = word_of(r[j].v[at / 4], (at ^ 1) % 4);
-                                        nibbles(word, s, s4, cc, h);
-                                        *tile_chunk(vt_, N, t, g * (D / 8) + (i3 ^ (odd ? 1 : 0)) * 8) = make_uint4(h[0], h[1], h[2], h[3]);
-                                    }
+                                for (int q = 0; q < WG; ++q) {
+                                    const int i3 = gl * WG + q, at = x * W + i3;
+                                    uint32_t h[4], word = word_of(r.v[at / 4], at % 4);
+                                    if (D == 128 && odd) word = word_of(r.v[at / 4], (at ^ 1) % 4);
+                                    nibbles(word, s, s4, cc, h);
+                                    *tile_chunk(vt_, N, t, g * (D / 8) + (i3 ^ (odd ? 1 : 0)) * 8) = make_uint4(h[0], h[1], h[2], h[3]);
                                 }
-                            } else {
-                                constexpr int W = D / 32;          // words of 4 dims
-                                const uint32_t cc = h2mul(f, H2_M1152);
+                            }
+                        } else {
+                            constexpr int W = D / 32;          // words of 4 dims
+                            const uint32_t cc = h2mul(f, H2_M1152);
 #pragma unroll
-                                for (int q = 0; q < W; q += 2) {
-                                    const int at = x * W + q;
-                                    uint32_t w0 = word_of(r[j].v[at / 4], at % 4), w1 = word_of(r[j].v[at / 4], at % 4 + 1);
-                                    if (D == 128 && odd)
-                                        w0 = word_of(r[j].v[at / 4], (at ^ 2) % 4), w1 = word_of(r[j].v[at / 4], (at ^ 2) % 4 + 1);
-                                    *tile_chunk(vt_, N, t, g * (D / 8) + (q ^ (odd ? 2 : 0)) * 4) = bytes8(w0, w1, f, cc);
-                                }
+                            for (int q = 0; q < W; q += 2) {
+                                const int at = x * W + q;
+                                uint32_t w0 = word_of(r.v[at / 4], at % 4), w1 = word_of(r.v[at / 4], at % 4 + 1);
+                                if (D == 128 && odd)
+                                    w0 = word_of(r.v[at / 4], (at ^ 2) % 4), w1 = word_of(r.v[at / 4], (at ^ 2) % 4 + 1);
+                                *tile_chunk(vt_, N, t, g * (D / 8) + (q ^ (odd ? 2 : 0)) * 4) = bytes8(w0, w1, f, cc);
                             }
                         }
                     }
                 }
-                if (i + 1 < n) {
-#pragma unroll
-                    for (int j = 0; j < C::UPW; ++j)
-                        load_values<BITS, D>(p.cache + next[j] * U::BYTES, next[j] >= 0, r[j]);
-                }
+                if (i + 1 < n) load_values<BITS, D>(p.cache + un * U::BYTES, un >= 0, r);
                 fence_async_smem();
                 mbar_arrive(&vfull[st]);
             }

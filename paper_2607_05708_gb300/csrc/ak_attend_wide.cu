@@ -16,9 +16,10 @@
 //   softmax warps       a thread a row, 64 scores at a time: maximum, weights and total
 //       need no shuffle.  P (fp16) replaces its scores.  The maximum is raised,
 //       and O rescaled, only when a weight would exceed 2^14.
-// Keys are v 2^-9 relative to their tile's largest exponent (its power of two is
-// a factor of the scores), values relative to the item's largest so far: where
-// fp16's normal range ends they are rounded to 2^-17 of that largest.
+// Keys are staged without their row's power of two, as v 2^-9 / 2^T (8 bits: as codes): that factor is
+// the softmax's, in fp32, so that a score depends on its own key alone.  Where fp16's normal range
+// ends they are rounded to 2^-17 of their row's largest.  Values are relative to the item's
+// largest so far.
 // Measured (4 bits): two requests of 2048 rows behind 10240 tokens, 32 heads on 8, D = 128 (514
 // GFLOP) 682 us, 0.75 PFLOP/s, and 905 us with capped scores; a step of 256 rows and 128
 // tokens 2.8 us, of which the products are 1.06: scores, softmax and O += P V of a row tile
@@ -44,20 +45,17 @@ struct Wide {
     static constexpr int SN = MT == 2 ? N : HT;          // columns of S computed at once
     // Warps: softmax, dequantising, one that issues.  At D <= 128 the registers of five
     // warpgroups are split by need, so that a unit of a tile has a warp of its own.
-    // For softmax, dequantising, the last one, a thread; together the 96 of the launch.  Two
-    // requests of 2048 rows and 10240 tokens, 8 key/value heads, D = 128, us:
-    //   4 bits  685 with 120, 80, 80; 695 with 128, 88, 48 and with 144, 72, 48
-    //   8 bits  839 with 144, 72, 48; 976 with 128, 88, 48; 1042 with 120, 80, 80 (two
-    //           factors a token more in the softmax)
-    template <int BITS>
-    static constexpr int regs(int role) {
-        return BITS == 4 ? (role == 0 ? 120 : 80) : role == 0 ? 144 : role == 1 ? 72 : 48;
-    }
+    // For softmax, dequantising, the last one, a thread; together the 96 of the launch.  Requests
+    // of 2048 and 1600 rows behind 10240 and 8000 tokens, 32 heads on 8, D = 128, us:
+    //                    120, 80, 80   144, 72, 48   152, 64, 48   160, 56, 48   168, 48, 48
+    //   4 bits                   820           725           720           724           773
+    //   4 bits, capped          1165          1127           924           949          1031
+    //   8 bits                   976           809           806           888           947
+    static constexpr int regs(int role) { return role == 0 ? 152 : role == 1 ? 64 : 48; }
     static constexpr bool SPLIT = MT == 2;
     static constexpr int SOFT = 4 * MT, DEQ = SPLIT ? 8 : 4;
     static constexpr int THREADS = 32 * (SOFT + DEQ + (SPLIT ? 4 : 1));
-    static_assert(!SPLIT || (256 * (regs<4>(0) + regs<4>(1)) + 128 * regs<4>(2) <= THREADS * 96 &&
-                             256 * (regs<8>(0) + regs<8>(1)) + 128 * regs<8>(2) <= THREADS * 96), "registers");
+    static_assert(!SPLIT || 256 * (regs(0) + regs(1)) + 128 * regs(2) <= THREADS * 96, "registers");
     static_assert(UNITS == DEQ, "a dequantising warp has one unit of every tile");
     static constexpr int STAGES = 2;
     // An item's beginning and end (query rows in, result out, an empty pipeline: 7 to 10 us; a step
@@ -74,13 +72,21 @@ struct Wide {
 // What the consumers of a tile need beside the operands.
 template <int N>
 struct alignas(16) Meta {           // pairs of its floats are read at once
-    float ksig[N], vsig[N];         // 8 bits: significands of the tokens' scales
+    float ksig[N];                  // the keys' scales (kv_key_factor), 1 where there is no token
+    float vsig[N];                  // 8 bits: significands of the values' scales
     int tag[N];
-    // read at once: factor of the scores, first token, exponent of the values, units listed
-    alignas(16) float kf;
-    int tok, rv;
-    uint32_t have;
+    // read at once: first token, exponent of the values, units listed
+    alignas(16) int tok;
+    int rv;
+    uint32_t have, pad;
 };
+// Factors of the scores: of the key, its row's power of two or bf16 scale, times 2^-12, so that times a
+// product of any size it stays in fp32's range (a stored infinity has T = 125), and of
+// the row, the rest: 2^12, and 2^9 of the staged keys.
+constexpr float ROW_FACTOR_4 = 2097152.f, ROW_FACTOR_8 = 4096.f;
+__device__ __forceinline__ float kv_key_factor(uint32_t scale) {   // as fp32 bits
+    return __uint_as_float(scale - (12u << 23));
+}
 static_assert(offsetof(Meta<64>, ksig) % 8 == 0 && offsetof(Meta<64>, vsig) % 8 == 0 &&
                   offsetof(Meta<128>, ksig) % 8 == 0 && offsetof(Meta<128>, vsig) % 8 == 0 &&
                   offsetof(Meta<64>, tag) % 16 == 0 && offsetof(Meta<128>, tag) % 16 == 0,
@@ -222,6 +228,12 @@ __device__ __forceinline__ uint4 bytes8(uint32_t w0, uint32_t w1, uint32_t f, ui
                       h2fma(__byte_perm(w1, 0x64646464u, 0x4140), f, c),
                       h2fma(__byte_perm(w1, 0x64646464u, 0x4342), f, c));
 }
+__device__ __forceinline__ uint4 codes8(uint32_t w0, uint32_t w1) {
+    return make_uint4(h2add(__byte_perm(w0, 0x64646464u, 0x4140), H2_M1152),
+                      h2add(__byte_perm(w0, 0x64646464u, 0x4342), H2_M1152),
+                      h2add(__byte_perm(w1, 0x64646464u, 0x4140), H2_M1152),
+                      h2add(__byte_perm(w1, 0x64646464u, 0x4342), H2_M1152));
+}
 __device__ __forceinline__ uint32_t word_of(const uint4 &x, int i) {
     return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
 }
@@ -262,7 +274,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
     __shared__ Meta<N> meta[ST];
     __shared__ uint64_t kfull[ST], vfull[ST], empty[ST];      // tiles: keys, values, both read
     __shared__ uint64_t sfull[MT][2], pfull[MT][2], odone[MT][2], qfull[MT], drained, texch;
-    __shared__ int2 tmaxs[2][C::DEQ];          // largest exponents of a warp's keys and values
+    __shared__ int tmaxs[2][C::DEQ];           // largest exponents of a warp's values
     __shared__ float qscale[ROWS];
     __shared__ uint32_t tmem_slot;
     __shared__ int dead_word;
@@ -313,7 +325,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
 
     if (warp >= C::SOFT && warp < C::SOFT + C::DEQ) {
         // ---------------- dequantising
-        if constexpr (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::template regs<BITS>(1)));
+        if constexpr (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::regs(1)));
         const int w = warp - C::SOFT, g = lane >> 2, c = lane & 3;
         const bool far = D == 128 && c >= 2, odd = D == 128 && (g & 1);    // (shared memory banks)
         uint32_t n_tile = 0;                   // tiles since the kernel began
@@ -367,27 +379,19 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     if (lane < 16) m.tag[lt] = max(tag_next, -1);
                 }
                 const uint32_t ok = __ballot_sync(0xffffffffu, mine);      // the unit's valid tokens
-                // exponents: keys relative to the tile's largest, values to the item's
-                int kt[2], vt[4], kmax = -126, vmax = -127;
+                if (c < 2) {
+                    const uint32_t s = BITS == 4 ? (r.ke >> (8 * c) & 255u) << 23 : (c ? r.ks[0] & 0xffff0000u : r.ks[0] << 16);
+                    m.ksig[t0 + g + 8 * c] = ok >> (g + 8 * c) & 1u ? kv_key_factor(s) : 1.f;
+                }
+                // exponents of the values, relative to the item's largest
+                int vt[4], vmax = -127;
                 if constexpr (BITS == 4) {
-                    kt[0] = (int)(r.ke & 255u) - 127, kt[1] = (int)(r.ke >> 8 & 255u) - 127;
 #pragma unroll
                     for (int x = 0; x < 4; ++x) vt[x] = (int)(r.ve >> (8 * x) & 255u) - 127;
                 } else {
-                    kt[0] = (int)(r.ks[0] >> 7 & 255u) - 127, kt[1] = (int)(r.ks[0] >> 23 & 255u) - 127;
 #pragma unroll
                     for (int x = 0; x < 4; ++x) vt[x] = (int)(r.vs[x >> 1] >> (7 + 16 * (x & 1)) & 255u) - 127;
-                }
-                if (!(ok >> g & 1u)) kt[0] = -1000;
-                if (!(ok >> (g + 8) & 1u)) kt[1] = -1000;
-                kmax = max(kmax, max(kt[0], kt[1]));
-                if constexpr (BITS == 8) {
-                    // significands; 1 where there is no token
-                    if (c < 2) {
-                        const uint32_t s = c ? r.ks[0] >> 16 : r.ks[0];
-                        m.ksig[t0 + g + 8 * c] = (c ? kt[1] : kt[0]) == -1000 ? 1.f : __uint_as_float((s & 0x7fu) << 16 | 0x3f800000u);
-                    }
-                    if (g < 4) {
+                    if (g < 4) {               // significands; 1 where there is no token
                         const uint32_t s = r.vs[g >> 1] >> (16 * (g & 1));
                         const int t = 2 * c + (g & 1) + (g >> 1) * 8;
                         m.vsig[t0 + t] = ok >> t & 1u ? __uint_as_float((s & 0x7fu) << 16 | 0x3f800000u) : 1.f;
@@ -400,24 +404,17 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 }
                 vmax = max(vmax, __shfl_xor_sync(0xffffffffu, vmax, 1));
                 vmax = max(vmax, __shfl_xor_sync(0xffffffffu, vmax, 2));
-                kmax = max(kmax, __shfl_xor_sync(0xffffffffu, kmax, 4));
-                kmax = max(kmax, __shfl_xor_sync(0xffffffffu, kmax, 8));
-                kmax = max(kmax, __shfl_xor_sync(0xffffffffu, kmax, 16));
                 if (lane == 0) {
-                    tmaxs[n_tile & 1][w] = make_int2(kmax, vmax);
+                    tmaxs[n_tile & 1][w] = vmax;
                     if (w == 0) m.tok = tok, m.have = 0;
                     mbar_arrive(&texch);
                 }
                 if (!wide_wait(&texch, n_tile & 1, dead, p.status)) break;
 #pragma unroll
-                for (int x = 0; x < C::DEQ; ++x) {
-                    const int2 y = tmaxs[n_tile & 1][x];
-                    kmax = max(kmax, y.x), rv = max(rv, y.y);
-                }
-                const uint32_t kfh[2] = {pow2_h2(kt[0] - kmax), pow2_h2(kt[1] - kmax)};
+                for (int x = 0; x < C::DEQ; ++x) rv = max(rv, tmaxs[n_tile & 1][x]);
                 if (lane == 0) {
                     atomicOr(&m.have, (have ? 1u : 0u) << w);
-                    if (w == 0) m.rv = rv, m.kf = pow2i(kmax) * (BITS == 4 ? 512.f : 1.f);
+                    if (w == 0) m.rv = rv;
                 }
                 // ---- keys
                 unsigned char *kt_ = sk + st * C::KV_BYTES, *vt_ = sv + st * C::KV_BYTES;
@@ -441,8 +438,8 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         for (int gr = 0; gr < PERG; ++gr) {
                             const int b = i2 * PERG + gr;
                             const uint32_t by = (r.ks[b / 4] >> (8 * (b & 3))) & 255u;
-                            const uint32_t s = h2mul(by * 0x00400040u + 0x3c003c00u, kfh[i2]);
-                            const uint32_t s4 = h2mul(s, H2_2_4), cc = h2mul(s, H2_M2_21);
+                            const uint32_t s = by * 0x00400040u + 0x3c003c00u;
+                            const uint32_t s4 = s - 0x10001000u, cc = h2mul(s, H2_M2_21);
 #pragma unroll
                             for (int q = 0; q < 2; ++q) {
                                 const int x = gr * 2 + q;      // word of the token
@@ -455,17 +452,15 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 } else {
                     constexpr int CH = D / 64;
 #pragma unroll
-                    for (int i2 = 0; i2 < 2; ++i2) {
-                        const uint32_t cc = h2mul(kfh[i2], H2_M1152);
+                    for (int i2 = 0; i2 < 2; ++i2)
 #pragma unroll
                         for (int q = 0; q < CH; ++q) {
                             uint4 x = r.k[i2 * CH + q];
                             if (D == 128 && far) x = r.k[i2 * CH + (q ^ 1)];
                             const int d = c * (D / 4) + (q ^ (far ? 1 : 0)) * 16;
-                            *tile_chunk(kt_, N, t0 + g + 8 * i2, d) = bytes8(x.x, x.y, kfh[i2], cc);
-                            *tile_chunk(kt_, N, t0 + g + 8 * i2, d + 8) = bytes8(x.z, x.w, kfh[i2], cc);
+                            *tile_chunk(kt_, N, t0 + g + 8 * i2, d) = codes8(x.x, x.y);
+                            *tile_chunk(kt_, N, t0 + g + 8 * i2, d + 8) = codes8(x.z, x.w);
                         }
-                    }
                 }
                 if (i + 1 < n) {
                     places(i + 1);
@@ -521,7 +516,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
         }
     } else if (warp >= C::SOFT + C::DEQ) {
         // ---------------- issuing
-        if constexpr (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::template regs<BITS>(2)));
+        if constexpr (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::regs(2)));
         if (warp == C::SOFT + C::DEQ) {
             constexpr uint32_t id_s = idesc_f16(C::SN), id_o = idesc_f16(D) | IDESC_B_MN_MAJOR;
             const uint32_t go = lane == 0;
@@ -621,7 +616,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
         __syncwarp();
     } else {
         // ---------------- softmax: a lane is row 32 (warp % 4) + lane of row tile t
-        if constexpr (C::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::template regs<BITS>(0)));
+        if constexpr (C::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::regs(0)));
         const int t = warp >> 2, rt = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t o_at = tmem + lanes + t * D;
@@ -691,7 +686,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 const bool real = r < rows;
                 const int i = real ? (row_first + r) / p.group : 0;
                 const int hd = cur.head * p.group + (real ? row_first + r - i * p.group : 0);
-                const float qf = qscale[r] * p.scale * LOG2E_F;
+                const float qf = qscale[r] * p.scale * LOG2E_F * (BITS == 4 ? ROW_FACTOR_4 : ROW_FACTOR_8);
                 const int limit = real ? attend_limit(p, sq, i) : sq.kv, pos = sq.kv - sq.nq + i;
                 const float slope = real && p.slopes ? p.slopes[hd] * LOG2E_F : 0.f;
                 // a slot without a token has tag -1 here, and a row that sees none -2
@@ -701,7 +696,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 float mm = 0.f, l = 0.f;
                 bool unset = real;             // no key seen yet: mm = 0
                 int rv = -127;
-                uint4 about = make_uint4(0, 0, 0, 0);      // the tile's Meta from kf on
+                uint4 about = make_uint4(0, 0, 0, 0);      // the tile's Meta from tok on
                 for (int h = 0; h < n * HPT; ++h, ++halves) {
                     const uint32_t x_tile = n_tile + h / HPT, st = x_tile % ST, b = halves & 1;
                     const uint32_t s_at = tmem + lanes + C::S_COL + (t * 2 + b) * HT;
@@ -709,7 +704,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         // what the dequantising warps wrote beside the tile, while its scores
                         // are computed
                         ok = wide_wait(&kfull[st], (x_tile / ST) & 1, dead, p.status);
-                        about = *(const uint4 *)&meta[st].kf;
+                        about = *(const uint4 *)&meta[st].tok;
                         if (ok) ok = wide_wait(&sfull[t][b], halves >> 1 & 1, dead, p.status);
                         ok = __all_sync(0xffffffffu, ok);
                         if (!ok) break;
@@ -719,9 +714,9 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     tmem_ld32(s_at, *(uint32_t(*)[32])x);
                     tmem_ld32(s_at + 32, *(uint32_t(*)[32])(x + 32));
                     const Meta<N> &m = meta[st];
-                    const int half = h % HPT * HT, tok = (int)about.y + half, rv_new = (int)about.z;
-                    const uint32_t have = about.w >> (half / KV_UNIT) & 15u;
-                    float f = qf * __uint_as_float(about.x);   // of the scores, log2 units
+                    const int half = h % HPT * HT, tok = (int)about.x + half, rv_new = (int)about.y;
+                    const uint32_t have = about.z >> (half / KV_UNIT) & 15u;
+                    float f = qf;              // of the scores, log2 units
                     const bool masked = tags || tok > safe || have != 15u;
                     tmem_ld_wait();
                     auto pair = [&](int k) { return f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])); };
@@ -729,9 +724,8 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         const float2 y = f2_open(v);
                         x[k] = __float_as_uint(y.x), x[k + 1] = __float_as_uint(y.y);
                     };
-                    if constexpr (BITS == 8)
 #pragma unroll
-                        for (int k = 0; k < HT; k += 2) put(k, f2_mul(pair(k), *(const uint64_t *)&m.ksig[half + k]));
+                    for (int k = 0; k < HT; k += 2) put(k, f2_mul(pair(k), *(const uint64_t *)&m.ksig[half + k]));
                     if (heavy || masked) {
                         // in place, from here on the factor is 1
 #pragma unroll

@@ -14,15 +14,15 @@
 //  * a nibble n in the low bits of a half is the subnormal n 2^-24; one fused
 //    multiply-add by e 2^15 and -8 e 2^-9 gives (n - 8) e 2^-9: one instruction
 //    for two values.  Where that is below fp16's normal range it is rounded to
-//    its steps of 2^-24, 2^-17 of the row's largest.  The row's 2^T goes to the
-//    score; for values into the group's scale, relative to the largest T so far,
-//    and 2^-10: rounded to 2^-16 of the largest value so far.
+//    its steps of 2^-24, 2^-17 of the row's largest.  A key's 2^T goes to its
+//    score, a value's to its weight, in fp32: a row's result depends on what it sees
+//    alone.
 //  * a warp has its own share of all units (16 tokens), brought by bulk copies
 //    into its own ring across the items' ends, with its own running maximum, sum and
 //    accumulators: no barrier in the loop.  Where a share begins or ends inside an
 //    item, the parts are added up after it, first within the CTA.
-//  * P is fp16, 2^6 p: weights down to 2^-20 of the largest so far keep 11 bits; sums,
-//    maxima and accumulators are fp32.  The maximum is raised only when a
+//  * P is fp16, p 2^T in units of a power of two (R_SHIFT): those down to 2^-16 of the largest
+//    so far keep 11 bits; sums, maxima and accumulators are fp32.  The maximum is raised only when a
 //    score exceeds it by 2^8, so that the accumulators are rarely rescaled.
 // Measured (one query row of 32 heads a sequence, 8 key/value heads, D = 128, 4 bits): 64
 // sequences of 4096, 8192 and 16384 tokens 77, 130 and 237 us, so 5.7 TB/s (84 % of a
@@ -69,7 +69,7 @@ struct Narrow {
     static constexpr int UPS = D <= 128 ? 2 : 1, STEP = UPS * KV_UNIT;
     static constexpr int STAGE = UPS * (U::BYTES + 64);  // a step's units, then their tags
     static constexpr int ACC = ROWS * D * 4;             // a warp's accumulators
-    static constexpr int SMALL = NW * ROWS * 4 * 4 + 2 * NW * ROWS * 8 + 2 * NW * 48 + NW * 64 + 64;
+    static constexpr int SMALL = NW * ROWS * 4 * 4 + 2 * NW * ROWS * 12 + 2 * NW * 48 + NW * 64 + 64;
     static_assert(NW * ACC >= (NW * 32 + 1) * 8, "the plan's sums lie where parts come later");
     static constexpr int WANT = (225 * 512 - NW * ACC - SMALL) / (NW * (STAGE + 16));
     static constexpr int MOST = (225 * 1024 - NW * ACC - SMALL) / (NW * (STAGE + 16));
@@ -92,9 +92,13 @@ struct Fetch {
 // A warp's part of an item, left for the joining of the CTA's warps.
 struct Entry {
     int64_t start;                             // of the item, in all steps
-    int seq, head, tile, unit, n, units, tref;
+    int seq, head, tile, unit, n, units;
 };
 static_assert(sizeof(Entry) <= 48 && sizeof(Fetch) <= 64, "Narrow::SMALL");
+
+__device__ __forceinline__ int r_of(float rf) {  // R of 2^-R
+    return 127 - (int)(__float_as_uint(rf) >> 23);
+}
 
 // A lane's part of the B fragments of a tile's query rows: row g of each 8, dims
 // c D/4 + 4 kk + {0..3}.  bf16 rows are scaled by a power of two to a largest
@@ -147,7 +151,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
     using C = Narrow<BITS, D, NB>;
     using U = typename C::U;
     constexpr int ROWS = C::ROWS, NS = C::NS, MT = D / 16, UPS = C::UPS, STEP = C::STEP;
-    constexpr int UP = BITS == 4 ? 10 : 0;     // values are staged as v 2^-10
+    constexpr int UP = BITS == 4 ? 9 : 0;      // values are staged as v 2^-9 / 2^T
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, c = lane & 3;
@@ -160,6 +164,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
     unsigned char *listed = at + warp * NS * 2;           at += NW * NS * 4;
     float *em = (float *)at;                              at += 2 * NW * ROWS * 4;   // of entries
     float *el = (float *)at;                              at += 2 * NW * ROWS * 4;
+    float *er = (float *)at;                              at += 2 * NW * ROWS * 4;
     float *slope = (float *)at + warp * ROWS;             at += NW * ROWS * 4;       // of rows
     int *limit = (int *)at + warp * ROWS;                 at += NW * ROWS * 4;
     int *pos = (int *)at + warp * ROWS;                   at += NW * ROWS * 4;
@@ -278,7 +283,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
     uint32_t stage = 0, phase = 0;
     const float cap_l = p.cap * LOG2E_F;
     float o[NB][MT][4], mm[NB][2], l[NB][2];
-    int tref = -127;
+    float rf[NB][2], rf_most;                  // 2^-R of the rows, the lane's largest
     int64_t done = 0;
     bool tail = false;                         // the accumulators hold the last item's part
     while (left > 0) {
@@ -315,13 +320,13 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                            (BITS == 4 ? 512.f : 1.f);
         const int safe = limit[0] - STEP;   // keys below limit[0] are seen by every row
 
-        tref = -127;
         uint32_t unset = (1u << (2 * NB)) - 1u;    // rows that have not seen a key yet: mm = 0
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
             for (int t = 0; t < MT; ++t) o[b][t][0] = o[b][t][1] = o[b][t][2] = o[b][t][3] = 0.f;
             mm[b][0] = mm[b][1] = 0.f, l[b][0] = l[b][1] = 0.f;
+            rf[b][0] = rf[b][1] = rf_most = pow2i(-R_MIN);
         }
 
         int tok = cur.unit * STEP;
@@ -457,8 +462,27 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                         most = fmaxf(fmaxf(most, s[j][b][0]), fmaxf(fmaxf(s[j][b][1], s[j][b][2]), s[j][b][3]));
                     }
                 }
-                // ---- running maxima
-                if (__any_sync(0xffffffffu, unset || most > P_SHIFT + M_SLACK)) {
+                // ---- the values' scales, of tokens g and g + 8
+                float v[UPS][2], vmax = 0.f;
+#pragma unroll
+                for (int j = 0; j < UPS; ++j) {
+                    const unsigned char *un = st + j * U::BYTES;
+                    if constexpr (BITS == 4) {
+                        v[j][0] = __uint_as_float((uint32_t)un[U::V_EXP + (g >> 1) * 4 + (g & 1)] << 23);
+                        v[j][1] = __uint_as_float((uint32_t)un[U::V_EXP + (g >> 1) * 4 + 2 + (g & 1)] << 23);
+                    } else {
+                        const uint16_t *vs = (const uint16_t *)(un + U::V_SCALES) + (g >> 1) * 4 + (g & 1);
+                        v[j][0] = __uint_as_float((uint32_t)vs[0] << 16), v[j][1] = __uint_as_float((uint32_t)vs[2] << 16);
+                    }
+                    // where no token was written there may be any bits: times a weight of 0
+                    if (masked) v[j][0] = fminf(fabsf(v[j][0]), 1e38f), v[j][1] = fminf(fabsf(v[j][1]), 1e38f);
+                    vmax = fmaxf(vmax, fmaxf(v[j][0], v[j][1]));
+                }
+                // ---- running maxima, and R.  Whether there is something to raise, a bound says that
+                // takes in all of the lane's tokens and rows; by how much, a row's own.
+                if (__any_sync(0xffffffffu, unset || most > P_SHIFT + M_SLACK ||
+                                                ex2(most) * (vmax * rf_most) > (float)(1 << R_SLACK))) {
+                    rf_most = 0.f;
 #pragma unroll
                     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -470,102 +494,57 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
                             x -= P_SHIFT;                      // the maximum's rise
                             const bool fresh = unset >> (2 * b + r) & 1u;
-                            if (fresh ? x > -INFINITY : x > 0.f) {
-                                const float f = fresh ? 0.f : ex2(-x);
+                            const bool rise = fresh ? x > -INFINITY : x > M_SLACK;
+                            const int rr = r_of(rf[b][r]);
+                            int rn = rr;
+                            float o_down = 0.f;                // log2
+                            if (rise) {                        // R falls by as much: O keeps its scale
                                 unset &= ~(1u << (2 * b + r));
                                 mm[b][r] += x;
 #pragma unroll
                                 for (int j = 0; j < UPS; ++j) s[j][b][r] -= x, s[j][b][r + 2] -= x;
-                                l[b][r] *= f;
-#pragma unroll
-                                for (int t = 0; t < MT; ++t) o[b][t][r] *= f, o[b][t][r + 2] *= f;
+                                l[b][r] *= fresh ? 0.f : ex2(-x);
+                                rn = fresh ? R_MIN : max(R_MIN, rr - (int)fminf(ceilf(x), 300.f));
+                                if (!fresh) o_down = -x;       // (a fresh row's O is 0)
                             }
+                            float y = -INFINITY;               // the largest weight times its value's 2^T, log2
+#pragma unroll
+                            for (int j = 0; j < UPS; ++j)
+#pragma unroll
+                                for (int i = 0; i < 2; ++i)
+                                    y = fmaxf(y, s[j][b][r + 2 * i] + (float)((int)(__float_as_uint(v[j][i]) >> 23) - 127));
+                            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 4));
+                            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
+                            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));
+                            if (y > (float)(rn + R_SLACK)) rn = min(R_MAX, (int)ceilf(y) - R_SHIFT);
+                            if (rise || rn != rr) {
+                                const float2 f = ex2_wide(o_down + (float)(rr - rn));
+                                rf[b][r] = pow2i(-rn);
+#pragma unroll
+                                for (int t = 0; t < MT; ++t)
+                                    o[b][t][r] = o[b][t][r] * f.x * f.y, o[b][t][r + 2] = o[b][t][r + 2] * f.x * f.y;
+                            }
+                            rf_most = fmaxf(rf_most, rf[b][r]);
                         }
                 }
-                // ---- weights, and P^T as the B operand
+                // ---- weights times their values' scales, and P^T as the B operand
                 uint32_t pb[UPS][NB][2];
 #pragma unroll
-                for (int j = 0; j < UPS; ++j) {
-                    float vf0 = 1.f, vf1 = 1.f;    // 8 bits: the significands of the values' scales
-                    if constexpr (BITS == 8) {
-                        const uint16_t *vs = (const uint16_t *)(st + j * U::BYTES + U::V_SCALES);
-                        vf0 = __uint_as_float(((uint32_t)(vs[U::v_row(0) + (g >> 1) * 4 + (g & 1)] & 0x7fu) << 16) | 0x3f800000u);
-                        vf1 = __uint_as_float(((uint32_t)(vs[U::v_row(8) + (g >> 1) * 4 + (g & 1)] & 0x7fu) << 16) | 0x3f800000u);
-                    }
+                for (int j = 0; j < UPS; ++j)
 #pragma unroll
                     for (int b = 0; b < NB; ++b) {
                         float (&z)[4] = s[j][b];
 #pragma unroll
                         for (int r = 0; r < 4; ++r) z[r] = ex2(z[r]);
                         l[b][0] += z[0] + z[2], l[b][1] += z[1] + z[3];
-                        if constexpr (BITS == 8) z[0] *= vf0, z[1] *= vf0, z[2] *= vf1, z[3] *= vf1;
-                        pb[j][b][0] = transpose8(pack_h2(z[0], z[1]));
-                        pb[j][b][1] = transpose8(pack_h2(z[2], z[3]));
+                        pb[j][b][0] = transpose8(pack_h2(z[0] * rf[b][0] * v[j][0], z[1] * rf[b][1] * v[j][0]));
+                        pb[j][b][1] = transpose8(pack_h2(z[2] * rf[b][0] * v[j][1], z[3] * rf[b][1] * v[j][1]));
                     }
-                }
-                // ---- the values' exponents relative to tref, as fp16 powers of two: of
-                // tokens 2c and 2c + 1 of each unit in f[j][0], 2c + 8 and 2c + 9 in f[j][1].
-                // In the common case all lie in [tref - 14, tref + 1] and are put together
-                // in place.
-                uint32_t te[UPS][2], f[UPS][2], wide = 0;      // te: T + 127, two to a word
-                const uint32_t low = (uint32_t)(tref + 127 - 14) * 0x00010001u;
-#pragma unroll
-                for (int j = 0; j < UPS; ++j) {
-                    const unsigned char *un = st + j * U::BYTES;
-                    if constexpr (BITS == 4) {
-                        const uint32_t x = *(const uint32_t *)(un + U::V_EXP + c * 4);
-                        te[j][0] = __byte_perm(x, 0, 0x4140), te[j][1] = __byte_perm(x, 0, 0x4342);
-                    } else {
-                        const uint2 x = *(const uint2 *)(un + U::V_SCALES + c * 8);
-                        te[j][0] = (x.x >> 7) & 0x00ff00ffu, te[j][1] = (x.y >> 7) & 0x00ff00ffu;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const uint32_t d = te[j][i] - low;
-                        f[j][i] = (d << 10) + 0x04000400u;
-                        wide |= d;
-                    }
-                }
-                if (masked || __any_sync(0xffffffffu, wide & 0xfff0fff0u)) {
-                    int ti[UPS][4], x = -1000;
-#pragma unroll
-                    for (int j = 0; j < UPS; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            ti[j][i] = (int)(te[j][i >> 1] >> (16 * (i & 1)) & 0xffffu) - 127;
-                            if (masked) {          // a slot without a token adds nothing
-                                const int t = j * 16 + 2 * c + (i & 1) + (i >> 1) * 8;
-                                const uint32_t state = have >> (8 * j) & 3u;
-                                if (!state || tok + t >= sq.kv || (state == 1 && tg[t] < 0)) ti[j][i] = -1000;
-                            }
-                            x = max(x, ti[j][i]);
-                        }
-                    if (__any_sync(0xffffffffu, x > tref + 1)) {
-                        x = max(x, __shfl_xor_sync(0xffffffffu, x, 1));
-                        x = max(max(x, __shfl_xor_sync(0xffffffffu, x, 2)), tref);
-                        const float down = pow2i(max(-126, tref - x));
-                        tref = x;
-#pragma unroll
-                        for (int b = 0; b < NB; ++b)
-#pragma unroll
-                            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                                for (int r = 0; r < 4; ++r) o[b][t][r] *= down;
-                    }
-#pragma unroll
-                    for (int j = 0; j < UPS; ++j)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int a = ti[j][2 * i] - tref, b = ti[j][2 * i + 1] - tref;
-                            f[j][i] = pack_h2(a < -40 ? 0.f : pow2i(a), b < -40 ? 0.f : pow2i(b));
-                        }
-                }
 
                 // ---- O^T += V^T P^T
 #pragma unroll
                 for (int j = 0; j < UPS; ++j) {
                 const unsigned char *un = st + j * U::BYTES;
-                const uint32_t f0 = f[j][0], f1 = f[j][1];
                 auto values = [&](int mt, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
                     for (int b = 0; b < NB; ++b) mma16(o[b][mt], a0, a1, a2, a3, pb[j][b][0], pb[j][b][1]);
@@ -594,9 +573,9 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                     for (int gl = 0; gl < GL; ++gl) {
                         const int gr = D == 64 ? g >> 1 : g * GL + gl;
                         const uint32_t x = *(const uint32_t *)(un + U::V_SCALES + (gr * 4 + c) * 4);
-                        const uint32_t s0 = h2mul(__byte_perm(x, 0, 0x4140) * 64u + 0x38003800u, f0);
-                        const uint32_t s1 = h2mul(__byte_perm(x, 0, 0x4342) * 64u + 0x38003800u, f1);
-                        const uint32_t s04 = h2mul(s0, H2_2_4), s14 = h2mul(s1, H2_2_4);
+                        const uint32_t s0 = __byte_perm(x, 0, 0x4140) * 64u + 0x3c003c00u;
+                        const uint32_t s1 = __byte_perm(x, 0, 0x4342) * 64u + 0x3c003c00u;
+                        const uint32_t s04 = s0 - 0x10001000u, s14 = s1 - 0x10001000u;
                         const uint32_t c0 = h2mul(s0, H2_M2_21), c1 = h2mul(s1, H2_M2_21);
                         constexpr int WG = W / GL;             // words of a group
 #pragma unroll
@@ -629,7 +608,6 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                                 w[i][q * 4] = x.x, w[i][q * 4 + 1] = x.y, w[i][q * 4 + 2] = x.z, w[i][q * 4 + 3] = x.w;
                             }
                     }
-                    const uint32_t c0 = h2mul(f0, H2_M1152), c1 = h2mul(f1, H2_M1152);
 #pragma unroll
                     for (int i = 0; i < W; ++i)
 #pragma unroll
@@ -638,10 +616,10 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                             const uint32_t x = __byte_perm(w[0][i], w[1][i], sel);
                             const uint32_t y = __byte_perm(w[2][i], w[3][i], sel);
                             values(i * 2 + half,
-                                   h2fma(__byte_perm(x, 0x64646464u, 0x4140), f0, c0),
-                                   h2fma(__byte_perm(x, 0x64646464u, 0x4342), f0, c0),
-                                   h2fma(__byte_perm(y, 0x64646464u, 0x4140), f1, c1),
-                                   h2fma(__byte_perm(y, 0x64646464u, 0x4342), f1, c1));
+                                   h2add(__byte_perm(x, 0x64646464u, 0x4140), H2_M1152),
+                                   h2add(__byte_perm(x, 0x64646464u, 0x4342), H2_M1152),
+                                   h2add(__byte_perm(y, 0x64646464u, 0x4140), H2_M1152),
+                                   h2add(__byte_perm(y, 0x64646464u, 0x4342), H2_M1152));
                         }
                 }
                 }
@@ -672,7 +650,8 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                     const int i = row / p.group;
                     const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + cur.head * p.group + (row - i * p.group);
                     const float inv = l[b][r] > 0.f ? 1.f / l[b][r] : l[b][r];   // a NaN stays one
-                    const float up = scale2(1.f, (tref + UP) / 2), up2 = scale2(1.f, (tref + UP) - (tref + UP) / 2);
+                    const int e = r_of(rf[b][r]) + UP;
+                    const float up = pow2i(e / 2), up2 = pow2i(e - e / 2);
 #pragma unroll
                     for (int t = 0; t < MT; ++t)
                         store_pair(p, bf16, dst * D + g * (D / 8) + 2 * t, o[b][t][r] * inv * up * up2,
@@ -685,12 +664,15 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
             tail = done != 0;
             const int e = 2 * warp + (tail ? 1 : 0);
             if (lane == 0)
-                entries[e] = Entry{first + done - cur.unit, cur.seq, cur.head, cur.tile, cur.unit, n, cur.units, tref};
+                entries[e] = Entry{first + done - cur.unit, cur.seq, cur.head, cur.tile, cur.unit, n, cur.units};
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    if (g == 0) em[e * ROWS + b * 8 + 2 * c + r] = mm[b][r], el[e * ROWS + b * 8 + 2 * c + r] = l[b][r];
+                    if (g == 0) {
+                        const int x = e * ROWS + b * 8 + 2 * c + r;
+                        em[x] = mm[b][r], el[x] = l[b][r], er[x] = (float)r_of(rf[b][r]);
+                    }
                     if (!tail)
 #pragma unroll
                         for (int t = 0; t < MT; ++t)
@@ -721,12 +703,12 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
             ++e0;
             continue;
         }
-        int e1 = e0 + 1, end = a.unit + a.n, tmax = a.tref;
+        int e1 = e0 + 1, end = a.unit + a.n;
         for (int e = e1; e < 2 * NW; ++e) {
             const Entry &x = entries[e];
             if (x.seq < 0) continue;
             if (x.start != a.start) break;
-            e1 = e + 1, end = x.unit + x.n, tmax = max(tmax, x.tref);
+            e1 = e + 1, end = x.unit + x.n;
         }
         const AttendSeq sq = attend_seq(p, a.seq);
         const int row_first = a.tile * ROWS, rows = min(ROWS, sq.nq * p.group - row_first);
@@ -734,25 +716,30 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
         float *part = p.partial + ((int64_t)blockIdx.x * 2 + (a.unit == 0)) * attend_slot_floats(ROWS, D);
         for (int x = tid; x < ROWS * (D / 2); x += NW * 32) {
             const int r = x / (D / 2), d = x % (D / 2) * 2;
-            float mx = NEG, tot = 0.f, v0 = 0.f, v1 = 0.f;
+            // a part's sums are in units of its maximum's weight times 2^R: the largest of these
+            // units, to a whole power of two, is the sum's
+            float mx = NEG, rx = R_MIN, tot = 0.f, v0 = 0.f, v1 = 0.f;
             for (int e = e0; e < e1; ++e)
                 if (entries[e].seq >= 0) mx = fmaxf(mx, em[e * ROWS + r]);
+            for (int e = e0; e < e1; ++e)
+                if (entries[e].seq >= 0) rx = fmaxf(rx, er[e * ROWS + r] + floorf(em[e * ROWS + r] - mx));
             for (int e = e0; e < e1; ++e) {
                 if (entries[e].seq < 0) continue;
-                const float f = ex2(em[e * ROWS + r] - mx), ft = f * pow2i(max(-126, entries[e].tref - tmax));
+                const float z = em[e * ROWS + r] - mx, ft = ex2(z + (er[e * ROWS + r] - rx));
                 const float *acc = e & 1 ? (const float *)(smem + (e >> 1) * C::RING) : heads + (e >> 1) * ROWS * D;
                 const float2 y = *(const float2 *)(acc + r * D + d);
-                tot += f * el[e * ROWS + r];
+                tot += ex2(z) * el[e * ROWS + r];
                 v0 += ft * y.x, v1 += ft * y.y;
             }
+            const int up = (int)rx + UP;
             if (!whole) {
-                *(float2 *)(part + r * D + d) = make_float2(scale2(v0, tmax + UP), scale2(v1, tmax + UP));
+                *(float2 *)(part + r * D + d) = make_float2(scale2(v0, up), scale2(v1, up));
                 if (d == 0) part[ROWS * D + r] = mx, part[ROWS * D + ROWS + r] = tot;
             } else if (r < rows) {
                 const float inv = tot > 0.f ? 1.f / tot : tot;
                 const int row = row_first + r, i = row / p.group;
                 const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + a.head * p.group + (row - i * p.group);
-                store_pair(p, bf16, dst * D + d, scale2(v0 * inv, tmax + UP), scale2(v1 * inv, tmax + UP));
+                store_pair(p, bf16, dst * D + d, scale2(v0 * inv, up), scale2(v1 * inv, up));
                 if (d == 0 && p.lse) p.lse[dst] = lse_of(mx, tot);
             }
         }

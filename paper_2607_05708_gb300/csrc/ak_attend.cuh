@@ -274,6 +274,15 @@ __host__ __device__ __forceinline__ int64_t attend_slot_floats(int rows, int dim
 // ------------------------------------------------------------------ arithmetic
 constexpr float NEG = -1e30f;                 // "no score yet", finite: no NaN from differences
 constexpr float P_SHIFT = 6.f, M_SLACK = 8.f; // log2 units
+// A row's weights, times their values' powers of two 2^T (8 bits: scales in [2^T, 2^(T+1))), are divided
+// by 2^R before they become fp16.  R goes by the greatest of these products that the row has seen, not by
+// tokens that it does not see or that weigh nothing: raised when one would pass 2^(R + R_SLACK),
+// so that it comes to 2^(R_SHIFT - 1) to 2^(R_SHIFT + 1): fp16 then has room for the 2^8 by which weights may
+// still grow, and values of eight times the size, and 2^-27 of the greatest as its smallest step.
+// (With 6 and 13 for these two the many-row kernel looked for the greatest often: two capped prompts of 2048
+// rows, all factors in use, 1300 us for 1159.)
+// Within R_MIN and R_MAX 2^-R is a normal number.
+constexpr int R_MIN = -126, R_MAX = 126, R_SLACK = 14, R_SHIFT = 3;
 
 __device__ __forceinline__ uint32_t h2fma(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t d;
@@ -299,6 +308,10 @@ __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+__device__ __forceinline__ float2 ex2_wide(float x) {   // 2^x as two factors, x from -252
+    const float a = fmaxf(x, -126.f);
+    return make_float2(ex2(a), ex2(fmaxf(x - a, -126.f)));
 }
 __device__ __forceinline__ float scale2(float x, int e) {   // x 2^e, |e| <= 252
     return x * pow2i(e / 2) * pow2i(e - e / 2);
@@ -373,7 +386,6 @@ __device__ __forceinline__ void nibbles(uint32_t w, uint32_t s, uint32_t s4, uin
     h[3] = h2fma(w8 & 0x00f000f0u, s4, c);
 }
 constexpr uint32_t H2_M2_21 = 0x80088008u;   // -2^-21, twice
-constexpr uint32_t H2_2_4 = 0x2c002c00u;     // 2^-4, twice
 constexpr uint32_t H2_M1152 = 0xe480e480u;   // -1152, twice
 // Two adjacent values of a result row, and its log-sum-exp.
 __device__ __forceinline__ void store_pair(const AttendParams &p, bool bf16, int64_t at, float a, float b) {

@@ -16,10 +16,17 @@
 //   softmax warps       a thread a row, 64 scores at a time: maximum, weights and total
 //       need no shuffle.  P (fp16) replaces its scores.  The maximum is raised,
 //       and O rescaled, only when a weight would exceed 2^14.
-// Keys are staged without their row's power of two, as v 2^-9 / 2^T (8 bits: as codes): that factor is
-// the softmax's, in fp32, so that a score depends on its own key alone.  Where fp16's normal range
-// ends they are rounded to 2^-17 of their row's largest.  Values are relative to the item's
-// largest so far.
+// A 4-bit key or value is staged in fp16 as it is, c e 2^T (times 2^STAGE), where its row's T lies in a window
+// (KEY_LO and so on); outside of it at the window's end, with the rest of its power of two as a factor, in
+// fp32, of the key's scores or the value's weight.  8 bits: as codes, the scale the factor.  So a
+// score and a weight depend on their own key and value alone, whatever else is in the tile, and
+// a half of a tile whose factors are all 1 skips them.  Where fp16's normal range ends keys and
+// values are rounded to 2^-17 of their own row's largest.  (Factors for all 4-bit rows: prompts of 2048 and
+// 1600 rows 734 us for 710, capped 1060 for 932, though a word of codes takes 11 instructions for 9;
+// with all values outside of the window 1134.)
+// A weight times its value's factor is divided by the row's 2^R before it becomes fp16.  R goes by what the
+// row has seen: raised, and O rescaled, only when a product would pass 2^14 (R_SLACK); 0 while all
+// of the row's values have been within the window.
 // Measured (4 bits): two requests of 2048 rows behind 10240 tokens, 32 heads on 8, D = 128 (514
 // GFLOP) 682 us, 0.75 PFLOP/s, and 905 us with capped scores; a step of 256 rows and 128
 // tokens 2.8 us, of which the products are 1.06: scores, softmax and O += P V of a row tile
@@ -72,21 +79,24 @@ struct Wide {
 // What the consumers of a tile need beside the operands.
 template <int N>
 struct alignas(16) Meta {           // pairs of its floats are read at once
-    float ksig[N];                  // the keys' scales (kv_key_factor), 1 where there is no token
-    float vsig[N];                  // 8 bits: significands of the values' scales
+    // The factors of the keys (times 2^-KEY_DOWN) and of the values, 1 where there is no token; 4 bits:
+    // written where a unit has one that is not 1 (bent)
+    float ksig[N], vsig[N];
     int tag[N];
-    // read at once: first token, exponent of the values, units listed
-    alignas(16) int tok;
-    int rv;
-    uint32_t have, pad;
+    int tok;                        // first token
+    // of each unit: the largest exponent of its values' factors, biased by 127, 0 if it has no
+    // token; whether it is bent
+    alignas(8) unsigned char vtop[N / KV_UNIT], bent[N / KV_UNIT];
 };
-// Factors of the scores: of the key, its row's power of two or bf16 scale, times 2^-12, so that times a
-// product of any size it stays in fp32's range (a stored infinity has T = 125), and of
-// the row, the rest: 2^12, and 2^9 of the staged keys.
-constexpr float ROW_FACTOR_4 = 2097152.f, ROW_FACTOR_8 = 4096.f;
-__device__ __forceinline__ float kv_key_factor(uint32_t scale) {   // as fp32 bits
-    return __uint_as_float(scale - (12u << 23));
-}
+// The windows of T.  Upwards 72 s (values8) has to stay in fp16's range; downwards a row's largest, 7 2^(T + STAGE), is
+// 2^17 times the roundings where e is small (from T = -7 on all is exact).  Values: twelve powers of two
+// only, so that the weights' smallest step times the window's largest value is small beside its
+// smallest.
+constexpr int STAGE = 2, KEY_LO = -10, KEY_HI = 6, VAL_LO = -10, VAL_HI = 2;
+// Keys' factors are stored times 2^-KEY_DOWN, and the row's is multiplied by it where they are used: a key
+// of T = 125 (a stored infinity) times any product of a query row stays in fp32's range.
+template <int BITS>
+constexpr int KEY_DOWN = BITS == 4 ? 26 : 12;
 static_assert(offsetof(Meta<64>, ksig) % 8 == 0 && offsetof(Meta<64>, vsig) % 8 == 0 &&
                   offsetof(Meta<128>, ksig) % 8 == 0 && offsetof(Meta<128>, vsig) % 8 == 0 &&
                   offsetof(Meta<64>, tag) % 16 == 0 && offsetof(Meta<128>, tag) % 16 == 0,
@@ -104,6 +114,21 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
         "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
         "r"(r[29]), "r"(r[30]), "r"(r[31])
         : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]),
+                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t (&r)[4]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+                 "r"(r[2]), "r"(r[3])
+                 : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -218,15 +243,33 @@ __device__ __forceinline__ void load_values(const unsigned char *un, bool have, 
 __device__ __forceinline__ uint4 *tile_chunk(unsigned char *tile, int rows, int t, int d) {
     return (uint4 *)(tile + (d >> 6) * (rows * 128) + t * 128 + ((((d & 63) >> 3) ^ (t & 7)) << 4));
 }
-__device__ __forceinline__ uint32_t pow2_h2(int e) {       // 2^e twice in fp16, e <= 0
-    const float f = e < -40 ? 0.f : pow2i(e);
-    return pack_h2(f, f);
+// 2^(T + STAGE), T within the window, twice in fp16, from T + 127.
+template <int LO, int HI>
+__device__ __forceinline__ uint32_t window_h2(uint32_t biased) {
+    static_assert(LO + STAGE >= -14 && HI + STAGE <= 15, "normal numbers");
+    return (uint32_t)(min(max((int)biased, LO + 127), HI + 127) + STAGE - 112) * 0x04000400u;
 }
-__device__ __forceinline__ uint4 bytes8(uint32_t w0, uint32_t w1, uint32_t f, uint32_t c) {
-    return make_uint4(h2fma(__byte_perm(w0, 0x64646464u, 0x4140), f, c),
-                      h2fma(__byte_perm(w0, 0x64646464u, 0x4342), f, c),
-                      h2fma(__byte_perm(w1, 0x64646464u, 0x4140), f, c),
-                      h2fma(__byte_perm(w1, 0x64646464u, 0x4342), f, c));
+// The values of a word of 8 nibbles, adjacent pairs: (n - 8) s, s = e 2^(T + STAGE) twice.  A nibble under 2^10 is
+// 1024 + n, one of bits 4 to 7 under 2 (64 + n) / 32: (64 + n) / 32 times 32 s less 72 s in one rounding, and
+// 72 s has nine bits.  (1032 s has 13: the others take two instructions.)
+struct NibbleScale {
+    uint32_t s, s32, c;
+};
+__device__ __forceinline__ void values8(uint32_t w, const NibbleScale &k, uint32_t (&h)[4]) {
+    const uint32_t w8 = w >> 8;
+    h[0] = h2mul(h2add((w & 0x000f000fu) | 0x64006400u, 0xe408e408u), k.s);               // - 1032
+    h[1] = h2fma((w & 0x00f000f0u) | 0x40004000u, k.s32, k.c);
+    h[2] = h2mul(h2add((w8 & 0x000f000fu) | 0x64006400u, 0xe408e408u), k.s);
+    h[3] = h2fma((w8 & 0x00f000f0u) | 0x40004000u, k.s32, k.c);
+}
+// Of a scale byte, and of its row's 2^T (window_h2).
+__device__ __forceinline__ NibbleScale nibble_scale(uint32_t by, uint32_t pow) {
+    NibbleScale k;
+    const uint32_t e = by * 0x00400040u + 0x14001400u;         // e 2^5
+    k.s32 = h2mul(e, pow);
+    k.s = h2mul(k.s32, 0x28002800u);                           // / 32
+    k.c = h2mul(k.s32, 0xc080c080u);                           // times -72 / 32
+    return k;
 }
 __device__ __forceinline__ uint4 codes8(uint32_t w0, uint32_t w1) {
     return make_uint4(h2add(__byte_perm(w0, 0x64646464u, 0x4140), H2_M1152),
@@ -267,14 +310,12 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
     using C = Wide<D>;
     using U = KvUnit<BITS, D>;
     constexpr int N = C::N, MT = C::MT, ROWS = C::ROWS, ST = C::STAGES, HT = C::HT, HPT = C::HPT;
-    constexpr int UP = 9;                      // values are staged as v 2^-9 (4 bits)
     extern __shared__ unsigned char raw_smem[];
     unsigned char *smem = (unsigned char *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
     unsigned char *sq_ = smem, *sk = smem + C::Q_BYTES, *sv = sk + ST * C::KV_BYTES;
     __shared__ Meta<N> meta[ST];
     __shared__ uint64_t kfull[ST], vfull[ST], empty[ST];      // tiles: keys, values, both read
-    __shared__ uint64_t sfull[MT][2], pfull[MT][2], odone[MT][2], qfull[MT], drained, texch;
-    __shared__ int tmaxs[2][C::DEQ];           // largest exponents of a warp's values
+    __shared__ uint64_t sfull[MT][2], pfull[MT][2], odone[MT][2], qfull[MT], drained;
     __shared__ float qscale[ROWS];
     __shared__ uint32_t tmem_slot;
     __shared__ int dead_word;
@@ -299,7 +340,6 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
             mbar_init(&qfull[t], 4);
         }
         mbar_init(&drained, 1);
-        mbar_init(&texch, C::DEQ);
         mbar_fence_init();
         dead_word = 0;
         p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
@@ -366,7 +406,6 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
             places(0);
             load_keys<BITS, D>(p.cache + un * U::BYTES, un >= 0, r);
             load_values<BITS, D>(p.cache + un * U::BYTES, un >= 0, r);
-            int rv = -127;
             for (int i = 0; i < n; ++i, ++n_tile) {
                 const int st = n_tile % ST, tok = (first_tile + i) * N;
                 if (!wide_wait(&empty[st], ((n_tile / ST) & 1) ^ 1, dead, p.status)) break;
@@ -379,43 +418,42 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     if (lane < 16) m.tag[lt] = max(tag_next, -1);
                 }
                 const uint32_t ok = __ballot_sync(0xffffffffu, mine);      // the unit's valid tokens
+                float kf = 1.f, vf = 1.f;      // the lane's token's factors
+                bool bent = BITS == 8;         // one is not 1
                 if (c < 2) {
-                    const uint32_t s = BITS == 4 ? (r.ke >> (8 * c) & 255u) << 23 : (c ? r.ks[0] & 0xffff0000u : r.ks[0] << 16);
-                    m.ksig[t0 + g + 8 * c] = ok >> (g + 8 * c) & 1u ? kv_key_factor(s) : 1.f;
-                }
-                // exponents of the values, relative to the item's largest
-                int vt[4], vmax = -127;
-                if constexpr (BITS == 4) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) vt[x] = (int)(r.ve >> (8 * x) & 255u) - 127;
-                } else {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) vt[x] = (int)(r.vs[x >> 1] >> (7 + 16 * (x & 1)) & 255u) - 127;
-                    if (g < 4) {               // significands; 1 where there is no token
-                        const uint32_t s = r.vs[g >> 1] >> (16 * (g & 1));
-                        const int t = 2 * c + (g & 1) + (g >> 1) * 8;
-                        m.vsig[t0 + t] = ok >> t & 1u ? __uint_as_float((s & 0x7fu) << 16 | 0x3f800000u) : 1.f;
+                    uint32_t s = c ? r.ks[0] & 0xffff0000u : r.ks[0] << 16;
+                    const bool valid = ok >> (g + 8 * c) & 1u;
+                    if constexpr (BITS == 4) {
+                        const int T = (int)(r.ke >> (8 * c) & 255u) - 127, rest = T - min(max(T, KEY_LO), KEY_HI);
+                        s = (uint32_t)(rest + 127) << 23;
+                        bent = valid && rest;
                     }
+                    kf = valid ? __uint_as_float(s - ((uint32_t)KEY_DOWN<BITS> << 23)) : 1.f;
                 }
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    if (!(ok >> (2 * c + (x & 1) + (x >> 1) * 8) & 1u)) vt[x] = -1000;
-                    vmax = max(vmax, vt[x]);
+                uint32_t vmax = 0;
+                if (g < 4) {                   // lane: token 2c + (g & 1) + 8 (g >> 1)
+                    const int t = 2 * c + (g & 1) + (g >> 1) * 8;
+                    const bool valid = ok >> t & 1u;
+                    uint32_t s = 0;
+                    if constexpr (BITS == 4) {
+                        const int T = (int)(r.ve >> (8 * g) & 255u) - 127, rest = T - min(max(T, VAL_LO), VAL_HI);
+                        s = (uint32_t)(rest + 127) << 23;
+                        bent = bent || (valid && rest);
+                    } else {
+                        s = (r.vs[g >> 1] >> (16 * (g & 1))) << 16;
+                    }
+                    vf = valid ? __uint_as_float(s) : 1.f;
+                    if (valid) vmax = s >> 23;
                 }
-                vmax = max(vmax, __shfl_xor_sync(0xffffffffu, vmax, 1));
-                vmax = max(vmax, __shfl_xor_sync(0xffffffffu, vmax, 2));
-                if (lane == 0) {
-                    tmaxs[n_tile & 1][w] = vmax;
-                    if (w == 0) m.tok = tok, m.have = 0;
-                    mbar_arrive(&texch);
+                if (__any_sync(0xffffffffu, bent)) {
+                    vmax = __reduce_max_sync(0xffffffffu, vmax);
+                    if (c < 2) m.ksig[t0 + g + 8 * c] = kf;
+                    if (g < 4) m.vsig[t0 + 2 * c + (g & 1) + (g >> 1) * 8] = vf;
+                    if (lane == 0) m.vtop[w] = (unsigned char)vmax, m.bent[w] = 1;
+                } else if (lane == 0) {
+                    m.vtop[w] = ok ? 127 : 0, m.bent[w] = 0;
                 }
-                if (!wide_wait(&texch, n_tile & 1, dead, p.status)) break;
-#pragma unroll
-                for (int x = 0; x < C::DEQ; ++x) rv = max(rv, tmaxs[n_tile & 1][x]);
-                if (lane == 0) {
-                    atomicOr(&m.have, (have ? 1u : 0u) << w);
-                    if (w == 0) m.rv = rv;
-                }
+                if (w == 0 && lane == 0) m.tok = tok;
                 // ---- keys
                 unsigned char *kt_ = sk + st * C::KV_BYTES, *vt_ = sv + st * C::KV_BYTES;
                 if (!have) {
@@ -424,6 +462,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         *tile_chunk(kt_, N, t0 + x / (D / 8), x % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
                 } else if constexpr (BITS == 4) {
                     constexpr int W = D / 32, PERG = D / 64;
+                    const uint32_t kp[2] = {window_h2<KEY_LO, KEY_HI>(r.ke & 255u), window_h2<KEY_LO, KEY_HI>(r.ke >> 8 & 255u)};
                     if constexpr (D == 128) {
                         // lanes c and c + 2 meet in the same banks (64 dims apart): the
                         // latter take their two groups the other way round
@@ -438,14 +477,13 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         for (int gr = 0; gr < PERG; ++gr) {
                             const int b = i2 * PERG + gr;
                             const uint32_t by = (r.ks[b / 4] >> (8 * (b & 3))) & 255u;
-                            const uint32_t s = by * 0x00400040u + 0x3c003c00u;
-                            const uint32_t s4 = s - 0x10001000u, cc = h2mul(s, H2_M2_21);
+                            const NibbleScale s = nibble_scale(by, kp[i2]);
 #pragma unroll
                             for (int q = 0; q < 2; ++q) {
                                 const int x = gr * 2 + q;      // word of the token
                                 const int at = D == 64 ? i2 * 2 + x : i2 * W + x;
                                 uint32_t h[4];
-                                nibbles(word_of(r.k[at / 4], at % 4), s, s4, cc, h);
+                                values8(word_of(r.k[at / 4], at % 4), s, h);
                                 *tile_chunk(kt_, N, t0 + g + 8 * i2, c * (D / 4) + (x ^ (far ? 2 : 0)) * 8) = make_uint4(h[0], h[1], h[2], h[3]);
                             }
                         }
@@ -476,33 +514,31 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         const int t = t0 + 2 * c + (x & 1) + (x >> 1) * 8;
-                        const uint32_t f = pow2_h2(vt[x] - rv);
                         if constexpr (BITS == 4) {
                             constexpr int W = D / 64, GL = D == 256 ? 2 : 1, WG = W / GL;
+                            const uint32_t vp = window_h2<VAL_LO, VAL_HI>(r.ve >> (8 * x) & 255u);
 #pragma unroll
                             for (int gl = 0; gl < GL; ++gl) {
                                 const uint32_t by = (r.vs[gl] >> (8 * x)) & 255u;
-                                const uint32_t s = h2mul(by * 0x00400040u + 0x3c003c00u, f);
-                                const uint32_t s4 = h2mul(s, H2_2_4), cc = h2mul(s, H2_M2_21);
+                                const NibbleScale s = nibble_scale(by, vp);
 #pragma unroll
                                 for (int q = 0; q < WG; ++q) {
                                     const int i3 = gl * WG + q, at = x * W + i3;
                                     uint32_t h[4], word = word_of(r.v[at / 4], at % 4);
                                     if (D == 128 && odd) word = word_of(r.v[at / 4], (at ^ 1) % 4);
-                                    nibbles(word, s, s4, cc, h);
+                                    values8(word, s, h);
                                     *tile_chunk(vt_, N, t, g * (D / 8) + (i3 ^ (odd ? 1 : 0)) * 8) = make_uint4(h[0], h[1], h[2], h[3]);
                                 }
                             }
                         } else {
                             constexpr int W = D / 32;          // words of 4 dims
-                            const uint32_t cc = h2mul(f, H2_M1152);
 #pragma unroll
                             for (int q = 0; q < W; q += 2) {
                                 const int at = x * W + q;
                                 uint32_t w0 = word_of(r.v[at / 4], at % 4), w1 = word_of(r.v[at / 4], at % 4 + 1);
                                 if (D == 128 && odd)
                                     w0 = word_of(r.v[at / 4], (at ^ 2) % 4), w1 = word_of(r.v[at / 4], (at ^ 2) % 4 + 1);
-                                *tile_chunk(vt_, N, t, g * (D / 8) + (q ^ (odd ? 2 : 0)) * 4) = bytes8(w0, w1, f, cc);
+                                *tile_chunk(vt_, N, t, g * (D / 8) + (q ^ (odd ? 2 : 0)) * 4) = codes8(w0, w1);
                             }
                         }
                     }
@@ -686,7 +722,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 const bool real = r < rows;
                 const int i = real ? (row_first + r) / p.group : 0;
                 const int hd = cur.head * p.group + (real ? row_first + r - i * p.group : 0);
-                const float qf = qscale[r] * p.scale * LOG2E_F * (BITS == 4 ? ROW_FACTOR_4 : ROW_FACTOR_8);
+                const float qf = qscale[r] * p.scale * LOG2E_F * (BITS == 4 ? 1.f / (1 << STAGE) : 1.f);
                 const int limit = real ? attend_limit(p, sq, i) : sq.kv, pos = sq.kv - sq.nq + i;
                 const float slope = real && p.slopes ? p.slopes[hd] * LOG2E_F : 0.f;
                 // a slot without a token has tag -1 here, and a row that sees none -2
@@ -695,8 +731,8 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
 
                 float mm = 0.f, l = 0.f;
                 bool unset = real;             // no key seen yet: mm = 0
-                int rv = -127;
-                uint4 about = make_uint4(0, 0, 0, 0);      // the tile's Meta from tok on
+                int rr = 0, tile_tok = 0;      // rr: R
+                bool plain = BITS == 4;        // R is 0 for all rows of the warp
                 for (int h = 0; h < n * HPT; ++h, ++halves) {
                     const uint32_t x_tile = n_tile + h / HPT, st = x_tile % ST, b = halves & 1;
                     const uint32_t s_at = tmem + lanes + C::S_COL + (t * 2 + b) * HT;
@@ -704,28 +740,47 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         // what the dequantising warps wrote beside the tile, while its scores
                         // are computed
                         ok = wide_wait(&kfull[st], (x_tile / ST) & 1, dead, p.status);
-                        about = *(const uint4 *)&meta[st].tok;
+                        tile_tok = meta[st].tok;
                         if (ok) ok = wide_wait(&sfull[t][b], halves >> 1 & 1, dead, p.status);
                         ok = __all_sync(0xffffffffu, ok);
                         if (!ok) break;
                         tc_fence_after();
                     }
+                    const Meta<N> &m = meta[st];
+                    const int half = h % HPT * HT, tok = tile_tok + half;
+                    const uint32_t vtop = *(const uint32_t *)&m.vtop[half / KV_UNIT];
+                    const uint32_t bends = BITS == 4 ? *(const uint32_t *)&m.bent[half / KV_UNIT] : 0x01010101u;
+                    const bool flat = bends == 0;
+                    if (BITS == 4 && !flat) {
+                        // the keys' factors (short loops, here and below: what is rare costs the rest no registers)
+#pragma unroll 1
+                        for (int k0 = 0; k0 < HT; k0 += 8) {
+                            const bool bent = bends >> (k0 / KV_UNIT * 8) & 1u;
+                            uint32_t y[8];
+                            tmem_ld8(s_at + k0, y);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                y[k] = __float_as_uint(__uint_as_float(y[k]) * (bent ? m.ksig[half + k0 + k] : pow2i(-KEY_DOWN<BITS>)));
+                            tmem_st8(s_at + k0, y);
+                        }
+                        tmem_st_wait();
+                    }
                     uint32_t x[HT];
                     tmem_ld32(s_at, *(uint32_t(*)[32])x);
                     tmem_ld32(s_at + 32, *(uint32_t(*)[32])(x + 32));
-                    const Meta<N> &m = meta[st];
-                    const int half = h % HPT * HT, tok = (int)about.x + half, rv_new = (int)about.y;
-                    const uint32_t have = about.z >> (half / KV_UNIT) & 15u;
-                    float f = qf;              // of the scores, log2 units
-                    const bool masked = tags || tok > safe || have != 15u;
+                    float f = flat ? qf : qf * pow2i(KEY_DOWN<BITS>);      // of the scores, log2 units
+                    // (a byte of vtop is 0)
+                    const bool masked = tags || tok > safe || ((vtop - 0x01010101u) & ~vtop & 0x80808080u);
                     tmem_ld_wait();
                     auto pair = [&](int k) { return f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])); };
                     auto put = [&](int k, uint64_t v) {
                         const float2 y = f2_open(v);
                         x[k] = __float_as_uint(y.x), x[k + 1] = __float_as_uint(y.y);
                     };
+                    if constexpr (BITS == 8)
 #pragma unroll
-                    for (int k = 0; k < HT; k += 2) put(k, f2_mul(pair(k), *(const uint64_t *)&m.ksig[half + k]));
+                        for (int k = 0; k < HT; k += 2) put(k, f2_mul(pair(k), *(const uint64_t *)&m.ksig[half + k]));
                     if (heavy || masked) {
                         // in place, from here on the factor is 1
 #pragma unroll
@@ -741,7 +796,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         if (masked) {
 #pragma unroll
                             for (int u = 0; u < HT / 16; ++u) {
-                                const int end = have >> u & 1u ? limit - tok - u * 16 : 0;
+                                const int end = vtop >> (8 * u) & 255u ? limit - tok - u * 16 : 0;
 #pragma unroll
                                 for (int k = 0; k < 16; ++k)
                                     if (k >= end) x[u * 16 + k] = 0xff800000u;
@@ -764,34 +819,100 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     for (int k = 1; k < HT; ++k) top = fmaxf(top, __uint_as_float(x[k]));
                     top *= f;
                     // the maximum is raised when a weight would pass 2^14
-                    float down = 1.f;          // of what was summed so far
+                    float x_up = 0.f;
                     if (unset ? top > -INFINITY : top - mm > P_SHIFT + M_SLACK) {
-                        down = unset ? 0.f : ex2(mm + P_SHIFT - top);
+                        x_up = unset ? INFINITY : top - P_SHIFT - mm;
                         unset = false;
                         mm = top - P_SHIFT;
                     }
-                    uint64_t sum[2] = {0, 0};
-                    const uint64_t n2 = f2_pack(-mm, -mm);
-                    uint32_t pk[HT / 2];
+                    const float down = ex2(-x_up);             // of what was summed so far
+                    float2 od = make_float2(down, 1.f);        // of O, two factors
+                    float n1 = -mm, unit = 1.f;
+                    bool loop = false;
+                    if (!(flat && plain)) {
+                        // R: falls as the maximum rises, so that O keeps its scale, and is raised by what the row
+                        // sees.  That there is nothing to look for the half's largest exponent says,
+                        // whoever sees it.
+                        int rn = rr;
+                        if (x_up > 0.f) rn = x_up < INFINITY ? max(R_MIN, rr - (int)fminf(ceilf(x_up), 300.f)) : R_MIN;
+                        float wm = top - mm;                   // the largest product, log2
+                        if (!flat) {
+                            const int t4 = max(max(vtop & 255u, vtop >> 8 & 255u), max(vtop >> 16 & 255u, vtop >> 24));
+                            if (__any_sync(0xffffffffu, wm + (float)(t4 - 127) > (float)(rn + R_SLACK))) {
+                                wm = -INFINITY;
+                                tmem_st32(s_at, *(const uint32_t(*)[32])x);
+                                tmem_st32(s_at + 32, *(const uint32_t(*)[32])(x + 32));
+                                tmem_st_wait();
+#pragma unroll 1
+                                for (int k0 = 0; k0 < HT; k0 += 8) {
+                                    const bool bent = bends >> (k0 / KV_UNIT * 8) & 1u;
+                                    uint32_t y[8];
+                                    tmem_ld8(s_at + k0, y);
+                                    tmem_ld_wait();
 #pragma unroll
-                    for (int k = 0; k < HT; k += 2) {
-                        const float2 u = f2_open(f2_fma(pair(k), f2_pack(f, f), n2));
-                        uint64_t e2 = f2_pack(ex2(u.x), ex2(u.y));
-                        sum[k / 2 % 2] = f2_add(sum[k / 2 % 2], e2);
-                        if constexpr (BITS == 8) e2 = f2_mul(e2, *(const uint64_t *)&m.vsig[half + k]);
-                        const float2 y = f2_open(e2);
-                        pk[k / 2] = pack_h2(y.x, y.y);
+                                    for (int k = 0; k < 8; ++k) {              // (rounded as top - mm is)
+                                        const int e = bent ? (int)(__float_as_uint(m.vsig[half + k0 + k]) >> 23) - 127 : 0;
+                                        wm = fmaxf(wm, __fsub_rn(__fmul_rn(__uint_as_float(y[k]), f), mm) + (float)e);
+                                    }
+                                }
+                            } else {
+                                wm = -INFINITY;
+                            }
+                        }
+                        if (wm > (float)(rn + R_SLACK))
+                            rn = BITS == 4 && wm >= (float)(R_SHIFT - 1) && wm <= (float)R_SLACK ? 0 : min(R_MAX, (int)ceilf(wm) - R_SHIFT);
+                        od = ex2_wide((float)(rr - rn) - (x_up < INFINITY ? x_up : 0.f));
+                        rr = rn;
+                        plain = BITS == 4 && __all_sync(0xffffffffu, rr == 0);
+                        // The weights over 2^R: the exponential of the score less both, or, where that could
+                        // leave fp32's range (values beyond 2^64 or so, or below 2^-64), R as a factor.  (A
+                        // row's own R decides how its weights are computed; a row that sees nothing has none.)
+                        const bool far = !unset && abs(rr) > 64;
+                        const int r_in = far || unset ? 0 : rr;
+                        n1 = -mm - (float)r_in, unit = pow2i(r_in);
+                        loop = __any_sync(0xffffffffu, far) || BITS == 4;
+                        if (loop) {
+                            const float rf = far ? pow2i(-rr) : 1.f;
+                            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                            tmem_st32(s_at, *(const uint32_t(*)[32])x);
+                            tmem_st32(s_at + 32, *(const uint32_t(*)[32])(x + 32));
+                            tmem_st_wait();
+#pragma unroll 1
+                            for (int k0 = 0; k0 < HT; k0 += 8) {
+                                const bool bent = bends >> (k0 / KV_UNIT * 8) & 1u;
+                                uint32_t y[8], w[4];
+                                tmem_ld8(s_at + k0, y);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int k = 0; k < 8; k += 2) {
+                                    const float e0 = ex2(fmaf(__uint_as_float(y[k]), f, n1)), e1 = ex2(fmaf(__uint_as_float(y[k + 1]), f, n1));
+                                    sum[k % 4] += e0, sum[k % 4 + 1] += e1;
+                                    w[k / 2] = pack_h2(e0 * rf * (bent ? m.vsig[half + k0 + k] : 1.f),
+                                                       e1 * rf * (bent ? m.vsig[half + k0 + k + 1] : 1.f));
+                                }
+                                tmem_st4(s_at + k0 / 2, w);    // (over scores that have been read)
+                            }
+                            l = l * down + ((sum[0] + sum[2]) + (sum[1] + sum[3])) * unit;
+                        }
                     }
-                    {
+                    if (!loop) {
+                        uint64_t sum[2] = {0, 0};              // (in the order of the loop above)
+                        const uint64_t n2 = f2_pack(n1, n1);
+                        uint32_t pk[HT / 2];
+#pragma unroll
+                        for (int k = 0; k < HT; k += 2) {
+                            const float2 u = f2_open(f2_fma(pair(k), f2_pack(f, f), n2));
+                            uint64_t e2 = f2_pack(ex2(u.x), ex2(u.y));
+                            sum[k / 2 % 2] = f2_add(sum[k / 2 % 2], e2);
+                            if constexpr (BITS == 8) e2 = f2_mul(e2, *(const uint64_t *)&m.vsig[half + k]);
+                            const float2 y = f2_open(e2);
+                            pk[k / 2] = pack_h2(y.x, y.y);
+                        }
                         const float2 y = f2_open(f2_add(sum[0], sum[1]));
-                        l = l * down + (y.x + y.y);
+                        l = l * down + (y.x + y.y) * unit;
+                        tmem_st32(s_at, pk);
                     }
-                    if (rv_new != rv) {
-                        down *= pow2i(max(-126, rv - rv_new));
-                        rv = rv_new;
-                    }
-                    tmem_st32(s_at, pk);
-                    if (h > 0 && __any_sync(0xffffffffu, down != 1.f)) {
+                    if (h > 0 && __any_sync(0xffffffffu, od.x != 1.f || od.y != 1.f)) {
                         // once the products before have been added
                         ok = wide_wait(&odone[t][b ^ 1], (halves - 1) >> 1 & 1, dead, p.status);
                         ok = __all_sync(0xffffffffu, ok);
@@ -803,7 +924,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                             tmem_ld32(o_at + d, y);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * down);
+                            for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * od.x * od.y);
                             tmem_st32(o_at + d, y);
                         }
                     }
@@ -820,7 +941,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 const bool whole = n == cur.units;
                 if (unset) mm = NEG;
                 float *part = p.partial + ((int64_t)blockIdx.x * 2 + (mine.from == 0)) * attend_slot_floats(ROWS, D);
-                const int up = rv + (BITS == 4 ? UP : 0);
+                const int up = rr - (BITS == 4 ? STAGE : 0);
                 const float inv = whole ? (l > 0.f ? 1.f / l : l) : 1.f, up0 = pow2i(up / 2), up1 = pow2i(up - up / 2);
                 const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + hd;
 #pragma unroll 1

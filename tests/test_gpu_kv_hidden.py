@@ -101,3 +101,51 @@ def test_hidden_keys_change_nothing(bits, dim, dtype, nq, kv, what):
     if nq > 1:
         _by_time(bits, dim, dtype, nq, kv, "keys", what)
     _by_tags(bits, dim, dtype, nq, kv, "keys", what)
+
+
+@pytest.mark.parametrize("what", ["inf", "1e30", "65536"])
+@pytest.mark.parametrize("nq,kv", SHAPES)
+@pytest.mark.parametrize("bits,dim,dtype", FORMS)
+def test_hidden_values_change_nothing(bits, dim, dtype, nq, kv, what):
+    if nq > 1:
+        _by_time(bits, dim, dtype, nq, kv, "values", what)
+    _by_tags(bits, dim, dtype, nq, kv, "values", what)
+
+
+@pytest.mark.parametrize("nq,kv", SHAPES)
+@pytest.mark.parametrize("bits,dim,dtype", FORMS[:3])
+def test_hidden_tokens_behind_a_prefix_and_a_bias(bits, dim, dtype, nq, kv):
+    """Both at once, under a prefix and a distance bias."""
+    if nq > 1:
+        c = _Call(nq + kv + 2, bits, dim, dtype, nq, kv, 0, causal=True,
+                  prefix_len=_gpu(np.array([kv // 2], np.int32)), slopes=_gpu(np.array([0.5, 0.01], np.float32)))
+        a = c(c.k, c.v)
+        at = kv - nq + 1                       # row 0 sees none of these
+        k, v = c.k.clone(), c.v.clone()
+        k[at:], v[at:] = _extreme("inf", k[at:], c.rng), _extreme("inf", v[at:], c.rng)
+        b = c(k, v)
+        assert torch.equal(a[0][0], b[0][0]) and torch.equal(a[1][0], b[1][0])
+    _by_tags(bits, dim, dtype, nq, kv, "both", "inf")
+
+
+@pytest.mark.parametrize("nq,kv", SHAPES)
+@pytest.mark.parametrize("bits,dim,dtype", FORMS)
+def test_hidden_tokens_under_a_cap(bits, dim, dtype, nq, kv):
+    """Which of its two forms a capped score takes goes by the warp's largest, so that here
+    a score may differ by the forms' difference, 2^-21 of the cap and less."""
+    c = _Call(nq + kv + 3, bits, dim, dtype, nq, kv, 2, causal=False, cap=5.0)
+    qt = np.arange(nq) % 2
+    c.args["q_tags"] = _gpu(qt.astype(np.int32))
+    a = c(c.k, c.v)
+    hide = torch.from_numpy(c.tags == 1)
+    k, v = c.k.clone(), c.v.clone()
+    k[hide], v[hide] = _extreme("inf", k[hide], c.rng), _extreme("inf", v[hide], c.rng)
+    b = c(k, v)
+    rows = _gpu(np.flatnonzero(qt == 0))
+    # scores off by t: weights by 2 t relative and by another rounding to fp16 (a step is
+    # 2^-10); the result is rounded twice
+    t = 5 * 2.0 ** -20
+    size = float(c.v[~hide].abs().max())
+    far = (a[0][rows].double() - b[0][rows].double()).abs().max()
+    assert far <= (2 * t + 2.0 ** -10 + torch.finfo(DT[dtype]).eps) * size
+    assert (a[1][rows] - b[1][rows]).abs().max() <= 2 * t

@@ -419,10 +419,15 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                 }
                 }
 
-                // ---- scores in log2 units less the running maximum (mm = m - 6);
-                // what a row does not see is -inf
+                // ---- scores in log2 units less the running maximum (mm = m - 6); what a row does not
+                // see is -inf.  (The row's factor first: with the key's, 2^125 for a stored infinity,
+                // it may be infinite, and a score of 0 then NaN.)
                 const int *tg = (const int *)(st + UPS * U::BYTES);
                 const bool masked = tok > safe || have != (UPS == 2 ? 0x303u : 3u);
+                auto less = [](float a, float f, float m) {    // a f - m, a f rounded: at 2^24 and more its
+                    // rounding error is 1 and more, and equal scores would not have equal weights
+                    return BITS == 4 ? fmaf(a, f, -m) : __fsub_rn(__fmul_rn(a, f), m);   // (4 bits: exact)
+                };
                 float most = NEG;
 #pragma unroll
                 for (int j = 0; j < UPS; ++j) {
@@ -432,7 +437,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                             uint32_t x[4];
 #pragma unroll
                             for (int r = 0; r < 4; ++r)
-                                x[r] = __float_as_uint(s[j][b][r] * ((r < 2 ? kf0[j] : kf1[j]) * qk[b][r & 1]));
+                                x[r] = __float_as_uint(s[j][b][r] * qk[b][r & 1] * (r < 2 ? kf0[j] : kf1[j]));
                             if (p.cap > 0.f) cap_scores<4>(x, cap_l);
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
@@ -446,7 +451,7 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                         } else {
 #pragma unroll
                             for (int r = 0; r < 4; ++r)
-                                s[j][b][r] = fmaf(s[j][b][r], (r < 2 ? kf0[j] : kf1[j]) * qk[b][r & 1], -mm[b][r & 1]);
+                                s[j][b][r] = less(s[j][b][r] * qk[b][r & 1], r < 2 ? kf0[j] : kf1[j], mm[b][r & 1]);
                         }
                         if (masked) {
 #pragma unroll

@@ -733,6 +733,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 bool unset = real;             // no key seen yet: mm = 0
                 int rr = 0, tile_tok = 0;      // rr: R
                 bool plain = BITS == 4;        // R is 0 for all rows of the warp
+                bool big = false, any_big = false;         // the maximum has been beyond 2^20: the row's, one of the warp's
                 for (int h = 0; h < n * HPT; ++h, ++halves) {
                     const uint32_t x_tile = n_tile + h / HPT, st = x_tile % ST, b = halves & 1;
                     const uint32_t s_at = tmem + lanes + C::S_COL + (t * 2 + b) * HT;
@@ -766,18 +767,18 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         }
                         tmem_st_wait();
                     }
-                    uint32_t x[HT];
-                    tmem_ld32(s_at, *(uint32_t(*)[32])x);
-                    tmem_ld32(s_at + 32, *(uint32_t(*)[32])(x + 32));
-                    float f = flat ? qf : qf * pow2i(KEY_DOWN<BITS>);      // of the scores, log2 units
                     // (a byte of vtop is 0)
                     const bool masked = tags || tok > safe || ((vtop - 0x01010101u) & ~vtop & 0x80808080u);
-                    tmem_ld_wait();
+                    uint32_t x[HT];
                     auto pair = [&](int k) { return f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])); };
                     auto put = [&](int k, uint64_t v) {
                         const float2 y = f2_open(v);
                         x[k] = __float_as_uint(y.x), x[k + 1] = __float_as_uint(y.y);
                     };
+                    tmem_ld32(s_at, *(uint32_t(*)[32])x);
+                    tmem_ld32(s_at + 32, *(uint32_t(*)[32])(x + 32));
+                    float f = flat ? qf : qf * pow2i(KEY_DOWN<BITS>);      // of the scores, log2 units
+                    tmem_ld_wait();
                     if constexpr (BITS == 8)
 #pragma unroll
                         for (int k = 0; k < HT; k += 2) put(k, f2_mul(pair(k), *(const uint64_t *)&m.ksig[half + k]));
@@ -819,8 +820,22 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     for (int k = 1; k < HT; ++k) top = fmaxf(top, __uint_as_float(x[k]));
                     top *= f;
                     // the maximum is raised when a weight would pass 2^14
+                    const bool rises = unset ? top > -INFINITY : top - mm > P_SHIFT + M_SLACK;
+                    bool moves = __any_sync(0xffffffffu, rises);               // O changes its scale
+                    // Scores of 2^20 and more are rounded before the maximum is taken from them: of 2^33, x f
+                    // unrounded is as much as 2^9 away from the maximum that is its own rounding.
+                    if (moves && !heavy) {
+                        big = big || (rises && fabsf(top) > 1048576.f);
+                        any_big = __any_sync(0xffffffffu, big);
+                    }
+                    if (any_big && !masked) {
+                        const float in = big ? f : 1.f;
+                        f = big ? 1.f : f;
+#pragma unroll
+                        for (int k = 0; k < HT; k += 2) put(k, f2_mul(pair(k), f2_pack(in, in)));
+                    }
                     float x_up = 0.f;
-                    if (unset ? top > -INFINITY : top - mm > P_SHIFT + M_SLACK) {
+                    if (rises) {
                         x_up = unset ? INFINITY : top - P_SHIFT - mm;
                         unset = false;
                         mm = top - P_SHIFT;
@@ -862,6 +877,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         if (wm > (float)(rn + R_SLACK))
                             rn = BITS == 4 && wm >= (float)(R_SHIFT - 1) && wm <= (float)R_SLACK ? 0 : min(R_MAX, (int)ceilf(wm) - R_SHIFT);
                         od = ex2_wide((float)(rr - rn) - (x_up < INFINITY ? x_up : 0.f));
+                        moves = __any_sync(0xffffffffu, x_up != 0.f || rr != rn);
                         rr = rn;
                         plain = BITS == 4 && __all_sync(0xffffffffu, rr == 0);
                         // The weights over 2^R: the exponential of the score less both, or, where that could
@@ -912,7 +928,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         l = l * down + (y.x + y.y) * unit;
                         tmem_st32(s_at, pk);
                     }
-                    if (h > 0 && __any_sync(0xffffffffu, od.x != 1.f || od.y != 1.f)) {
+                    if (h > 0 && moves) {
                         // once the products before have been added
                         ok = wide_wait(&odone[t][b ^ 1], (halves - 1) >> 1 & 1, dead, p.status);
                         ok = __all_sync(0xffffffffu, ok);

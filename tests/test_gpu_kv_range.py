@@ -1,0 +1,61 @@
+"""Attention at the ends of fp32's range: keys and values that are stored infinities, scores and
+sums that are nearly as large."""
+import numpy as np
+import pytest
+
+import _kv_oracle as orc
+from test_gpu_kv_cache import DT, _built, _cache, _gpu  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+FORMS = [(4, 128), (8, 64), (4, 256), (8, 128), (4, 64), (8, 256)]
+# 1 row: a CTA an item; 3 rows of a long list: parts that are joined; 300 rows: the kernel for
+# many, whose parts are joined too
+SHAPES = [(1, 90), (3, 9000), (300, 9000)]
+
+
+def _attend(bits, dim, q, k, v, T=16, **args):
+    """Attention over all of k, v [kv, 1, dim] (fp32) for q [nq, heads, dim] bf16."""
+    n = -(-len(k) // T)
+    c = _cache(n, 1, dim, block_tokens=T, bits=bits)
+    c.write(k.cuda(), v.cuda(), torch.arange(len(k), device="cuda"))
+    got = c.attend(q.cuda(), torch.arange(n, device="cuda")[None],
+                   kv_len=_gpu(np.array([len(k)], np.int32)), causal=False, **args)
+    c.sync()
+    return got
+
+
+def _normal(seed, *shape):
+    return torch.from_numpy(np.random.default_rng(seed).standard_normal(shape)).bfloat16().float()
+
+
+@pytest.mark.parametrize("nq,kv", SHAPES)
+@pytest.mark.parametrize("bits,dim", FORMS)
+def test_infinite_keys_that_are_seen(bits, dim, nq, kv):
+    """A key that is infinite in one dim is stored as the largest fp32 there and 0 elsewhere.
+    Queries of 0 there score it 0; of either sign, all or nothing."""
+    q, k, v = _normal(1, nq, 2, dim), _normal(2, kv, 1, dim), _normal(3, kv, 1, dim)
+    k[40, 0], k[40, 0, 5] = 0, float("inf")
+    q[:, 0, 5] = 0
+    out, lse = _attend(bits, dim, q.bfloat16(), k, v)
+    k0 = k.clone()
+    k0[40] = 0                                  # the same scores for head 0
+    want, wlse = _attend(bits, dim, q.bfloat16(), k0, v)
+    assert torch.equal(out[:, 0], want[:, 0]) and torch.equal(lse[:, 0], wlse[:, 0])
+    # head 1, positive: that token's value; its score is q max / sqrt(dim)
+    q[:, 1, 5] = 0.5
+    out, lse = _attend(bits, dim, q.bfloat16(), k, v)
+    value = torch.from_numpy(orc.stored(v[40].double().numpy(), bits))[0]
+    key = float(orc.stored(k[40].double().numpy(), bits)[0, 5])
+    assert torch.equal(out[:, 1].cpu(), value.bfloat16().expand(nq, dim))
+    assert torch.allclose(lse[:, 1].double().cpu(), torch.tensor(0.5 * key / dim ** 0.5, dtype=torch.float64), rtol=1e-6)
+    # negative: as if the token were not there
+    q[:, 1, 5] = -0.5
+    out, lse = _attend(bits, dim, q.bfloat16(), k, v)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    keep = torch.arange(kv) != 40
+    want, wlse = _attend(bits, dim, q.bfloat16(), k[keep], v[keep])
+    # (tokens in other places: two roundings of the result, of weights and of scores)
+    assert (out[:, 1].double() - want[:, 1].double()).abs().max() <= 2.0 ** -7 * float(v.abs().max())
+    assert (lse[:, 1] - wlse[:, 1]).abs().max() <= 2.0 ** -14

@@ -737,11 +737,11 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
                 v0 += ft * y.x, v1 += ft * y.y;
             }
             const int up = (int)rx + UP;
+            const float inv = tot > 0.f ? 1.f / tot : tot;
             if (!whole) {
-                *(float2 *)(part + r * D + d) = make_float2(scale2(v0, up), scale2(v1, up));
+                *(float2 *)(part + r * D + d) = make_float2(scale2(v0 * inv, up), scale2(v1 * inv, up));
                 if (d == 0) part[ROWS * D + r] = mx, part[ROWS * D + ROWS + r] = tot;
             } else if (r < rows) {
-                const float inv = tot > 0.f ? 1.f / tot : tot;
                 const int row = row_first + r, i = row / p.group;
                 const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + a.head * p.group + (row - i * p.group);
                 store_pair(p, bf16, dst * D + d, scale2(v0 * inv, up), scale2(v1 * inv, up));
@@ -762,8 +762,7 @@ constexpr int JOIN_ROWS = 8, JOIN_CTAS = 1024;     // of the kernel before, at m
 template <int D>
 __global__ void __launch_bounds__(256)
 k_attend_join(const AttendParams p, const int rows, const bool bf16) {
-    __shared__ float factor[JOIN_ROWS * JOIN_CTAS];
-    __shared__ float inv[JOIN_ROWS];
+    __shared__ float factor[JOIN_ROWS * JOIN_CTAS];    // a slot's share of the row's total
     griddep_wait();
     const int4 j = p.joins[blockIdx.x];
     if (j.x < 0) return;
@@ -783,14 +782,15 @@ k_attend_join(const AttendParams p, const int rows, const bool bf16) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
         for (int k = lane; k < parts; k += 32) {
-            const float f = ex2(slot(k)[rows * D + r] - mx);
+            const float f = ex2(slot(k)[rows * D + r] - mx) * slot(k)[rows * D + rows + r];
             factor[warp * parts + k] = f;
-            tot += f * slot(k)[rows * D + rows + r];
+            tot += f;
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, o);
+        const float inv = tot > 0.f ? 1.f / tot : tot;         // a NaN stays one
+        for (int k = lane; k < parts; k += 32) factor[warp * parts + k] *= inv;
         if (lane == 0) {
-            inv[warp] = tot > 0.f ? 1.f / tot : tot;
             const int row = j.z * rows + r, i = row / p.group;
             if (p.lse)
                 p.lse[(int64_t)(sq.row0 + i) * p.q_heads + j.y * p.group + (row - i * p.group)] = lse_of(mx, tot);
@@ -808,8 +808,8 @@ k_attend_join(const AttendParams p, const int rows, const bool bf16) {
         }
         const int row = j.z * rows + r0 + r, i = row / p.group;
         const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + j.y * p.group + (row - i * p.group);
-        store_pair(p, bf16, dst * D + d, v.x * inv[r], v.y * inv[r]);
-        store_pair(p, bf16, dst * D + d + 2, v.z * inv[r], v.w * inv[r]);
+        store_pair(p, bf16, dst * D + d, v.x, v.y);
+        store_pair(p, bf16, dst * D + d + 2, v.z, v.w);
     }
 }
 

@@ -262,11 +262,12 @@ __device__ __forceinline__ AttendPart attend_part(const AttendCursor &c, int lef
 }
 
 // An item whose steps lie in several CTAs' shares: each leaves its rows'
-// unnormalised sums, maxima and totals in a slot of the workspace (two a CTA: slot 0 for
+// results over its part, maxima and totals in a slot of the workspace (two a CTA: slot 0 for
 // the item that began before its share, slot 1 for one that begins in it), the CTA in
 // which the item begins notes it in joins, and the joining kernel adds the slots
 // up in the order of the CTAs.
-//   slot: float acc[rows][D], m[rows] (log2 units), l[rows]
+//   slot: float out[rows][D], m[rows] (log2 units), l[rows]
+// (Results, not the weighted sums: of values near the largest fp32 those are infinite.)
 __host__ __device__ __forceinline__ int64_t attend_slot_floats(int rows, int dim) {
     return (int64_t)rows * (dim + 2);
 }

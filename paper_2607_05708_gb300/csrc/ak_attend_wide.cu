@@ -958,7 +958,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                 if (unset) mm = NEG;
                 float *part = p.partial + ((int64_t)blockIdx.x * 2 + (mine.from == 0)) * attend_slot_floats(ROWS, D);
                 const int up = rr - (BITS == 4 ? STAGE : 0);
-                const float inv = whole ? (l > 0.f ? 1.f / l : l) : 1.f, up0 = pow2i(up / 2), up1 = pow2i(up - up / 2);
+                const float inv = l > 0.f ? 1.f / l : l, up0 = pow2i(up / 2), up1 = pow2i(up - up / 2);
                 const int64_t dst = (int64_t)(sq.row0 + i) * p.q_heads + hd;
 #pragma unroll 1
                 for (int d = 0; d < D; d += 32) {

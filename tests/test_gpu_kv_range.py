@@ -59,3 +59,19 @@ def test_infinite_keys_that_are_seen(bits, dim, nq, kv):
     # (tokens in other places: two roundings of the result, of weights and of scores)
     assert (out[:, 1].double() - want[:, 1].double()).abs().max() <= 2.0 ** -7 * float(v.abs().max())
     assert (lse[:, 1] - wlse[:, 1]).abs().max() <= 2.0 ** -14
+
+
+@pytest.mark.parametrize("size", [1e37, 3e38])
+@pytest.mark.parametrize("nq,kv", SHAPES)
+@pytest.mark.parametrize("bits,dim", FORMS)
+def test_values_near_the_largest_fp32(bits, dim, nq, kv, size):
+    """Their weighted mean is in range, so the result is, whatever their sum."""
+    q, k = _normal(5, nq, 2, dim) * 0.25, _normal(6, kv, 1, dim)
+    v = torch.full((kv, 1, dim), size)
+    v[:, :, 1::2] *= -0.5
+    out, lse = _attend(bits, dim, q.bfloat16(), k, v)
+    value = torch.from_numpy(orc.stored(v[:1].double().numpy(), bits))[0, 0]
+    assert torch.isfinite(out).all()
+    # all values alike: weights' roundings and the result's
+    assert ((out.double().cpu() - value).abs() <= (2.0 ** -11 + 2.0 ** -8 + 2.0 ** -17) * value.abs()).all()
+    assert torch.isfinite(lse).all()

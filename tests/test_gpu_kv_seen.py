@@ -90,3 +90,26 @@ def test_keys_and_values_of_any_size(bits, dim, dtype, nq, kv, size):
     a = (q.double().numpy(), orc.stored(k.double().numpy(), bits), orc.stored(v.double().numpy(), bits),
          np.arange(-(-kv // 16))[None], 16, [kv], [0, nq])
     _close(got, _kv_seen.add(orc.attend(*a), *a), dim, dtype, bits)
+
+
+@pytest.mark.parametrize("nq,kv", SHAPES)
+@pytest.mark.parametrize("bits,dim,dtype", FORMS)
+def test_an_infinite_value_that_is_seen(bits, dim, dtype, nq, kv):
+    """One token's value is infinite (stored as the largest fp32) in one dim, and comes
+    early, in the middle or last: that dim of the rows that see it is as large as its
+    weight says, and the total as it was."""
+    for at in (1, kv // 2, kv - 1):
+        c = _Call(nq + kv + at, bits, dim, "bf16", nq, kv, 0, causal=False)
+        v = c.v.clone()
+        v[at, 0, 9] = float("inf")
+        plain, ref = c(c.k, c.v), orc.stored(v.double().numpy(), bits)
+        got = c(c.k, v)
+        # the exponent less the maximum and R, at most 2^8 in size, is rounded: 2^-17 a weight; sums 2^-20
+        assert (plain[1] - got[1]).abs().max() <= 2.0 ** -16
+        a = (c.q.double().cpu().numpy(), orc.stored(c.k.double().numpy(), bits), ref,
+             np.arange(-(-kv // 16))[None], 16, [kv], [0, nq])
+        want = _kv_seen.add(orc.attend(*a, causal=False), *a, causal=False)
+        out = got[0].double().cpu().numpy()
+        t_out, _ = _kv_seen.tolerances(want, dim, torch.finfo(torch.bfloat16).eps / 2, bits, "bf16")
+        assert np.isfinite(out).all()
+        assert (np.abs(out - want["out"]) <= t_out).all()

@@ -273,7 +273,7 @@ __host__ __device__ __forceinline__ int64_t attend_slot_floats(int rows, int dim
 }
 
 // ------------------------------------------------------------------ arithmetic
-constexpr float NEG = -1e30f;                 // "no score yet", finite: no NaN from differences
+constexpr float NEG = -3.402823466e38f;       // "no score yet": below all scores, finite: no NaN from differences
 constexpr float P_SHIFT = 6.f, M_SLACK = 8.f; // log2 units
 // A row's weights, times their values' powers of two 2^T (8 bits: scales in [2^T, 2^(T+1))), are divided
 // by 2^R before they become fp16.  R goes by the greatest of these products that the row has seen, not by

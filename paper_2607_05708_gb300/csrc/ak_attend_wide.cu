@@ -824,11 +824,11 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     bool moves = __any_sync(0xffffffffu, rises);               // O changes its scale
                     // Scores of 2^20 and more are rounded before the maximum is taken from them: of 2^33, x f
                     // unrounded is as much as 2^9 away from the maximum that is its own rounding.
-                    if (moves && !heavy) {
+                    if (moves) {
                         big = big || (rises && fabsf(top) > 1048576.f);
                         any_big = __any_sync(0xffffffffu, big);
                     }
-                    if (any_big && !masked) {
+                    if (any_big && !heavy && !masked) {
                         const float in = big ? f : 1.f;
                         f = big ? 1.f : f;
 #pragma unroll
@@ -881,9 +881,10 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         rr = rn;
                         plain = BITS == 4 && __all_sync(0xffffffffu, rr == 0);
                         // The weights over 2^R: the exponential of the score less both, or, where that could
-                        // leave fp32's range (values beyond 2^64 or so, or below 2^-64), R as a factor.  (A
-                        // row's own R decides how its weights are computed; a row that sees nothing has none.)
-                        const bool far = !unset && abs(rr) > 64;
+                        // leave fp32's range (values beyond 2^64 or so, or below 2^-64) or the score swallows R,
+                        // R as a factor.  (A row's own R and maximum decide how its weights are
+                        // computed; a row that sees nothing has none.)
+                        const bool far = !unset && (abs(rr) > 64 || big);
                         const int r_in = far || unset ? 0 : rr;
                         n1 = -mm - (float)r_in, unit = pow2i(r_in);
                         loop = __any_sync(0xffffffffu, far) || BITS == 4;

@@ -75,3 +75,20 @@ def test_values_near_the_largest_fp32(bits, dim, nq, kv, size):
     # all values alike: weights' roundings and the result's
     assert ((out.double().cpu() - value).abs() <= (2.0 ** -11 + 2.0 ** -8 + 2.0 ** -17) * value.abs()).all()
     assert torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("nq,kv", SHAPES)
+@pytest.mark.parametrize("bits,dim", FORMS)
+def test_scores_far_below_zero(bits, dim, nq, kv):
+    """All scores -6.6e36 or -1.5e32: equal weights all the same."""
+    for size in (1e32, 4.2e36):
+        q, k, v = torch.zeros(nq, 2, dim), torch.zeros(kv, 1, dim), _normal(4, kv, 1, dim)
+        q[:, :, 3], k[:, :, 3] = -1.5, size
+        out, lse = _attend(bits, dim, q.bfloat16(), k, v, scale=1.0)
+        stored = orc.stored(v.double().numpy(), bits)[:, 0]
+        mean = torch.from_numpy(stored.mean(0))
+        # weights equal and exact; values rounded to 2^-17 of their row's largest; fp32 sums, the result
+        bound = 2.0 ** -17 * np.abs(stored).max(1).mean() + 2.0 ** -18 * np.abs(stored).max() + 2.0 ** -8 * mean.abs()
+        assert ((out.double().cpu() - mean).abs() <= bound).all()
+        key = orc.stored(k[:1].double().numpy(), bits)[0, 0, 3]
+        assert torch.allclose(lse.double().cpu(), torch.tensor(-1.5 * key, dtype=torch.float64), rtol=1e-6)

@@ -740,7 +740,12 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     if (h % HPT == 0) {
                         // what the dequantising warps wrote beside the tile, while its scores
                         // are computed
-                        ok = wide_wait(&kfull[st], (x_tile / ST) & 1, dead, p.status);
+                        // A row tile that had no rows in the items before has not followed the keys' barriers, and
+                        // a wait by parity takes a phase two before for its own.  Its scores, of which it
+                        // has seen every phase, come after their tile's keys, and nothing goes on to the
+                        // phase after that without its weights.
+                        if (t > 0 && h == 0) ok = wide_wait(&sfull[t][b], halves >> 1 & 1, dead, p.status);
+                        if (ok) ok = wide_wait(&kfull[st], (x_tile / ST) & 1, dead, p.status);
                         tile_tok = meta[st].tok;
                         if (ok) ok = wide_wait(&sfull[t][b], halves >> 1 & 1, dead, p.status);
                         ok = __all_sync(0xffffffffu, ok);
@@ -986,12 +991,6 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     p.lse[dst] = lse_of(mm, l);
                 }
                 tc_fence_before();
-            } else {
-                // No rows here.  All the same the warps keep up with the tiles: the parity
-                // that they wait for next has to be that of the next phase.
-                for (int it = 0; ok && it < n; ++it)
-                    ok = wide_wait(&kfull[(n_tile + it) % ST], ((n_tile + it) / ST) & 1, dead, p.status);
-                ok = __all_sync(0xffffffffu, ok);
             }
             n_tile += n;
             left -= mine.used, done += mine.used;

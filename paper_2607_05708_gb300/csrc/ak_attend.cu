@@ -331,7 +331,9 @@ k_attend_narrow(const __grid_constant__ AttendParams p, const bool bf16, const i
 
         int tok = cur.unit * STEP;
         for (int it = 0; ok && it < n; ++it, tok += STEP) {
-            if (!mbar_test_wait(bar + stage, phase) && !mbar_wait(bar + stage, phase, p.status)) {
+            // (one answer for all lanes: one that gave up alone would leave the others in a shuffle)
+            if (!__all_sync(0xffffffffu, mbar_test_wait(bar + stage, phase)) &&
+                !__all_sync(0xffffffffu, mbar_wait(bar + stage, phase, p.status))) {
                 ok = false;                    // the other copies still land: wait for them
                 const int out = min(left - it, NS);
                 for (int k = 1; k < out; ++k) {

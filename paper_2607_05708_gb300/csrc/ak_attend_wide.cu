@@ -179,16 +179,19 @@ constexpr uint32_t idesc_f16(int n) {
     return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
-// Bounded wait of one role; when any role's wait has expired the others give up too.
+// Bounded wait of a warp of one role; when any role's wait has expired the others give up too.  One
+// answer for all lanes: a lane that gave up beside others that did not would leave them in
+// their next shuffle.
 __device__ __forceinline__ bool wide_wait(uint64_t *bar, uint32_t parity, volatile int *dead,
                                           int *status) {
-    if (mbar_test_wait(bar, parity)) return true;
-    for (uint32_t i = 0; i < WAIT_LIMIT; ++i) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if ((i & 255u) == 255u && *dead) return false;
+    bool there = mbar_test_wait(bar, parity);
+    for (uint32_t i = 0; !there && i < WAIT_LIMIT; ++i) {
+        there = mbar_try_wait(bar, parity);
+        if ((i & 255u) == 255u && *dead) break;
     }
+    if (__all_sync(0xffffffffu, there)) return true;
+    if (!there && !*dead) set_status(status, AKASHIC_ETIMEOUT);
     *dead = 1;
-    set_status(status, AKASHIC_ETIMEOUT);
     return false;
 }
 
@@ -369,7 +372,7 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
         const int w = warp - C::SOFT, g = lane >> 2, c = lane & 3;
         const bool far = D == 128 && c >= 2, odd = D == 128 && (g & 1);    // (shared memory banks)
         uint32_t n_tile = 0;                   // tiles since the kernel began
-        while (left > 0 && !*dead) {
+        while (left > 0 && !__any_sync(0xffffffffu, *dead)) {
             const AttendPart part = attend_part(cur, left);
             const int n = part.n, units = (cur.q.kv + KV_UNIT - 1) / KV_UNIT;
             if (n <= 0) break;
@@ -602,20 +605,21 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     uint32_t polls = 0;
                     while (ok && v_next < nh) {
                         bool moved = false;
+                        // (one answer for all lanes, as above)
                         if (s_next < nh && s_next - v_next <= 1 &&
-                            mbar_test_wait(&kfull[(n_tile + s_next) % ST], ((n_tile + s_next) / ST) & 1)) {
+                            __all_sync(0xffffffffu, mbar_test_wait(&kfull[(n_tile + s_next) % ST], ((n_tile + s_next) / ST) & 1))) {
                             scores(0, s_next++);
                             moved = true;
                         }
                         const uint32_t c = ph0 + v_next;
-                        if (v_next < s_next && mbar_test_wait(&pfull[0][c & 1], c >> 1 & 1)) {
+                        if (v_next < s_next && __all_sync(0xffffffffu, mbar_test_wait(&pfull[0][c & 1], c >> 1 & 1))) {
                             values(0, v_next);
                             umma_commit_if(go, &empty[(n_tile + v_next++) % ST]);
                             moved = true;
                         }
                         // a bounded wait, like the others (wide_wait)
                         polls = moved ? 0 : polls + 1;
-                        if ((polls & 1023u) == 1023u && *dead) ok = false;
+                        if ((polls & 1023u) == 1023u && __any_sync(0xffffffffu, *dead)) ok = false;
                         if (polls >= SPIN_LIMIT) {
                             *dead = 1;
                             set_status(p.status, AKASHIC_ETIMEOUT);
@@ -748,7 +752,6 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                         if (ok) ok = wide_wait(&kfull[st], (x_tile / ST) & 1, dead, p.status);
                         tile_tok = meta[st].tok;
                         if (ok) ok = wide_wait(&sfull[t][b], halves >> 1 & 1, dead, p.status);
-                        ok = __all_sync(0xffffffffu, ok);
                         if (!ok) break;
                         tc_fence_after();
                     }
@@ -937,7 +940,6 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     if (h > 0 && moves) {
                         // once the products before have been added
                         ok = wide_wait(&odone[t][b ^ 1], (halves - 1) >> 1 & 1, dead, p.status);
-                        ok = __all_sync(0xffffffffu, ok);
                         if (!ok) break;
                         tc_fence_after();
 #pragma unroll 1
@@ -956,7 +958,6 @@ k_attend_wide(const __grid_constant__ AttendParams p, const bool bf16, const int
                     if (lane == 0) mbar_arrive(&pfull[t][b]);
                 }
                 if (ok) ok = wide_wait(&odone[t][(halves - 1) & 1], (halves - 1) >> 1 & 1, dead, p.status);
-                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
                 // ---- whole items are written, others left for the joining kernel

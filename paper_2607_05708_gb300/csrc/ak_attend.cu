@@ -25,11 +25,11 @@
 //    so far keep 11 bits; sums, maxima and accumulators are fp32.  The maximum is raised only when a
 //    score exceeds it by 2^8, so that the accumulators are rarely rescaled.
 // Measured (one query row of 32 heads a sequence, 8 key/value heads, D = 128, 4 bits): 64
-// sequences of 4096, 8192 and 16384 tokens 77, 130 and 237 us, so 5.7 TB/s (84 % of a
-// copy) for what is added and 24 us beside it: the plan and the first fetches (8), the rings'
-// filling and the warps' uneven ends, the join (4).  In the loop some 300 instructions a unit
-// issue in 2.3 of 4 slots (ALU pipe 49 %): they, not the 75 KB in flight an SM, are next to
-// the bytes.  8 heads of 700 tokens 12 us, of which 10 are there for 100 tokens too.
+// sequences of 4096, 8192 and 16384 tokens 80, 134 and 241 us, so 5.7 TB/s (84 % of a
+// copy) for what is added and 26 us beside it: the plan and the first fetches (8), the rings'
+// filling and the warps' uneven ends, the join (4).  In the loop some 310 instructions a unit
+// issue in 2.4 of 4 slots (ALU pipe 49 %): they, not the 75 KB in flight an SM, are next to
+// the bytes.  8 heads of 700 tokens 13 us, of which 10 are there for 100 tokens too.
 #include <atomic>
 
 #include "ak_attend.cuh"
@@ -914,22 +914,22 @@ akashic_status_t attend_check(const akashic_mem_kv_config_t *cfg, const akashic_
 // (query rows times group) one takes them all; else each takes the sequences on
 // its side of wide_from() rows.
 // Microseconds of the kernel for few rows and of the one for many, 4 bits, 2 key/value heads:
-//   16 sequences of 5000 tokens, D = 128: 64 rows 51.7 and 47.8, 80 rows 67.2 and 48.6;
-//       D = 256: 32 rows 62.7 and 62.1, 40 rows 82.1 and 63.3
-//   1024 of 200 tokens, D = 128: 64 rows 212 and 247, 80 rows 289 and 249
+//   16 sequences of 5000 tokens, D = 128: 64 rows 52.0 and 45.3, 80 rows 67.5 and 46.0;
+//       D = 256: 32 rows 63.5 and 61.4, 40 rows 82.5 and 62.9
+//   1024 of 200 tokens, D = 128: 64 rows 199 and 210, 80 rows 283 and 219
 // Where so few items share the GPU that more than 16 CTAs leave parts of one to be
 // joined, and the work is little, the former stays ahead for longer:
-//   one sequence of 20000, D = 128: 128 rows 40.0 and 47.7, 256 rows 52.6 and 56.7;
-//       D = 256: 128 rows 63.5 and 72.8, 256 rows 101 and 70
-//   one of 200000, D = 128: 64 rows 93.3 and 90.8, 128 rows 157 and 94.6
+//   one sequence of 20000, D = 128: 128 rows 40.8 and 41.4, 256 rows 53.1 and 47.0;
+//       D = 256: 128 rows 64.5 and 63.1, 256 rows 99.6 and 64.9
+//   one of 200000, D = 128: 64 rows 92.6 and 87.8, 128 rows 177 and 91.5
 int wide_from(const akashic_mem_kv_config_t *cfg, const akashic_mem_kv_attend_t *a, int sms) {
     const int64_t items = (int64_t)a->n_seq * cfg->heads;
     const bool shared = items * 16 < sms && items * a->max_blocks * cfg->block_tokens < (1 << 17);
-    return cfg->head_dim == 256 ? (shared ? 129 : 33) : (shared ? 257 : 65);
+    return shared ? 129 : cfg->head_dim == 256 ? 33 : 65;
 }
 // Short lists and no more items than CTAs at once: a CTA an item, as planning and joining would
-// take longer than the uneven shares (8 heads of 700 tokens 13.3 and 17.8 us, of 1400
-// 17.5 and 18.2, of 2000 20.0 and 18.7).
+// take longer than the uneven shares (8 heads of 700 tokens 13.1 and 18.2 us, of 1400
+// 17.2 and 18.7, of 2000 19.5 and 18.9).
 constexpr int DIRECT_STEPS = 48;   // of 32 tokens: six a warp
 struct AttendRoute {
     int from = 0;                                 // rows from which the kernel for many takes a sequence

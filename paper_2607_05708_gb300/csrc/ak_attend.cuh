@@ -346,8 +346,8 @@ __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
 
 // cap tanh(x / cap) of a lane's scores, in place (log2 units, like cap).  Where all of the
 // warp's are within 0.7 cap: x q(t), t = (x / cap)^2 <= 1/2, q the polynomial of degree 5
-// nearest to tanh(sqrt t) / sqrt t there in relative error (1.5e-8; fitted by
-// iteratively reweighted least squares), two scores an instruction.  Else
+// nearest to tanh(sqrt t) / sqrt t there in relative error (3.6e-8 with its coefficients in fp32; fitted
+// by iteratively reweighted least squares), two scores an instruction.  Else
 // 1 - 2 / (1 + e^(2y)), which alone would lose small scores under a large cap.
 template <int N>
 __device__ __forceinline__ void cap_scores(uint32_t (&x)[N], float cap) {

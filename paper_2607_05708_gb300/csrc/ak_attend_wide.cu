@@ -27,10 +27,11 @@
 // A weight times its value's factor is divided by the row's 2^R before it becomes fp16.  R goes by what the
 // row has seen: raised, and O rescaled, only when a product would pass 2^14 (R_SLACK); 0 while all
 // of the row's values have been within the window.
-// Measured (4 bits): two requests of 2048 rows behind 10240 tokens, 32 heads on 8, D = 128 (514
-// GFLOP) 682 us, 0.75 PFLOP/s, and 905 us with capped scores; a step of 256 rows and 128
-// tokens 2.8 us, of which the products are 1.06: scores, softmax and O += P V of a row tile
-// follow each other, and tensor memory (O of two tiles, and S) has no room for a second S.
+// Measured (4 bits): requests of 2048 and 1668 rows behind 10240 and 8341 tokens, 32 heads on 8, D = 128 (514
+// GFLOP) 749 us, 0.69 PFLOP/s, and 1013 us with capped scores; some 3.4 us a step of 256 rows and
+// 128 tokens, items' ends apart, of which the products are 1.06: scores, softmax and O += P V of a
+// row tile follow each other, and tensor memory (O of two tiles, and S) has no room for a
+// second S at D = 128.  One request of 2048 rows behind 8192 tokens: D = 64 272, 128 351, 256 869 us.
 #include <stddef.h>
 
 #include <atomic>
@@ -54,11 +55,12 @@ struct Wide {
     // warpgroups are split by need, so that a unit of a tile has a warp of its own.
     // For softmax, dequantising, the last one, a thread; together the 96 of the launch.  Requests
     // of 2048 and 1600 rows behind 10240 and 8000 tokens, 32 heads on 8, D = 128, us:
-    //                    120, 80, 80   144, 72, 48   152, 64, 48   160, 56, 48   168, 48, 48
-    //   4 bits                   820           725           720           724           773
-    //   4 bits, capped          1165          1127           924           949          1031
-    //   8 bits                   976           809           806           888           947
-    static constexpr int regs(int role) { return role == 0 ? 152 : role == 1 ? 64 : 48; }
+    //                    120, 80, 80   136, 80, 48   144, 72, 48   152, 64, 48   160, 56, 48
+    //   4 bits                   691           711           712           710           706
+    //   4 bits, capped           908           915           921           906           923
+    //   8 bits                  1273          1001           929           782           786
+    //   8 bits, capped          1672          1349          1280          1158          1117
+    static constexpr int regs(int role) { return role == 0 ? 160 : role == 1 ? 56 : 48; }
     static constexpr bool SPLIT = MT == 2;
     static constexpr int SOFT = 4 * MT, DEQ = SPLIT ? 8 : 4;
     static constexpr int THREADS = 32 * (SOFT + DEQ + (SPLIT ? 4 : 1));
@@ -66,8 +68,8 @@ struct Wide {
     static_assert(UNITS == DEQ, "a dequantising warp has one unit of every tile");
     static constexpr int STAGES = 2;
     // An item's beginning and end (query rows in, result out, an empty pipeline: 7 to 10 us; a step
-    // 2.8) count as steps: 0, 1, 2 and 3 of them 131, 110, 113 and 124 us for 7 documents in
-    // 6007 tokens at D = 64, 8 bits; 148, 116, 113 and 123 at D = 128, 4 bits.
+    // 3) count as steps: 0, 1, 2 and 3 of them 145, 124, 124 and 130 us for 7 documents in
+    // 6007 tokens at D = 64, 8 bits; 177, 146, 143 and 149 at D = 128, 4 bits (L2 cold).
     static constexpr int EXTRA = 2;
     static constexpr int Q_BYTES = ROWS * D * 2, KV_BYTES = N * D * 2;
     static constexpr int S_COL = MT * D;                 // tensor memory: O, then S

@@ -415,7 +415,9 @@ akashic_status_t akashic_mem_kv_cache_bytes(const akashic_mem_kv_config_t *cfg, 
  *   slots     device int64[n]: the slot of each token, -1 to skip it (its k and
  *             v are not read).  A slot may appear only once in a call
  *   tags      device int32, one a slot, or NULL: the tags of written slots are set to
- *   new_tags  device int32[n], or to 0 where new_tags is NULL
+ *   new_tags  device int32[n], or to 0 where new_tags is NULL.  A slot keeps its token and tag until
+ *             it is written again: where a block is given to fewer tokens than it held,
+ *             the caller sets the tags of the others to -1
  * EINVAL for a bad config, dtype, n outside [0, 2^31 - 1], a NULL or misaligned
  * pointer, or new_tags without tags; ECUDA if the launch fails. */
 akashic_status_t akashic_mem_kv_write(const akashic_mem_kv_config_t *cfg, void *cache,
@@ -443,7 +445,10 @@ akashic_status_t akashic_mem_kv_read(const akashic_mem_kv_config_t *cfg, const v
  *   out = sum_j exp(z_j) v_j / sum_j exp(z_j),  lse = log sum_j exp(z_j)
  * over the keys that the row sees: those of entries other than -1 with
  * j < kv_len, and, if causal, j <= pos or j < prefix_len[s], and, with tags, a tag
- * that equals the row's and is >= 0.  A row that sees none gives 0, lse -inf.
+ * that equals the row's and is >= 0.  A row that sees none gives 0, lse -inf.  What a row
+ * does not see, be it infinite, changes no bit of its result (with a cap: nothing beyond the
+ * scores' rounding).  Weights meet values in 16 bits: 11 bits of a weight, fewer where
+ * it, times its value's power of two, is below 2^-16 of the row's largest, none below 2^-27.
  * Query rows behind the last sequence are not read, nor their results written. */
 typedef struct {
     const void *q;             /* device, (row, head, d) at row * q_row_stride + head *

@@ -384,7 +384,9 @@ class KVCache:
     A block per stored chunk, block ID = chunk ID, makes what
     MemStore.retrieve returns the list of blocks to attend over.  With
     `tagged`, every slot has an int32 tag (-1 while it holds no token): a
-    namespace or a document, which attention can be restricted to.  No
+    namespace or a document, which attention can be restricted to.  A slot keeps
+    its token and tag until it is written again: set `tags` to -1 where a
+    block is given to fewer tokens than it held.  No
     gradient is recorded through any of the calls.  The memory is `data`
     (uint8), `tags` (int32 [n_blocks * block_tokens] or None) and `status`
     (int32 [1], read and cleared by sync())."""

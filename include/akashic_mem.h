@@ -427,6 +427,42 @@ akashic_status_t akashic_mem_kv_write(const akashic_mem_kv_config_t *cfg, void *
                                       const int64_t *slots, const int32_t *new_tags,
                                       int32_t *status, void *stream);
 
+/* The rotation of rows to their positions, for the append calls.  Of a row's first
+ * rotary_dim values pair i, (x[i], x[i + rotary_dim / 2]) or, interleaved, (x[2i],
+ * x[2i + 1]), becomes (a c - b s, b c + a s), c = cos[position][i] and s =
+ * sin[position][i]: in fp32, each product and the sum rounded once.
+ * Query rows of the same tokens can be rotated in the same call: q_out may be q
+ * itself with the same strides (not another overlapping array). */
+typedef struct {
+    const int64_t *positions;  /* device int64[n]                                    */
+    const float *cos, *sin;    /* device float[table_rows][rotary_dim / 2], 16-byte
+                                  aligned                                            */
+    int64_t table_rows;        /* positions lie in [0, table_rows)                   */
+    int32_t rotary_dim;        /* multiple of 32, at most the width of the rows      */
+    int32_t interleaved;
+    const void *q;             /* device, (token, head, d) at token * q_row_stride +
+                                  head * q_head_stride + d, of the call's dtype, or
+                                  NULL                                               */
+    int64_t q_row_stride, q_head_stride;
+    int32_t q_heads;
+    void *q_out;               /* rows of q, rounded once to dtype; zeros for tokens
+                                  that are skipped                                   */
+    int64_t q_out_row_stride, q_out_head_stride;
+} akashic_mem_rotation_t;
+
+/* akashic_mem_kv_write with the keys rotated on the way (values are not): what is
+ * quantised is the rotation's fp32 result.  Query rows are head_dim wide; what lies behind
+ * rotary_dim is copied.  A token whose slot is -1 is skipped, its position not read; one whose
+ * slot or position is out of range is recorded (EDEVICE) and skipped.
+ * EINVAL as akashic_mem_kv_write, and for a bad rotation (as noted above). */
+akashic_status_t akashic_mem_kv_append(const akashic_mem_kv_config_t *cfg, void *cache,
+                                       int32_t *tags, const void *k, int64_t k_row_stride,
+                                       int64_t k_head_stride, const void *v, int64_t v_row_stride,
+                                       int64_t v_head_stride, int32_t dtype, int64_t n,
+                                       const int64_t *slots, const int32_t *new_tags,
+                                       const akashic_mem_rotation_t *rotation, int32_t *status,
+                                       void *stream);
+
 /* The values that the cache stands for, rounded once to dtype: k, v device
  * [n][heads][head_dim], contiguous, rows of slot -1 zero.  A slot may appear any
  * number of times.  Errors as akashic_mem_kv_write. */
@@ -487,6 +523,101 @@ akashic_status_t akashic_mem_kv_attend_scratch(const akashic_mem_kv_config_t *cf
 akashic_status_t akashic_mem_kv_attend(const akashic_mem_kv_config_t *cfg, const void *cache,
                                        const akashic_mem_kv_attend_t *a, void *scratch,
                                        int64_t scratch_bytes, int32_t *status, void *stream);
+
+/* ------------------------------------------------------------------ latent vectors
+ * The cache of models whose heads share one latent vector a token: a slot holds a row
+ * [latent | rotated key] of latent_dim + rope_dim values in 16 bits, and two forms of the
+ * attention that reads it.  With c_j the latent vector and r_j the rotated part of token j,
+ *   absorbed:  the caller has taken the query heads into the latent space;
+ *              z = scale (<q[:latent_dim], c_j> + <q[latent_dim:], r_j>),  values c_j;
+ *   expanded:  every head has a key w_k c_j and a value w_v c_j;
+ *              z = scale (<q[:nope_dim], w_k c_j> + <q[nope_dim:], r_j>).
+ * The absorbed form reads each row once for all heads: for single tokens and drafts.
+ * The expanded form has fewer products where a sequence has hundreds of rows: for prompts.
+ * Sequences, lists of blocks, masks, tags, scratch, status and streams are those of
+ * akashic_mem_kv_attend: a block per chunk of the store makes retrieved IDs the list.
+ *
+ * The cache is device memory, n_blocks * block_tokens rows, contiguous, 16-byte aligned,
+ * and holds finite values throughout: zeroed before its first use, then written by
+ * akashic_mem_latent_append, which stores NaN as 0 and what is beyond the type's range as
+ * its largest value.  So what a row does not see meets only weights of 0. */
+typedef struct {
+    int32_t latent_dim;   /* 128, 256 or 512                                       */
+    int32_t rope_dim;     /* 32 or 64                                              */
+    int32_t block_tokens; /* multiple of 16, 16..4096                              */
+    int32_t dtype;        /* BF16 or FP16                                          */
+    int64_t n_blocks;     /* >= 1, n_blocks * block_tokens <= 2^31 - 2^13          */
+    int32_t device;       /* CUDA device ordinal                                   */
+} akashic_mem_latent_config_t;
+
+/* Bytes of the cache. */
+akashic_status_t akashic_mem_latent_cache_bytes(const akashic_mem_latent_config_t *cfg,
+                                                int64_t *bytes);
+
+/* Round n tokens into their slots.
+ *   latent    device, dtype BF16, FP16 or FP32, value (i, d) at i * latent_stride + d
+ *   k_rope    device, the same with rope_dim values a token
+ *   slots, tags, new_tags  as for akashic_mem_kv_write
+ *   rotation  NULL: k_rope is stored as it is.  Else k_rope, and query rows of rope_dim
+ *             values if given, are rotated; rotary_dim must be rope_dim
+ * Errors as akashic_mem_kv_append. */
+akashic_status_t akashic_mem_latent_append(const akashic_mem_latent_config_t *cfg, void *cache,
+                                           int32_t *tags, const void *latent,
+                                           int64_t latent_stride, const void *k_rope,
+                                           int64_t k_rope_stride, int32_t dtype, int64_t n,
+                                           const int64_t *slots, const int32_t *new_tags,
+                                           const akashic_mem_rotation_t *rotation,
+                                           int32_t *status, void *stream);
+
+/* Arguments of both forms; fields named as in akashic_mem_kv_attend_t mean the same.  q and
+ * out are of the cache's type.  Scores, maxima and totals are fp32; weights, and the expanded
+ * form's keys and values, are rounded to the cache's type before their products. */
+typedef struct {
+    const void *q;             /* device; absorbed: rows of latent_dim + rope_dim, expanded:
+                                  of nope_dim + rope_dim values                      */
+    int64_t q_row_stride, q_head_stride;
+    int32_t n_q, q_heads;      /* q_heads 1..1024                                    */
+    int32_t n_seq;
+    const int32_t *q_start;
+    const int32_t *kv_len;
+    const int64_t *blocks;
+    int64_t max_blocks;
+    int32_t causal;
+    const int32_t *prefix_len;
+    float scale;               /* not 0                                              */
+    const int32_t *tags;
+    const int32_t *q_tags;
+    void *out;                 /* device [n_q][q_heads][latent_dim or value_dim], 4-byte
+                                  aligned                                            */
+    float *lse;                /* device float[n_q][q_heads] or NULL; expanded: NULL */
+    /* expanded only */
+    const void *w_k, *w_v;     /* device, of the cache's type, 16-byte aligned: row d of
+                                  head h at h * head_stride + d * row_stride, latent_dim
+                                  values                                             */
+    int64_t w_k_head_stride, w_k_row_stride, w_v_head_stride, w_v_row_stride;
+    int32_t nope_dim;          /* rows of w_k: 64 or 128                             */
+    int32_t value_dim;         /* rows of w_v: 64 or 128                             */
+} akashic_mem_latent_attend_t;
+
+/* Bytes of scratch of a call, as akashic_mem_kv_attend_scratch. */
+akashic_status_t akashic_mem_latent_attend_scratch(const akashic_mem_latent_config_t *cfg,
+                                                   const akashic_mem_latent_attend_t *a,
+                                                   int64_t *bytes);
+akashic_status_t akashic_mem_latent_expanded_scratch(const akashic_mem_latent_config_t *cfg,
+                                                     const akashic_mem_latent_attend_t *a,
+                                                     int64_t *bytes);
+
+/* EINVAL, ECUDA as akashic_mem_kv_attend; EINVAL for weights' strides that are not multiples
+ * of 8, or head strides that are not multiples of the row stride. */
+akashic_status_t akashic_mem_latent_attend(const akashic_mem_latent_config_t *cfg,
+                                           const void *cache,
+                                           const akashic_mem_latent_attend_t *a, void *scratch,
+                                           int64_t scratch_bytes, int32_t *status, void *stream);
+akashic_status_t akashic_mem_latent_attend_expanded(const akashic_mem_latent_config_t *cfg,
+                                                    const void *cache,
+                                                    const akashic_mem_latent_attend_t *a,
+                                                    void *scratch, int64_t scratch_bytes,
+                                                    int32_t *status, void *stream);
 
 /* Thread-local description of the last failure on this thread ("" if none). */
 const char *akashic_mem_last_error(void);

@@ -4,8 +4,8 @@ Thin Python binding of the C ABI in ``include/akashic_mem.h``
 (``libakashic_mem.so``, built in-tree by ``_build.build()``).  It only
 marshals arguments: every step of retrieval (score, relation propagation,
 top-k, page resolve), of the relation update (cosine top-M, CSR insert) and of the
-quantised key and value cache (write, read, attention) runs in the library's
-CUDA kernels.  PyTorch is used for device memory and
+quantised key and value cache (write, read, rotation, attention) and the latent cache (append,
+attention) runs in the library's CUDA kernels.  PyTorch is used for device memory and
 streams.  There is no CPU fallback: without the built library every call
 raises.
 """
@@ -17,7 +17,7 @@ import os
 from ._build import LIB as LIB_PATH
 from ._build import build
 
-__all__ = ["MemStore", "KVCache", "AkashicError", "load_library", "build", "EXPORTS", "STATUS", "PHASES",
+__all__ = ["MemStore", "KVCache", "LatentCache", "AkashicError", "load_library", "build", "EXPORTS", "STATUS", "PHASES",
            "softmax_scores_noalloc", "sort_pairs"]
 
 STATUS = {0: "OK", 1: "EINVAL", 2: "ENOMEM", 3: "ECAPACITY", 4: "ECUDA", 5: "ETIMEOUT",
@@ -35,7 +35,9 @@ EXPORTS = (
     "akashic_mem_relocate", "akashic_mem_compact_pages", "akashic_mem_page_stats",
     "akashic_mem_export_pages", "akashic_mem_check_wait_timeout", "akashic_mem_sort_pairs",
     "akashic_mem_kv_cache_bytes", "akashic_mem_kv_write", "akashic_mem_kv_read",
-    "akashic_mem_kv_attend_scratch", "akashic_mem_kv_attend",
+    "akashic_mem_kv_attend_scratch", "akashic_mem_kv_attend", "akashic_mem_kv_append",
+    "akashic_mem_latent_cache_bytes", "akashic_mem_latent_append", "akashic_mem_latent_attend_scratch",
+    "akashic_mem_latent_expanded_scratch", "akashic_mem_latent_attend", "akashic_mem_latent_attend_expanded",
 )
 
 
@@ -68,6 +70,36 @@ class _KVAttend(ctypes.Structure):
                 ("scale", ctypes.c_float), ("cap", ctypes.c_float), ("slopes", ctypes.c_void_p),
                 ("tags", ctypes.c_void_p), ("q_tags", ctypes.c_void_p), ("out", ctypes.c_void_p),
                 ("lse", ctypes.c_void_p)]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p),
+                ("table_rows", ctypes.c_int64), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("q", ctypes.c_void_p),
+                ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+                ("q_heads", ctypes.c_int32), ("q_out", ctypes.c_void_p),
+                ("q_out_row_stride", ctypes.c_int64), ("q_out_head_stride", ctypes.c_int64)]
+
+
+class _LatentConfig(ctypes.Structure):
+    _fields_ = [("latent_dim", ctypes.c_int32), ("rope_dim", ctypes.c_int32),
+                ("block_tokens", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("n_blocks", ctypes.c_int64), ("device", ctypes.c_int32)]
+
+
+class _LatentAttend(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_row_stride", ctypes.c_int64),
+                ("q_head_stride", ctypes.c_int64), ("n_q", ctypes.c_int32),
+                ("q_heads", ctypes.c_int32), ("n_seq", ctypes.c_int32),
+                ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("blocks", ctypes.c_void_p), ("max_blocks", ctypes.c_int64),
+                ("causal", ctypes.c_int32), ("prefix_len", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("tags", ctypes.c_void_p), ("q_tags", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("w_k", ctypes.c_void_p),
+                ("w_v", ctypes.c_void_p), ("w_k_head_stride", ctypes.c_int64),
+                ("w_k_row_stride", ctypes.c_int64), ("w_v_head_stride", ctypes.c_int64),
+                ("w_v_row_stride", ctypes.c_int64), ("nope_dim", ctypes.c_int32),
+                ("value_dim", ctypes.c_int32)]
 
 
 _lib = None
@@ -119,7 +151,17 @@ def load_library(path: str | None = None):
                                            P64], ctypes.c_int),
         "akashic_mem_kv_attend": ([ctypes.POINTER(_KVConfig), V, ctypes.POINTER(_KVAttend), V, I64,
                                    V, V], ctypes.c_int),
+        "akashic_mem_kv_append": ([ctypes.POINTER(_KVConfig), V, V, V, I64, I64, V, I64, I64, I32,
+                                   I64, V, V, ctypes.POINTER(_Rotation), V, V], ctypes.c_int),
+        "akashic_mem_latent_cache_bytes": ([ctypes.POINTER(_LatentConfig), P64], ctypes.c_int),
+        "akashic_mem_latent_append": ([ctypes.POINTER(_LatentConfig), V, V, V, I64, V, I64, I32, I64, V, V,
+                                       ctypes.POINTER(_Rotation), V, V], ctypes.c_int),
     }
+    latent = [ctypes.POINTER(_LatentConfig), V, ctypes.POINTER(_LatentAttend), V, I64, V, V]
+    for name in ("attend", "attend_expanded"):
+        sig[f"akashic_mem_latent_{name}"] = (latent, ctypes.c_int)
+    for name in ("attend", "expanded"):
+        sig[f"akashic_mem_latent_{name}_scratch"] = ([latent[0], latent[2], P64], ctypes.c_int)
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -377,50 +419,33 @@ class MemStore:
         return {p: (ms[i], ln[i]) for i, p in enumerate(PHASES)}
 
 
-class KVCache:
-    """Keys and values of `heads` heads in 4 or 8 bits, in blocks of
-    `block_tokens` tokens (akashic_mem_kv_*; the format is in the header).
+class _BlockCache:
+    """What the caches share: device, streams, checks of tensors, the status word."""
 
-    A block per stored chunk, block ID = chunk ID, makes what
-    MemStore.retrieve returns the list of blocks to attend over.  With
-    `tagged`, every slot has an int32 tag (-1 while it holds no token): a
-    namespace or a document, which attention can be restricted to.  A slot keeps
-    its token and tag until it is written again: set `tags` to -1 where a
-    block is given to fewer tokens than it held.  No
-    gradient is recorded through any of the calls.  The memory is `data`
-    (uint8), `tags` (int32 [n_blocks * block_tokens] or None) and `status`
-    (int32 [1], read and cleared by sync())."""
-
-    def __init__(self, n_blocks: int, heads: int, head_dim: int, block_tokens: int = 64,
-                 bits: int = 4, device: int = 0, tagged: bool = False):
+    def _open(self, n_blocks, block_tokens, device, tagged):
         import torch
         self._torch = torch
         self._lib = load_library()
-        self.n_blocks, self.heads, self.head_dim = n_blocks, heads, head_dim
-        self.block_tokens, self.bits, self.device = block_tokens, bits, device
-        self._cfg = ctypes.byref(_KVConfig(bits, heads, head_dim, block_tokens, n_blocks, device))
-        size = ctypes.c_int64()
-        _check(self._lib.akashic_mem_kv_cache_bytes(self._cfg, ctypes.byref(size)))
-        dev = torch.device("cuda", device)
-        self.data = torch.empty(size.value, dtype=torch.uint8, device=dev)
-        self.tags = (torch.full((n_blocks * block_tokens,), -1, dtype=torch.int32, device=dev)
-                     if tagged else None)
-        self.status = torch.zeros(1, dtype=torch.int32, device=dev)
-        # the first call may be on another stream than the one that filled these
-        torch.cuda.current_stream(dev).synchronize()
+        self.n_blocks, self.block_tokens, self.device = n_blocks, block_tokens, device
         self._dtypes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
         self._scratch = {}
-        # what every call needs, looked up once
-        self._dev = self.data.device
+        self._tagged = tagged
+
+    def _fill(self, data):
+        """The cache's memory, and what every call needs, looked up once."""
+        torch = self._torch
+        self.data, self._dev = data, data.device
+        self.tags = (torch.full((self.n_blocks * self.block_tokens,), -1, dtype=torch.int32, device=self._dev)
+                     if self._tagged else None)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self._dev)
+        # the first call may be on another stream than the one that filled these
+        torch.cuda.current_stream(self._dev).synchronize()
         # the current stream's handle without a Stream object (4 us a call)
         self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda device: torch.cuda.current_stream(device).cuda_stream)
         self._data_ptr, self._status_ptr = self.data.data_ptr(), self.status.data_ptr()
         self._tags_ptr = None if self.tags is None else self.tags.data_ptr()
-        self._write, self._read = self._lib.akashic_mem_kv_write, self._lib.akashic_mem_kv_read
-        self._attend = self._lib.akashic_mem_kv_attend
 
-    # -- helpers
     def _vec(self, t, dtype, name, numel):
         """The pointer of a contiguous tensor of that type and length (None: NULL)."""
         if t is None:
@@ -433,8 +458,8 @@ class KVCache:
             raise ValueError(f"{name} must be contiguous, of {numel} elements")
         return t.data_ptr()
 
-    def _rows(self, t, name, heads=None):
-        """dtype code, shape and strides of rows [n, heads, head_dim] whose last
+    def _rows(self, t, name, width, heads=None):
+        """dtype code, shape and strides of rows [n, heads, width] whose last
         dimension is contiguous."""
         code = self._dtypes.get(t.dtype)
         if code is None:
@@ -442,8 +467,8 @@ class KVCache:
         if t.get_device() != self.device:
             raise ValueError(f"{name} must be a CUDA tensor on device {self.device}")
         shape, strides = t.shape, t.stride()
-        if len(shape) != 3 or shape[2] != self.head_dim or (heads and shape[1] != heads):
-            raise ValueError(f"{name} must be [n, {heads or 'heads'}, {self.head_dim}]")
+        if len(shape) != 3 or shape[2] != width or (heads and shape[1] != heads):
+            raise ValueError(f"{name} must be [n, {heads or 'heads'}, {width}]")
         if strides[2] != 1 and t.numel():
             raise ValueError(f"{name} must be contiguous in its last dimension")
         return code, shape, strides
@@ -460,6 +485,86 @@ class KVCache:
     def _on(self, stream):
         return self._current(self.device) if stream is None else stream.cuda_stream
 
+    def _rotation(self, n, width, dt, positions, cos, sin, q, q_out, interleaved, stream):
+        """The rotation of n tokens as the ABI takes it, and q_out."""
+        f32 = self._torch.float32
+        if positions is None or cos is None or sin is None:
+            raise ValueError("a rotation needs positions, cos and sin")
+        if cos.dim() != 2 or sin.shape != cos.shape:
+            raise ValueError("cos and sin must be [positions, rotary_dim / 2]")
+        rows, half = cos.shape
+        r = _Rotation(self._vec(positions, self._torch.int64, "positions", n),
+                      self._vec(cos, f32, "cos", rows * half), self._vec(sin, f32, "sin", rows * half), rows,
+                      2 * half, 1 if interleaved else 0)
+        if q is None:
+            if q_out is not None:
+                raise ValueError("q_out needs q")
+            return r, None
+        code, shape, st = self._rows(q, "q", width)
+        if code != dt or shape[0] != n:
+            raise ValueError(f"q must be of the rows' type, {n} tokens")
+        if q_out is None:
+            q_out = self._empty(shape, q.dtype, stream)
+            so = q_out.stride()
+        else:
+            code, other, so = self._rows(q_out, "q_out", width)
+            if code != dt or other != shape:
+                raise ValueError("q_out must be of q's type and shape")
+        r.q, r.q_row_stride, r.q_head_stride, r.q_heads = q.data_ptr(), st[0], st[1], shape[1]
+        r.q_out, r.q_out_row_stride, r.q_out_head_stride = q_out.data_ptr(), so[0], so[1]
+        return r, q_out
+
+    def sync(self, stream=None):
+        """Wait for the stream, then raise (and clear) what the kernels recorded: a slot,
+        block ID, length or row range out of bounds (EDEVICE), an expired wait."""
+        s = stream if stream is not None else self._torch.cuda.current_stream(self.device)
+        s.synchronize()
+        code = int(self.status.item())
+        if code:
+            self.status.zero_()
+            self._torch.cuda.current_stream(self.device).synchronize()   # before any other stream's calls
+            raise AkashicError(code, f"{self._name}: an index or length was out of bounds" if code == 6
+                               else f"{self._name}: a kernel of the cache failed")
+
+
+class KVCache(_BlockCache):
+    """Keys and values of `heads` heads in 4 or 8 bits, in blocks of
+    `block_tokens` tokens (akashic_mem_kv_*; the format is in the header).
+
+    A block per stored chunk, block ID = chunk ID, makes what
+    MemStore.retrieve returns the list of blocks to attend over.  With
+    `tagged`, every slot has an int32 tag (-1 while it holds no token): a
+    namespace or a document, which attention can be restricted to.  A slot keeps
+    its token and tag until it is written again: set `tags` to -1 where a
+    block is given to fewer tokens than it held.  No
+    gradient is recorded through any of the calls.  The memory is `data`
+    (uint8), `tags` (int32 [n_blocks * block_tokens] or None) and `status`
+    (int32 [1], read and cleared by sync())."""
+
+    _name = "kv"
+
+    def __init__(self, n_blocks: int, heads: int, head_dim: int, block_tokens: int = 64,
+                 bits: int = 4, device: int = 0, tagged: bool = False):
+        self._open(n_blocks, block_tokens, device, tagged)
+        torch = self._torch
+        self.heads, self.head_dim, self.bits = heads, head_dim, bits
+        self._cfg = ctypes.byref(_KVConfig(bits, heads, head_dim, block_tokens, n_blocks, device))
+        size = ctypes.c_int64()
+        _check(self._lib.akashic_mem_kv_cache_bytes(self._cfg, ctypes.byref(size)))
+        self._fill(torch.empty(size.value, dtype=torch.uint8, device=torch.device("cuda", device)))
+        self._write, self._read = self._lib.akashic_mem_kv_write, self._lib.akashic_mem_kv_read
+        self._append, self._attend = self._lib.akashic_mem_kv_append, self._lib.akashic_mem_kv_attend
+
+    def _kv(self, k, v, tags):
+        """Checks of keys and values: dtype code, tokens, strides."""
+        dt, shape, sk = self._rows(k, "k", self.head_dim, self.heads)
+        dtv, shape_v, sv = self._rows(v, "v", self.head_dim, self.heads)
+        if dtv != dt or shape_v != shape:
+            raise ValueError("k and v must be of one type and shape")
+        if tags is not None and self.tags is None:
+            raise ValueError("tags need a tagged cache")
+        return dt, shape[0], sk, sv
+
     # -- ABI
     def write(self, k, v, slots, tags=None, stream=None):
         """Quantise k, v [n, heads, head_dim] (bfloat16, float16 or float32; any strides
@@ -467,13 +572,7 @@ class KVCache:
         place; -1 skips a row; a slot at most once).  tags (int32 [n], tagged caches
         only): the tags of the rows, 0 if not given."""
         torch = self._torch
-        dt, shape, sk = self._rows(k, "k", self.heads)
-        dtv, shape_v, sv = self._rows(v, "v", self.heads)
-        if dtv != dt or shape_v != shape:
-            raise ValueError("k and v must be of one type and shape")
-        n = shape[0]
-        if tags is not None and self.tags is None:
-            raise ValueError("tags need a tagged cache")
+        dt, n, sk, sv = self._kv(k, v, tags)
         rc = self._write(self._cfg, self._data_ptr, self._tags_ptr, k.data_ptr(), sk[0], sk[1],
                          v.data_ptr(), sv[0], sv[1], dt, n,
                          self._vec(slots, torch.int64, "slots", n),
@@ -481,6 +580,24 @@ class KVCache:
                          self._on(stream))
         if rc:
             _check(rc)
+
+    def append(self, k, v, slots, positions, cos, sin, q=None, q_out=None, interleaved=False, tags=None,
+               stream=None):
+        """write() with the keys rotated to their positions (int64 [n]) on the way: of a head's
+        first 2 * cos.shape[1] values (a multiple of 32) pair i, (x[i], x[i + half]) or, interleaved,
+        (x[2i], x[2i + 1]), is turned by the angle whose cosine and sine the tables
+        (float32 [positions, pairs]) hold.  q [n, q_heads, head_dim] of k's type: rotated too
+        and returned, in q_out (q itself, or another tensor that does not overlap it)
+        if given; zero for tokens that are skipped."""
+        dt, n, sk, sv = self._kv(k, v, tags)
+        r, q_out = self._rotation(n, self.head_dim, dt, positions, cos, sin, q, q_out, interleaved, stream)
+        rc = self._append(self._cfg, self._data_ptr, self._tags_ptr, k.data_ptr(), sk[0], sk[1], v.data_ptr(),
+                          sv[0], sv[1], dt, n, self._vec(slots, self._torch.int64, "slots", n),
+                          self._vec(tags, self._torch.int32, "tags", n), ctypes.byref(r), self._status_ptr,
+                          self._on(stream))
+        if rc:
+            _check(rc)
+        return q_out
 
     def read(self, slots, dtype=None, k=None, v=None, stream=None):
         """The values that slots (int64 [n], -1: zeros) stand for: k, v [n, heads,
@@ -523,7 +640,7 @@ class KVCache:
         lse float32 [n_q, q_heads]); rows behind the last sequence are left as they
         were (zero in tensors allocated here)."""
         torch = self._torch
-        dt, (n_q, q_heads, _), sq = self._rows(q, "q")
+        dt, (n_q, q_heads, _), sq = self._rows(q, "q", self.head_dim)
         if dt == 2:
             raise TypeError("q must be bfloat16 or float16, got torch.float32")
         if blocks.dim() != 2:
@@ -566,14 +683,142 @@ class KVCache:
             _check(rc)
         return out, lse
 
-    def sync(self, stream=None):
-        """Wait for the stream, then raise (and clear) what the kernels recorded: a slot,
-        block ID, length or row range out of bounds (EDEVICE), an expired wait."""
-        s = stream if stream is not None else self._torch.cuda.current_stream(self.device)
-        s.synchronize()
-        code = int(self.status.item())
-        if code:
-            self.status.zero_()
-            self._torch.cuda.current_stream(self.device).synchronize()   # before any other stream's calls
-            raise AkashicError(code, "kv: an index or length was out of bounds" if code == 6
-                               else "kv: a kernel of the cache failed")
+
+class LatentCache(_BlockCache):
+    """One latent vector and one rotated key a token, shared by all heads, in bfloat16 or
+    float16, in blocks of `block_tokens` tokens (akashic_mem_latent_*).
+
+    A block per stored chunk, block ID = chunk ID, makes what MemStore.retrieve returns the
+    list of blocks to attend over; `tagged` as for KVCache.  No gradient is recorded
+    through any of the calls.  The memory is `data` [n_blocks * block_tokens,
+    latent_dim + rope_dim] (zero until it is written; it has to stay finite), `tags`
+    and `status` as KVCache's."""
+
+    _name = "latent"
+
+    def __init__(self, n_blocks: int, latent_dim: int, rope_dim: int, block_tokens: int = 64,
+                 dtype=None, device: int = 0, tagged: bool = False):
+        self._open(n_blocks, block_tokens, device, tagged)
+        torch = self._torch
+        self.latent_dim, self.rope_dim, self.dtype = latent_dim, rope_dim, dtype or torch.bfloat16
+        if self.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError(f"dtype must be bfloat16 or float16, got {dtype}")
+        self._cfg = ctypes.byref(_LatentConfig(latent_dim, rope_dim, block_tokens, self._dtypes[self.dtype],
+                                               n_blocks, device))
+        size = ctypes.c_int64()
+        _check(self._lib.akashic_mem_latent_cache_bytes(self._cfg, ctypes.byref(size)))
+        self._fill(torch.zeros(n_blocks * block_tokens, latent_dim + rope_dim, dtype=self.dtype,
+                               device=torch.device("cuda", device)))
+        self._append = self._lib.akashic_mem_latent_append
+        self._calls = {False: (self._lib.akashic_mem_latent_attend, self._lib.akashic_mem_latent_attend_scratch),
+                       True: (self._lib.akashic_mem_latent_attend_expanded,
+                              self._lib.akashic_mem_latent_expanded_scratch)}
+
+    def append(self, latent, k_rope, slots, positions=None, cos=None, sin=None, q=None, q_out=None,
+               interleaved=False, tags=None, stream=None):
+        """Round latent [n, latent_dim] and k_rope [n, rope_dim] (bfloat16, float16 or float32; any
+        stride of the first dimension) into slots (as KVCache.write), k_rope rotated
+        where positions, cos and sin (float32 [positions, rope_dim / 2]) are given, and with it
+        q [n, q_heads, rope_dim] as in KVCache.append.  Returns q_out (None without q)."""
+        dt, (n, _, _), sl = self._rows(latent[:, None], "latent", self.latent_dim, 1)
+        dtk, (nk, _, _), sk = self._rows(k_rope[:, None], "k_rope", self.rope_dim, 1)
+        if dtk != dt or nk != n:
+            raise ValueError("latent and k_rope must be of one type and length")
+        if tags is not None and self.tags is None:
+            raise ValueError("tags need a tagged cache")
+        ref = None
+        if positions is not None or cos is not None or sin is not None or q is not None or q_out is not None:
+            r, q_out = self._rotation(n, self.rope_dim, dt, positions, cos, sin, q, q_out, interleaved, stream)
+            ref = ctypes.byref(r)
+        rc = self._append(self._cfg, self._data_ptr, self._tags_ptr, latent.data_ptr(), sl[0], k_rope.data_ptr(),
+                          sk[0], dt, n, self._vec(slots, self._torch.int64, "slots", n),
+                          self._vec(tags, self._torch.int32, "tags", n), ref, self._status_ptr, self._on(stream))
+        if rc:
+            _check(rc)
+        return q_out
+
+    def _run(self, a, q, blocks, width, expanded, kv_len, q_start, prefix_len, q_tags, out, lse, stream):
+        torch = self._torch
+        vec, i32 = self._vec, torch.int32
+        n_q, q_heads, _ = q.shape
+        if blocks.dim() != 2:
+            raise ValueError("blocks must be [n_seq, max_blocks]")
+        if q_tags is not None and self.tags is None:
+            raise ValueError("q_tags need a tagged cache")
+        n_seq, listed = blocks.shape
+        a.n_q, a.q_heads, a.n_seq, a.max_blocks = n_q, q_heads, n_seq, listed
+        a.q_start, a.kv_len = vec(q_start, i32, "q_start", n_seq + 1), vec(kv_len, i32, "kv_len", n_seq)
+        a.blocks = vec(blocks, torch.int64, "blocks", n_seq * listed)
+        a.prefix_len = vec(prefix_len, i32, "prefix_len", n_seq)
+        if q_tags is not None:
+            a.tags, a.q_tags = self._tags_ptr, vec(q_tags, i32, "q_tags", n_q)
+        behind = q_start is not None or n_seq == 0         # rows that no sequence has
+        if out is None:
+            out = self._empty((n_q, q_heads, width), self.dtype, stream, zero=behind)
+            a.out = out.data_ptr()
+        else:
+            a.out = vec(out, self.dtype, "out", n_q * q_heads * width)
+        if not expanded:
+            if lse is None:
+                lse = self._empty((n_q, q_heads), torch.float32, stream, zero=behind)
+                a.lse = lse.data_ptr()
+            else:
+                a.lse = vec(lse, torch.float32, "lse", n_q * q_heads)
+        call, scratch_of = self._calls[expanded]
+        ref = ctypes.byref(a)
+        key = (expanded, n_q, q_heads, n_seq, listed, q_start is None, q_tags is None, a.nope_dim, a.value_dim)
+        size = self._scratch.get(key)
+        if size is None:
+            need = ctypes.c_int64()
+            _check(scratch_of(self._cfg, ref, ctypes.byref(need)))
+            if len(self._scratch) > 4096:
+                self._scratch.clear()
+            size = self._scratch[key] = need.value
+        scratch = self._empty((size,), torch.uint8, stream) if size else None
+        rc = call(self._cfg, self._data_ptr, ref, scratch.data_ptr() if size else None, size, self._status_ptr,
+                  self._on(stream))
+        if rc:
+            _check(rc)
+        return out, lse
+
+    def attend(self, q, blocks, scale, kv_len=None, q_start=None, causal=True, prefix_len=None, q_tags=None,
+               out=None, lse=None, stream=None):
+        """Absorbed attention of q [n_q, q_heads, latent_dim + rope_dim] (the cache's type; a head's first
+        latent_dim values its query times w_k) over the listed blocks; sequences, masks and
+        tags as in KVCache.attend.  scale: of the scores (the width of a head before it was absorbed
+        is not known here).  Returns (out [n_q, q_heads, latent_dim], to be multiplied by
+        w_v, and lse float32 [n_q, q_heads]).  For single tokens and drafts; prompts
+        take fewer products in attend_expanded."""
+        dt, _, sq = self._rows(q, "q", self.latent_dim + self.rope_dim)
+        if q.dtype is not self.dtype:
+            raise TypeError(f"q must be {self.dtype}, got {q.dtype}")
+        a = _LatentAttend(q=q.data_ptr(), q_row_stride=sq[0], q_head_stride=sq[1], causal=1 if causal else 0,
+                          scale=scale)
+        return self._run(a, q, blocks, self.latent_dim, False, kv_len, q_start, prefix_len, q_tags, out, lse, stream)
+
+    def attend_expanded(self, q, w_k, w_v, blocks, scale=None, kv_len=None, q_start=None, causal=True,
+                        prefix_len=None, q_tags=None, out=None, stream=None):
+        """Attention of q [n_q, q_heads, nope_dim + rope_dim] through per-head keys and values:
+        w_k [q_heads, nope_dim, latent_dim] and w_v [q_heads, value_dim, latent_dim] (the
+        cache's type, a head's rows evenly spaced: halves of one projection's rows do; nope_dim and
+        value_dim 64 or 128).  scale: 1 / sqrt(nope_dim + rope_dim) if not given.  Returns out
+        [n_q, q_heads, value_dim].  For prompts; other arguments as in attend."""
+        for t, name in ((w_k, "w_k"), (w_v, "w_v")):
+            if t.dtype is not self.dtype:
+                raise TypeError(f"{name} must be {self.dtype}, got {t.dtype}")
+            if t.dim() != 3 or t.shape[2] != self.latent_dim or t.stride(2) != 1:
+                raise ValueError(f"{name} must be [q_heads, rows, {self.latent_dim}], contiguous in its last dimension")
+            if t.get_device() != self.device:
+                raise ValueError(f"{name} must be a CUDA tensor on device {self.device}")
+        nope, value = w_k.shape[1], w_v.shape[1]
+        dt, shape, sq = self._rows(q, "q", nope + self.rope_dim)
+        if q.dtype is not self.dtype:
+            raise TypeError(f"q must be {self.dtype}, got {q.dtype}")
+        if w_k.shape[0] != shape[1] or w_v.shape[0] != shape[1]:
+            raise ValueError("w_k and w_v must have q's heads")
+        a = _LatentAttend(q=q.data_ptr(), q_row_stride=sq[0], q_head_stride=sq[1], causal=1 if causal else 0,
+                          scale=(nope + self.rope_dim) ** -0.5 if scale is None else scale,
+                          w_k=w_k.data_ptr(), w_v=w_v.data_ptr(), w_k_head_stride=w_k.stride(0),
+                          w_k_row_stride=w_k.stride(1), w_v_head_stride=w_v.stride(0),
+                          w_v_row_stride=w_v.stride(1), nope_dim=nope, value_dim=value)
+        return self._run(a, q, blocks, value, True, kv_len, q_start, prefix_len, q_tags, out, None, stream)[0]

@@ -18,6 +18,7 @@
 #include <stdio.h>
 
 #include "ak_attend.cuh"
+#include "ak_rotate.cuh"
 
 namespace ak {
 
@@ -73,6 +74,7 @@ struct KvRows {
     int *status;
     int64_t n;
     bool wide;                     // 16-byte loads and stores are aligned
+    RotateArgs turn;               // write with rotation
 };
 
 struct KvPlace {
@@ -90,13 +92,6 @@ __device__ __forceinline__ KvPlace kv_place(int64_t s, int h, int heads, uint32_
     const uint32_t u = (uint32_t)(s >> 4), b = u / per_block;
     return {((int64_t)b * heads + h) * per_block + (u - b * per_block), (int)(s & 15)};
 }
-
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ void from_f32(float x, float &y) { y = x; }
-__device__ __forceinline__ void from_f32(float x, __half &y) { y = __float2half_rn(x); }
-__device__ __forceinline__ void from_f32(float x, __nv_bfloat16 &y) { y = __float2bfloat16_rn(x); }
 
 // The 16 codes of a group, biased to be positive, `bits` wide and in the cache's
 // order (ak_kv.cuh).  q = x / s correctly rounded (one Newton step on x inv); where
@@ -139,16 +134,38 @@ __device__ __forceinline__ void kv_codes(const float (&f)[16], float s, uint32_t
     }
 }
 
-template <typename T, int BITS, int D, bool WIDE>
+// TURN: keys are rotated to their positions on the way, in fp32, and the grid's third layer rotates
+// the query rows of the same tokens (`tokens_q` at a time).
+template <typename T, int BITS, int D, bool WIDE, bool TURN>
 __global__ void __launch_bounds__(256)
 k_kv_write(unsigned char *__restrict__ cache, const T *__restrict__ k, const T *__restrict__ v,
            int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head,
            const int64_t *__restrict__ slots, int32_t *__restrict__ tags,
            const int32_t *__restrict__ new_tags, int64_t n, int heads, uint32_t units,
-           uint32_t per_block, int tokens, int *status) {
+           uint32_t per_block, int tokens, int *status, const RotateArgs turn, int tokens_q) {
     using U = KvUnit<BITS, D>;
     constexpr int G = U::GROUPS;
     griddep_wait();
+    if constexpr (TURN) {
+        if (blockIdx.y == 2) {
+            for (int64_t i0 = (int64_t)blockIdx.x * tokens_q; i0 < n; i0 += (int64_t)gridDim.x * tokens_q) {
+                const uint32_t total = (uint32_t)min((int64_t)tokens_q, n - i0) * turn.q_heads * G;
+                for (uint32_t x = threadIdx.x; x < total; x += 256) {
+                    const uint32_t row = x / G, ti = row / (uint32_t)turn.q_heads, h = row - ti * turn.q_heads;
+                    const int64_t i = i0 + ti;
+                    int64_t pos = -1;
+                    if (kv_place(slots[i], 0, heads, units, per_block, status).unit >= 0 &&
+                        !rotate_at(turn, i, pos, status))
+                        pos = -1;
+                    const T *src = (const T *)turn.q + i * turn.q_row + h * turn.q_head;
+                    T *dst = (T *)turn.q_out + i * turn.o_row + h * turn.o_head;
+                    if (turn.wide) rotate_query<true>(turn, src, dst, x % G, pos);
+                    else rotate_query<false>(turn, src, dst, x % G, pos);
+                }
+            }
+            return;
+        }
+    }
     const bool is_v = blockIdx.y;
     const T *base = is_v ? v : k;
     const int64_t row_stride = is_v ? v_row : k_row, head_stride = is_v ? v_head : k_head;
@@ -158,11 +175,16 @@ k_kv_write(unsigned char *__restrict__ cache, const T *__restrict__ k, const T *
         for (uint32_t x = threadIdx.x; x < ((total + 31) & ~31u); x += 256) {
             const uint32_t row = x / G, gr = x % G, ti = row / (uint32_t)heads, h = row - ti * heads;
             const int64_t i = i0 + ti, slot = x < total ? slots[i] : -1;
-            const KvPlace at = kv_place(slot, h, heads, units, per_block, status);
+            KvPlace at = kv_place(slot, h, heads, units, per_block, status);
+            int64_t pos = 0;
+            if constexpr (TURN)
+                if (at.unit >= 0 && !rotate_at(turn, i, pos, status)) at.unit = -1;
             float f[16];
 #pragma unroll
             for (int w = 0; w < 16; ++w) f[w] = 0.f;
-            if (at.unit >= 0) {
+            if (TURN && !is_v && at.unit >= 0) {
+                turn_group<WIDE>(turn, base + i * row_stride + h * head_stride, gr * 16, pos, f);
+            } else if (at.unit >= 0) {
                 const T *src = base + i * row_stride + h * head_stride + gr * 16;
                 alignas(16) T raw[16];
                 if constexpr (WIDE) {
@@ -194,7 +216,8 @@ k_kv_write(unsigned char *__restrict__ cache, const T *__restrict__ k, const T *
             if constexpr (BITS == 4) {
                 const int E = kv_row_exp(a);
                 const uint32_t b = kv_scale_byte(ag, E);
-                kv_codes<T, 4>(f, kv_scale_of(b) * pow2i(E), w);
+                if (TURN && !is_v) kv_codes<float, 4>(f, kv_scale_of(b) * pow2i(E), w);
+                else kv_codes<T, 4>(f, kv_scale_of(b) * pow2i(E), w);
                 if (is_v) {
                     if (U::v_code(0, 8) == U::v_code(0, 0) + 4)
                         *(uint2 *)(dst + U::v_code(t, d0)) = make_uint2(w[0], w[1]);
@@ -211,7 +234,8 @@ k_kv_write(unsigned char *__restrict__ cache, const T *__restrict__ k, const T *
                 }
             } else {
                 const uint32_t sb = kv_scale_bf16(a);
-                kv_codes<T, 8>(f, __uint_as_float(sb << 16), w);
+                if (TURN && !is_v) kv_codes<float, 8>(f, __uint_as_float(sb << 16), w);
+                else kv_codes<T, 8>(f, __uint_as_float(sb << 16), w);
                 if (is_v) {
                     if (U::v_code(0, 8) == U::v_code(0, 0) + 8)
                         *(uint4 *)(dst + U::v_code(t, d0)) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -314,15 +338,22 @@ unsigned kv_grid(int64_t n, int tokens) {
     return (unsigned)(want < most ? want : most);
 }
 
-template <typename T, int BITS, int D>
+template <typename T, int BITS, int D, bool TURN>
 cudaError_t launch_write(const KvRows &r, cudaStream_t st) {
     const int tokens = kv_tokens(r.cfg->heads, D / 16);
     const uint32_t per = (uint32_t)(r.cfg->block_tokens / KV_UNIT);
     const uint32_t units = (uint32_t)(r.cfg->n_blocks * per);
-    auto *kernel = r.wide ? k_kv_write<T, BITS, D, true> : k_kv_write<T, BITS, D, false>;
-    return launch_pdl(kernel, dim3(kv_grid(r.n, tokens), 2), dim3(256), 0, st, r.cache, (const T *)r.in[0],
+    auto *kernel = r.wide ? k_kv_write<T, BITS, D, true, TURN> : k_kv_write<T, BITS, D, false, TURN>;
+    unsigned grid = kv_grid(r.n, tokens), layers = 2;
+    int tokens_q = 1;
+    if (TURN && r.turn.q) {
+        tokens_q = kv_tokens(r.turn.q_heads, D / 16);
+        const unsigned want = kv_grid(r.n, tokens_q);
+        grid = want > grid ? want : grid, layers = 3;
+    }
+    return launch_pdl(kernel, dim3(grid, layers), dim3(256), 0, st, r.cache, (const T *)r.in[0],
                       (const T *)r.in[1], r.row_stride[0], r.head_stride[0], r.row_stride[1], r.head_stride[1],
-                      r.slots, r.tags, r.new_tags, r.n, r.cfg->heads, units, per, tokens, r.status);
+                      r.slots, r.tags, r.new_tags, r.n, r.cfg->heads, units, per, tokens, r.status, r.turn, tokens_q);
 }
 template <typename T, int BITS, int D>
 cudaError_t launch_read(const KvRows &r, cudaStream_t st) {
@@ -334,35 +365,67 @@ cudaError_t launch_read(const KvRows &r, cudaStream_t st) {
                       (T *)r.out[1], r.slots, r.n, r.cfg->heads, units, per, tokens, r.status);
 }
 
+enum KvCall { KV_WRITE, KV_READ, KV_APPEND };
+template <typename T, int BITS, int D>
+cudaError_t launch_rows(const KvRows &r, cudaStream_t st, KvCall call) {
+    return call == KV_WRITE  ? launch_write<T, BITS, D, false>(r, st)
+           : call == KV_READ ? launch_read<T, BITS, D>(r, st)
+                             : launch_write<T, BITS, D, true>(r, st);
+}
 template <typename T, int BITS>
-cudaError_t launch_rows_dim(const KvRows &r, cudaStream_t st, bool write) {
+cudaError_t launch_rows_dim(const KvRows &r, cudaStream_t st, KvCall call) {
     switch (r.cfg->head_dim) {
-    case 64: return write ? launch_write<T, BITS, 64>(r, st) : launch_read<T, BITS, 64>(r, st);
-    case 128: return write ? launch_write<T, BITS, 128>(r, st) : launch_read<T, BITS, 128>(r, st);
-    default: return write ? launch_write<T, BITS, 256>(r, st) : launch_read<T, BITS, 256>(r, st);
+    case 64: return launch_rows<T, BITS, 64>(r, st, call);
+    case 128: return launch_rows<T, BITS, 128>(r, st, call);
+    default: return launch_rows<T, BITS, 256>(r, st, call);
     }
 }
 template <typename T>
-cudaError_t launch_rows_bits(const KvRows &r, cudaStream_t st, bool write) {
-    return r.cfg->bits == 4 ? launch_rows_dim<T, 4>(r, st, write) : launch_rows_dim<T, 8>(r, st, write);
+cudaError_t launch_rows_bits(const KvRows &r, cudaStream_t st, KvCall call) {
+    return r.cfg->bits == 4 ? launch_rows_dim<T, 4>(r, st, call) : launch_rows_dim<T, 8>(r, st, call);
 }
 
-akashic_status_t run_rows(const char *who, const KvRows &r, int32_t dtype, void *stream, bool write) {
+akashic_status_t run_rows(const char *who, const KvRows &r, int32_t dtype, void *stream, KvCall call) {
     KvDevice dev(r.cfg->device);
     if (!dev.ok) return kv_fail(AKASHIC_ECUDA, "%s: device %d cannot be made current", who, r.cfg->device);
     cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = dtype == AKASHIC_DTYPE_BF16   ? launch_rows_bits<__nv_bfloat16>(r, st, write)
-                          : dtype == AKASHIC_DTYPE_FP16 ? launch_rows_bits<__half>(r, st, write)
-                                                        : launch_rows_bits<float>(r, st, write);
+    const cudaError_t e = dtype == AKASHIC_DTYPE_BF16   ? launch_rows_bits<__nv_bfloat16>(r, st, call)
+                          : dtype == AKASHIC_DTYPE_FP16 ? launch_rows_bits<__half>(r, st, call)
+                                                        : launch_rows_bits<float>(r, st, call);
     if (e != cudaSuccess) return kv_fail(AKASHIC_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return AKASHIC_OK;
 }
+
+}  // namespace
 
 int dtype_size(int32_t dtype) {
     return dtype == AKASHIC_DTYPE_FP32 ? 4 : dtype == AKASHIC_DTYPE_BF16 || dtype == AKASHIC_DTYPE_FP16 ? 2 : 0;
 }
 
-}  // namespace
+bool rotate_args(const akashic_mem_rotation_t *r, int width, int size, RotateArgs *a, const char **why) {
+    *why = r->rotary_dim < 32 || r->rotary_dim % 32 || r->rotary_dim > width
+               ? "rotary_dim must be a multiple of 32, at most the row's width"
+           : r->table_rows < 1                        ? "table_rows must be >= 1"
+           : !r->positions || !r->cos || !r->sin      ? "NULL positions or table"
+           : ((uintptr_t)r->cos | (uintptr_t)r->sin) & 15u || (uintptr_t)r->positions & 7u
+               ? "tables must be 16-byte aligned, positions to their element"
+           : !r->q != !r->q_out                       ? "q and q_out come together"
+           : r->q && (r->q_heads < 1 || r->q_heads > KV_MAX_HEADS * KV_MAX_HEADS)
+               ? "q_heads must be in [1, 2^20]"
+           : ((uintptr_t)r->q | (uintptr_t)r->q_out) & (uintptr_t)(size - 1)
+               ? "q and q_out must be aligned to their element"
+               : nullptr;
+    if (*why) return false;
+    a->positions = r->positions, a->cos = r->cos, a->sin = r->sin;
+    a->table_rows = r->table_rows, a->rotary = r->rotary_dim, a->pairs = r->interleaved != 0;
+    a->q = r->q, a->q_out = r->q_out, a->q_heads = r->q_heads;
+    a->q_row = r->q_row_stride, a->q_head = r->q_head_stride;
+    a->o_row = r->q_out_row_stride, a->o_head = r->q_out_head_stride;
+    a->wide = !(((uintptr_t)r->q | (uintptr_t)r->q_out |
+                 (uintptr_t)((r->q_row_stride | r->q_head_stride | r->q_out_row_stride | r->q_out_head_stride) * size)) & 15u);
+    return true;
+}
+
 }  // namespace ak
 
 using namespace ak;
@@ -377,25 +440,31 @@ extern "C" akashic_status_t akashic_mem_kv_cache_bytes(const akashic_mem_kv_conf
     return AKASHIC_OK;
 }
 
-extern "C" akashic_status_t akashic_mem_kv_write(
-    const akashic_mem_kv_config_t *cfg, void *cache, int32_t *tags, const void *k,
-    int64_t k_row_stride, int64_t k_head_stride, const void *v, int64_t v_row_stride,
-    int64_t v_head_stride, int32_t dtype, int64_t n, const int64_t *slots,
-    const int32_t *new_tags, int32_t *status, void *stream) {
+namespace {
+
+akashic_status_t kv_write_rows(const char *who, const akashic_mem_kv_config_t *cfg, void *cache, int32_t *tags,
+                               const void *k, int64_t k_row_stride, int64_t k_head_stride, const void *v,
+                               int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, int64_t n,
+                               const int64_t *slots, const int32_t *new_tags, const akashic_mem_rotation_t *rot,
+                               int32_t *status, void *stream, KvCall call) {
     set_last_error("");
-    if (akashic_status_t s = kv_check_config(cfg, "kv_write")) return s;
+    if (akashic_status_t s = kv_check_config(cfg, who)) return s;
     const int size = dtype_size(dtype);
-    if (!size) return kv_fail(AKASHIC_EINVAL, "kv_write: dtype must be BF16, FP16 or FP32");
-    if (n < 0 || n > 0x7fffffffLL) return kv_fail(AKASHIC_EINVAL, "kv_write: n must be in [0, 2^31-1]");
+    if (!size) return kv_fail(AKASHIC_EINVAL, "%s: dtype must be BF16, FP16 or FP32", who);
+    if (n < 0 || n > 0x7fffffffLL) return kv_fail(AKASHIC_EINVAL, "%s: n must be in [0, 2^31-1]", who);
+    if (call == KV_APPEND && !rot) return kv_fail(AKASHIC_EINVAL, "%s: NULL rotation", who);
     if (n == 0) return AKASHIC_OK;
-    if (!cache || !k || !v || !slots) return kv_fail(AKASHIC_EINVAL, "kv_write: NULL argument");
-    if ((uintptr_t)cache & 15u) return kv_fail(AKASHIC_EINVAL, "kv_write: cache must be 16-byte aligned");
+    if (!cache || !k || !v || !slots) return kv_fail(AKASHIC_EINVAL, "%s: NULL argument", who);
+    if ((uintptr_t)cache & 15u) return kv_fail(AKASHIC_EINVAL, "%s: cache must be 16-byte aligned", who);
     if (((uintptr_t)k | (uintptr_t)v) & (uintptr_t)(size - 1))
-        return kv_fail(AKASHIC_EINVAL, "kv_write: k and v must be aligned to their element");
+        return kv_fail(AKASHIC_EINVAL, "%s: k and v must be aligned to their element", who);
     if ((uintptr_t)slots & 7u || ((uintptr_t)tags | (uintptr_t)new_tags) & 3u)
-        return kv_fail(AKASHIC_EINVAL, "kv_write: slots and tags must be aligned to their element");
-    if (new_tags && !tags) return kv_fail(AKASHIC_EINVAL, "kv_write: new_tags needs the cache's tags");
+        return kv_fail(AKASHIC_EINVAL, "%s: slots and tags must be aligned to their element", who);
+    if (new_tags && !tags) return kv_fail(AKASHIC_EINVAL, "%s: new_tags needs the cache's tags", who);
     KvRows r = {};
+    const char *why = nullptr;
+    if (call == KV_APPEND && !rotate_args(rot, cfg->head_dim, size, &r.turn, &why))
+        return kv_fail(AKASHIC_EINVAL, "%s: %s", who, why);
     r.cfg = cfg;
     r.cache = (unsigned char *)cache;
     r.in[0] = k, r.in[1] = v;
@@ -404,7 +473,27 @@ extern "C" akashic_status_t akashic_mem_kv_write(
     r.slots = slots, r.tags = tags, r.new_tags = new_tags, r.status = status, r.n = n;
     r.wide = !(((uintptr_t)k | (uintptr_t)v |
                 (uintptr_t)((k_row_stride | k_head_stride | v_row_stride | v_head_stride) * size)) & 15u);
-    return run_rows("kv_write", r, dtype, stream, true);
+    return run_rows(who, r, dtype, stream, call);
+}
+
+}  // namespace
+
+extern "C" akashic_status_t akashic_mem_kv_write(
+    const akashic_mem_kv_config_t *cfg, void *cache, int32_t *tags, const void *k,
+    int64_t k_row_stride, int64_t k_head_stride, const void *v, int64_t v_row_stride,
+    int64_t v_head_stride, int32_t dtype, int64_t n, const int64_t *slots,
+    const int32_t *new_tags, int32_t *status, void *stream) {
+    return kv_write_rows("kv_write", cfg, cache, tags, k, k_row_stride, k_head_stride, v, v_row_stride, v_head_stride,
+                         dtype, n, slots, new_tags, nullptr, status, stream, KV_WRITE);
+}
+
+extern "C" akashic_status_t akashic_mem_kv_append(
+    const akashic_mem_kv_config_t *cfg, void *cache, int32_t *tags, const void *k,
+    int64_t k_row_stride, int64_t k_head_stride, const void *v, int64_t v_row_stride,
+    int64_t v_head_stride, int32_t dtype, int64_t n, const int64_t *slots,
+    const int32_t *new_tags, const akashic_mem_rotation_t *rotation, int32_t *status, void *stream) {
+    return kv_write_rows("kv_append", cfg, cache, tags, k, k_row_stride, k_head_stride, v, v_row_stride, v_head_stride,
+                         dtype, n, slots, new_tags, rotation, status, stream, KV_APPEND);
 }
 
 extern "C" akashic_status_t akashic_mem_kv_read(const akashic_mem_kv_config_t *cfg,
@@ -428,5 +517,5 @@ extern "C" akashic_status_t akashic_mem_kv_read(const akashic_mem_kv_config_t *c
     r.out[0] = k, r.out[1] = v;
     r.slots = slots, r.status = status, r.n = n;
     r.wide = !(((uintptr_t)k | (uintptr_t)v) & 15u);
-    return run_rows("kv_read", r, dtype, stream, false);
+    return run_rows("kv_read", r, dtype, stream, KV_READ);
 }

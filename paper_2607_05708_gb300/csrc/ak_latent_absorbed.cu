@@ -1,0 +1,570 @@
+// Absorbed attention over the latent cache, on tcgen05.
+//
+// Every head reads the same rows [latent | rotated key], so a token's 2 (R + P) bytes meet
+// 2 H (2R + P) flops: bytes bound up to some 64 heads.  Rows of a tile are (query row, head)
+// pairs, 16, 32 or 64 of them; a step is 128 tokens.  The products are transposed,
+//   S^T = K Q^T      M = 128 tokens, N = rows, K = R + P
+//   O^T += C^T P^T   M = 128 latent dims at a time, N = rows, K = 128 tokens
+// so that M is full whatever the number of heads, and the R x rows accumulators (4 x 64 columns of
+// 128 lanes at R = 512) leave tensor memory for two S.  One copy of a tile in shared memory serves both
+// products: as K it is K-major, as C^T the same bytes are MN-major.
+//   copying warp   the tile's boxes of tokens, from the listed blocks, in pairs of 64-dim chunks;
+//                  blocks that are not listed read as zeros
+//   issuing warp   scores of the next tile and O^T += of this one, whichever is ready
+//   softmax warps  a thread a token and up to 32 rows.  Weights are relative to a reference of the row, not
+//                  to its running maximum, and the reference is raised, O^T and the totals rescaled, only when a
+//                  weight would pass 2^15: maxima over tokens, which lie across the lanes, are then not
+//                  needed tile by tile.  P^T goes to shared memory, MN-major.
+// Tiles are shared out evenly over the CTAs (ak_attend.cuh); parts of an item are joined after it.
+#include <atomic>
+
+#include "ak_latent.cuh"
+#include "ak_umma.cuh"
+
+namespace ak {
+
+namespace {
+
+template <int R, int NR>
+struct Absorbed {
+    static constexpr int TOK = 128;                      // tokens of a tile
+    static constexpr int PAIRS = R / 128, CHUNKS = R / 64 + 1;
+    static constexpr int CW = NR < 32 ? NR : 32;         // rows of a softmax thread
+    static constexpr int SOFT = NR / CW * 4;             // softmax warps
+    static constexpr int THREADS = 32 * (SOFT + 2);
+    static constexpr int PAIR_BYTES = TOK * 256, ROPE_BYTES = TOK * 128;
+    static constexpr int Q_BYTES = CHUNKS * NR * 128;
+    // P^T: a row a token; 64 bytes of it, in the 64-byte swizzle, hold 32 rows' weights
+    static constexpr int P_ROW = NR > 32 ? 128 : 64, P_BYTES = TOK * P_ROW;
+    // Where R = 512 and 64 rows leave no room, the rotated keys lie where P^T will: they are
+    // read before it is written.
+    static constexpr bool ALIAS = R == 512 && NR == 64;
+    static constexpr int ROOM = 232448 - 1024 - 5120 - Q_BYTES - P_BYTES;
+    static constexpr int fit(int ropes) { return (ROOM - ropes * ROPE_BYTES) / PAIR_BYTES; }
+    static constexpr int ROPES = ALIAS ? 0 : fit(2) > PAIRS ? 2 : 1;
+    static constexpr int STAGES = fit(ROPES) < 6 ? fit(ROPES) : 6;
+    static_assert(STAGES >= PAIRS, "a tile");
+    static_assert(!ALIAS || P_BYTES == ROPE_BYTES, "the same place");
+    static constexpr int ROPE_SLOTS = ALIAS ? 1 : ROPES;
+    static constexpr int SMEM = 1024 + Q_BYTES + P_BYTES + ROPES * ROPE_BYTES + STAGES * PAIR_BYTES;
+    static constexpr int S_COL = 256;                    // tensor memory: O^T, then two S^T
+    static_assert(PAIRS * NR <= S_COL && S_COL + 2 * NR <= 512, "tensor memory");
+    static constexpr int METAS = 8;                      // tiles whose places are kept
+    static_assert(METAS > STAGES / PAIRS + 1, "a tile's places are read before they are written again");
+    // An item's beginning and end (rows in, result out, an empty pipeline) count as steps.
+    static constexpr int EXTRA = 1;
+};
+
+// Weights are held between 2^-OFF of the reference's and 2^(OFF + SLACK): fp16 has room for both.
+constexpr float OFF = 7.f, SLACK = 8.f;
+
+// Whether any thread of the barrier's has `x`, for all of them.
+__device__ __forceinline__ bool bar_any(int id, int threads, bool x) {
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %3, 0;\n\t"
+        "barrier.cta.red.or.pred q, %1, %2, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(any)
+        : "r"(id), "r"(threads), "r"((uint32_t)x)
+        : "memory");
+    return any != 0;
+}
+// v[c], c < N, combined over the warp's lanes: lane L has column L % N.
+template <int N, typename F>
+__device__ __forceinline__ float over_lanes(float (&v)[N], F f) {
+    const int lane = threadIdx.x & 31;
+    if constexpr (N == 16) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = f(v[j], __shfl_xor_sync(0xffffffffu, v[j], 16));
+    }
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int j = 0; j < o; ++j) {
+            const float keep = up ? v[j + o] : v[j], give = up ? v[j] : v[j + o];
+            v[j] = f(keep, __shfl_xor_sync(0xffffffffu, give, o));
+        }
+    }
+    return v[0];
+}
+template <int N>
+__device__ __forceinline__ void tmem_ldn(uint32_t at, uint32_t (&r)[N]) {
+    if constexpr (N == 32) tmem_ld32(at, r);
+    else tmem_ld16(at, r);
+}
+template <int N>
+__device__ __forceinline__ void tmem_stn(uint32_t at, const uint32_t (&r)[N]) {
+    if constexpr (N == 32) tmem_st32(at, r);
+    else tmem_st16(at, r);
+}
+
+template <int R, int NR>
+__global__ void __launch_bounds__(Absorbed<R, NR>::THREADS, 1)
+k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ LatentParams lp,
+                  const int box, const int n_rows) {
+    using C = Absorbed<R, NR>;
+    constexpr int TOK = C::TOK, PAIRS = C::PAIRS, ST = C::STAGES, CW = C::CW, THR = 32 * C::SOFT;
+    const AttendParams &p = lp.a;
+    extern __shared__ unsigned char raw_smem[];
+    unsigned char *smem = (unsigned char *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
+    unsigned char *s_pair = smem, *s_rope = s_pair + ST * C::PAIR_BYTES, *s_p = s_rope + C::ROPES * C::ROPE_BYTES;
+    unsigned char *s_q = s_p + C::P_BYTES;
+    if (C::ALIAS) s_rope = s_p;
+    __shared__ uint64_t full[ST], empty[ST], rope_full[C::ROPE_SLOTS], rope_empty[C::ROPE_SLOTS];
+    __shared__ uint64_t sfull[2], pfull, odone, qfull, mfull[C::METAS], drained;
+    __shared__ int m_row[C::METAS][8];                   // first row of each of a tile's boxes, -1: none
+    __shared__ alignas(16) float c_ref[NR], c_fac[NR];
+    __shared__ alignas(16) int c_limit[NR], c_tag[NR];
+    __shared__ float c_part[4][NR];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int dead_word;
+    volatile int *dead = &dead_word;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    griddep_wait();
+    if (tid == 0) {
+        for (int i = 0; i < ST; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
+        for (int i = 0; i < C::ROPE_SLOTS; ++i) mbar_init(&rope_full[i], 1), mbar_init(&rope_empty[i], 1);
+        for (int i = 0; i < C::METAS; ++i) mbar_init(&mfull[i], 1);
+        for (int i = 0; i < 2; ++i) mbar_init(&sfull[i], 1);
+        mbar_init(&pfull, C::SOFT), mbar_init(&odone, 1), mbar_init(&qfull, C::SOFT), mbar_init(&drained, 1);
+        mbar_fence_init();
+        dead_word = 0;
+        p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    }
+    if (warp == 0) {
+        tmem_alloc(&tmem_slot, 512);
+        tmem_relinquish();
+    }
+    int64_t *prefix = (int64_t *)s_q;                    // until the warps have found their items
+    constexpr int ALL = 0x7fffffff;
+    attend_sums(p, NR, TOK, C::EXTRA, 1, ALL, prefix);
+    const int64_t total = prefix[C::THREADS];
+    const int64_t per = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x);
+    const int64_t first = per * blockIdx.x;
+    int left = (int)max((int64_t)0, min(per, total - first));
+    AttendCursor cur = {};
+    if (left > 0) cur = attend_find(p, NR, TOK, C::EXTRA, 1, ALL, prefix, first);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    if (warp == C::SOFT) {
+        // ---------------- copying
+        const int nb = TOK / box, T = p.per_block * KV_UNIT;           // boxes of a chunk
+        uint32_t n_tile = 0, n_pair = 0, n_rope = 0;
+        bool ok = true;
+        while (left > 0 && ok) {
+            const AttendPart part = attend_part(cur, left);
+            if (part.n <= 0) break;
+            const int64_t *list = p.blocks + cur.seq * p.max_blocks;
+            // lane: the row of box lane % nb of a tile
+            auto place = [&](int i) {
+                const int tok = (part.from + i) * TOK + lane % nb * box;
+                if (i >= part.n || tok >= cur.q.kv) return -1;
+                const int b = tok / T;
+                const int64_t id = list[b];
+                if (id >= 0 && id < p.n_blocks) return (int)(id * T + (tok - b * T));
+                if (id != -1) set_status(p.status, AKASHIC_EDEVICE);
+                return -1;
+            };
+            int next = place(0);
+            for (int i = 0; ok && i < part.n; ++i, ++n_tile) {
+                const int row = next;
+                next = place(i + 1);
+                const int y = row < 0 ? n_rows : row;    // behind the last row: zeros
+                for (int k = 0; k < PAIRS; ++k, ++n_pair) {
+                    const uint32_t st = n_pair % ST;
+                    ok = wide_wait(&empty[st], ((n_pair / ST) & 1) ^ 1, dead, p.status);
+                    if (!ok) break;
+                    if (k == 0) {
+                        if (lane < nb) m_row[n_tile % C::METAS][lane] = row;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&mfull[n_tile % C::METAS]);
+                    }
+                    if (lane == 0) mbar_expect_tx(&full[st], C::PAIR_BYTES);
+                    __syncwarp();
+                    if (lane < 2 * nb) {
+                        const int c = lane / nb;
+                        tma_load_2d(s_pair + st * C::PAIR_BYTES + c * C::ROPE_BYTES + lane % nb * box * 128, &rows_map,
+                                    &full[st], (2 * k + c) * 64, y);
+                    }
+                }
+                if (!ok) break;
+                const uint32_t sr = n_tile % C::ROPE_SLOTS;
+                ok = wide_wait(&rope_empty[sr], ((n_tile / C::ROPE_SLOTS) & 1) ^ 1, dead, p.status);
+                if (!ok) break;
+                if (lane == 0) mbar_expect_tx(&rope_full[sr], C::ROPE_BYTES);
+                __syncwarp();
+                if (lane < nb)
+                    tma_load_2d(s_rope + sr * C::ROPE_BYTES + lane * box * 128, &rows_map, &rope_full[sr], R, y);
+                ++n_rope;
+            }
+            left -= part.used;
+            if (left > 0) attend_next(p, NR, TOK, C::EXTRA, 1, ALL, cur);
+        }
+        // nothing is on its way when the CTA ends (where a wait gave up; else all has been read)
+        for (uint32_t i = 0; !ok && i < ST; ++i)
+            if (n_pair > i) mbar_wait(&full[i], ((n_pair - i - 1) / ST) & 1, p.status);
+        for (uint32_t i = 0; !ok && i < C::ROPE_SLOTS; ++i)
+            if (n_rope > i) mbar_wait(&rope_full[i], ((n_rope - i - 1) / C::ROPE_SLOTS) & 1, p.status);
+        __syncwarp();
+    } else if (warp == C::SOFT + 1) {
+        // ---------------- issuing
+        const uint32_t id_s = idesc_f16(NR, lp.bf16);
+        const uint32_t id_o = idesc_f16(NR, lp.bf16) | IDESC_A_MN_MAJOR | IDESC_B_MN_MAJOR;
+        const uint32_t go = lane == 0;
+        const uint32_t q_at = desc_k(smem_u32(s_q)), kk_at = desc_k(smem_u32(s_pair)), r_at = desc_k(smem_u32(s_rope));
+        const uint32_t v_at = desc_mn(smem_u32(s_pair), C::ROPE_BYTES), p_at = desc_mn(smem_u32(s_p), 0);
+        const int rope_steps = lp.P / 16;
+        uint32_t n_tile = 0, items = 0;
+        bool ok = true;
+        while (left > 0 && ok) {
+            const AttendPart part = attend_part(cur, left);
+            const uint32_t n = part.n;
+            if (part.n <= 0) break;
+            ok = wide_wait(&qfull, items++ & 1, dead, p.status);
+            uint32_t s_next = 0, s_pair_next = 0, v_next = 0, polls = 0;
+            while (ok && v_next < n) {
+                bool moved = false;
+                // (one answer for all lanes)
+                if (s_next < n && s_next <= v_next + 1) {
+                    const uint32_t t = n_tile + s_next, d = tmem + C::S_COL + (t & 1) * NR;
+                    if (s_pair_next < PAIRS) {
+                        const uint32_t x = t * PAIRS + s_pair_next, st = x % ST;
+                        if (__all_sync(0xffffffffu, mbar_test_wait(&full[st], (x / ST) & 1))) {
+                            tc_fence_after();
+                            const uint32_t ka = kk_at + st * (C::PAIR_BYTES >> 4);
+                            const uint32_t qa = q_at + s_pair_next * (2 * NR * 128 >> 4);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                umma_ss(go, d, ka + (k / 4) * (C::ROPE_BYTES >> 4) + 2 * (k % 4),
+                                        qa + (k / 4) * (NR * 128 >> 4) + 2 * (k % 4), id_s, s_pair_next > 0 || k > 0);
+                            ++s_pair_next;
+                            moved = true;
+                        }
+                    } else {
+                        const uint32_t sr = t % C::ROPE_SLOTS;
+                        if (__all_sync(0xffffffffu, mbar_test_wait(&rope_full[sr], (t / C::ROPE_SLOTS) & 1))) {
+                            tc_fence_after();
+                            for (int k = 0; k < rope_steps; ++k)
+                                umma_ss(go, d, r_at + sr * (C::ROPE_BYTES >> 4) + 2 * k,
+                                        q_at + ((C::CHUNKS - 1) * NR * 128 >> 4) + 2 * k, id_s, 1);
+                            umma_commit_if(go, &sfull[t & 1]);
+                            if (!C::ALIAS) umma_commit_if(go, &rope_empty[sr]);
+                            ++s_next, s_pair_next = 0;
+                            moved = true;
+                        }
+                    }
+                }
+                const uint32_t t = n_tile + v_next;
+                if (v_next < s_next && __all_sync(0xffffffffu, mbar_test_wait(&pfull, t & 1))) {
+                    tc_fence_after();
+#pragma unroll
+                    for (int m = 0; m < PAIRS; ++m) {
+                        const uint32_t st = (t * PAIRS + m) % ST, va = v_at + st * (C::PAIR_BYTES >> 4);
+#pragma unroll
+                        for (int k = 0; k < TOK / 16; ++k)
+                            umma_ss_b<C::P_ROW == 128 ? DESC_HI : DESC_HI_64>(
+                                go, tmem + m * NR, va + (2048 * k >> 4), p_at + (16 * C::P_ROW * k >> 4), id_o,
+                                v_next > 0 || k > 0);
+                        umma_commit_if(go, &empty[st]);
+                    }
+                    umma_commit_if(go, &odone);
+                    if (C::ALIAS) umma_commit_if(go, &rope_empty[0]);
+                    ++v_next;
+                    moved = true;
+                }
+                // a bounded wait, like the others (wide_wait)
+                polls = moved ? 0 : polls + 1;
+                if ((polls & 1023u) == 1023u && __any_sync(0xffffffffu, *dead)) ok = false;
+                if (polls >= SPIN_LIMIT) {
+                    *dead = 1;
+                    set_status(p.status, AKASHIC_ETIMEOUT);
+                    ok = false;
+                }
+            }
+            n_tile += n;
+            left -= part.used;
+            if (left > 0) attend_next(p, NR, TOK, C::EXTRA, 1, ALL, cur);
+        }
+        umma_commit_if(go, &drained);          // what was issued ends before the tensor memory goes
+        mbar_wait(&drained, 0, p.status);
+        __syncwarp();
+    } else {
+        // ---------------- softmax: a lane is token 32 (warp % 4) + lane, rows [c0, c0 + CW)
+        const int quad = warp & 3, c0 = warp / 4 * CW, key = quad * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        const float f = p.scale * LOG2E_F;
+        const bool tags = p.tags != nullptr;
+        uint32_t n_tile = 0;
+        // After a wait that gave up the warps wait for nothing more, but go on to the end: they meet at
+        // barriers, which have no limit.
+        bool ok = true;
+        int64_t done = 0;
+        while (left > 0) {
+            const AttendPart mine = attend_part(cur, left);
+            const int n = mine.n;
+            if (n <= 0) break;
+            const AttendSeq sq = cur.q;
+            const int row_first = cur.tile * NR, rows = min(NR, sq.nq * p.group - row_first);
+            // ---- query rows, 16 bytes at a time
+            constexpr int G = R / 8;
+            const int g_all = G + lp.P / 8;
+            for (int x = tid; x < NR * g_all; x += THR) {
+                const int r = x / g_all, g = x - r * g_all;
+                uint4 z = make_uint4(0, 0, 0, 0);
+                if (r < rows) {
+                    const uint32_t at = row_first + r, i = at / (uint32_t)p.group;
+                    const uint16_t *src = (const uint16_t *)p.q + (int64_t)(sq.row0 + (int)i) * p.q_row +
+                                          (int64_t)(at - i * p.group) * p.q_head + g * 8;
+                    if (p.q_wide) {
+                        z = *(const uint4 *)src;
+                    } else {
+                        alignas(16) uint16_t h[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) h[k] = src[k];
+                        z = *(const uint4 *)h;
+                    }
+                }
+                *(uint4 *)(s_q + (g >> 3) * (NR * 128) + r * 128 + (((g & 7) ^ (r & 7)) << 4)) = z;
+            }
+            named_bar(1, THR);                 // (the item before has been written)
+            if (tid < NR) {
+                const uint32_t at = row_first + min(tid, rows - 1);
+                const int i = (int)(at / (uint32_t)p.group);
+                c_ref[tid] = NEG;
+                c_limit[tid] = attend_limit(p, sq, i);
+                // a slot without a token has tag -1 here, and a row that sees none -2
+                const int qt = tags ? p.q_tags[sq.row0 + i] : 0;
+                c_tag[tid] = qt < 0 ? -2 : qt;
+            }
+            fence_async_smem();
+            named_bar(1, THR);
+            if (lane == 0) mbar_arrive(&qfull);
+            const int safe = attend_limit(p, sq, row_first / p.group) - TOK;
+            float l[CW];
+#pragma unroll
+            for (int c = 0; c < CW; ++c) l[c] = 0.f;
+            for (int i = 0; i < n; ++i, ++n_tile) {
+                const int tok = (mine.from + i) * TOK;
+                ok = ok && wide_wait(&mfull[n_tile % C::METAS], (n_tile / C::METAS) & 1, dead, p.status);
+                const int row = m_row[n_tile % C::METAS][key / box];
+                const bool have = row >= 0;
+                int tag = -1;
+                if (tags && have) tag = max(-1, p.tags[(int64_t)row + key % box]);
+                const bool masked = __any_sync(0xffffffffu, !have) || tags || tok > safe;
+                ok = ok && wide_wait(&sfull[n_tile & 1], n_tile >> 1 & 1, dead, p.status);
+                tc_fence_after();
+                uint32_t raw[CW];
+                tmem_ldn<CW>(tmem + lanes + C::S_COL + (n_tile & 1) * NR + c0, raw);
+                tmem_ld_wait();
+                float x[CW];
+#pragma unroll
+                for (int c = 0; c < CW; ++c) x[c] = __uint_as_float(raw[c]) * f;
+                if (masked) {
+                    const int j = have ? tok + key : 0x7fffffff;
+#pragma unroll
+                    for (int c = 0; c < CW; c += 4) {
+                        const int4 lim = *(const int4 *)&c_limit[c0 + c];
+                        x[c] = j < lim.x ? x[c] : -INFINITY;
+                        x[c + 1] = j < lim.y ? x[c + 1] : -INFINITY;
+                        x[c + 2] = j < lim.z ? x[c + 2] : -INFINITY;
+                        x[c + 3] = j < lim.w ? x[c + 3] : -INFINITY;
+                        if (!tags) continue;
+                        const int4 y = *(const int4 *)&c_tag[c0 + c];
+                        x[c] = tag == y.x ? x[c] : -INFINITY;
+                        x[c + 1] = tag == y.y ? x[c + 1] : -INFINITY;
+                        x[c + 2] = tag == y.z ? x[c + 2] : -INFINITY;
+                        x[c + 3] = tag == y.w ? x[c + 3] : -INFINITY;
+                    }
+                }
+                float most = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < CW; c += 4) {
+                    const float4 m = *(const float4 *)&c_ref[c0 + c];
+                    most = fmaxf(fmaxf(most, x[c] - m.x), fmaxf(x[c + 1] - m.y, fmaxf(x[c + 2] - m.z, x[c + 3] - m.w)));
+                }
+                bool waited = false;           // for the products before
+                if (bar_any(2, THR, most > OFF + SLACK)) {
+                    // ---- a row's reference is raised: its maximum over the tile's tokens
+                    float v[CW];
+#pragma unroll
+                    for (int c = 0; c < CW; ++c) v[c] = x[c];
+                    const float top = over_lanes<CW>(v, [](float a, float b) { return fmaxf(a, b); });
+                    if (lane < CW) c_part[quad][c0 + lane] = top;
+                    named_bar(1, THR);
+                    if (tid < NR) {
+                        const float m = fmaxf(fmaxf(c_part[0][tid], c_part[1][tid]), fmaxf(c_part[2][tid], c_part[3][tid]));
+                        const float was = c_ref[tid];
+                        float now = was, fac = 1.f;
+                        if (m - was > OFF + SLACK) now = m - OFF, fac = was == NEG ? 0.f : ex2(was - now);
+                        c_ref[tid] = now, c_fac[tid] = fac;
+                    }
+                    named_bar(1, THR);
+                    float fac[CW];
+#pragma unroll
+                    for (int c = 0; c < CW; c += 4) *(float4 *)&fac[c] = *(const float4 *)&c_fac[c0 + c];
+#pragma unroll
+                    for (int c = 0; c < CW; ++c) l[c] *= fac[c];
+                    if (i > 0) {
+                        ok = ok && wide_wait(&odone, (n_tile - 1) & 1, dead, p.status);
+                        waited = true;
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int m = 0; m < PAIRS; ++m) {
+                            uint32_t o[CW];
+                            tmem_ldn<CW>(tmem + lanes + m * NR + c0, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int c = 0; c < CW; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * fac[c]);
+                            tmem_stn<CW>(tmem + lanes + m * NR + c0, o);
+                        }
+                        tmem_st_wait();
+                    }
+                }
+                uint32_t w[CW / 2];
+#pragma unroll
+                for (int c = 0; c < CW; c += 4) {
+                    const float4 m = *(const float4 *)&c_ref[c0 + c];
+                    const float e0 = ex2(x[c] - m.x), e1 = ex2(x[c + 1] - m.y), e2 = ex2(x[c + 2] - m.z),
+                                e3 = ex2(x[c + 3] - m.w);
+                    l[c] += e0, l[c + 1] += e1, l[c + 2] += e2, l[c + 3] += e3;
+                    if (lp.bf16) {
+                        const __nv_bfloat162 a = __floats2bfloat162_rn(e0, e1), b = __floats2bfloat162_rn(e2, e3);
+                        w[c / 2] = *(const uint32_t *)&a, w[c / 2 + 1] = *(const uint32_t *)&b;
+                    } else {
+                        w[c / 2] = pack_h2(e0, e1), w[c / 2 + 1] = pack_h2(e2, e3);
+                    }
+                }
+                if (!waited && n_tile > 0)     // P^T has been read
+                    ok = ok && wide_wait(&odone, (n_tile - 1) & 1, dead, p.status);
+#pragma unroll
+                for (int c = 0; c < CW / 2; c += 4) {
+                    const int ch = c0 / 8 + c / 4;       // 16 bytes of the token's weights
+                    const int sw = C::P_ROW == 128 ? ch ^ (key & 7) : ch ^ (key >> 1 & 3);
+                    *(uint4 *)(s_p + key * C::P_ROW + (sw << 4)) = make_uint4(w[c], w[c + 1], w[c + 2], w[c + 3]);
+                }
+                fence_async_smem();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&pfull);
+            }
+            // ---- totals
+            const float sum = over_lanes<CW>(l, [](float a, float b) { return a + b; });
+            if (lane < CW) c_part[quad][c0 + lane] = sum;
+            ok = ok && wide_wait(&odone, (n_tile - 1) & 1, dead, p.status);
+            named_bar(1, THR);
+            tc_fence_after();
+            // ---- whole items are written, others left for the joining kernel
+            const bool whole = n == cur.units;
+            float *part = p.partial + ((int64_t)blockIdx.x * 2 + (mine.from == 0)) * attend_slot_floats(NR, R);
+            const int64_t dst = (int64_t)sq.row0 * p.group + row_first;
+            if (tid < NR) {
+                const float tot = (c_part[0][tid] + c_part[1][tid]) + (c_part[2][tid] + c_part[3][tid]);
+                c_fac[tid] = tot > 0.f ? 1.f / tot : tot;      // a NaN stays one
+                if (!whole) part[NR * R + tid] = c_ref[tid], part[NR * R + NR + tid] = tot;
+                else if (tid < rows && p.lse) p.lse[dst + tid] = lse_of(c_ref[tid], tot);
+                if (!whole && tid == 0 && mine.from == 0)
+                    p.joins[blockIdx.x] =
+                        make_int4(cur.seq, 0, cur.tile, (int)((first + done - cur.unit + cur.units - 1) / per));
+            }
+            named_bar(1, THR);
+#pragma unroll 1
+            for (int m = 0; m < PAIRS; ++m) {
+                uint32_t o[CW];
+                tmem_ldn<CW>(tmem + lanes + m * NR + c0, o);
+                tmem_ld_wait();
+                const int d = m * 128 + key;
+#pragma unroll
+                for (int c = 0; c < CW; ++c) {
+                    const float y = __uint_as_float(o[c]) * c_fac[c0 + c];
+                    if (!whole) part[(c0 + c) * R + d] = y;
+                    else if (c0 + c < rows) {
+                        const int64_t at = (dst + c0 + c) * R + d;
+                        if (lp.bf16) ((__nv_bfloat16 *)p.out)[at] = __float2bfloat16_rn(y);
+                        else ((__half *)p.out)[at] = __float2half_rn(y);
+                    }
+                }
+            }
+            tc_fence_before();
+            left -= mine.used, done += mine.used;
+            if (left > 0) attend_next(p, NR, TOK, C::EXTRA, 1, ALL, cur);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+template <int R, int NR>
+cudaError_t run_absorbed(const LatentParams &p, const CUtensorMap &map, int box, int n_rows, int ctas, cudaStream_t st) {
+    using C = Absorbed<R, NR>;
+    auto *kernel = k_latent_absorbed<R, NR>;
+    // once a device (the attribute stays; another thread that comes first does the same)
+    static std::atomic<bool> ready[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !ready[dev].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) ready[dev].store(true, std::memory_order_release);
+    }
+    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, map, p, box, n_rows);
+}
+template <int R>
+cudaError_t run_absorbed_rows(const LatentParams &p, const CUtensorMap &map, int box, int n_rows, int rows, int ctas,
+                              cudaStream_t st) {
+    return rows == 16   ? run_absorbed<R, 16>(p, map, box, n_rows, ctas, st)
+           : rows == 32 ? run_absorbed<R, 32>(p, map, box, n_rows, ctas, st)
+                        : run_absorbed<R, 64>(p, map, box, n_rows, ctas, st);
+}
+
+// Rows of a tile, from the sequences' rows on average: a tile costs about the same whatever its
+// rows while bytes bound it, and fewer leave more room for tokens on their way.
+int tile_rows(const LatentParams &p) {
+    const int64_t rows = ceil_div((int64_t)p.a.n_q, (int64_t)p.a.n_seq) * p.a.q_heads;
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+}
+
+}  // namespace
+
+int64_t latent_joins_bytes(int ctas) { return ceil_div((int64_t)ctas * 16, (int64_t)256) * 256; }
+
+int64_t latent_absorbed_scratch(const LatentParams &p) {
+    const int ctas = device_sm_count();
+    return latent_joins_bytes(ctas) + (int64_t)ctas * 2 * attend_slot_floats(tile_rows(p), p.R) * 4;
+}
+
+int latent_box(const LatentParams &p) {
+    const int T = p.a.per_block * KV_UNIT;
+    return (T & -T) < 128 ? (T & -T) : 128;
+}
+cudaError_t latent_rows_map(const LatentParams &p, CUtensorMap *map) {
+    const uint64_t rows = (uint64_t)p.a.n_blocks * p.a.per_block * KV_UNIT, wide = p.R + p.P;
+    return make_tmap_2d(map, p.a.cache, p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                        wide, rows, wide * 2, 64, (uint32_t)latent_box(p));
+}
+
+cudaError_t launch_latent_absorbed(LatentParams &p, void *scratch, cudaStream_t st) {
+    const int ctas = device_sm_count(), rows = tile_rows(p), box = latent_box(p);
+    const int n_rows = (int)(p.a.n_blocks * p.a.per_block * KV_UNIT);
+    p.a.joins = (int4 *)scratch;
+    p.a.partial = (float *)((unsigned char *)scratch + latent_joins_bytes(ctas));
+    CUtensorMap map;
+    cudaError_t e = latent_rows_map(p, &map);
+    if (e != cudaSuccess) return e;
+    e = p.R == 128   ? run_absorbed_rows<128>(p, map, box, n_rows, rows, ctas, st)
+        : p.R == 256 ? run_absorbed_rows<256>(p, map, box, n_rows, rows, ctas, st)
+                     : run_absorbed_rows<512>(p, map, box, n_rows, rows, ctas, st);
+    if (e != cudaSuccess) return e;
+    return launch_attend_join(p.a, p.bf16 ? AKASHIC_DTYPE_BF16 : AKASHIC_DTYPE_FP16, p.R, ctas, rows, st);
+}
+
+}  // namespace ak

@@ -1,0 +1,523 @@
+// Expanded attention over the latent cache, on tcgen05: query rows of a head over its keys
+// [w_k c | rotated key] and values w_v c, which ak_latent_expand.cu has left in the scratch (the rotated keys
+// come from the cache, for all heads the same).
+//
+// 2 (nope + P + value) flops a visible pair bound it.  A CTA takes 256 query rows of a sequence and head,
+// two row tiles of 128, and runs over tiles of 128 tokens:
+//   copying warp   keys and values by tensor maps, a ring of its own each; beside them which tokens are
+//                  there, and their tags
+//   issuing warp   S = Q K^T into tensor memory, O += P V with P from there.  While one row tile's
+//                  scores are in the softmax, the tensor cores work on the other's
+//   softmax warps  a thread a row, 64 scores at a time: maximum, weights and total need no shuffle.  P replaces
+//                  its scores.  The maximum is raised, and O rescaled, only when a weight would pass 2^14
+// Tiles are shared out evenly over the CTAs (ak_attend.cuh); parts of an item are joined after it.
+#include <atomic>
+
+#include "ak_latent.cuh"
+#include "ak_umma.cuh"
+
+namespace ak {
+
+namespace {
+
+template <int DN, int DV>
+struct WideLatent {
+    static constexpr int ROWS = 256, TOK = 128, HALF = 64;
+    static constexpr int CHUNK = TOK * 128;              // 64 values of 128 rows
+    static constexpr int KC = DN / 64 + 1, VC = DV / 64; // chunks of a key, of a value
+    static constexpr int K_BYTES = KC * CHUNK, V_BYTES = VC * CHUNK, Q_BYTES = 2 * K_BYTES;
+    static constexpr int K_STAGES = 2, V_STAGES = Q_BYTES + 2 * (K_BYTES + V_BYTES) <= 229376 ? 2 : 1;
+    static constexpr int METAS = 3;                      // tiles whose tags are kept: the third's keys wait for the
+                                                         // second's scores, these for the first's weights
+    static constexpr int SMEM = 1024 + Q_BYTES + K_STAGES * K_BYTES + V_STAGES * V_BYTES;
+    static constexpr int SOFT = 8, THREADS = 32 * (SOFT + 2);
+    static constexpr int S_COL = 2 * DV;                 // tensor memory: O, then S
+    static_assert(S_COL + 2 * TOK <= 512, "tensor memory");
+    static constexpr int EXTRA = 2;                      // an item's beginning and end count as steps
+};
+
+__device__ __forceinline__ void store_row32h(const LatentParams &lp, int64_t at, const uint32_t (&y)[32]) {
+    uint32_t h[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const float a = __uint_as_float(y[2 * k]), b = __uint_as_float(y[2 * k + 1]);
+        if (lp.bf16) {
+            const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+            h[k] = *(const uint32_t *)&v;
+        } else {
+            h[k] = pack_h2(a, b);
+        }
+    }
+    uint32_t *dst = (uint32_t *)((uint16_t *)lp.a.out + at);
+    if (lp.a.out_wide) {
+#pragma unroll
+        for (int k = 0; k < 16; k += 4) *(uint4 *)(dst + k) = make_uint4(h[k], h[k + 1], h[k + 2], h[k + 3]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) dst[k] = h[k];
+    }
+}
+
+template <int DN, int DV>
+__global__ void __launch_bounds__(WideLatent<DN, DV>::THREADS, 1)
+k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap k_map,
+              const __grid_constant__ CUtensorMap v_map, const __grid_constant__ LatentParams lp,
+              const __grid_constant__ LatentSpace sp, const int box, const int n_rows) {
+    using C = WideLatent<DN, DV>;
+    constexpr int TOK = C::TOK, ROWS = C::ROWS, KS = C::K_STAGES, VS = C::V_STAGES, HT = C::HALF;
+    const AttendParams &p = lp.a;          // (heads: those of the group; its first is sp.head0)
+    extern __shared__ unsigned char raw_smem[];
+    unsigned char *smem = (unsigned char *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
+    unsigned char *s_q = smem, *s_k = smem + C::Q_BYTES, *s_v = s_k + KS * C::K_BYTES;
+    __shared__ uint64_t kfull[KS], kempty[KS], vfull[VS], vempty[VS], mfull[C::METAS];
+    __shared__ uint64_t sfull[2], pfull[2][2], odone[2][2], qfull[2], drained;
+    __shared__ alignas(16) int m_tag[C::METAS][TOK];
+    __shared__ uint32_t m_there[C::METAS]; // of a tile: a bit every 16 tokens that are listed
+    __shared__ uint32_t tmem_slot;
+    __shared__ int dead_word;
+    volatile int *dead = &dead_word;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    griddep_wait();
+    if (tid == 0) {
+        for (int i = 0; i < KS; ++i) mbar_init(&kfull[i], 1), mbar_init(&kempty[i], 1);
+        for (int i = 0; i < VS; ++i) mbar_init(&vfull[i], 1), mbar_init(&vempty[i], 1);
+        for (int i = 0; i < C::METAS; ++i) mbar_init(&mfull[i], 1);
+        for (int t = 0; t < 2; ++t) {
+            // One a half: two may be under way, and a wait knows only the last phase from the one
+            // before it.
+            for (int b = 0; b < 2; ++b) mbar_init(&pfull[t][b], 4), mbar_init(&odone[t][b], 1);
+            mbar_init(&sfull[t], 1), mbar_init(&qfull[t], 4);
+        }
+        mbar_init(&drained, 1);
+        mbar_fence_init();
+        dead_word = 0;
+        p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    }
+    if (warp == 0) {
+        tmem_alloc(&tmem_slot, 512);
+        tmem_relinquish();
+    }
+    int64_t *prefix = (int64_t *)s_q;      // until the warps have found their items
+    constexpr int ALL = 0x7fffffff;
+    attend_sums(p, ROWS, TOK, C::EXTRA, 1, ALL, prefix);
+    const int64_t total = prefix[C::THREADS];
+    const int64_t per = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x);
+    const int64_t first = per * blockIdx.x;
+    int left = (int)max((int64_t)0, min(per, total - first));
+    AttendCursor cur = {};
+    if (left > 0) cur = attend_find(p, ROWS, TOK, C::EXTRA, 1, ALL, prefix, first);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const bool tags = p.tags != nullptr;
+
+    if (warp == C::SOFT) {
+        // ---------------- copying
+        const int nb = TOK / box, T = p.per_block * KV_UNIT;
+        uint32_t n_tile = 0, n_k = 0, n_v = 0;
+        bool ok = true;
+        while (left > 0 && ok) {
+            const AttendPart part = attend_part(cur, left);
+            if (part.n <= 0) break;
+            const int first_tile = part.from + (p.ranges ? p.ranges[attend_range_at(p, cur.q, cur.tile, ROWS)].x : 0);
+            const int64_t *list = p.blocks + cur.seq * p.max_blocks;
+            // lane: the row of 16 tokens lane % 8 of a tile, -1: not listed
+            auto place = [&](int i) {
+                const int tok = (first_tile + i) * TOK + lane % 8 * 16;
+                if (i >= part.n || tok >= cur.q.kv) return -1;
+                const int b = tok / T;
+                const int64_t id = list[b];
+                if (id >= 0 && id < p.n_blocks) return (int)(id * T + (tok - b * T));
+                if (id != -1) set_status(p.status, AKASHIC_EDEVICE);
+                return -1;
+            };
+            // lane: the tags of four tokens
+            auto tags_of = [&](int row) {
+                const int r = __shfl_sync(0xffffffffu, row, lane / 4);
+                return tags && r >= 0 ? *(const int4 *)(p.tags + (int64_t)r + lane % 4 * 4) : make_int4(-1, -1, -1, -1);
+            };
+            const int64_t at = ((int64_t)cur.head * p.n_seq + cur.seq) * sp.seq_rows;
+            int next = place(0);
+            int4 next_tags = tags_of(next);
+            for (int i = 0; ok && i < part.n; ++i, ++n_tile) {
+                const int row = next, tok = (first_tile + i) * TOK;
+                const int4 tag = next_tags;
+                next = place(i + 1);
+                const uint32_t st = n_tile % KS, me = n_tile % C::METAS, sv = n_tile % VS;
+                ok = wide_wait(&kempty[st], ((n_tile / KS) & 1) ^ 1, dead, p.status);
+                if (!ok) break;
+                const uint32_t there = __ballot_sync(0xffffffffu, row >= 0) & 255u;
+                if (tags)
+                    *(int4 *)&m_tag[me][4 * lane] = make_int4(max(tag.x, -1), max(tag.y, -1), max(tag.z, -1), max(tag.w, -1));
+                if (lane == 0) m_there[me] = there;
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&mfull[me]);
+                    mbar_expect_tx(&kfull[st], C::K_BYTES);
+                }
+                // the sequence's rows in the scratch end with its tiles: behind them zeros
+                const int y = tok < max(cur.q.kv, 1) ? (int)(at + tok) : (int)sp.rows;
+                const int box_row = __shfl_sync(0xffffffffu, row, lane % nb * (box / 16));
+                __syncwarp();
+                unsigned char *kt = s_k + st * C::K_BYTES;
+                if (lane < nb)
+                    tma_load_2d(kt + (C::KC - 1) * C::CHUNK + lane * box * 128, &rows_map, &kfull[st], lp.R,
+                                box_row < 0 ? n_rows : box_row);
+                else if (lane >= 16 && lane < 16 + C::KC - 1)
+                    tma_load_2d(kt + (lane - 16) * C::CHUNK, &k_map, &kfull[st], (lane - 16) * 64, y);
+                ++n_k;
+                next_tags = tags_of(next);
+                ok = wide_wait(&vempty[sv], ((n_tile / VS) & 1) ^ 1, dead, p.status);
+                if (!ok) break;
+                if (lane == 0) mbar_expect_tx(&vfull[sv], C::V_BYTES);
+                __syncwarp();
+                if (lane < C::VC) tma_load_2d(s_v + sv * C::V_BYTES + lane * C::CHUNK, &v_map, &vfull[sv], lane * 64, y);
+                ++n_v;
+            }
+            left -= part.used;
+            if (left > 0) attend_next(p, ROWS, TOK, C::EXTRA, 1, ALL, cur);
+        }
+        // nothing is on its way when the CTA ends (where a wait gave up; else all has been read)
+        for (uint32_t i = 0; !ok && i < KS; ++i)
+            if (n_k > i) mbar_wait(&kfull[i], ((n_k - i - 1) / KS) & 1, p.status);
+        for (uint32_t i = 0; !ok && i < VS; ++i)
+            if (n_v > i) mbar_wait(&vfull[i], ((n_v - i - 1) / VS) & 1, p.status);
+        __syncwarp();
+    } else if (warp == C::SOFT + 1) {
+        // ---------------- issuing
+        const uint32_t id_s = idesc_f16(TOK, lp.bf16), id_o = idesc_f16(DV, lp.bf16) | IDESC_B_MN_MAJOR;
+        const uint32_t go = lane == 0;
+        const uint32_t q_at = desc_k(smem_u32(s_q)), k_at = desc_k(smem_u32(s_k)), v_at = desc_mn(smem_u32(s_v), C::CHUNK);
+        const int rope_steps = lp.P / 16;
+        uint32_t n_tile = 0, q_phase = 0, tiles0 = 0, tiles1 = 0;      // tiles: of the row tile, so far
+        bool ok = true;
+        // S of the item's tile i for row tile t; the row tiles share a tile's keys
+        auto scores = [&](int t, int i, int mt) {
+            const uint32_t x = n_tile + i, st = x % KS;
+            if (ok && t == 0) ok = wide_wait(&kfull[st], (x / KS) & 1, dead, p.status);
+            if (!ok) return;
+            tc_fence_after();
+            const uint32_t d = tmem + C::S_COL + t * TOK;
+            const uint32_t qa = q_at + t * (C::K_BYTES >> 4), ka = k_at + st * (C::K_BYTES >> 4);
+#pragma unroll
+            for (int k = 0; k < DN / 16; ++k) {
+                const uint32_t o = k / 4 * (C::CHUNK >> 4) + 2 * (k % 4);
+                umma_ss(go, d, qa + o, ka + o, id_s, k > 0);
+            }
+            for (int k = 0; k < rope_steps; ++k) {
+                const uint32_t o = (C::KC - 1) * (C::CHUNK >> 4) + 2 * k;
+                umma_ss(go, d, qa + o, ka + o, id_s, 1);
+            }
+            umma_commit_if(go, &sfull[t]);
+            if (t == mt - 1) umma_commit_if(go, &kempty[st]);
+        };
+        auto values = [&](int t, int i, int b, int mt) {
+            const uint32_t x = n_tile + i, sv = x % VS, c = (t ? tiles1 : tiles0) + i;
+            if (ok && t == 0 && b == 0) ok = wide_wait(&vfull[sv], (x / VS) & 1, dead, p.status);
+            if (ok) ok = wide_wait(&pfull[t][b], c & 1, dead, p.status);
+            if (!ok) return;
+            tc_fence_after();
+            const uint32_t va = v_at + sv * (C::V_BYTES >> 4) + b * (HT * 128 >> 4);
+#pragma unroll
+            for (int k = 0; k < HT / 16; ++k)
+                umma_ts(go, tmem + t * DV, tmem + C::S_COL + t * TOK + b * HT + k * 8, va + (2048 * k >> 4), id_o,
+                        i > 0 || b > 0 || k > 0);
+            umma_commit_if(go, &odone[t][b]);
+            if (t == mt - 1 && b == 1) umma_commit_if(go, &vempty[sv]);
+        };
+        while (left > 0 && ok) {
+            const AttendPart part = attend_part(cur, left);
+            const int n = part.n;
+            if (n <= 0) break;
+            const int mt = cur.q.nq * p.group - cur.tile * ROWS > 128 ? 2 : 1;
+            for (int t = 0; t < mt; ++t) {
+                if (ok) ok = wide_wait(&qfull[t], q_phase >> t & 1, dead, p.status);
+                q_phase ^= 1u << t;
+                scores(t, 0, mt);
+            }
+            for (int i = 0; ok && i < n; ++i) {
+                for (int t = 0; t < mt; ++t) values(t, i, 0, mt);
+                for (int t = 0; t < mt; ++t) {
+                    values(t, i, 1, mt);
+                    if (i + 1 < n) scores(t, i + 1, mt);
+                }
+            }
+            tiles0 += n;
+            if (mt > 1) tiles1 += n;
+            n_tile += n;
+            left -= part.used;
+            if (left > 0) attend_next(p, ROWS, TOK, C::EXTRA, 1, ALL, cur);
+        }
+        umma_commit_if(go, &drained);          // what was issued ends before the tensor memory goes
+        mbar_wait(&drained, 0, p.status);
+        __syncwarp();
+    } else {
+        // ---------------- softmax: a lane is row 32 (warp % 4) + lane of row tile t
+        const int t = warp >> 2, rt = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t o_at = tmem + lanes + t * DV;
+        const float f = p.scale * LOG2E_F;
+        uint32_t n_tile = 0, tiles = 0;        // tiles: of this row tile, so far
+        bool ok = true;
+        int64_t done = 0;
+        while (left > 0 && ok) {
+            const AttendPart mine = attend_part(cur, left);
+            const int n = mine.n;
+            if (n <= 0) break;
+            const AttendSeq sq = cur.q;
+            const int row_first = cur.tile * ROWS, rows = min(ROWS, sq.nq - row_first);
+            const int first_tile = mine.from + (p.ranges ? p.ranges[attend_range_at(p, sq, cur.tile, ROWS)].x : 0);
+            if (t == 0 || rows > 128) {
+                // ---- the warp's 32 query rows, 16 bytes a lane
+                const int g_all = (DN + lp.P) / 8, head = sp.head0 + cur.head;
+#pragma unroll 4
+                for (int x = lane; x < 32 * g_all; x += 32) {
+                    const int y = x / g_all, g = x - y * g_all, row = (warp & 3) * 32 + y;
+                    uint4 z = make_uint4(0, 0, 0, 0);
+                    if (t * 128 + row < rows) {
+                        const uint16_t *src = (const uint16_t *)p.q + (int64_t)(sq.row0 + row_first + t * 128 + row) * p.q_row +
+                                              head * p.q_head + g * 8;
+                        if (p.q_wide) {
+                            z = *(const uint4 *)src;
+                        } else {
+                            alignas(16) uint16_t h[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) h[k] = src[k];
+                            z = *(const uint4 *)h;
+                        }
+                    }
+                    *(uint4 *)(s_q + t * C::K_BYTES + (g >> 3) * C::CHUNK + row * 128 + (((g & 7) ^ (row & 7)) << 4)) = z;
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&qfull[t]);
+                const int r = t * 128 + rt;
+                const bool real = r < rows;
+                const int limit = real ? attend_limit(p, sq, row_first + r) : sq.kv;
+                // a slot without a token has tag -1, and a row that sees none -2
+                const int qt = real && tags ? p.q_tags[sq.row0 + row_first + r] : -2, qtag = qt < 0 ? -2 : qt;
+                const int safe = attend_limit(p, sq, row_first + t * 128) - HT;
+                float mm = 0.f, l = 0.f;
+                bool unset = real;             // no key seen yet: mm = 0
+                for (int i = 0; i < n; ++i, ++tiles) {
+                    const uint32_t me = (n_tile + i) % C::METAS;
+                    // (the scores first: a row tile that had no rows in the items before has not followed the
+                    // other barrier, and by their time it can be in no later phase)
+                    ok = wide_wait(&sfull[t], tiles & 1, dead, p.status);
+                    if (ok) ok = wide_wait(&mfull[me], ((n_tile + i) / C::METAS) & 1, dead, p.status);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t there = m_there[me];
+#pragma unroll 1
+                    for (int b = 0; b < 2; ++b) {
+                        const uint32_t s_at = tmem + lanes + C::S_COL + t * TOK + b * HT;
+                        const int tok = (first_tile + i) * TOK + b * HT;
+                        const uint32_t bits = there >> (4 * b) & 15u;
+                        uint32_t x[HT];
+                        auto pair = [&](int k) { return f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])); };
+                        tmem_ld32(s_at, *(uint32_t(*)[32])x);
+                        tmem_ld32(s_at + 32, *(uint32_t(*)[32])(x + 32));
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int k = 0; k < HT; k += 2) {
+                            const float2 y = f2_open(f2_mul(pair(k), f2_pack(f, f)));
+                            x[k] = __float_as_uint(y.x), x[k + 1] = __float_as_uint(y.y);
+                        }
+                        if (tags || tok > safe || bits != 15u) {
+#pragma unroll
+                            for (int u = 0; u < HT / 16; ++u) {
+                                const int end = bits >> u & 1u ? limit - tok - u * 16 : 0;
+#pragma unroll
+                                for (int k = 0; k < 16; ++k)
+                                    if (k >= end) x[u * 16 + k] = 0xff800000u;
+                                if (!tags) continue;
+#pragma unroll
+                                for (int k = 0; k < 16; k += 4) {
+                                    const int4 y = *(const int4 *)&m_tag[me][b * HT + u * 16 + k];
+                                    x[u * 16 + k] = y.x == qtag ? x[u * 16 + k] : 0xff800000u;
+                                    x[u * 16 + k + 1] = y.y == qtag ? x[u * 16 + k + 1] : 0xff800000u;
+                                    x[u * 16 + k + 2] = y.z == qtag ? x[u * 16 + k + 2] : 0xff800000u;
+                                    x[u * 16 + k + 3] = y.w == qtag ? x[u * 16 + k + 3] : 0xff800000u;
+                                }
+                            }
+                        }
+                        float top = __uint_as_float(x[0]);
+#pragma unroll
+                        for (int k = 1; k < HT; ++k) top = fmaxf(top, __uint_as_float(x[k]));
+                        // the maximum is raised when a weight would pass 2^14
+                        const bool rises = unset ? top > -INFINITY : top - mm > P_SHIFT + M_SLACK;
+                        const bool moves = __any_sync(0xffffffffu, rises);         // O changes its scale
+                        float down = 1.f;
+                        if (rises) {
+                            down = unset ? 0.f : ex2(mm - (top - P_SHIFT));
+                            unset = false;
+                            mm = top - P_SHIFT;
+                        }
+                        uint64_t sum[2] = {0, 0};
+                        uint32_t pk[HT / 2];
+#pragma unroll
+                        for (int k = 0; k < HT; k += 2) {
+                            const float2 u = f2_open(f2_add(pair(k), f2_pack(-mm, -mm)));
+                            const float e0 = ex2(u.x), e1 = ex2(u.y);
+                            sum[k / 2 % 2] = f2_add(sum[k / 2 % 2], f2_pack(e0, e1));
+                            if (lp.bf16) {
+                                const __nv_bfloat162 w = __floats2bfloat162_rn(e0, e1);
+                                pk[k / 2] = *(const uint32_t *)&w;
+                            } else {
+                                pk[k / 2] = pack_h2(e0, e1);
+                            }
+                        }
+                        const float2 y = f2_open(f2_add(sum[0], sum[1]));
+                        l = l * down + (y.x + y.y);
+                        tmem_st32(s_at, pk);
+                        if (i + b > 0 && moves) {
+                            // once the products before have been added
+                            ok = wide_wait(&odone[t][b ^ 1], (b ? tiles : tiles - 1) & 1, dead, p.status);
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int d = 0; d < DV; d += 32) {
+                                uint32_t z[32];
+                                tmem_ld32(o_at + d, z);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) z[k] = __float_as_uint(__uint_as_float(z[k]) * down);
+                                tmem_st32(o_at + d, z);
+                            }
+                        }
+                        tmem_st_wait();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&pfull[t][b]);
+                    }
+                    if (!ok) break;
+                }
+                if (ok) ok = wide_wait(&odone[t][1], (tiles - 1) & 1, dead, p.status);
+                if (!ok) break;
+                tc_fence_after();
+                // ---- whole items are written, others left for the joining kernel
+                const bool whole = n == cur.units;
+                if (unset) mm = NEG;
+                float *part = p.partial + ((int64_t)blockIdx.x * 2 + (mine.from == 0)) * attend_slot_floats(ROWS, DV);
+                const float inv = l > 0.f ? 1.f / l : l;       // a NaN stays one
+                const int64_t dst = (int64_t)(sq.row0 + row_first + r) * p.q_heads + head;
+#pragma unroll 1
+                for (int d = 0; d < DV; d += 32) {
+                    uint32_t y[32];
+                    tmem_ld32(o_at + d, y);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * inv);
+                    if (!real) continue;
+                    if (whole) {
+                        store_row32h(lp, dst * DV + d, y);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4)
+                            *(uint4 *)(part + r * DV + d + k) = make_uint4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+                    }
+                }
+                if (!whole) {
+                    part[ROWS * DV + r] = mm, part[ROWS * DV + ROWS + r] = l;
+                    if (r == 0 && mine.from == 0)
+                        p.joins[blockIdx.x] =
+                            make_int4(cur.seq, head, cur.tile, (int)((first + done - cur.unit + cur.units - 1) / per));
+                }
+                tc_fence_before();
+            }
+            n_tile += n;
+            left -= mine.used, done += mine.used;
+            if (left > 0) attend_next(p, ROWS, TOK, C::EXTRA, 1, ALL, cur);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+template <int DN, int DV>
+cudaError_t run_wide(const LatentParams &p, const LatentSpace &sp, int ctas, cudaStream_t st) {
+    using C = WideLatent<DN, DV>;
+    auto *kernel = k_latent_wide<DN, DV>;
+    // once a device (the attribute stays; another thread that comes first does the same)
+    static std::atomic<bool> ready[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !ready[dev].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) ready[dev].store(true, std::memory_order_release);
+    }
+    const CUtensorMapDataType type = p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    CUtensorMap rows, k, v;
+    e = latent_rows_map(p, &rows);
+    if (e == cudaSuccess) e = make_tmap_2d(&k, sp.k, type, 2, DN, (uint64_t)sp.rows, DN * 2, 64, C::TOK);
+    if (e == cudaSuccess) e = make_tmap_2d(&v, sp.v, type, 2, DV, (uint64_t)sp.rows, DV * 2, 64, C::TOK);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, rows, k, v, p, sp, latent_box(p),
+                      (int)(p.a.n_blocks * p.a.per_block * KV_UNIT));
+}
+
+constexpr int WIDE_ROWS = 256;
+// The heads whose keys and values are in the scratch at a time: all, as far as these take 2 GB.
+struct Plan {
+    int64_t seq_rows, joins, ranges, partial, k, v;    // rows a sequence and head; bytes
+    int heads, ctas;
+};
+Plan plan_of(const LatentParams &p) {
+    Plan x;
+    x.ctas = device_sm_count();
+    x.seq_rows = ceil_div((int64_t)(p.a.max_kv > 0 ? p.a.max_kv : 1), (int64_t)128) * 128;
+    const int64_t rows = x.seq_rows * p.a.n_seq, room = (2LL << 30) / (rows * (p.nope + p.value) * 2);
+    const int64_t most = room < 1 ? 1 : room < p.a.q_heads ? room : p.a.q_heads;
+    x.heads = (int)ceil_div((int64_t)p.a.q_heads, ceil_div((int64_t)p.a.q_heads, most));
+    x.joins = latent_joins_bytes(x.ctas);
+    x.ranges = p.a.tags ? ceil_div(attend_ranges(p.a.n_q, 1, p.a.n_seq, WIDE_ROWS) * 8, (int64_t)256) * 256 : 0;
+    x.partial = x.ctas * 2 * attend_slot_floats(WIDE_ROWS, p.value) * 4;
+    x.k = rows * x.heads * p.nope * 2, x.v = rows * x.heads * p.value * 2;
+    return x;
+}
+
+}  // namespace
+
+int64_t latent_expanded_scratch(const LatentParams &p) {
+    const Plan x = plan_of(p);
+    if (x.seq_rows * p.a.n_seq * x.heads > 0x7fffffffLL - 8192) return -1;
+    return x.joins + x.ranges + x.partial + x.k + x.v;
+}
+
+cudaError_t launch_latent_expanded(LatentParams &p, void *scratch, cudaStream_t st) {
+    const Plan x = plan_of(p);
+    unsigned char *at = (unsigned char *)scratch;
+    AttendParams &a = p.a;
+    LatentSpace sp = {};
+    a.joins = (int4 *)at, at += x.joins;
+    int2 *ranges = (int2 *)at;
+    at += x.ranges;
+    a.partial = (float *)at, at += x.partial;
+    sp.k = at, sp.v = at + x.k;
+    sp.seq_rows = x.seq_rows;
+    sp.k_step = p.k_head / p.k_row, sp.v_step = p.v_head / p.v_row;
+    cudaError_t e = cudaSuccess;
+    if (x.ranges) {
+        a.ranges = ranges;
+        e = launch_attend_ranges(a, 128, {WIDE_ROWS, x.ctas}, 1, 0x7fffffff, st);
+    }
+    for (int h = 0; e == cudaSuccess && h < a.q_heads; h += x.heads) {
+        sp.head0 = h, sp.heads = a.heads = a.q_heads - h < x.heads ? a.q_heads - h : x.heads;
+        sp.rows = x.seq_rows * a.n_seq * sp.heads;
+        e = launch_latent_expand(p, sp, st);
+        if (e == cudaSuccess)
+            e = p.nope == 64 ? p.value == 64 ? run_wide<64, 64>(p, sp, x.ctas, st) : run_wide<64, 128>(p, sp, x.ctas, st)
+                : p.value == 64 ? run_wide<128, 64>(p, sp, x.ctas, st) : run_wide<128, 128>(p, sp, x.ctas, st);
+        if (e == cudaSuccess)
+            e = launch_attend_join(a, p.bf16 ? AKASHIC_DTYPE_BF16 : AKASHIC_DTYPE_FP16, p.value, x.ctas, WIDE_ROWS, st);
+    }
+    return e;
+}
+
+}  // namespace ak

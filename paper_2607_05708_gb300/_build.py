@@ -18,7 +18,8 @@ LIB = os.path.join(HERE, "libakashic_mem.so")
 SOURCES = ["ak_api.cu", "ak_score.cu", "ak_graph.cu", "ak_select.cu", "ak_update.cu",
            "ak_inedges.cu", "ak_delete.cu", "ak_mm.cu", "ak_noalloc.cu", "ak_reach.cu", "ak_kv.cu",
            "ak_attend.cu", "ak_attend_wide.cu", "ak_latent.cu",
-           "ak_latent_absorbed.cu", "ak_latent_expand.cu", "ak_latent_wide.cu"]
+           "ak_latent_absorbed.cu", "ak_latent_expand.cu", "ak_latent_wide.cu",
+           "ak_latent_join.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

@@ -874,7 +874,7 @@ cudaError_t launch_attend_narrow(const AttendParams &p, int bits, int dim, int d
 cudaError_t launch_attend_join(const AttendParams &p, int dtype, int dim, int ctas, int rows,
                                cudaStream_t st) {
     const bool bf16 = dtype == AKASHIC_DTYPE_BF16;
-    auto *kernel = dim == 64 ? k_attend_join<64> : dim == 128 ? k_attend_join<128> : dim == 256 ? k_attend_join<256> : k_attend_join<512>;
+    auto *kernel = dim == 64 ? k_attend_join<64> : dim == 128 ? k_attend_join<128> : k_attend_join<256>;
     if (ctas > JOIN_CTAS) return cudaErrorInvalidValue;        // (a GPU of more than 512 SMs)
     return launch_pdl(kernel, dim3(ctas, (rows + JOIN_ROWS - 1) / JOIN_ROWS), dim3(256), 0, st, p, rows, bf16);
 }

@@ -23,6 +23,96 @@ struct LatentParams {
     int64_t k_head, k_row, v_head, v_row;
 };
 
+__device__ __forceinline__ uint16_t round16(float x, bool bf16) {
+    return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
+}
+// Eight values of a query row.
+__device__ __forceinline__ uint4 load_row8(const uint16_t *src, bool wide) {
+    if (wide) return *(const uint4 *)src;
+    alignas(16) uint16_t h[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) h[k] = src[k];
+    return *(const uint4 *)h;
+}
+
+// attend_sums and attend_find in one where every thread has a sequence at most: the thread whose sequence has
+// the CTA's first step knows where (3500 cycles less at a kernel's beginning).  All threads call it; prefix: blockDim.x + 1
+// words of shared memory.  first, left: the CTA's share.
+struct LatentShare {
+    AttendCursor cur;
+    int64_t first, per;
+    int left;
+};
+__device__ __forceinline__ LatentShare latent_share(const AttendParams &p, int rows, int step, int extra,
+                                                    int64_t *prefix) {
+    constexpr int ALL = 0x7fffffff;
+    __shared__ AttendCursor found;
+    __shared__ int have_found;
+    const int nt = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    LatentShare r;
+    AttendSeq q = {};
+    int64_t sum = 0, before = 0;
+    const bool one = p.n_seq <= nt;
+    if (tid == 0) have_found = 0;
+    if (one) {
+        const bool have = tid < p.n_seq;
+        q = attend_seq(p, have ? tid : 0);
+        sum = attend_seq_units(p, q, have, rows, step, extra, 1, ALL) * p.heads;
+        int64_t incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        if (lane == 31) prefix[warp] = incl;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) before += prefix[w];
+        __syncthreads();
+        before += incl - sum;
+        prefix[tid] = before;
+        if (tid == nt - 1) prefix[nt] = before + sum;
+        __syncthreads();
+    } else {
+        attend_sums(p, rows, step, extra, 1, ALL, prefix);
+    }
+    const int64_t total = prefix[nt], g = gridDim.x;
+    r.per = total + g < 0x7fffffff ? max(1u, ((uint32_t)total + (uint32_t)g - 1u) / (uint32_t)g) : (total + g - 1) / g;
+    r.first = r.per * blockIdx.x;
+    r.left = (int)max((int64_t)0, min(r.per, total - r.first));
+    r.cur = {};
+    if (r.left <= 0) return r;                 // (the whole CTA)
+    if (one) {
+        int64_t rest = r.first - before;
+        if (rest >= 0 && rest < sum && attend_tiles(p, q, rows) <= 8 && sum < 0x7fffffff) {
+            const int of_head = (int)sum / p.heads;
+            AttendCursor c = {};
+            c.seq = tid, c.q = q;
+            c.head = (int)rest / of_head;
+            int x = (int)rest - c.head * of_head;
+            while (x >= (c.units = extra + attend_units(p, q, c.tile, rows, step))) x -= c.units, ++c.tile;
+            c.units -= extra;
+            c.unit = x - extra;
+            found = c;
+            have_found = 1;
+        }
+        __syncthreads();
+        if (have_found) {
+            r.cur = found;
+            return r;
+        }
+    }
+    r.cur = attend_find(p, rows, step, extra, 1, ALL, prefix, r.first);
+    return r;
+}
+
+// What the joining kernel has to join, an entry a CTA of the kernel before: of an item that begins in its
+// share and ends in another's the row of out (and lse) of its first row, its rows (0: none) and the last
+// CTA.  From one of its rows to the next it is `step` rows of out.
+struct alignas(16) LatentJoin {
+    int64_t dst;
+    int rows, last;
+};
+
 // The expanded form's keys and values of a group of heads: row (head, sequence, token) at (head *
 // n_seq + sequence) * seq_rows + token.
 struct LatentSpace {
@@ -37,6 +127,8 @@ struct LatentSpace {
 int64_t latent_joins_bytes(int ctas);
 int latent_box(const LatentParams &p);
 cudaError_t latent_rows_map(const LatentParams &p, CUtensorMap *map);
+
+cudaError_t launch_latent_join(const LatentParams &p, int dim, int ctas, int rows, int step, cudaStream_t st);
 
 int64_t latent_absorbed_scratch(const LatentParams &p);
 int64_t latent_expanded_scratch(const LatentParams &p);  // -1: too many tokens

@@ -8,8 +8,9 @@
 // so that M is full whatever the number of heads, and the R x rows accumulators (4 x 64 columns of
 // 128 lanes at R = 512) leave tensor memory for two S.  One copy of a tile in shared memory serves both
 // products: as K it is K-major, as C^T the same bytes are MN-major.
-//   copying warp   the tile's boxes of tokens, from the listed blocks, in pairs of 64-dim chunks;
-//                  blocks that are not listed read as zeros
+//   a warp ahead   looks up the tiles' blocks and starts their rows' way into L2
+//   copying warp   the tile's boxes of tokens in pairs of 64-dim chunks; blocks that are not listed
+//                  read as zeros
 //   issuing warp   scores of the next tile and O^T += of this one, whichever is ready
 //   softmax warps  a thread a token and up to 32 rows.  Weights are relative to a reference of the row, not
 //                  to its running maximum, and the reference is raised, O^T and the totals rescaled, only when a
@@ -31,7 +32,7 @@ struct Absorbed {
     static constexpr int PAIRS = R / 128, CHUNKS = R / 64 + 1;
     static constexpr int CW = NR < 32 ? NR : 32;         // rows of a softmax thread
     static constexpr int SOFT = NR / CW * 4;             // softmax warps
-    static constexpr int THREADS = 32 * (SOFT + 2);
+    static constexpr int THREADS = 32 * (SOFT + 3);
     static constexpr int PAIR_BYTES = TOK * 256, ROPE_BYTES = TOK * 128;
     static constexpr int Q_BYTES = CHUNKS * NR * 128;
     // P^T: a row a token; 64 bytes of it, in the 64-byte swizzle, hold 32 rows' weights
@@ -49,8 +50,8 @@ struct Absorbed {
     static constexpr int SMEM = 1024 + Q_BYTES + P_BYTES + ROPES * ROPE_BYTES + STAGES * PAIR_BYTES;
     static constexpr int S_COL = 256;                    // tensor memory: O^T, then two S^T
     static_assert(PAIRS * NR <= S_COL && S_COL + 2 * NR <= 512, "tensor memory");
-    static constexpr int METAS = 8;                      // tiles whose places are kept
-    static_assert(METAS > STAGES / PAIRS + 1, "a tile's places are read before they are written again");
+    static constexpr int METAS = R == 512 ? 3 : R == 256 ? 5 : 8;      // tiles whose places are known
+    static_assert(METAS > STAGES / PAIRS, "the tiles on their way");
     // An item's beginning and end (rows in, result out, an empty pipeline) count as steps.
     static constexpr int EXTRA = 1;
 };
@@ -114,7 +115,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
     unsigned char *s_q = s_p + C::P_BYTES;
     if (C::ALIAS) s_rope = s_p;
     __shared__ uint64_t full[ST], empty[ST], rope_full[C::ROPE_SLOTS], rope_empty[C::ROPE_SLOTS];
-    __shared__ uint64_t sfull[2], pfull, odone, qfull, mfull[C::METAS], drained;
+    __shared__ uint64_t sfull[2], pfull, odone, qfull, mfull[C::METAS], mempty[C::METAS], drained;
     __shared__ int m_row[C::METAS][8];                   // first row of each of a tile's boxes, -1: none
     __shared__ alignas(16) float c_ref[NR], c_fac[NR];
     __shared__ alignas(16) int c_limit[NR], c_tag[NR];
@@ -128,26 +129,22 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
     if (tid == 0) {
         for (int i = 0; i < ST; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
         for (int i = 0; i < C::ROPE_SLOTS; ++i) mbar_init(&rope_full[i], 1), mbar_init(&rope_empty[i], 1);
-        for (int i = 0; i < C::METAS; ++i) mbar_init(&mfull[i], 1);
+        for (int i = 0; i < C::METAS; ++i) mbar_init(&mfull[i], 1), mbar_init(&mempty[i], 1);
         for (int i = 0; i < 2; ++i) mbar_init(&sfull[i], 1);
         mbar_init(&pfull, C::SOFT), mbar_init(&odone, 1), mbar_init(&qfull, C::SOFT), mbar_init(&drained, 1);
         mbar_fence_init();
         dead_word = 0;
-        p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        ((LatentJoin *)p.joins)[blockIdx.x] = {0, 0, 0};
     }
     if (warp == 0) {
         tmem_alloc(&tmem_slot, 512);
         tmem_relinquish();
     }
-    int64_t *prefix = (int64_t *)s_q;                    // until the warps have found their items
     constexpr int ALL = 0x7fffffff;
-    attend_sums(p, NR, TOK, C::EXTRA, 1, ALL, prefix);
-    const int64_t total = prefix[C::THREADS];
-    const int64_t per = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x);
-    const int64_t first = per * blockIdx.x;
-    int left = (int)max((int64_t)0, min(per, total - first));
-    AttendCursor cur = {};
-    if (left > 0) cur = attend_find(p, NR, TOK, C::EXTRA, 1, ALL, prefix, first);
+    const LatentShare share = latent_share(p, NR, TOK, C::EXTRA, (int64_t *)s_q);      // (until it holds query rows)
+    const int64_t first = share.first, per = share.per;
+    int left = share.left;
+    AttendCursor cur = share.cur;
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -155,37 +152,20 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
 
     if (warp == C::SOFT) {
         // ---------------- copying
-        const int nb = TOK / box, T = p.per_block * KV_UNIT;           // boxes of a chunk
+        const int nb = TOK / box;              // boxes of a chunk
         uint32_t n_tile = 0, n_pair = 0, n_rope = 0;
         bool ok = true;
         while (left > 0 && ok) {
             const AttendPart part = attend_part(cur, left);
             if (part.n <= 0) break;
-            const int64_t *list = p.blocks + cur.seq * p.max_blocks;
-            // lane: the row of box lane % nb of a tile
-            auto place = [&](int i) {
-                const int tok = (part.from + i) * TOK + lane % nb * box;
-                if (i >= part.n || tok >= cur.q.kv) return -1;
-                const int b = tok / T;
-                const int64_t id = list[b];
-                if (id >= 0 && id < p.n_blocks) return (int)(id * T + (tok - b * T));
-                if (id != -1) set_status(p.status, AKASHIC_EDEVICE);
-                return -1;
-            };
-            int next = place(0);
             for (int i = 0; ok && i < part.n; ++i, ++n_tile) {
-                const int row = next;
-                next = place(i + 1);
-                const int y = row < 0 ? n_rows : row;    // behind the last row: zeros
-                for (int k = 0; k < PAIRS; ++k, ++n_pair) {
+                const uint32_t me = n_tile % C::METAS;
+                ok = wide_wait(&mfull[me], (n_tile / C::METAS) & 1, dead, p.status);
+                const int row = m_row[me][lane % nb], y = row < 0 ? n_rows : row;      // behind the last row: zeros
+                for (int k = 0; ok && k < PAIRS; ++k, ++n_pair) {
                     const uint32_t st = n_pair % ST;
                     ok = wide_wait(&empty[st], ((n_pair / ST) & 1) ^ 1, dead, p.status);
                     if (!ok) break;
-                    if (k == 0) {
-                        if (lane < nb) m_row[n_tile % C::METAS][lane] = row;
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&mfull[n_tile % C::METAS]);
-                    }
                     if (lane == 0) mbar_expect_tx(&full[st], C::PAIR_BYTES);
                     __syncwarp();
                     if (lane < 2 * nb) {
@@ -194,9 +174,8 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                                     &full[st], (2 * k + c) * 64, y);
                     }
                 }
-                if (!ok) break;
                 const uint32_t sr = n_tile % C::ROPE_SLOTS;
-                ok = wide_wait(&rope_empty[sr], ((n_tile / C::ROPE_SLOTS) & 1) ^ 1, dead, p.status);
+                if (ok) ok = wide_wait(&rope_empty[sr], ((n_tile / C::ROPE_SLOTS) & 1) ^ 1, dead, p.status);
                 if (!ok) break;
                 if (lane == 0) mbar_expect_tx(&rope_full[sr], C::ROPE_BYTES);
                 __syncwarp();
@@ -213,13 +192,50 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
         for (uint32_t i = 0; !ok && i < C::ROPE_SLOTS; ++i)
             if (n_rope > i) mbar_wait(&rope_full[i], ((n_rope - i - 1) / C::ROPE_SLOTS) & 1, p.status);
         __syncwarp();
+    } else if (warp == C::SOFT + 2) {
+        // ---------------- looking ahead: the tiles' places, and their rows, which are contiguous within a
+        // box, on their way into L2 while the tiles before are worked on.  (The copies take 128 bytes of
+        // a row at a time, and shared memory holds little more than a tile: alone they left latency
+        // uncovered.)
+        const int nb = TOK / box, T = p.per_block * KV_UNIT, wide = (R + lp.P) * 2;
+        uint32_t n_tile = 0;
+        bool ok = true;
+        while (left > 0 && ok) {
+            const AttendPart part = attend_part(cur, left);
+            if (part.n <= 0) break;
+            const int64_t *list = p.blocks + cur.seq * p.max_blocks;
+            // lane: the row of box lane of a tile, -1: none
+            auto place = [&](int i) {
+                const int tok = (part.from + i) * TOK + lane * box;
+                if (lane >= nb || i >= part.n || tok >= cur.q.kv) return -1;
+                const int b = tok / T;
+                const int64_t id = list[b];
+                if (id >= 0 && id < p.n_blocks) return (int)(id * T + (tok - b * T));
+                if (id != -1) set_status(p.status, AKASHIC_EDEVICE);
+                return -1;
+            };
+            int next = place(0);
+            for (int i = 0; i < part.n; ++i, ++n_tile) {
+                const uint32_t me = n_tile % C::METAS;
+                const int row = next;
+                next = place(i + 1);
+                ok = wide_wait(&mempty[me], ((n_tile / C::METAS) & 1) ^ 1, dead, p.status);
+                if (!ok) break;
+                if (row >= 0) prefetch_l2(p.cache + (int64_t)row * wide, box * wide);
+                if (lane < nb) m_row[me][lane] = row;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&mfull[me]);
+            }
+            left -= part.used;
+            if (left > 0) attend_next(p, NR, TOK, C::EXTRA, 1, ALL, cur);
+        }
     } else if (warp == C::SOFT + 1) {
         // ---------------- issuing
         const uint32_t id_s = idesc_f16(NR, lp.bf16);
         const uint32_t id_o = idesc_f16(NR, lp.bf16) | IDESC_A_MN_MAJOR | IDESC_B_MN_MAJOR;
-        const uint32_t go = lane == 0;
-        const uint32_t q_at = desc_k(smem_u32(s_q)), kk_at = desc_k(smem_u32(s_pair)), r_at = desc_k(smem_u32(s_rope));
-        const uint32_t v_at = desc_mn(smem_u32(s_pair), C::ROPE_BYTES), p_at = desc_mn(smem_u32(s_p), 0);
+        const uint64_t q_at = desc64(desc_k(smem_u32(s_q))), kk_at = desc64(desc_k(smem_u32(s_pair)));
+        const uint64_t r_at = desc64(desc_k(smem_u32(s_rope))), v_at = desc64(desc_mn(smem_u32(s_pair), C::ROPE_BYTES));
+        const uint64_t p_at = desc64(desc_mn(smem_u32(s_p), 0), C::P_ROW == 128 ? DESC_HI : DESC_HI_64);
         const int rope_steps = lp.P / 16;
         uint32_t n_tile = 0, items = 0;
         bool ok = true;
@@ -238,12 +254,15 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                         const uint32_t x = t * PAIRS + s_pair_next, st = x % ST;
                         if (__all_sync(0xffffffffu, mbar_test_wait(&full[st], (x / ST) & 1))) {
                             tc_fence_after();
-                            const uint32_t ka = kk_at + st * (C::PAIR_BYTES >> 4);
-                            const uint32_t qa = q_at + s_pair_next * (2 * NR * 128 >> 4);
+                            if (elect_one()) {
+                                const uint64_t ka = kk_at + st * (C::PAIR_BYTES >> 4);
+                                const uint64_t qa = q_at + s_pair_next * (2 * NR * 128 >> 4);
 #pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                umma_ss(go, d, ka + (k / 4) * (C::ROPE_BYTES >> 4) + 2 * (k % 4),
-                                        qa + (k / 4) * (NR * 128 >> 4) + 2 * (k % 4), id_s, s_pair_next > 0 || k > 0);
+                                for (int k = 0; k < 8; ++k)
+                                    mma_ss(d, ka + (k / 4) * (C::ROPE_BYTES >> 4) + 2 * (k % 4),
+                                           qa + (k / 4) * (NR * 128 >> 4) + 2 * (k % 4), id_s, s_pair_next > 0 || k > 0);
+                            }
+                            __syncwarp();
                             ++s_pair_next;
                             moved = true;
                         }
@@ -251,11 +270,14 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                         const uint32_t sr = t % C::ROPE_SLOTS;
                         if (__all_sync(0xffffffffu, mbar_test_wait(&rope_full[sr], (t / C::ROPE_SLOTS) & 1))) {
                             tc_fence_after();
-                            for (int k = 0; k < rope_steps; ++k)
-                                umma_ss(go, d, r_at + sr * (C::ROPE_BYTES >> 4) + 2 * k,
-                                        q_at + ((C::CHUNKS - 1) * NR * 128 >> 4) + 2 * k, id_s, 1);
-                            umma_commit_if(go, &sfull[t & 1]);
-                            if (!C::ALIAS) umma_commit_if(go, &rope_empty[sr]);
+                            if (elect_one()) {
+                                for (int k = 0; k < rope_steps; ++k)
+                                    mma_ss(d, r_at + sr * (C::ROPE_BYTES >> 4) + 2 * k,
+                                           q_at + ((C::CHUNKS - 1) * NR * 128 >> 4) + 2 * k, id_s, true);
+                                umma_commit(&sfull[t & 1]);
+                                if (!C::ALIAS) umma_commit(&rope_empty[sr]);
+                            }
+                            __syncwarp();
                             ++s_next, s_pair_next = 0;
                             moved = true;
                         }
@@ -264,18 +286,22 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 const uint32_t t = n_tile + v_next;
                 if (v_next < s_next && __all_sync(0xffffffffu, mbar_test_wait(&pfull, t & 1))) {
                     tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll 1
+                        for (int m = 0; m < PAIRS; ++m) {      // (short code: the first pass through it is a cold one)
+                            const uint32_t st = (t * PAIRS + m) % ST;
+                            const uint64_t va = v_at + st * (C::PAIR_BYTES >> 4);
 #pragma unroll
-                    for (int m = 0; m < PAIRS; ++m) {
-                        const uint32_t st = (t * PAIRS + m) % ST, va = v_at + st * (C::PAIR_BYTES >> 4);
-#pragma unroll
-                        for (int k = 0; k < TOK / 16; ++k)
-                            umma_ss_b<C::P_ROW == 128 ? DESC_HI : DESC_HI_64>(
-                                go, tmem + m * NR, va + (2048 * k >> 4), p_at + (16 * C::P_ROW * k >> 4), id_o,
-                                v_next > 0 || k > 0);
-                        umma_commit_if(go, &empty[st]);
+                            for (int k = 0; k < TOK / 16; ++k)
+                                mma_ss(tmem + m * NR, va + (2048 * k >> 4), p_at + (16 * C::P_ROW * k >> 4), id_o,
+                                       v_next > 0 || k > 0);
+                            umma_commit(&empty[st]);
+                        }
+                        umma_commit(&odone);
+                        umma_commit(&mempty[t % C::METAS]);
+                        if (C::ALIAS) umma_commit(&rope_empty[0]);
                     }
-                    umma_commit_if(go, &odone);
-                    if (C::ALIAS) umma_commit_if(go, &rope_empty[0]);
+                    __syncwarp();
                     ++v_next;
                     moved = true;
                 }
@@ -292,7 +318,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
             left -= part.used;
             if (left > 0) attend_next(p, NR, TOK, C::EXTRA, 1, ALL, cur);
         }
-        umma_commit_if(go, &drained);          // what was issued ends before the tensor memory goes
+        if (elect_one()) umma_commit(&drained);                // what was issued ends before the tensor memory goes
         mbar_wait(&drained, 0, p.status);
         __syncwarp();
     } else {
@@ -313,25 +339,27 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
             const AttendSeq sq = cur.q;
             const int row_first = cur.tile * NR, rows = min(NR, sq.nq * p.group - row_first);
             // ---- query rows, 16 bytes at a time
-            constexpr int G = R / 8;
+            constexpr int G = R / 8, AT_ONCE = NR * (G + 8) / THR < 9 ? NR * (G + 8) / THR : 9;
             const int g_all = G + lp.P / 8;
-            for (int x = tid; x < NR * g_all; x += THR) {
-                const int r = x / g_all, g = x - r * g_all;
-                uint4 z = make_uint4(0, 0, 0, 0);
-                if (r < rows) {
-                    const uint32_t at = row_first + r, i = at / (uint32_t)p.group;
-                    const uint16_t *src = (const uint16_t *)p.q + (int64_t)(sq.row0 + (int)i) * p.q_row +
-                                          (int64_t)(at - i * p.group) * p.q_head + g * 8;
-                    if (p.q_wide) {
-                        z = *(const uint4 *)src;
-                    } else {
-                        alignas(16) uint16_t h[8];
+#pragma unroll 1
+            for (int x0 = tid; x0 < NR * g_all; x0 += THR * AT_ONCE) {
+                uint4 z[AT_ONCE];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) h[k] = src[k];
-                        z = *(const uint4 *)h;
+                for (int y = 0; y < AT_ONCE; ++y) {
+                    const int x = x0 + y * THR, r = lp.P == 64 ? x / (G + 8) : x / (G + 4), g = x - r * g_all;
+                    z[y] = make_uint4(0, 0, 0, 0);
+                    if (r < rows) {
+                        const uint32_t at = row_first + r, i = at / (uint32_t)p.group;
+                        const uint16_t *src = (const uint16_t *)p.q + (int64_t)(sq.row0 + (int)i) * p.q_row +
+                                              (int64_t)(at - i * p.group) * p.q_head + g * 8;
+                        z[y] = load_row8(src, p.q_wide);
                     }
                 }
-                *(uint4 *)(s_q + (g >> 3) * (NR * 128) + r * 128 + (((g & 7) ^ (r & 7)) << 4)) = z;
+#pragma unroll
+                for (int y = 0; y < AT_ONCE; ++y) {
+                    const int x = x0 + y * THR, r = lp.P == 64 ? x / (G + 8) : x / (G + 4), g = x - r * g_all;
+                    if (r < NR) *(uint4 *)(s_q + (g >> 3) * (NR * 128) + r * 128 + (((g & 7) ^ (r & 7)) << 4)) = z[y];
+                }
             }
             named_bar(1, THR);                 // (the item before has been written)
             if (tid < NR) {
@@ -470,25 +498,26 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 if (!whole) part[NR * R + tid] = c_ref[tid], part[NR * R + NR + tid] = tot;
                 else if (tid < rows && p.lse) p.lse[dst + tid] = lse_of(c_ref[tid], tot);
                 if (!whole && tid == 0 && mine.from == 0)
-                    p.joins[blockIdx.x] =
-                        make_int4(cur.seq, 0, cur.tile, (int)((first + done - cur.unit + cur.units - 1) / per));
+                    ((LatentJoin *)p.joins)[blockIdx.x] = {dst, rows, (int)((first + done - cur.unit + cur.units - 1) / per)};
             }
             named_bar(1, THR);
+            float inv[CW];
+#pragma unroll
+            for (int c = 0; c < CW; c += 4) *(float4 *)&inv[c] = *(const float4 *)&c_fac[c0 + c];
 #pragma unroll 1
             for (int m = 0; m < PAIRS; ++m) {
                 uint32_t o[CW];
                 tmem_ldn<CW>(tmem + lanes + m * NR + c0, o);
                 tmem_ld_wait();
-                const int d = m * 128 + key;
+                if (!whole) {
+                    float *to = part + c0 * R + m * 128 + key;
 #pragma unroll
-                for (int c = 0; c < CW; ++c) {
-                    const float y = __uint_as_float(o[c]) * c_fac[c0 + c];
-                    if (!whole) part[(c0 + c) * R + d] = y;
-                    else if (c0 + c < rows) {
-                        const int64_t at = (dst + c0 + c) * R + d;
-                        if (lp.bf16) ((__nv_bfloat16 *)p.out)[at] = __float2bfloat16_rn(y);
-                        else ((__half *)p.out)[at] = __float2half_rn(y);
-                    }
+                    for (int c = 0; c < CW; ++c) to[c * R] = __uint_as_float(o[c]) * inv[c];
+                } else {
+                    uint16_t *to = (uint16_t *)p.out + (dst + c0) * R + m * 128 + key;
+#pragma unroll
+                    for (int c = 0; c < CW; ++c)
+                        if (c0 + c < rows) to[c * R] = round16(__uint_as_float(o[c]) * inv[c], lp.bf16);
                 }
             }
             tc_fence_before();
@@ -564,7 +593,7 @@ cudaError_t launch_latent_absorbed(LatentParams &p, void *scratch, cudaStream_t 
         : p.R == 256 ? run_absorbed_rows<256>(p, map, box, n_rows, rows, ctas, st)
                      : run_absorbed_rows<512>(p, map, box, n_rows, rows, ctas, st);
     if (e != cudaSuccess) return e;
-    return launch_attend_join(p.a, p.bf16 ? AKASHIC_DTYPE_BF16 : AKASHIC_DTYPE_FP16, p.R, ctas, rows, st);
+    return launch_latent_join(p, p.R, ctas, rows, 1, st);
 }
 
 }  // namespace ak

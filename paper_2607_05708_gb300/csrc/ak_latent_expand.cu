@@ -157,8 +157,8 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
         __syncwarp();
     } else if (warp == 5) {
         // ---------------- issuing
-        const uint32_t go = lane == 0, idesc = idesc_f16(rows_w, lp.bf16);
-        const uint32_t a_at = desc_k(smem_u32(s_a)), w_at = desc_k(smem_u32(s_w));
+        const uint32_t idesc = idesc_f16(rows_w, lp.bf16);
+        const uint64_t a_at = desc64(desc_k(smem_u32(s_a))), w_at = desc64(desc_k(smem_u32(s_w)));
         uint32_t n_tile = 0, n_w = 0;
         bool ok = true, fresh = true;
         for (int64_t i = 0; i < left && ok; ++i) {
@@ -170,18 +170,24 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
                 ok = wide_wait(&wfull[st], (n_w / ST) & 1, dead, p.status);
                 if (!ok) break;
                 tc_fence_after();
+                if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    umma_ss(go, tmem + acc * 256, a_at + c * (C::A_CHUNK >> 4) + 2 * k,
-                            w_at + st * (C::W_BYTES >> 4) + 2 * k, idesc, c > 0 || k > 0);
-                umma_commit_if(go, &wempty[st]);
+                    for (int k = 0; k < 4; ++k)
+                        mma_ss(tmem + acc * 256, a_at + c * (C::A_CHUNK >> 4) + 2 * k,
+                               w_at + st * (C::W_BYTES >> 4) + 2 * k, idesc, c > 0 || k > 0);
+                    umma_commit(&wempty[st]);
+                }
+                __syncwarp();
             }
             if (!ok) break;
-            umma_commit_if(go, &tfull[acc]);
             fresh = next(cur);
-            if (fresh) umma_commit_if(go, &aempty);
+            if (elect_one()) {
+                umma_commit(&tfull[acc]);
+                if (fresh) umma_commit(&aempty);
+            }
+            __syncwarp();
         }
-        umma_commit_if(go, &drained);
+        if (elect_one()) umma_commit(&drained);
         mbar_wait(&drained, 0, p.status);
         __syncwarp();
     } else {

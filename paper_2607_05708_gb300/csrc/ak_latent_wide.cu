@@ -92,21 +92,17 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
         mbar_init(&drained, 1);
         mbar_fence_init();
         dead_word = 0;
-        p.joins[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        ((LatentJoin *)p.joins)[blockIdx.x] = {0, 0, 0};
     }
     if (warp == 0) {
         tmem_alloc(&tmem_slot, 512);
         tmem_relinquish();
     }
-    int64_t *prefix = (int64_t *)s_q;      // until the warps have found their items
     constexpr int ALL = 0x7fffffff;
-    attend_sums(p, ROWS, TOK, C::EXTRA, 1, ALL, prefix);
-    const int64_t total = prefix[C::THREADS];
-    const int64_t per = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x);
-    const int64_t first = per * blockIdx.x;
-    int left = (int)max((int64_t)0, min(per, total - first));
-    AttendCursor cur = {};
-    if (left > 0) cur = attend_find(p, ROWS, TOK, C::EXTRA, 1, ALL, prefix, first);
+    const LatentShare share = latent_share(p, ROWS, TOK, C::EXTRA, (int64_t *)s_q);    // (until it holds query rows)
+    const int64_t first = share.first, per = share.per;
+    int left = share.left;
+    AttendCursor cur = share.cur;
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -188,8 +184,8 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
     } else if (warp == C::SOFT + 1) {
         // ---------------- issuing
         const uint32_t id_s = idesc_f16(TOK, lp.bf16), id_o = idesc_f16(DV, lp.bf16) | IDESC_B_MN_MAJOR;
-        const uint32_t go = lane == 0;
-        const uint32_t q_at = desc_k(smem_u32(s_q)), k_at = desc_k(smem_u32(s_k)), v_at = desc_mn(smem_u32(s_v), C::CHUNK);
+        const uint64_t q_at = desc64(desc_k(smem_u32(s_q))), k_at = desc64(desc_k(smem_u32(s_k)));
+        const uint64_t v_at = desc64(desc_mn(smem_u32(s_v), C::CHUNK));
         const int rope_steps = lp.P / 16;
         uint32_t n_tile = 0, q_phase = 0, tiles0 = 0, tiles1 = 0;      // tiles: of the row tile, so far
         bool ok = true;
@@ -199,19 +195,22 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             if (ok && t == 0) ok = wide_wait(&kfull[st], (x / KS) & 1, dead, p.status);
             if (!ok) return;
             tc_fence_after();
-            const uint32_t d = tmem + C::S_COL + t * TOK;
-            const uint32_t qa = q_at + t * (C::K_BYTES >> 4), ka = k_at + st * (C::K_BYTES >> 4);
+            if (elect_one()) {
+                const uint32_t d = tmem + C::S_COL + t * TOK;
+                const uint64_t qa = q_at + t * (C::K_BYTES >> 4), ka = k_at + st * (C::K_BYTES >> 4);
 #pragma unroll
-            for (int k = 0; k < DN / 16; ++k) {
-                const uint32_t o = k / 4 * (C::CHUNK >> 4) + 2 * (k % 4);
-                umma_ss(go, d, qa + o, ka + o, id_s, k > 0);
+                for (int k = 0; k < DN / 16; ++k) {
+                    const uint32_t o = k / 4 * (C::CHUNK >> 4) + 2 * (k % 4);
+                    mma_ss(d, qa + o, ka + o, id_s, k > 0);
+                }
+                for (int k = 0; k < rope_steps; ++k) {
+                    const uint32_t o = (C::KC - 1) * (C::CHUNK >> 4) + 2 * k;
+                    mma_ss(d, qa + o, ka + o, id_s, true);
+                }
+                umma_commit(&sfull[t]);
+                if (t == mt - 1) umma_commit(&kempty[st]);
             }
-            for (int k = 0; k < rope_steps; ++k) {
-                const uint32_t o = (C::KC - 1) * (C::CHUNK >> 4) + 2 * k;
-                umma_ss(go, d, qa + o, ka + o, id_s, 1);
-            }
-            umma_commit_if(go, &sfull[t]);
-            if (t == mt - 1) umma_commit_if(go, &kempty[st]);
+            __syncwarp();
         };
         auto values = [&](int t, int i, int b, int mt) {
             const uint32_t x = n_tile + i, sv = x % VS, c = (t ? tiles1 : tiles0) + i;
@@ -219,13 +218,16 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             if (ok) ok = wide_wait(&pfull[t][b], c & 1, dead, p.status);
             if (!ok) return;
             tc_fence_after();
-            const uint32_t va = v_at + sv * (C::V_BYTES >> 4) + b * (HT * 128 >> 4);
+            if (elect_one()) {
+                const uint64_t va = v_at + sv * (C::V_BYTES >> 4) + b * (HT * 128 >> 4);
 #pragma unroll
-            for (int k = 0; k < HT / 16; ++k)
-                umma_ts(go, tmem + t * DV, tmem + C::S_COL + t * TOK + b * HT + k * 8, va + (2048 * k >> 4), id_o,
-                        i > 0 || b > 0 || k > 0);
-            umma_commit_if(go, &odone[t][b]);
-            if (t == mt - 1 && b == 1) umma_commit_if(go, &vempty[sv]);
+                for (int k = 0; k < HT / 16; ++k)
+                    mma_ts(tmem + t * DV, tmem + C::S_COL + t * TOK + b * HT + k * 8, va + (2048 * k >> 4), id_o,
+                           i > 0 || b > 0 || k > 0);
+                umma_commit(&odone[t][b]);
+                if (t == mt - 1 && b == 1) umma_commit(&vempty[sv]);
+            }
+            __syncwarp();
         };
         while (left > 0 && ok) {
             const AttendPart part = attend_part(cur, left);
@@ -250,7 +252,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             left -= part.used;
             if (left > 0) attend_next(p, ROWS, TOK, C::EXTRA, 1, ALL, cur);
         }
-        umma_commit_if(go, &drained);          // what was issued ends before the tensor memory goes
+        if (elect_one()) umma_commit(&drained);                // what was issued ends before the tensor memory goes
         mbar_wait(&drained, 0, p.status);
         __syncwarp();
     } else {
@@ -272,23 +274,25 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             if (t == 0 || rows > 128) {
                 // ---- the warp's 32 query rows, 16 bytes a lane
                 const int g_all = (DN + lp.P) / 8, head = sp.head0 + cur.head;
-#pragma unroll 4
-                for (int x = lane; x < 32 * g_all; x += 32) {
-                    const int y = x / g_all, g = x - y * g_all, row = (warp & 3) * 32 + y;
-                    uint4 z = make_uint4(0, 0, 0, 0);
-                    if (t * 128 + row < rows) {
-                        const uint16_t *src = (const uint16_t *)p.q + (int64_t)(sq.row0 + row_first + t * 128 + row) * p.q_row +
-                                              head * p.q_head + g * 8;
-                        if (p.q_wide) {
-                            z = *(const uint4 *)src;
-                        } else {
-                            alignas(16) uint16_t h[8];
+#pragma unroll 1
+                for (int x0 = lane; x0 < 32 * g_all; x0 += 32 * 8) {
+                    uint4 z[8];
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) h[k] = src[k];
-                            z = *(const uint4 *)h;
-                        }
+                    for (int k = 0; k < 8; ++k) {
+                        const int x = x0 + 32 * k, y = lp.P == 64 ? x / (DN / 8 + 8) : x / (DN / 8 + 4), g = x - y * g_all;
+                        const int row = t * 128 + (warp & 3) * 32 + y;
+                        z[k] = make_uint4(0, 0, 0, 0);
+                        if (y < 32 && row < rows)
+                            z[k] = load_row8((const uint16_t *)p.q + (int64_t)(sq.row0 + row_first + row) * p.q_row +
+                                             head * p.q_head + g * 8, p.q_wide);
                     }
-                    *(uint4 *)(s_q + t * C::K_BYTES + (g >> 3) * C::CHUNK + row * 128 + (((g & 7) ^ (row & 7)) << 4)) = z;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int x = x0 + 32 * k, y = lp.P == 64 ? x / (DN / 8 + 8) : x / (DN / 8 + 4), g = x - y * g_all;
+                        const int row = (warp & 3) * 32 + y;
+                        if (y < 32)
+                            *(uint4 *)(s_q + t * C::K_BYTES + (g >> 3) * C::CHUNK + row * 128 + (((g & 7) ^ (row & 7)) << 4)) = z[k];
+                    }
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -422,8 +426,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 if (!whole) {
                     part[ROWS * DV + r] = mm, part[ROWS * DV + ROWS + r] = l;
                     if (r == 0 && mine.from == 0)
-                        p.joins[blockIdx.x] =
-                            make_int4(cur.seq, head, cur.tile, (int)((first + done - cur.unit + cur.units - 1) / per));
+                        ((LatentJoin *)p.joins)[blockIdx.x] = {dst, rows, (int)((first + done - cur.unit + cur.units - 1) / per)};
                 }
                 tc_fence_before();
             }
@@ -514,8 +517,7 @@ cudaError_t launch_latent_expanded(LatentParams &p, void *scratch, cudaStream_t 
         if (e == cudaSuccess)
             e = p.nope == 64 ? p.value == 64 ? run_wide<64, 64>(p, sp, x.ctas, st) : run_wide<64, 128>(p, sp, x.ctas, st)
                 : p.value == 64 ? run_wide<128, 64>(p, sp, x.ctas, st) : run_wide<128, 128>(p, sp, x.ctas, st);
-        if (e == cudaSuccess)
-            e = launch_attend_join(a, p.bf16 ? AKASHIC_DTYPE_BF16 : AKASHIC_DTYPE_FP16, p.value, x.ctas, WIDE_ROWS, st);
+        if (e == cudaSuccess) e = launch_latent_join(p, p.value, x.ctas, WIDE_ROWS, a.q_heads, st);
     }
     return e;
 }

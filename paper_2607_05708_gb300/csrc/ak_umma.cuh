@@ -53,6 +53,10 @@ __device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t (&r)[4])
 __device__ __forceinline__ void tmem_st_wait() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
+// Starts contiguous global memory's way into L2 (address and size multiples of 16).
+__device__ __forceinline__ void prefetch_l2(const void *at, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at), "r"(bytes) : "memory");
+}
 // D[tmem] (+)= A[smem] B[smem]^T and D[tmem] (+)= A[tmem] B[smem], fp16, by the lane that
 // has `go`.  The whole warp comes here, so that addresses stay in uniform registers
 // (behind a branch on the lane an issue took 120 cycles and more; the product takes 64),
@@ -68,22 +72,6 @@ __device__ __forceinline__ void umma_ss(uint32_t go, uint32_t d, uint32_t a, uin
         "mov.b64 y, {%3, %6};\n\t"
         "@q tcgen05.mma.cta_group::1.kind::f16 [%1], x, y, %4, p;\n\t}" ::"r"(go),
         "r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(DESC_HI)
-        : "memory");
-}
-// The same with B in the 64-byte swizzle: atoms of 8 K-rows x 32 values along N, 512 bytes, one after
-// the other along K (MN-major).
-constexpr uint32_t DESC_HI_64 = (512u >> 4) | (1u << 14) | (4u << 29);
-template <uint32_t B_HI>
-__device__ __forceinline__ void umma_ss_b(uint32_t go, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
-                                          uint32_t acc) {
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t.reg .b64 x, y;\n\t"
-        "setp.ne.b32 p, %5, 0;\n\t"
-        "setp.ne.b32 q, %0, 0;\n\t"
-        "mov.b64 x, {%2, %6};\n\t"
-        "mov.b64 y, {%3, %7};\n\t"
-        "@q tcgen05.mma.cta_group::1.kind::f16 [%1], x, y, %4, p;\n\t}" ::"r"(go),
-        "r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(DESC_HI), "r"(B_HI)
         : "memory");
 }
 __device__ __forceinline__ void umma_ts(uint32_t go, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
@@ -105,6 +93,28 @@ __device__ __forceinline__ void umma_commit_if(uint32_t go, uint64_t *bar) {
         "r"(smem_u32(bar))
         : "memory");
 }
+// One thread's products behind elect.sync, of which the compiler knows that one thread comes through: an
+// issue then costs what the product does (M = 128, 16 of K, cycles: N = 16 40, 32 41, 64 49, 128 65, 256 129, A in
+// tensor memory 11, 18, 33, 65, 129; by predicate, as above, none under 70).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t x;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(x));
+    return x != 0;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+    umma_bf16(d, a, b, idesc, acc);
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+        : "memory");
+}
+// High words of descriptors: 128-byte swizzle (DESC_HI), and 64-byte swizzle: atoms of 8 K-rows x 32 values along N, 512
+// bytes, one after the other along K (MN-major).
+constexpr uint32_t DESC_HI_64 = (512u >> 4) | (1u << 14) | (4u << 29);
+__device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi = DESC_HI) { return (uint64_t)hi << 32 | lo; }
 // Low words of the descriptors of K-major and MN-major tiles.
 __device__ __forceinline__ uint32_t desc_k(uint32_t saddr) { return ((saddr & 0x3ffffu) >> 4) | 1u << 16; }
 __device__ __forceinline__ uint32_t desc_mn(uint32_t saddr, uint32_t lbo) {

@@ -123,10 +123,11 @@ struct LatentSpace {
 };
 
 // Scratch of the joins, the tokens of a box of the copies from the cache (boxes do not cross blocks), and
-// the cache's tensor map: boxes of 64 values.
+// the cache's tensor map: boxes of 64 values of at most
+// `most` tokens.
 int64_t latent_joins_bytes(int ctas);
-int latent_box(const LatentParams &p);
-cudaError_t latent_rows_map(const LatentParams &p, CUtensorMap *map);
+int latent_box(const LatentParams &p, int most);
+cudaError_t latent_rows_map(const LatentParams &p, int most, CUtensorMap *map);
 
 cudaError_t launch_latent_join(const LatentParams &p, int dim, int ctas, int rows, int step, cudaStream_t st);
 

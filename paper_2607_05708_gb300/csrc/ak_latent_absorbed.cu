@@ -26,34 +26,32 @@ namespace ak {
 
 namespace {
 
+#ifndef TOK_OF
+#define TOK_OF(R, NR) ((R) == 512 ? 64 : 128)
+#endif
 template <int R, int NR>
 struct Absorbed {
-    static constexpr int TOK = 128;                      // tokens of a tile
+    static constexpr int TOK = TOK_OF(R, NR);            // tokens of a tile
     static constexpr int PAIRS = R / 128, CHUNKS = R / 64 + 1;
     static constexpr int CW = NR < 32 ? NR : 32;         // rows of a softmax thread
     static constexpr int SOFT = NR / CW * 4;             // softmax warps
-    static constexpr int THREADS = 32 * (SOFT + 3);
+    static constexpr int THREADS = 32 * (SOFT + 4);
     static constexpr int PAIR_BYTES = TOK * 256, ROPE_BYTES = TOK * 128;
     static constexpr int Q_BYTES = CHUNKS * NR * 128;
     // P^T: a row a token; 64 bytes of it, in the 64-byte swizzle, hold 32 rows' weights
     static constexpr int P_ROW = NR > 32 ? 128 : 64, P_BYTES = TOK * P_ROW;
-    // Where R = 512 and 64 rows leave no room, the rotated keys lie where P^T will: they are
-    // read before it is written.
-    static constexpr bool ALIAS = R == 512 && NR == 64;
     static constexpr int ROOM = 232448 - 1024 - 5120 - Q_BYTES - P_BYTES;
     static constexpr int fit(int ropes) { return (ROOM - ropes * ROPE_BYTES) / PAIR_BYTES; }
-    static constexpr int ROPES = ALIAS ? 0 : fit(2) > PAIRS ? 2 : 1;
-    static constexpr int STAGES = fit(ROPES) < 6 ? fit(ROPES) : 6;
-    static_assert(STAGES >= PAIRS, "a tile");
-    static_assert(!ALIAS || P_BYTES == ROPE_BYTES, "the same place");
-    static constexpr int ROPE_SLOTS = ALIAS ? 1 : ROPES;
+    static constexpr int ROPES = fit(2) >= 2 * PAIRS ? 2 : 1;
+    static constexpr int STAGES = fit(ROPES) < 3 * PAIRS ? fit(ROPES) : 3 * PAIRS;
+    static_assert(STAGES > PAIRS, "a tile, and the next on its way");
     static constexpr int SMEM = 1024 + Q_BYTES + P_BYTES + ROPES * ROPE_BYTES + STAGES * PAIR_BYTES;
     static constexpr int S_COL = 256;                    // tensor memory: O^T, then two S^T
     static_assert(PAIRS * NR <= S_COL && S_COL + 2 * NR <= 512, "tensor memory");
-    static constexpr int METAS = R == 512 ? 3 : R == 256 ? 5 : 8;      // tiles whose places are known
+    static constexpr int METAS = 3 * 512 / R * (128 / TOK) < 8 ? 3 * 512 / R * (128 / TOK) : 8;  // tiles whose places are known
     static_assert(METAS > STAGES / PAIRS, "the tiles on their way");
     // An item's beginning and end (rows in, result out, an empty pipeline) count as steps.
-    static constexpr int EXTRA = 1;
+    static constexpr int EXTRA = 128 / TOK;
 };
 
 // Weights are held between 2^-OFF of the reference's and 2^(OFF + SLACK): fp16 has room for both.
@@ -104,8 +102,8 @@ __device__ __forceinline__ void tmem_stn(uint32_t at, const uint32_t (&r)[N]) {
 
 template <int R, int NR>
 __global__ void __launch_bounds__(Absorbed<R, NR>::THREADS, 1)
-k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ LatentParams lp,
-                  const int box, const int n_rows) {
+k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap pair_map,
+                  const __grid_constant__ LatentParams lp, const int box, const int n_rows) {
     using C = Absorbed<R, NR>;
     constexpr int TOK = C::TOK, PAIRS = C::PAIRS, ST = C::STAGES, CW = C::CW, THR = 32 * C::SOFT;
     const AttendParams &p = lp.a;
@@ -113,9 +111,8 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
     unsigned char *smem = (unsigned char *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
     unsigned char *s_pair = smem, *s_rope = s_pair + ST * C::PAIR_BYTES, *s_p = s_rope + C::ROPES * C::ROPE_BYTES;
     unsigned char *s_q = s_p + C::P_BYTES;
-    if (C::ALIAS) s_rope = s_p;
-    __shared__ uint64_t full[ST], empty[ST], rope_full[C::ROPE_SLOTS], rope_empty[C::ROPE_SLOTS];
-    __shared__ uint64_t sfull[2], pfull, odone, qfull, mfull[C::METAS], mempty[C::METAS], drained;
+    __shared__ uint64_t full[ST], empty[ST], rope_full[C::ROPES], rope_empty[C::ROPES];
+    __shared__ uint64_t sfull[2], pfull[2], odone, qfull, mfull[C::METAS], mempty[C::METAS], drained[2];
     __shared__ int m_row[C::METAS][8];                   // first row of each of a tile's boxes, -1: none
     __shared__ alignas(16) float c_ref[NR], c_fac[NR];
     __shared__ alignas(16) int c_limit[NR], c_tag[NR];
@@ -128,10 +125,10 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
     griddep_wait();
     if (tid == 0) {
         for (int i = 0; i < ST; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-        for (int i = 0; i < C::ROPE_SLOTS; ++i) mbar_init(&rope_full[i], 1), mbar_init(&rope_empty[i], 1);
+        for (int i = 0; i < C::ROPES; ++i) mbar_init(&rope_full[i], 1), mbar_init(&rope_empty[i], 1);
         for (int i = 0; i < C::METAS; ++i) mbar_init(&mfull[i], 1), mbar_init(&mempty[i], 1);
-        for (int i = 0; i < 2; ++i) mbar_init(&sfull[i], 1);
-        mbar_init(&pfull, C::SOFT), mbar_init(&odone, 1), mbar_init(&qfull, C::SOFT), mbar_init(&drained, 1);
+        for (int i = 0; i < 2; ++i) mbar_init(&sfull[i], 1), mbar_init(&pfull[i], C::SOFT);
+        mbar_init(&odone, 1), mbar_init(&qfull, C::SOFT), mbar_init(&drained[0], 1), mbar_init(&drained[1], 1);
         mbar_fence_init();
         dead_word = 0;
         ((LatentJoin *)p.joins)[blockIdx.x] = {0, 0, 0};
@@ -161,26 +158,37 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
             for (int i = 0; ok && i < part.n; ++i, ++n_tile) {
                 const uint32_t me = n_tile % C::METAS;
                 ok = wide_wait(&mfull[me], (n_tile / C::METAS) & 1, dead, p.status);
-                const int row = m_row[me][lane % nb], y = row < 0 ? n_rows : row;      // behind the last row: zeros
+                const int *rows = m_row[me];
                 for (int k = 0; ok && k < PAIRS; ++k, ++n_pair) {
                     const uint32_t st = n_pair % ST;
                     ok = wide_wait(&empty[st], ((n_pair / ST) & 1) ^ 1, dead, p.status);
                     if (!ok) break;
-                    if (lane == 0) mbar_expect_tx(&full[st], C::PAIR_BYTES);
-                    __syncwarp();
-                    if (lane < 2 * nb) {
-                        const int c = lane / nb;
-                        tma_load_2d(s_pair + st * C::PAIR_BYTES + c * C::ROPE_BYTES + lane % nb * box * 128, &rows_map,
-                                    &full[st], (2 * k + c) * 64, y);
+                    if (elect_one()) {
+                        unsigned char *to = s_pair + st * C::PAIR_BYTES;
+                        mbar_expect_tx(&full[st], C::PAIR_BYTES);
+                        // (rows behind the last one: zeros)
+                        if (nb == 1) {
+                            tma_load_3d(to, &pair_map, &full[st], 0, rows[0] < 0 ? n_rows : rows[0], 2 * k);
+                        } else {
+                            for (int b = 0; b < nb; ++b) {
+                                const int y = rows[b] < 0 ? n_rows : rows[b];
+                                tma_load_2d(to + b * box * 128, &rows_map, &full[st], k * 128, y);
+                                tma_load_2d(to + C::ROPE_BYTES + b * box * 128, &rows_map, &full[st], k * 128 + 64, y);
+                            }
+                        }
                     }
+                    __syncwarp();
                 }
-                const uint32_t sr = n_tile % C::ROPE_SLOTS;
-                if (ok) ok = wide_wait(&rope_empty[sr], ((n_tile / C::ROPE_SLOTS) & 1) ^ 1, dead, p.status);
+                const uint32_t sr = n_tile % C::ROPES;
+                if (ok) ok = wide_wait(&rope_empty[sr], ((n_tile / C::ROPES) & 1) ^ 1, dead, p.status);
                 if (!ok) break;
-                if (lane == 0) mbar_expect_tx(&rope_full[sr], C::ROPE_BYTES);
+                if (elect_one()) {
+                    mbar_expect_tx(&rope_full[sr], C::ROPE_BYTES);
+                    for (int b = 0; b < nb; ++b)
+                        tma_load_2d(s_rope + sr * C::ROPE_BYTES + b * box * 128, &rows_map, &rope_full[sr], R,
+                                    rows[b] < 0 ? n_rows : rows[b]);
+                }
                 __syncwarp();
-                if (lane < nb)
-                    tma_load_2d(s_rope + sr * C::ROPE_BYTES + lane * box * 128, &rows_map, &rope_full[sr], R, y);
                 ++n_rope;
             }
             left -= part.used;
@@ -189,8 +197,8 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
         // nothing is on its way when the CTA ends (where a wait gave up; else all has been read)
         for (uint32_t i = 0; !ok && i < ST; ++i)
             if (n_pair > i) mbar_wait(&full[i], ((n_pair - i - 1) / ST) & 1, p.status);
-        for (uint32_t i = 0; !ok && i < C::ROPE_SLOTS; ++i)
-            if (n_rope > i) mbar_wait(&rope_full[i], ((n_rope - i - 1) / C::ROPE_SLOTS) & 1, p.status);
+        for (uint32_t i = 0; !ok && i < C::ROPES; ++i)
+            if (n_rope > i) mbar_wait(&rope_full[i], ((n_rope - i - 1) / C::ROPES) & 1, p.status);
         __syncwarp();
     } else if (warp == C::SOFT + 2) {
         // ---------------- looking ahead: the tiles' places, and their rows, which are contiguous within a
@@ -218,112 +226,112 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
             for (int i = 0; i < part.n; ++i, ++n_tile) {
                 const uint32_t me = n_tile % C::METAS;
                 const int row = next;
-                next = place(i + 1);
                 ok = wide_wait(&mempty[me], ((n_tile / C::METAS) & 1) ^ 1, dead, p.status);
                 if (!ok) break;
-                if (row >= 0) prefetch_l2(p.cache + (int64_t)row * wide, box * wide);
                 if (lane < nb) m_row[me][lane] = row;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&mfull[me]);
+                for (int k = 0; k < nb; ++k) {
+                    const int r = __shfl_sync(0xffffffffu, row, k);
+                    if (r < 0) continue;
+                    const unsigned char *at = p.cache + (int64_t)r * wide;
+#pragma unroll 4
+                    for (int x = lane * 128; x < box * wide; x += 32 * 128) prefetch_l2(at + x);
+                }
+                next = place(i + 1);
             }
             left -= part.used;
             if (left > 0) attend_next(p, NR, TOK, C::EXTRA, 1, ALL, cur);
         }
     } else if (warp == C::SOFT + 1) {
-        // ---------------- issuing
-        const uint32_t id_s = idesc_f16(NR, lp.bf16);
-        const uint32_t id_o = idesc_f16(NR, lp.bf16) | IDESC_A_MN_MAJOR | IDESC_B_MN_MAJOR;
-        const uint64_t q_at = desc64(desc_k(smem_u32(s_q))), kk_at = desc64(desc_k(smem_u32(s_pair)));
-        const uint64_t r_at = desc64(desc_k(smem_u32(s_rope))), v_at = desc64(desc_mn(smem_u32(s_pair), C::ROPE_BYTES));
-        const uint64_t p_at = desc64(desc_mn(smem_u32(s_p), 0), C::P_ROW == 128 ? DESC_HI : DESC_HI_64);
+        // ---------------- issuing S^T = K Q^T, of a tile once the weights of the one before the last are there
+        const uint32_t id_s = idesc_f16(NR, lp.bf16, TOK);
+        const uint64_t q_at = desc64(desc_k(smem_u32(s_q))), k_at = desc64(desc_k(smem_u32(s_pair)));
+        const uint64_t r_at = desc64(desc_k(smem_u32(s_rope)));
         const int rope_steps = lp.P / 16;
-        uint32_t n_tile = 0, items = 0;
+        uint32_t t = 0, items = 0, x = 0;      // tiles and pairs since the kernel began
         bool ok = true;
         while (left > 0 && ok) {
             const AttendPart part = attend_part(cur, left);
-            const uint32_t n = part.n;
             if (part.n <= 0) break;
             ok = wide_wait(&qfull, items++ & 1, dead, p.status);
-            uint32_t s_next = 0, s_pair_next = 0, v_next = 0, polls = 0;
-            while (ok && v_next < n) {
-                bool moved = false;
-                // (one answer for all lanes)
-                if (s_next < n && s_next <= v_next + 1) {
-                    const uint32_t t = n_tile + s_next, d = tmem + C::S_COL + (t & 1) * NR;
-                    if (s_pair_next < PAIRS) {
-                        const uint32_t x = t * PAIRS + s_pair_next, st = x % ST;
-                        if (__all_sync(0xffffffffu, mbar_test_wait(&full[st], (x / ST) & 1))) {
-                            tc_fence_after();
-                            if (elect_one()) {
-                                const uint64_t ka = kk_at + st * (C::PAIR_BYTES >> 4);
-                                const uint64_t qa = q_at + s_pair_next * (2 * NR * 128 >> 4);
-#pragma unroll
-                                for (int k = 0; k < 8; ++k)
-                                    mma_ss(d, ka + (k / 4) * (C::ROPE_BYTES >> 4) + 2 * (k % 4),
-                                           qa + (k / 4) * (NR * 128 >> 4) + 2 * (k % 4), id_s, s_pair_next > 0 || k > 0);
-                            }
-                            __syncwarp();
-                            ++s_pair_next;
-                            moved = true;
-                        }
-                    } else {
-                        const uint32_t sr = t % C::ROPE_SLOTS;
-                        if (__all_sync(0xffffffffu, mbar_test_wait(&rope_full[sr], (t / C::ROPE_SLOTS) & 1))) {
-                            tc_fence_after();
-                            if (elect_one()) {
-                                for (int k = 0; k < rope_steps; ++k)
-                                    mma_ss(d, r_at + sr * (C::ROPE_BYTES >> 4) + 2 * k,
-                                           q_at + ((C::CHUNKS - 1) * NR * 128 >> 4) + 2 * k, id_s, true);
-                                umma_commit(&sfull[t & 1]);
-                                if (!C::ALIAS) umma_commit(&rope_empty[sr]);
-                            }
-                            __syncwarp();
-                            ++s_next, s_pair_next = 0;
-                            moved = true;
-                        }
-                    }
-                }
-                const uint32_t t = n_tile + v_next;
-                if (v_next < s_next && __all_sync(0xffffffffu, mbar_test_wait(&pfull, t & 1))) {
+            for (int i = 0; ok && i < part.n; ++i, ++t) {
+                const uint32_t d = tmem + C::S_COL + (t & 1) * NR, sr = t % C::ROPES;
+                if (t > 1) ok = wide_wait(&pfull[t & 1], (t - 2) >> 1 & 1, dead, p.status);
+                for (int k = 0; ok && k < PAIRS; ++k, ++x) {
+                    const uint32_t st = x % ST;
+                    ok = wide_wait(&full[st], (x / ST) & 1, dead, p.status);
+                    if (!ok) break;
                     tc_fence_after();
                     if (elect_one()) {
-#pragma unroll 1
-                        for (int m = 0; m < PAIRS; ++m) {      // (short code: the first pass through it is a cold one)
-                            const uint32_t st = (t * PAIRS + m) % ST;
-                            const uint64_t va = v_at + st * (C::PAIR_BYTES >> 4);
+                        const uint64_t ka = k_at + st * (C::PAIR_BYTES >> 4), qa = q_at + k * (2 * NR * 128 >> 4);
 #pragma unroll
-                            for (int k = 0; k < TOK / 16; ++k)
-                                mma_ss(tmem + m * NR, va + (2048 * k >> 4), p_at + (16 * C::P_ROW * k >> 4), id_o,
-                                       v_next > 0 || k > 0);
-                            umma_commit(&empty[st]);
-                        }
-                        umma_commit(&odone);
-                        umma_commit(&mempty[t % C::METAS]);
-                        if (C::ALIAS) umma_commit(&rope_empty[0]);
+                        for (int y = 0; y < 8; ++y)
+                            mma_ss(d, ka + (y / 4) * (C::ROPE_BYTES >> 4) + 2 * (y % 4),
+                                   qa + (y / 4) * (NR * 128 >> 4) + 2 * (y % 4), id_s, k > 0 || y > 0);
                     }
                     __syncwarp();
-                    ++v_next;
-                    moved = true;
                 }
-                // a bounded wait, like the others (wide_wait)
-                polls = moved ? 0 : polls + 1;
-                if ((polls & 1023u) == 1023u && __any_sync(0xffffffffu, *dead)) ok = false;
-                if (polls >= SPIN_LIMIT) {
-                    *dead = 1;
-                    set_status(p.status, AKASHIC_ETIMEOUT);
-                    ok = false;
+                if (ok) ok = wide_wait(&rope_full[sr], (t / C::ROPES) & 1, dead, p.status);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    for (int y = 0; y < rope_steps; ++y)
+                        mma_ss(d, r_at + sr * (C::ROPE_BYTES >> 4) + 2 * y, q_at + ((C::CHUNKS - 1) * NR * 128 >> 4) + 2 * y,
+                               id_s, true);
+                    umma_commit(&sfull[t & 1]);
+                    umma_commit(&rope_empty[sr]);
                 }
+                __syncwarp();
             }
-            n_tile += n;
             left -= part.used;
             if (left > 0) attend_next(p, NR, TOK, C::EXTRA, 1, ALL, cur);
         }
-        if (elect_one()) umma_commit(&drained);                // what was issued ends before the tensor memory goes
-        mbar_wait(&drained, 0, p.status);
+        if (elect_one()) umma_commit(&drained[0]);             // what was issued ends before the tensor memory goes
+        mbar_wait(&drained[0], 0, p.status);
+        __syncwarp();
+    } else if (warp == C::SOFT + 3) {
+        // ---------------- issuing O^T += C^T P^T
+        const uint32_t id_o = idesc_f16(NR, lp.bf16) | IDESC_A_MN_MAJOR | IDESC_B_MN_MAJOR;
+        const uint64_t v_at = desc64(desc_mn(smem_u32(s_pair), C::ROPE_BYTES));
+        const uint64_t p_at = desc64(desc_mn(smem_u32(s_p), 0), C::P_ROW == 128 ? DESC_HI : DESC_HI_64);
+        uint32_t t = 0;
+        bool ok = true;
+        while (left > 0 && ok) {
+            const AttendPart part = attend_part(cur, left);
+            if (part.n <= 0) break;
+            for (int i = 0; i < part.n; ++i, ++t) {
+                ok = wide_wait(&pfull[t & 1], t >> 1 & 1, dead, p.status);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll 1
+                    for (int m = 0; m < PAIRS; ++m) {          // (short code: the first pass through it is a cold one)
+                        const uint32_t st = (t * PAIRS + m) % ST;
+                        const uint64_t va = v_at + st * (C::PAIR_BYTES >> 4);
+#pragma unroll
+                        for (int k = 0; k < TOK / 16; ++k)
+                            mma_ss(tmem + m * NR, va + (2048 * k >> 4), p_at + (16 * C::P_ROW * k >> 4), id_o,
+                                   i > 0 || k > 0);
+                        umma_commit(&empty[st]);
+                    }
+                    umma_commit(&odone);
+                    umma_commit(&mempty[t % C::METAS]);
+                }
+                __syncwarp();
+            }
+            left -= part.used;
+            if (left > 0) attend_next(p, NR, TOK, C::EXTRA, 1, ALL, cur);
+        }
+        if (elect_one()) umma_commit(&drained[1]);
+        mbar_wait(&drained[1], 0, p.status);
         __syncwarp();
     } else {
-        // ---------------- softmax: a lane is token 32 (warp % 4) + lane, rows [c0, c0 + CW)
-        const int quad = warp & 3, c0 = warp / 4 * CW, key = quad * 32 + lane;
+        // ---------------- softmax: a lane is token 32 (warp % 4) + lane, rows [c0, c0 + CW).  (Scores of M = 64
+        // lie in the first 16 lanes of every 32.)
+        const int quad = warp & 3, c0 = warp / 4 * CW, dim = quad * 32 + lane;
+        const int key = TOK == 128 ? dim : quad * 16 + (lane & 15);
+        const bool used = TOK == 128 || lane < 16;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const float f = p.scale * LOG2E_F;
         const bool tags = p.tags != nullptr;
@@ -382,10 +390,10 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 const int tok = (mine.from + i) * TOK;
                 ok = ok && wide_wait(&mfull[n_tile % C::METAS], (n_tile / C::METAS) & 1, dead, p.status);
                 const int row = m_row[n_tile % C::METAS][key / box];
-                const bool have = row >= 0;
+                const bool have = row >= 0 && used;
                 int tag = -1;
                 if (tags && have) tag = max(-1, p.tags[(int64_t)row + key % box]);
-                const bool masked = __any_sync(0xffffffffu, !have) || tags || tok > safe;
+                const bool masked = __any_sync(0xffffffffu, used && !have) || tags || tok > safe;
                 ok = ok && wide_wait(&sfull[n_tile & 1], n_tile >> 1 & 1, dead, p.status);
                 tc_fence_after();
                 uint32_t raw[CW];
@@ -410,6 +418,10 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                         x[c + 2] = tag == y.z ? x[c + 2] : -INFINITY;
                         x[c + 3] = tag == y.w ? x[c + 3] : -INFINITY;
                     }
+                }
+                if (TOK == 64) {
+#pragma unroll
+                    for (int c = 0; c < CW; ++c) x[c] = used ? x[c] : -INFINITY;
                 }
                 float most = -INFINITY;
 #pragma unroll
@@ -472,7 +484,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 if (!waited && n_tile > 0)     // P^T has been read
                     ok = ok && wide_wait(&odone, (n_tile - 1) & 1, dead, p.status);
 #pragma unroll
-                for (int c = 0; c < CW / 2; c += 4) {
+                for (int c = 0; used && c < CW / 2; c += 4) {
                     const int ch = c0 / 8 + c / 4;       // 16 bytes of the token's weights
                     const int sw = C::P_ROW == 128 ? ch ^ (key & 7) : ch ^ (key >> 1 & 3);
                     *(uint4 *)(s_p + key * C::P_ROW + (sw << 4)) = make_uint4(w[c], w[c + 1], w[c + 2], w[c + 3]);
@@ -480,9 +492,10 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 fence_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&pfull);
+                if (lane == 0) mbar_arrive(&pfull[n_tile & 1]);
             }
             // ---- totals
+            if (left == mine.used) griddep_launch();
             const float sum = over_lanes<CW>(l, [](float a, float b) { return a + b; });
             if (lane < CW) c_part[quad][c0 + lane] = sum;
             ok = ok && wide_wait(&odone, (n_tile - 1) & 1, dead, p.status);
@@ -510,11 +523,11 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 tmem_ldn<CW>(tmem + lanes + m * NR + c0, o);
                 tmem_ld_wait();
                 if (!whole) {
-                    float *to = part + c0 * R + m * 128 + key;
+                    float *to = part + c0 * R + m * 128 + dim;
 #pragma unroll
                     for (int c = 0; c < CW; ++c) to[c * R] = __uint_as_float(o[c]) * inv[c];
                 } else {
-                    uint16_t *to = (uint16_t *)p.out + (dst + c0) * R + m * 128 + key;
+                    uint16_t *to = (uint16_t *)p.out + (dst + c0) * R + m * 128 + dim;
 #pragma unroll
                     for (int c = 0; c < CW; ++c)
                         if (c0 + c < rows) to[c * R] = round16(__uint_as_float(o[c]) * inv[c], lp.bf16);
@@ -532,7 +545,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
 }
 
 template <int R, int NR>
-cudaError_t run_absorbed(const LatentParams &p, const CUtensorMap &map, int box, int n_rows, int ctas, cudaStream_t st) {
+cudaError_t run_absorbed(const LatentParams &p, const CUtensorMap &map, const CUtensorMap &pairs, int box, int n_rows, int ctas, cudaStream_t st) {
     using C = Absorbed<R, NR>;
     auto *kernel = k_latent_absorbed<R, NR>;
     // once a device (the attribute stays; another thread that comes first does the same)
@@ -545,14 +558,14 @@ cudaError_t run_absorbed(const LatentParams &p, const CUtensorMap &map, int box,
         if (e != cudaSuccess) return e;
         if (dev < 64) ready[dev].store(true, std::memory_order_release);
     }
-    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, map, p, box, n_rows);
+    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, map, pairs, p, box, n_rows);
 }
 template <int R>
-cudaError_t run_absorbed_rows(const LatentParams &p, const CUtensorMap &map, int box, int n_rows, int rows, int ctas,
+cudaError_t run_absorbed_rows(const LatentParams &p, const CUtensorMap &map, const CUtensorMap &pairs, int box, int n_rows, int rows, int ctas,
                               cudaStream_t st) {
-    return rows == 16   ? run_absorbed<R, 16>(p, map, box, n_rows, ctas, st)
-           : rows == 32 ? run_absorbed<R, 32>(p, map, box, n_rows, ctas, st)
-                        : run_absorbed<R, 64>(p, map, box, n_rows, ctas, st);
+    return rows == 16   ? run_absorbed<R, 16>(p, map, pairs, box, n_rows, ctas, st)
+           : rows == 32 ? run_absorbed<R, 32>(p, map, pairs, box, n_rows, ctas, st)
+                        : run_absorbed<R, 64>(p, map, pairs, box, n_rows, ctas, st);
 }
 
 // Rows of a tile, from the sequences' rows on average: a tile costs about the same whatever its
@@ -571,27 +584,31 @@ int64_t latent_absorbed_scratch(const LatentParams &p) {
     return latent_joins_bytes(ctas) + (int64_t)ctas * 2 * attend_slot_floats(tile_rows(p), p.R) * 4;
 }
 
-int latent_box(const LatentParams &p) {
+int latent_box(const LatentParams &p, int most) {
     const int T = p.a.per_block * KV_UNIT;
-    return (T & -T) < 128 ? (T & -T) : 128;
+    return (T & -T) < most ? (T & -T) : most;
 }
-cudaError_t latent_rows_map(const LatentParams &p, CUtensorMap *map) {
+cudaError_t latent_rows_map(const LatentParams &p, int most, CUtensorMap *map) {
     const uint64_t rows = (uint64_t)p.a.n_blocks * p.a.per_block * KV_UNIT, wide = p.R + p.P;
     return make_tmap_2d(map, p.a.cache, p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-                        wide, rows, wide * 2, 64, (uint32_t)latent_box(p));
+                        wide, rows, wide * 2, 64, (uint32_t)latent_box(p, most));
 }
 
 cudaError_t launch_latent_absorbed(LatentParams &p, void *scratch, cudaStream_t st) {
-    const int ctas = device_sm_count(), rows = tile_rows(p), box = latent_box(p);
+    const int ctas = device_sm_count(), rows = tile_rows(p);
+    const int tok = p.R == 512 ? 64 : 128, box = latent_box(p, tok);
     const int n_rows = (int)(p.a.n_blocks * p.a.per_block * KV_UNIT);
     p.a.joins = (int4 *)scratch;
     p.a.partial = (float *)((unsigned char *)scratch + latent_joins_bytes(ctas));
-    CUtensorMap map;
-    cudaError_t e = latent_rows_map(p, &map);
+    CUtensorMap map, pairs;
+    cudaError_t e = latent_rows_map(p, tok, &map);
+    if (e == cudaSuccess)
+        e = make_tmap_cols(&pairs, p.a.cache, p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                           p.R, n_rows, (p.R + p.P) * 2, box, 2);
     if (e != cudaSuccess) return e;
-    e = p.R == 128   ? run_absorbed_rows<128>(p, map, box, n_rows, rows, ctas, st)
-        : p.R == 256 ? run_absorbed_rows<256>(p, map, box, n_rows, rows, ctas, st)
-                     : run_absorbed_rows<512>(p, map, box, n_rows, rows, ctas, st);
+    e = p.R == 128   ? run_absorbed_rows<128>(p, map, pairs, box, n_rows, rows, ctas, st)
+        : p.R == 256 ? run_absorbed_rows<256>(p, map, pairs, box, n_rows, rows, ctas, st)
+                     : run_absorbed_rows<512>(p, map, pairs, box, n_rows, rows, ctas, st);
     if (e != cudaSuccess) return e;
     return launch_latent_join(p, p.R, ctas, rows, 1, st);
 }

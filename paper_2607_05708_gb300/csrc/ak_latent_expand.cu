@@ -253,13 +253,13 @@ cudaError_t run_expand(const LatentParams &p, const LatentSpace &sp, cudaStream_
     }
     const CUtensorMapDataType type = p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     CUtensorMap rows, k, v;
-    e = latent_rows_map(p, &rows);
+    e = latent_rows_map(p, 128, &rows);
     if (e == cudaSuccess)
         e = make_tmap_2d(&k, p.w_k, type, 2, R, (uint64_t)sp.k_step * (p.a.q_heads - 1) + p.nope, p.k_row * 2, 64, p.nope);
     if (e == cudaSuccess)
         e = make_tmap_2d(&v, p.w_v, type, 2, R, (uint64_t)sp.v_step * (p.a.q_heads - 1) + p.value, p.v_row * 2, 64, p.value);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kernel, dim3(device_sm_count()), dim3(C::THREADS), C::SMEM, st, rows, k, v, p, sp, latent_box(p),
+    return launch_pdl(kernel, dim3(device_sm_count()), dim3(C::THREADS), C::SMEM, st, rows, k, v, p, sp, latent_box(p, 128),
                       (int)(p.a.n_blocks * p.a.per_block * KV_UNIT));
 }
 

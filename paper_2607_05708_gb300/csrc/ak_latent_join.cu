@@ -2,8 +2,8 @@
 // added in the order of the CTAs.
 //
 // Items of few parts: a warp a row.  Of many (a long sequence is one item in the shares of all CTAs): a
-// CTA a row, its parts in groups of threads that each add every so-manieth part up; 152 parts one
-// after the other took 80 us.  The CTAs look for their rows among the items themselves: a CTA a
+// CTA 128 values of a row, its parts in groups of threads that each add every so-manieth part up; 152 parts
+// one after the other took 80 us.  The CTAs look for their rows among the items themselves: a CTA a
 // row of what might be an item would be thousands that find none.
 #include "ak_latent.cuh"
 
@@ -17,7 +17,7 @@ constexpr int FEW_PARTS = 32;                  // of an item whose rows take a w
 template <int D>
 __global__ void __launch_bounds__(JOIN_THREADS)
 k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int rows, const int step) {
-    constexpr int LANES = D / 4, GROUPS = JOIN_THREADS / LANES;
+    constexpr int WIDE = D < 128 ? D : 128, SLICES = D / WIDE, LANES = WIDE / 4, GROUPS = JOIN_THREADS / LANES;
     const AttendParams &p = lp.a;
     __shared__ int before[JOIN_CTAS + 1];      // rows, or runs of rows, of the items that begin in the CTAs before
     __shared__ int sums[JOIN_WARPS];
@@ -30,7 +30,7 @@ k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int
     auto rows_of = [&](int b) {
         if (b >= ctas) return 0;
         const LatentJoin j = joins[b];
-        return j.last - b < FEW_PARTS ? (j.rows + JOIN_WARPS - 1) / JOIN_WARPS : j.rows;
+        return j.last - b < FEW_PARTS ? (j.rows + JOIN_WARPS - 1) / JOIN_WARPS : j.rows * SLICES;
     };
     const int r0 = rows_of(2 * tid), r1 = rows_of(2 * tid + 1);
     int incl = r0 + r1;
@@ -55,11 +55,11 @@ k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int
             else hi = mid;
         }
         const LatentJoin j = joins[lo];
-        const int r = u - before[lo], parts = j.last - lo + 1;
+        const int at = u - before[lo], parts = j.last - lo + 1;
         const float *base = p.partial + (int64_t)lo * 2 * floats;
         auto slot = [&](int k) { return base + (k ? (int64_t)k * 2 : 1) * floats; };
         if (parts <= FEW_PARTS) {
-            const int rw = r * JOIN_WARPS + warp;
+            const int rw = at * JOIN_WARPS + warp;
             if (rw >= j.rows) continue;
             // lane: a part
             const float m = lane < parts ? slot(lane)[rows * D + rw] : NEG;
@@ -98,6 +98,7 @@ k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int
             continue;
         }
         // ---- the parts' weights
+        const int r = at / SLICES, d0 = at % SLICES * WIDE;
         float mx = NEG, tot = 0.f;
         for (int k = tid; k < parts; k += JOIN_THREADS) mx = fmaxf(mx, slot(k)[rows * D + r]);
 #pragma unroll
@@ -118,7 +119,7 @@ k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int
         for (int w = 0; w < JOIN_WARPS; ++w) tot += red[1][w];
         const float inv = tot > 0.f ? 1.f / tot : tot;         // a NaN stays one
         // ---- the sum
-        const int g = tid / LANES, d = tid % LANES * 4;
+        const int g = tid / LANES, d = d0 + tid % LANES * 4;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
         for (int k = g; k < parts; k += GROUPS) {
@@ -136,7 +137,7 @@ k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int
             const int64_t dst = j.dst + (int64_t)r * step;
             store_pair(p, lp.bf16, dst * D + d, v.x * inv, v.y * inv);
             store_pair(p, lp.bf16, dst * D + d + 2, v.z * inv, v.w * inv);
-            if (tid == 0 && p.lse) p.lse[dst] = lse_of(mx, tot);
+            if (tid == 0 && d0 == 0 && p.lse) p.lse[dst] = lse_of(mx, tot);
         }
         __syncthreads();
     }

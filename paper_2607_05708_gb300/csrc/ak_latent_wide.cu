@@ -457,11 +457,11 @@ cudaError_t run_wide(const LatentParams &p, const LatentSpace &sp, int ctas, cud
     }
     const CUtensorMapDataType type = p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     CUtensorMap rows, k, v;
-    e = latent_rows_map(p, &rows);
+    e = latent_rows_map(p, 128, &rows);
     if (e == cudaSuccess) e = make_tmap_2d(&k, sp.k, type, 2, DN, (uint64_t)sp.rows, DN * 2, 64, C::TOK);
     if (e == cudaSuccess) e = make_tmap_2d(&v, sp.v, type, 2, DV, (uint64_t)sp.rows, DV * 2, 64, C::TOK);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, rows, k, v, p, sp, latent_box(p),
+    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, rows, k, v, p, sp, latent_box(p, 128),
                       (int)(p.a.n_blocks * p.a.per_block * KV_UNIT));
 }
 

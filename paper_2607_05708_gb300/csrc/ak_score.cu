@@ -138,6 +138,19 @@ cudaError_t make_tmap_2d(CUtensorMap *map, const void *base, CUtensorMapDataType
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+cudaError_t make_tmap_cols(CUtensorMap *map, const void *base, CUtensorMapDataType dtype, uint64_t cols, uint64_t rows,
+                           uint64_t row_bytes, uint32_t box_rows, uint32_t box_cols) {
+    auto fn = tmap_encoder();
+    if (!fn) return cudaErrorNotSupported;
+    cuuint64_t dims[3] = {64, rows, cols / 64};
+    cuuint64_t strides[2] = {row_bytes, 128};
+    cuuint32_t box[3] = {64, box_rows, box_cols};
+    cuuint32_t es[3] = {1, 1, 1};
+    CUresult r = fn(map, dtype, 3, const_cast<void *>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 // ------------------------------------------------------------------ tcgen05 GEMM
 // C[j, c] = <e_j, q_c> for 128-row tiles of E against column tiles of BP
 // (<= 256) query rows, on the 5th-generation tensor cores: bf16 operands

@@ -107,6 +107,14 @@ __device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, u
         "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y)
         : "memory");
 }
+__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, uint64_t *bar,
+                                            int x, int y, int z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+        "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
 // An L2 policy that evicts the lines it covers first (for data read once,
 // so that it does not displace data that is reused).
 __device__ __forceinline__ uint64_t l2_evict_first_policy() {
@@ -344,5 +352,9 @@ cudaError_t make_tmap_2d(CUtensorMap *map, const void *base, CUtensorMapDataType
                          int elem_bytes, uint64_t inner, uint64_t outer, uint64_t row_bytes,
                          uint32_t box_inner, uint32_t box_outer,
                          CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B);
+// A row-major matrix of 16-bit values as [cols / 64][rows][64]: a box of 64 x box_rows x box_cols lies in shared
+// memory as box_cols tiles of 64 columns, one after the other (128-byte swizzle).
+cudaError_t make_tmap_cols(CUtensorMap *map, const void *base, CUtensorMapDataType dtype, uint64_t cols, uint64_t rows,
+                           uint64_t row_bytes, uint32_t box_rows, uint32_t box_cols);
 
 }  // namespace ak

@@ -53,10 +53,13 @@ __device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t (&r)[4])
 __device__ __forceinline__ void tmem_st_wait() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
-// Starts contiguous global memory's way into L2 (address and size multiples of 16).
-__device__ __forceinline__ void prefetch_l2(const void *at, uint32_t bytes) {
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at), "r"(bytes) : "memory");
+// Starts a line of global memory's way into L2.
+__device__ __forceinline__ void prefetch_l2(const void *at) {
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(at) : "memory");
 }
+// The kernel behind this one may be scheduled as soon as all CTAs have come here or ended (it waits for the
+// end of this one all the same: griddep_wait).
+__device__ __forceinline__ void griddep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 // D[tmem] (+)= A[smem] B[smem]^T and D[tmem] (+)= A[tmem] B[smem], fp16, by the lane that
 // has `go`.  The whole warp comes here, so that addresses stay in uniform registers
 // (behind a branch on the lane an issue took 120 cycles and more; the product takes 64),
@@ -101,6 +104,8 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(x));
     return x != 0;
 }
+// A value that is the same in all lanes, told to the compiler: what an issue takes then stays in uniform registers.
+__device__ __forceinline__ uint32_t same(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
     umma_bf16(d, a, b, idesc, acc);
 }
@@ -120,9 +125,9 @@ __device__ __forceinline__ uint32_t desc_k(uint32_t saddr) { return ((saddr & 0x
 __device__ __forceinline__ uint32_t desc_mn(uint32_t saddr, uint32_t lbo) {
     return ((saddr & 0x3ffffu) >> 4) | (lbo >> 4) << 16;
 }
-// Instruction descriptor: D fp32, A and B fp16 (or both bf16), M = 128.
-__host__ __device__ constexpr uint32_t idesc_f16(int n, bool bf16 = false) {
-    return (1u << 4) | (bf16 ? 1u << 7 | 1u << 10 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+// Instruction descriptor: D fp32, A and B fp16 (or both bf16), M = 128 or 64.
+__host__ __device__ constexpr uint32_t idesc_f16(int n, bool bf16 = false, int m = 128) {
+    return (1u << 4) | (bf16 ? 1u << 7 | 1u << 10 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 // The A operand is MN-major (M contiguous in shared memory) instead of K-major.
 constexpr uint32_t IDESC_A_MN_MAJOR = 1u << 15;

@@ -8,7 +8,7 @@
 // so that M is full whatever the number of heads, and the R x rows accumulators (4 x 64 columns of
 // 128 lanes at R = 512) leave tensor memory for two S.  One copy of a tile in shared memory serves both
 // products: as K it is K-major, as C^T the same bytes are MN-major.
-//   a warp ahead   looks up the tiles' blocks and starts their rows' way into L2
+//   a warp ahead   looks up the tiles' blocks
 //   copying warp   the tile's boxes of tokens in pairs of 64-dim chunks; blocks that are not listed
 //                  read as zeros
 //   issuing warp   scores of the next tile and O^T += of this one, whichever is ready
@@ -48,10 +48,9 @@ struct Absorbed {
     static constexpr int SMEM = 1024 + Q_BYTES + P_BYTES + ROPES * ROPE_BYTES + STAGES * PAIR_BYTES;
     static constexpr int S_COL = 256;                    // tensor memory: O^T, then two S^T
     static_assert(PAIRS * NR <= S_COL && S_COL + 2 * NR <= 512, "tensor memory");
-    static constexpr int METAS = 3 * 512 / R * (128 / TOK) < 8 ? 3 * 512 / R * (128 / TOK) : 8;  // tiles whose places are known
-    static_assert(METAS > STAGES / PAIRS, "the tiles on their way");
+    static constexpr int METAS = STAGES / PAIRS + 2;     // tiles whose places are known
     // An item's beginning and end (rows in, result out, an empty pipeline) count as steps.
-    static constexpr int EXTRA = 128 / TOK;
+    static constexpr int EXTRA = 4;
 };
 
 // Weights are held between 2^-OFF of the reference's and 2^(OFF + SLACK): fp16 has room for both.
@@ -201,11 +200,8 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
             if (n_rope > i) mbar_wait(&rope_full[i], ((n_rope - i - 1) / C::ROPES) & 1, p.status);
         __syncwarp();
     } else if (warp == C::SOFT + 2) {
-        // ---------------- looking ahead: the tiles' places, and their rows, which are contiguous within a
-        // box, on their way into L2 while the tiles before are worked on.  (The copies take 128 bytes of
-        // a row at a time, and shared memory holds little more than a tile: alone they left latency
-        // uncovered.)
-        const int nb = TOK / box, T = p.per_block * KV_UNIT, wide = (R + lp.P) * 2;
+        // ---------------- looking ahead: the tiles' places
+        const int nb = TOK / box, T = p.per_block * KV_UNIT;
         uint32_t n_tile = 0;
         bool ok = true;
         while (left > 0 && ok) {
@@ -231,13 +227,6 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 if (lane < nb) m_row[me][lane] = row;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&mfull[me]);
-                for (int k = 0; k < nb; ++k) {
-                    const int r = __shfl_sync(0xffffffffu, row, k);
-                    if (r < 0) continue;
-                    const unsigned char *at = p.cache + (int64_t)r * wide;
-#pragma unroll 4
-                    for (int x = lane * 128; x < box * wide; x += 32 * 128) prefetch_l2(at + x);
-                }
                 next = place(i + 1);
             }
             left -= part.used;

@@ -53,10 +53,6 @@ __device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t (&r)[4])
 __device__ __forceinline__ void tmem_st_wait() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
-// Starts a line of global memory's way into L2.
-__device__ __forceinline__ void prefetch_l2(const void *at) {
-    asm volatile("prefetch.global.L2 [%0];" ::"l"(at) : "memory");
-}
 // The kernel behind this one may be scheduled as soon as all CTAs have come here or ended (it waits for the
 // end of this one all the same: griddep_wait).
 __device__ __forceinline__ void griddep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -104,8 +100,6 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(x));
     return x != 0;
 }
-// A value that is the same in all lanes, told to the compiler: what an issue takes then stays in uniform registers.
-__device__ __forceinline__ uint32_t same(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
     umma_bf16(d, a, b, idesc, acc);
 }

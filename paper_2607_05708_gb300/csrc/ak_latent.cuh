@@ -17,6 +17,7 @@ struct LatentParams {
     AttendParams a;
     int R, P;                         // latent and rotated values of a row
     bool bf16;                        // else fp16
+    bool q_map;                       // query rows come by a tensor map
     // expanded
     int nope, value;
     const void *w_k, *w_v;
@@ -33,6 +34,27 @@ __device__ __forceinline__ uint4 load_row8(const uint16_t *src, bool wide) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) h[k] = src[k];
     return *(const uint4 *)h;
+}
+
+// attend_seq with its loads side by side.
+__device__ __forceinline__ AttendSeq latent_seq(const AttendParams &p, int s) {
+    int a = 0, b = 0, n = p.max_kv, prefix = 0;
+    if (p.q_start) a = __ldg(p.q_start + s), b = __ldg(p.q_start + s + 1);
+    if (p.kv_len) n = __ldg(p.kv_len + s);
+    if (p.prefix) prefix = __ldg(p.prefix + s);
+    AttendSeq q;
+    if (p.q_start) {
+        q.row0 = max(0, min(a, p.n_q));
+        q.nq = max(0, min(b, p.n_q) - q.row0);
+    } else {
+        q.nq = p.n_q / p.n_seq;
+        q.row0 = s * q.nq;
+    }
+    q.kv = max(0, min(n, p.max_kv));
+    q.prefix = max(0, min(prefix, q.kv));
+    q.seq = s;
+    if (a < 0 || b < a || b > p.n_q || n < 0 || n > p.max_kv) set_status(p.status, AKASHIC_EDEVICE);
+    return q;
 }
 
 // attend_sums and attend_find in one where every thread has a sequence at most: the thread whose sequence has
@@ -56,7 +78,7 @@ __device__ __forceinline__ LatentShare latent_share(const AttendParams &p, int r
     if (tid == 0) have_found = 0;
     if (one) {
         const bool have = tid < p.n_seq;
-        q = attend_seq(p, have ? tid : 0);
+        q = latent_seq(p, have ? tid : 0);
         sum = attend_seq_units(p, q, have, rows, step, extra, 1, ALL) * p.heads;
         int64_t incl = sum;
 #pragma unroll

@@ -61,8 +61,9 @@ __device__ __forceinline__ void store_row32h(const LatentParams &lp, int64_t at,
 template <int DN, int DV>
 __global__ void __launch_bounds__(WideLatent<DN, DV>::THREADS, 1)
 k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap k_map,
-              const __grid_constant__ CUtensorMap v_map, const __grid_constant__ LatentParams lp,
-              const __grid_constant__ LatentSpace sp, const int box, const int n_rows) {
+              const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap q_map,
+              const __grid_constant__ LatentParams lp, const __grid_constant__ LatentSpace sp, const int box,
+              const int n_rows) {
     using C = WideLatent<DN, DV>;
     constexpr int TOK = C::TOK, ROWS = C::ROWS, KS = C::K_STAGES, VS = C::V_STAGES, HT = C::HALF;
     const AttendParams &p = lp.a;          // (heads: those of the group; its first is sp.head0)
@@ -70,7 +71,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
     unsigned char *smem = (unsigned char *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
     unsigned char *s_q = smem, *s_k = smem + C::Q_BYTES, *s_v = s_k + KS * C::K_BYTES;
     __shared__ uint64_t kfull[KS], kempty[KS], vfull[VS], vempty[VS], mfull[C::METAS];
-    __shared__ uint64_t sfull[2], pfull[2][2], odone[2][2], qfull[2], drained;
+    __shared__ uint64_t sfull[2], pfull[2][2], odone[2][2], qfull[2], qempty, drained;
     __shared__ alignas(16) int m_tag[C::METAS][TOK];
     __shared__ uint32_t m_there[C::METAS]; // of a tile: a bit every 16 tokens that are listed
     __shared__ uint32_t tmem_slot;
@@ -87,9 +88,9 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             // One a half: two may be under way, and a wait knows only the last phase from the one
             // before it.
             for (int b = 0; b < 2; ++b) mbar_init(&pfull[t][b], 4), mbar_init(&odone[t][b], 1);
-            mbar_init(&sfull[t], 1), mbar_init(&qfull[t], 4);
+            mbar_init(&sfull[t], 1), mbar_init(&qfull[t], lp.q_map ? 1 : 4);
         }
-        mbar_init(&drained, 1);
+        mbar_init(&qempty, 1), mbar_init(&drained, 1);
         mbar_fence_init();
         dead_word = 0;
         ((LatentJoin *)p.joins)[blockIdx.x] = {0, 0, 0};
@@ -103,6 +104,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
     const int64_t first = share.first, per = share.per;
     int left = share.left;
     AttendCursor cur = share.cur;
+    fence_async_smem();                    // (copies write where the plan stood)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -112,12 +114,27 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
     if (warp == C::SOFT) {
         // ---------------- copying
         const int nb = TOK / box, T = p.per_block * KV_UNIT;
-        uint32_t n_tile = 0, n_k = 0, n_v = 0;
+        uint32_t n_tile = 0, n_k = 0, n_v = 0, items = 0, q_tiles[2] = {0, 0};
         bool ok = true;
         while (left > 0 && ok) {
             const AttendPart part = attend_part(cur, left);
             if (part.n <= 0) break;
             const int first_tile = part.from + (p.ranges ? p.ranges[attend_range_at(p, cur.q, cur.tile, ROWS)].x : 0);
+            if (lp.q_map) {
+                // query rows, a row tile's 64 values at a time (those behind the item's are others' or zeros: their
+                // results are not written)
+                const int rows = cur.q.nq - cur.tile * ROWS;
+                ok = wide_wait(&qempty, (items++ & 1) ^ 1, dead, p.status);
+                if (!ok) break;
+                for (int t = 0; t < (rows > 128 ? 2 : 1); ++t, __syncwarp()) {
+                    ++q_tiles[t];
+                    if (!elect_one()) continue;
+                    mbar_expect_tx(&qfull[t], C::K_BYTES);
+                    for (int c = 0; c < C::KC; ++c)
+                        tma_load_3d(s_q + t * C::K_BYTES + c * C::CHUNK, &q_map, &qfull[t], c * 64,
+                                    cur.q.row0 + cur.tile * ROWS + t * 128, sp.head0 + cur.head);
+                }
+            }
             const int64_t *list = p.blocks + cur.seq * p.max_blocks;
             // lane: the row of 16 tokens lane % 8 of a tile, -1: not listed
             auto place = [&](int i) {
@@ -176,6 +193,8 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             if (left > 0) attend_next(p, ROWS, TOK, C::EXTRA, 1, ALL, cur);
         }
         // nothing is on its way when the CTA ends (where a wait gave up; else all has been read)
+        for (int t = 0; !ok && t < 2; ++t)
+            if (q_tiles[t]) mbar_wait(&qfull[t], (q_tiles[t] - 1) & 1, p.status);
         for (uint32_t i = 0; !ok && i < KS; ++i)
             if (n_k > i) mbar_wait(&kfull[i], ((n_k - i - 1) / KS) & 1, p.status);
         for (uint32_t i = 0; !ok && i < VS; ++i)
@@ -190,7 +209,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
         uint32_t n_tile = 0, q_phase = 0, tiles0 = 0, tiles1 = 0;      // tiles: of the row tile, so far
         bool ok = true;
         // S of the item's tile i for row tile t; the row tiles share a tile's keys
-        auto scores = [&](int t, int i, int mt) {
+        auto scores = [&](int t, int i, int mt, bool last) {
             const uint32_t x = n_tile + i, st = x % KS;
             if (ok && t == 0) ok = wide_wait(&kfull[st], (x / KS) & 1, dead, p.status);
             if (!ok) return;
@@ -209,6 +228,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 }
                 umma_commit(&sfull[t]);
                 if (t == mt - 1) umma_commit(&kempty[st]);
+                if (t == mt - 1 && last) umma_commit(&qempty);
             }
             __syncwarp();
         };
@@ -237,13 +257,13 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             for (int t = 0; t < mt; ++t) {
                 if (ok) ok = wide_wait(&qfull[t], q_phase >> t & 1, dead, p.status);
                 q_phase ^= 1u << t;
-                scores(t, 0, mt);
+                scores(t, 0, mt, n == 1);
             }
             for (int i = 0; ok && i < n; ++i) {
                 for (int t = 0; t < mt; ++t) values(t, i, 0, mt);
                 for (int t = 0; t < mt; ++t) {
                     values(t, i, 1, mt);
-                    if (i + 1 < n) scores(t, i + 1, mt);
+                    if (i + 1 < n) scores(t, i + 1, mt, i + 2 == n);
                 }
             }
             tiles0 += n;
@@ -272,31 +292,22 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             const int row_first = cur.tile * ROWS, rows = min(ROWS, sq.nq - row_first);
             const int first_tile = mine.from + (p.ranges ? p.ranges[attend_range_at(p, sq, cur.tile, ROWS)].x : 0);
             if (t == 0 || rows > 128) {
-                // ---- the warp's 32 query rows, 16 bytes a lane
-                const int g_all = (DN + lp.P) / 8, head = sp.head0 + cur.head;
-#pragma unroll 1
-                for (int x0 = lane; x0 < 32 * g_all; x0 += 32 * 8) {
-                    uint4 z[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int x = x0 + 32 * k, y = lp.P == 64 ? x / (DN / 8 + 8) : x / (DN / 8 + 4), g = x - y * g_all;
-                        const int row = t * 128 + (warp & 3) * 32 + y;
-                        z[k] = make_uint4(0, 0, 0, 0);
-                        if (y < 32 && row < rows)
-                            z[k] = load_row8((const uint16_t *)p.q + (int64_t)(sq.row0 + row_first + row) * p.q_row +
-                                             head * p.q_head + g * 8, p.q_wide);
+                const int head = sp.head0 + cur.head;
+                if (!lp.q_map) {
+                    // ---- the warp's 32 query rows, whose strides no tensor map has
+                    const int g_all = (DN + lp.P) / 8;
+                    for (int x = lane; x < 32 * g_all; x += 32) {
+                        const int row = (warp & 3) * 32 + x / g_all, g = x % g_all;
+                        uint4 z = make_uint4(0, 0, 0, 0);
+                        if (t * 128 + row < rows)
+                            z = load_row8((const uint16_t *)p.q + (int64_t)(sq.row0 + row_first + t * 128 + row) * p.q_row +
+                                          head * p.q_head + g * 8, p.q_wide);
+                        *(uint4 *)(s_q + t * C::K_BYTES + (g >> 3) * C::CHUNK + row * 128 + (((g & 7) ^ (row & 7)) << 4)) = z;
                     }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int x = x0 + 32 * k, y = lp.P == 64 ? x / (DN / 8 + 8) : x / (DN / 8 + 4), g = x - y * g_all;
-                        const int row = (warp & 3) * 32 + y;
-                        if (y < 32)
-                            *(uint4 *)(s_q + t * C::K_BYTES + (g >> 3) * C::CHUNK + row * 128 + (((g & 7) ^ (row & 7)) << 4)) = z[k];
-                    }
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&qfull[t]);
                 }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&qfull[t]);
                 const int r = t * 128 + rt;
                 const bool real = r < rows;
                 const int limit = real ? attend_limit(p, sq, row_first + r) : sq.kv;
@@ -442,7 +453,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
 }
 
 template <int DN, int DV>
-cudaError_t run_wide(const LatentParams &p, const LatentSpace &sp, int ctas, cudaStream_t st) {
+cudaError_t run_wide(LatentParams &p, const LatentSpace &sp, int ctas, cudaStream_t st) {
     using C = WideLatent<DN, DV>;
     auto *kernel = k_latent_wide<DN, DV>;
     // once a device (the attribute stays; another thread that comes first does the same)
@@ -460,8 +471,14 @@ cudaError_t run_wide(const LatentParams &p, const LatentSpace &sp, int ctas, cud
     e = latent_rows_map(p, 128, &rows);
     if (e == cudaSuccess) e = make_tmap_2d(&k, sp.k, type, 2, DN, (uint64_t)sp.rows, DN * 2, 64, C::TOK);
     if (e == cudaSuccess) e = make_tmap_2d(&v, sp.v, type, 2, DV, (uint64_t)sp.rows, DV * 2, 64, C::TOK);
+    const int64_t far = 1LL << 32;             // (bytes: a tensor map's strides are below 2^40)
+    p.q_map = p.a.q_wide && p.a.q_row > 0 && p.a.q_head > 0 && p.a.q_row < far && p.a.q_head < far;
+    CUtensorMap q = rows;
+    if (e == cudaSuccess && p.q_map)
+        p.q_map = make_tmap_3d(&q, p.a.q, type, DN + p.P, (uint64_t)p.a.n_q, p.a.q_row * 2, (uint64_t)p.a.q_heads,
+                               p.a.q_head * 2, 64, 128) == cudaSuccess;
     if (e != cudaSuccess) return e;
-    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, rows, k, v, p, sp, latent_box(p, 128),
+    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, rows, k, v, q, p, sp, latent_box(p, 128),
                       (int)(p.a.n_blocks * p.a.per_block * KV_UNIT));
 }
 

@@ -138,17 +138,26 @@ cudaError_t make_tmap_2d(CUtensorMap *map, const void *base, CUtensorMapDataType
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-cudaError_t make_tmap_cols(CUtensorMap *map, const void *base, CUtensorMapDataType dtype, uint64_t cols, uint64_t rows,
-                           uint64_t row_bytes, uint32_t box_rows, uint32_t box_cols) {
+static cudaError_t make_tmap_planes(CUtensorMap *map, const void *base, CUtensorMapDataType dtype, const uint64_t (&size)[3],
+                                    const uint64_t (&stride)[2], const uint32_t (&box_size)[3]) {
     auto fn = tmap_encoder();
     if (!fn) return cudaErrorNotSupported;
-    cuuint64_t dims[3] = {64, rows, cols / 64};
-    cuuint64_t strides[2] = {row_bytes, 128};
-    cuuint32_t box[3] = {64, box_rows, box_cols};
+    cuuint64_t dims[3] = {size[0], size[1], size[2]};
+    cuuint64_t strides[2] = {stride[0], stride[1]};
+    cuuint32_t box[3] = {box_size[0], box_size[1], box_size[2]};
     cuuint32_t es[3] = {1, 1, 1};
     CUresult r = fn(map, dtype, 3, const_cast<void *>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+cudaError_t make_tmap_3d(CUtensorMap *map, const void *base, CUtensorMapDataType dtype, uint64_t inner, uint64_t rows,
+                         uint64_t row_bytes, uint64_t planes, uint64_t plane_bytes, uint32_t box_inner,
+                         uint32_t box_rows) {
+    return make_tmap_planes(map, base, dtype, {inner, rows, planes}, {row_bytes, plane_bytes}, {box_inner, box_rows, 1});
+}
+cudaError_t make_tmap_cols(CUtensorMap *map, const void *base, CUtensorMapDataType dtype, uint64_t cols, uint64_t rows,
+                           uint64_t row_bytes, uint32_t box_rows, uint32_t box_cols) {
+    return make_tmap_planes(map, base, dtype, {64, rows, cols / 64}, {row_bytes, 128}, {64, box_rows, box_cols});
 }
 
 // ------------------------------------------------------------------ tcgen05 GEMM

@@ -352,6 +352,10 @@ cudaError_t make_tmap_2d(CUtensorMap *map, const void *base, CUtensorMapDataType
                          int elem_bytes, uint64_t inner, uint64_t outer, uint64_t row_bytes,
                          uint32_t box_inner, uint32_t box_outer,
                          CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B);
+// 16-bit values [planes][rows][inner], strides in bytes; boxes of box_inner x box_rows of one plane (128-byte swizzle).
+cudaError_t make_tmap_3d(CUtensorMap *map, const void *base, CUtensorMapDataType dtype, uint64_t inner, uint64_t rows,
+                         uint64_t row_bytes, uint64_t planes, uint64_t plane_bytes, uint32_t box_inner,
+                         uint32_t box_rows);
 // A row-major matrix of 16-bit values as [cols / 64][rows][64]: a box of 64 x box_rows x box_cols lies in shared
 // memory as box_cols tiles of 64 columns, one after the other (128-byte swizzle).
 cudaError_t make_tmap_cols(CUtensorMap *map, const void *base, CUtensorMapDataType dtype, uint64_t cols, uint64_t rows,

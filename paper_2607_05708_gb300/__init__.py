@@ -485,21 +485,34 @@ class _BlockCache:
     def _on(self, stream):
         return self._current(self.device) if stream is None else stream.cuda_stream
 
+    def _rows2(self, t, name, width):
+        """_rows of one head's rows [n, width]: dtype code, length, stride."""
+        code = self._dtypes.get(t.dtype)
+        if code is None:
+            raise TypeError(f"{name} must be bfloat16, float16 or float32, got {t.dtype}")
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} must be a CUDA tensor on device {self.device}")
+        shape, strides = t.shape, t.stride()
+        if len(shape) != 2 or shape[1] != width:
+            raise ValueError(f"{name} must be [n, {width}]")
+        if strides[1] != 1 and t.numel():
+            raise ValueError(f"{name} must be contiguous in its last dimension")
+        return code, shape[0], strides[0]
+
     def _rotation(self, n, width, dt, positions, cos, sin, q, q_out, interleaved, stream):
         """The rotation of n tokens as the ABI takes it, and q_out."""
-        f32 = self._torch.float32
+        vec, f32 = self._vec, self._torch.float32
         if positions is None or cos is None or sin is None:
             raise ValueError("a rotation needs positions, cos and sin")
         if cos.dim() != 2 or sin.shape != cos.shape:
             raise ValueError("cos and sin must be [positions, rotary_dim / 2]")
         rows, half = cos.shape
-        r = _Rotation(self._vec(positions, self._torch.int64, "positions", n),
-                      self._vec(cos, f32, "cos", rows * half), self._vec(sin, f32, "sin", rows * half), rows,
-                      2 * half, 1 if interleaved else 0)
+        at = vec(positions, self._torch.int64, "positions", n)
+        pc, ps = vec(cos, f32, "cos", rows * half), vec(sin, f32, "sin", rows * half)
         if q is None:
             if q_out is not None:
                 raise ValueError("q_out needs q")
-            return r, None
+            return ctypes.byref(_Rotation(at, pc, ps, rows, 2 * half, 1 if interleaved else 0)), None
         code, shape, st = self._rows(q, "q", width)
         if code != dt or shape[0] != n:
             raise ValueError(f"q must be of the rows' type, {n} tokens")
@@ -510,9 +523,8 @@ class _BlockCache:
             code, other, so = self._rows(q_out, "q_out", width)
             if code != dt or other != shape:
                 raise ValueError("q_out must be of q's type and shape")
-        r.q, r.q_row_stride, r.q_head_stride, r.q_heads = q.data_ptr(), st[0], st[1], shape[1]
-        r.q_out, r.q_out_row_stride, r.q_out_head_stride = q_out.data_ptr(), so[0], so[1]
-        return r, q_out
+        return ctypes.byref(_Rotation(at, pc, ps, rows, 2 * half, 1 if interleaved else 0, q.data_ptr(), st[0], st[1],
+                                      shape[1], q_out.data_ptr(), so[0], so[1])), q_out
 
     def sync(self, stream=None):
         """Wait for the stream, then raise (and clear) what the kernels recorded: a slot,
@@ -593,7 +605,7 @@ class KVCache(_BlockCache):
         r, q_out = self._rotation(n, self.head_dim, dt, positions, cos, sin, q, q_out, interleaved, stream)
         rc = self._append(self._cfg, self._data_ptr, self._tags_ptr, k.data_ptr(), sk[0], sk[1], v.data_ptr(),
                           sv[0], sv[1], dt, n, self._vec(slots, self._torch.int64, "slots", n),
-                          self._vec(tags, self._torch.int32, "tags", n), ctypes.byref(r), self._status_ptr,
+                          self._vec(tags, self._torch.int32, "tags", n), r, self._status_ptr,
                           self._on(stream))
         if rc:
             _check(rc)
@@ -720,24 +732,24 @@ class LatentCache(_BlockCache):
         stride of the first dimension) into slots (as KVCache.write), k_rope rotated
         where positions, cos and sin (float32 [positions, rope_dim / 2]) are given, and with it
         q [n, q_heads, rope_dim] as in KVCache.append.  Returns q_out (None without q)."""
-        dt, (n, _, _), sl = self._rows(latent[:, None], "latent", self.latent_dim, 1)
-        dtk, (nk, _, _), sk = self._rows(k_rope[:, None], "k_rope", self.rope_dim, 1)
+        dt, n, sl = self._rows2(latent, "latent", self.latent_dim)
+        dtk, nk, sk = self._rows2(k_rope, "k_rope", self.rope_dim)
         if dtk != dt or nk != n:
             raise ValueError("latent and k_rope must be of one type and length")
         if tags is not None and self.tags is None:
             raise ValueError("tags need a tagged cache")
         ref = None
         if positions is not None or cos is not None or sin is not None or q is not None or q_out is not None:
-            r, q_out = self._rotation(n, self.rope_dim, dt, positions, cos, sin, q, q_out, interleaved, stream)
-            ref = ctypes.byref(r)
-        rc = self._append(self._cfg, self._data_ptr, self._tags_ptr, latent.data_ptr(), sl[0], k_rope.data_ptr(),
-                          sk[0], dt, n, self._vec(slots, self._torch.int64, "slots", n),
+            ref, q_out = self._rotation(n, self.rope_dim, dt, positions, cos, sin, q, q_out, interleaved, stream)
+        rc = self._append(self._cfg, self._data_ptr, self._tags_ptr, latent.data_ptr(), sl, k_rope.data_ptr(),
+                          sk, dt, n, self._vec(slots, self._torch.int64, "slots", n),
                           self._vec(tags, self._torch.int32, "tags", n), ref, self._status_ptr, self._on(stream))
         if rc:
             _check(rc)
         return q_out
 
-    def _run(self, a, q, blocks, width, expanded, kv_len, q_start, prefix_len, q_tags, out, lse, stream):
+    def _run(self, q, sq, blocks, scale, width, kv_len, q_start, causal, prefix_len, q_tags, out, lse, stream,
+             weights=()):
         torch = self._torch
         vec, i32 = self._vec, torch.int32
         n_q, q_heads, _ = q.shape
@@ -746,27 +758,26 @@ class LatentCache(_BlockCache):
         if q_tags is not None and self.tags is None:
             raise ValueError("q_tags need a tagged cache")
         n_seq, listed = blocks.shape
-        a.n_q, a.q_heads, a.n_seq, a.max_blocks = n_q, q_heads, n_seq, listed
-        a.q_start, a.kv_len = vec(q_start, i32, "q_start", n_seq + 1), vec(kv_len, i32, "kv_len", n_seq)
-        a.blocks = vec(blocks, torch.int64, "blocks", n_seq * listed)
-        a.prefix_len = vec(prefix_len, i32, "prefix_len", n_seq)
-        if q_tags is not None:
-            a.tags, a.q_tags = self._tags_ptr, vec(q_tags, i32, "q_tags", n_q)
         behind = q_start is not None or n_seq == 0         # rows that no sequence has
         if out is None:
             out = self._empty((n_q, q_heads, width), self.dtype, stream, zero=behind)
-            a.out = out.data_ptr()
+            po = out.data_ptr()
         else:
-            a.out = vec(out, self.dtype, "out", n_q * q_heads * width)
-        if not expanded:
+            po = vec(out, self.dtype, "out", n_q * q_heads * width)
+        pl = None
+        if not weights:
             if lse is None:
                 lse = self._empty((n_q, q_heads), torch.float32, stream, zero=behind)
-                a.lse = lse.data_ptr()
+                pl = lse.data_ptr()
             else:
-                a.lse = vec(lse, torch.float32, "lse", n_q * q_heads)
-        call, scratch_of = self._calls[expanded]
-        ref = ctypes.byref(a)
-        key = (expanded, n_q, q_heads, n_seq, listed, q_start is None, q_tags is None, a.nope_dim, a.value_dim)
+                pl = vec(lse, torch.float32, "lse", n_q * q_heads)
+        ref = ctypes.byref(_LatentAttend(
+            q.data_ptr(), sq[0], sq[1], n_q, q_heads, n_seq, vec(q_start, i32, "q_start", n_seq + 1),
+            vec(kv_len, i32, "kv_len", n_seq), vec(blocks, torch.int64, "blocks", n_seq * listed), listed,
+            1 if causal else 0, vec(prefix_len, i32, "prefix_len", n_seq), scale,
+            None if q_tags is None else self._tags_ptr, vec(q_tags, i32, "q_tags", n_q), po, pl, *weights))
+        call, scratch_of = self._calls[len(weights) > 0]
+        key = (n_q, q_heads, n_seq, listed, q_start is None, q_tags is None, weights[-2:])
         size = self._scratch.get(key)
         if size is None:
             need = ctypes.c_int64()
@@ -792,9 +803,8 @@ class LatentCache(_BlockCache):
         dt, _, sq = self._rows(q, "q", self.latent_dim + self.rope_dim)
         if q.dtype is not self.dtype:
             raise TypeError(f"q must be {self.dtype}, got {q.dtype}")
-        a = _LatentAttend(q=q.data_ptr(), q_row_stride=sq[0], q_head_stride=sq[1], causal=1 if causal else 0,
-                          scale=scale)
-        return self._run(a, q, blocks, self.latent_dim, False, kv_len, q_start, prefix_len, q_tags, out, lse, stream)
+        return self._run(q, sq, blocks, scale, self.latent_dim, kv_len, q_start, causal, prefix_len, q_tags, out, lse,
+                         stream)
 
     def attend_expanded(self, q, w_k, w_v, blocks, scale=None, kv_len=None, q_start=None, causal=True,
                         prefix_len=None, q_tags=None, out=None, stream=None):
@@ -816,9 +826,7 @@ class LatentCache(_BlockCache):
             raise TypeError(f"q must be {self.dtype}, got {q.dtype}")
         if w_k.shape[0] != shape[1] or w_v.shape[0] != shape[1]:
             raise ValueError("w_k and w_v must have q's heads")
-        a = _LatentAttend(q=q.data_ptr(), q_row_stride=sq[0], q_head_stride=sq[1], causal=1 if causal else 0,
-                          scale=(nope + self.rope_dim) ** -0.5 if scale is None else scale,
-                          w_k=w_k.data_ptr(), w_v=w_v.data_ptr(), w_k_head_stride=w_k.stride(0),
-                          w_k_row_stride=w_k.stride(1), w_v_head_stride=w_v.stride(0),
-                          w_v_row_stride=w_v.stride(1), nope_dim=nope, value_dim=value)
-        return self._run(a, q, blocks, value, True, kv_len, q_start, prefix_len, q_tags, out, None, stream)[0]
+        scale = (nope + self.rope_dim) ** -0.5 if scale is None else scale
+        return self._run(q, sq, blocks, scale, value, kv_len, q_start, causal, prefix_len, q_tags, out, None, stream,
+                         (w_k.data_ptr(), w_v.data_ptr(), w_k.stride(0), w_k.stride(1), w_v.stride(0), w_v.stride(1),
+                          nope, value))[0]

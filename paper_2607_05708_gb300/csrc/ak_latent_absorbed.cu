@@ -33,7 +33,7 @@ template <int R, int NR>
 struct Absorbed {
     static constexpr int TOK = TOK_OF(R, NR);            // tokens of a tile
     static constexpr int PAIRS = R / 128, CHUNKS = R / 64 + 1;
-    static constexpr int CW = NR < 32 ? NR : 32;         // rows of a softmax thread
+    static constexpr int CW = 16;                         // rows of a softmax thread
     static constexpr int SOFT = NR / CW * 4;             // softmax warps
     static constexpr int THREADS = 32 * (SOFT + 4);
     static constexpr int PAIR_BYTES = TOK * 256, ROPE_BYTES = TOK * 128;
@@ -382,18 +382,15 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
             float l[CW];
 #pragma unroll
             for (int c = 0; c < CW; ++c) l[c] = 0.f;
-            // The CTA's first tile is preceded by one in which nothing is seen and nothing told: its instructions come
-            // from memory while the tokens do (4,000 to 10,000 cycles less to the first weights).
-            for (int i = n_tile ? 0 : -1; i < n; ++i) {
-                const bool dry = i < 0;
+            for (int i = 0; i < n; ++i, ++n_tile) {
                 const int tok = (mine.from + i) * TOK;
-                if (!dry) ok = ok && wide_wait(&mfull[n_tile % C::METAS], (n_tile / C::METAS) & 1, dead, p.status);
-                const int row = dry ? -1 : m_row[n_tile % C::METAS][key / box];
+                ok = ok && wide_wait(&mfull[n_tile % C::METAS], (n_tile / C::METAS) & 1, dead, p.status);
+                const int row = m_row[n_tile % C::METAS][key / box];
                 const bool have = row >= 0 && used;
                 int tag = -1;
                 if (tags && have) tag = max(-1, p.tags[(int64_t)row + key % box]);
                 const bool masked = __any_sync(0xffffffffu, used && !have) || tags || tok > safe;
-                if (!dry) ok = ok && wide_wait(&sfull[n_tile & 1], n_tile >> 1 & 1, dead, p.status);
+                ok = ok && wide_wait(&sfull[n_tile & 1], n_tile >> 1 & 1, dead, p.status);
                 tc_fence_after();
                 uint32_t raw[CW];
                 tmem_ldn<CW>(tmem + lanes + C::S_COL + (n_tile & 1) * NR + c0, raw);
@@ -429,7 +426,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                     most = fmaxf(fmaxf(most, x[c] - m.x), fmaxf(x[c + 1] - m.y, fmaxf(x[c + 2] - m.z, x[c + 3] - m.w)));
                 }
                 bool waited = false;           // for the products before
-                if (bar_any(2, THR, dry || most > OFF + SLACK)) {
+                if (bar_any(2, THR, most > OFF + SLACK)) {
                     // ---- a row's reference is raised: its maximum over the tile's tokens
                     float v[CW];
 #pragma unroll
@@ -491,9 +488,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 fence_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (dry) continue;
                 if (lane == 0) mbar_arrive(&pfull[n_tile & 1]);
-                ++n_tile;
             }
             // ---- totals
             if (left == mine.used) griddep_launch();

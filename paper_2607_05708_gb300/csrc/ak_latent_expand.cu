@@ -141,7 +141,7 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
                 const uint32_t st = n_w % ST;
                 ok = wide_wait(&wempty[st], ((n_w / ST) & 1) ^ 1, dead, p.status);
                 if (!ok) break;
-                if (lane == 0) {
+                if (elect_one()) {
                     mbar_expect_tx(&wfull[st], rows_w * 128);
                     tma_load_2d(s_w + st * C::W_BYTES, &k_map, &wfull[st], c * 64, (int)(h * sp.k_step));
                     tma_load_2d(s_w + st * C::W_BYTES + lp.nope * 128, &v_map, &wfull[st], c * 64, (int)(h * sp.v_step));
@@ -223,7 +223,11 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
                 uint16_t *dst = c < lp.nope ? (uint16_t *)sp.k + row * lp.nope + c
                                             : (uint16_t *)sp.v + row * lp.value + (c - lp.nope);
 #pragma unroll
-                for (int k = 0; k < 16; k += 4) *(uint4 *)(dst + 2 * k) = make_uint4(h[k], h[k + 1], h[k + 2], h[k + 3]);
+                for (int k = 0; k < 16; k += 8)                // whole sectors
+                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 2 * k), "r"(h[k]),
+                                 "r"(h[k + 1]), "r"(h[k + 2]), "r"(h[k + 3]), "r"(h[k + 4]), "r"(h[k + 5]),
+                                 "r"(h[k + 6]), "r"(h[k + 7])
+                                 : "memory");
             }
             tc_fence_before();
             __syncwarp();

@@ -26,10 +26,16 @@ struct WideLatent {
     static constexpr int CHUNK = TOK * 128;              // 64 values of 128 rows
     static constexpr int KC = DN / 64 + 1, VC = DV / 64; // chunks of a key, of a value
     static constexpr int K_BYTES = KC * CHUNK, V_BYTES = VC * CHUNK, Q_BYTES = 2 * K_BYTES;
-    static constexpr int K_STAGES = 2, V_STAGES = Q_BYTES + 2 * (K_BYTES + V_BYTES) <= 229376 ? 2 : 1;
-    static constexpr int METAS = 3;                      // tiles whose tags are kept: the third's keys wait for the
-                                                         // second's scores, these for the first's weights
-    static constexpr int SMEM = 1024 + Q_BYTES + K_STAGES * K_BYTES + V_STAGES * V_BYTES;
+    // Keys and values in one ring of chunks, tile by tile.  Two tiles where there is room; else (DN = DV = 128) eight
+    // chunks of a tile's five: keys then wait for the values of the tile before the last, values for the scores of
+    // the last, which are both over long before.  (Values in a buffer of their own waited for the
+    // products with the ones before them: a step of 256 rows and 128 tokens 5000 cycles.)
+    static constexpr int TILE = KC + VC, SLOTS = Q_BYTES / CHUNK + 2 * TILE <= 14 ? 2 * TILE : 14 - Q_BYTES / CHUNK;
+    static constexpr bool TWO = SLOTS == 2 * TILE;
+    static_assert(TWO || (KC == 3 && VC == 2 && SLOTS == 8), "what waits for what");
+    __device__ static uint32_t slot(uint32_t tile, int chunk) { return (tile * TILE + chunk) % SLOTS; }
+    static constexpr int METAS = 3;                      // tiles whose tags are kept
+    static constexpr int SMEM = 1024 + Q_BYTES + SLOTS * CHUNK;
     static constexpr int SOFT = 8, THREADS = 32 * (SOFT + 2);
     static constexpr int S_COL = 2 * DV;                 // tensor memory: O, then S
     static_assert(S_COL + 2 * TOK <= 512, "tensor memory");
@@ -65,12 +71,12 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
               const __grid_constant__ LatentParams lp, const __grid_constant__ LatentSpace sp, const int box,
               const int n_rows) {
     using C = WideLatent<DN, DV>;
-    constexpr int TOK = C::TOK, ROWS = C::ROWS, KS = C::K_STAGES, VS = C::V_STAGES, HT = C::HALF;
+    constexpr int TOK = C::TOK, ROWS = C::ROWS, HT = C::HALF;
     const AttendParams &p = lp.a;          // (heads: those of the group; its first is sp.head0)
     extern __shared__ unsigned char raw_smem[];
     unsigned char *smem = (unsigned char *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
-    unsigned char *s_q = smem, *s_k = smem + C::Q_BYTES, *s_v = s_k + KS * C::K_BYTES;
-    __shared__ uint64_t kfull[KS], kempty[KS], vfull[VS], vempty[VS], mfull[C::METAS];
+    unsigned char *s_q = smem, *s_kv = smem + C::Q_BYTES;
+    __shared__ uint64_t kfull[2], kempty[2], vfull[2], vempty[2], mfull[C::METAS];
     __shared__ uint64_t sfull[2], pfull[2][2], odone[2][2], qfull[2], qempty, drained;
     __shared__ alignas(16) int m_tag[C::METAS][TOK];
     __shared__ uint32_t m_there[C::METAS]; // of a tile: a bit every 16 tokens that are listed
@@ -81,8 +87,10 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
 
     griddep_wait();
     if (tid == 0) {
-        for (int i = 0; i < KS; ++i) mbar_init(&kfull[i], 1), mbar_init(&kempty[i], 1);
-        for (int i = 0; i < VS; ++i) mbar_init(&vfull[i], 1), mbar_init(&vempty[i], 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&kfull[i], 1), mbar_init(&kempty[i], 1);
+            mbar_init(&vfull[i], 1), mbar_init(&vempty[i], 1);
+        }
         for (int i = 0; i < C::METAS; ++i) mbar_init(&mfull[i], 1);
         for (int t = 0; t < 2; ++t) {
             // One a half: two may be under way, and a wait knows only the last phase from the one
@@ -158,8 +166,10 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 const int row = next, tok = (first_tile + i) * TOK;
                 const int4 tag = next_tags;
                 next = place(i + 1);
-                const uint32_t st = n_tile % KS, me = n_tile % C::METAS, sv = n_tile % VS;
-                ok = wide_wait(&kempty[st], ((n_tile / KS) & 1) ^ 1, dead, p.status);
+                const uint32_t b = n_tile & 1, me = n_tile % C::METAS;
+                // (a tile's meta goes where that of the third before it was: its weights came before the scores of
+                // the tile after it, which came before the weights, and so the values, of the second before this)
+                if (n_tile > 1) ok = wide_wait(C::TWO ? &kempty[b] : &vempty[b], (n_tile - 2) >> 1 & 1, dead, p.status);
                 if (!ok) break;
                 const uint32_t there = __ballot_sync(0xffffffffu, row >= 0) & 255u;
                 if (tags)
@@ -168,25 +178,26 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(&mfull[me]);
-                    mbar_expect_tx(&kfull[st], C::K_BYTES);
+                    mbar_expect_tx(&kfull[b], C::K_BYTES);
                 }
                 // the sequence's rows in the scratch end with its tiles: behind them zeros
                 const int y = tok < max(cur.q.kv, 1) ? (int)(at + tok) : (int)sp.rows;
                 const int box_row = __shfl_sync(0xffffffffu, row, lane % nb * (box / 16));
                 __syncwarp();
-                unsigned char *kt = s_k + st * C::K_BYTES;
+                auto chunk = [&](int c) { return s_kv + C::slot(n_tile, c) * C::CHUNK; };
                 if (lane < nb)
-                    tma_load_2d(kt + (C::KC - 1) * C::CHUNK + lane * box * 128, &rows_map, &kfull[st], lp.R,
+                    tma_load_2d(chunk(C::KC - 1) + lane * box * 128, &rows_map, &kfull[b], lp.R,
                                 box_row < 0 ? n_rows : box_row);
                 else if (lane >= 16 && lane < 16 + C::KC - 1)
-                    tma_load_2d(kt + (lane - 16) * C::CHUNK, &k_map, &kfull[st], (lane - 16) * 64, y);
+                    tma_load_2d(chunk(lane - 16), &k_map, &kfull[b], (lane - 16) * 64, y);
                 ++n_k;
                 next_tags = tags_of(next);
-                ok = wide_wait(&vempty[sv], ((n_tile / VS) & 1) ^ 1, dead, p.status);
+                if (C::TWO && n_tile > 1) ok = wide_wait(&vempty[b], (n_tile - 2) >> 1 & 1, dead, p.status);
+                if (!C::TWO && n_tile > 0) ok = wide_wait(&kempty[b ^ 1], (n_tile - 1) >> 1 & 1, dead, p.status);
                 if (!ok) break;
-                if (lane == 0) mbar_expect_tx(&vfull[sv], C::V_BYTES);
+                if (lane == 0) mbar_expect_tx(&vfull[b], C::V_BYTES);
                 __syncwarp();
-                if (lane < C::VC) tma_load_2d(s_v + sv * C::V_BYTES + lane * C::CHUNK, &v_map, &vfull[sv], lane * 64, y);
+                if (lane < C::VC) tma_load_2d(chunk(C::KC + lane), &v_map, &vfull[b], lane * 64, y);
                 ++n_v;
             }
             left -= part.used;
@@ -195,57 +206,61 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
         // nothing is on its way when the CTA ends (where a wait gave up; else all has been read)
         for (int t = 0; !ok && t < 2; ++t)
             if (q_tiles[t]) mbar_wait(&qfull[t], (q_tiles[t] - 1) & 1, p.status);
-        for (uint32_t i = 0; !ok && i < KS; ++i)
-            if (n_k > i) mbar_wait(&kfull[i], ((n_k - i - 1) / KS) & 1, p.status);
-        for (uint32_t i = 0; !ok && i < VS; ++i)
-            if (n_v > i) mbar_wait(&vfull[i], ((n_v - i - 1) / VS) & 1, p.status);
+        for (uint32_t i = 0; !ok && i < 2; ++i) {
+            if (n_k > i) mbar_wait(&kfull[(n_k - i - 1) & 1], (n_k - i - 1) >> 1 & 1, p.status);
+            if (n_v > i) mbar_wait(&vfull[(n_v - i - 1) & 1], (n_v - i - 1) >> 1 & 1, p.status);
+        }
         __syncwarp();
     } else if (warp == C::SOFT + 1) {
         // ---------------- issuing
-        const uint32_t id_s = idesc_f16(TOK, lp.bf16), id_o = idesc_f16(DV, lp.bf16) | IDESC_B_MN_MAJOR;
-        const uint64_t q_at = desc64(desc_k(smem_u32(s_q))), k_at = desc64(desc_k(smem_u32(s_k)));
-        const uint64_t v_at = desc64(desc_mn(smem_u32(s_v), C::CHUNK));
+        const uint32_t id_s = idesc_f16(TOK, lp.bf16), id_o = idesc_f16(64, lp.bf16) | IDESC_B_MN_MAJOR;
+        const uint64_t q_at = desc64(desc_k(smem_u32(s_q))), k_at = desc64(desc_k(smem_u32(s_kv)));
+        const uint64_t v_at = desc64(desc_mn(smem_u32(s_kv), 0));
         const int rope_steps = lp.P / 16;
         uint32_t n_tile = 0, q_phase = 0, tiles0 = 0, tiles1 = 0;      // tiles: of the row tile, so far
         bool ok = true;
         // S of the item's tile i for row tile t; the row tiles share a tile's keys
         auto scores = [&](int t, int i, int mt, bool last) {
-            const uint32_t x = n_tile + i, st = x % KS;
-            if (ok && t == 0) ok = wide_wait(&kfull[st], (x / KS) & 1, dead, p.status);
+            const uint32_t x = n_tile + i;
+            if (ok && t == 0) ok = wide_wait(&kfull[x & 1], x >> 1 & 1, dead, p.status);
             if (!ok) return;
             tc_fence_after();
             if (elect_one()) {
                 const uint32_t d = tmem + C::S_COL + t * TOK;
-                const uint64_t qa = q_at + t * (C::K_BYTES >> 4), ka = k_at + st * (C::K_BYTES >> 4);
+                const uint64_t qa = q_at + t * (C::K_BYTES >> 4);
 #pragma unroll
-                for (int k = 0; k < DN / 16; ++k) {
-                    const uint32_t o = k / 4 * (C::CHUNK >> 4) + 2 * (k % 4);
-                    mma_ss(d, qa + o, ka + o, id_s, k > 0);
+                for (int c = 0; c < C::KC - 1; ++c) {
+                    const uint64_t ka = k_at + C::slot(x, c) * (C::CHUNK >> 4);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_ss(d, qa + c * (C::CHUNK >> 4) + 2 * k, ka + 2 * k, id_s, c > 0 || k > 0);
                 }
-                for (int k = 0; k < rope_steps; ++k) {
-                    const uint32_t o = (C::KC - 1) * (C::CHUNK >> 4) + 2 * k;
-                    mma_ss(d, qa + o, ka + o, id_s, true);
-                }
+                const uint64_t ka = k_at + C::slot(x, C::KC - 1) * (C::CHUNK >> 4);
+                for (int k = 0; k < rope_steps; ++k)
+                    mma_ss(d, qa + (C::KC - 1) * (C::CHUNK >> 4) + 2 * k, ka + 2 * k, id_s, true);
                 umma_commit(&sfull[t]);
-                if (t == mt - 1) umma_commit(&kempty[st]);
+                if (t == mt - 1) umma_commit(&kempty[x & 1]);
                 if (t == mt - 1 && last) umma_commit(&qempty);
             }
             __syncwarp();
         };
         auto values = [&](int t, int i, int b, int mt) {
-            const uint32_t x = n_tile + i, sv = x % VS, c = (t ? tiles1 : tiles0) + i;
-            if (ok && t == 0 && b == 0) ok = wide_wait(&vfull[sv], (x / VS) & 1, dead, p.status);
+            const uint32_t x = n_tile + i, c = (t ? tiles1 : tiles0) + i;
+            if (ok && t == 0 && b == 0) ok = wide_wait(&vfull[x & 1], x >> 1 & 1, dead, p.status);
             if (ok) ok = wide_wait(&pfull[t][b], c & 1, dead, p.status);
             if (!ok) return;
             tc_fence_after();
             if (elect_one()) {
-                const uint64_t va = v_at + sv * (C::V_BYTES >> 4) + b * (HT * 128 >> 4);
+                // 64 values at a time: a tile's chunks need not lie one behind the other (2 x 33 cycles for 65)
 #pragma unroll
-                for (int k = 0; k < HT / 16; ++k)
-                    mma_ts(tmem + t * DV, tmem + C::S_COL + t * TOK + b * HT + k * 8, va + (2048 * k >> 4), id_o,
-                           i > 0 || b > 0 || k > 0);
+                for (int y = 0; y < C::VC; ++y) {
+                    const uint64_t va = v_at + C::slot(x, C::KC + y) * (C::CHUNK >> 4) + b * (HT * 128 >> 4);
+#pragma unroll
+                    for (int k = 0; k < HT / 16; ++k)
+                        mma_ts(tmem + t * DV + y * 64, tmem + C::S_COL + t * TOK + b * HT + k * 8, va + (2048 * k >> 4),
+                               id_o, i > 0 || b > 0 || k > 0);
+                }
                 umma_commit(&odone[t][b]);
-                if (t == mt - 1 && b == 1) umma_commit(&vempty[sv]);
+                if (t == mt - 1 && b == 1) umma_commit(&vempty[x & 1]);
             }
             __syncwarp();
         };

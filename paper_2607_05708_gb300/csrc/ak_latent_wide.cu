@@ -213,9 +213,10 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
         __syncwarp();
     } else if (warp == C::SOFT + 1) {
         // ---------------- issuing
-        const uint32_t id_s = idesc_f16(TOK, lp.bf16), id_o = idesc_f16(64, lp.bf16) | IDESC_B_MN_MAJOR;
+        const uint32_t id_s = idesc_f16(TOK, lp.bf16), id_o = idesc_f16(DV, lp.bf16) | IDESC_B_MN_MAJOR;
+        const uint32_t id_half = idesc_f16(64, lp.bf16) | IDESC_B_MN_MAJOR;
         const uint64_t q_at = desc64(desc_k(smem_u32(s_q))), k_at = desc64(desc_k(smem_u32(s_kv)));
-        const uint64_t v_at = desc64(desc_mn(smem_u32(s_kv), 0));
+        const uint64_t v_at = desc64(desc_mn(smem_u32(s_kv), C::CHUNK));
         const int rope_steps = lp.P / 16;
         uint32_t n_tile = 0, q_phase = 0, tiles0 = 0, tiles1 = 0;      // tiles: of the row tile, so far
         bool ok = true;
@@ -250,14 +251,22 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             if (!ok) return;
             tc_fence_after();
             if (elect_one()) {
-                // 64 values at a time: a tile's chunks need not lie one behind the other (2 x 33 cycles for 65)
-#pragma unroll
-                for (int y = 0; y < C::VC; ++y) {
-                    const uint64_t va = v_at + C::slot(x, C::KC + y) * (C::CHUNK >> 4) + b * (HT * 128 >> 4);
+                const uint32_t first = C::slot(x, C::KC);
+                const uint64_t va = v_at + first * (C::CHUNK >> 4) + b * (HT * 128 >> 4);
+                if (C::VC == 1 || C::slot(x, C::KC + 1) == first + 1) {
 #pragma unroll
                     for (int k = 0; k < HT / 16; ++k)
-                        mma_ts(tmem + t * DV + y * 64, tmem + C::S_COL + t * TOK + b * HT + k * 8, va + (2048 * k >> 4),
-                               id_o, i > 0 || b > 0 || k > 0);
+                        mma_ts(tmem + t * DV, tmem + C::S_COL + t * TOK + b * HT + k * 8, va + (2048 * k >> 4), id_o,
+                               i > 0 || b > 0 || k > 0);
+                } else {
+                    // the ring's end lies between the chunks: 64 values at a time
+                    const uint64_t vb = v_at + C::slot(x, C::KC + 1) * (C::CHUNK >> 4) + b * (HT * 128 >> 4);
+#pragma unroll
+                    for (int k = 0; k < HT / 16; ++k) {
+                        const uint32_t pa = tmem + C::S_COL + t * TOK + b * HT + k * 8;
+                        mma_ts(tmem + t * DV, pa, va + (2048 * k >> 4), id_half, i > 0 || b > 0 || k > 0);
+                        mma_ts(tmem + t * DV + 64, pa, vb + (2048 * k >> 4), id_half, i > 0 || b > 0 || k > 0);
+                    }
                 }
                 umma_commit(&odone[t][b]);
                 if (t == mt - 1 && b == 1) umma_commit(&vempty[x & 1]);
@@ -275,8 +284,8 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 scores(t, 0, mt, n == 1);
             }
             for (int i = 0; ok && i < n; ++i) {
-                for (int t = 0; t < mt; ++t) values(t, i, 0, mt);
                 for (int t = 0; t < mt; ++t) {
+                    values(t, i, 0, mt);
                     values(t, i, 1, mt);
                     if (i + 1 < n) scores(t, i + 1, mt, i + 2 == n);
                 }

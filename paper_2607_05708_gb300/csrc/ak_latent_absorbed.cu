@@ -173,6 +173,18 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 const uint32_t me = n_tile % C::METAS;
                 ok = wide_wait(&mfull[me], (n_tile / C::METAS) & 1, dead, p.status);
                 const int *rows = m_row[me];
+                // the rotated keys first: their place is free before the others'
+                const uint32_t sr = n_tile % C::ROPES;
+                if (ok) ok = wide_wait(&rope_empty[sr], ((n_tile / C::ROPES) & 1) ^ 1, dead, p.status);
+                if (!ok) break;
+                if (elect_one()) {
+                    mbar_expect_tx(&rope_full[sr], C::ROPE_BYTES);
+                    for (int b = 0; b < nb; ++b)
+                        tma_load_2d(s_rope + sr * C::ROPE_BYTES + b * box * 128, &rows_map, &rope_full[sr], R,
+                                    rows[b] < 0 ? n_rows : rows[b]);
+                }
+                __syncwarp();
+                ++n_rope;
                 for (int k = 0; ok && k < PAIRS; ++k, ++n_pair) {
                     const uint32_t st = n_pair % ST;
                     ok = wide_wait(&empty[st], ((n_pair / ST) & 1) ^ 1, dead, p.status);
@@ -193,17 +205,6 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                     }
                     __syncwarp();
                 }
-                const uint32_t sr = n_tile % C::ROPES;
-                if (ok) ok = wide_wait(&rope_empty[sr], ((n_tile / C::ROPES) & 1) ^ 1, dead, p.status);
-                if (!ok) break;
-                if (elect_one()) {
-                    mbar_expect_tx(&rope_full[sr], C::ROPE_BYTES);
-                    for (int b = 0; b < nb; ++b)
-                        tma_load_2d(s_rope + sr * C::ROPE_BYTES + b * box * 128, &rows_map, &rope_full[sr], R,
-                                    rows[b] < 0 ? n_rows : rows[b]);
-                }
-                __syncwarp();
-                ++n_rope;
             }
             left -= part.used;
             if (left > 0) attend_next(p, NR, TOK, C::EXTRA, 1, ALL, cur);
@@ -263,7 +264,17 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
             for (int i = 0; ok && i < part.n; ++i, ++t) {
                 const uint32_t d = tmem + C::S_COL + (t & 1) * NR, sr = t % C::ROPES;
                 if (t > 1) ok = wide_wait(&pfull[t & 1], (t - 2) >> 1 & 1, dead, p.status);
-                for (int k = 0; ok && k < PAIRS; ++k, ++x) {
+                if (ok) ok = wide_wait(&rope_full[sr], (t / C::ROPES) & 1, dead, p.status);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    for (int y = 0; y < rope_steps; ++y)
+                        mma_ss(d, r_at + sr * (C::ROPE_BYTES >> 4) + 2 * y, q_at + ((C::CHUNKS - 1) * NR * 128 >> 4) + 2 * y,
+                               id_s, y > 0);
+                    umma_commit(&rope_empty[sr]);
+                }
+                __syncwarp();
+                for (int k = 0; k < PAIRS; ++k, ++x) {
                     const uint32_t st = x % ST;
                     ok = wide_wait(&full[st], (x / ST) & 1, dead, p.status);
                     if (!ok) break;
@@ -273,22 +284,12 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
 #pragma unroll
                         for (int y = 0; y < 8; ++y)
                             mma_ss(d, ka + (y / 4) * (C::ROPE_BYTES >> 4) + 2 * (y % 4),
-                                   qa + (y / 4) * (NR * 128 >> 4) + 2 * (y % 4), id_s, k > 0 || y > 0);
+                                   qa + (y / 4) * (NR * 128 >> 4) + 2 * (y % 4), id_s, true);
+                        if (k == PAIRS - 1) umma_commit(&sfull[t & 1]);
+                        if (k == PAIRS - 1 && i == part.n - 1) umma_commit(&qempty);
                     }
                     __syncwarp();
                 }
-                if (ok) ok = wide_wait(&rope_full[sr], (t / C::ROPES) & 1, dead, p.status);
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
-                    for (int y = 0; y < rope_steps; ++y)
-                        mma_ss(d, r_at + sr * (C::ROPE_BYTES >> 4) + 2 * y, q_at + ((C::CHUNKS - 1) * NR * 128 >> 4) + 2 * y,
-                               id_s, true);
-                    umma_commit(&sfull[t & 1]);
-                    umma_commit(&rope_empty[sr]);
-                    if (i == part.n - 1) umma_commit(&qempty);
-                }
-                __syncwarp();
             }
             left -= part.used;
             if (left > 0) attend_next(p, NR, TOK, C::EXTRA, 1, ALL, cur);
@@ -379,6 +380,8 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
             named_bar(1, THR);
             if (!lp.q_map && lane == 0) mbar_arrive(&qfull);
             const int safe = attend_limit(p, sq, row_first / p.group) - TOK;
+            // heads of one query row have one tag: a token has it or not
+            const bool one_tag = row_first / p.group == (row_first + rows - 1) / p.group;
             float l[CW];
 #pragma unroll
             for (int c = 0; c < CW; ++c) l[c] = 0.f;
@@ -386,10 +389,11 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 const int tok = (mine.from + i) * TOK;
                 ok = ok && wide_wait(&mfull[n_tile % C::METAS], (n_tile / C::METAS) & 1, dead, p.status);
                 const int row = m_row[n_tile % C::METAS][key / box];
-                const bool have = row >= 0 && used;
+                bool have = row >= 0 && used;
                 int tag = -1;
                 if (tags && have) tag = max(-1, p.tags[(int64_t)row + key % box]);
-                const bool masked = __any_sync(0xffffffffu, used && !have) || tags || tok > safe;
+                if (tags && one_tag) have = have && tag == c_tag[0];
+                const bool masked = __any_sync(0xffffffffu, used && !have) || (tags && !one_tag) || tok > safe;
                 ok = ok && wide_wait(&sfull[n_tile & 1], n_tile >> 1 & 1, dead, p.status);
                 tc_fence_after();
                 uint32_t raw[CW];
@@ -407,7 +411,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                         x[c + 1] = j < lim.y ? x[c + 1] : -INFINITY;
                         x[c + 2] = j < lim.z ? x[c + 2] : -INFINITY;
                         x[c + 3] = j < lim.w ? x[c + 3] : -INFINITY;
-                        if (!tags) continue;
+                        if (!tags || one_tag) continue;
                         const int4 y = *(const int4 *)&c_tag[c0 + c];
                         x[c] = tag == y.x ? x[c] : -INFINITY;
                         x[c + 1] = tag == y.y ? x[c + 1] : -INFINITY;

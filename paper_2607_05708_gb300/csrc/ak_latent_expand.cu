@@ -21,7 +21,8 @@ struct Expand {
     static constexpr int W_BYTES = 256 * 128;            // 64 of R, of all rows of a head's weights
     static constexpr int STAGES = R == 512 ? 3 : 4;
     static constexpr int SMEM = 1024 + A_BYTES + STAGES * W_BYTES;
-    static constexpr int THREADS = 192;                  // four warps that write, copying, issuing
+    static constexpr int WRITE = 4;                      // warps that write
+    static constexpr int THREADS = 32 * (WRITE + 2);
 };
 
 // A share's place in the order (sequence, tile of 128 tokens, head).
@@ -44,7 +45,6 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
     unsigned char *smem = (unsigned char *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
     unsigned char *s_a = smem, *s_w = smem + C::A_BYTES;
     __shared__ uint64_t wfull[ST], wempty[ST], afull, aempty, tfull[2], tempty[2], drained;
-    __shared__ int64_t prefix[C::THREADS + 1];
     __shared__ uint32_t tmem_slot;
     __shared__ int dead_word;
     volatile int *dead = &dead_word;
@@ -52,7 +52,7 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
     griddep_wait();
     if (tid == 0) {
         for (int i = 0; i < ST; ++i) mbar_init(&wfull[i], 1), mbar_init(&wempty[i], 1);
-        for (int i = 0; i < 2; ++i) mbar_init(&tfull[i], 1), mbar_init(&tempty[i], 4);
+        for (int i = 0; i < 2; ++i) mbar_init(&tfull[i], 1), mbar_init(&tempty[i], C::WRITE);
         mbar_init(&afull, 1), mbar_init(&aempty, 1), mbar_init(&drained, 1);
         mbar_fence_init();
         dead_word = 0;
@@ -62,6 +62,7 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
         tmem_relinquish();
     }
     // ---- every CTA an equal share of all (tile, head): sums over runs of sequences
+    int64_t *prefix = (int64_t *)s_w;      // (until the weights come)
     const int nt = C::THREADS, run = (p.n_seq + nt - 1) / nt;
     {
         int64_t sum = 0;
@@ -81,10 +82,7 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
         prefix[tid] = before + incl - sum;
         if (tid == nt - 1) prefix[nt] = before + incl;
     }
-    tc_fence_before();
     __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = tmem_slot;
     const int64_t total = prefix[nt] * sp.heads, per = (total + gridDim.x - 1) / gridDim.x;
     const int64_t first = per * blockIdx.x;
     const int64_t left = max((int64_t)0, min(per, total - first));
@@ -101,6 +99,11 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
         while (rest >= (cur.tiles = expand_tiles(p, cur.seq))) rest -= cur.tiles, ++cur.seq;
         cur.tile = (int)rest;
     }
+    fence_async_smem();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
     auto next = [&](ExpandCursor &c) {         // true: another tile
         if (++c.head < sp.heads) return false;
         c.head = 0;
@@ -112,7 +115,7 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
     };
     const int rows_w = lp.nope + lp.value;
 
-    if (warp == 4) {
+    if (warp == C::WRITE) {
         // ---------------- copying
         const int nb = C::TOK / box, T = p.per_block * KV_UNIT;
         uint32_t n_tile = 0, n_w = 0;
@@ -155,7 +158,7 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
         for (uint32_t i = 0; !ok && i < ST; ++i)
             if (n_w > i) mbar_wait(&wfull[i], ((n_w - i - 1) / ST) & 1, p.status);
         __syncwarp();
-    } else if (warp == 5) {
+    } else if (warp == C::WRITE + 1) {
         // ---------------- issuing
         const uint32_t idesc = idesc_f16(rows_w, lp.bf16);
         const uint64_t a_at = desc64(desc_k(smem_u32(s_a))), w_at = desc64(desc_k(smem_u32(s_w)));

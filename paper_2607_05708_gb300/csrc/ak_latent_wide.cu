@@ -20,6 +20,8 @@ namespace ak {
 
 namespace {
 
+constexpr int MIXED = -3;
+
 template <int DN, int DV>
 struct WideLatent {
     static constexpr int ROWS = 256, TOK = 128, HALF = 64;
@@ -79,6 +81,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
     __shared__ uint64_t kfull[2], kempty[2], vfull[2], vempty[2], mfull[C::METAS];
     __shared__ uint64_t sfull[2], pfull[2][2], odone[2][2], qfull[2], qempty, drained;
     __shared__ alignas(16) int m_tag[C::METAS][TOK];
+    __shared__ alignas(16) int m_group[C::METAS][TOK / 16];    // the tag of 16 tokens, MIXED: several
     __shared__ uint32_t m_there[C::METAS]; // of a tile: a bit every 16 tokens that are listed
     __shared__ uint32_t tmem_slot;
     __shared__ int dead_word;
@@ -172,8 +175,17 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 if (n_tile > 1) ok = wide_wait(C::TWO ? &kempty[b] : &vempty[b], (n_tile - 2) >> 1 & 1, dead, p.status);
                 if (!ok) break;
                 const uint32_t there = __ballot_sync(0xffffffffu, row >= 0) & 255u;
-                if (tags)
-                    *(int4 *)&m_tag[me][4 * lane] = make_int4(max(tag.x, -1), max(tag.y, -1), max(tag.z, -1), max(tag.w, -1));
+                if (tags) {
+                    const int4 y = make_int4(max(tag.x, -1), max(tag.y, -1), max(tag.z, -1), max(tag.w, -1));
+                    *(int4 *)&m_tag[me][4 * lane] = y;
+                    int least = min(min(y.x, y.y), min(y.z, y.w)), most = max(max(y.x, y.y), max(y.z, y.w));
+#pragma unroll
+                    for (int o = 1; o < 4; o *= 2) {
+                        least = min(least, __shfl_xor_sync(0xffffffffu, least, o));
+                        most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+                    }
+                    if (lane % 4 == 0) m_group[me][lane / 4] = least == most ? least : MIXED;
+                }
                 if (lane == 0) m_there[me] = there;
                 __syncwarp();
                 if (lane == 0) {
@@ -364,14 +376,25 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                             const float2 y = f2_open(f2_mul(pair(k), f2_pack(f, f)));
                             x[k] = __float_as_uint(y.x), x[k + 1] = __float_as_uint(y.y);
                         }
-                        if (tags || tok > safe || bits != 15u) {
+                        // Tags 16 tokens at a time: documents and chunks are longer, so that a row sees all of
+                        // them or none (compared one by one a half took 2400 cycles, not 1100).
+                        bool masked = tok > safe || bits != 15u;
+                        int4 group = make_int4(0, 0, 0, 0);
+                        if (tags) {
+                            group = *(const int4 *)&m_group[me][4 * b];
+                            const bool all = group.x == group.y && group.y == group.z && group.z == group.w && group.x == qtag;
+                            masked = masked || !__all_sync(0xffffffffu, all || !real);
+                        }
+                        if (masked) {
 #pragma unroll
                             for (int u = 0; u < HT / 16; ++u) {
-                                const int end = bits >> u & 1u ? limit - tok - u * 16 : 0;
+                                const int of = u == 0 ? group.x : u == 1 ? group.y : u == 2 ? group.z : group.w;
+                                int end = bits >> u & 1u ? limit - tok - u * 16 : 0;
+                                if (tags && of != MIXED && of != qtag) end = 0;
 #pragma unroll
                                 for (int k = 0; k < 16; ++k)
                                     if (k >= end) x[u * 16 + k] = 0xff800000u;
-                                if (!tags) continue;
+                                if (!tags || of != MIXED) continue;
 #pragma unroll
                                 for (int k = 0; k < 16; k += 4) {
                                     const int4 y = *(const int4 *)&m_tag[me][b * HT + u * 16 + k];

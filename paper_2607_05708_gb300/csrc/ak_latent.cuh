@@ -72,6 +72,14 @@ __device__ __forceinline__ LatentShare latent_share(const AttendParams &p, int r
     __shared__ int have_found;
     const int nt = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     LatentShare r;
+    if (p.direct) {                            // a CTA an item: p.direct tiles a sequence
+        const int s = blockIdx.x / p.direct;
+        r.cur = {};
+        r.cur.seq = s, r.cur.tile = blockIdx.x - s * p.direct, r.cur.q = latent_seq(p, s);
+        r.cur.units = attend_units(p, r.cur.q, r.cur.tile, rows, step), r.cur.unit = -extra;
+        r.first = 0, r.left = r.cur.units + extra, r.per = r.left;
+        return r;
+    }
     AttendSeq q = {};
     int64_t sum = 0, before = 0;
     const bool one = p.n_seq <= nt;

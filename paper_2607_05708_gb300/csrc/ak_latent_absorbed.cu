@@ -131,7 +131,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
         mbar_init(&odone, 1), mbar_init(&qfull, lp.q_map ? 1 : C::SOFT), mbar_init(&qempty, 1), mbar_init(&drained[0], 1), mbar_init(&drained[1], 1);
         mbar_fence_init();
         dead_word = 0;
-        ((LatentJoin *)p.joins)[blockIdx.x] = {0, 0, 0};
+        if (!p.direct) ((LatentJoin *)p.joins)[blockIdx.x] = {0, 0, 0};
     }
     if (warp == 0) {
         tmem_alloc(&tmem_slot, 512);
@@ -568,11 +568,24 @@ cudaError_t run_absorbed_rows(const LatentParams &p, const CUtensorMap &map, con
                         : run_absorbed<R, 64>(p, map, pairs, q, box, n_rows, ctas, st);
 }
 
+int tile_tokens(const LatentParams &p) { return p.R == 512 ? 64 : 128; }
+
 // Rows of a tile, from the sequences' rows on average: a tile costs about the same whatever its
 // rows while bytes bound it, and fewer leave more room for tokens on their way.
 int tile_rows(const LatentParams &p) {
     const int64_t rows = ceil_div((int64_t)p.a.n_q, (int64_t)p.a.n_seq) * p.a.q_heads;
     return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+}
+
+// Short lists and no more items than SMs: a CTA an item, no scratch and no joining kernel.  (One request of 700
+// tokens, 16 heads, R = 256: six steps one after the other take as long as one step and the joining kernel, 12 us,
+// and the call a launch and an allocation less of the host, 21 -> 17 us.)
+constexpr int DIRECT_STEPS = 6;
+int direct_tiles(const LatentParams &p, int sms) {
+    if (p.a.q_start) return 0;
+    const int64_t tiles = ceil_div((int64_t)p.a.n_q / p.a.n_seq * p.a.q_heads, (int64_t)tile_rows(p));
+    const int steps = (int)ceil_div((int64_t)p.a.max_kv, (int64_t)tile_tokens(p));
+    return tiles * p.a.n_seq <= sms && steps <= DIRECT_STEPS ? (int)tiles : 0;
 }
 
 }  // namespace
@@ -581,6 +594,7 @@ int64_t latent_joins_bytes(int ctas) { return ceil_div((int64_t)ctas * 16, (int6
 
 int64_t latent_absorbed_scratch(const LatentParams &p) {
     const int ctas = device_sm_count();
+    if (direct_tiles(p, ctas)) return 0;
     return latent_joins_bytes(ctas) + (int64_t)ctas * 2 * attend_slot_floats(tile_rows(p), p.R) * 4;
 }
 
@@ -595,11 +609,15 @@ cudaError_t latent_rows_map(const LatentParams &p, int most, CUtensorMap *map) {
 }
 
 cudaError_t launch_latent_absorbed(LatentParams &p, void *scratch, cudaStream_t st) {
-    const int ctas = device_sm_count(), rows = tile_rows(p);
-    const int tok = p.R == 512 ? 64 : 128, box = latent_box(p, tok);
+    const int rows = tile_rows(p), tok = tile_tokens(p), box = latent_box(p, tok);
+    int ctas = device_sm_count();
+    p.a.direct = direct_tiles(p, ctas);
+    if (p.a.direct) ctas = p.a.direct * p.a.n_seq;
     const int n_rows = (int)(p.a.n_blocks * p.a.per_block * KV_UNIT);
-    p.a.joins = (int4 *)scratch;
-    p.a.partial = (float *)((unsigned char *)scratch + latent_joins_bytes(ctas));
+    if (!p.a.direct) {
+        p.a.joins = (int4 *)scratch;
+        p.a.partial = (float *)((unsigned char *)scratch + latent_joins_bytes(ctas));
+    }
     CUtensorMap map, pairs, q;
     cudaError_t e = latent_rows_map(p, tok, &map);
     if (e == cudaSuccess)
@@ -615,7 +633,7 @@ cudaError_t launch_latent_absorbed(LatentParams &p, void *scratch, cudaStream_t 
     e = p.R == 128   ? run_absorbed_rows<128>(p, map, pairs, q, box, n_rows, rows, ctas, st)
         : p.R == 256 ? run_absorbed_rows<256>(p, map, pairs, q, box, n_rows, rows, ctas, st)
                      : run_absorbed_rows<512>(p, map, pairs, q, box, n_rows, rows, ctas, st);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || p.a.direct) return e;
     return launch_latent_join(p, p.R, ctas, rows, 1, st);
 }
 

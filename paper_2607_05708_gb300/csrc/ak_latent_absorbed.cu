@@ -14,7 +14,7 @@
 //   issuing warp   scores of the next tile and O^T += of this one, whichever is ready
 //   softmax warps  a thread a token and up to 32 rows.  Weights are relative to a reference of the row, not
 //                  to its running maximum, and the reference is raised, O^T and the totals rescaled, only when a
-//                  weight would pass 2^15: maxima over tokens, which lie across the lanes, are then not
+//                  weight would pass 2^SLACK times that: maxima over tokens, which lie across the lanes, are then not
 //                  needed tile by tile.  P^T goes to shared memory, MN-major.
 // Tiles are shared out evenly over the CTAs (ak_attend.cuh); parts of an item are joined after it.
 #include <atomic>
@@ -26,14 +26,16 @@ namespace ak {
 
 namespace {
 
-#ifndef TOK_OF
-#define TOK_OF(R, NR) ((R) == 512 ? 64 : 128)
-#endif
+// Tokens of a tile.  At R = 512 two tiles of 128 have no room, and one and its successor's first chunks wait for
+// each other (16 heads over 200,000 tokens 67 us, with tiles of 64 62; 64 heads do not fit at all); at R = 256 tiles of 64 only
+// double the waits (44 and 48 us).
+constexpr int tokens_of(int R) { return R == 512 ? 64 : 128; }
+
 template <int R, int NR>
 struct Absorbed {
-    static constexpr int TOK = TOK_OF(R, NR);            // tokens of a tile
+    static constexpr int TOK = tokens_of(R);
     static constexpr int PAIRS = R / 128, CHUNKS = R / 64 + 1;
-    static constexpr int CW = 16;                         // rows of a softmax thread
+    static constexpr int CW = 16;                        // rows of a softmax thread
     static constexpr int SOFT = NR / CW * 4;             // softmax warps
     static constexpr int THREADS = 32 * (SOFT + 4);
     static constexpr int PAIR_BYTES = TOK * 256, ROPE_BYTES = TOK * 128;
@@ -53,8 +55,10 @@ struct Absorbed {
     static constexpr int EXTRA = 4;
 };
 
-// Weights are held between 2^-OFF of the reference's and 2^(OFF + SLACK): fp16 has room for both.
-constexpr float OFF = 7.f, SLACK = 8.f;
+// A weight is 2^off where its score is the one that set the row's reference, and 2^(off + SLACK) at most.  fp16 has room
+// for 2^15 and down to 2^-24; bf16's weights stay below 2^-8, so that values near the type's largest, which weigh 1 in
+// all, do not add up to infinities.
+constexpr float SLACK = 8.f;
 
 // Whether any thread of the barrier's has `x`, for all of them.
 __device__ __forceinline__ bool bar_any(int id, int threads, bool x) {
@@ -128,7 +132,8 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
         for (int i = 0; i < C::ROPES; ++i) mbar_init(&rope_full[i], 1), mbar_init(&rope_empty[i], 1);
         for (int i = 0; i < C::METAS; ++i) mbar_init(&mfull[i], 1), mbar_init(&mempty[i], 1);
         for (int i = 0; i < 2; ++i) mbar_init(&sfull[i], 1), mbar_init(&pfull[i], C::SOFT);
-        mbar_init(&odone, 1), mbar_init(&qfull, lp.q_map ? 1 : C::SOFT), mbar_init(&qempty, 1), mbar_init(&drained[0], 1), mbar_init(&drained[1], 1);
+        mbar_init(&odone, 1), mbar_init(&qfull, lp.q_map ? 1 : C::SOFT), mbar_init(&qempty, 1);
+        mbar_init(&drained[0], 1), mbar_init(&drained[1], 1);
         mbar_fence_init();
         dead_word = 0;
         if (!p.direct) ((LatentJoin *)p.joins)[blockIdx.x] = {0, 0, 0};
@@ -340,7 +345,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
         const int key = TOK == 128 ? dim : quad * 16 + (lane & 15);
         const bool used = TOK == 128 || lane < 16;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const float f = p.scale * LOG2E_F;
+        const float f = p.scale * LOG2E_F, off = lp.bf16 ? -16.f : 7.f;
         const bool tags = p.tags != nullptr;
         uint32_t n_tile = 0;
         // After a wait that gave up the warps wait for nothing more, but go on to the end: they meet at
@@ -388,7 +393,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
             for (int i = 0; i < n; ++i, ++n_tile) {
                 const int tok = (mine.from + i) * TOK;
                 ok = ok && wide_wait(&mfull[n_tile % C::METAS], (n_tile / C::METAS) & 1, dead, p.status);
-                const int row = m_row[n_tile % C::METAS][key / box];
+                const int row = ok ? m_row[n_tile % C::METAS][key / box] : -1;
                 bool have = row >= 0 && used;
                 int tag = -1;
                 if (tags && have) tag = max(-1, p.tags[(int64_t)row + key % box]);
@@ -430,7 +435,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                     most = fmaxf(fmaxf(most, x[c] - m.x), fmaxf(x[c + 1] - m.y, fmaxf(x[c + 2] - m.z, x[c + 3] - m.w)));
                 }
                 bool waited = false;           // for the products before
-                if (bar_any(2, THR, most > OFF + SLACK)) {
+                if (bar_any(2, THR, most > off + SLACK)) {
                     // ---- a row's reference is raised: its maximum over the tile's tokens
                     float v[CW];
 #pragma unroll
@@ -442,7 +447,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                         const float m = fmaxf(fmaxf(c_part[0][tid], c_part[1][tid]), fmaxf(c_part[2][tid], c_part[3][tid]));
                         const float was = c_ref[tid];
                         float now = was, fac = 1.f;
-                        if (m - was > OFF + SLACK) now = m - OFF, fac = was == NEG ? 0.f : ex2(was - now);
+                        if (m - was > off + SLACK) now = m - off, fac = was == NEG ? 0.f : ex2(was - now);
                         c_ref[tid] = now, c_fac[tid] = fac;
                     }
                     named_bar(1, THR);
@@ -544,8 +549,11 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
     if (warp == 0) tmem_dealloc(tmem, 512);
 }
 
+struct AbsorbedMaps {
+    CUtensorMap rows, pairs, q;        // boxes of 64 values, of 128, of a tile's query rows
+};
 template <int R, int NR>
-cudaError_t run_absorbed(const LatentParams &p, const CUtensorMap &map, const CUtensorMap &pairs, const CUtensorMap &q, int box, int n_rows, int ctas, cudaStream_t st) {
+cudaError_t run_absorbed(const LatentParams &p, const AbsorbedMaps &m, int box, int n_rows, int ctas, cudaStream_t st) {
     using C = Absorbed<R, NR>;
     auto *kernel = k_latent_absorbed<R, NR>;
     // once a device (the attribute stays; another thread that comes first does the same)
@@ -558,17 +566,15 @@ cudaError_t run_absorbed(const LatentParams &p, const CUtensorMap &map, const CU
         if (e != cudaSuccess) return e;
         if (dev < 64) ready[dev].store(true, std::memory_order_release);
     }
-    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, map, pairs, q, p, box, n_rows);
+    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, m.rows, m.pairs, m.q, p, box, n_rows);
 }
 template <int R>
-cudaError_t run_absorbed_rows(const LatentParams &p, const CUtensorMap &map, const CUtensorMap &pairs, const CUtensorMap &q, int box, int n_rows, int rows, int ctas,
+cudaError_t run_absorbed_rows(const LatentParams &p, const AbsorbedMaps &m, int box, int n_rows, int rows, int ctas,
                               cudaStream_t st) {
-    return rows == 16   ? run_absorbed<R, 16>(p, map, pairs, q, box, n_rows, ctas, st)
-           : rows == 32 ? run_absorbed<R, 32>(p, map, pairs, q, box, n_rows, ctas, st)
-                        : run_absorbed<R, 64>(p, map, pairs, q, box, n_rows, ctas, st);
+    return rows == 16   ? run_absorbed<R, 16>(p, m, box, n_rows, ctas, st)
+           : rows == 32 ? run_absorbed<R, 32>(p, m, box, n_rows, ctas, st)
+                        : run_absorbed<R, 64>(p, m, box, n_rows, ctas, st);
 }
-
-int tile_tokens(const LatentParams &p) { return p.R == 512 ? 64 : 128; }
 
 // Rows of a tile, from the sequences' rows on average: a tile costs about the same whatever its
 // rows while bytes bound it, and fewer leave more room for tokens on their way.
@@ -584,7 +590,7 @@ constexpr int DIRECT_STEPS = 6;
 int direct_tiles(const LatentParams &p, int sms) {
     if (p.a.q_start) return 0;
     const int64_t tiles = ceil_div((int64_t)p.a.n_q / p.a.n_seq * p.a.q_heads, (int64_t)tile_rows(p));
-    const int steps = (int)ceil_div((int64_t)p.a.max_kv, (int64_t)tile_tokens(p));
+    const int steps = (int)ceil_div((int64_t)p.a.max_kv, (int64_t)tokens_of(p.R));
     return tiles * p.a.n_seq <= sms && steps <= DIRECT_STEPS ? (int)tiles : 0;
 }
 
@@ -609,7 +615,7 @@ cudaError_t latent_rows_map(const LatentParams &p, int most, CUtensorMap *map) {
 }
 
 cudaError_t launch_latent_absorbed(LatentParams &p, void *scratch, cudaStream_t st) {
-    const int rows = tile_rows(p), tok = tile_tokens(p), box = latent_box(p, tok);
+    const int rows = tile_rows(p), tok = tokens_of(p.R), box = latent_box(p, tok);
     int ctas = device_sm_count();
     p.a.direct = direct_tiles(p, ctas);
     if (p.a.direct) ctas = p.a.direct * p.a.n_seq;
@@ -618,21 +624,20 @@ cudaError_t launch_latent_absorbed(LatentParams &p, void *scratch, cudaStream_t 
         p.a.joins = (int4 *)scratch;
         p.a.partial = (float *)((unsigned char *)scratch + latent_joins_bytes(ctas));
     }
-    CUtensorMap map, pairs, q;
-    cudaError_t e = latent_rows_map(p, tok, &map);
-    if (e == cudaSuccess)
-        e = make_tmap_cols(&pairs, p.a.cache, p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                           p.R, n_rows, (p.R + p.P) * 2, box, 2);
+    const CUtensorMapDataType type = p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    AbsorbedMaps m;
+    cudaError_t e = latent_rows_map(p, tok, &m.rows);
+    if (e == cudaSuccess) e = make_tmap_cols(&m.pairs, p.a.cache, type, p.R, n_rows, (p.R + p.P) * 2, box, 2);
+    if (e != cudaSuccess) return e;
     // rows of (row, head) evenly spaced
     p.q_map = p.a.q_wide && p.a.q_head > 0 && p.a.q_head < (1 << 30) && p.a.q_row == p.a.q_head * p.a.q_heads;
-    q = map;
-    if (e == cudaSuccess && p.q_map)
-        p.q_map = make_tmap_2d(&q, p.a.q, p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-                               p.R + p.P, (uint64_t)p.a.n_q * p.a.q_heads, p.a.q_head * 2, 64, rows) == cudaSuccess;
-    if (e != cudaSuccess) return e;
-    e = p.R == 128   ? run_absorbed_rows<128>(p, map, pairs, q, box, n_rows, rows, ctas, st)
-        : p.R == 256 ? run_absorbed_rows<256>(p, map, pairs, q, box, n_rows, rows, ctas, st)
-                     : run_absorbed_rows<512>(p, map, pairs, q, box, n_rows, rows, ctas, st);
+    m.q = m.rows;
+    if (p.q_map)
+        p.q_map = make_tmap_2d(&m.q, p.a.q, type, 2, p.R + p.P, (uint64_t)p.a.n_q * p.a.q_heads, p.a.q_head * 2, 64,
+                               rows) == cudaSuccess;
+    e = p.R == 128   ? run_absorbed_rows<128>(p, m, box, n_rows, rows, ctas, st)
+        : p.R == 256 ? run_absorbed_rows<256>(p, m, box, n_rows, rows, ctas, st)
+                     : run_absorbed_rows<512>(p, m, box, n_rows, rows, ctas, st);
     if (e != cudaSuccess || p.a.direct) return e;
     return launch_latent_join(p, p.R, ctas, rows, 1, st);
 }

@@ -9,7 +9,7 @@
 //   issuing warp   S = Q K^T into tensor memory, O += P V with P from there.  While one row tile's
 //                  scores are in the softmax, the tensor cores work on the other's
 //   softmax warps  a thread a row, 64 scores at a time: maximum, weights and total need no shuffle.  P replaces
-//                  its scores.  The maximum is raised, and O rescaled, only when a weight would pass 2^14
+//                  its scores.  The maximum is raised, and O rescaled, only when a weight would grow by 2^8
 // Tiles are shared out evenly over the CTAs (ak_attend.cuh); parts of an item are joined after it.
 #include <atomic>
 
@@ -317,6 +317,9 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t o_at = tmem + lanes + t * DV;
         const float f = p.scale * LOG2E_F;
+        // A weight is 2^shift where its score set the row's maximum, 2^(shift + M_SLACK) at most: within fp16's range; bf16's
+        // far below 1, so that values near the type's largest do not add up to infinities.
+        const float shift = lp.bf16 ? -16.f : P_SHIFT;
         uint32_t n_tile = 0, tiles = 0;        // tiles: of this row tile, so far
         bool ok = true;
         int64_t done = 0;
@@ -408,14 +411,14 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                         float top = __uint_as_float(x[0]);
 #pragma unroll
                         for (int k = 1; k < HT; ++k) top = fmaxf(top, __uint_as_float(x[k]));
-                        // the maximum is raised when a weight would pass 2^14
-                        const bool rises = unset ? top > -INFINITY : top - mm > P_SHIFT + M_SLACK;
+                        // the maximum is raised when a weight would pass 2^(shift + M_SLACK)
+                        const bool rises = unset ? top > -INFINITY : top - mm > shift + M_SLACK;
                         const bool moves = __any_sync(0xffffffffu, rises);         // O changes its scale
                         float down = 1.f;
                         if (rises) {
-                            down = unset ? 0.f : ex2(mm - (top - P_SHIFT));
+                            down = unset ? 0.f : ex2(mm - (top - shift));
                             unset = false;
-                            mm = top - P_SHIFT;
+                            mm = top - shift;
                         }
                         uint64_t sum[2] = {0, 0};
                         uint32_t pk[HT / 2];

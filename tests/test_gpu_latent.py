@@ -462,3 +462,127 @@ def test_tensors_that_are_refused():
             LatentCache(**{**dict(n_blocks=1, latent_dim=128, rope_dim=32), **bad})
     with pytest.raises(TypeError):
         LatentCache(1, 128, 32, dtype=torch.float32)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dt", ["bf16", "fp16"])
+def test_values_near_the_types_largest(form, dt):
+    """Equal values of the type's largest: their mean is that, however many there are."""
+    from paper_2607_05708_gb300 import LatentCache
+    n, R, P, H = 600, 128, 32, 3
+    c = LatentCache(10, R, P, dtype=DT[dt])
+    # the largest of which the expanded form's product with 1/2 and its sums stay in range
+    big = torch.finfo(DT[dt]).max if form == "absorbed" else torch.finfo(DT[dt]).max / 4
+    rows = torch.zeros(n, R + P, dtype=DT[dt])
+    rows[:, 1::2] = big
+    rows[:, R:] = torch.randn(n, P, generator=torch.Generator().manual_seed(0)).to(DT[dt])
+    c.append(rows[:, :R].cuda(), rows[:, R:].cuda(), torch.arange(n).cuda())
+    blocks = torch.arange(10).cuda()[None]
+    kv = torch.tensor([n], dtype=torch.int32).cuda()
+    if form == "absorbed":
+        q = torch.zeros(2, H, R + P, dtype=DT[dt])
+        q[..., R:] = 1.0
+        out, lse = c.attend(q.cuda(), blocks, 1.0, kv_len=kv)
+        assert torch.isfinite(lse).all()
+        want = rows[0, :R].double()
+    else:
+        q = torch.zeros(2, H, 64 + P, dtype=DT[dt])
+        q[..., 64:] = 1.0
+        w = torch.zeros(H, 128, R, dtype=DT[dt])
+        w[:, 64:, 1] = 0.5
+        out = c.attend_expanded(q.cuda(), w[:, :64].cuda(), w[:, 64:].cuda(), blocks, kv_len=kv)
+        want = torch.full((64,), float(rows[0, 1]) / 2, dtype=torch.float64)
+    c.sync()
+    # weights and the result are rounded by half a step each
+    assert ((out.double().cpu() - want).abs() <= 1.01 * torch.finfo(DT[dt]).eps * want.abs()).all()
+
+
+@pytest.mark.parametrize("heads,nq", [(3, 4), (16, 1), (40, 2), (64, 2)])
+@pytest.mark.parametrize("R", [256, 512])
+def test_short_lists_agree_with_long_ones(heads, nq, R):
+    """A call whose lists are short takes no scratch; the same sequences in wider lists do."""
+    c, call, want, x = problem(21, kv=[300, 1, 250, 64], nq=[nq] * 4, heads=heads, R=R, T=32, tags=2)
+    args = {k: v for k, v in x["args"].items() if k != "q_start"}
+    q, blocks = x["q"].cuda(), _gpu(x["blocks"])
+    compare(c.attend(q, blocks, x["scale"], **args), want)
+    wide = torch.full((4, 200), -1, dtype=torch.int64, device="cuda")
+    wide[:, :blocks.shape[1]] = blocks
+    compare(c.attend(q, wide, x["scale"], **args), want)
+    c.sync()
+
+
+@pytest.mark.parametrize("T", [16, 32, 48, 64, 80, 112, 128, 256, 4096])
+@pytest.mark.parametrize("form", FORMS)
+def test_block_sizes(T, form):
+    c, call, want, _ = problem(22, kv=[500, 70, T + 1 if T < 1000 else 3], nq=[3, 2, 1], heads=5, R=512, T=T, form=form,
+                               holes=T < 100)
+    got = call()
+    c.sync()
+    compare(got, want)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_infinite_and_nan_query_rows_stay_theirs(form):
+    """A row of NaN or infinities makes no other row's result other than it was."""
+    c, call, want, x = problem(23, kv=[400, 300], nq=[3, 140], heads=2, R=128, P=32, form=form)
+    first = (lambda g: g[0]) if form == "absorbed" else (lambda g: g)
+    good = first(call()).clone()
+    q = x["q"].clone()
+    q[1, 0, 5], q[2, 1, :] = float("nan"), float("inf")
+    q[77, 1, 3] = -float("inf")
+    if form == "absorbed":
+        out = c.attend(q.cuda(), _gpu(x["blocks"]), x["scale"], **x["args"])[0]
+    else:
+        rng = np.random.default_rng(23)
+        rng.permutation(len(x["rows"]) // 64), rng.standard_normal(x["rows"].shape), rng.standard_normal(x["q"].shape)
+        w, _ = _round(rng.standard_normal((2, 128, 128)) * 128 ** -0.5, "bf16")
+        out = c.attend_expanded(q.cuda(), w[:, :64].cuda(), w[:, 64:].cuda(), _gpu(x["blocks"]), **x["args"])
+    keep = torch.ones(143, 2, dtype=torch.bool)
+    keep[1, 0] = keep[2, 1] = keep[77, 1] = False
+    assert torch.equal(out[keep.cuda()], good[keep.cuda()])
+    assert torch.isnan(out[1, 0]).all()
+
+
+def test_heads_in_several_goes():
+    """Keys and values of all heads beyond what the scratch takes at a time."""
+    from paper_2607_05708_gb300 import LatentCache
+    g = torch.Generator("cuda").manual_seed(5)
+    H, T, S, width = 40, 64, 30, 160                     # 30 x 10240 tokens: 79 MB a head
+    c = LatentCache(64, 128, 32, block_tokens=T)
+    rows = torch.randn(64 * T, 160, device="cuda", generator=g).bfloat16()
+    c.append(rows[:, :128], rows[:, 128:], torch.arange(64 * T, device="cuda"))
+    blocks = torch.full((S, width), -1, dtype=torch.int64, device="cuda")
+    blocks[:, :3] = torch.randint(64, (S, 3), device="cuda", generator=g)
+    q = torch.randn(S, H, 96, device="cuda", generator=g).bfloat16()
+    w = (torch.randn(H, 128, 128, device="cuda", generator=g) / 11).bfloat16()
+    kv = torch.full((S,), 150, dtype=torch.int32, device="cuda")
+    out = c.attend_expanded(q, w[:, :64], w[:, 64:], blocks, kv_len=kv)
+    narrow = c.attend_expanded(q, w[:, :64], w[:, 64:], blocks[:, :3].contiguous(), kv_len=kv)
+    c.sync()
+    n_q, _, _ = q.shape
+    want = orc.attend(q.double().cpu().numpy(), rows.double().cpu().numpy(), blocks.cpu().numpy(), T, [150] * S,
+                      np.arange(S + 1), 96 ** -0.5, True, 128, w_k=w[:, :64].double().cpu().numpy(),
+                      w_v=w[:, 64:].double().cpu().numpy())
+    compare(out, want)
+    compare(narrow, want)
+
+
+def test_another_current_device_and_streams_in_turn():
+    """Calls on streams of their own that follow each other by events, without the host between."""
+    c, call, want, x = problem(24, kv=[900, 130], nq=[1, 2], heads=16, R=256)
+    q, blocks = x["q"].cuda(), _gpu(x["blocks"])
+    good = c.attend(q, blocks, x["scale"], **x["args"])[0].clone()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    rows = c.data.clone()
+    slots = torch.arange(len(rows), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(a):
+            c.data.zero_()
+            c.append(rows[:, :256], rows[:, 256:], slots)
+        b.wait_stream(a)
+        out = c.attend(q, blocks, x["scale"], stream=b, **x["args"])[0]
+        a.wait_stream(b)
+        b.synchronize()
+        assert torch.equal(out, good)

@@ -43,9 +43,8 @@ struct Absorbed {
     // P^T: a row a token; 64 bytes of it, in the 64-byte swizzle, hold 32 rows' weights
     static constexpr int P_ROW = NR > 32 ? 128 : 64, P_BYTES = TOK * P_ROW;
     static constexpr int ROOM = 232448 - 1024 - 5120 - Q_BYTES - P_BYTES;
-    static constexpr int fit(int ropes) { return (ROOM - ropes * ROPE_BYTES) / PAIR_BYTES; }
-    static constexpr int ROPES = fit(2) >= 2 * PAIRS ? 2 : 1;
-    static constexpr int STAGES = fit(ROPES) < 3 * PAIRS ? fit(ROPES) : 3 * PAIRS;
+    static constexpr int TILES = ROOM / (PAIRS * PAIR_BYTES + ROPE_BYTES);     // whole tiles on their way
+    static constexpr int ROPES = TILES < 1 ? 1 : TILES, STAGES = (ROOM - ROPES * ROPE_BYTES) / PAIR_BYTES;
     static_assert(STAGES > PAIRS, "a tile, and the next on its way");
     static constexpr int SMEM = 1024 + Q_BYTES + P_BYTES + ROPES * ROPE_BYTES + STAGES * PAIR_BYTES;
     static constexpr int S_COL = 256;                    // tensor memory: O^T, then two S^T

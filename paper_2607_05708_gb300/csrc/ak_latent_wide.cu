@@ -408,9 +408,16 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                                 }
                             }
                         }
-                        float top = __uint_as_float(x[0]);
+                        float tops[4];
 #pragma unroll
-                        for (int k = 1; k < HT; ++k) top = fmaxf(top, __uint_as_float(x[k]));
+                        for (int k = 0; k < 4; ++k) tops[k] = __uint_as_float(x[k]);
+#pragma unroll
+                        for (int k = 4; k < HT; k += 8)
+#pragma unroll
+                            for (int y = 0; y < 4; ++y)
+                                tops[y] = fmaxf(fmaxf(tops[y], __uint_as_float(x[k + y])),
+                                                k + 4 + y < HT ? __uint_as_float(x[k + 4 + y]) : -INFINITY);
+                        const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                         // the maximum is raised when a weight would pass 2^(shift + M_SLACK)
                         const bool rises = unset ? top > -INFINITY : top - mm > shift + M_SLACK;
                         const bool moves = __any_sync(0xffffffffu, rises);         // O changes its scale

@@ -17,6 +17,7 @@ constexpr int FEW_PARTS = 32;                  // of an item whose rows take a w
 template <int D>
 __global__ void __launch_bounds__(JOIN_THREADS)
 k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int rows, const int step) {
+    constexpr int RW = D < 128 ? 4 : 512 / D;  // rows of a warp where parts are few: four loads a lane are under way
     constexpr int WIDE = D < 128 ? D : 128, SLICES = D / WIDE, LANES = WIDE / 4, GROUPS = JOIN_THREADS / LANES;
     const AttendParams &p = lp.a;
     __shared__ int before[JOIN_CTAS + 1];      // rows, or runs of rows, of the items that begin in the CTAs before
@@ -30,7 +31,7 @@ k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int
     auto rows_of = [&](int b) {
         if (b >= ctas) return 0;
         const LatentJoin j = joins[b];
-        return j.last - b < FEW_PARTS ? (j.rows + JOIN_WARPS - 1) / JOIN_WARPS : j.rows * SLICES;
+        return j.last - b < FEW_PARTS ? (j.rows + JOIN_WARPS * RW - 1) / (JOIN_WARPS * RW) : j.rows * SLICES;
     };
     const int r0 = rows_of(2 * tid), r1 = rows_of(2 * tid + 1);
     int incl = r0 + r1;
@@ -59,42 +60,65 @@ k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int
         const float *base = p.partial + (int64_t)lo * 2 * floats;
         auto slot = [&](int k) { return base + (k ? (int64_t)k * 2 : 1) * floats; };
         if (parts <= FEW_PARTS) {
-            const int rw = at * JOIN_WARPS + warp;
-            if (rw >= j.rows) continue;
+            const int rw = (at * JOIN_WARPS + warp) * RW, n = min(RW, j.rows - rw);
+            if (n <= 0) continue;
             // lane: a part
-            const float m = lane < parts ? slot(lane)[rows * D + rw] : NEG;
-            const float l = lane < parts ? slot(lane)[rows * D + rows + rw] : 0.f;
-            float mx = m;
+            float f[RW], mx[RW], tot[RW];
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            const float f = lane < parts ? ex2(m - mx) * l : 0.f;
-            float tot = f;
+            for (int y = 0; y < RW; ++y) {
+                const bool have = lane < parts && y < n;
+                mx[y] = have ? slot(lane)[rows * D + rw + y] : NEG;
+                f[y] = have ? slot(lane)[rows * D + rows + rw + y] : 0.f;
+            }
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, o);
-            const float inv = tot > 0.f ? 1.f / tot : tot;     // a NaN stays one
+            for (int y = 0; y < RW; ++y) {
+                const float m = mx[y];
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], o));
+                f[y] = lane < parts ? ex2(m - mx[y]) * f[y] : 0.f;
+                tot[y] = f[y];
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) tot[y] += __shfl_xor_sync(0xffffffffu, tot[y], o);
+            }
             constexpr int STRIPS = D > 128 ? D / 128 : 1;
-            float4 v[STRIPS];
+            float4 v[RW][STRIPS];
 #pragma unroll
-            for (int i = 0; i < STRIPS; ++i) v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int y = 0; y < RW; ++y)
+#pragma unroll
+                for (int i = 0; i < STRIPS; ++i) v[y][i] = make_float4(0.f, 0.f, 0.f, 0.f);
             const bool mine = lane < D / 4;
-#pragma unroll 4
+#pragma unroll 2
             for (int k = 0; k < parts; ++k) {
-                const float fk = __shfl_sync(0xffffffffu, f, k);
                 const float *src = slot(k) + rw * D + lane * 4;
+                float4 x[RW][STRIPS];
 #pragma unroll
-                for (int i = 0; i < STRIPS; ++i) {
-                    const float4 y = mine ? *(const float4 *)(src + i * 128) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    v[i].x += fk * y.x, v[i].y += fk * y.y, v[i].z += fk * y.z, v[i].w += fk * y.w;
+                for (int y = 0; y < RW; ++y)
+#pragma unroll
+                    for (int i = 0; i < STRIPS; ++i)
+                        x[y][i] = mine && y < n ? *(const float4 *)(src + y * D + i * 128) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int y = 0; y < RW; ++y) {
+                    const float fk = __shfl_sync(0xffffffffu, f[y], k);
+#pragma unroll
+                    for (int i = 0; i < STRIPS; ++i) {
+                        v[y][i].x += fk * x[y][i].x, v[y][i].y += fk * x[y][i].y;
+                        v[y][i].z += fk * x[y][i].z, v[y][i].w += fk * x[y][i].w;
+                    }
                 }
             }
-            const int64_t dst = j.dst + (int64_t)rw * step;
 #pragma unroll
-            for (int i = 0; i < STRIPS; ++i)
-                if (mine) {
-                    store_pair(p, lp.bf16, dst * D + lane * 4 + i * 128, v[i].x * inv, v[i].y * inv);
-                    store_pair(p, lp.bf16, dst * D + lane * 4 + i * 128 + 2, v[i].z * inv, v[i].w * inv);
-                }
-            if (lane == 0 && p.lse) p.lse[dst] = lse_of(mx, tot);
+            for (int y = 0; y < RW; ++y) {
+                if (y >= n) continue;
+                const int64_t dst = j.dst + (int64_t)(rw + y) * step;
+                const float inv = tot[y] > 0.f ? 1.f / tot[y] : tot[y];        // a NaN stays one
+#pragma unroll
+                for (int i = 0; i < STRIPS; ++i)
+                    if (mine) {
+                        store_pair(p, lp.bf16, dst * D + lane * 4 + i * 128, v[y][i].x * inv, v[y][i].y * inv);
+                        store_pair(p, lp.bf16, dst * D + lane * 4 + i * 128 + 2, v[y][i].z * inv, v[y][i].w * inv);
+                    }
+                if (lane == 0 && p.lse) p.lse[dst] = lse_of(mx[y], tot[y]);
+            }
             continue;
         }
         // ---- the parts' weights

@@ -32,6 +32,13 @@ __device__ __forceinline__ void from_f32(float x, float &y) { y = x; }
 __device__ __forceinline__ void from_f32(float x, __half &y) { y = __float2half_rn(x); }
 __device__ __forceinline__ void from_f32(float x, __nv_bfloat16 &y) { y = __float2bfloat16_rn(x); }
 
+// Two adjacent values, 16-bit ones in one conversion.
+__device__ __forceinline__ void pair_from_f32(float a, float b, float *y) { y[0] = a, y[1] = b; }
+__device__ __forceinline__ void pair_from_f32(float a, float b, __half *y) { *(__half2 *)y = __floats2half2_rn(a, b); }
+__device__ __forceinline__ void pair_from_f32(float a, float b, __nv_bfloat16 *y) {
+    *(__nv_bfloat162 *)y = __floats2bfloat162_rn(a, b);
+}
+
 // N (8 or 16) consecutive values.
 template <int N, bool WIDE, typename T>
 __device__ __forceinline__ void load_run(const T *src, float *f) {
@@ -50,7 +57,7 @@ template <int N, bool WIDE, typename T>
 __device__ __forceinline__ void store_run(T *dst, const float *f) {
     alignas(16) T raw[N];
 #pragma unroll
-    for (int w = 0; w < N; ++w) from_f32(f[w], raw[w]);
+    for (int w = 0; w < N; w += 2) pair_from_f32(f[w], f[w + 1], raw + w);
     if constexpr (WIDE) {
 #pragma unroll
         for (int w = 0; w < (int)sizeof(raw) / 16; ++w) __stcs((int4 *)dst + w, ((const int4 *)raw)[w]);

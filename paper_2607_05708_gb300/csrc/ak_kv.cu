@@ -152,15 +152,17 @@ k_kv_write(unsigned char *__restrict__ cache, const T *__restrict__ k, const T *
                 const uint32_t total = (uint32_t)min((int64_t)tokens_q, n - i0) * turn.q_heads * G;
                 for (uint32_t x = threadIdx.x; x < total; x += 256) {
                     const uint32_t row = x / G, ti = row / (uint32_t)turn.q_heads, h = row - ti * turn.q_heads;
-                    const int64_t i = i0 + ti;
-                    int64_t pos = -1;
-                    if (kv_place(slots[i], 0, heads, units, per_block, status).unit >= 0 &&
-                        !rotate_at(turn, i, pos, status))
-                        pos = -1;
+                    const int64_t i = i0 + ti, slot = slots[i];
+                    int64_t pos = turn.positions[i];
                     const T *src = (const T *)turn.q + i * turn.q_row + h * turn.q_head;
                     T *dst = (T *)turn.q_out + i * turn.o_row + h * turn.o_head;
-                    if (turn.wide) rotate_query<true>(turn, src, dst, x % G, pos);
-                    else rotate_query<false>(turn, src, dst, x % G, pos);
+                    alignas(16) T raw[16];         // (on its way before the slot and the position are known)
+                    if (turn.wide) load_query<true>(turn, src, x % G, raw);
+                    else load_query<false>(turn, src, x % G, raw);
+                    if (kv_place(slot, 0, heads, units, per_block, status).unit < 0 || !rotate_at(turn, pos, status))
+                        pos = -1;
+                    if (turn.wide) store_query<true>(turn, raw, dst, x % G, pos);
+                    else store_query<false>(turn, raw, dst, x % G, pos);
                 }
             }
             return;
@@ -177,8 +179,10 @@ k_kv_write(unsigned char *__restrict__ cache, const T *__restrict__ k, const T *
             const int64_t i = i0 + ti, slot = x < total ? slots[i] : -1;
             KvPlace at = kv_place(slot, h, heads, units, per_block, status);
             int64_t pos = 0;
-            if constexpr (TURN)
-                if (at.unit >= 0 && !rotate_at(turn, i, pos, status)) at.unit = -1;
+            if constexpr (TURN) {
+                pos = x < total ? turn.positions[i] : 0;
+                if (at.unit >= 0 && !rotate_at(turn, pos, status)) at.unit = -1;
+            }
             float f[16];
 #pragma unroll
             for (int w = 0; w < 16; ++w) f[w] = 0.f;

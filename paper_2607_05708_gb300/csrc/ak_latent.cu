@@ -31,28 +31,42 @@ k_latent_append(S *__restrict__ cache, const T *__restrict__ latent, const T *__
         const int64_t i = total < 0x7fffffff ? (uint32_t)x / (uint32_t)per : x / per;
         const int u = (int)(x - i * per);
         const int64_t slot = slots[i];
+        const int64_t pos = turn.positions ? turn.positions[i] : 0;
+        const int y = u - R / 16;              // unit of the rotated part
+        alignas(16) T raw[16];                 // (on its way before the slot and the position are known)
+        if (query) {
+            const T *src = (const T *)turn.q + i * turn.q_row + u / (P / 16) * turn.q_head;
+            if (turn.wide) load_query<true>(turn, src, u % (P / 16), raw);
+            else load_query<false>(turn, src, u % (P / 16), raw);
+        } else if (y < 0) {
+            load_raw<16, WIDE>(latent + i * l_row + 16 * u, raw);
+        } else if (turn.positions) {
+            load_unit<WIDE>(turn, rope + i * r_row, y, raw);
+        } else {
+            load_raw<16, WIDE>(rope + i * r_row + 16 * y, raw);
+        }
         bool have = slot != -1;
         if (have && (slot < 0 || slot >= rows)) {
             set_status(status, AKASHIC_EDEVICE);
             have = false;
         }
-        int64_t pos = 0;
-        if (have && turn.positions) have = rotate_at(turn, i, pos, status);
         if (query) {
-            const int h = u / (P / 16);
-            const T *src = (const T *)turn.q + i * turn.q_row + h * turn.q_head;
-            T *dst = (T *)turn.q_out + i * turn.o_row + h * turn.o_head;
-            if (turn.wide) rotate_query<true>(turn, src, dst, u % (P / 16), have ? pos : -1);
-            else rotate_query<false>(turn, src, dst, u % (P / 16), have ? pos : -1);
+            if (have) have = rotate_at(turn, pos, status);
+            T *dst = (T *)turn.q_out + i * turn.o_row + u / (P / 16) * turn.o_head;
+            if (turn.wide) store_query<true>(turn, raw, dst, u % (P / 16), have ? pos : -1);
+            else store_query<false>(turn, raw, dst, u % (P / 16), have ? pos : -1);
             continue;
         }
+        if (have && turn.positions) have = rotate_at(turn, pos, status);
         if (!have) continue;
         S *dst = cache + slot * (R + P);
         float f[16];
-        const int y = u - R / 16;              // unit of the rotated part
-        if (y < 0) load_run<16, WIDE>(latent + i * l_row + 16 * u, f);
-        else if (turn.positions) turn_unit<WIDE>(turn, rope + i * r_row, y, pos, f);
-        else load_run<16, WIDE>(rope + i * r_row + 16 * y, f);
+        if (y >= 0 && turn.positions) {
+            turn_unit(turn, raw, y, pos, f);
+        } else {
+#pragma unroll
+            for (int w = 0; w < 16; ++w) f[w] = to_f32(raw[w]);
+        }
 #pragma unroll
         for (int w = 0; w < 16; ++w) f[w] = latent_finite<S>(f[w]);
         if (y >= 0 && turn.positions && !turn.pairs) {

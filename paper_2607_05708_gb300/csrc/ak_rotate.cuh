@@ -39,17 +39,22 @@ __device__ __forceinline__ void pair_from_f32(float a, float b, __nv_bfloat16 *y
     *(__nv_bfloat162 *)y = __floats2bfloat162_rn(a, b);
 }
 
-// N (8 or 16) consecutive values.
+// N (8 or 16) consecutive values, as they are: what is converted later keeps no instruction waiting
+// before the loads behind it.
 template <int N, bool WIDE, typename T>
-__device__ __forceinline__ void load_run(const T *src, float *f) {
-    alignas(16) T raw[N];
+__device__ __forceinline__ void load_raw(const T *src, T *raw) {
     if constexpr (WIDE) {
 #pragma unroll
-        for (int w = 0; w < (int)sizeof(raw) / 16; ++w) ((int4 *)raw)[w] = __ldcs((const int4 *)src + w);
+        for (int w = 0; w < N * (int)sizeof(T) / 16; ++w) ((int4 *)raw)[w] = __ldcs((const int4 *)src + w);
     } else {
 #pragma unroll
         for (int w = 0; w < N; ++w) raw[w] = src[w];
     }
+}
+template <int N, bool WIDE, typename T>
+__device__ __forceinline__ void load_run(const T *src, float *f) {
+    alignas(16) T raw[N];
+    load_raw<N, WIDE>(src, raw);
 #pragma unroll
     for (int w = 0; w < N; ++w) f[w] = to_f32(raw[w]);
 }
@@ -67,8 +72,7 @@ __device__ __forceinline__ void store_run(T *dst, const float *f) {
     }
 }
 // Whether a token's position is in the tables; one that is not is recorded.
-__device__ __forceinline__ bool rotate_at(const RotateArgs &a, int64_t i, int64_t &pos, int *status) {
-    pos = a.positions[i];
+__device__ __forceinline__ bool rotate_at(const RotateArgs &a, int64_t pos, int *status) {
     if (pos >= 0 && pos < a.table_rows) return true;
     set_status(status, AKASHIC_EDEVICE);
     return false;
@@ -90,22 +94,30 @@ __device__ __forceinline__ float turn_a(float a, float b, float c, float s) {
 __device__ __forceinline__ float turn_b(float a, float b, float c, float s) {
     return __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
 }
-// Pairs [8u, 8u + 8) of a row at src, turned; f as loaded: pairs side by side where
-// interleaved, else eight first members and eight second ones.
+// Pairs [8u, 8u + 8) of a row: side by side where interleaved, else eight first members and eight
+// second ones.
 template <bool WIDE, typename T>
-__device__ __forceinline__ void turn_unit(const RotateArgs &a, const T *src, int u, int64_t pos, float (&f)[16]) {
+__device__ __forceinline__ void load_unit(const RotateArgs &a, const T *src, int u, T *raw) {
+    if (a.pairs) {
+        load_raw<16, WIDE>(src + 16 * u, raw);
+    } else {
+        load_raw<8, WIDE>(src + 8 * u, raw);
+        load_raw<8, WIDE>(src + a.rotary / 2 + 8 * u, raw + 8);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void turn_unit(const RotateArgs &a, const T *raw, int u, int64_t pos, float (&f)[16]) {
     float c[8], s[8];
     rotate_table(a, pos, 8 * u, c, s);
+#pragma unroll
+    for (int w = 0; w < 16; ++w) f[w] = to_f32(raw[w]);
     if (a.pairs) {
-        load_run<16, WIDE>(src + 16 * u, f);
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
             const float x = f[2 * w], y = f[2 * w + 1];
             f[2 * w] = turn_a(x, y, c[w], s[w]), f[2 * w + 1] = turn_b(x, y, c[w], s[w]);
         }
     } else {
-        load_run<8, WIDE>(src + 8 * u, f);
-        load_run<8, WIDE>(src + a.rotary / 2 + 8 * u, f + 8);
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
             const float x = f[w], y = f[w + 8];
@@ -116,14 +128,22 @@ __device__ __forceinline__ void turn_unit(const RotateArgs &a, const T *src, int
 // Unit u (16 values) of a query row: turned, or, behind the rotated values, copied.
 // pos < 0: a row of no token, zeros.
 template <bool WIDE, typename T>
-__device__ __forceinline__ void rotate_query(const RotateArgs &a, const T *src, T *dst, int u, int64_t pos) {
+__device__ __forceinline__ void load_query(const RotateArgs &a, const T *src, int u, T *raw) {
+    if (16 * u < a.rotary) load_unit<WIDE>(a, src, u, raw);
+    else load_raw<16, WIDE>(src + 16 * u, raw);
+}
+template <bool WIDE, typename T>
+__device__ __forceinline__ void store_query(const RotateArgs &a, const T *raw, T *dst, int u, int64_t pos) {
     float f[16];
-#pragma unroll
-    for (int w = 0; w < 16; ++w) f[w] = 0.f;
     const bool turned = 16 * u < a.rotary;
-    if (pos >= 0) {
-        if (turned) turn_unit<WIDE>(a, src, u, pos, f);
-        else load_run<16, WIDE>(src + 16 * u, f);
+    if (pos < 0) {
+#pragma unroll
+        for (int w = 0; w < 16; ++w) f[w] = 0.f;
+    } else if (turned) {
+        turn_unit(a, raw, u, pos, f);
+    } else {
+#pragma unroll
+        for (int w = 0; w < 16; ++w) f[w] = to_f32(raw[w]);
     }
     if (turned && !a.pairs) {
         store_run<8, WIDE>(dst + 8 * u, f);
@@ -140,7 +160,9 @@ __device__ __forceinline__ void turn_group(const RotateArgs &a, const T *src, in
     if (d0 >= a.rotary) return;
     const int half = a.rotary / 2;
     if (a.pairs) {
-        turn_unit<WIDE>(a, src, d0 / 16, pos, f);
+        alignas(16) T raw[16];
+        load_unit<WIDE>(a, src, d0 / 16, raw);
+        turn_unit(a, raw, d0 / 16, pos, f);
         return;
     }
     const bool second = d0 >= half;

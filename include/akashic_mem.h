@@ -571,7 +571,8 @@ akashic_status_t akashic_mem_latent_append(const akashic_mem_latent_config_t *cf
 
 /* Arguments of both forms; fields named as in akashic_mem_kv_attend_t mean the same.  q and
  * out are of the cache's type.  Scores, maxima and totals are fp32; weights, and the expanded
- * form's keys and values, are rounded to the cache's type before their products. */
+ * form's keys and values, are rounded to the cache's type before their products (what is
+ * beyond its range to its largest value). */
 typedef struct {
     const void *q;             /* device; absorbed: rows of latent_dim + rope_dim, expanded:
                                   of nope_dim + rope_dim values                      */
@@ -599,7 +600,10 @@ typedef struct {
     int32_t value_dim;         /* rows of w_v: 64 or 128                             */
 } akashic_mem_latent_attend_t;
 
-/* Bytes of scratch of a call, as akashic_mem_kv_attend_scratch. */
+/* Bytes of scratch of a call, as akashic_mem_kv_attend_scratch.  The expanded form's holds keys
+ * and values of as many heads as fit 2 GB (of one, where that takes more), for n_seq *
+ * max_blocks * block_tokens tokens whatever the lengths are: give it lists no wider than the
+ * longest sequence's.  EINVAL where these tokens are 2^31 or more. */
 akashic_status_t akashic_mem_latent_attend_scratch(const akashic_mem_latent_config_t *cfg,
                                                    const akashic_mem_latent_attend_t *a,
                                                    int64_t *bytes);

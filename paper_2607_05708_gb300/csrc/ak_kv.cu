@@ -135,7 +135,12 @@ __device__ __forceinline__ void kv_codes(const float (&f)[16], float s, uint32_t
 }
 
 // TURN: keys are rotated to their positions on the way, in fp32, and the grid's third layer rotates
-// the query rows of the same tokens (`tokens_q` at a time).
+// the query rows of the same tokens (`tokens_q` at a time).  A thread reads its group and the group of the
+// other members of its pairs, which a second thread of the row reads too (L1): exchanging them between
+// lanes would tie the split to the rotated width.  Measured (8192 tokens, 8 heads, D = 128, 4 bits, bf16):
+// 23 us where writing alone takes 16, with 32 query heads 48 (178 MB: 3.7 TB/s); the layers one beside the
+// other instead of one after the other took the same time, and four heads a thread twice that.  A single
+// token with 32 query heads: 3 us.
 template <typename T, int BITS, int D, bool WIDE, bool TURN>
 __global__ void __launch_bounds__(256)
 k_kv_write(unsigned char *__restrict__ cache, const T *__restrict__ k, const T *__restrict__ v,

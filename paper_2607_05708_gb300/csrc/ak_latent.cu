@@ -1,8 +1,10 @@
 // The latent cache: rows of one latent vector and one rotated key a token rounded into their
 // slots, and the entry points of the attention that reads them.
 //
-// Appending is one pass over the rows, bound by memory: a thread 16 values (of the rotated
-// part eight pairs).
+// Appending is one pass over the rows, bound by memory: a thread 16 values (of the rotated part eight
+// pairs), the query rows of the same tokens in the grid's second layer.  Measured (bf16, R = 512, P = 64):
+// 16384 rows without a rotation 8.2 us (38 MB), with it 10.5, with 16 query heads 23 (109 MB: 4.7 TB/s);
+// 48 rows with 64 query heads 2.3 us.
 #include "ak_latent.cuh"
 #include "ak_rotate.cuh"
 
@@ -106,7 +108,8 @@ cudaError_t launch_append(const LatentRows &r, cudaStream_t st) {
 }
 template <typename T>
 cudaError_t launch_append_to(const LatentRows &r, cudaStream_t st) {
-    return r.cfg->dtype == AKASHIC_DTYPE_BF16 ? launch_append<T, __nv_bfloat16>(r, st) : launch_append<T, __half>(r, st);
+    return r.cfg->dtype == AKASHIC_DTYPE_BF16 ? launch_append<T, __nv_bfloat16>(r, st)
+                                              : launch_append<T, __half>(r, st);
 }
 
 akashic_status_t latent_check(const akashic_mem_latent_config_t *c, const char *who) {
@@ -150,7 +153,8 @@ akashic_status_t attend_check(const akashic_mem_latent_config_t *cfg, const akas
     for (auto &w : st)
         if (w[1] < cfg->latent_dim || w[1] % 8 || w[1] > (1 << 30) || w[0] < 0 || w[0] % w[1] ||
             w[0] / w[1] * (a->q_heads - 1) > 0x7fffffffLL - 256)
-            return kv_fail(AKASHIC_EINVAL, "%s: rows of w_k and w_v must be evenly spaced, by a multiple of 8 from latent_dim on", who);
+            return kv_fail(AKASHIC_EINVAL,
+                           "%s: rows of w_k and w_v must be evenly spaced, by a multiple of 8 from latent_dim on", who);
     return AKASHIC_OK;
 }
 
@@ -221,7 +225,8 @@ akashic_status_t attend_scratch(const akashic_mem_latent_config_t *cfg, const ak
     p.R = cfg->latent_dim, p.P = cfg->rope_dim;
     p.nope = a->nope_dim, p.value = a->value_dim;
     *bytes = a->n_seq == 0 || a->n_q == 0 ? 0 : expanded ? latent_expanded_scratch(p) : latent_absorbed_scratch(p);
-    if (*bytes < 0) return kv_fail(AKASHIC_EINVAL, "%s: sequences times the tokens of a list must be below 2^31", who);
+    if (*bytes < 0)
+        return kv_fail(AKASHIC_EINVAL, "%s: sequences times the tokens of a list must be below 2^31", who);
     return AKASHIC_OK;
 }
 

@@ -57,9 +57,9 @@ __device__ __forceinline__ AttendSeq latent_seq(const AttendParams &p, int s) {
     return q;
 }
 
-// attend_sums and attend_find in one where every thread has a sequence at most: the thread whose sequence has
-// the CTA's first step knows where (3500 cycles less at a kernel's beginning).  All threads call it; prefix: blockDim.x + 1
-// words of shared memory.  first, left: the CTA's share.
+// attend_sums and attend_find in one where every thread has a sequence at most: the thread whose sequence
+// has the CTA's first step knows where (3500 cycles less at a kernel's beginning).  All threads call it;
+// prefix: blockDim.x + 1 words of shared memory.  first, left: the CTA's share.
 struct LatentShare {
     AttendCursor cur;
     int64_t first, per;

@@ -1,22 +1,31 @@
 // Absorbed attention over the latent cache, on tcgen05.
 //
 // Every head reads the same rows [latent | rotated key], so a token's 2 (R + P) bytes meet
-// 2 H (2R + P) flops: bytes bound up to some 64 heads.  Rows of a tile are (query row, head)
-// pairs, 16, 32 or 64 of them; a step is 128 tokens.  The products are transposed,
-//   S^T = K Q^T      M = 128 tokens, N = rows, K = R + P
-//   O^T += C^T P^T   M = 128 latent dims at a time, N = rows, K = 128 tokens
+// 2 H (2R + P) flops: bytes bound it up to some 64 heads.  Rows of a tile are (query row, head) pairs,
+// 16, 32 or 64 of them; a step is 64 tokens at R = 512, else 128.  The products are transposed,
+//   S^T = K Q^T      M = tokens, N = rows, K = R + P
+//   O^T += C^T P^T   M = 128 latent dims at a time, N = rows, K = tokens
 // so that M is full whatever the number of heads, and the R x rows accumulators (4 x 64 columns of
 // 128 lanes at R = 512) leave tensor memory for two S.  One copy of a tile in shared memory serves both
 // products: as K it is K-major, as C^T the same bytes are MN-major.
 //   a warp ahead   looks up the tiles' blocks
-//   copying warp   the tile's boxes of tokens in pairs of 64-dim chunks; blocks that are not listed
-//                  read as zeros
-//   issuing warp   scores of the next tile and O^T += of this one, whichever is ready
-//   softmax warps  a thread a token and up to 32 rows.  Weights are relative to a reference of the row, not
-//                  to its running maximum, and the reference is raised, O^T and the totals rescaled, only when a
-//                  weight would pass 2^SLACK times that: maxima over tokens, which lie across the lanes, are then not
-//                  needed tile by tile.  P^T goes to shared memory, MN-major.
-// Tiles are shared out evenly over the CTAs (ak_attend.cuh); parts of an item are joined after it.
+//   copying warp   query rows, then the tiles' boxes of tokens: rotated keys, and the latent dims 128 at
+//                  a time; blocks that are not listed read as zeros
+//   issuing warps  one the scores of the next tile, one O^T += of this one: one warp for both waited for
+//                  the softmax of one tile while the next one's scores could have been under way
+//   softmax warps  a thread a token and 16 rows.  Weights are relative to a reference of the row, not to its
+//                  running maximum, and the reference is raised, O^T and the totals rescaled, only when a
+//                  weight would pass 2^SLACK times that: maxima over tokens, which lie across the lanes, are
+//                  then not needed tile by tile.  P^T goes to shared memory, MN-major.
+// Tiles are shared out evenly over the CTAs (ak_attend.cuh); parts of an item are joined after it
+// (ak_latent_join.cu).
+//
+// Measured (the GPU's time, with the join; R = 512, bf16): 64 requests of up to 8192 tokens, 32 heads, 73 us
+// (337 MB: 50 at a copy's rate); 64 heads over 200,000 tokens 63 us (231 MB: 34); 5 drafted rows of 16
+// requests, 40 heads, 71 us.  The kernel alone takes 68, 59 and 70 us under the profiler, DRAM 64 and 50 %
+// busy in the first two, the tensor pipe 18 and 30 %.  A step of 64 rows takes 2.6 to 3.5 thousand cycles
+// (its products 2000, its bytes 3200 at DRAM's rate with all SMs); a beginning takes 5000, the first pass
+// through cold instructions 10000, another item 5000, the join 9 to 12 us.
 #include <atomic>
 
 #include "ak_latent.cuh"
@@ -26,9 +35,9 @@ namespace ak {
 
 namespace {
 
-// Tokens of a tile.  At R = 512 two tiles of 128 have no room, and one and its successor's first chunks wait for
-// each other (16 heads over 200,000 tokens 67 us, with tiles of 64 62; 64 heads do not fit at all); at R = 256 tiles of 64 only
-// double the waits (44 and 48 us).
+// Tokens of a tile.  At R = 512 two tiles of 128 have no room, and one and its successor's first chunks
+// wait for each other (16 heads over 200,000 tokens 67 us, with tiles of 64 62; 64 heads do not fit at
+// all); at R = 256 tiles of 64 only double the waits (44 us with tiles of 128, 48 with 64).
 constexpr int tokens_of(int R) { return R == 512 ? 64 : 128; }
 
 template <int R, int NR>
@@ -50,13 +59,15 @@ struct Absorbed {
     static constexpr int S_COL = 256;                    // tensor memory: O^T, then two S^T
     static_assert(PAIRS * NR <= S_COL && S_COL + 2 * NR <= 512, "tensor memory");
     static constexpr int METAS = STAGES / PAIRS + 2;     // tiles whose places are known
-    // An item's beginning and end (rows in, result out, an empty pipeline) count as steps.
+    // An item's beginning and end (rows in, result out, an empty pipeline) count as steps.  (2, 4, 7 of
+    // them: 5 drafted rows of 16 requests 108, 103, 104 us, 64 requests of 32 heads 91, 89, 89, when measured.)
     static constexpr int EXTRA = 4;
 };
 
-// A weight is 2^off where its score is the one that set the row's reference, and 2^(off + SLACK) at most.  fp16 has room
-// for 2^15 and down to 2^-24; bf16's weights stay below 2^-8, so that values near the type's largest, which weigh 1 in
-// all, do not add up to infinities.
+// A weight is 2^off where its score is the one that set the row's reference, and 2^(off + SLACK) at
+// most.  fp16 has room for 2^15 and down to 2^-24; bf16's weights stay below 2^-8, so that values near the
+// type's largest, which weigh 1 in all, do not add up to infinities.  Weights are rounded to the cache's
+// type because a product's operands have one type; totals add up the unrounded ones.
 constexpr float SLACK = 8.f;
 
 // Whether any thread of the barrier's has `x`, for all of them.
@@ -273,8 +284,8 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 tc_fence_after();
                 if (elect_one()) {
                     for (int y = 0; y < rope_steps; ++y)
-                        mma_ss(d, r_at + sr * (C::ROPE_BYTES >> 4) + 2 * y, q_at + ((C::CHUNKS - 1) * NR * 128 >> 4) + 2 * y,
-                               id_s, y > 0);
+                        mma_ss(d, r_at + sr * (C::ROPE_BYTES >> 4) + 2 * y,
+                               q_at + ((C::CHUNKS - 1) * NR * 128 >> 4) + 2 * y, id_s, y > 0);
                     umma_commit(&rope_empty[sr]);
                 }
                 __syncwarp();
@@ -443,7 +454,8 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                     if (lane < CW) c_part[quad][c0 + lane] = top;
                     named_bar(1, THR);
                     if (tid < NR) {
-                        const float m = fmaxf(fmaxf(c_part[0][tid], c_part[1][tid]), fmaxf(c_part[2][tid], c_part[3][tid]));
+                        const float m = fmaxf(fmaxf(c_part[0][tid], c_part[1][tid]),
+                                              fmaxf(c_part[2][tid], c_part[3][tid]));
                         const float was = c_ref[tid];
                         float now = was, fac = 1.f;
                         if (m - was > off + SLACK) now = m - off, fac = was == NEG ? 0.f : ex2(was - now);
@@ -515,7 +527,8 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
                 if (!whole) part[NR * R + tid] = c_ref[tid], part[NR * R + NR + tid] = tot;
                 else if (tid < rows && p.lse) p.lse[dst + tid] = lse_of(c_ref[tid], tot);
                 if (!whole && tid == 0 && mine.from == 0)
-                    ((LatentJoin *)p.joins)[blockIdx.x] = {dst, rows, (int)((first + done - cur.unit + cur.units - 1) / per)};
+                    ((LatentJoin *)p.joins)[blockIdx.x] = {dst, rows,
+                                                           (int)((first + done - cur.unit + cur.units - 1) / per)};
             }
             named_bar(1, THR);
             float inv[CW];
@@ -575,16 +588,16 @@ cudaError_t run_absorbed_rows(const LatentParams &p, const AbsorbedMaps &m, int 
                         : run_absorbed<R, 64>(p, m, box, n_rows, ctas, st);
 }
 
-// Rows of a tile, from the sequences' rows on average: a tile costs about the same whatever its
-// rows while bytes bound it, and fewer leave more room for tokens on their way.
+// Rows of a tile, from the sequences' rows on average: a tile costs about the same whatever its rows
+// while bytes bound it, and fewer leave more room for tokens on their way.
 int tile_rows(const LatentParams &p) {
     const int64_t rows = ceil_div((int64_t)p.a.n_q, (int64_t)p.a.n_seq) * p.a.q_heads;
     return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
 
-// Short lists and no more items than SMs: a CTA an item, no scratch and no joining kernel.  (One request of 700
-// tokens, 16 heads, R = 256: six steps one after the other take as long as one step and the joining kernel, 12 us,
-// and the call a launch and an allocation less of the host, 21 -> 17 us.)
+// Short lists and no more items than SMs: a CTA an item, no scratch and no joining kernel.  (One request
+// of 700 tokens, 16 heads, R = 256: six steps one after the other take the GPU as long as one step and the
+// joining kernel, 14 us, and the host a launch and an allocation less: the call 21 -> 14 us.)
 constexpr int DIRECT_STEPS = 6;
 int direct_tiles(const LatentParams &p, int sms) {
     if (p.a.q_start) return 0;

@@ -3,8 +3,9 @@
 // Of a row's first `rotary` values pair i, (x[i], x[i + rotary / 2]) or, interleaved,
 // (x[2i], x[2i + 1]), becomes (a c - b s, b c + a s) with c and s from the tables' row of the
 // token's position: fp32, both products and the sum rounded (no fused multiply-add, so that
-// the stored codes are defined to the bit).  A thread turns 16 values: eight whole pairs, so that
-// query rows can be turned in place.
+// the stored codes are defined to the bit; two pairs an instruction were faster and came out fused).
+// A thread turns 16 values: eight whole pairs, so that query rows can be turned in place.  Tables come
+// from L1: the heads of a token share a row of them.
 #pragma once
 
 #include <cuda_fp16.h>

@@ -110,8 +110,8 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
         : "memory");
 }
-// High words of descriptors: 128-byte swizzle (DESC_HI), and 64-byte swizzle: atoms of 8 K-rows x 32 values along N, 512
-// bytes, one after the other along K (MN-major).
+// High words of descriptors: 128-byte swizzle (DESC_HI), and 64-byte swizzle: atoms of 8 K-rows x 32
+// values along N, 512 bytes, one after the other along K (MN-major).
 constexpr uint32_t DESC_HI_64 = (512u >> 4) | (1u << 14) | (4u << 29);
 __device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi = DESC_HI) { return (uint64_t)hi << 32 | lo; }
 // Low words of the descriptors of K-major and MN-major tiles.

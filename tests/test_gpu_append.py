@@ -129,7 +129,6 @@ def test_bad_positions_and_slots_are_reported_and_skipped():
     for bad_slot, bad_pos in ((5, 10), (5, -1), (5, 1 << 40), (48, 3), (-2, 3), (1 << 34, 3)):
         c = KVCache(3, 2, 64, block_tokens=16, tagged=True)
         c.write(torch.zeros_like(k).cuda().expand(3, 2, 64), torch.zeros_like(k).cuda(), _gpu(np.array([4, 5, 6])))
-        before = c.data.clone()
         slots, pos = np.array([4, bad_slot, 6]), np.array([1, bad_pos, 2])
         out = c.append(k.cuda(), k.cuda(), _gpu(slots), _gpu(pos), _gpu(cos), _gpu(sin), q=k.cuda(),
                        tags=_gpu(np.array([7, 8, 9], np.int32)))
@@ -139,7 +138,6 @@ def test_bad_positions_and_slots_are_reported_and_skipped():
         assert torch.equal(out.cpu(), want)
         rk, _ = c.read(_gpu(np.array([4, 5, 6])), dtype=torch.float32)
         assert (rk[1] == 0).all() and (rk[0] != 0).any() and c.tags[5] == 0 and c.tags[4] == 7
-        assert len(before) == len(c.data)
         m = LatentCache(3, 128, 64, block_tokens=16, tagged=True)
         lat = _rand(rng, (3, 128), "bf16")
         out = m.append(lat.cuda(), k[:, 0].cuda(), _gpu(slots), _gpu(pos), _gpu(cos), _gpu(sin), q=k.cuda(),

@@ -567,7 +567,7 @@ def test_heads_in_several_goes():
     compare(narrow, want)
 
 
-def test_another_current_device_and_streams_in_turn():
+def test_streams_in_turn():
     """Calls on streams of their own that follow each other by events, without the host between."""
     c, call, want, x = problem(24, kv=[900, 130], nq=[1, 2], heads=16, R=256)
     q, blocks = x["q"].cuda(), _gpu(x["blocks"])

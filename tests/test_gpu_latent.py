@@ -567,6 +567,35 @@ def test_heads_in_several_goes():
     compare(narrow, want)
 
 
+@pytest.mark.parametrize("R,dt,S,width,H", [(512, "bf16", 4, 256, 2), (256, "fp16", 5, 100, 13),
+                                            (512, "fp16", 200, 8, 1), (256, "bf16", 1, 900, 3)])
+def test_wide_lists(R, dt, S, width, H):
+    """Lists far wider than the contexts: where keys and values are made by pairs of CTAs; an odd number
+    of tiles, more sequences than threads, sequences without tokens."""
+    from paper_2607_05708_gb300 import LatentCache
+    rng = np.random.default_rng(S)
+    T, P, N, V = 64, 64, 128, 128
+    kv = rng.integers(0, 300, S)
+    kv[0], kv[S // 2] = 130 if sum(-(-n // 128) for n in kv[1:]) % 2 else 300, 0 if S > 1 else 300
+    need = -(-kv // T)
+    n_blocks = max(int(need.max()), 6)
+    blocks = np.full((S, width), -1, np.int64)
+    for i, m in enumerate(need):
+        blocks[i, :m] = rng.permutation(n_blocks)[:m]
+    rows, rows64 = _round(rng.standard_normal((n_blocks * T, R + P)), dt)
+    c = LatentCache(n_blocks, R, P, block_tokens=T, dtype=DT[dt])
+    c.append(rows[:, :R].cuda(), rows[:, R:].cuda(), torch.arange(n_blocks * T).cuda())
+    q, q64 = _round(rng.standard_normal((S, H, N + P)), dt)
+    w, w64 = _round(rng.standard_normal((H, N + V, R)) * R ** -0.5, dt)
+    w = w.cuda()
+    out = [c.attend_expanded(q.cuda(), w[:, :N], w[:, N:], _gpu(blocks), kv_len=_gpu(kv.astype(np.int32)))
+           for _ in range(3)]
+    c.sync()
+    assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
+    compare(out[0], orc.attend(q64, rows64, blocks, T, kv, np.arange(S + 1), (N + P) ** -0.5, dt == "bf16", R,
+                               w_k=w64[:, :N], w_v=w64[:, N:]))
+
+
 def test_streams_in_turn():
     """Calls on streams of their own that follow each other by events, without the host between."""
     c, call, want, x = problem(24, kv=[900, 130], nq=[1, 2], heads=16, R=256)

@@ -65,8 +65,9 @@ struct LatentShare {
     int64_t first, per;
     int left;
 };
+// ctas: that have one together.
 __device__ __forceinline__ LatentShare latent_share(const AttendParams &p, int rows, int step, int extra,
-                                                    int64_t *prefix) {
+                                                    int64_t *prefix, int ctas = 1) {
     constexpr int ALL = 0x7fffffff;
     __shared__ AttendCursor found;
     __shared__ int have_found;
@@ -105,9 +106,9 @@ __device__ __forceinline__ LatentShare latent_share(const AttendParams &p, int r
     } else {
         attend_sums(p, rows, step, extra, 1, ALL, prefix);
     }
-    const int64_t total = prefix[nt], g = gridDim.x;
+    const int64_t total = prefix[nt], g = gridDim.x / ctas;
     r.per = total + g < 0x7fffffff ? max(1u, ((uint32_t)total + (uint32_t)g - 1u) / (uint32_t)g) : (total + g - 1) / g;
-    r.first = r.per * blockIdx.x;
+    r.first = r.per * (blockIdx.x / ctas);
     r.left = (int)max((int64_t)0, min(r.per, total - r.first));
     r.cur = {};
     if (r.left <= 0) return r;                 // (the whole CTA)
@@ -151,6 +152,32 @@ struct LatentSpace {
     int64_t k_step, v_step;           // rows of w_k and w_v from one head to the next
     int head0, heads;
 };
+
+// Pairs of CTAs: how many fit on the GPU at a time, and a launch of so many.
+template <typename K>
+cudaError_t pairs_that_fit(K *kernel, int threads, size_t smem, int *pairs) {
+    cudaLaunchAttribute at = {};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = 2, at.val.clusterDim.y = 1, at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(device_sm_count() & ~1)), cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem, cfg.attrs = &at, cfg.numAttrs = 1;
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(pairs, kernel, &cfg);
+    return e != cudaSuccess ? e : *pairs < 1 ? cudaErrorLaunchOutOfResources : cudaSuccess;
+}
+template <typename K, typename... Args>
+cudaError_t launch_pairs(K *kernel, int pairs, int threads, size_t smem, cudaStream_t st, const Args &...args) {
+    cudaLaunchAttribute at[2] = {};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;       // see griddep_wait
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 2, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * pairs), cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem, cfg.stream = st, cfg.attrs = at, cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    return e == cudaSuccess ? cudaGetLastError() : e;
+}
 
 // Scratch of the joins, the tokens of a box of the copies from the cache (boxes do not cross blocks), and
 // the cache's tensor map: boxes of 64 values of at most

@@ -308,13 +308,6 @@ template <int R, bool PAIR>
 cudaError_t run_expand(const LatentParams &p, const LatentSpace &sp, cudaStream_t st) {
     using C = Expand<R, PAIR>;
     auto *kernel = k_latent_expand<R, PAIR>;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;       // see griddep_wait
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = C::CTAS, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(C::THREADS), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = st;
     // the CTAs or pairs that fit on the GPU, once a device (another thread that comes first finds the same)
     static std::atomic<int> fit[64];
     int dev = 0;
@@ -325,15 +318,10 @@ cudaError_t run_expand(const LatentParams &p, const LatentSpace &sp, cudaStream_
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
         if (e != cudaSuccess) return e;
         shares = device_sm_count();
-        if (PAIR) {
-            cfg.gridDim = dim3((unsigned)(shares & ~1)), cfg.attrs = at + 1, cfg.numAttrs = 1;
-            e = cudaOccupancyMaxActiveClusters(&shares, kernel, &cfg);
-            if (e != cudaSuccess) return e;
-        }
-        if (shares < 1) return cudaErrorLaunchOutOfResources;
+        if (PAIR) e = pairs_that_fit(kernel, C::THREADS, C::SMEM, &shares);
+        if (e != cudaSuccess) return e;
         if (dev < 64) fit[dev].store(shares, std::memory_order_release);
     }
-    cfg.gridDim = dim3(C::CTAS * shares), cfg.attrs = at, cfg.numAttrs = PAIR ? 2 : 1;
     const CUtensorMapDataType type = p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     CUtensorMap rows, k, v;
     e = latent_rows_map(p, 128, &rows);
@@ -343,9 +331,9 @@ cudaError_t run_expand(const LatentParams &p, const LatentSpace &sp, cudaStream_
     if (e == cudaSuccess)
         e = make_tmap_2d(&v, p.w_v, type, 2, R, sp.v_step * heads + p.value, p.v_row * 2, 64, p.value);
     if (e != cudaSuccess) return e;
-    e = cudaLaunchKernelEx(&cfg, kernel, rows, k, v, p, sp, latent_box(p, 128),
-                           (int)(p.a.n_blocks * p.a.per_block * KV_UNIT));
-    return e == cudaSuccess ? cudaGetLastError() : e;
+    const int box = latent_box(p, 128), n_rows = (int)(p.a.n_blocks * p.a.per_block * KV_UNIT);
+    if constexpr (PAIR) return launch_pairs(kernel, shares, C::THREADS, C::SMEM, st, rows, k, v, p, sp, box, n_rows);
+    else return launch_pdl(kernel, dim3(shares), dim3(C::THREADS), C::SMEM, st, rows, k, v, p, sp, box, n_rows);
 }
 // Pairs where weights are widest and a CTA has PAIR_TILES products or more (by the lists' widths; lengths only the
 // device knows).  Whole calls of 64 rows with pairs and without, us, by products a CTA: R = 512, 128 + 128 dims, 1:

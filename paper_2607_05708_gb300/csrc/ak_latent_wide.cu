@@ -32,22 +32,38 @@ namespace {
 
 constexpr int MIXED = -3;
 
-template <int DN, int DV>
+// PAIR: clusters of two CTAs share an item of twice the rows.  Each has two row tiles of its own, the keys
+// of half a tile's tokens and half the dims of its values; the first one's products (cta_group::2) read both
+// halves, so that a product of scores reads 6 KB of a CTA's shared memory where it read 8.
+template <int DN, int DV, bool PAIR>
 struct WideLatent {
-    static constexpr int ROWS = 256, TOK = 128, HALF = 64;
+    static constexpr int CTAS = PAIR ? 2 : 1;
+    static constexpr int TILE_ROWS = 128 * CTAS, ROWS = 2 * TILE_ROWS, TOK = 128, HALF = 64;
     static constexpr int CHUNK = TOK * 128;              // 64 values of 128 rows
     static constexpr int KC = DN / 64 + 1, VC = DV / 64; // chunks of a key, of a value
-    static constexpr int K_BYTES = KC * CHUNK, V_BYTES = VC * CHUNK, Q_BYTES = 2 * K_BYTES;
+    static constexpr int Q_TILE = KC * CHUNK, Q_BYTES = 2 * Q_TILE;
+    static constexpr int K_ROWS = TOK / CTAS, K_CHUNK = K_ROWS * 128;    // of a CTA
+    static constexpr int K_BYTES = KC * K_CHUNK, V_BYTES = VC * CHUNK / CTAS;
     // Keys and values in one ring of chunks, tile by tile.  Two tiles where there is room; else (DN = DV = 128) eight
     // chunks of a tile's five: keys then wait for the values of the tile before the last, values for the scores of
     // the last, which are both over long before.  (Values in a buffer of their own waited for the
     // products with the ones before them: a step of 256 rows and 128 tokens 5000 cycles.)
+    // Pairs have room for three tiles.
     static constexpr int TILE = KC + VC, SLOTS = Q_BYTES / CHUNK + 2 * TILE <= 14 ? 2 * TILE : 14 - Q_BYTES / CHUNK;
     static constexpr bool TWO = SLOTS == 2 * TILE;
-    static_assert(TWO || (KC == 3 && VC == 2 && SLOTS == 8), "what waits for what");
+    static_assert(PAIR || TWO || (KC == 3 && VC == 2 && SLOTS == 8), "what waits for what");
+    static_assert(!PAIR || V_BYTES == CHUNK, "half the dims of a value are one chunk");
+    static constexpr int DEEP = PAIR ? 3 : 2;            // tiles on their way
     __device__ static uint32_t slot(uint32_t tile, int chunk) { return (tile * TILE + chunk) % SLOTS; }
+    // where a tile's chunk stands: of its keys, of its values
+    __device__ static uint32_t key_at(uint32_t tile, int c) {
+        return PAIR ? tile % DEEP * (K_BYTES + V_BYTES) + c * K_CHUNK : slot(tile, c) * CHUNK;
+    }
+    __device__ static uint32_t value_at(uint32_t tile, int c) {
+        return PAIR ? tile % DEEP * (K_BYTES + V_BYTES) + K_BYTES : slot(tile, KC + c) * CHUNK;
+    }
     static constexpr int METAS = 3;                      // tiles whose tags are kept
-    static constexpr int SMEM = 1024 + Q_BYTES + SLOTS * CHUNK;
+    static constexpr int SMEM = 1024 + Q_BYTES + (PAIR ? DEEP * (K_BYTES + V_BYTES) : SLOTS * CHUNK);
     static constexpr int SOFT = 8, THREADS = 32 * (SOFT + 2);
     static constexpr int S_COL = 2 * DV;                 // tensor memory: O, then S
     static_assert(S_COL + 2 * TOK <= 512, "tensor memory");
@@ -76,19 +92,19 @@ __device__ __forceinline__ void store_row32h(const LatentParams &lp, int64_t at,
     }
 }
 
-template <int DN, int DV>
-__global__ void __launch_bounds__(WideLatent<DN, DV>::THREADS, 1)
+template <int DN, int DV, bool PAIR>
+__global__ void __launch_bounds__(WideLatent<DN, DV, PAIR>::THREADS, 1)
 k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap k_map,
               const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap q_map,
               const __grid_constant__ LatentParams lp, const __grid_constant__ LatentSpace sp, const int box,
               const int n_rows) {
-    using C = WideLatent<DN, DV>;
-    constexpr int TOK = C::TOK, ROWS = C::ROWS, HT = C::HALF;
+    using C = WideLatent<DN, DV, PAIR>;
+    constexpr int TOK = C::TOK, ROWS = C::ROWS, HT = C::HALF, ND = C::DEEP;
     const AttendParams &p = lp.a;          // (heads: those of the group; its first is sp.head0)
     extern __shared__ unsigned char raw_smem[];
     unsigned char *smem = (unsigned char *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
     unsigned char *s_q = smem, *s_kv = smem + C::Q_BYTES;
-    __shared__ uint64_t kfull[2], kempty[2], vfull[2], vempty[2], mfull[C::METAS];
+    __shared__ uint64_t kfull[ND], kempty[ND], vfull[ND], vempty[ND], mfull[C::METAS];
     __shared__ uint64_t sfull[2], pfull[2][2], odone[2][2], qfull[2], qempty, drained;
     __shared__ alignas(16) int m_tag[C::METAS][TOK];
     __shared__ alignas(16) int m_group[C::METAS][TOK / 16];    // the tag of 16 tokens, MIXED: several
@@ -97,10 +113,12 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
     __shared__ int dead_word;
     volatile int *dead = &dead_word;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t rank = PAIR ? cluster_ctarank() : 0u, share_at = blockIdx.x / C::CTAS;
+    const bool lead = rank == 0;               // issues the products
 
     griddep_wait();
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < ND; ++i) {
             mbar_init(&kfull[i], 1), mbar_init(&kempty[i], 1);
             mbar_init(&vfull[i], 1), mbar_init(&vempty[i], 1);
         }
@@ -108,33 +126,44 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
         for (int t = 0; t < 2; ++t) {
             // One a half: two may be under way, and a wait knows only the last phase from the one
             // before it.
-            for (int b = 0; b < 2; ++b) mbar_init(&pfull[t][b], 4), mbar_init(&odone[t][b], 1);
+            for (int b = 0; b < 2; ++b) mbar_init(&pfull[t][b], 4 * C::CTAS), mbar_init(&odone[t][b], 1);
             mbar_init(&sfull[t], 1), mbar_init(&qfull[t], lp.q_map ? 1 : 4);
         }
         mbar_init(&qempty, 1), mbar_init(&drained, 1);
         mbar_fence_init();
         dead_word = 0;
-        ((LatentJoin *)p.joins)[blockIdx.x] = {0, 0, 0};
+        if (lead) ((LatentJoin *)p.joins)[share_at] = {0, 0, 0};
     }
     if (warp == 0) {
-        tmem_alloc(&tmem_slot, 512);
-        tmem_relinquish();
+        if constexpr (PAIR) {
+            tmem_alloc2(&tmem_slot, 512);
+            tmem_relinquish2();
+        } else {
+            tmem_alloc(&tmem_slot, 512);
+            tmem_relinquish();
+        }
     }
     constexpr int ALL = 0x7fffffff;
-    const LatentShare share = latent_share(p, ROWS, TOK, C::EXTRA, (int64_t *)s_q);    // (until it holds query rows)
+    const LatentShare share = latent_share(p, ROWS, TOK, C::EXTRA, (int64_t *)s_q, C::CTAS);   // (until s_q holds query rows)
     const int64_t first = share.first, per = share.per;
     int left = share.left;
     AttendCursor cur = share.cur;
     fence_async_smem();                    // (copies write where the plan stood)
     tc_fence_before();
     __syncthreads();
+    if constexpr (PAIR) cluster_sync();        // the other CTA's barriers are there
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
     const bool tags = p.tags != nullptr;
+    // a copy whose end the issuing CTA's barrier tells
+    auto load = [&](unsigned char *to, const CUtensorMap *map, uint64_t *bar, int x, int y) {
+        if (lead) tma_load_2d(to, map, bar, x, y);
+        else tma_load_2d_pair(to, map, bar, 0, x, y);
+    };
 
     if (warp == C::SOFT) {
         // ---------------- copying
-        const int nb = TOK / box, T = p.per_block * KV_UNIT;
+        const int nb = C::K_ROWS / box, T = p.per_block * KV_UNIT;
         uint32_t n_tile = 0, n_k = 0, n_v = 0, items = 0, q_tiles[2] = {0, 0};
         bool ok = true;
         while (left > 0 && ok) {
@@ -147,13 +176,16 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 const int rows = cur.q.nq - cur.tile * ROWS;
                 ok = wide_wait(&qempty, (items++ & 1) ^ 1, dead, p.status);
                 if (!ok) break;
-                for (int t = 0; t < (rows > 128 ? 2 : 1); ++t, __syncwarp()) {
+                for (int t = 0; t < (rows > C::TILE_ROWS ? 2 : 1); ++t, __syncwarp()) {
                     ++q_tiles[t];
                     if (!elect_one()) continue;
-                    mbar_expect_tx(&qfull[t], C::K_BYTES);
-                    for (int c = 0; c < C::KC; ++c)
-                        tma_load_3d(s_q + t * C::K_BYTES + c * C::CHUNK, &q_map, &qfull[t], c * 64,
-                                    cur.q.row0 + cur.tile * ROWS + t * 128, sp.head0 + cur.head);
+                    const int y = cur.q.row0 + cur.tile * ROWS + t * C::TILE_ROWS + (int)rank * 128;
+                    if (lead) mbar_expect_tx(&qfull[t], C::CTAS * C::Q_TILE);
+                    for (int c = 0; c < C::KC; ++c) {
+                        unsigned char *to = s_q + t * C::Q_TILE + c * C::CHUNK;
+                        if (lead) tma_load_3d(to, &q_map, &qfull[t], c * 64, y, sp.head0 + cur.head);
+                        else tma_load_3d_pair(to, &q_map, &qfull[t], 0, c * 64, y, sp.head0 + cur.head);
+                    }
                 }
             }
             const int64_t *list = p.blocks + cur.seq * p.max_blocks;
@@ -179,10 +211,11 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 const int row = next, tok = (first_tile + i) * TOK;
                 const int4 tag = next_tags;
                 next = place(i + 1);
-                const uint32_t b = n_tile & 1, me = n_tile % C::METAS;
+                const uint32_t b = n_tile % ND, me = n_tile % C::METAS;
                 // (a tile's meta goes where that of the third before it was: its weights came before the scores of
                 // the tile after it, which came before the weights, and so the values, of the second before this)
-                if (n_tile > 1) ok = wide_wait(C::TWO ? &kempty[b] : &vempty[b], (n_tile - 2) >> 1 & 1, dead, p.status);
+                if (n_tile >= ND)
+                    ok = wide_wait(C::TWO && !PAIR ? &kempty[b] : &vempty[b], (n_tile / ND - 1) & 1, dead, p.status);
                 if (!ok) break;
                 const uint32_t there = __ballot_sync(0xffffffffu, row >= 0) & 255u;
                 if (tags) {
@@ -200,90 +233,111 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(&mfull[me]);
-                    mbar_expect_tx(&kfull[b], C::K_BYTES);
+                    if (lead) mbar_expect_tx(&kfull[b], C::CTAS * C::K_BYTES);
                 }
                 // the sequence's rows in the scratch end with its tiles: behind them zeros
                 const int y = tok < max(cur.q.kv, 1) ? (int)(at + tok) : (int)sp.rows;
-                const int box_row = __shfl_sync(0xffffffffu, row, lane % nb * (box / 16));
+                const int box_row = __shfl_sync(0xffffffffu, row, (int)rank * (C::K_ROWS / 16) + lane % nb * (box / 16));
                 __syncwarp();
-                auto chunk = [&](int c) { return s_kv + C::slot(n_tile, c) * C::CHUNK; };
                 if (lane < nb)
-                    tma_load_2d(chunk(C::KC - 1) + lane * box * 128, &rows_map, &kfull[b], lp.R,
-                                box_row < 0 ? n_rows : box_row);
+                    load(s_kv + C::key_at(n_tile, C::KC - 1) + lane * box * 128, &rows_map, &kfull[b], lp.R,
+                         box_row < 0 ? n_rows : box_row);
                 else if (lane >= 16 && lane < 16 + C::KC - 1)
-                    tma_load_2d(chunk(lane - 16), &k_map, &kfull[b], (lane - 16) * 64, y);
+                    load(s_kv + C::key_at(n_tile, lane - 16), &k_map, &kfull[b], (lane - 16) * 64,
+                         y + (int)rank * C::K_ROWS);
                 ++n_k;
                 next_tags = tags_of(next);
-                if (C::TWO && n_tile > 1) ok = wide_wait(&vempty[b], (n_tile - 2) >> 1 & 1, dead, p.status);
-                if (!C::TWO && n_tile > 0) ok = wide_wait(&kempty[b ^ 1], (n_tile - 1) >> 1 & 1, dead, p.status);
+                if (!PAIR && C::TWO && n_tile > 1) ok = wide_wait(&vempty[b], (n_tile - 2) >> 1 & 1, dead, p.status);
+                if (!PAIR && !C::TWO && n_tile > 0)
+                    ok = wide_wait(&kempty[b ^ 1], (n_tile - 1) >> 1 & 1, dead, p.status);
                 if (!ok) break;
-                if (lane == 0) mbar_expect_tx(&vfull[b], C::V_BYTES);
+                if (lead && lane == 0) mbar_expect_tx(&vfull[b], C::CTAS * C::V_BYTES);
                 __syncwarp();
-                if (lane < C::VC) tma_load_2d(chunk(C::KC + lane), &v_map, &vfull[b], lane * 64, y);
+                if (lane < C::VC / C::CTAS)
+                    load(s_kv + C::value_at(n_tile, lane), &v_map, &vfull[b], lane * 64 + (int)rank * (DV / 2), y);
                 ++n_v;
             }
             left -= part.used;
             if (left > 0) attend_next(p, ROWS, TOK, C::EXTRA, 1, ALL, cur);
         }
-        // nothing is on its way when the CTA ends (where a wait gave up; else all has been read)
-        for (int t = 0; !ok && t < 2; ++t)
+        // nothing is on its way when the CTA ends (where a wait gave up; else all has been read); what the
+        // other CTA's barriers tell of is given time instead
+        for (int t = 0; !ok && lead && t < 2; ++t)
             if (q_tiles[t]) mbar_wait(&qfull[t], (q_tiles[t] - 1) & 1, p.status);
-        for (uint32_t i = 0; !ok && i < 2; ++i) {
-            if (n_k > i) mbar_wait(&kfull[(n_k - i - 1) & 1], (n_k - i - 1) >> 1 & 1, p.status);
-            if (n_v > i) mbar_wait(&vfull[(n_v - i - 1) & 1], (n_v - i - 1) >> 1 & 1, p.status);
+        for (uint32_t i = 0; !ok && lead && i < ND; ++i) {
+            if (n_k > i) mbar_wait(&kfull[(n_k - i - 1) % ND], (n_k - i - 1) / ND & 1, p.status);
+            if (n_v > i) mbar_wait(&vfull[(n_v - i - 1) % ND], (n_v - i - 1) / ND & 1, p.status);
         }
+        for (int i = 0; !ok && !lead && i < 200; ++i) __nanosleep(1000);
         __syncwarp();
+    } else if (PAIR && warp == C::SOFT + 1 && !lead) {
+        // (the other CTA issues the pair's products)
     } else if (warp == C::SOFT + 1) {
         // ---------------- issuing
-        const uint32_t id_s = idesc_f16(TOK, lp.bf16), id_o = idesc_f16(DV, lp.bf16) | IDESC_B_MN_MAJOR;
+        const uint32_t id_s = idesc_f16(TOK, lp.bf16, C::TILE_ROWS);
+        const uint32_t id_o = idesc_f16(DV, lp.bf16, C::TILE_ROWS) | IDESC_B_MN_MAJOR;
         const uint32_t id_half = idesc_f16(64, lp.bf16) | IDESC_B_MN_MAJOR;
         const uint64_t q_at = desc64(desc_k(smem_u32(s_q))), k_at = desc64(desc_k(smem_u32(s_kv)));
         const uint64_t v_at = desc64(desc_mn(smem_u32(s_kv), C::CHUNK));
         const int rope_steps = lp.P / 16;
         uint32_t n_tile = 0, q_phase = 0, tiles0 = 0, tiles1 = 0;      // tiles: of the row tile, so far
         bool ok = true;
+        auto commit = [&](uint64_t *bar) {
+            if constexpr (PAIR) {
+                umma2_commit(bar);
+                umma2_commit_to(bar, 1);
+            } else {
+                umma_commit(bar);
+            }
+        };
+        auto product = [&](uint32_t d, uint64_t a, uint64_t b, bool add) {
+            if constexpr (PAIR) umma2_bf16(d, a, b, id_s, add);
+            else mma_ss(d, a, b, id_s, add);
+        };
         // S of the item's tile i for row tile t; the row tiles share a tile's keys
         auto scores = [&](int t, int i, int mt, bool last) {
             const uint32_t x = n_tile + i;
-            if (ok && t == 0) ok = wide_wait(&kfull[x & 1], x >> 1 & 1, dead, p.status);
+            if (ok && t == 0) ok = wide_wait(&kfull[x % ND], x / ND & 1, dead, p.status);
             if (!ok) return;
             tc_fence_after();
             if (elect_one()) {
                 const uint32_t d = tmem + C::S_COL + t * TOK;
-                const uint64_t qa = q_at + t * (C::K_BYTES >> 4);
+                const uint64_t qa = q_at + t * (C::Q_TILE >> 4);
 #pragma unroll
                 for (int c = 0; c < C::KC - 1; ++c) {
-                    const uint64_t ka = k_at + C::slot(x, c) * (C::CHUNK >> 4);
+                    const uint64_t ka = k_at + (C::key_at(x, c) >> 4);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        mma_ss(d, qa + c * (C::CHUNK >> 4) + 2 * k, ka + 2 * k, id_s, c > 0 || k > 0);
+                        product(d, qa + c * (C::CHUNK >> 4) + 2 * k, ka + 2 * k, c > 0 || k > 0);
                 }
-                const uint64_t ka = k_at + C::slot(x, C::KC - 1) * (C::CHUNK >> 4);
+                const uint64_t ka = k_at + (C::key_at(x, C::KC - 1) >> 4);
                 for (int k = 0; k < rope_steps; ++k)
-                    mma_ss(d, qa + (C::KC - 1) * (C::CHUNK >> 4) + 2 * k, ka + 2 * k, id_s, true);
-                umma_commit(&sfull[t]);
-                if (t == mt - 1) umma_commit(&kempty[x & 1]);
-                if (t == mt - 1 && last) umma_commit(&qempty);
+                    product(d, qa + (C::KC - 1) * (C::CHUNK >> 4) + 2 * k, ka + 2 * k, true);
+                commit(&sfull[t]);
+                if (!PAIR && t == mt - 1) umma_commit(&kempty[x & 1]);
+                if (t == mt - 1 && last) commit(&qempty);
             }
             __syncwarp();
         };
         auto values = [&](int t, int i, int b, int mt) {
             const uint32_t x = n_tile + i, c = (t ? tiles1 : tiles0) + i;
-            if (ok && t == 0 && b == 0) ok = wide_wait(&vfull[x & 1], x >> 1 & 1, dead, p.status);
+            if (ok && t == 0 && b == 0) ok = wide_wait(&vfull[x % ND], x / ND & 1, dead, p.status);
             if (ok) ok = wide_wait(&pfull[t][b], c & 1, dead, p.status);
             if (!ok) return;
             tc_fence_after();
             if (elect_one()) {
-                const uint32_t first = C::slot(x, C::KC);
-                const uint64_t va = v_at + first * (C::CHUNK >> 4) + b * (HT * 128 >> 4);
-                if (C::VC == 1 || C::slot(x, C::KC + 1) == first + 1) {
+                const uint64_t va = v_at + (C::value_at(x, 0) >> 4) + b * (HT * 128 >> 4);
+                if (PAIR || C::VC == 1 || C::value_at(x, 1) == C::value_at(x, 0) + C::CHUNK) {
 #pragma unroll
-                    for (int k = 0; k < HT / 16; ++k)
-                        mma_ts(tmem + t * DV, tmem + C::S_COL + t * TOK + b * HT + k * 8, va + (2048 * k >> 4), id_o,
-                               i > 0 || b > 0 || k > 0);
+                    for (int k = 0; k < HT / 16; ++k) {
+                        const uint32_t pa = tmem + C::S_COL + t * TOK + b * HT + k * 8;
+                        const bool add = i > 0 || b > 0 || k > 0;
+                        if constexpr (PAIR) mma2_ts(tmem + t * DV, pa, va + (2048 * k >> 4), id_o, add);
+                        else mma_ts(tmem + t * DV, pa, va + (2048 * k >> 4), id_o, add);
+                    }
                 } else {
                     // the ring's end lies between the chunks: 64 values at a time
-                    const uint64_t vb = v_at + C::slot(x, C::KC + 1) * (C::CHUNK >> 4) + b * (HT * 128 >> 4);
+                    const uint64_t vb = v_at + (C::value_at(x, 1) >> 4) + b * (HT * 128 >> 4);
 #pragma unroll
                     for (int k = 0; k < HT / 16; ++k) {
                         const uint32_t pa = tmem + C::S_COL + t * TOK + b * HT + k * 8;
@@ -291,8 +345,8 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                         mma_ts(tmem + t * DV + 64, pa, vb + (2048 * k >> 4), id_half, i > 0 || b > 0 || k > 0);
                     }
                 }
-                umma_commit(&odone[t][b]);
-                if (t == mt - 1 && b == 1) umma_commit(&vempty[x & 1]);
+                commit(&odone[t][b]);
+                if (t == mt - 1 && b == 1) commit(&vempty[x % ND]);
             }
             __syncwarp();
         };
@@ -300,7 +354,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             const AttendPart part = attend_part(cur, left);
             const int n = part.n;
             if (n <= 0) break;
-            const int mt = cur.q.nq * p.group - cur.tile * ROWS > 128 ? 2 : 1;
+            const int mt = cur.q.nq * p.group - cur.tile * ROWS > C::TILE_ROWS ? 2 : 1;
             for (int t = 0; t < mt; ++t) {
                 if (ok) ok = wide_wait(&qfull[t], q_phase >> t & 1, dead, p.status);
                 q_phase ^= 1u << t;
@@ -319,7 +373,10 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             left -= part.used;
             if (left > 0) attend_next(p, ROWS, TOK, C::EXTRA, 1, ALL, cur);
         }
-        if (elect_one()) umma_commit(&drained);                // what was issued ends before the tensor memory goes
+        if (elect_one()) {
+            if constexpr (PAIR) umma2_commit(&drained);
+            else umma_commit(&drained);
+        }                                      // what was issued ends before the tensor memory goes
         mbar_wait(&drained, 0, p.status);
         __syncwarp();
     } else {
@@ -341,9 +398,9 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             const AttendSeq sq = cur.q;
             const int row_first = cur.tile * ROWS, rows = min(ROWS, sq.nq - row_first);
             const int first_tile = mine.from + (p.ranges ? p.ranges[attend_range_at(p, sq, cur.tile, ROWS)].x : 0);
-            if (t == 0 || rows > 128) {
+            if (t == 0 || rows > C::TILE_ROWS) {
                 const int head = sp.head0 + cur.head;
-                if (!lp.q_map) {
+                if (!PAIR && !lp.q_map) {
                     // ---- the warp's 32 query rows, whose strides no tensor map has
                     const int g_all = (DN + lp.P) / 8;
                     for (int x = lane; x < 32 * g_all; x += 32) {
@@ -352,19 +409,19 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                         if (t * 128 + row < rows)
                             z = load_row8((const uint16_t *)p.q + head * p.q_head + g * 8 +
                                           (int64_t)(sq.row0 + row_first + t * 128 + row) * p.q_row, p.q_wide);
-                        *(uint4 *)(s_q + t * C::K_BYTES + (g >> 3) * C::CHUNK + row * 128 +
+                        *(uint4 *)(s_q + t * C::Q_TILE + (g >> 3) * C::CHUNK + row * 128 +
                                    (((g & 7) ^ (row & 7)) << 4)) = z;
                     }
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&qfull[t]);
                 }
-                const int r = t * 128 + rt;
+                const int tile_row = t * C::TILE_ROWS + (int)rank * 128, r = tile_row + rt;
                 const bool real = r < rows;
                 const int limit = real ? attend_limit(p, sq, row_first + r) : sq.kv;
                 // a slot without a token has tag -1, and a row that sees none -2
                 const int qt = real && tags ? p.q_tags[sq.row0 + row_first + r] : -2, qtag = qt < 0 ? -2 : qt;
-                const int safe = attend_limit(p, sq, row_first + t * 128) - HT;
+                const int safe = attend_limit(p, sq, row_first + tile_row) - HT;
                 float mm = 0.f, l = 0.f;
                 bool unset = real;             // no key seen yet: mm = 0
                 for (int i = 0; i < n; ++i, ++tiles) {
@@ -475,7 +532,10 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                         tmem_st_wait();
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&pfull[t][b]);
+                        if (lane == 0) {
+                            if (lead) mbar_arrive(&pfull[t][b]);
+                            else mbar_arrive_remote(&pfull[t][b], 0);
+                        }
                     }
                     if (!ok) break;
                 }
@@ -485,7 +545,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 // ---- whole items are written, others left for the joining kernel
                 const bool whole = n == cur.units;
                 if (unset) mm = NEG;
-                float *part = p.partial + ((int64_t)blockIdx.x * 2 + (mine.from == 0)) * attend_slot_floats(ROWS, DV);
+                float *part = p.partial + ((int64_t)share_at * 2 + (mine.from == 0)) * attend_slot_floats(ROWS, DV);
                 const float inv = l > 0.f ? 1.f / l : l;       // a NaN stays one
                 const int64_t dst = (int64_t)(sq.row0 + row_first + r) * p.q_heads + head;
 #pragma unroll 1
@@ -507,7 +567,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 if (!whole) {
                     part[ROWS * DV + r] = mm, part[ROWS * DV + ROWS + r] = l;
                     if (r == 0 && mine.from == 0)
-                        ((LatentJoin *)p.joins)[blockIdx.x] = {
+                        ((LatentJoin *)p.joins)[share_at] = {
                             dst, rows, (int)((first + done - cur.unit + cur.units - 1) / per)};
                 }
                 tc_fence_before();
@@ -519,38 +579,62 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
     }
     tc_fence_before();
     __syncthreads();
-    tc_fence_after();
-    if (warp == 0) tmem_dealloc(tmem, 512);
+    if constexpr (PAIR) {
+        cluster_sync();                        // neither leaves while the other may still need it
+        tc_fence_after();
+        if (warp == 0) tmem_dealloc2(tmem, 512);
+    } else {
+        tc_fence_after();
+        if (warp == 0) tmem_dealloc(tmem, 512);
+    }
 }
 
-template <int DN, int DV>
-cudaError_t run_wide(LatentParams &p, const LatentSpace &sp, int ctas, cudaStream_t st) {
-    using C = WideLatent<DN, DV>;
-    auto *kernel = k_latent_wide<DN, DV>;
-    // once a device (the attribute stays; another thread that comes first does the same)
-    static std::atomic<bool> ready[64];
+// Whether query rows come by a tensor map, whose strides are below 2^40 bytes.
+bool q_spaced(const LatentParams &p) {
+    const int64_t far = 1LL << 32;
+    return p.a.q_wide && p.a.q_row > 0 && p.a.q_head > 0 && p.a.q_row < far && p.a.q_head < far;
+}
+
+// The CTAs or pairs that a call's steps are shared out to.
+template <int DN, int DV, bool PAIR>
+cudaError_t wide_shares(int *shares) {
+    using C = WideLatent<DN, DV, PAIR>;
+    auto *kernel = k_latent_wide<DN, DV, PAIR>;
+    // once a device (another thread that comes first finds the same)
+    static std::atomic<int> fit[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev >= 64 || !ready[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-        if (e != cudaSuccess) return e;
-        if (dev < 64) ready[dev].store(true, std::memory_order_release);
-    }
+    if (dev < 64 && (*shares = fit[dev].load(std::memory_order_acquire)) > 0) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    *shares = device_sm_count();
+    if (PAIR && e == cudaSuccess) e = pairs_that_fit(kernel, C::THREADS, C::SMEM, shares);
+    if (e == cudaSuccess && dev < 64) fit[dev].store(*shares, std::memory_order_release);
+    return e;
+}
+
+template <int DN, int DV, bool PAIR = false>
+cudaError_t run_wide(LatentParams &p, const LatentSpace &sp, int shares, cudaStream_t st) {
+    using C = WideLatent<DN, DV, PAIR>;
+    auto *kernel = k_latent_wide<DN, DV, PAIR>;
+    cudaError_t e = cudaSuccess;
     const CUtensorMapDataType type = p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     CUtensorMap rows, k, v;
-    e = latent_rows_map(p, 128, &rows);
-    if (e == cudaSuccess) e = make_tmap_2d(&k, sp.k, type, 2, DN, (uint64_t)sp.rows, DN * 2, 64, C::TOK);
+    e = latent_rows_map(p, C::K_ROWS, &rows);
+    if (e == cudaSuccess) e = make_tmap_2d(&k, sp.k, type, 2, DN, (uint64_t)sp.rows, DN * 2, 64, C::K_ROWS);
     if (e == cudaSuccess) e = make_tmap_2d(&v, sp.v, type, 2, DV, (uint64_t)sp.rows, DV * 2, 64, C::TOK);
-    const int64_t far = 1LL << 32;             // (bytes: a tensor map's strides are below 2^40)
-    p.q_map = p.a.q_wide && p.a.q_row > 0 && p.a.q_head > 0 && p.a.q_row < far && p.a.q_head < far;
     CUtensorMap q = rows;
+    p.q_map = q_spaced(p);
     if (e == cudaSuccess && p.q_map)
         p.q_map = make_tmap_3d(&q, p.a.q, type, DN + p.P, (uint64_t)p.a.n_q, p.a.q_row * 2, (uint64_t)p.a.q_heads,
                                p.a.q_head * 2, 64, 128) == cudaSuccess;
+    if (PAIR && !p.q_map) e = cudaErrorInvalidValue;
     if (e != cudaSuccess) return e;
-    return launch_pdl(kernel, dim3(ctas), dim3(C::THREADS), C::SMEM, st, rows, k, v, q, p, sp, latent_box(p, 128),
-                      (int)(p.a.n_blocks * p.a.per_block * KV_UNIT));
+    const int box = latent_box(p, C::K_ROWS), n_rows = (int)(p.a.n_blocks * p.a.per_block * KV_UNIT);
+    if constexpr (PAIR)
+        return launch_pairs(kernel, shares, C::THREADS, C::SMEM, st, rows, k, v, q, p, sp, box, n_rows);
+    else
+        return launch_pdl(kernel, dim3(shares), dim3(C::THREADS), C::SMEM, st, rows, k, v, q, p, sp, box, n_rows);
 }
 
 constexpr int WIDE_ROWS = 256;
@@ -573,6 +657,12 @@ Plan plan_of(const LatentParams &p) {
     return x;
 }
 
+// Pairs of CTAs where keys and values are widest and sequences have rows for them.
+constexpr int PAIR_ROWS = 512;
+bool pairs_for(const LatentParams &p) {
+    return p.nope == 128 && p.value == 128 && q_spaced(p) && p.a.n_q >= (int64_t)PAIR_ROWS * p.a.n_seq;
+}
+
 }  // namespace
 
 int64_t latent_expanded_scratch(const LatentParams &p) {
@@ -593,21 +683,30 @@ cudaError_t launch_latent_expanded(LatentParams &p, void *scratch, cudaStream_t 
     sp.k = at, sp.v = at + x.k;
     sp.seq_rows = x.seq_rows;
     sp.k_step = p.k_head / p.k_row, sp.v_step = p.v_head / p.v_row;
-    cudaError_t e = cudaSuccess;
-    if (x.ranges) {
+    // (a pair's part has twice the rows, and there are at most half as many: the scratch is the same)
+    const bool pair = pairs_for(p);
+    const int rows = pair ? 2 * WIDE_ROWS : WIDE_ROWS;
+    int shares = 0;
+    cudaError_t e = pair                               ? wide_shares<128, 128, true>(&shares)
+                    : p.nope == 64 && p.value == 64    ? wide_shares<64, 64, false>(&shares)
+                    : p.nope == 64                     ? wide_shares<64, 128, false>(&shares)
+                    : p.value == 64                    ? wide_shares<128, 64, false>(&shares)
+                                                       : wide_shares<128, 128, false>(&shares);
+    if (x.ranges && e == cudaSuccess) {
         a.ranges = ranges;
-        e = launch_attend_ranges(a, 128, {WIDE_ROWS, x.ctas}, 1, 0x7fffffff, st);
+        e = launch_attend_ranges(a, 128, {rows, shares}, 1, 0x7fffffff, st);
     }
     for (int h = 0; e == cudaSuccess && h < a.q_heads; h += x.heads) {
         sp.head0 = h, sp.heads = a.heads = a.q_heads - h < x.heads ? a.q_heads - h : x.heads;
         sp.rows = x.seq_rows * a.n_seq * sp.heads;
         e = launch_latent_expand(p, sp, st);
         if (e == cudaSuccess)
-            e = p.nope == 64 ? p.value == 64 ? run_wide<64, 64>(p, sp, x.ctas, st)
-                                             : run_wide<64, 128>(p, sp, x.ctas, st)
-                : p.value == 64 ? run_wide<128, 64>(p, sp, x.ctas, st)
-                                : run_wide<128, 128>(p, sp, x.ctas, st);
-        if (e == cudaSuccess) e = launch_latent_join(p, p.value, x.ctas, WIDE_ROWS, a.q_heads, st);
+            e = pair                            ? run_wide<128, 128, true>(p, sp, shares, st)
+                : p.nope == 64 && p.value == 64 ? run_wide<64, 64>(p, sp, shares, st)
+                : p.nope == 64                  ? run_wide<64, 128>(p, sp, shares, st)
+                : p.value == 64                 ? run_wide<128, 64>(p, sp, shares, st)
+                                                : run_wide<128, 128>(p, sp, shares, st);
+        if (e == cudaSuccess) e = launch_latent_join(p, p.value, shares, rows, a.q_heads, st);
     }
     return e;
 }

@@ -110,6 +110,15 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
         : "memory");
 }
+// The same by the even CTA of a pair, for both (ak_sm100.cuh): A's rows in the tensor memory of the CTA that has
+// them.
+__device__ __forceinline__ void mma2_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+        : "memory");
+}
 // High words of descriptors: 128-byte swizzle (DESC_HI), and 64-byte swizzle: atoms of 8 K-rows x 32
 // values along N, 512 bytes, one after the other along K (MN-major).
 constexpr uint32_t DESC_HI_64 = (512u >> 4) | (1u << 14) | (4u << 29);

@@ -596,6 +596,30 @@ def test_wide_lists(R, dt, S, width, H):
                                w_k=w64[:, :N], w_v=w64[:, N:]))
 
 
+# prompts with rows for pairs of CTAs, of 512 rows an item: ends in either CTA's rows and row tiles
+PROMPTS = {
+    "causal": dict(kv=[700, 1300], nq=[700, 600]),
+    "prefix": dict(kv=[1600, 513], nq=[513, 512], prefix=[1000, 400], dt="fp16"),
+    "uneven": dict(kv=[1100, 10, 40, 1500], nq=[1100, 0, 5, 1500], T=48, heads=1, tail=3),
+    "bidirectional": dict(kv=[900], nq=[640], causal=False, R=128, P=32),
+    "tags": dict(kv=[1000, 1040], nq=[700, 800], tags=3, T=16, holes=True, causal=False),
+    "tags_causal": dict(kv=[2000], nq=[1537], tags=2, prefix=[300], dt="fp16", R=512),
+    "loud": dict(kv=[800], nq=[650], gain=8.0, R=512),
+}
+
+
+@pytest.mark.parametrize("case", PROMPTS)
+def test_long_prompts(case):
+    kw = {"heads": 2, **PROMPTS[case]}
+    c, call, want, _ = problem(len(case), form="expanded", nope=128, value=128, **kw)
+    got = [call() for _ in range(3)]
+    c.sync()
+    rows = len(want["out"])
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+    compare(got[0], want, rows)
+    assert (got[0][rows:] == 0).all()
+
+
 def test_streams_in_turn():
     """Calls on streams of their own that follow each other by events, without the host between."""
     c, call, want, x = problem(24, kv=[900, 130], nq=[1, 2], heads=16, R=256)

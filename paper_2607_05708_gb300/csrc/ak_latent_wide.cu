@@ -16,11 +16,11 @@
 // (ak_latent_join.cu).
 //
 // Measured (2 requests of 2048 rows behind 10240 tokens, 32 heads, 128 + 64 and 128 dims): 643 GFLOP in
-// 515 us, two thirds of a plain matrix product's burst rate; the tensor pipe 55 % busy.  A step of 256 rows
-// and 128 tokens takes 4400 cycles, its 40 products 2600 at the pipe's rate: a product of scores reads
-// 8 KB of shared memory in the 65 cycles that it should take, which is all that shared memory gives, beside
-// 80 KB a step that come in.  Scaling inside the exponent (32 instructions less of a half's 220) changed
-// nothing.
+// 500 us, two thirds of a plain matrix product's burst rate; by CTAs alone 515, the tensor pipe 55 % busy.  A
+// step of 256 rows and 128 tokens takes 4300 cycles, its 40 products 2600 at the pipe's rate.  What did not
+// help: scaling inside the exponent (32 instructions less of 220 for 64 scores); sixteen softmax warps, two a
+// row (661 us for the call's 638: 18 warps leave 96 registers a thread); scores of 64 tokens at a time into
+// the columns that the softmax has read, ahead of the weights (716: 24 products of N = 64 more).
 #include <atomic>
 
 #include "ak_latent.cuh"
@@ -144,7 +144,8 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
         }
     }
     constexpr int ALL = 0x7fffffff;
-    const LatentShare share = latent_share(p, ROWS, TOK, C::EXTRA, (int64_t *)s_q, C::CTAS);   // (until s_q holds query rows)
+    // (the plan stands in s_q until query rows come)
+    const LatentShare share = latent_share(p, ROWS, TOK, C::EXTRA, (int64_t *)s_q, C::CTAS);
     const int64_t first = share.first, per = share.per;
     int left = share.left;
     AttendCursor cur = share.cur;
@@ -237,7 +238,7 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
                 }
                 // the sequence's rows in the scratch end with its tiles: behind them zeros
                 const int y = tok < max(cur.q.kv, 1) ? (int)(at + tok) : (int)sp.rows;
-                const int box_row = __shfl_sync(0xffffffffu, row, (int)rank * (C::K_ROWS / 16) + lane % nb * (box / 16));
+                const int box_row = __shfl_sync(0xffffffffu, row, ((int)rank * C::K_ROWS + lane % nb * box) / 16);
                 __syncwarp();
                 if (lane < nb)
                     load(s_kv + C::key_at(n_tile, C::KC - 1) + lane * box * 128, &rows_map, &kfull[b], lp.R,
@@ -657,10 +658,14 @@ Plan plan_of(const LatentParams &p) {
     return x;
 }
 
-// Pairs of CTAs where keys and values are widest and sequences have rows for them.
-constexpr int PAIR_ROWS = 512;
+// Pairs of CTAs where keys and values are widest, sequences have rows for them and lists are long: their products
+// are faster, beginnings and ends of items slower.  Whole calls with pairs and without, us, sequences x rows /
+// context, heads: 2 x 2048 / 10240, 32: 669, 721; 4 x 1024 / 4096, 16: 208, 215; 1 x 8192 / 8192, 16: 336, 335; 16 x
+// 700 / 700, 16: 173, 147; 8 x 512 / 512, 16: 85, 75.  (Contexts shorter than their lists only the device knows.)
+constexpr int PAIR_ROWS = 512, PAIR_KV = 8192;
 bool pairs_for(const LatentParams &p) {
-    return p.nope == 128 && p.value == 128 && q_spaced(p) && p.a.n_q >= (int64_t)PAIR_ROWS * p.a.n_seq;
+    return p.nope == 128 && p.value == 128 && q_spaced(p) && p.a.n_q >= (int64_t)PAIR_ROWS * p.a.n_seq &&
+           p.a.max_kv >= PAIR_KV;
 }
 
 }  // namespace

@@ -35,12 +35,12 @@ def _round(x, dt):
 
 
 def problem(seed, kv, nq, heads=4, R=256, P=64, T=64, dt="bf16", form="absorbed", nope=64, value=64, causal=True,
-            prefix=None, tags=0, holes=False, tail=0, gain=1.0, tag_rows=None):
+            prefix=None, tags=0, holes=False, tail=0, gain=1.0, tag_rows=None, listed=0):
     """A cache, a call on it and what it should give."""
     from paper_2607_05708_gb300 import LatentCache
     rng = np.random.default_rng(seed)
     need = [-(-n // T) for n in kv]
-    n_blocks, S, width = sum(need) + 2, len(kv), max(max(need), 1)
+    n_blocks, S, width = sum(need) + 2, len(kv), max(max(need), 1, listed // T)
     order = rng.permutation(n_blocks)
     blocks = np.full((S, width), -1, np.int64)
     at = 0
@@ -596,7 +596,8 @@ def test_wide_lists(R, dt, S, width, H):
                                w_k=w64[:, :N], w_v=w64[:, N:]))
 
 
-# prompts with rows for pairs of CTAs, of 512 rows an item: ends in either CTA's rows and row tiles
+# prompts with rows for pairs of CTAs, of 512 rows an item, which are taken where lists are long: ends in
+# either CTA's rows and row tiles
 PROMPTS = {
     "causal": dict(kv=[700, 1300], nq=[700, 600]),
     "prefix": dict(kv=[1600, 513], nq=[513, 512], prefix=[1000, 400], dt="fp16"),
@@ -608,10 +609,11 @@ PROMPTS = {
 }
 
 
+@pytest.mark.parametrize("listed", [0, 8256])
 @pytest.mark.parametrize("case", PROMPTS)
-def test_long_prompts(case):
+def test_long_prompts(case, listed):
     kw = {"heads": 2, **PROMPTS[case]}
-    c, call, want, _ = problem(len(case), form="expanded", nope=128, value=128, **kw)
+    c, call, want, _ = problem(len(case), form="expanded", nope=128, value=128, listed=listed, **kw)
     got = [call() for _ in range(3)]
     c.sync()
     rows = len(want["out"])

@@ -16,7 +16,7 @@
 // (ak_latent_join.cu).
 //
 // Measured (2 requests of 2048 rows behind 10240 tokens, 32 heads, 128 + 64 and 128 dims): 643 GFLOP in
-// 500 us, two thirds of a plain matrix product's burst rate; by CTAs alone 515, the tensor pipe 55 % busy.  A
+// 509 us, two thirds of a plain matrix product's burst rate, the tensor pipe 58 % busy; by CTAs alone 517.  A
 // step of 256 rows and 128 tokens takes 4300 cycles, its 40 products 2600 at the pipe's rate.  What did not
 // help: scaling inside the exponent (32 instructions less of 220 for 64 scores); sixteen softmax warps, two a
 // row (661 us for the call's 638: 18 warps leave 96 registers a thread); scores of 64 tokens at a time into

@@ -641,6 +641,9 @@ cudaError_t run_wide(LatentParams &p, const LatentSpace &sp, int shares, cudaStr
 }
 
 constexpr int WIDE_ROWS = 256;
+// Keys and values are stored 32 bytes at a time, and the caller's scratch need only be 16-byte aligned: they begin at
+// the next whole line, for which the scratch has room.
+constexpr int KEYS_AT = 128;
 // The heads whose keys and values are in the scratch at a time: all, as far as these take 2 GB.
 struct Plan {
     int64_t seq_rows, joins, ranges, partial, k, v;    // rows a sequence and head; bytes
@@ -675,7 +678,7 @@ bool pairs_for(const LatentParams &p) {
 int64_t latent_expanded_scratch(const LatentParams &p) {
     const Plan x = plan_of(p);
     if (x.seq_rows * p.a.n_seq * x.heads > 0x7fffffffLL - 8192) return -1;
-    return x.joins + x.ranges + x.partial + x.k + x.v;
+    return x.joins + x.ranges + x.partial + KEYS_AT - 16 + x.k + x.v;
 }
 
 cudaError_t launch_latent_expanded(LatentParams &p, void *scratch, cudaStream_t st) {
@@ -687,7 +690,8 @@ cudaError_t launch_latent_expanded(LatentParams &p, void *scratch, cudaStream_t 
     int2 *ranges = (int2 *)at;
     at += x.ranges;
     a.partial = (float *)at, at += x.partial;
-    sp.k = at, sp.v = at + x.k;
+    at = (unsigned char *)(((uintptr_t)at + KEYS_AT - 1) & ~(uintptr_t)(KEYS_AT - 1));
+    sp.k = at, sp.v = at + x.k;            // (x.k: a multiple of 128 rows)
     sp.seq_rows = x.seq_rows;
     sp.k_step = p.k_head / p.k_row, sp.v_step = p.v_head / p.v_row;
     // (a pair's part has twice the rows, and there are at most half as many: the scratch is the same)

@@ -149,6 +149,10 @@ akashic_status_t attend_check(const akashic_mem_latent_config_t *cfg, const akas
     if ((a->nope_dim != 64 && a->nope_dim != 128) || (a->value_dim != 64 && a->value_dim != 128))
         return kv_fail(AKASHIC_EINVAL, "%s: nope_dim and value_dim must be 64 or 128", who);
     if (a->lse) return kv_fail(AKASHIC_EINVAL, "%s: the expanded form has no lse", who);
+    // (before anything is multiplied by their product; what else a call needs of the scratch is 2 GB, or one head's)
+    if (a->n_seq > 0 && a->n_q > 0 &&
+        latent_seq_rows(a->max_blocks * cfg->block_tokens) > (0x7fffffffLL - 8192) / a->n_seq)
+        return kv_fail(AKASHIC_EINVAL, "%s: sequences times the tokens of a list must be below 2^31", who);
     const int64_t st[2][2] = {{a->w_k_head_stride, a->w_k_row_stride}, {a->w_v_head_stride, a->w_v_row_stride}};
     for (auto &w : st)
         if (w[1] < cfg->latent_dim || w[1] % 8 || w[1] > (1 << 30) || w[0] < 0 || w[0] % w[1] ||
@@ -202,7 +206,6 @@ akashic_status_t run_attend(const akashic_mem_latent_config_t *cfg, const void *
         p.v_head = a->w_v_head_stride, p.v_row = a->w_v_row_stride;
     }
     const int64_t need = expanded ? latent_expanded_scratch(p) : latent_absorbed_scratch(p);
-    if (need < 0) return kv_fail(AKASHIC_EINVAL, "%s: sequences times the tokens of a list must be below 2^31", who);
     if (scratch_bytes < need) return kv_fail(AKASHIC_EINVAL, "%s: scratch needs %lld bytes", who, (long long)need);
     const cudaError_t e = expanded ? launch_latent_expanded(p, scratch, (cudaStream_t)stream)
                                    : launch_latent_absorbed(p, scratch, (cudaStream_t)stream);
@@ -225,8 +228,6 @@ akashic_status_t attend_scratch(const akashic_mem_latent_config_t *cfg, const ak
     p.R = cfg->latent_dim, p.P = cfg->rope_dim;
     p.nope = a->nope_dim, p.value = a->value_dim;
     *bytes = a->n_seq == 0 || a->n_q == 0 ? 0 : expanded ? latent_expanded_scratch(p) : latent_absorbed_scratch(p);
-    if (*bytes < 0)
-        return kv_fail(AKASHIC_EINVAL, "%s: sequences times the tokens of a list must be below 2^31", who);
     return AKASHIC_OK;
 }
 

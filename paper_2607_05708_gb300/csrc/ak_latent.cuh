@@ -144,11 +144,13 @@ struct alignas(16) LatentJoin {
     int rows, last;
 };
 
+// Rows that the expanded form's scratch has for a sequence and head.
+inline int64_t latent_seq_rows(int64_t tokens) { return ceil_div(tokens > 0 ? tokens : 1, (int64_t)128) * 128; }
 // The expanded form's keys and values of a group of heads: row (head, sequence, token) at (head *
 // n_seq + sequence) * seq_rows + token.
 struct LatentSpace {
     void *k, *v;                      // [rows][nope], [rows][value]
-    int64_t seq_rows, rows;           // seq_rows: a multiple of 128
+    int64_t seq_rows, rows;           // seq_rows: latent_seq_rows; all rows: coordinates of tensor maps
     int64_t k_step, v_step;           // rows of w_k and w_v from one head to the next
     int head0, heads;
 };
@@ -189,7 +191,7 @@ cudaError_t latent_rows_map(const LatentParams &p, int most, CUtensorMap *map);
 cudaError_t launch_latent_join(const LatentParams &p, int dim, int ctas, int rows, int step, cudaStream_t st);
 
 int64_t latent_absorbed_scratch(const LatentParams &p);
-int64_t latent_expanded_scratch(const LatentParams &p);  // -1: too many tokens
+int64_t latent_expanded_scratch(const LatentParams &p);
 cudaError_t launch_latent_absorbed(LatentParams &p, void *scratch, cudaStream_t st);
 cudaError_t launch_latent_expand(const LatentParams &p, const LatentSpace &sp, cudaStream_t st);
 cudaError_t launch_latent_expanded(LatentParams &p, void *scratch, cudaStream_t st);

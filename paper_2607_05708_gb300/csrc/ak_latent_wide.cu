@@ -652,7 +652,7 @@ struct Plan {
 Plan plan_of(const LatentParams &p) {
     Plan x;
     x.ctas = device_sm_count();
-    x.seq_rows = ceil_div((int64_t)(p.a.max_kv > 0 ? p.a.max_kv : 1), (int64_t)128) * 128;
+    x.seq_rows = latent_seq_rows(p.a.max_kv);
     const int64_t rows = x.seq_rows * p.a.n_seq, room = (2LL << 30) / (rows * (p.nope + p.value) * 2);
     const int64_t most = room < 1 ? 1 : room < p.a.q_heads ? room : p.a.q_heads;
     x.heads = (int)ceil_div((int64_t)p.a.q_heads, ceil_div((int64_t)p.a.q_heads, most));
@@ -677,7 +677,6 @@ bool pairs_for(const LatentParams &p) {
 
 int64_t latent_expanded_scratch(const LatentParams &p) {
     const Plan x = plan_of(p);
-    if (x.seq_rows * p.a.n_seq * x.heads > 0x7fffffffLL - 8192) return -1;
     return x.joins + x.ranges + x.partial + KEYS_AT - 16 + x.k + x.v;
 }
 

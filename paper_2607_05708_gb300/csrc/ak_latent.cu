@@ -156,7 +156,7 @@ akashic_status_t attend_check(const akashic_mem_latent_config_t *cfg, const akas
     const int64_t st[2][2] = {{a->w_k_head_stride, a->w_k_row_stride}, {a->w_v_head_stride, a->w_v_row_stride}};
     for (auto &w : st)
         if (w[1] < cfg->latent_dim || w[1] % 8 || w[1] > (1 << 30) || w[0] < 0 || w[0] % w[1] ||
-            w[0] / w[1] * (a->q_heads - 1) > 0x7fffffffLL - 256)
+            (a->q_heads > 1 && w[0] / w[1] > (0x7fffffffLL - 256) / (a->q_heads - 1)))
             return kv_fail(AKASHIC_EINVAL,
                            "%s: rows of w_k and w_v must be evenly spaced, by a multiple of 8 from latent_dim on", who);
     return AKASHIC_OK;

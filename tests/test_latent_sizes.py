@@ -38,6 +38,12 @@ def test_more_tokens_than_the_scratch_can_number(lib, n_seq, max_blocks):
     _refused(lib, _config(4096), R=128, n_q=n_seq, q_heads=1, n_seq=n_seq, max_blocks=max_blocks)
 
 
+@pytest.mark.parametrize("name", ["w_k_head_stride", "w_v_head_stride"])
+@pytest.mark.parametrize("stride,heads", [(128 << 55, 513), (128 << 54, 1024), ((1 << 63) - 128, 3), (128 << 31, 2)])
+def test_head_strides_beyond_64_bits(lib, name, stride, heads):
+    _refused(lib, _config(), R=128, n_q=1, q_heads=heads, n_seq=1, max_blocks=1, **{name: stride})
+
+
 def test_nothing_to_do_is_no_error(lib):
     from paper_2607_05708_gb300 import _LatentAttend
     a = ctypes.byref(_LatentAttend(n_q=0, q_heads=1, n_seq=1 << 25, max_blocks=1 << 18, scale=1.0, w_k_head_stride=128,

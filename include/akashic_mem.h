@@ -572,7 +572,9 @@ akashic_status_t akashic_mem_latent_append(const akashic_mem_latent_config_t *cf
 /* Arguments of both forms; fields named as in akashic_mem_kv_attend_t mean the same.  q and
  * out are of the cache's type.  Scores, maxima and totals are fp32; weights, and the expanded
  * form's keys and values, are rounded to the cache's type before their products (what is
- * beyond its range to its largest value). */
+ * beyond its range to its largest value).  Where a sum of w_k c_j or w_v c_j is not finite in
+ * fp32 (w_k or w_v is not, or products pass fp32's range), the head's rows that see token j
+ * are NaN, in all values; rows that do not see it are as without it. */
 typedef struct {
     const void *q;             /* device; absorbed: rows of latent_dim + rope_dim, expanded:
                                   of nope_dim + rope_dim values                      */

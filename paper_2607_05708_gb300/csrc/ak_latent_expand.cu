@@ -256,15 +256,21 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
             const bool real = cur.seq < p.n_seq;
             const int64_t row = (int64_t)cur.head * sp.seq_rows * p.n_seq + (int64_t)cur.seq * sp.seq_rows +
                                 cur.tile * C::TOK + warp * 32 + lane;
+            // What a row does not see meets a weight of 0: what is stored of a value is finite.  A token one of whose
+            // sums is no number (not finite: of weights that are not, of infinities of both signs) gets a key
+            // that is none, so that the rows that see it, and no others, are NaN.  The key's first value is the last
+            // to be written.
+            float odd = 0.f;                   // not 0 with a sum that is not finite
 #pragma unroll 1
-            for (int c = 0; real && c < rows_w; c += 32) {
+            for (int c = rows_w - 32; real && c >= 0; c -= 32) {
                 uint32_t y[32];
                 tmem_ld32(tmem + lanes + acc * 256 + c, y);
                 tmem_ld_wait();
+#pragma unroll
+                for (int k = 0; k < 32; ++k) odd = fmaf(__uint_as_float(y[k]), 0.f, odd);
                 uint32_t h[16];
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
-                    // (finite: a value that a row does not see meets a weight of 0)
                     const float a = fminf(fmaxf(__uint_as_float(y[2 * k]), -most), most);
                     const float b = fminf(fmaxf(__uint_as_float(y[2 * k + 1]), -most), most);
                     if (lp.bf16) {
@@ -274,6 +280,7 @@ k_latent_expand(const __grid_constant__ CUtensorMap rows_map, const __grid_const
                         h[k] = pack_h2(a, b);
                     }
                 }
+                if (c == 0 && odd != 0.f) h[0] |= 0x7fffu;     // a NaN of either type
                 uint16_t *dst = c < lp.nope ? (uint16_t *)sp.k + row * lp.nope + c
                                             : (uint16_t *)sp.v + row * lp.value + (c - lp.nope);
 #pragma unroll

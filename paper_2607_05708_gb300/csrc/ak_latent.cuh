@@ -24,6 +24,10 @@ struct LatentParams {
     int64_t k_head, k_row, v_head, v_row;
 };
 
+// The power of two of a bf16 weight whose score set its row's reference: below 2^(-1 - M_SLACK) / kv, so that kv
+// weights of 2^M_SLACK times that, the most one may have, add up to less than 1 (2^-16 for up to 127 tokens, 2^-23
+// for 8192; fp32 holds 2^-86 of it at the longest context).
+__device__ __forceinline__ float latent_off_bf16(int kv) { return (float)(__clz(kv) - 33) - M_SLACK; }
 __device__ __forceinline__ uint16_t round16(float x, bool bf16) {
     return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
 }

@@ -65,10 +65,10 @@ struct Absorbed {
 };
 
 // A weight is 2^off where its score is the one that set the row's reference, and 2^(off + SLACK) at
-// most.  fp16 has room for 2^15 and down to 2^-24; bf16's weights stay below 2^-8, so that values near the
-// type's largest, which weigh 1 in all, do not add up to infinities.  Weights are rounded to the cache's
-// type because a product's operands have one type; totals add up the unrounded ones.
-constexpr float SLACK = 8.f;
+// most.  fp16 has room for 2^15 and down to 2^-24.  bf16's weights are so small (latent_off_bf16) that a row's
+// add up to less than 1 in all its parts: values near the type's largest then add up to no infinity.  Weights are
+// rounded to the cache's type because a product's operands have one type; totals add up the unrounded ones.
+constexpr float SLACK = M_SLACK;
 
 // Whether any thread of the barrier's has `x`, for all of them.
 __device__ __forceinline__ bool bar_any(int id, int threads, bool x) {
@@ -355,7 +355,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
         const int key = TOK == 128 ? dim : quad * 16 + (lane & 15);
         const bool used = TOK == 128 || lane < 16;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const float f = p.scale * LOG2E_F, off = lp.bf16 ? -16.f : 7.f;
+        const float f = p.scale * LOG2E_F;
         const bool tags = p.tags != nullptr;
         uint32_t n_tile = 0;
         // After a wait that gave up the warps wait for nothing more, but go on to the end: they meet at
@@ -368,6 +368,7 @@ k_latent_absorbed(const __grid_constant__ CUtensorMap rows_map, const __grid_con
             if (n <= 0) break;
             const AttendSeq sq = cur.q;
             const int row_first = cur.tile * NR, rows = min(NR, sq.nq * p.group - row_first);
+            const float off = lp.bf16 ? latent_off_bf16(sq.kv) : 7.f;
             if (!lp.q_map) {
                 // ---- query rows whose strides no tensor map has
                 for (int x = tid; x < NR * (R + lp.P) / 8; x += THR) {

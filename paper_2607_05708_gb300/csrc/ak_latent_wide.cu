@@ -388,9 +388,6 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t o_at = tmem + lanes + t * DV;
         const float f = p.scale * LOG2E_F;
-        // A weight is 2^shift where its score set the row's maximum, 2^(shift + M_SLACK) at most: within fp16's
-        // range; bf16's far below 1, so that values near the type's largest do not add up to infinities.
-        const float shift = lp.bf16 ? -16.f : P_SHIFT;
         uint32_t n_tile = 0, tiles = 0;        // tiles: of this row tile, so far
         bool ok = true;
         int64_t done = 0;
@@ -401,6 +398,10 @@ k_latent_wide(const __grid_constant__ CUtensorMap rows_map, const __grid_constan
             const AttendSeq sq = cur.q;
             const int row_first = cur.tile * ROWS, rows = min(ROWS, sq.nq - row_first);
             const int first_tile = mine.from + (p.ranges ? p.ranges[attend_range_at(p, sq, cur.tile, ROWS)].x : 0);
+            // A weight is 2^shift where its score set the row's maximum, 2^(shift + M_SLACK) at most: within fp16's
+            // range; a row's bf16 ones less than 1 in all, so that values near the type's largest add up to no
+            // infinity.
+            const float shift = lp.bf16 ? latent_off_bf16(sq.kv) : P_SHIFT;
             if (t == 0 || rows > C::TILE_ROWS) {
                 const int head = sp.head0 + cur.head;
                 if (!PAIR && !lp.q_map) {

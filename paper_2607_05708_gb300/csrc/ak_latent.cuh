@@ -28,7 +28,15 @@ struct LatentParams {
 // weights of 2^M_SLACK times that, the most one may have, add up to less than 1 (2^-16 for up to 127 tokens, 2^-23
 // for 8192; fp32 holds 2^-86 of it at the longest context).
 __device__ __forceinline__ float latent_off_bf16(int kv) { return (float)(__clz(kv) - 33) - M_SLACK; }
+// A result in the type's range.  It is a mean of finite values, which its weights' rounding can put half a step beyond
+// the type's largest, and its own rounding then to infinity.  A NaN stays one.
+__device__ __forceinline__ float latent_result(float x, bool bf16) {
+    float y;
+    asm("min.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(bf16 ? 3.38953139e38f : 65504.f));
+    return y;
+}
 __device__ __forceinline__ uint16_t round16(float x, bool bf16) {
+    x = latent_result(x, bf16);
     return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
 }
 // Eight values of a query row.

@@ -52,6 +52,9 @@ k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int
     __syncthreads();
     const int total = before[JOIN_CTAS];
     const int64_t floats = attend_slot_floats(rows, D);
+    auto store = [&](int64_t at, float a, float b) {
+        store_pair(p, lp.bf16, at, latent_result(a, lp.bf16), latent_result(b, lp.bf16));
+    };
     for (int u = blockIdx.x; u < total; u += gridDim.x) {
         int lo = 0, hi = JOIN_CTAS;            // the last CTA with before <= u: the one whose item has row u
         while (hi - lo > 1) {
@@ -119,8 +122,8 @@ k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int
 #pragma unroll
                 for (int i = 0; i < STRIPS; ++i)
                     if (mine) {
-                        store_pair(p, lp.bf16, dst * D + lane * 4 + i * 128, v[y][i].x * inv, v[y][i].y * inv);
-                        store_pair(p, lp.bf16, dst * D + lane * 4 + i * 128 + 2, v[y][i].z * inv, v[y][i].w * inv);
+                        store(dst * D + lane * 4 + i * 128, v[y][i].x * inv, v[y][i].y * inv);
+                        store(dst * D + lane * 4 + i * 128 + 2, v[y][i].z * inv, v[y][i].w * inv);
                     }
                 if (lane == 0 && p.lse) p.lse[dst] = lse_of(mx[y], tot[y]);
             }
@@ -164,8 +167,8 @@ k_latent_join(const __grid_constant__ LatentParams lp, const int ctas, const int
                 v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
             }
             const int64_t dst = j.dst + (int64_t)r * step;
-            store_pair(p, lp.bf16, dst * D + d, v.x * inv, v.y * inv);
-            store_pair(p, lp.bf16, dst * D + d + 2, v.z * inv, v.w * inv);
+            store(dst * D + d, v.x * inv, v.y * inv);
+            store(dst * D + d + 2, v.z * inv, v.w * inv);
             if (tid == 0 && d0 == 0 && p.lse) p.lse[dst] = lse_of(mx, tot);
         }
         __syncthreads();

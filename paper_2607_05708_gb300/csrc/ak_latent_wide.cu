@@ -76,7 +76,8 @@ __device__ __forceinline__ void store_row32h(const LatentParams &lp, int64_t at,
     uint32_t h[16];
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-        const float a = __uint_as_float(y[2 * k]), b = __uint_as_float(y[2 * k + 1]);
+        const float a = latent_result(__uint_as_float(y[2 * k]), lp.bf16);
+        const float b = latent_result(__uint_as_float(y[2 * k + 1]), lp.bf16);
         if (lp.bf16) {
             const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
             h[k] = *(const uint32_t *)&v;

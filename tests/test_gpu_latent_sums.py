@@ -75,3 +75,56 @@ def test_expanded(dt, n, quiet, seqs, rows_of, heads, width, listed):
     want = torch.zeros(width, dtype=torch.float64)
     want[::2] = V
     _check(out, want.cuda(), dt)
+
+
+def _leaning(dt, n):
+    """Scores of n tokens: every 64th 0, the others such that a weight, a power of two times that, is rounded up by
+    three quarters of half a step (bf16 0.0033, fp16 0.0004 of itself; from the middle between the type's largest and
+    the next power of two on, 0.002 and 0.00025 above the largest, a result would round to infinity)."""
+    eps = torch.finfo(DT[dt]).eps
+    z = torch.log(torch.tensor((1 + 0.58 * eps) / 2, dtype=torch.float64))
+    a = z.to(DT[dt])
+    b = (z - a.double()).to(DT[dt])
+    rope = torch.zeros(n, 32, dtype=DT[dt])
+    rope[:, 0], rope[:, 1] = a, b
+    rope[::64] = 0
+    w = torch.exp(rope.double().sum(1)[1])
+    up = float((w.to(DT[dt]).double() - w) / w)
+    assert up > 1.3 * eps / 4 / (2 - eps) * 2
+    return rope
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dt", ["bf16", "fp16"])
+@pytest.mark.parametrize("form", ["absorbed", "absorbed_joined", "expanded", "expanded_pairs"])
+def test_means_of_the_largest_are_finite(form, dt, sign):
+    from paper_2607_05708_gb300 import LatentCache
+    R, n, most = 128, 700, torch.finfo(DT[dt]).max
+    c = LatentCache(-(-n // 64), R, 32, dtype=DT[dt])
+    rows = torch.zeros(n, R + 32, dtype=DT[dt])
+    rows[:, 1:R:2] = sign * most
+    rows[:, R:] = _leaning(dt, n)
+    c.append(rows[:, :R].cuda(), rows[:, R:].cuda(), torch.arange(n).cuda())
+    blocks = torch.arange(-(-n // 64)).cuda()
+    if form.startswith("absorbed"):
+        # 151 whole items on as many CTAs, or two tiles of rows that all CTAs share
+        seqs, rows_of, heads, listed = (151, 1, 16, 0) if form == "absorbed" else (1, 40, 3, 4096)
+        wide, want = R, rows[0, :R].double()
+    else:
+        seqs, rows_of, heads, listed = (200, 1, 4, 0) if form == "expanded" else (12, 600, 8, 8256)
+        wide = 128
+        want = torch.zeros(wide, dtype=torch.float64)
+        want[::2] = sign * most
+    lists = torch.full((seqs, max(len(blocks), listed // 64)), -1, dtype=torch.int64, device="cuda")
+    lists[:, :len(blocks)] = blocks
+    kv = torch.full((seqs,), n, dtype=torch.int32).cuda()
+    q = torch.zeros(seqs * rows_of, heads, wide + 32, dtype=DT[dt])
+    q[..., wide:wide + 2] = 1.0
+    if form.startswith("absorbed"):
+        out = c.attend(q.cuda(), lists, 1.0, kv_len=kv, causal=False)[0]
+    else:
+        w = torch.zeros(heads, 2 * wide, R, dtype=DT[dt])
+        w[:, wide::2, 1] = 1.0
+        out = c.attend_expanded(q.cuda(), w[:, :wide].cuda(), w[:, wide:].cuda(), lists, scale=1.0, kv_len=kv, causal=False)
+    c.sync()
+    _check(out, want.cuda(), dt)

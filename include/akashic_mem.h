@@ -432,7 +432,8 @@ akashic_status_t akashic_mem_kv_write(const akashic_mem_kv_config_t *cfg, void *
  * x[2i + 1]), becomes (a c - b s, b c + a s), c = cos[position][i] and s =
  * sin[position][i]: in fp32, each product and the sum rounded once.
  * Query rows of the same tokens can be rotated in the same call: q_out may be q
- * itself with the same strides (not another overlapping array). */
+ * itself with the same strides (not another overlapping array), and its rows do not overlap
+ * each other (EINVAL where the strides alone say that they do). */
 typedef struct {
     const int64_t *positions;  /* device int64[n]                                    */
     const float *cos, *sin;    /* device float[table_rows][rotary_dim / 2], 16-byte

@@ -599,8 +599,8 @@ class KVCache(_BlockCache):
         first 2 * cos.shape[1] values (a multiple of 32) pair i, (x[i], x[i + half]) or, interleaved,
         (x[2i], x[2i + 1]), is turned by the angle whose cosine and sine the tables
         (float32 [positions, pairs]) hold.  q [n, q_heads, head_dim] of k's type: rotated too
-        and returned, in q_out (q itself, or another tensor that does not overlap it)
-        if given; zero for tokens that are skipped."""
+        and returned, in q_out (q itself, or another tensor that does not overlap it; its
+        rows apart from each other) if given; zero for tokens that are skipped."""
         dt, n, sk, sv = self._kv(k, v, tags)
         r, q_out = self._rotation(n, self.head_dim, dt, positions, cos, sin, q, q_out, interleaved, stream)
         rc = self._append(self._cfg, self._data_ptr, self._tags_ptr, k.data_ptr(), sk[0], sk[1], v.data_ptr(),

@@ -411,7 +411,13 @@ int dtype_size(int32_t dtype) {
     return dtype == AKASHIC_DTYPE_FP32 ? 4 : dtype == AKASHIC_DTYPE_BF16 || dtype == AKASHIC_DTYPE_FP16 ? 2 : 0;
 }
 
-bool rotate_args(const akashic_mem_rotation_t *r, int width, int size, RotateArgs *a, const char **why) {
+bool rotate_args(const akashic_mem_rotation_t *r, int width, int size, int64_t n, RotateArgs *a, const char **why) {
+    // neighbouring rows or heads of q_out that share memory; q in place with other strides
+    const bool rows = n > 1, heads = r->q_heads > 1;
+    auto close = [&](int64_t stride) { return stride > -width && stride < width; };
+    const bool over = r->q && ((rows && close(r->q_out_row_stride)) || (heads && close(r->q_out_head_stride)) ||
+                               (r->q == r->q_out && ((rows && r->q_row_stride != r->q_out_row_stride) ||
+                                                     (heads && r->q_head_stride != r->q_out_head_stride))));
     *why = r->rotary_dim < 32 || r->rotary_dim % 32 || r->rotary_dim > width
                ? "rotary_dim must be a multiple of 32, at most the row's width"
            : r->table_rows < 1                        ? "table_rows must be >= 1"
@@ -423,7 +429,8 @@ bool rotate_args(const akashic_mem_rotation_t *r, int width, int size, RotateArg
                ? "q_heads must be in [1, 2^20]"
            : ((uintptr_t)r->q | (uintptr_t)r->q_out) & (uintptr_t)(size - 1)
                ? "q and q_out must be aligned to their element"
-               : nullptr;
+           : over ? "rows of q_out must not overlap, nor rows of q, but for those that they replace"
+                  : nullptr;
     if (*why) return false;
     a->positions = r->positions, a->cos = r->cos, a->sin = r->sin;
     a->table_rows = r->table_rows, a->rotary = r->rotary_dim, a->pairs = r->interleaved != 0;
@@ -472,7 +479,7 @@ akashic_status_t kv_write_rows(const char *who, const akashic_mem_kv_config_t *c
     if (new_tags && !tags) return kv_fail(AKASHIC_EINVAL, "%s: new_tags needs the cache's tags", who);
     KvRows r = {};
     const char *why = nullptr;
-    if (call == KV_APPEND && !rotate_args(rot, cfg->head_dim, size, &r.turn, &why))
+    if (call == KV_APPEND && !rotate_args(rot, cfg->head_dim, size, n, &r.turn, &why))
         return kv_fail(AKASHIC_EINVAL, "%s: %s", who, why);
     r.cfg = cfg;
     r.cache = (unsigned char *)cache;

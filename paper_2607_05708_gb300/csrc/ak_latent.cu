@@ -266,7 +266,7 @@ extern "C" akashic_status_t akashic_mem_latent_append(
         const char *why = nullptr;
         if (rotation->rotary_dim != cfg->rope_dim)
             return kv_fail(AKASHIC_EINVAL, "%s: rotary_dim must be rope_dim", who);
-        if (!rotate_args(rotation, cfg->rope_dim, size, &r.turn, &why))
+        if (!rotate_args(rotation, cfg->rope_dim, size, n, &r.turn, &why))
             return kv_fail(AKASHIC_EINVAL, "%s: %s", who, why);
     }
     r.cfg = cfg, r.cache = cache, r.latent = latent, r.rope = k_rope;

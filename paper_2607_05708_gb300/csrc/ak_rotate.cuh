@@ -179,8 +179,8 @@ __device__ __forceinline__ void turn_group(const RotateArgs &a, const T *src, in
     }
 }
 
-// Checks a call's rotation and takes it over (false: *why says what is wrong).
+// Checks the rotation of a call of n tokens and takes it over (false: *why says what is wrong).
 int dtype_size(int32_t dtype);   // bytes, 0: no type of rows
-bool rotate_args(const akashic_mem_rotation_t *r, int width, int size, RotateArgs *a, const char **why);
+bool rotate_args(const akashic_mem_rotation_t *r, int width, int size, int64_t n, RotateArgs *a, const char **why);
 
 }  // namespace ak

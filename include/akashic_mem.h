@@ -606,7 +606,8 @@ typedef struct {
 /* Bytes of scratch of a call, as akashic_mem_kv_attend_scratch.  The expanded form's holds keys
  * and values of as many heads as fit 2 GB (of one, where that takes more), for n_seq *
  * max_blocks * block_tokens tokens whatever the lengths are: give it lists no wider than the
- * longest sequence's.  EINVAL where these tokens are 2^31 or more. */
+ * longest sequence's.  EINVAL where these tokens, a list's rounded up to 128, are more than
+ * 2^31 - 2^13. */
 akashic_status_t akashic_mem_latent_attend_scratch(const akashic_mem_latent_config_t *cfg,
                                                    const akashic_mem_latent_attend_t *a,
                                                    int64_t *bytes);

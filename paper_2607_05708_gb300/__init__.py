@@ -800,7 +800,7 @@ class LatentCache(_BlockCache):
         is not known here).  Returns (out [n_q, q_heads, latent_dim], to be multiplied by
         w_v, and lse float32 [n_q, q_heads]).  For single tokens and drafts; prompts
         take fewer products in attend_expanded."""
-        dt, _, sq = self._rows(q, "q", self.latent_dim + self.rope_dim)
+        _, _, sq = self._rows(q, "q", self.latent_dim + self.rope_dim)
         if q.dtype is not self.dtype:
             raise TypeError(f"q must be {self.dtype}, got {q.dtype}")
         return self._run(q, sq, blocks, scale, self.latent_dim, kv_len, q_start, causal, prefix_len, q_tags, out, lse,
@@ -821,7 +821,7 @@ class LatentCache(_BlockCache):
             if t.get_device() != self.device:
                 raise ValueError(f"{name} must be a CUDA tensor on device {self.device}")
         nope, value = w_k.shape[1], w_v.shape[1]
-        dt, shape, sq = self._rows(q, "q", nope + self.rope_dim)
+        _, shape, sq = self._rows(q, "q", nope + self.rope_dim)
         if q.dtype is not self.dtype:
             raise TypeError(f"q must be {self.dtype}, got {q.dtype}")
         if w_k.shape[0] != shape[1] or w_v.shape[0] != shape[1]:

@@ -26,7 +26,8 @@ struct LatentParams {
 
 // The power of two of a bf16 weight whose score set its row's reference: below 2^(-1 - M_SLACK) / kv, so that kv
 // weights of 2^M_SLACK times that, the most one may have, add up to less than 1 (2^-16 for up to 127 tokens, 2^-23
-// for 8192; fp32 holds 2^-86 of it at the longest context).
+// for 8192; fp32 holds 2^-86 of it at the longest context).  For scores within 2^24, beyond which fp32 tells a reference
+// from one so much higher no longer.
 __device__ __forceinline__ float latent_off_bf16(int kv) { return (float)(__clz(kv) - 33) - M_SLACK; }
 // A result in the type's range.  It is a mean of finite values, which its weights' rounding can put half a step beyond
 // the type's largest, and its own rounding then to infinity.  A NaN stays one.

@@ -20,12 +20,12 @@
 // Tiles are shared out evenly over the CTAs (ak_attend.cuh); parts of an item are joined after it
 // (ak_latent_join.cu).
 //
-// Measured (the GPU's time, with the join; R = 512, bf16): 64 requests of up to 8192 tokens, 32 heads, 73 us
+// Measured (the GPU's time, with the join; R = 512, bf16): 64 requests of up to 8192 tokens, 32 heads, 74 us
 // (337 MB: 50 at a copy's rate); 64 heads over 200,000 tokens 63 us (231 MB: 34); 5 drafted rows of 16
-// requests, 40 heads, 71 us.  The kernel alone takes 68, 59 and 70 us under the profiler, DRAM 64 and 50 %
-// busy in the first two, the tensor pipe 18 and 30 %.  A step of 64 rows takes 2.6 to 3.5 thousand cycles
-// (its products 2000, its bytes 3200 at DRAM's rate with all SMs); a beginning takes 5000, the first pass
-// through cold instructions 10000, another item 5000, the join 9 to 12 us.
+// requests, 40 heads, 71 us.  The kernel alone takes 71, 60 and 73 us under the profiler, which empties the caches,
+// DRAM 61 and 49 % busy in the first two, the tensor pipe 20 and 32 %.  A step of 64 rows takes 2.6 to 3.5 thousand
+// cycles (its products 2000, its bytes 3200 at DRAM's rate with all SMs); a beginning takes 5000, the first pass
+// through cold instructions 10000, another item 5000, the join 8 to 12 us.
 #include <atomic>
 
 #include "ak_latent.cuh"
@@ -596,9 +596,12 @@ int tile_rows(const LatentParams &p) {
     return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
 
-// Short lists and no more items than SMs: a CTA an item, no scratch and no joining kernel.  (One request
-// of 700 tokens, 16 heads, R = 256: six steps one after the other take the GPU as long as one step and the
-// joining kernel, 14 us, and the host a launch and an allocation less: the call 21 -> 14 us.)
+// Short lists and no more items than SMs: a CTA an item, no scratch and no joining kernel, up to as many steps one after
+// the other as take the GPU no longer than a step a CTA and the join.  The GPU's time in this form and shared out,
+// us, by steps, one request of 16 heads: R = 128, 4: 8.4, 12.1; 6: 10.0, 12.8; 8: 11.6, 13.6; 12: 14.9, 15.0; 16: 18.1,
+// 16.2.  R = 256, 4: 9.4, 12.1; 6: 11.7, 12.6; 8: 14.0, 13.1.  R = 512, 4: 10.9, 12.5; 6: 13.6, 12.7; 8: 16.4, 13.3.  128
+// heads, R = 512, 4: 13.8, 15.4; 6: 17.4, 15.8.  64 requests, R = 512, 6: 14.0, 20.8; 16: 28.0, 26.9.  A call one after
+// the other, host and all: up to 8 steps 13 to 16 where shared out 22 to 24 (a launch and an allocation less).
 constexpr int DIRECT_STEPS = 6;
 int direct_tiles(const LatentParams &p, int sms) {
     if (p.a.q_start) return 0;

@@ -7,8 +7,8 @@
 // in shared memory for all heads of its share and streams the heads' weights past them, 64 of
 // R at a time.  Two accumulators, so that one is rounded and written while the other is computed.
 //
-// Measured (18,600 tokens, 32 heads, R = 512, 128 + 128 dims): 156 GFLOP in 103 us, 0.8 of a plain product's
-// burst rate, the tensor pipe 70 % busy, 1.1 GB from L2.  A CTA alone took 127 us: a head's weights come from
+// Measured (18,600 tokens, 32 heads, R = 512, 128 + 128 dims): 156 GFLOP in 102 us, 0.8 of a plain product's
+// burst rate, the tensor pipe 69 % busy, 1.1 GB from L2.  A CTA alone took 127 us: a head's weights come from
 // L2 once a tile of tokens, 1.8 GB at 14 TB/s.  Eight warps that write instead of four: no gain.
 #include <atomic>
 

@@ -1,13 +1,14 @@
 // Items of the latent attention whose steps lay in several CTAs' shares: the parts' results, weighed and
 // added in the order of the CTAs, so that results are the same bits every time.
 //
-// Items of few parts: a warp some rows of an item, whose parts' loads are then under way together (two
-// prompts of 2048 rows and 32 heads 14 us less than with a row a warp, whose join took 25).  Of many (a long
+// Items of few parts: a warp some rows of an item, whose parts' loads are then under way together (with a row a
+// warp packed documents take 91.4 us, not 90.1, two prompts of 2048 rows 632 either way; 256 retrieved lists, of 16
+// rows an item, 46.8, not 48.0).  Of many (a long
 // sequence is one item in the shares of all CTAs): a CTA 128 values of a row, its parts in groups of threads
 // that each add every so-manieth part up; 152 parts one after the other took 80 us.  The CTAs look for their
 // rows among the items themselves: a CTA a row of what might be an item would be thousands that find none.
-// Measured: 152 parts of 64 rows x 512, 11 us; 64 items of three or four such parts, 9 us; beginnings and
-// latencies, not bytes, bound both.
+// Measured: 152 parts of 64 rows x 512, 12 us; 64 items of three or four such parts, 10 us; two prompts of 2048 rows and
+// 32 heads 21; beginnings and latencies, not bytes, bound them.
 #include "ak_latent.cuh"
 
 namespace ak {

@@ -16,7 +16,7 @@
 // (ak_latent_join.cu).
 //
 // Measured (2 requests of 2048 rows behind 10240 tokens, 32 heads, 128 + 64 and 128 dims): 643 GFLOP in
-// 509 us, two thirds of a plain matrix product's burst rate, the tensor pipe 58 % busy; by CTAs alone 517.  A
+// 510 us, two thirds of a plain matrix product's burst rate, the tensor pipe 58 % busy; by CTAs alone 517.  A
 // step of 256 rows and 128 tokens takes 4300 cycles, its 40 products 2600 at the pipe's rate.  What did not
 // help: scaling inside the exponent (32 instructions less of 220 for 64 scores); sixteen softmax warps, two a
 // row (661 us for the call's 638: 18 warps leave 96 registers a thread); scores of 64 tokens at a time into
@@ -666,9 +666,13 @@ Plan plan_of(const LatentParams &p) {
 }
 
 // Pairs of CTAs where keys and values are widest, sequences have rows for them and lists are long: their products
-// are faster, beginnings and ends of items slower.  Whole calls with pairs and without, us, sequences x rows /
-// context, heads: 2 x 2048 / 10240, 32: 669, 721; 4 x 1024 / 4096, 16: 208, 215; 1 x 8192 / 8192, 16: 336, 335; 16 x
-// 700 / 700, 16: 173, 147; 8 x 512 / 512, 16: 85, 75.  (Contexts shorter than their lists only the device knows.)
+// are faster, beginnings and ends of items slower.  The GPU's time of whole calls with pairs and without, us, sequences
+// x rows / context, heads (R = 512): 1 x 1024 / 2048, 16: 60, 57; 4 x 1024 / 2048, 16: 131, 127; 1 x 4096 / 4096, 16: 137,
+// 133; 4 x 1024 / 4096, 16: 208, 214; 4 x 1024 / 4096, 32: 356, 374; 4 x 512 / 6144, 32: 352, 366; 1 x 8192 / 8192, 16: 334,
+// 331; 2 x 2048 / 8192, 32: 549, 582; 2 x 2048 / 10240, 32: 675, 725; 2 x 600 / 10240, 32: 415, 387; 1 x 2048 / 16384, 16:
+// 308, 324; R = 256, 1 x 512 / 32768, 16: 227, 239.  From 4096 on what is gained or lost goes by how items fall on the
+// CTAs; from 8192 on it is a gain in most.  Contexts shorter than their lists only the device knows: in lists of 8192,
+// 4 x 1024 / 2048, 16: 131, 127; 16 x 700 / 700, 16: 172, 148; 8 x 512 / 512, 16: 80, 72.
 constexpr int PAIR_ROWS = 512, PAIR_KV = 8192;
 bool pairs_for(const LatentParams &p) {
     return p.nope == 128 && p.value == 128 && q_spaced(p) && p.a.n_q >= (int64_t)PAIR_ROWS * p.a.n_seq &&
